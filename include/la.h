@@ -225,6 +225,93 @@ int la_unembed_argmax_noalloc(la_model *m, const float *hidden, int Bp, int32_t 
  * (Chunked prefill is the paper's named future work, Section 8.) */
 int la_prefill(la_model *m, la_kv *kv, const int32_t *tok, int n, int L0, void *stream);
 
+/* logits[b, :] = (rmsnorm(hidden[b]) * g_final) . unembed, what la_unembed_argmax takes the largest of: logits is
+ * device float, row b at logits + b * row_stride (row_stride >= vocab).  On the matrix-core path the normalised rows are
+ * multiplied as two half-precision numbers each, which keep 22 significant bits, so that the logits have float's accuracy
+ * (la_unembed_argmax rounds them to 11; logits closer than that may be ordered otherwise here).  Allocates nothing.
+ * LA_EINVAL: Bp not in 1..LA_MAX_ROWS, a NULL pointer, rows that overlap, a model without final norm or unembedding. */
+int la_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int64_t row_stride, void *stream);
+
+/* ---- sampling ------------------------------------------------------------------------------- */
+
+/* How la_sample chooses: device arrays with one entry per row, each but `u` may be NULL (its filter is off).
+ *   temperature  divides the logits (NULL: 1); 0, negative or NaN: the row's largest logit, ties to the lowest index
+ *   top_k        keeps the k largest (0, negative or >= vocab: all)
+ *   top_p        keeps, of those, the fewest largest whose weight is top_p of theirs at least, never fewer than one (>= 1 or NaN: all)
+ *   min_p        keeps those of at least min_p times the largest weight (0, negative or NaN: all; above 1: as 1)
+ *   u            the random numbers, in [0, 1); row b takes u[b], or u[u_index[b]] (u_index clamped to [0, n_u))
+ *   n_u          entries of u */
+typedef struct {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p, *u;
+  const int32_t *u_index;
+  int32_t n_u;
+} la_sampling;
+
+#define LA_MAX_SAMPLE_VOCAB (1 << 19)
+
+/* ids[b] = a token of row b, drawn by u from the distribution that the filters leave.  A token's weight is exp((logit - largest) /
+ * temperature); a logit of NaN counts as -inf, +inf as the largest finite number, and a weight below 2^-64 as none.  Order:
+ * larger logits first, equal ones by index.  Of the kept tokens in index order the first whose sum of weights passes u times
+ * their total is drawn (the last one if none does).  A row without any token gets -1.  prob (device float [B], or NULL) receives the
+ * drawn token's weight over that total (1 for temperature 0, 0 for id -1).  Weights and sums are formed in 64 bits: the result does
+ * not depend on the rows beside it or on the order of any sum.
+ * logits: device, la_dtype `dtype`, row b at logits + b * row_stride elements; any alignment of the type.  ids: device int32 [B].
+ * workspace: device memory of la_sample_workspace(B, V) bytes, 16-byte aligned, which the call may overwrite and which no other call
+ * may use meanwhile; nothing is kept in it.
+ * LA_EINVAL: V outside 1..LA_MAX_SAMPLE_VOCAB, rows that overlap, n_u too small, a NULL pointer; LA_ENOMEM: workspace too small.  B = 0 does nothing. */
+size_t la_sample_workspace(int B, int V);
+int la_sample(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_sampling *how, int32_t *ids, float *prob, void *workspace,
+              size_t workspace_bytes, void *stream);
+
+/* ---- a cache that several requests share ------------------------------------------------------ */
+
+/* Pages of page_size positions, handed to requests one at a time; k and v are device memory of the caller's, each
+ * [n_layers, n_pages, n_kv_heads, page_size, head_dim] of la_dtype `dtype`, 16-byte aligned.  head_dim: a multiple of 8, at most 256.
+ * Position t of a request lies in page table[t / page_size], at place t % page_size; its slot is page * page_size + place
+ * (n_pages * page_size < 2^31).  Keys are stored after RoPE. */
+typedef struct {
+  void *k, *v;
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim, dtype;
+} la_pages_desc;
+
+/* Block tables and slot maps from the requests' lengths.  Request r's cache goes from old_len[r] to new_len[r] positions: it takes the pages
+ * for new ones (a finished request goes to 0, a cropped one to fewer positions, and gives pages back).
+ * table: device int32, row r at table + r * table_stride, max_blocks entries; entries of pages it keeps are read, those it takes are written, others
+ * left as they are.  ring: device int32 [n_pages], the free pages from its head on, in a circle; heads: device int32 [4] = {head, free pages, rows,
+ * error}, read from heads_in (its first two words), written to heads_out, which must be other memory.  At first ring holds every page once and
+ * heads_in = {0, n_pages}.  Pages are taken from the head on and given back behind the last free one, both in the order of the requests and
+ * their blocks; what this call gives back, it does not hand out.
+ * The new tokens, old_len[r] <= t < new_len[r] of request 0, 1, ...: row i of them has slot[i], pos[i] = t and req[i] = r (device int32
+ * [max_rows]; -1 in rows behind the last token), and request r's begin at row first[r] (device int32 [R + 1]).
+ * Errors that only the device sees go to heads_out[3], and then nothing is taken, given back or mapped (all rows -1, first all 0): 1 too few free pages,
+ * 2 more than max_rows new tokens, 3 a length outside [0, max_blocks * page_size], 4 heads that are no place in the ring.
+ * LA_EINVAL: a NULL pointer, a size that is not positive, heads_in == heads_out, table rows that overlap, n_pages * page_size >= 2^31. */
+int la_page_map(const int32_t *old_len, const int32_t *new_len, int R, int page_size, int32_t *table, int64_t table_stride, int max_blocks,
+                int32_t *ring, int n_pages, const int32_t *heads_in, int32_t *heads_out, int32_t *slot, int32_t *pos, int32_t *req, int max_rows,
+                int32_t *first, void *stream);
+
+/* Writes row i of k and v (device, the pages' dtype, [n_kv_heads, head_dim] at k + i * k_stride elements) to slot[i] of one layer, i < n.  A slot outside
+ * [0, n_pages * page_size) is skipped.  Rows must be 16-byte aligned.  Slots must differ: of two rows with one slot it is not said which is left,
+ * nor that K and V are of the same. */
+int la_paged_write(const la_pages_desc *pages, int layer, const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot, int n,
+                   void *stream);
+
+/* Attention of single tokens over the pages of one layer: out[b, h] = sum_t softmax_t(scale * q[b, h] . K[t, h / g]) V[t, h / g] over positions
+ * 0 <= t <= pos[b] of request req[b] (NULL: request b), g = n_q_heads / n_kv_heads.  q, out: device, the pages' dtype, [n_q_heads, head_dim] at
+ * q + b * q_stride elements, rows 16-byte aligned.  table: device int32, request r's pages at table + r * table_stride, max_blocks entries; n_requests rows.
+ * A row of pos < 0, or whose request is outside [0, n_requests), sees nothing and gets zeros; pos is clamped to max_blocks * page_size - 1, and
+ * positions whose table entry is not a page (outside [0, n_pages)) are not seen.  Whatever lies in places that a row does not see is not
+ * looked at.  Scores, softmax and sums are float; 16-bit types multiply as stored, the probabilities rounded to that type.
+ * workspace: device memory of la_paged_attend_workspace bytes (0 where none is needed), 16-byte aligned, which the call may overwrite and which no
+ * other call may use meanwhile; nothing is kept in it.
+ * LA_EINVAL: a NULL pointer, bad dimensions or alignment; LA_ENOMEM: workspace too small; LA_ERANGE: layer.  B = 0 does nothing. */
+size_t la_paged_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int B);
+int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table,
+                    int64_t table_stride, int n_requests, int max_blocks, const int32_t *req, const int32_t *pos, int B, void *out, int64_t out_stride,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- n-gram pool and acceptance (Section 4.3) ----------------------------------------- */
 
 /* Pool keyed by token id: per key at most G distinct (N-1)-token continuations, refreshed

@@ -52,6 +52,15 @@ class la_step_state(C.Structure):
                 ("cand", C.c_int32 * LA_MAX_ROWS)]
 
 
+class la_sampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "u", "u_index")] + [("n_u", C.c_int32)]
+
+
+class la_pages_desc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
 class la_profile_entry(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int32), ("total_ms", C.c_float)]
 
@@ -62,7 +71,8 @@ STATE_OFF = {n: getattr(la_step_state, n).offset for n, _ in la_step_state._fiel
 EXPORTS = [
     "la_init_model", "la_model_set_layer", "la_free_model", "la_kv_alloc", "la_kv_set_len", "la_kv_get_len",
     "la_kv_fill", "la_kv_read", "la_free_kv", "la_embed", "la_forward_layers", "la_unembed_argmax",
-    "la_unembed_argmax_noalloc", "la_causal_layout", "la_set_barrier_timeout",
+    "la_unembed_argmax_noalloc", "la_unembed_logits", "la_sample", "la_sample_workspace", "la_page_map", "la_paged_write", "la_paged_attend",
+    "la_paged_attend_workspace", "la_causal_layout", "la_set_barrier_timeout",
     "la_prefill", "la_jacobi_init", "la_jacobi_accept", "la_rtt_fixed_overhead", "la_rtt_project", "la_jacobi_project",
     "la_pool_alloc", "la_free_pool", "la_state_init", "la_ngram_accept", "la_lookahead_layout",
     "la_profile_enable", "la_profile_select", "la_profile_read", "la_profile_copy", "la_last_error",
@@ -75,7 +85,7 @@ def _load():
             f"{LIB_PATH} is missing: build it with `python -m paper_2602_16760_amd.build` "
             "(there is no fallback path)")
     lib = C.CDLL(LIB_PATH)
-    vp, i32, f32 = C.c_void_p, C.c_int, C.c_float
+    vp, i32, i64, f32 = C.c_void_p, C.c_int, C.c_int64, C.c_float
     sig = {
         "la_init_model": (i32, [C.POINTER(la_model_desc), C.POINTER(la_layer_weights), vp, vp, vp, vp, C.POINTER(vp)]),
         "la_model_set_layer": (i32, [vp, i32, C.POINTER(la_layer_weights), vp]),
@@ -90,6 +100,13 @@ def _load():
         "la_forward_layers": (i32, [vp, i32, i32, vp, i32, vp, vp, vp, vp]),
         "la_unembed_argmax": (i32, [vp, vp, i32, vp, vp, vp]),
         "la_unembed_argmax_noalloc": (i32, [vp, vp, i32, vp, vp, vp]),
+        "la_unembed_logits": (i32, [vp, vp, i32, vp, i64, vp]),
+        "la_sample_workspace": (C.c_size_t, [i32, i32]),
+        "la_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, C.c_size_t, vp]),
+        "la_page_map": (i32, [vp, vp, i32, i32, vp, i64, i32, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp]),
+        "la_paged_write": (i32, [vp, i32, vp, vp, i64, i64, vp, i32, vp]),
+        "la_paged_attend_workspace": (C.c_size_t, [vp, i32, i32, i32]),
+        "la_paged_attend": (i32, [vp, i32, vp, i64, i32, f32, vp, i64, i32, i32, vp, vp, i32, vp, i64, vp, C.c_size_t, vp]),
         "la_pool_alloc": (i32, [i32, i32, i32, C.POINTER(vp)]),
         "la_free_pool": (None, [vp]),
         "la_state_init": (i32, [vp, vp, C.POINTER(la_lookahead_desc), vp, i32, i32, i32, vp, vp]),
@@ -229,6 +246,132 @@ def la_unembed_argmax(model, hidden, ids, top2=None, stream=None):
 def la_unembed_argmax_noalloc(model, hidden, ids, top2=None, stream=None):
     assert ids.dtype == torch.int32
     _check(lib.la_unembed_argmax_noalloc(model, _ptr(hidden), hidden.shape[0], _ptr(ids), _ptr(top2), _stream(stream)))
+
+
+# ---- sampling and the shared cache: operators on plain tensors, of any model or none ---------------------
+_DTYPES = {torch.float32: LA_F32, torch.bfloat16: LA_BF16, torch.float16: LA_F16}
+
+
+def _need(cond, text):
+    if not cond:
+        raise LaError(-1, text)
+
+
+def _array(t, name, dtype, shape, device):
+    """Address of a contiguous array of that type and shape on that device."""
+    _need(t.dtype is dtype and t.is_contiguous() and t.device == device and t.shape == shape,
+          f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _here(t, name):
+    """The current device, on which every tensor of the call has to be: the launch goes to one of its streams."""
+    device = t.device
+    _need(t.is_cuda and device.index == _torch._cuda_getDevice(), f"{name} is on {device}, not on the current CUDA device")
+    return device
+
+
+def _workspace(size, device, stream):
+    """Memory for one call: of the stream that runs it, so that nobody else is given it before the call is through."""
+    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    if stream is not None and stream != torch.cuda.current_stream():
+        ws.record_stream(stream)
+    return ws
+
+
+def la_unembed_logits(model, hidden, logits, stream=None):
+    """logits: float32 [Bp, vocab], rows may be strided."""
+    _need(hidden.dtype is torch.float32 and hidden.dim() == 2, "hidden: need float32 [Bp, d_model]")
+    _need(logits.is_cuda and logits.dtype is torch.float32 and logits.dim() == 2 and logits.shape[0] == hidden.shape[0] and logits.stride(1) == 1,
+          "logits: need float32 [Bp, vocab] with contiguous rows")
+    _check(lib.la_unembed_logits(model, _ptr(hidden), hidden.shape[0], logits.data_ptr(), logits.stride(0) if logits.shape[0] > 1 else logits.shape[1], _stream(stream)))
+
+
+def la_sample(logits, u, ids, prob=None, temperature=None, top_k=None, top_p=None, min_p=None, u_index=None, stream=None):
+    """ids[b] = a token of row b of logits [B, V] (float32, bfloat16 or float16, rows may be strided), drawn by u[b] (with u_index: by
+    u[u_index[b]]).  temperature, top_p, min_p: float32 [B] or None; top_k, u_index: int32 [B] or None; prob: float32 [B] or None."""
+    _need(logits.dim() == 2 and logits.dtype in _DTYPES and logits.stride(1) == 1, "logits: need [B, V] of float32, bfloat16 or float16 with contiguous rows")
+    device = _here(logits, "logits")
+    B, V = logits.shape
+    n, f32, i32 = (B,), torch.float32, torch.int32
+    opt = lambda t, name, dtype: None if t is None else _array(t, name, dtype, n, device)
+    how = la_sampling(opt(temperature, "temperature", f32), opt(top_k, "top_k", i32), opt(top_p, "top_p", f32), opt(min_p, "min_p", f32),
+                      _array(u, "u", f32, u.shape if u_index is not None and u.dim() == 1 else n, device), opt(u_index, "u_index", i32), u.shape[0])
+    size = lib.la_sample_workspace(B, V)
+    ws = _workspace(size, device, stream) if size else None
+    _check(lib.la_sample(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, B, V, C.byref(how), _array(ids, "ids", i32, n, device),
+                         opt(prob, "prob", f32), ws.data_ptr() if size else None, size, _stream(stream)))
+
+
+class la_pages:
+    """Pages of K and V, both [n_layers, n_pages, n_kv_heads, page_size, head_dim], and the descriptor that calls on them take."""
+
+    def __init__(self, k, v):
+        _need(k.dim() == 5 and k.dtype in _DTYPES and k.is_cuda and k.is_contiguous(), "k: need a contiguous CUDA tensor [n_layers, n_pages, n_kv_heads, page_size, head_dim]")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.desc = la_pages_desc(k.data_ptr(), _array(v, "v", k.dtype, k.shape, k.device), self.n_layers, self.n_pages, self.page_size, self.n_kv_heads,
+                                  self.head_dim, _DTYPES[k.dtype])
+        self.ref = C.byref(self.desc)
+
+    @property
+    def is_cuda(self):
+        return True
+
+    def _rows(self, t, name, heads):
+        """Address and row stride of [n, heads, head_dim] rows of the pages' type."""
+        s = t.stride()
+        _need(t.dtype is self.dtype and t.device == self.device and t.dim() == 3 and t.shape[2] == self.head_dim and t.shape[1] == heads and
+              s[2] == 1 and s[1] == self.head_dim,
+              f"{name}: need {self.dtype} [n, {heads}, {self.head_dim}] with contiguous rows on {self.device}, got {t.dtype}, {tuple(t.shape)}, strides {s} on {t.device}")
+        return t.data_ptr(), s[0]
+
+
+def _table(table, device):
+    _need(table.dtype is torch.int32 and table.device == device and table.dim() == 2 and table.stride(1) == 1,
+          f"table: need int32 [n_requests, max_blocks] with contiguous rows on {device}")
+    R, blocks = table.shape
+    return table.data_ptr(), table.stride(0) if R > 1 else blocks, R, blocks
+
+
+def la_page_map(old_len, new_len, page_size, table, ring, heads_in, heads_out, slot, pos, req, first, stream=None):
+    """Pages and slots of the requests' new tokens: see la.h.  All int32: old_len, new_len [R], table [R, max_blocks], ring [n_pages],
+    heads_in, heads_out [4] = {head, free pages, rows, error}, slot, pos, req [max_rows], first [R + 1]."""
+    device, i32 = _here(old_len, "old_len"), torch.int32
+    tp, ld, R, blocks = _table(table, device)
+    n, rows, four = (R,), slot.shape, (4,)
+    _check(lib.la_page_map(_array(old_len, "old_len", i32, n, device), _array(new_len, "new_len", i32, n, device), R, page_size, tp, ld, blocks,
+                           _array(ring, "ring", i32, (ring.numel(),), device), ring.numel(), _array(heads_in, "heads_in", i32, four, device),
+                           _array(heads_out, "heads_out", i32, four, device), _array(slot, "slot", i32, (slot.numel(),), device), _array(pos, "pos", i32, rows, device),
+                           _array(req, "req", i32, rows, device), slot.numel(), _array(first, "first", i32, (R + 1,), device), _stream(stream)))
+
+
+def la_paged_write(pages, layer, k, v, slot, stream=None):
+    """Rows of k, v [n, n_kv_heads, head_dim] (the rows themselves may be strided) into the slots slot [n] of one layer."""
+    device = _here(pages, "pages")
+    kp, ldk = pages._rows(k, "k", pages.n_kv_heads)
+    vp, ldv = pages._rows(v, "v", pages.n_kv_heads)
+    n = k.shape[0]
+    _need(v.shape[0] == n, f"{n} rows of k and {v.shape[0]} of v")
+    _check(lib.la_paged_write(pages.ref, layer, kp, vp, ldk, ldv, _array(slot, "slot", torch.int32, (n,), device), n, _stream(stream)))
+
+
+def la_paged_attend(pages, layer, q, table, req, pos, out, scale=None, stream=None):
+    """out[b] = attention of q[b] over positions 0 .. pos[b] of request req[b] (None: request b); q, out [B, n_q_heads, head_dim], rows may be
+    strided; scale None: head_dim ** -0.5."""
+    device, i32 = _here(pages, "pages"), torch.int32
+    _need(q.dim() == 3, "q: need [B, n_q_heads, head_dim]")
+    B, Hq = q.shape[:2]
+    qp, ldq = pages._rows(q, "q", Hq)
+    op, ldo = pages._rows(out, "out", Hq)
+    _need(out.shape[0] == B, f"{B} rows of q and {out.shape[0]} of out")
+    _need(B < 2 or ldo >= Hq * pages.head_dim, "out: rows overlap")
+    tp, ld, R, blocks = _table(table, device)
+    size = lib.la_paged_attend_workspace(pages.ref, Hq, blocks, B)
+    ws = _workspace(size, device, stream) if size else None
+    _check(lib.la_paged_attend(pages.ref, layer, qp, ldq, Hq, pages.head_dim ** -0.5 if scale is None else scale, tp, ld, R, blocks,
+                               None if req is None else _array(req, "req", i32, (B,), device), _array(pos, "pos", i32, (B,), device), B, op, ldo,
+                               ws.data_ptr() if size else None, size, _stream(stream)))
 
 
 def la_pool_alloc(vocab, N, G):

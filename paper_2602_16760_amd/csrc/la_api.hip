@@ -561,6 +561,16 @@ extern "C" int la_unembed_argmax(la_model *m, const float *hidden, int Bp, int32
   return generic_unembed_argmax(m, hidden, Bp, ids, top2, s);
 }
 
+extern "C" int la_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int64_t row_stride, void *stream) {
+  LA_REQUIRE(m && hidden && logits, LA_EINVAL, "NULL argument");
+  LA_REQUIRE(Bp >= 1 && Bp <= LA_MAX_ROWS, LA_EINVAL, "Bp=%d outside [1, %d]", Bp, LA_MAX_ROWS);
+  LA_REQUIRE(m->g_final && (m->unembed || m->use_mfma), LA_EINVAL, "model was created without final norm / unembedding");
+  LA_REQUIRE(row_stride >= m->d.vocab && row_stride <= 0x7fffffff, LA_EINVAL, "row_stride %lld for %d logits", (long long)row_stride, m->d.vocab);
+  LA_PENDING(m);
+  if (m->use_mfma) return mfma_unembed_logits(m, hidden, Bp, logits, row_stride, (hipStream_t)stream);
+  return generic_unembed_logits(m, hidden, Bp, logits, (int)row_stride, (hipStream_t)stream);
+}
+
 extern "C" int la_unembed_argmax_noalloc(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2, void *stream) {
   LA_REQUIRE(m && hidden && ids, LA_EINVAL, "NULL argument");
   LA_REQUIRE(Bp >= 1 && Bp <= LA_MAX_ROWS, LA_EINVAL, "Bp=%d outside [1, %d]", Bp, LA_MAX_ROWS);

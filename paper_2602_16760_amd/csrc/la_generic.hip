@@ -547,21 +547,24 @@ int generic_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int
   return plain_forward_t<uint16_t>(m, 0, d.n_layers, x, M, nullptr, nullptr, kv, b, s);
 }
 
-int generic_unembed_argmax(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2, hipStream_t s) {
+int generic_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int ldl, hipStream_t s) {
   const la_model_desc &d = m->d;
-  int rc;
   auto head = [&](auto t) {
     using T = decltype(t);
     if (plain_head(d)) {
       PlProduct p{};
-      p.A = hidden; p.lda = p.K = d.d_model; p.M = Bp; p.gain = m->g_final; p.eps = d.rms_eps; p.W = m->unembed; p.ldw = p.N = p.ldo = d.vocab; p.out = m->logits;
+      p.A = hidden; p.lda = p.K = d.d_model; p.M = Bp; p.gain = m->g_final; p.eps = d.rms_eps; p.W = m->unembed; p.ldw = p.N = d.vocab; p.ldo = ldl; p.out = logits;
       return plain_product<T, PL_STORE>("gemm_unembed", p, ceil_div(d.vocab, 16), s);
     }
-    return gemm<T>("gemm_unembed", hidden, d.d_model, m->g_final, d.rms_eps, m->unembed, d.vocab, m->logits, d.vocab, Bp, d.d_model, d.vocab, nullptr, false, s);
+    return gemm<T>("gemm_unembed", hidden, d.d_model, m->g_final, d.rms_eps, m->unembed, d.vocab, logits, ldl, Bp, d.d_model, d.vocab, nullptr, false, s);
   };
-  rc = d.dtype == LA_F32 ? head(float{}) : d.dtype == LA_F16 ? head(_Float16{}) : head(uint16_t{});
+  return d.dtype == LA_F32 ? head(float{}) : d.dtype == LA_F16 ? head(_Float16{}) : head(uint16_t{});
+}
+
+int generic_unembed_argmax(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2, hipStream_t s) {
+  const int rc = generic_unembed_logits(m, hidden, Bp, m->logits, m->d.vocab, s);
   if (rc) return rc;
-  return launch_argmax_rows(m->logits, Bp, d.vocab, ids, top2, s);
+  return launch_argmax_rows(m->logits, Bp, m->d.vocab, ids, top2, s);
 }
 
 }  // namespace la

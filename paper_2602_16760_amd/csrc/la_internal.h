@@ -119,6 +119,7 @@ int generic_forward(la_model *m, int lb, int le, float *hidden, int Bp, const in
                     const uint64_t *vis, la_kv *kv, hipStream_t s);
 int generic_unembed_argmax(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2,
                            hipStream_t s);
+int generic_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int ldl, hipStream_t s);
 int generic_prefill_rows(la_model *m, const la_kv *kv, int n, int *rows);  // of a chunk of an n-token prompt, scratch allocated; 0: by la_forward_layers
 int generic_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0, hipStream_t s);
 // (L_dev: that length is set to L, by the same launch)
@@ -136,6 +137,7 @@ int mfma_forward(la_model *m, int lb, int le, float *hidden, int Bp, const int32
                  const uint64_t *vis, la_kv *kv, hipStream_t s);
 int mfma_unembed_argmax(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2,
                         hipStream_t s);
+int mfma_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int64_t ldl, hipStream_t s);
 int mfma_reset_sync(la_model *m, hipStream_t s);
 int mfma_prefill_rows(la_model *m, int n, int *rows);  // of a large-M chunk of an n-token prompt, buffers allocated; 0: block kernel
 int mfma_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0, hipStream_t s);

@@ -6,6 +6,7 @@
 #include <mutex>
 #include <new>
 
+#include "la_prefill_plan.h"
 #include "la_rstack.h"
 
 namespace la {
@@ -177,6 +178,8 @@ struct MfmaModel {
   unsigned long long *trace = nullptr;  // LA_TRACE=1: per-phase timestamps, printed after each launch
   int trace_phases = 0;
   PfBuffers pf, pf_few;
+  uint16_t *lg_a = nullptr;  // stored logits: operand of the normalised rows, upper and lower halves (la_prefill.h), and their sums of squares
+  float *lg_ss = nullptr;
 };
 
 static int env_int(const char *name, int dflt) {
@@ -217,7 +220,7 @@ void mfma_destroy(la_model *m) {
   void *ps[] = {f->wstream, f->ustream, f->xa, f->attn_a, f->act_a, f->qf, f->xa_u, f->rsq_u, f->rsq, f->un_part,
                 f->sync, f->dev_gains, f->zero_len, f->trace, f->att_part, f->att_cnt,
                 f->sched[0][0], f->sched[0][1], f->sched[1][0], f->sched[1][1], f->sched[2][0], f->sched[2][1],
-                f->pf.base, f->pf_few.base};
+                f->pf.base, f->pf_few.base, f->lg_a, f->lg_ss};
   for (void *p : ps)
     if (p) (void)hipFree(p);
   delete f;
@@ -236,6 +239,7 @@ int mfma_reset_sync(la_model *m, hipStream_t s) {
 
 static int na_setup(int device);  // address of the static scratch array on this device (defined with its entry point below)
 static GemmDev dev_plan(const GemmPlan &p);
+int mfma_prepare_logits();  // (la_prefill.h)
 
 int mfma_create(la_model *m) {
   const la_model_desc &d = m->d;
@@ -420,7 +424,10 @@ int mfma_set_head(la_model *m, const void *unembed, hipStream_t s) {
   f->un_parts_per_cu = f->use_r ? passes : f->un_parts_bound;
   if (!f->un_part) f->un_part = (Top *)dalloc((size_t)f->n_wgs * f->un_parts_per_cu * 64 * sizeof(Top));
   LA_REQUIRE(f->un_part != nullptr, LA_ENOMEM, "device allocation failed");
-  return LA_OK;
+  if (!f->lg_a) f->lg_a = (uint16_t *)dalloc((size_t)2 * LA_MAX_ROWS * m->d.d_model * 2);
+  if (!f->lg_ss) f->lg_ss = (float *)dalloc((size_t)LA_MAX_ROWS * PF_CHUNKS * 4);
+  LA_REQUIRE(f->lg_a && f->lg_ss, LA_ENOMEM, "device allocation failed");
+  return mfma_prepare_logits();
 }
 
 static GemmDev dev_plan(const GemmPlan &p) { return GemmDev{p.KT, p.ntiles, p.ntp}; }

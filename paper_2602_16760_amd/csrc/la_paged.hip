@@ -1,0 +1,341 @@
+// A cache that several requests share: pages of page_size positions each, handed out per request.  Block tables and slot maps from the requests'
+// lengths (la_page_map), the rows' way into the pages (la_paged_write) and the attention that reads them (la_paged_attend).
+#include <algorithm>
+
+#include "la_device.h"
+#include "la_internal.h"
+
+namespace la {
+
+// ---- block tables and slot maps ---------------------------------------------------------------------------
+// Requests in order; request r grows from old[r] to new[r] positions (or shrinks).  With up(x) = ceil(x / page):
+//   pages taken   take_r = max(0, up(new) - up(old)), from the ring's head on;  pages given back  give_r = max(0, up(old) - up(new)), behind its last free one
+//   new tokens    add_r = max(0, new - old), rows first_r .. of the packed order, first = exclusive sum of add
+// Everything else follows from the three exclusive sums over the requests in front.  Every workgroup forms them for its own few requests by reading all
+// lengths (8 bytes a request, from L2): one launch and no words that workgroups pass to each other.  A row's page comes from the ring where the request took
+// it in this call, not from the table, which another workgroup may be writing.
+constexpr int MAP_THREADS = 256;
+struct PageMap {
+  const int32_t *old_len, *new_len;
+  int R, per_group, page;
+  int32_t *table;
+  int64_t ldt;
+  int max_blocks;
+  int32_t *ring;
+  int n_pages;
+  const int32_t *heads_in;
+  int32_t *heads_out, *slot, *pos, *req;
+  int max_rows;
+  int32_t *first;
+};
+
+__device__ __forceinline__ long long wave_sum(long long v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+__global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(PageMap a) {
+  __shared__ long long red[MAP_THREADS / 64][6], ends[3][MAP_THREADS];  // sums over waves; inclusive sums over the group's requests: rows, taken, given
+  __shared__ int old_s[MAP_THREADS], had_s[MAP_THREADS];
+  __shared__ int bad_s;
+  const int t = threadIdx.x, wave = t >> 6;
+  const int r0 = (int)blockIdx.x * a.per_group, nr = a.R - r0 < a.per_group ? a.R - r0 : a.per_group;
+  auto up = [&](int x) { return (int)(((long long)x + a.page - 1) / a.page); };
+  if (t == 0) bad_s = 0;
+  __syncthreads();
+  long long in_front[3] = {0, 0, 0}, total[3] = {0, 0, 0};
+  const long long cap = (long long)a.max_blocks * a.page;
+  bool bad = false;
+  for (int r = t; r < a.R; r += MAP_THREADS) {
+    const int x = a.old_len[r], y = a.new_len[r];
+    if (x < 0 || y < 0 || x > cap || y > cap) {
+      bad = true;
+      continue;
+    }
+    const int d = up(y) - up(x);
+    const long long v[3] = {y > x ? y - x : 0, d > 0 ? d : 0, d < 0 ? -d : 0};
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      total[i] += v[i];
+      if (r < r0) in_front[i] += v[i];
+    }
+  }
+  if (bad) bad_s = 1;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const long long f = wave_sum(in_front[i]), s = wave_sum(total[i]);
+    if ((t & 63) == 0) {
+      red[wave][i] = f;
+      red[wave][3 + i] = s;
+    }
+  }
+  int x = 0, y = 0;
+  if (t < nr) {
+    x = a.old_len[r0 + t];
+    y = a.new_len[r0 + t];
+  }
+  const int d = up(y) - up(x);
+  old_s[t] = x;
+  had_s[t] = up(x);
+  ends[0][t] = y > x ? y - x : 0;
+  ends[1][t] = d > 0 ? d : 0;
+  ends[2][t] = d < 0 ? -d : 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    in_front[i] = total[i] = 0;
+    for (int w = 0; w < MAP_THREADS / 64; ++w) {
+      in_front[i] += red[w][i];
+      total[i] += red[w][3 + i];
+    }
+  }
+  for (int o = 1; o < nr; o <<= 1) {
+    long long v[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] = t >= o ? ends[i][t - o] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) ends[i][t] += v[i];
+    __syncthreads();
+  }
+  const int head = a.heads_in[0], n_free = a.heads_in[1];
+  int error = 0;
+  if (head < 0 || head >= a.n_pages || n_free < 0 || n_free > a.n_pages) error = 4;
+  else if (bad_s) error = 3;
+  else if (total[0] > a.max_rows) error = 2;
+  else if (total[1] > n_free) error = 1;
+  const int part = blockIdx.y, parts = gridDim.y, stride = parts * MAP_THREADS, k0 = part * MAP_THREADS + t;
+  if (part == 0) {
+    if (t < nr) a.first[r0 + t] = error ? 0 : (int)(in_front[0] + (t > 0 ? ends[0][t - 1] : 0));
+    if (blockIdx.x == 0 && t == 0) {
+      a.first[a.R] = error ? 0 : (int)total[0];
+      a.heads_out[0] = error ? head : (int)((head + total[1]) % a.n_pages);
+      a.heads_out[1] = error ? n_free : (int)(n_free - total[1] + total[2]);
+      a.heads_out[2] = error ? 0 : (int)total[0];
+      a.heads_out[3] = error;
+    }
+  }
+  // rows that no token has
+  const long long grid_t = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * MAP_THREADS + t, grid_n = (long long)gridDim.x * parts * MAP_THREADS;
+  for (long long i = (error ? 0 : total[0]) + grid_t; i < a.max_rows; i += grid_n) a.slot[i] = a.pos[i] = a.req[i] = -1;
+  if (error) return;
+  auto find = [&](const long long *e, long long k) {  // first request of the group whose sum is above k
+    int lo = 0, hi = nr - 1;
+    while (lo < hi) {
+      const int m = (lo + hi) / 2;
+      if (e[m] > k) hi = m; else lo = m + 1;
+    }
+    return lo;
+  };
+  auto taken = [&](int q, int block) {  // the page that request r0 + q takes for a block behind those it had
+    const long long k = in_front[1] + (q > 0 ? ends[1][q - 1] : 0) + (block - had_s[q]);
+    return a.ring[(head + k) % a.n_pages];
+  };
+  const long long n_take = ends[1][nr - 1], n_give = ends[2][nr - 1], n_rows = ends[0][nr - 1];
+  for (long long k = k0; k < n_take; k += stride) {
+    const int q = find(ends[1], k), block = had_s[q] + (int)(k - (q > 0 ? ends[1][q - 1] : 0));
+    a.table[(r0 + q) * a.ldt + block] = taken(q, block);
+  }
+  for (long long k = k0; k < n_give; k += stride) {
+    const int q = find(ends[2], k), block = had_s[q] - (int)(ends[2][q] - k);  // (blocks up(new) .. up(old) - 1, in order)
+    a.ring[(head + n_free + in_front[2] + k) % a.n_pages] = a.table[(r0 + q) * a.ldt + block];
+  }
+  for (long long k = k0; k < n_rows; k += stride) {
+    const int q = find(ends[0], k), p = old_s[q] + (int)(k - (q > 0 ? ends[0][q - 1] : 0)), block = p / a.page;
+    const int page = block < had_s[q] ? a.table[(r0 + q) * a.ldt + block] : taken(q, block);
+    const long long i = in_front[0] + k;
+    a.slot[i] = (unsigned)page < (unsigned)a.n_pages ? page * a.page + (p - block * a.page) : -1;
+    a.pos[i] = p;
+    a.req[i] = r0 + q;
+  }
+}
+
+// ---- rows into pages ------------------------------------------------------------------------------------------
+// Pages are [page][kv head][place][channel]: what one head has in a page is contiguous.  Thread per 16 bytes of K and of V.
+__global__ __launch_bounds__(256) void paged_write_kernel(uint4 *kp, uint4 *vp, const uint4 *k, const uint4 *v, int64_t ldk, int64_t ldv, const int32_t *slot, int n, int Hkv,
+                                                          int per_head, int page, int n_pages) {
+  const int per_row = Hkv * per_head;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long long)n * per_row) return;
+  const int row = (int)(i / per_row), c = (int)(i - (long long)row * per_row), h = c / per_head;
+  const int s = slot[row], pg = s / page;
+  if (s < 0 || pg >= n_pages) return;
+  const size_t to = (((size_t)pg * Hkv + h) * page + (s - pg * page)) * per_head + (c - h * per_head);
+  kp[to] = k[row * ldk + c];
+  vp[to] = v[row * ldv + c];
+}
+
+// ---- attention over pages ---------------------------------------------------------------------------------------
+struct PagedAttend {
+  const void *K, *V;  // of the layer
+  int n_pages, page, Hkv, dh;
+  const void *q;
+  int64_t ldq;
+  int Hq;
+  float scale;
+  const int32_t *table;
+  int64_t ldt;
+  int n_req, max_blocks;
+  const int32_t *req, *pos;
+  void *out;
+  int64_t ldo;
+};
+
+// Row b's request and the keys it sees: none where the row is padding or names no request.
+__device__ __forceinline__ int paged_keys(const PagedAttend &a, int b, int &r) {
+  r = a.req ? a.req[b] : b;
+  if ((unsigned)r >= (unsigned)a.n_req) return 0;
+  const long long n = (long long)a.pos[b] + 1, cap = (long long)a.max_blocks * a.page;
+  return (int)(n < 0 ? 0 : n < cap ? n : cap);
+}
+
+// A workgroup per row and query head: online softmax over chunks of 256 keys, a key per thread for the scores; threads form 256 / dh groups of a channel each
+// for the output.
+template <typename T>
+__global__ __launch_bounds__(256) void paged_attend_kernel(PagedAttend a) {
+  __shared__ float qs[256], ps[256], red[4];
+  __shared__ long long at[256];
+  const int b = blockIdx.x, hq = blockIdx.y, t = threadIdx.x, h = hq / (a.Hq / a.Hkv), dh = a.dh;
+  int r;
+  const int n = paged_keys(a, b, r);
+  const T *q = (const T *)a.q + b * a.ldq + hq * dh, *K = (const T *)a.K, *V = (const T *)a.V;
+  if (t < dh) qs[t] = load_as_float<T>(q + t);
+  const int groups = 256 / dh, gi = t / dh, ch = t - gi * dh;
+  float m_run = -INFINITY, l_run = 0.f, acc = 0.f;
+  auto all = [&](float v, bool max) {
+    for (int o = 32; o > 0; o >>= 1) v = max ? fmaxf(v, __shfl_xor(v, o, 64)) : v + __shfl_xor(v, o, 64);
+    __syncthreads();
+    if ((t & 63) == 0) red[t >> 6] = v;
+    __syncthreads();
+    return max ? fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) : (red[0] + red[1]) + (red[2] + red[3]);
+  };
+  for (int k0 = 0; k0 < n; k0 += 256) {
+    const int j = k0 + t, block = j / a.page;
+    const int pg = j < n ? a.table[r * a.ldt + block] : -1;
+    const long long row = (unsigned)pg < (unsigned)a.n_pages ? (((long long)pg * a.Hkv + h) * a.page + (j - block * a.page)) * dh : -1;
+    __syncthreads();
+    at[t] = row;
+    float s = -INFINITY;
+    if (row >= 0) {
+      s = 0.f;
+      for (int i = 0; i < dh; ++i) s = fmaf(qs[i], load_as_float<T>(K + row + i), s);
+      s *= a.scale;
+    }
+    const float m_new = fmaxf(m_run, all(s, true));
+    const float p = s > -INFINITY ? expf(s - m_new) : 0.f, corr = m_run > -INFINITY ? expf(m_run - m_new) : 0.f;
+    ps[t] = p;
+    l_run = l_run * corr + all(p, false);  // (its barriers publish ps)
+    m_run = m_new;
+    if (gi < groups) {
+      acc *= corr;
+      const int end = n - k0 < 256 ? n - k0 : 256;
+      for (int u = gi; u < end; u += groups)
+        if (at[u] >= 0) acc = fmaf(ps[u], load_as_float<T>(V + at[u] + ch), acc);
+    }
+  }
+  __syncthreads();
+  ps[t] = gi < groups ? acc : 0.f;
+  __syncthreads();
+  if (t < dh) {
+    float o = 0.f;
+    for (int u = 0; u < groups; ++u) o += ps[u * dh + t];
+    store_from_float<T>((T *)a.out + b * a.ldo + hq * dh + t, l_run > 0.f ? o / l_run : 0.f);
+  }
+}
+
+static bool aligned16(std::initializer_list<const void *> ps) {
+  uintptr_t all = 0;
+  for (const void *p : ps) all |= (uintptr_t)p;
+  return all % 16 == 0;
+}
+
+int check_pages(const la_pages_desc *p, int layer) {
+  LA_REQUIRE(p && p->k && p->v, LA_EINVAL, "NULL pages");
+  LA_REQUIRE(p->n_layers > 0 && p->n_pages > 0 && p->page_size > 0 && p->n_kv_heads > 0, LA_EINVAL, "page dimensions must be positive");
+  LA_REQUIRE(p->head_dim > 0 && p->head_dim % 8 == 0 && p->head_dim <= 256, LA_EINVAL, "head_dim %d must be a multiple of 8, at most 256", p->head_dim);
+  LA_REQUIRE(p->dtype == LA_F32 || p->dtype == LA_BF16 || p->dtype == LA_F16, LA_EINVAL, "unknown dtype %d", p->dtype);
+  LA_REQUIRE((long long)p->n_pages * p->page_size < (1ll << 31), LA_EINVAL, "%d pages of %d positions: slots are 32-bit numbers", p->n_pages, p->page_size);
+  LA_REQUIRE(aligned16({p->k, p->v}), LA_EINVAL, "pages must be 16-byte aligned");
+  LA_REQUIRE(layer >= 0 && layer < p->n_layers, LA_ERANGE, "layer %d outside the pages' %d layers", layer, p->n_layers);
+  return LA_OK;
+}
+static size_t esize(const la_pages_desc *p) { return p->dtype == LA_F32 ? 4 : 2; }
+static size_t layer_bytes(const la_pages_desc *p) { return (size_t)p->n_pages * p->n_kv_heads * p->page_size * p->head_dim * esize(p); }
+
+}  // namespace la
+
+using namespace la;
+
+extern "C" int la_page_map(const int32_t *old_len, const int32_t *new_len, int R, int page_size, int32_t *table, int64_t table_stride, int max_blocks,
+                           int32_t *ring, int n_pages, const int32_t *heads_in, int32_t *heads_out, int32_t *slot, int32_t *pos, int32_t *req, int max_rows,
+                           int32_t *first, void *stream) {
+  LA_REQUIRE(old_len && new_len && table && ring && heads_in && heads_out && slot && pos && req && first, LA_EINVAL, "NULL argument");
+  LA_REQUIRE(heads_in != heads_out, LA_EINVAL, "heads_out must not be heads_in: every workgroup reads the one while one writes the other");
+  LA_REQUIRE(R >= 1 && page_size >= 1 && max_blocks >= 1 && n_pages >= 1 && max_rows >= 1, LA_EINVAL, "dimensions must be positive");
+  LA_REQUIRE(table_stride >= max_blocks || R == 1, LA_EINVAL, "table rows overlap");
+  LA_REQUIRE((long long)n_pages * page_size < (1ll << 31), LA_EINVAL, "%d pages of %d positions: slots are 32-bit numbers", n_pages, page_size);
+  hipStream_t s = (hipStream_t)stream;
+  // 16 requests a workgroup (more where there are very many, each of which reads all lengths), in as many parts as give a thread eight rows
+  int per_group = 16;
+  while (per_group < MAP_THREADS && R / per_group > 64) per_group *= 2;
+  const int groups = ceil_div(R, per_group), parts = std::min(64, std::max(1, max_rows / (groups * MAP_THREADS * 8)));
+  const PageMap a{old_len, new_len, R, per_group, page_size, table, table_stride, max_blocks, ring, n_pages, heads_in, heads_out, slot, pos, req, max_rows, first};
+  ProfScope ps("page_map", s);
+  page_map_kernel<<<dim3(groups, parts), MAP_THREADS, 0, s>>>(a);
+  LA_HIP(hipGetLastError());
+  return LA_OK;
+}
+
+extern "C" int la_paged_write(const la_pages_desc *pages, int layer, const void *k, const void *v, int64_t k_stride, int64_t v_stride, const int32_t *slot, int n,
+                              void *stream) {
+  if (const int rc = check_pages(pages, layer)) return rc;
+  const la_pages_desc &p = *pages;
+  const size_t e = esize(&p);
+  LA_REQUIRE(n >= 0, LA_EINVAL, "n=%d is negative", n);
+  if (n == 0) return LA_OK;
+  LA_REQUIRE(k && v && slot, LA_EINVAL, "NULL argument");
+  LA_REQUIRE(aligned16({k, v}) && k_stride * e % 16 == 0 && v_stride * e % 16 == 0, LA_EINVAL, "K and V rows must be 16-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  const int per_head = (int)(p.head_dim * e / 16);
+  const long long wgs = ((long long)n * p.n_kv_heads * per_head + 255) / 256;
+  LA_REQUIRE(wgs < (1ll << 31), LA_EINVAL, "%d rows are more than one launch takes", n);
+  ProfScope ps("paged_write", s);
+  paged_write_kernel<<<(unsigned)wgs, 256, 0, s>>>((uint4 *)((char *)p.k + layer * layer_bytes(&p)), (uint4 *)((char *)p.v + layer * layer_bytes(&p)), (const uint4 *)k,
+                                                   (const uint4 *)v, k_stride * (int64_t)e / 16, v_stride * (int64_t)e / 16, slot, n, p.n_kv_heads, per_head, p.page_size,
+                                                   p.n_pages);
+  LA_HIP(hipGetLastError());
+  return LA_OK;
+}
+
+extern "C" size_t la_paged_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int B) {
+  (void)pages; (void)n_q_heads; (void)max_blocks; (void)B;
+  return 0;
+}
+
+extern "C" int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table,
+                               int64_t table_stride, int n_requests, int max_blocks, const int32_t *req, const int32_t *pos, int B, void *out, int64_t out_stride,
+                               void *workspace, size_t workspace_bytes, void *stream) {
+  if (const int rc = check_pages(pages, layer)) return rc;
+  const la_pages_desc &p = *pages;
+  const size_t e = esize(&p);
+  LA_REQUIRE(B >= 0, LA_EINVAL, "B=%d is negative", B);
+  if (B == 0) return LA_OK;
+  LA_REQUIRE(q && table && pos && out, LA_EINVAL, "NULL argument");
+  LA_REQUIRE(n_q_heads > 0 && n_q_heads % p.n_kv_heads == 0, LA_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", n_q_heads, p.n_kv_heads);
+  LA_REQUIRE(n_requests >= 1 && max_blocks >= 1 && (table_stride >= max_blocks || n_requests == 1), LA_EINVAL, "bad table dimensions");
+  LA_REQUIRE(req || B <= n_requests, LA_EINVAL, "%d rows for %d requests and no row map", B, n_requests);
+  LA_REQUIRE(aligned16({q, out}) && q_stride * e % 16 == 0 && out_stride * e % 16 == 0, LA_EINVAL, "q and out rows must be 16-byte aligned");
+  LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
+  (void)workspace; (void)workspace_bytes;
+  hipStream_t s = (hipStream_t)stream;
+  const size_t at = layer * layer_bytes(&p);
+  const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride,
+                      n_requests, max_blocks, req, pos, out, out_stride};
+  ProfScope ps("paged_attend", s);
+  const dim3 grid(B, n_q_heads);
+  if (p.dtype == LA_F32) paged_attend_kernel<float><<<grid, 256, 0, s>>>(a);
+  else if (p.dtype == LA_F16) paged_attend_kernel<_Float16><<<grid, 256, 0, s>>>(a);
+  else paged_attend_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
+  LA_HIP(hipGetLastError());
+  return LA_OK;
+}

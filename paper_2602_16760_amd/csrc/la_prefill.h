@@ -39,7 +39,14 @@ struct PfGemm {
   uint16_t *Q;        // QKV: q fragments [Hq][RT][dh/32][64][8]
   int L0, Hq, Hkv, dh, f16;
   uint16_t *act;      // GATEUP: operand fragments of the down projection [F/32][RT][64][8]
+  float *logits;      // LOGITS
+  int64_t ldl;
 };
+
+// LOGITS: a workgroup's column tiles are neighbours in one stream, LG_COLS of a CU's (their 1 KB fragments lie side by side in memory): column tile j of group cg.
+constexpr int LG_COLS = 8;
+constexpr float LG_LOW = 2048.f;  // what the lower halves of the operand are multiplied by
+__device__ __forceinline__ int lg_tile(const PfGemm &p, int cg, int j) { return (cg / p.G * LG_COLS + j) * p.G + cg % p.G; }
 
 // The epilogue of a wave's tile.  The products are formed with the weight fragment as the MFMA's first operand, so
 // a lane holds FOUR CONSECUTIVE COLUMNS of one row (NM row tiles x NTW column tiles): acc[m][j][i] is row 16 (r0 + m) + c16, column 4 q4 + i of column
@@ -48,6 +55,25 @@ struct PfGemm {
 template <int MODE, int NM, int NTW>
 __device__ __forceinline__ void pf_epilogue(const PfGemm &p, const f32x4 (&acc)[NM][NTW], int r0, int t0, int lane, int slice, LDS_AS const float *rf) {
   const int q4 = lane >> 4, c16 = lane & 15;
+  if constexpr (MODE == PF_LOGITS) {  // row tiles 0 .. NM / 2 - 1: upper halves of the operand, the others: lower halves of the same rows
+    static_assert(NTW == 1, "a wave per column tile");
+    if (t0 >= p.ntiles) return;
+    const bool quads = ((uintptr_t)p.logits | (size_t)p.ldl * 4) % 16 == 0;
+#pragma unroll
+    for (int m = 0; m < NM / 2; ++m) {
+      const int row = 16 * m + c16;
+      if (row >= p.M) continue;
+      const f32x4 v = (acc[m][0] + acc[m + NM / 2][0] * (1.f / LG_LOW)) * rf[row];
+      float *to = p.logits + row * p.ldl + 16 * t0 + 4 * q4;
+      if (quads) {
+        *reinterpret_cast<f32x4 *>(to) = v;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = v[i];
+      }
+    }
+    return;
+  }
   float rsm[NM];  // row factors of the norm
 #pragma unroll
   for (int m = 0; m < NM; ++m) rsm[m] = MODE == PF_PART ? 0.f : rf[16 * m + c16];
@@ -158,7 +184,8 @@ __device__ __forceinline__ void pf_tile_body(const PfGemm &p, LDS_AS uint8_t *pf
   static_assert((NS - 1) * LPW <= 63, "load counter");
   const int wave = uni((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
   const int wm = wave % WM, wn = wave / WM;
-  const int n_cg = (p.ntiles - p.t_first + CTB - 1) / CTB, RB = ((p.M + 15) / 16 + RTB - 1) / RTB;
+  const int n_cg = MODE == PF_LOGITS ? p.G * (((p.ntiles + p.G - 1) / p.G + CTB - 1) / CTB) : (p.ntiles - p.t_first + CTB - 1) / CTB;
+  const int RB = ((p.M + 15) / 16 + RTB - 1) / RTB;
   // An XCD takes a run of the tiles, row blocks first (they share the weights in its L2), and all XCDs as many, to one: with whole
   // column groups dealt to them, some had a round of workgroups more than the chip needs (7B shape, 700 rows: down
   // 166 -> 91 us, O 61 -> 36; 1300 rows: 298 -> 160, 101 -> 57; 1600 rows: gate/up 452 -> 390; 12B shape, 300 rows: down 121 -> 67).
@@ -191,7 +218,7 @@ __device__ __forceinline__ void pf_tile_body(const PfGemm &p, LDS_AS uint8_t *pf
       inc[i] = uni((unsigned)(p.NW * p.RT) * 1024u);
       n_act = i + 1;
     } else {
-      const int tj = p.t_first + cg * CTB + f - RTB;
+      const int tj = MODE == PF_LOGITS ? lg_tile(p, cg, f - RTB) : p.t_first + cg * CTB + f - RTB;
       const int t = tj < p.ntiles ? tj : p.ntiles - 1;  // (a group past the last tile repeats it; its result is dropped)
       const int c = uni(t % p.G), lt = uni(t / p.G);
       unsigned off = p.frag0;
@@ -300,7 +327,8 @@ __device__ __forceinline__ void pf_tile_body(const PfGemm &p, LDS_AS uint8_t *pf
   }
   wait_vmcnt<0>();  // (the requests past the last k-tile land before the LDS is given back)
   const int r0 = rb * RTB + NM * wm;
-  if (r0 < p.RT) pf_epilogue<MODE, NM, NTW>(p, acc, r0, p.t_first + cg * CTB + wn * NTW, lane, slice, rf + 16 * NM * wm);
+  const int t0 = MODE == PF_LOGITS ? lg_tile(p, cg, wn) : p.t_first + cg * CTB + wn * NTW;
+  if (r0 < p.RT) pf_epilogue<MODE, NM, NTW>(p, acc, r0, t0, lane, slice, rf + 16 * NM * wm);
 }
 
 template <int MODE, int WM, int WN, int NTW, int NS, int NM>
@@ -403,6 +431,44 @@ template <int MT, int NS>
 __global__ __launch_bounds__(256, 2) void pf_qkv_few_kernel(PfGemm p) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t pf_lds[];
   pf_qkv_few_body<MT, NS>(p, (LDS_AS uint8_t *)pf_lds);
+}
+
+// The unembedding's operand for stored logits: x * gain as the sum of two half-precision numbers, the nearest one and LG_LOW times what it leaves, in
+// row tiles 0 .. T - 1 and T .. 2 T - 1 of the fragments; and the sums of squares, as pf_norm_kernel forms them.  Rows behind M are zeros.
+__global__ __launch_bounds__(256) void logits_operand_kernel(const float *x, const float *gain, int M, int d, int T, float *ss, uint16_t *A) {
+  const int rt = blockIdx.x, chunk = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
+  const int KT = d >> 5, per = (KT + PF_CHUNKS - 1) / PF_CHUNKS, k1 = (chunk + 1) * per < KT ? (chunk + 1) * per : KT;
+  const int row = 16 * rt + c16;
+  __shared__ float red[4][16];
+  float sq = 0.f;
+  for (int kt = chunk * per + wave; kt < k1; kt += 4) {
+    const int col = 32 * kt + 8 * q4;
+    u32x4 hi = {0u, 0u, 0u, 0u}, lo = hi;
+    if (row < M) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = x[(size_t)row * d + col + i];
+        sq += v * v;
+        y[i] = v * gain[col + i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hi[i] = pack_f16(y[2 * i], y[2 * i + 1]);
+        const float a = (float)__builtin_bit_cast(_Float16, (uint16_t)(hi[i] & 0xffffu)), b = (float)__builtin_bit_cast(_Float16, (uint16_t)(hi[i] >> 16));
+        lo[i] = pack_f16((y[2 * i] - a) * LG_LOW, (y[2 * i + 1] - b) * LG_LOW);
+      }
+    }
+    uint16_t *to = A + (((size_t)kt * 2 * T + rt) * 64 + lane) * 8;
+    *(u32x4 *)to = hi;
+    *(u32x4 *)(to + (size_t)T * 64 * 8) = lo;
+  }
+  sq += __shfl_xor(sq, 16, 64);
+  sq += __shfl_xor(sq, 32, 64);
+  if (q4 == 0) red[wave][c16] = sq;
+  __syncthreads();
+  if (threadIdx.x < 16 && 16 * rt + (int)threadIdx.x < M)
+    ss[(size_t)(16 * rt + threadIdx.x) * PF_CHUNKS + chunk] = (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
 }
 
 // The residual stream takes in the products of the projection before (x += the slices' products, added in slice order),
@@ -642,7 +708,7 @@ static int pf_launch_tile(const PfGemm &p, hipStream_t s, bool prepare) {
     LA_HIP(hipFuncSetAttribute((const void *)pf_tile_kernel<MODE, WM, WN, NTW, NS, NM>, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
     return LA_OK;
   }
-  const int n_cg = ceil_div(p.ntiles - p.t_first, WN * NTW), RB = ceil_div(ceil_div(p.M, 16), NM * WM);
+  const int n_cg = MODE == PF_LOGITS ? p.G * ceil_div(ceil_div(p.ntiles, p.G), WN * NTW) : ceil_div(p.ntiles - p.t_first, WN * NTW), RB = ceil_div(ceil_div(p.M, 16), NM * WM);
   pf_tile_kernel<MODE, WM, WN, NTW, NS, NM><<<(RB * p.S * n_cg + 7) / 8 * 8, 64 * WM * WN, bytes, s>>>(p);
   LA_HIP(hipGetLastError());
   return LA_OK;
@@ -863,6 +929,54 @@ int mfma_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0
   }
   LA_HIP(hipGetLastError());
   return LA_OK;
+}
+
+// ---- stored logits ------------------------------------------------------------------------------------
+template <int T>
+static int pf_launch_logits(const PfGemm &p, hipStream_t s, bool prepare) {
+  return pf_launch_tile<PF_LOGITS, 1, LG_COLS, 1, pf_stages(2 * T + LG_COLS), 2 * T>(p, s, prepare);
+}
+int mfma_prepare_logits() {
+  int rc = pf_launch_logits<1>(PfGemm{}, nullptr, true);
+  if (!rc) rc = pf_launch_logits<2>(PfGemm{}, nullptr, true);
+  if (!rc) rc = pf_launch_logits<3>(PfGemm{}, nullptr, true);
+  return rc ? rc : pf_launch_logits<4>(PfGemm{}, nullptr, true);
+}
+
+int mfma_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int64_t ldl, hipStream_t s) {
+  MfmaModel *f = m->mf;
+  const la_model_desc &d = m->d;
+  LA_REQUIRE(f->ustream != nullptr, LA_EINVAL, "model was created without an unembedding matrix");
+  LA_REQUIRE(f->use_r, LA_EINVAL, "stored logits read the register-streaming kernel's weight layout");
+  const int T = ceil_div(Bp, 16);
+  {
+    ProfScope ps("logits_operand", s);
+    logits_operand_kernel<<<dim3(T, PF_CHUNKS), 256, 0, s>>>(hidden, m->g_final, Bp, d.d_model, T, f->lg_ss, f->lg_a);
+  }
+  LA_HIP(hipGetLastError());
+  PfGemm p{};
+  p.wstream = f->ustream;
+  p.cu_bytes = f->ucu_bytes;
+  p.G = f->n_wgs;
+  p.NW = R_NW;
+  p.ntiles = f->p_un.ntiles;
+  p.KT = f->p_un.KT;
+  p.A = f->lg_a;
+  p.S = 1;
+  p.RT = 2 * T;
+  p.M = Bp;
+  p.ss = f->lg_ss;
+  p.inv_d = 1.0f / (float)d.d_model;
+  p.eps = d.rms_eps;
+  p.logits = logits;
+  p.ldl = ldl;
+  ProfScope ps("unembed_logits", s);
+  switch (T) {
+  case 1: return pf_launch_logits<1>(p, s, false);
+  case 2: return pf_launch_logits<2>(p, s, false);
+  case 3: return pf_launch_logits<3>(p, s, false);
+  default: return pf_launch_logits<4>(p, s, false);
+  }
 }
 
 }  // namespace la

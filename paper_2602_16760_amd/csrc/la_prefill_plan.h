@@ -80,7 +80,7 @@ constexpr PfTile PF_TILES[] = {
 };
 constexpr int PF_N_TILES = 6, PF_SMALLEST = 5;
 
-enum PfMode { PF_QKV = 0, PF_PART = 1, PF_GATEUP = 2 };
+enum PfMode { PF_QKV = 0, PF_PART = 1, PF_GATEUP = 2, PF_LOGITS = 3 };  // (PF_LOGITS: la_unembed_logits, by tiles of its own)
 
 struct PfProduct {
   int RT, M, KT, n_tiles, d;  // row tiles of the buffers, rows, k-tiles, column tiles wanted, row length of the products
