@@ -250,6 +250,7 @@ typedef struct {
 } la_sampling;
 
 #define LA_MAX_SAMPLE_VOCAB (1 << 19)
+#define LA_MAX_ATTEND_ROWS (1 << 20)
 
 /* ids[b] = a token of row b, drawn by u from the distribution that the filters leave.  A token's weight is exp((logit - largest) /
  * temperature); a logit of NaN counts as -inf, +inf as the largest finite number, and a weight below 2^-64 as none.  Order:

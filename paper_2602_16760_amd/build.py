@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblookahead.so")
 
-SOURCES = ["la_api.hip", "la_generic.hip", "la_accept.hip", "la_mfma.hip", "la_paged.hip", "la_sample.hip",
+SOURCES = ["la_api.hip", "la_generic.hip", "la_accept.hip", "la_mfma.hip", "la_paged.hip", "la_attend.hip", "la_sample.hip",
            "la_stack_mt1.hip", "la_stack_mt2.hip", "la_stack_mt3.hip", "la_stack_mt4.hip",
            "la_rstack_mt1.hip", "la_rstack_mt2.hip", "la_rstack_mt3.hip", "la_rstack_mt4.hip"]
 FLAGS = [

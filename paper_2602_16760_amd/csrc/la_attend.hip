@@ -1,0 +1,548 @@
+// Attention of single tokens over a paged cache (la_paged_attend): the keys of a row are split into items, an item is a workgroup, and a second launch joins
+// the items of rows that have several.
+#include <algorithm>
+#include <type_traits>
+
+#include "la_paged.h"
+
+namespace la {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 at_b8;
+typedef _Float16 __attribute__((ext_vector_type(8))) at_h8;
+typedef float __attribute__((ext_vector_type(4))) at_f4;
+typedef unsigned __attribute__((ext_vector_type(4))) at_u4;
+typedef unsigned __attribute__((ext_vector_type(2))) at_u2;
+
+struct PagedAttend {
+  const void *K, *V;  // of the layer
+  int n_pages, page, Hkv, dh;
+  const void *q;
+  int64_t ldq;
+  int Hq;
+  float scale;
+  const int32_t *table;
+  int64_t ldt;
+  int n_req, max_blocks;
+  const int32_t *req, *pos;
+  int B;
+  void *out;
+  int64_t ldo;
+  int target;    // items that all keys together are cut into, about; 0: every row is one item
+  int rec;       // floats of a head's record of an item: running maximum, sum, two of padding, dh sums
+  float *part;   // [item][Hq][rec]
+};
+
+constexpr int AT_WAVES = 4, AT_THREADS = 64 * AT_WAVES;
+constexpr int AT_ROWS = 16;       // query heads of a tile
+constexpr int AT_PIECE = 128;     // an item's keys are a multiple of this
+constexpr float AT_LOG2E = 1.4426950408889634f;
+
+// Keys that row b sees (none where it is padding or names no request), and its request.
+__device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
+  r = a.req ? a.req[b] : b;
+  const long long n = (long long)a.pos[b] + 1, cap = (long long)a.max_blocks * a.page;
+  return (unsigned)r >= (unsigned)a.n_req || n < 0 ? 0 : (int)(n < cap ? n : cap);
+}
+
+// The items: row b has max(1, ceil(keys / C)) of them, C = all rows' keys over `target`, rounded up to AT_PIECE.  Every wave forms that from the rows'
+// positions by itself.
+struct AtItem {
+  int b, r, n, C, index, first, count;  // row, its request and keys; keys per item; which of the row's items; the row's first item; how many it has
+};
+__device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (n + C - 1) / C : 1; }
+template <bool BY_ROW>
+__device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {  // the wanted item; BY_ROW: item 0 of the wanted row.  b = -1: there is none
+  const int lane = threadIdx.x & 63;
+  AtItem it;
+  int r = 0, n = 0;
+  it.C = 0x7fffffff;
+  if (a.target > 0) {
+    long long all = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      n = b0 + lane < a.B ? at_keys(a, b0 + lane, r) : 0;
+      long long s = n;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+      all += s;
+    }
+    const long long c = ((all + a.target - 1) / a.target + AT_PIECE - 1) / AT_PIECE * AT_PIECE;
+    it.C = (int)(c < AT_PIECE ? AT_PIECE : c < 0x7fffff80 ? c : 0x7fffff80);
+  }
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const bool in = b0 + lane < a.B;
+    if (a.target == 0 || a.B > 64) n = in ? at_keys(a, b0 + lane, r) : 0;
+    const int c = in ? at_rows_items(n, it.C) : 0;
+    int ends = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(ends, o, 64);
+      if (lane >= o) ends += y;
+    }
+    const int total = __builtin_amdgcn_readlane(ends, 63);
+    const bool here = BY_ROW ? wanted < b0 + 64 : wanted < before + total;
+    if (here) {
+      const int l = BY_ROW ? wanted - b0 : __builtin_popcountll(__ballot(before + ends <= wanted));
+      it.b = b0 + l;
+      it.r = __builtin_amdgcn_readlane(r, l);
+      it.n = __builtin_amdgcn_readlane(n, l);
+      it.count = __builtin_amdgcn_readlane(c, l);
+      it.first = before + __builtin_amdgcn_readlane(ends, l) - it.count;
+      it.index = BY_ROW ? 0 : wanted - it.first;
+      return it;
+    }
+    before += total;
+  }
+  it.b = -1;
+  return it;
+}
+
+__device__ __forceinline__ float at_max4(float v) {  // over the four lanes 16 apart
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float at_sum4(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+template <typename T>
+__device__ __forceinline__ unsigned at_pack(float lo, float hi) {  // to nearest even
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  if constexpr (std::is_same<T, _Float16>::value) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), h2));
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), b2));
+  }
+}
+template <typename T>
+__device__ __forceinline__ at_f4 at_mma(at_u4 x, at_u4 y, at_f4 c) {
+  if constexpr (std::is_same<T, _Float16>::value)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(at_h8, x), __builtin_bit_cast(at_h8, y), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(at_b8, x), __builtin_bit_cast(at_b8, y), c, 0, 0, 0);
+}
+
+// A workgroup takes an item's keys for one kv head and up to 16 of its query heads; its waves take blocks of KEYS keys in turn and meet once, at the end.
+// Scores are formed as K q^T (a lane holds one query head's scores of four keys of each 16-key tile), the output as V^T p^T: the contraction runs over the
+// keys in the order in which the lanes hold the scores, so the probabilities go from one product into the other without leaving their lanes.  V's operand
+// wants eight keys of one channel in a lane: a lane loads eight channels of its eight keys and turns them around in its registers (half an instruction per
+// element); which channels make up a tile of the output is free, so neighbouring channels of V end up in neighbouring registers.
+//   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
+// PAGED16: page_size is a multiple of 16, so that a 16-key tile lies in one page and its address is a scalar; otherwise a lane looks up its own keys' places.
+// FULL: head_dim = DH; otherwise what a lane would load behind a row's end is replaced by zeros.
+template <typename T, int DH, bool PAGED16, bool FULL>
+__global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_kernel(PagedAttend a) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES;
+  constexpr int KP = DH * E / 64;                  // 16-byte pieces of a key row per lane (four lanes a row)
+  constexpr int VW = DH * E / 16 < 16 ? 8 : 16;    // bytes of a V load: a row's share of each of 16 lanes, at most 16
+  constexpr int VH = DH * E / 16 / VW;             // such loads a row
+  constexpr int VC = VW / E;                       // channels of one
+  constexpr int DT = DH / 16;                      // tiles of the output: channel VH-th part, one of VC
+  constexpr int VK = 4 * TILES;                    // keys whose V a lane loads
+  extern __shared__ __attribute__((aligned(16))) float at_lds[];
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
+  const AtItem it = at_find<false>(a, blockIdx.x);
+  if (it.b < 0) return;
+  const int g = a.Hq / a.Hkv, tiles = (g + AT_ROWS - 1) / AT_ROWS, h = (int)blockIdx.y / tiles, g0 = (int)blockIdx.y % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
+  const int rows = g - g0 < AT_ROWS ? g - g0 : AT_ROWS, head0 = h * g + g0;
+  const int k_first = it.index * it.C, k_end = it.n - k_first < it.C ? it.n : k_first + it.C;  // (C is a multiple of the block)
+  // this lane's query head as an operand column
+  at_u4 q[KP];
+  {
+    const char *qp = (const char *)a.q + (it.b * a.ldq + (int64_t)(head0 + (c16 < rows ? c16 : 0)) * dh) * E;
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int at = 64 * i + 16 * q4;
+      q[i] = FULL || at < dh * E ? *(const at_u4 *)(qp + at) : at_u4{0, 0, 0, 0};
+    }
+  }
+  const float to_log2 = a.scale * AT_LOG2E;
+  const int row_bytes = dh * E;
+  const int32_t *tab = a.table + it.r * a.ldt;
+  const int n_blocks = (k_end - k_first + KEYS - 1) / KEYS, mine = n_blocks > wave ? (n_blocks - wave + AT_WAVES - 1) / AT_WAVES : 0;
+  // Where the tiles lie: PAGED16: lane i holds byte offset and number of keys of tile i of the next 64 of this wave; else lane j < KEYS the offset of key j of the block, -1: none.
+  unsigned off_lo = 0, off_hi = 0;
+  int n_keys = 0;
+  auto place = [&](long long key) {  // byte offset of the key's row, -1: not in a page
+    const int block = (int)key / a.page, pg = tab[block];
+    return (unsigned)pg < (unsigned)a.n_pages ? (((long long)pg * a.Hkv + h) * a.page + ((int)key - block * a.page)) * row_bytes : -1ll;
+  };
+  auto look_up = [&](int i) {  // for block i of this wave
+    if (PAGED16 ? i % (64 / TILES) == 0 : true) {
+      const long long key = PAGED16 ? k_first + (long long)KEYS * (wave + (long long)AT_WAVES * (i + lane / TILES)) + 16 * (lane % TILES)
+                                    : k_first + (long long)KEYS * (wave + (long long)AT_WAVES * i) + lane;
+      long long at = -1;
+      if (key < k_end && (PAGED16 || lane < KEYS)) at = place(key);
+      off_lo = (unsigned)at;
+      off_hi = (unsigned)(at >> 32);
+      if (PAGED16) n_keys = at < 0 ? 0 : k_end - key < 16 ? (int)(k_end - key) : 16;
+    }
+  };
+  at_u4 kr[TILES][KP];
+  unsigned vr[VK][VH][VW / 4];
+  const char *kb = (const char *)a.K, *vb = (const char *)a.V;
+  unsigned seen = 0;  // bit j: key j of the block whose K is in the registers
+  long long tile_at[TILES];  // PAGED16
+  auto locate = [&](int i) {
+    seen = 0;
+    if constexpr (PAGED16) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const int l = i % (64 / TILES) * TILES + t, n = __builtin_amdgcn_readlane(n_keys, l);
+        const long long at = (long long)(unsigned)__builtin_amdgcn_readlane((int)off_lo, l) | (long long)__builtin_amdgcn_readlane((int)off_hi, l) << 32;
+        seen |= ((1u << n) - 1u) << (16 * t);
+        tile_at[t] = n > 0 ? at : 0;
+      }
+    } else {
+      seen = (unsigned)__ballot((int)off_hi >= 0) & (F32 ? 0xffffu : 0xffffffffu);
+    }
+  };
+  // (a key that is not seen is read as the first row of all: its score and its V are replaced)
+  auto key_at = [&](int j) {
+    const unsigned lo = __shfl((int)off_lo, j, 64), hi = __shfl((int)off_hi, j, 64);
+    return (int)hi < 0 ? 0ll : (long long)lo | (long long)hi << 32;
+  };
+  auto load_k = [&]() {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const bool in = PAGED16 ? (seen >> (16 * t + c16)) & 1u : true;
+      const char *p = kb + (PAGED16 ? tile_at[t] + (unsigned)((in ? c16 : 0) * row_bytes) : key_at(16 * t + c16));
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        const int at = 64 * i + 16 * q4;
+        const bool there = FULL || at < row_bytes;
+        kr[t][i] = *(const at_u4 *)(p + (there ? at : 0));
+        if (!there) kr[t][i] = at_u4{0, 0, 0, 0};
+      }
+    }
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int j = 0; j < VK; ++j) {
+      const int t = j >> 2, key = 4 * q4 + (j & 3);
+      const bool in = (seen >> (16 * t + key)) & 1u;
+      const char *p = vb + (PAGED16 ? tile_at[t] + (unsigned)((in ? key : 0) * row_bytes) : key_at(16 * t + key));
+#pragma unroll
+      for (int u = 0; u < VH; ++u) {
+        const int at = 16 * VW * u + VW * c16;
+        const char *from = p + (FULL || at < row_bytes ? at : 0);  // (channels behind the row's end are never stored)
+        if constexpr (VW == 16) *(at_u4 *)vr[j][u] = *(const at_u4 *)from;
+        else *(at_u2 *)vr[j][u] = *(const at_u2 *)from;
+      }
+    }
+  };
+  at_f4 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = at_f4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+  if (mine > 0) {
+    look_up(0);
+    locate(0);
+    load_k();
+    load_v();
+  }
+  for (int i = 0; i < mine; ++i) {
+    const unsigned now = seen;
+    at_f4 s[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      s[t] = at_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KP; ++k) {
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[t][k][e]), __uint_as_float(q[k][e]), s[t], 0, 0, 0);
+        } else {
+          s[t] = at_mma<T>(kr[t][k], q[k], s[t]);
+        }
+      }
+    }
+    const unsigned all = F32 ? 0xffffu : 0xffffffffu;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][e] *= to_log2;
+        if (now != all && !((now >> (16 * t + 4 * q4 + e)) & 1u)) s[t][e] = -INFINITY;
+        mx = fmaxf(mx, s[t][e]);
+      }
+    mx = at_max4(mx);
+    const float m_new = fmaxf(m_run, mx), base = m_new > -INFINITY ? m_new : 0.f;
+    if (__any(m_new > m_run)) {
+      const float corr = __builtin_amdgcn_exp2f(m_run - base);
+      m_run = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][e] = __builtin_amdgcn_exp2f(s[t][e] - base);
+        l_run += s[t][e];
+      }
+    if (now != all) {
+#pragma unroll
+      for (int j = 0; j < VK; ++j)
+        if (!((now >> (16 * (j >> 2) + 4 * q4 + (j & 3))) & 1u))
+#pragma unroll
+          for (int u = 0; u < VH; ++u)
+#pragma unroll
+            for (int w = 0; w < VW / 4; ++w) vr[j][u][w] = 0u;
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int u = 0; u < VH; ++u)
+#pragma unroll
+          for (int w = 0; w < VC; ++w)
+            o[u * VC + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[e][u][w]), s[0][e], o[u * VC + w], 0, 0, 0);
+    } else {
+      const at_u4 p = {at_pack<T>(s[0][0], s[0][1]), at_pack<T>(s[0][2], s[0][3]), at_pack<T>(s[TILES - 1][0], s[TILES - 1][1]), at_pack<T>(s[TILES - 1][2], s[TILES - 1][3])};
+#pragma unroll
+      for (int u = 0; u < VH; ++u)
+#pragma unroll
+        for (int w = 0; w < VW / 4; ++w)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            at_u4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              v[j] = __builtin_amdgcn_perm(vr[(2 * j + 1) % VK][u][w], vr[2 * j % VK][u][w], half ? 0x07060302u : 0x05040100u);
+            o[u * VC + 2 * w + half] = at_mma<T>(v, p, o[u * VC + 2 * w + half]);
+          }
+    }
+    if (i + 1 < mine) {
+      look_up(i + 1);
+      locate(i + 1);
+      load_k();
+      load_v();
+    }
+  }
+  l_run = at_sum4(l_run);
+  // waves 1 .. leave their sums, wave 0 adds them in order: per wave and row [m, l, -, -][DH]; output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w
+  constexpr int REC = DH + 4;
+  float *rec = at_lds + (size_t)((wave - 1) * AT_ROWS + c16) * REC;
+  if (wave > 0 && c16 < rows) {
+    if (q4 == 0) {
+      rec[0] = m_run;
+      rec[1] = l_run;
+    }
+#pragma unroll
+    for (int u = 0; u < VH; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int w = 0; w < VC; w += 4) {
+          at_f4 v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = o[u * VC + w + x][e];
+          *(at_f4 *)(rec + 4 + 16 * VC * u + VC * (4 * q4 + e) + w) = v;
+        }
+  }
+  __syncthreads();
+  if (wave > 0 || c16 >= rows) return;
+  float m = m_run;
+  const float *recs = at_lds + (size_t)c16 * REC;
+  for (int w = 1; w < AT_WAVES; ++w) m = fmaxf(m, recs[(size_t)(w - 1) * AT_ROWS * REC]);
+  const float base = m > -INFINITY ? m : 0.f;
+  float f = __builtin_amdgcn_exp2f(m_run - base), l = l_run * f;
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] *= f;
+  for (int w = 1; w < AT_WAVES; ++w) {
+    const float *p = recs + (size_t)(w - 1) * AT_ROWS * REC;
+    f = __builtin_amdgcn_exp2f(p[0] - base);
+    l += p[1] * f;
+#pragma unroll
+    for (int u = 0; u < VH; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < VC; c += 4) {
+          const at_f4 v = *(const at_f4 *)(p + 4 + 16 * VC * u + VC * (4 * q4 + e) + c);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[u * VC + c + x][e] += v[x] * f;
+        }
+  }
+  const int head = head0 + c16;
+  if (it.count > 1) {
+    float *to = a.part + ((size_t)blockIdx.x * a.Hq + head) * a.rec;
+    if (q4 == 0) {
+      to[0] = m;
+      to[1] = l;
+    }
+#pragma unroll
+    for (int u = 0; u < VH; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int ch = 16 * VC * u + VC * (4 * q4 + e);
+        if (!FULL && ch >= dh) continue;
+#pragma unroll
+        for (int w = 0; w < VC; w += 4) {
+          at_f4 v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = o[u * VC + w + x][e];
+          *(at_f4 *)(to + 4 + ch + w) = v;
+        }
+      }
+    return;
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // (nothing seen: zeros)
+  T *to = (T *)a.out + it.b * a.ldo + (int64_t)head * dh;
+#pragma unroll
+  for (int u = 0; u < VH; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int ch = 16 * VC * u + VC * (4 * q4 + e);
+      if (!FULL && ch >= dh) continue;
+      unsigned y[VW / 4];
+#pragma unroll
+      for (int w = 0; w < VW / 4; ++w) {
+        if constexpr (F32) y[w] = __float_as_uint(o[u * VC + w][e] * inv);
+        else y[w] = at_pack<T>(o[u * VC + 2 * w][e] * inv, o[u * VC + 2 * w + 1][e] * inv);
+      }
+      if constexpr (VW == 16) *(at_u4 *)(to + ch) = at_u4{y[0], y[1], y[2], y[3]};
+      else *(at_u2 *)(to + ch) = at_u2{y[0], y[1]};
+    }
+}
+
+// The items of a row and head, in item order: a workgroup each, whose waves take every fourth item; two channels a lane, so up to two turns.
+template <typename T>
+__global__ __launch_bounds__(AT_THREADS) void paged_join_kernel(PagedAttend a) {
+  __shared__ float sums[AT_WAVES - 1][256];
+  const AtItem it = at_find<true>(a, blockIdx.x);
+  if (it.count < 2) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.y;
+  const float *rec = a.part + ((size_t)it.first * a.Hq + head) * a.rec;
+  const size_t step = (size_t)a.Hq * a.rec;
+  float m = -INFINITY;
+  for (int i = lane; i < it.count; i += 64) m = fmaxf(m, rec[i * step]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float base = m > -INFINITY ? m : 0.f;
+  float l = 0.f;
+  for (int i = lane; i < it.count; i += 64) l += rec[i * step + 1] * __builtin_amdgcn_exp2f(rec[i * step] - base);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};  // channels lane, lane + 64, ...
+#pragma unroll 4
+  for (int i = wave; i < it.count; i += AT_WAVES) {
+    const float f = __builtin_amdgcn_exp2f(rec[i * step] - base);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (lane + 64 * c < a.dh) acc[c] += rec[i * step + 4 + lane + 64 * c] * f;
+  }
+  if (wave > 0)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sums[wave - 1][lane + 64 * c] = acc[c];
+  __syncthreads();
+  if (wave > 0) return;
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int ch = lane + 64 * c;
+    if (ch >= a.dh) break;
+    for (int w = 0; w < AT_WAVES - 1; ++w) acc[c] += sums[w][ch];
+    const float y = acc[c] * inv;
+    T *to = (T *)a.out + it.b * a.ldo + (int64_t)head * a.dh + ch;
+    if constexpr (sizeof(T) == 4) *to = y;
+    else *(uint16_t *)to = (uint16_t)at_pack<T>(y, 0.f);
+  }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------
+// Workgroups for all keys together: about two per compute unit, which is what fits.  A row of a cache of up to AT_WHOLE positions is not cut: the second launch
+// would cost more than the few blocks of keys that a wave has left.
+constexpr int AT_WGS = 512, AT_WHOLE = 512;
+struct AtPlan {
+  int target, items, tiles;
+  size_t bytes;
+};
+static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
+  AtPlan r{};
+  r.tiles = ceil_div(Hq / p.n_kv_heads, AT_ROWS);
+  const long long cap = (long long)max_blocks * p.page_size;
+  r.items = B;
+  if (cap > AT_WHOLE) {
+    r.target = std::max(1, AT_WGS / (p.n_kv_heads * r.tiles));
+    r.items = (int)std::min<long long>((long long)r.target + B, B * ((cap + AT_PIECE - 1) / AT_PIECE));
+    r.bytes = (size_t)r.items * Hq * (p.head_dim + 4) * 4;
+  }
+  return r;
+}
+
+template <typename T, int DH, bool PAGED16, bool FULL>
+static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
+  constexpr int lds = (AT_WAVES - 1) * AT_ROWS * (DH + 4) * 4;
+  static_assert(lds <= 64 * 1024, "LDS that a launch may ask for");
+  {
+    ProfScope ps("paged_attend", s);
+    paged_attend_kernel<T, DH, PAGED16, FULL><<<dim3(plan.items, a.Hkv * plan.tiles), AT_THREADS, lds, s>>>(a);
+  }
+  if (plan.target > 0) {
+    ProfScope ps("paged_join", s);
+    paged_join_kernel<T><<<dim3(a.B, a.Hq), AT_THREADS, 0, s>>>(a);
+  }
+  LA_HIP(hipGetLastError());
+  return LA_OK;
+}
+template <typename T>
+static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
+  auto sized = [&](auto dh) {
+    constexpr int DH = decltype(dh)::value;
+    if constexpr (sizeof(T) == 4) {  // (not a type of large models: the one general kernel)
+      return at_launch<T, DH, false, false>(a, plan, s);
+    } else {
+      const bool in16 = a.page % 16 == 0;
+      if (a.dh == DH) return in16 ? at_launch<T, DH, true, true>(a, plan, s) : at_launch<T, DH, false, true>(a, plan, s);
+      return in16 ? at_launch<T, DH, true, false>(a, plan, s) : at_launch<T, DH, false, false>(a, plan, s);
+    }
+  };
+  if (a.dh <= 64) return sized(std::integral_constant<int, 64>{});
+  if (a.dh <= 128) return sized(std::integral_constant<int, 128>{});
+  return sized(std::integral_constant<int, 256>{});
+}
+
+}  // namespace la
+
+using namespace la;
+
+extern "C" size_t la_paged_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int B) {
+  if (check_pages(pages, 0) || n_q_heads < 1 || n_q_heads % pages->n_kv_heads || max_blocks < 1 || B < 1) return 0;  // (what the call itself refuses)
+  return at_plan(*pages, n_q_heads, max_blocks, B).bytes;
+}
+
+extern "C" int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table,
+                               int64_t table_stride, int n_requests, int max_blocks, const int32_t *req, const int32_t *pos, int B, void *out, int64_t out_stride,
+                               void *workspace, size_t workspace_bytes, void *stream) {
+  if (const int rc = check_pages(pages, layer)) return rc;
+  const la_pages_desc &p = *pages;
+  const size_t e = esize(&p);
+  LA_REQUIRE(B >= 0, LA_EINVAL, "B=%d is negative", B);
+  if (B == 0) return LA_OK;
+  LA_REQUIRE(q && table && pos && out, LA_EINVAL, "NULL argument");
+  LA_REQUIRE(n_q_heads > 0 && n_q_heads % p.n_kv_heads == 0, LA_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", n_q_heads, p.n_kv_heads);
+  LA_REQUIRE(n_requests >= 1 && max_blocks >= 1 && (table_stride >= max_blocks || n_requests == 1), LA_EINVAL, "bad table dimensions");
+  LA_REQUIRE((long long)max_blocks * p.page_size < (1ll << 31), LA_EINVAL, "%d blocks of %d positions: positions are 32-bit numbers", max_blocks, p.page_size);
+  LA_REQUIRE(req || B <= n_requests, LA_EINVAL, "%d rows for %d requests and no row map", B, n_requests);
+  LA_REQUIRE(B <= LA_MAX_ATTEND_ROWS && n_q_heads <= 65535, LA_EINVAL, "%d rows of %d heads, at most %d of 65535", B, n_q_heads, LA_MAX_ATTEND_ROWS);
+  LA_REQUIRE(aligned16({q, out}) && q_stride * e % 16 == 0 && out_stride * e % 16 == 0, LA_EINVAL, "q and out rows must be 16-byte aligned");
+  LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
+  const AtPlan plan = at_plan(p, n_q_heads, max_blocks, B);
+  LA_REQUIRE(workspace_bytes >= plan.bytes && (workspace || !plan.bytes), LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
+  LA_REQUIRE(aligned16({workspace}), LA_EINVAL, "workspace must be 16-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  const size_t at = layer * layer_bytes(&p);
+  const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride,
+                      n_requests, max_blocks, req, pos, B, out, out_stride, plan.target, p.head_dim + 4, (float *)workspace};
+  if (p.dtype == LA_F32) return at_launch<float>(a, plan, s);
+  if (p.dtype == LA_F16) return at_launch<_Float16>(a, plan, s);
+  return at_launch<uint16_t>(a, plan, s);
+}

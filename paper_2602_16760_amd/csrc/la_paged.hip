@@ -1,9 +1,8 @@
 // A cache that several requests share: pages of page_size positions each, handed out per request.  Block tables and slot maps from the requests'
-// lengths (la_page_map), the rows' way into the pages (la_paged_write) and the attention that reads them (la_paged_attend).
+// lengths (la_page_map) and the rows' way into the pages (la_paged_write); the attention that reads them is in la_attend.hip.
 #include <algorithm>
 
-#include "la_device.h"
-#include "la_internal.h"
+#include "la_paged.h"
 
 namespace la {
 
@@ -165,90 +164,6 @@ __global__ __launch_bounds__(256) void paged_write_kernel(uint4 *kp, uint4 *vp, 
   vp[to] = v[row * ldv + c];
 }
 
-// ---- attention over pages ---------------------------------------------------------------------------------------
-struct PagedAttend {
-  const void *K, *V;  // of the layer
-  int n_pages, page, Hkv, dh;
-  const void *q;
-  int64_t ldq;
-  int Hq;
-  float scale;
-  const int32_t *table;
-  int64_t ldt;
-  int n_req, max_blocks;
-  const int32_t *req, *pos;
-  void *out;
-  int64_t ldo;
-};
-
-// Row b's request and the keys it sees: none where the row is padding or names no request.
-__device__ __forceinline__ int paged_keys(const PagedAttend &a, int b, int &r) {
-  r = a.req ? a.req[b] : b;
-  if ((unsigned)r >= (unsigned)a.n_req) return 0;
-  const long long n = (long long)a.pos[b] + 1, cap = (long long)a.max_blocks * a.page;
-  return (int)(n < 0 ? 0 : n < cap ? n : cap);
-}
-
-// A workgroup per row and query head: online softmax over chunks of 256 keys, a key per thread for the scores; threads form 256 / dh groups of a channel each
-// for the output.
-template <typename T>
-__global__ __launch_bounds__(256) void paged_attend_kernel(PagedAttend a) {
-  __shared__ float qs[256], ps[256], red[4];
-  __shared__ long long at[256];
-  const int b = blockIdx.x, hq = blockIdx.y, t = threadIdx.x, h = hq / (a.Hq / a.Hkv), dh = a.dh;
-  int r;
-  const int n = paged_keys(a, b, r);
-  const T *q = (const T *)a.q + b * a.ldq + hq * dh, *K = (const T *)a.K, *V = (const T *)a.V;
-  if (t < dh) qs[t] = load_as_float<T>(q + t);
-  const int groups = 256 / dh, gi = t / dh, ch = t - gi * dh;
-  float m_run = -INFINITY, l_run = 0.f, acc = 0.f;
-  auto all = [&](float v, bool max) {
-    for (int o = 32; o > 0; o >>= 1) v = max ? fmaxf(v, __shfl_xor(v, o, 64)) : v + __shfl_xor(v, o, 64);
-    __syncthreads();
-    if ((t & 63) == 0) red[t >> 6] = v;
-    __syncthreads();
-    return max ? fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) : (red[0] + red[1]) + (red[2] + red[3]);
-  };
-  for (int k0 = 0; k0 < n; k0 += 256) {
-    const int j = k0 + t, block = j / a.page;
-    const int pg = j < n ? a.table[r * a.ldt + block] : -1;
-    const long long row = (unsigned)pg < (unsigned)a.n_pages ? (((long long)pg * a.Hkv + h) * a.page + (j - block * a.page)) * dh : -1;
-    __syncthreads();
-    at[t] = row;
-    float s = -INFINITY;
-    if (row >= 0) {
-      s = 0.f;
-      for (int i = 0; i < dh; ++i) s = fmaf(qs[i], load_as_float<T>(K + row + i), s);
-      s *= a.scale;
-    }
-    const float m_new = fmaxf(m_run, all(s, true));
-    const float p = s > -INFINITY ? expf(s - m_new) : 0.f, corr = m_run > -INFINITY ? expf(m_run - m_new) : 0.f;
-    ps[t] = p;
-    l_run = l_run * corr + all(p, false);  // (its barriers publish ps)
-    m_run = m_new;
-    if (gi < groups) {
-      acc *= corr;
-      const int end = n - k0 < 256 ? n - k0 : 256;
-      for (int u = gi; u < end; u += groups)
-        if (at[u] >= 0) acc = fmaf(ps[u], load_as_float<T>(V + at[u] + ch), acc);
-    }
-  }
-  __syncthreads();
-  ps[t] = gi < groups ? acc : 0.f;
-  __syncthreads();
-  if (t < dh) {
-    float o = 0.f;
-    for (int u = 0; u < groups; ++u) o += ps[u * dh + t];
-    store_from_float<T>((T *)a.out + b * a.ldo + hq * dh + t, l_run > 0.f ? o / l_run : 0.f);
-  }
-}
-
-static bool aligned16(std::initializer_list<const void *> ps) {
-  uintptr_t all = 0;
-  for (const void *p : ps) all |= (uintptr_t)p;
-  return all % 16 == 0;
-}
-
 int check_pages(const la_pages_desc *p, int layer) {
   LA_REQUIRE(p && p->k && p->v, LA_EINVAL, "NULL pages");
   LA_REQUIRE(p->n_layers > 0 && p->n_pages > 0 && p->page_size > 0 && p->n_kv_heads > 0, LA_EINVAL, "page dimensions must be positive");
@@ -259,8 +174,6 @@ int check_pages(const la_pages_desc *p, int layer) {
   LA_REQUIRE(layer >= 0 && layer < p->n_layers, LA_ERANGE, "layer %d outside the pages' %d layers", layer, p->n_layers);
   return LA_OK;
 }
-static size_t esize(const la_pages_desc *p) { return p->dtype == LA_F32 ? 4 : 2; }
-static size_t layer_bytes(const la_pages_desc *p) { return (size_t)p->n_pages * p->n_kv_heads * p->page_size * p->head_dim * esize(p); }
 
 }  // namespace la
 
@@ -307,35 +220,3 @@ extern "C" int la_paged_write(const la_pages_desc *pages, int layer, const void 
   return LA_OK;
 }
 
-extern "C" size_t la_paged_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int B) {
-  (void)pages; (void)n_q_heads; (void)max_blocks; (void)B;
-  return 0;
-}
-
-extern "C" int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table,
-                               int64_t table_stride, int n_requests, int max_blocks, const int32_t *req, const int32_t *pos, int B, void *out, int64_t out_stride,
-                               void *workspace, size_t workspace_bytes, void *stream) {
-  if (const int rc = check_pages(pages, layer)) return rc;
-  const la_pages_desc &p = *pages;
-  const size_t e = esize(&p);
-  LA_REQUIRE(B >= 0, LA_EINVAL, "B=%d is negative", B);
-  if (B == 0) return LA_OK;
-  LA_REQUIRE(q && table && pos && out, LA_EINVAL, "NULL argument");
-  LA_REQUIRE(n_q_heads > 0 && n_q_heads % p.n_kv_heads == 0, LA_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", n_q_heads, p.n_kv_heads);
-  LA_REQUIRE(n_requests >= 1 && max_blocks >= 1 && (table_stride >= max_blocks || n_requests == 1), LA_EINVAL, "bad table dimensions");
-  LA_REQUIRE(req || B <= n_requests, LA_EINVAL, "%d rows for %d requests and no row map", B, n_requests);
-  LA_REQUIRE(aligned16({q, out}) && q_stride * e % 16 == 0 && out_stride * e % 16 == 0, LA_EINVAL, "q and out rows must be 16-byte aligned");
-  LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
-  (void)workspace; (void)workspace_bytes;
-  hipStream_t s = (hipStream_t)stream;
-  const size_t at = layer * layer_bytes(&p);
-  const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride,
-                      n_requests, max_blocks, req, pos, out, out_stride};
-  ProfScope ps("paged_attend", s);
-  const dim3 grid(B, n_q_heads);
-  if (p.dtype == LA_F32) paged_attend_kernel<float><<<grid, 256, 0, s>>>(a);
-  else if (p.dtype == LA_F16) paged_attend_kernel<_Float16><<<grid, 256, 0, s>>>(a);
-  else paged_attend_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
-  LA_HIP(hipGetLastError());
-  return LA_OK;
-}
