@@ -256,12 +256,12 @@ typedef struct {
  * temperature); a logit of NaN counts as -inf, +inf as the largest finite number, and a weight below 2^-64 as none.  Order:
  * larger logits first, equal ones by index.  Of the kept tokens in index order the first whose sum of weights passes u times
  * their total is drawn (the last one if none does).  A row without any token gets -1.  prob (device float [B], or NULL) receives the
- * drawn token's weight over that total (1 for temperature 0, 0 for id -1).  Weights and sums are formed in 64 bits: the result does
- * not depend on the rows beside it or on the order of any sum.
+ * drawn token's weight over that total (1 for temperature 0, 0 for id -1).  Weights are formed in 64 bits and kept to 36 behind the point, sums in 64:
+ * the result does not depend on the rows beside it, and equal logits have equal shares.
  * logits: device, la_dtype `dtype`, row b at logits + b * row_stride elements; any alignment of the type.  ids: device int32 [B].
  * workspace: device memory of la_sample_workspace(B, V) bytes, 16-byte aligned, which the call may overwrite and which no other call
  * may use meanwhile; nothing is kept in it.
- * LA_EINVAL: V outside 1..LA_MAX_SAMPLE_VOCAB, rows that overlap, n_u too small, a NULL pointer; LA_ENOMEM: workspace too small.  B = 0 does nothing. */
+ * LA_EINVAL: V outside 1..LA_MAX_SAMPLE_VOCAB, rows that overlap, n_u too small, B above 65535, a NULL pointer; LA_ENOMEM: workspace too small.  B = 0 does nothing. */
 size_t la_sample_workspace(int B, int V);
 int la_sample(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_sampling *how, int32_t *ids, float *prob, void *workspace,
               size_t workspace_bytes, void *stream);

@@ -4,16 +4,30 @@
 
 namespace la {
 
+// Weights.  With y = logit * 8 log2(e) / temperature (64 bits) and a = floor(y), a token's weight is 2^(a / 8) 2^((y - a) / 8): its bin is the number of eighths of
+// an octave between its a and the row's largest, the second factor lies in [1, 1.091) and is rounded to 36 bits behind the point, wherever it is used.  Sums over a
+// bin are then sums of whole numbers: they do not depend on the order in which LDS atomics take them, and equal logits have equal shares.  Everything behind them
+// is added in a fixed order.  A sum of n weights is off by about 2^-38 / sqrt(n) of itself.  Bins reach 64 octaves down, below which a weight counts as none.
+constexpr int SMP_CHUNK = 8192;               // tokens of a workgroup of the first launch
+constexpr int SMP_BINS = 514, SMP_HIST = 520;  // (64 octaves below the largest token end in the 514th bin at the latest); row length of a chunk's sums
+constexpr int SMP_LIST = 4096;                // tokens of a bin that fit into LDS
+constexpr int SMP_SUB = 1024;                 // parts that a range of tokens is cut into at a time
+constexpr int SMP_COUNT_SHIFT = 50;           // a chunk's word of a bin: the number of its tokens above that bit, the sum of their factors below, in units of 2^-36
+constexpr unsigned long long SMP_SUM_MASK = (1ull << SMP_COUNT_SHIFT) - 1;
+constexpr double SMP_UNIT = 0x1p36, LEAST_WEIGHT = 0x1p-64;
+static_assert(SMP_CHUNK * 1.1 * SMP_UNIT < (double)SMP_SUM_MASK && SMP_CHUNK <= 1 << 13, "a chunk in one bin");
+static_assert(LA_MAX_SAMPLE_VOCAB * 1.1 * SMP_UNIT < 0x1p64 && LA_MAX_SAMPLE_VOCAB / SMP_CHUNK <= 64, "a row in one bin; a lane per chunk");
+
 struct Sample {
   const void *x;
   int64_t ld;
-  int V;
+  int V, chunks;
   la_sampling p;
   int32_t *ids;
   float *prob;
+  unsigned long long *best;  // [B][chunks] first token in order
+  unsigned long long *hist;  // [B][chunks][SMP_HIST]
 };
-
-constexpr double LEAST_WEIGHT = 0x1p-64;
 
 // A logit as it counts: NaN like -inf (no token), +inf like the largest finite value, -0 like 0.
 template <typename T>
@@ -21,123 +35,473 @@ __device__ __forceinline__ float sample_logit(const T *p) {
   const float x = load_as_float<T>(p);
   return x != x ? -INFINITY : fminf(x, 3.402823466e38f) + 0.f;
 }
-__device__ __forceinline__ uint32_t sample_key(float x) {  // keys are ordered as the values are
+// A token as a number: larger is in front, (value descending, index ascending).
+__device__ __forceinline__ unsigned long long sample_place(float x, int i) {
   const uint32_t u = __float_as_uint(x);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return (unsigned long long)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (0xffffffffu - (unsigned)i);
+}
+__device__ __forceinline__ float sample_value(unsigned long long c) {
+  const uint32_t k = (uint32_t)(c >> 32);
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ int sample_index(unsigned long long c) { return (int)(0xffffffffu - (uint32_t)c); }
+
+// 2^(f / 8), 0 <= f < 1, in units of 2^-36: the exponential's series around f = 1 / 2, whose seventh term is below 6e-14.
+__device__ __forceinline__ unsigned long long sample_factor(double f) {
+  const double z = (f - 0.5) * (0.6931471805599453094 / 8);
+  double s = 1.0 / 720;
+  s = __builtin_fma(s, z, 1.0 / 120);
+  s = __builtin_fma(s, z, 1.0 / 24);
+  s = __builtin_fma(s, z, 1.0 / 6);
+  s = __builtin_fma(s, z, 0.5);
+  s = __builtin_fma(s, z, 1.0);
+  s = __builtin_fma(s, z, 1.0);
+  return __double2ull_rn(s * (1.0442737824274138403 * SMP_UNIT));  // 2^(1 / 16)
+}
+__device__ __forceinline__ double sample_eighths(int t) {  // 2^(-t / 8) units
+  constexpr double e[8] = {1.0, 0.91700404320467123, 0.84089641525371454, 0.77110541270397041, 0.70710678118654752, 0.64841977732550483, 0.59460355750136053, 0.54525386633262883};
+  double v = e[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) v = (t & 7) == i ? e[i] : v;
+  return ldexp(v * (1 / SMP_UNIT), -(t >> 3));
 }
 
-constexpr int SMP_THREADS = 1024;
+// How row b is sampled; the filters that are off are out of reach.
+struct SampleRow {
+  bool greedy;
+  double rate;  // y = logit * rate
+  int k;        // V: off
+  float p, low;
+};
+__device__ __forceinline__ SampleRow sample_row(const Sample &a, int b) {
+  SampleRow r;
+  const float t = a.p.temperature ? a.p.temperature[b] : 1.f;
+  r.greedy = !(t > 0.f);
+  r.rate = 8 * 1.44269504088896340736 / (double)t;
+  const int k = a.p.top_k ? a.p.top_k[b] : 0;
+  r.k = k > 0 && k < a.V ? k : a.V;
+  r.p = a.p.top_p ? a.p.top_p[b] : 1.f;
+  if (!(r.p < 1.f)) r.p = 1.f;
+  if (!(r.p > 0.f)) {  // the first token alone
+    r.p = 1.f;
+    r.k = 1;
+  }
+  r.low = a.p.min_p ? a.p.min_p[b] : 0.f;
+  r.low = r.low > 0.f ? fminf(r.low, 1.f) : 0.f;
+  return r;
+}
+
+// First launch, a workgroup per chunk of a row: its first token in order, and its bins' sums, relative to that token's.
+constexpr int SMP_SUM_THREADS = 512;
+template <typename T>
+__global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
+  constexpr int N = SMP_CHUNK / SMP_SUM_THREADS, WAVES = SMP_SUM_THREADS / 64;
+  __shared__ unsigned long long hist[SMP_HIST], red[WAVES];
+  const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, i0 = c * SMP_CHUNK + t;
+  const T *x = (const T *)a.x + b * a.ld;
+  float v[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = i0 + SMP_SUM_THREADS * j;
+    v[j] = i < a.V ? sample_logit<T>(x + i) : -INFINITY;
+  }
+  const SampleRow r = sample_row(a, b);
+  for (int i = t; i < SMP_HIST; i += SMP_SUM_THREADS) hist[i] = 0;
+  unsigned long long best = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const unsigned long long at = sample_place(v[j], i0 + SMP_SUM_THREADS * j);
+    best = at > best ? at : best;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const unsigned long long y = __shfl_xor(best, o, 64);
+    best = y > best ? y : best;
+  }
+  if ((t & 63) == 0) red[t >> 6] = best;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) best = red[w] > best ? red[w] : best;
+  const size_t at = (size_t)b * a.chunks + c;
+  if (t == 0) a.best[at] = best;
+  const float top = sample_value(best);
+  if (r.greedy || !(top > -INFINITY)) return;
+  const double first = floor((double)top * r.rate);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const double y = (double)v[j] * r.rate, low = floor(y);
+    const double d = first - low;
+    if (v[j] > -INFINITY && d < SMP_BINS) atomicAdd(&hist[(int)d], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low));
+  }
+  __syncthreads();
+  for (int i = t; i < SMP_HIST; i += SMP_SUM_THREADS) a.hist[at * SMP_HIST + i] = hist[i];
+}
+
+// Second launch, a workgroup per row: where the filters cut, what is left of every chunk, and in the chunk where u falls the token.
+constexpr int SMP_THREADS = 1024, SMP_WAVES = SMP_THREADS / 64;
+struct SampleShared {
+  unsigned long long list[SMP_LIST];
+  unsigned long long sub_w[SMP_SUB];
+  unsigned sub_n[SMP_SUB];
+  double through_w[SMP_BINS];  // sums over the bins up to and with this one
+  int through_n[SMP_BINS];
+  unsigned long long best[64], chunk_in[64];
+  int shift[64];
+  double chunk[64], before[64];
+  double red_d[SMP_WAVES];
+  unsigned long long red_u[SMP_WAVES];
+  unsigned red_n[SMP_WAVES];
+  unsigned long long lo, hi, base_w, kept_w, found;
+  unsigned n_list, base_n, part_n;
+  int hit, last, where;
+};
 
 template <typename T>
 __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
-  __shared__ double red[SMP_THREADS / 64], scan[SMP_THREADS / 64];
-  __shared__ unsigned long long redu[SMP_THREADS / 64];
-  __shared__ int found;
-  const int b = blockIdx.x, t = threadIdx.x, V = a.V;
+  __shared__ SampleShared m;
+  const int b = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63, V = a.V, C = a.chunks;
   const T *x = (const T *)a.x + b * a.ld;
-  auto sum = [&](double v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    __syncthreads();
-    if ((t & 63) == 0) red[t >> 6] = v;
-    __syncthreads();
-    double s = 0;
-    for (int w = 0; w < SMP_THREADS / 64; ++w) s += red[w];
-    return s;
-  };
-  // the row's first token in order: (value descending, index ascending), as one number
-  auto place = [&](int i) { return (unsigned long long)sample_key(sample_logit<T>(x + i)) << 32 | (0xffffffffu - (unsigned)i); };
-  unsigned long long best = 0;
-  for (int i = t; i < V; i += SMP_THREADS) {
-    const unsigned long long c = place(i);
-    best = c > best ? c : best;
+  const SampleRow r = sample_row(a, b);
+  if (t < 64) {
+    unsigned long long best = t < C ? a.best[(size_t)b * C + t] : 0;
+    m.best[t] = best;
+    m.chunk_in[t] = 0;
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    const unsigned long long c = __shfl_xor(best, o, 64);
-    best = c > best ? c : best;
-  }
-  if ((t & 63) == 0) redu[t >> 6] = best;
   __syncthreads();
-  for (int w = 0; w < SMP_THREADS / 64; ++w) best = redu[w] > best ? redu[w] : best;
-  const int i_top = (int)(0xffffffffu - (unsigned)best);
-  const float top = sample_logit<T>(x + i_top);
-  const float temp = a.p.temperature ? a.p.temperature[b] : 1.f;
-  if (!(top > -INFINITY) || !(temp > 0.f)) {
+  unsigned long long best = m.best[lane];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const unsigned long long y = __shfl_xor(best, o, 64);
+    best = y > best ? y : best;
+  }
+  const float top = sample_value(best);
+  if (r.greedy || !(top > -INFINITY)) {
     if (t == 0) {
-      a.ids[b] = top > -INFINITY ? i_top : -1;
+      a.ids[b] = top > -INFINITY ? sample_index(best) : -1;
       if (a.prob) a.prob[b] = top > -INFINITY ? 1.f : 0.f;
     }
     return;
   }
-  auto weight = [&](int i) {
-    const float v = sample_logit<T>(x + i);
-    const double w = v > -INFINITY ? exp(((double)v - (double)top) / (double)temp) : 0.0;
-    return w < LEAST_WEIGHT ? 0.0 : w;
-  };
-  // the last token that is kept, by bisection over the order
-  const int k = a.p.top_k && a.p.top_k[b] > 0 && a.p.top_k[b] < V ? a.p.top_k[b] : V;
-  const float p = a.p.top_p ? a.p.top_p[b] : 1.f, low = a.p.min_p ? a.p.min_p[b] : 0.f;
-  auto last_with = [&](auto enough) {  // the largest c whose tokens at c or in front of it are enough
-    unsigned long long c = 0;
-    for (int bit = 63; bit >= 0; --bit)
-      if (enough(c | 1ull << bit)) c |= 1ull << bit;
-    return c;
-  };
-  unsigned long long cut = k < V ? last_with([&](unsigned long long c) {
-    double n = 0;
-    for (int i = t; i < V; i += SMP_THREADS) n += place(i) >= c;
-    return sum(n) >= (double)k;
-  }) : 0;
-  auto mass = [&](unsigned long long c) {
-    double n = 0;
-    for (int i = t; i < V; i += SMP_THREADS)
-      if (place(i) >= c) n += weight(i);
-    return sum(n);
-  };
-  if (p < 1.f) {
-    const double want = (double)p * mass(cut);
-    const unsigned long long c = p > 0.f ? last_with([&](unsigned long long c) { return mass(c) >= want; }) : best;
-    cut = c > cut ? c : cut;
+  const double y_top = (double)top * r.rate, first = floor(y_top), w_top = (double)sample_factor(y_top - first) * (1 / SMP_UNIT);
+  if (t < 64) {
+    const double d = t < C ? first - floor((double)sample_value(m.best[t]) * r.rate) : (double)SMP_BINS;
+    m.shift[t] = d < SMP_BINS ? (int)d : SMP_BINS;  // (a chunk without a token: NaN or infinite, and never looked at)
   }
-  const double least = low > 0.f ? (low < 1.f ? (double)low : 1.0) : 0.0;
-  auto kept = [&](int i) {
-    const double w = i < V && place(i) >= cut ? weight(i) : 0.0;
-    return w >= least ? w : 0.0;
-  };
-  // sums in index order, tiles of a token per thread; the second time until the sum passes u of the whole
-  double want = -1.0, total = 0.0;
-  for (int turn = 0; turn < 2; ++turn) {
-    double before = 0.0;
-    for (int i0 = 0; i0 < V; i0 += SMP_THREADS) {
-      const double w = kept(i0 + t);
-      double s = w;
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(s, o, 64);
-        if ((t & 63) >= o) s += y;
+  __syncthreads();
+  const unsigned long long *hist = a.hist + (size_t)b * C * SMP_HIST;
+  // ---- the row's bins, summed up from the largest weights on
+  {
+    double w = 0;
+    int n = 0;
+    if (t < SMP_BINS) {
+#pragma unroll 8
+      for (int c = 0; c < C; ++c) {
+        const int l = t - m.shift[c];
+        const unsigned long long h = l >= 0 ? hist[(size_t)c * SMP_HIST + l] : 0;
+        w += (double)(h & SMP_SUM_MASK);
+        n += (int)(h >> SMP_COUNT_SHIFT);
       }
-      __syncthreads();
-      if ((t & 63) == 63) scan[t >> 6] = s;
-      if (t == 0) found = 0x7fffffff;
-      __syncthreads();
-      double front = before, all = before;
-      for (int q = 0; q < SMP_THREADS / 64; ++q) {
-        if (q < (t >> 6)) front += scan[q];
-        all += scan[q];
+      w *= sample_eighths(t);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double yw = __shfl_up(w, o, 64);
+      const int yn = __shfl_up(n, o, 64);
+      if (lane >= o) {
+        w += yw;
+        n += yn;
       }
-      if (turn == 1) {
-        if (w > 0.0 && front + s > want) atomicMin(&found, i0 + t);
-        __syncthreads();
-        if (found != 0x7fffffff) {
-          if (t == 0) a.ids[b] = found;
-          if (i0 + t == found && a.prob) a.prob[b] = (float)(w / total);
-          return;
+    }
+    if (lane == 63) {
+      m.red_d[wave] = w;
+      m.red_n[wave] = n;
+    }
+    __syncthreads();
+    for (int q = 0; q < wave; ++q) {
+      w += m.red_d[q];
+      n += m.red_n[q];
+    }
+    if (t < SMP_BINS) {
+      m.through_w[t] = w;
+      m.through_n[t] = n;
+    }
+    if (t == 0) m.hit = SMP_BINS;
+    __syncthreads();
+  }
+  auto in_bins = [&](double y, int t0, int t1) { return y >= first - t1 && (t0 == 0 || y < first - t0 + 1); };
+  int listed0 = SMP_BINS, listed1 = -1;            // bins whose tokens are in the list
+  unsigned long long ends_lo = 0, ends_hi = ~0ull;  // no token of theirs lies outside
+  // Tokens of bins t0 .. t1 into the list, and their ends of the order (whether they fit or not).
+  auto gather = [&](int t0, int t1) {
+    __syncthreads();
+    if (t == 0) {
+      m.n_list = 0;
+      m.lo = ~0ull;
+      m.hi = 0;
+    }
+    __syncthreads();
+    unsigned long long lo = ~0ull, hi = 0;
+    for (int i0 = 0; i0 < V; i0 += 8 * SMP_THREADS) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + t + SMP_THREADS * j;
+        v[j] = i < V ? sample_logit<T>(x + i) : -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + t + SMP_THREADS * j;
+        if (v[j] > -INFINITY && in_bins((double)v[j] * r.rate, t0, t1)) {
+          const unsigned long long c = sample_place(v[j], i);
+          lo = c < lo ? c : lo;
+          hi = c > hi ? c : hi;
+          const unsigned s = atomicAdd(&m.n_list, 1u);
+          if (s < SMP_LIST) m.list[s] = c;
         }
       }
-      before = all;
     }
-    total = before;
-    float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
-    u = u > 0.f ? u : 0.f;
-    want = fmin((double)u, 1.0 - 0x1p-30) * total;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const unsigned long long yl = __shfl_xor(lo, o, 64), yh = __shfl_xor(hi, o, 64);
+      lo = yl < lo ? yl : lo;
+      hi = yh > hi ? yh : hi;
+    }
+    if (lane == 0) {
+      atomicMin(&m.lo, lo);
+      atomicMax(&m.hi, hi);
+    }
+    __syncthreads();
+    ends_lo = m.lo;
+    ends_hi = m.hi;
+    listed0 = m.n_list <= SMP_LIST ? t0 : SMP_BINS;
+    listed1 = m.n_list <= SMP_LIST ? t1 : -1;
+  };
+  // Every token of bin `bin` and of places lo .. hi: f(its place, its factor).
+  auto each = [&](int bin, unsigned long long lo, unsigned long long hi, auto f) {
+    auto take = [&](unsigned long long c, float v) {
+      const double y = (double)v * r.rate;
+      if (c >= lo && c <= hi && in_bins(y, bin, bin)) f(c, sample_factor(y - floor(y)));
+    };
+    if (bin >= listed0 && bin <= listed1) {
+      const int n = (int)m.n_list;
+      for (int i = t; i < n; i += SMP_THREADS) take(m.list[i], sample_value(m.list[i]));
+    } else {
+      for (int i = t; i < V; i += SMP_THREADS) {
+        const float v = sample_logit<T>(x + i);
+        if (v > -INFINITY) take(sample_place(v, i), v);
+      }
+    }
+  };
+  // The last of the tokens that are kept of a bin: the rank-th in order, or the first with which their sum of factors reaches want;
+  // the last one at `from` or in front of it if none does.  m.kept_w: their sum.  The range of places is cut into SMP_SUB parts until one token is left, which
+  // takes seven turns at most (a place has 64 bits, a turn settles ten); a range without any token ends it too.
+  auto last_kept = [&](int bin, unsigned long long from, unsigned rank, double want) {
+    __syncthreads();
+    if (t == 0) {
+      m.lo = ends_lo > from ? ends_lo : from;
+      m.hi = ends_hi;
+      m.base_n = 0;
+      m.base_w = m.kept_w = 0;
+      m.found = ~0ull;
+    }
+    __syncthreads();
+    for (int turn = 0; turn < 8; ++turn) {
+      const unsigned long long lo = m.lo, hi = m.hi;
+      const int bits = 64 - __builtin_clzll((hi - lo) | 1), sh = bits > 10 ? bits - 10 : 0;
+      m.sub_n[t] = 0;
+      m.sub_w[t] = 0;
+      __syncthreads();
+      each(bin, lo, hi, [&](unsigned long long c, unsigned long long f) {
+        const unsigned s = (unsigned)((c - lo) >> sh);
+        atomicAdd(&m.sub_n[s], 1u);
+        atomicAdd(&m.sub_w[s], f);
+      });
+      if (t == 0) {
+        m.hit = SMP_THREADS;
+        m.last = -1;
+      }
+      __syncthreads();
+      const int s = SMP_SUB - 1 - t;  // from the front of the order on
+      const unsigned own_n = m.sub_n[s];
+      const unsigned long long own_w = m.sub_w[s];
+      unsigned n = own_n;
+      unsigned long long w = own_w;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const unsigned yn = __shfl_up(n, o, 64);
+        const unsigned long long yw = __shfl_up(w, o, 64);
+        if (lane >= o) {
+          n += yn;
+          w += yw;
+        }
+      }
+      if (lane == 63) {
+        m.red_n[wave] = n;
+        m.red_u[wave] = w;
+      }
+      __syncthreads();
+      n += m.base_n;
+      w += m.base_w;
+      for (int q = 0; q < wave; ++q) {
+        n += m.red_n[q];
+        w += m.red_u[q];
+      }
+      if (own_n > 0) {
+        if (rank ? n >= rank : (double)w >= want) atomicMin(&m.hit, t);
+        atomicMax(&m.last, t);
+      }
+      __syncthreads();
+      if (m.last < 0) break;
+      if (t == (m.hit < SMP_THREADS ? m.hit : m.last)) {
+        const unsigned long long at = lo + ((unsigned long long)s << sh), end = at + ((1ull << sh) - 1);
+        m.lo = at;
+        m.hi = end < at || end > hi ? hi : end;
+        m.base_n = n - own_n;
+        m.base_w = w - own_w;
+        m.kept_w = w;
+        m.part_n = own_n;
+      }
+      __syncthreads();
+      if (m.part_n == 1) {
+        each(bin, m.lo, m.hi, [&](unsigned long long c, unsigned long long) { m.found = c; });  // (one thread has it)
+        break;
+      }
+    }
+    __syncthreads();
+    return m.found;
+  };
+  // ---- what is kept: the bins in front of `cut_bin`, and of that one the tokens at `cut` or in front of it
+  int cut_bin = SMP_BINS;
+  unsigned long long cut = 0;
+  double partial = 0;  // sum of the latter
+  auto first_bin = [&](auto ok) {
+    __syncthreads();
+    if (t == 0) m.hit = SMP_BINS;
+    __syncthreads();
+    if (t < SMP_BINS && ok(t)) atomicMin(&m.hit, t);
+    __syncthreads();
+    return m.hit;
+  };
+  auto cut_at = [&](int bin, unsigned long long from, unsigned rank, double want) {
+    cut = last_kept(bin, from, rank, want);
+    cut_bin = bin;
+    partial = (double)m.kept_w * sample_eighths(bin);
+  };
+  if (r.k < V) {
+    const int h = first_bin([&](int i) { return m.through_n[i] >= r.k; });
+    if (h < SMP_BINS) {
+      if (m.through_n[h] == r.k) {
+        cut_bin = h + 1;
+        cut = ~0ull;
+      } else {
+        gather(m.through_n[h] <= SMP_LIST ? 0 : h, h);
+        cut_at(h, 0, (unsigned)(r.k - (h > 0 ? m.through_n[h - 1] : 0)), 0);
+      }
+    }
+  }
+  if (r.p < 1.f) {
+    const double want = (double)r.p * ((cut_bin > 0 ? m.through_w[cut_bin - 1] : 0) + partial);
+    const int h = first_bin([&](int i) { return i < cut_bin && m.through_w[i] >= want; });
+    const bool inside = h < SMP_BINS;
+    if (inside || (cut_bin < SMP_BINS && cut != ~0ull)) {
+      const int bin = inside ? h : cut_bin;
+      if (bin < listed0 || bin > listed1) gather(bin, bin);
+      cut_at(bin, inside ? 0 : cut, 0, (want - (bin > 0 ? m.through_w[bin - 1] : 0)) / sample_eighths(bin));
+    }
+  }
+  double w_least = LEAST_WEIGHT * w_top;
+  if (r.low > 0.f) {
+    const double d = first - floor(y_top + 8 * log2((double)r.low));
+    w_least = fmax(w_least, (double)r.low * w_top);
+    if (d < cut_bin) {
+      cut_bin = (int)d;
+      cut = 0;
+    }
+  }
+  auto kept = [&](unsigned long long f, int bin, unsigned long long c) {  // the token's weight, 0: not kept
+    const double w = (double)f * sample_eighths(bin);
+    return (bin < cut_bin || (bin == cut_bin && c >= cut)) && w >= w_least ? w : 0.0;
+  };
+  // ---- what is left of each chunk
+  __syncthreads();
+  for (int c = wave; c < C; c += SMP_WAVES) {
+    double s = 0;
+    for (int l = lane; l + m.shift[c] < (cut_bin < SMP_BINS ? cut_bin : SMP_BINS); l += 64)
+      s += (double)(hist[(size_t)c * SMP_HIST + l] & SMP_SUM_MASK) * sample_eighths(l + m.shift[c]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) m.chunk[c] = s;
+  }
+  if (cut_bin < SMP_BINS && cut != ~0ull)
+    each(cut_bin, cut, ~0ull, [&](unsigned long long c, unsigned long long f) {
+      if (kept(f, cut_bin, c) > 0.0) atomicAdd(&m.chunk_in[sample_index(c) / SMP_CHUNK], f);
+    });
+  __syncthreads();
+  double mine = lane < C ? m.chunk[lane] + (double)m.chunk_in[lane] * sample_eighths(cut_bin) : 0.0, ends = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(ends, o, 64);
+    if (lane >= o) ends += y;
+  }
+  const double total = __shfl(ends, 63, 64);
+  float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
+  u = u > 0.f ? fminf(u, 1.f) : 0.f;
+  const double want = (double)u * total;
+  const unsigned long long past = __ballot(mine > 0.0 && ends > want), some = __ballot(mine > 0.0);
+  if (wave == 0) m.before[lane] = ends - mine;
+  // ---- the token in the chunk (in the last chunk that has any where u is 1; a chunk whose sum is all of weights that count as none is passed over)
+  for (int c = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some | 1); c < C; ++c) {
+    if (!((some >> c) & 1)) continue;
+    constexpr int N = SMP_CHUNK / SMP_THREADS;
+    const int i0 = c * SMP_CHUNK + t * N;
+    double w[N], sum = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float v = i0 + j < V ? sample_logit<T>(x + i0 + j) : -INFINITY;
+      const double y = (double)v * r.rate, low = floor(y), d = first - low;
+      w[j] = v > -INFINITY && d < SMP_BINS ? kept(sample_factor(y - low), (int)d, sample_place(v, i0 + j)) : 0.0;
+      sum += w[j];
+    }
+    double run = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(run, o, 64);
+      if (lane >= o) run += y;
+    }
+    __syncthreads();
+    if (lane == 63) m.red_d[wave] = run;
+    if (t == 0) {
+      m.where = 0x7fffffff;
+      m.last = -1;
+    }
+    __syncthreads();
+    run = (run - sum) + m.before[c];
+    for (int q = 0; q < wave; ++q) run += m.red_d[q];
+    int hit = 0x7fffffff, last = -1;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      run += w[j];
+      if (w[j] > 0.0) {
+        last = i0 + j;
+        if (run > want && hit == 0x7fffffff) hit = i0 + j;
+      }
+    }
+    if (hit != 0x7fffffff) atomicMin(&m.where, hit);
+    if (last >= 0) atomicMax(&m.last, last);
+    __syncthreads();
+    const int id = m.where != 0x7fffffff ? m.where : m.last;
+    if (id < 0) continue;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (i0 + j == id) {
+        a.ids[b] = id;
+        if (a.prob) a.prob[b] = (float)(w[j] / total);
+      }
+    return;
+  }
+  if (t == 0) {  // (not reached: the largest token is always kept)
+    a.ids[b] = sample_index(best);
+    if (a.prob) a.prob[b] = 1.f;
   }
 }
 
@@ -145,28 +509,45 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
 
 using namespace la;
 
+static size_t sample_best_bytes(int B, int chunks) { return ((size_t)B * chunks * 8 + 15) / 16 * 16; }
 extern "C" size_t la_sample_workspace(int B, int V) {
-  (void)B; (void)V;
-  return 0;
+  if (B < 1 || V < 1 || V > LA_MAX_SAMPLE_VOCAB) return 0;  // (what the call itself refuses)
+  const int chunks = ceil_div(V, SMP_CHUNK);
+  return sample_best_bytes(B, chunks) + (size_t)B * chunks * SMP_HIST * 8;
+}
+
+template <typename T>
+static int sample_launch(const Sample &a, int B, hipStream_t s) {
+  {
+    ProfScope ps("sample_sum", s);
+    sample_sum_kernel<T><<<dim3(a.chunks, B), SMP_SUM_THREADS, 0, s>>>(a);
+  }
+  {
+    ProfScope ps("sample", s);
+    sample_kernel<T><<<B, SMP_THREADS, 0, s>>>(a);
+  }
+  LA_HIP(hipGetLastError());
+  return LA_OK;
 }
 
 extern "C" int la_sample(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_sampling *how, int32_t *ids, float *prob, void *workspace,
                          size_t workspace_bytes, void *stream) {
   LA_REQUIRE(how != nullptr, LA_EINVAL, "NULL argument");
-  LA_REQUIRE(B >= 0, LA_EINVAL, "B=%d is negative", B);
+  LA_REQUIRE(B >= 0 && B <= 65535, LA_EINVAL, "B=%d outside [0, 65535]", B);
   if (B == 0) return LA_OK;
   LA_REQUIRE(logits && ids && how->u, LA_EINVAL, "NULL argument");
   LA_REQUIRE(dtype == LA_F32 || dtype == LA_BF16 || dtype == LA_F16, LA_EINVAL, "unknown dtype %d", dtype);
   LA_REQUIRE(V >= 1 && V <= LA_MAX_SAMPLE_VOCAB, LA_EINVAL, "vocab %d outside [1, %d]", V, LA_MAX_SAMPLE_VOCAB);
   LA_REQUIRE(row_stride >= V || B == 1, LA_EINVAL, "rows overlap");
   LA_REQUIRE(how->n_u >= (how->u_index ? 1 : B), LA_EINVAL, "%d random numbers for %d rows", how->n_u, B);
-  (void)workspace; (void)workspace_bytes;
+  const size_t need = la_sample_workspace(B, V);
+  LA_REQUIRE(workspace && workspace_bytes >= need, LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  LA_REQUIRE((uintptr_t)workspace % 16 == 0, LA_EINVAL, "workspace must be 16-byte aligned");
   hipStream_t s = (hipStream_t)stream;
-  const Sample a{logits, row_stride, V, *how, ids, prob};
-  ProfScope ps("sample", s);
-  if (dtype == LA_F32) sample_kernel<float><<<B, SMP_THREADS, 0, s>>>(a);
-  else if (dtype == LA_F16) sample_kernel<_Float16><<<B, SMP_THREADS, 0, s>>>(a);
-  else sample_kernel<uint16_t><<<B, SMP_THREADS, 0, s>>>(a);
-  LA_HIP(hipGetLastError());
-  return LA_OK;
+  const int chunks = ceil_div(V, SMP_CHUNK);
+  const Sample a{logits, row_stride, V, chunks, *how, ids, prob, (unsigned long long *)workspace,
+                 (unsigned long long *)((char *)workspace + sample_best_bytes(B, chunks))};
+  if (dtype == LA_F32) return sample_launch<float>(a, B, s);
+  if (dtype == LA_F16) return sample_launch<_Float16>(a, B, s);
+  return sample_launch<uint16_t>(a, B, s);
 }
