@@ -313,6 +313,16 @@ int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_
                     int64_t table_stride, int n_requests, int max_blocks, const int32_t *req, const int32_t *pos, int B, void *out, int64_t out_stride,
                     void *workspace, size_t workspace_bytes, void *stream);
 
+/* Runs one token each of up to LA_MAX_ROWS rows of several requests through layers [layer_begin, layer_end), in place, as la_forward_layers runs a block of one:
+ * per layer RMSNorm, QKV projection, RoPE at pos[b], write of the row's K and V to slot[b] (negative: not written), la_paged_attend over positions 0 .. pos[b] of request
+ * req[b] (NULL: request b), output projection + residual, RMSNorm, SwiGLU MLP + residual.  hidden: device float [B, d], 16-byte aligned; pos, req, slot, table: as
+ * la_page_map leaves them (rows of pos -1 see nothing, and what becomes of their hidden states is of no use).  pages: n_layers >= layer_end, heads and dtype of
+ * the model; head_dim a multiple of 8.  Rows of one request in one call see each other's keys up to their own positions.
+ * The model's first call allocates scratch memory that stays with it (of a few MB, on the matrix-core path that of a short prompt beside it), also where it is captured.
+ * LA_EINVAL: B not in 1..LA_MAX_ROWS, pages of another shape or type, the LDS-ring kernel's weight layout; LA_ERANGE: layer range; LA_ENOMEM. */
+int la_forward_paged(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const int32_t *req, const int32_t *slot,
+                     const la_pages_desc *pages, const int32_t *table, int64_t table_stride, int n_requests, int max_blocks, void *stream);
+
 /* ---- n-gram pool and acceptance (Section 4.3) ----------------------------------------- */
 
 /* Pool keyed by token id: per key at most G distinct (N-1)-token continuations, refreshed

@@ -72,7 +72,7 @@ EXPORTS = [
     "la_init_model", "la_model_set_layer", "la_free_model", "la_kv_alloc", "la_kv_set_len", "la_kv_get_len",
     "la_kv_fill", "la_kv_read", "la_free_kv", "la_embed", "la_forward_layers", "la_unembed_argmax",
     "la_unembed_argmax_noalloc", "la_unembed_logits", "la_sample", "la_sample_workspace", "la_page_map", "la_paged_write", "la_paged_attend",
-    "la_paged_attend_workspace", "la_causal_layout", "la_set_barrier_timeout",
+    "la_paged_attend_workspace", "la_forward_paged", "la_causal_layout", "la_set_barrier_timeout",
     "la_prefill", "la_jacobi_init", "la_jacobi_accept", "la_rtt_fixed_overhead", "la_rtt_project", "la_jacobi_project",
     "la_pool_alloc", "la_free_pool", "la_state_init", "la_ngram_accept", "la_lookahead_layout",
     "la_profile_enable", "la_profile_select", "la_profile_read", "la_profile_copy", "la_last_error",
@@ -107,6 +107,7 @@ def _load():
         "la_paged_write": (i32, [vp, i32, vp, vp, i64, i64, vp, i32, vp]),
         "la_paged_attend_workspace": (C.c_size_t, [vp, i32, i32, i32]),
         "la_paged_attend": (i32, [vp, i32, vp, i64, i32, f32, vp, i64, i32, i32, vp, vp, i32, vp, i64, vp, C.c_size_t, vp]),
+        "la_forward_paged": (i32, [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i64, i32, i32, vp]),
         "la_pool_alloc": (i32, [i32, i32, i32, C.POINTER(vp)]),
         "la_free_pool": (None, [vp]),
         "la_state_init": (i32, [vp, vp, C.POINTER(la_lookahead_desc), vp, i32, i32, i32, vp, vp]),
@@ -372,6 +373,16 @@ def la_paged_attend(pages, layer, q, table, req, pos, out, scale=None, stream=No
     _check(lib.la_paged_attend(pages.ref, layer, qp, ldq, Hq, pages.head_dim ** -0.5 if scale is None else scale, tp, ld, R, blocks,
                                None if req is None else _array(req, "req", i32, (B,), device), _array(pos, "pos", i32, (B,), device), B, op, ldo,
                                ws.data_ptr() if size else None, size, _stream(stream)))
+
+
+def la_forward_paged(model, layer_begin, layer_end, hidden, pos, req, slot, pages, table, stream=None):
+    """One token each of several requests through the layers: hidden float32 [B, d_model] in place, pos, req (None: row b is request b), slot int32 [B]."""
+    device, i32 = _here(pages, "pages"), torch.int32
+    n = (hidden.shape[0],)
+    _need(hidden.dtype is torch.float32 and hidden.dim() == 2, "hidden: need float32 [B, d_model]")
+    tp, ld, R, blocks = _table(table, device)
+    _check(lib.la_forward_paged(model, layer_begin, layer_end, _ptr(hidden), n[0], _array(pos, "pos", i32, n, device), None if req is None else _array(req, "req", i32, n, device),
+                                _array(slot, "slot", i32, n, device), pages.ref, tp, ld, R, blocks, _stream(stream)))
 
 
 def la_pool_alloc(vocab, N, G):

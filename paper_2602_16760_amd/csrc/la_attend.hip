@@ -28,6 +28,8 @@ struct PagedAttend {
   void *out;
   int64_t ldo;
   int target;    // items that all keys together are cut into, about; 0: every row is one item
+  int q_tiles;   // > 0: q lies in operand fragments, [head][q_tiles][dh / 32][lane][8] of a 16-bit type; 0: rows
+  int kind;      // PagedOut
   int rec;       // floats of a head's record of an item: running maximum, sum, two of padding, dh sums
   float *part;   // [item][Hq][rec]
 };
@@ -124,6 +126,16 @@ __device__ __forceinline__ at_f4 at_mma(at_u4 x, at_u4 y, at_f4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(at_b8, x), __builtin_bit_cast(at_b8, y), c, 0, 0, 0);
 }
 
+// A value of the output where a model's next product wants it (the fragments' type takes +-65504 at most).
+__device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int col, float y) {
+  if (a.kind == AT_OUT_FLOAT) {
+    ((float *)a.out)[b * a.ldo + col] = y;
+  } else {
+    _Float16 *to = (_Float16 *)a.out + (((size_t)(col >> 5) * a.q_tiles + (b >> 4)) * 64 + (b & 15) + 16 * ((col & 31) >> 3)) * 8 + (col & 7);
+    *to = (_Float16)fminf(fmaxf(y, -65504.f), 65504.f);
+  }
+}
+
 // A workgroup takes an item's keys for one kv head and up to 16 of its query heads; its waves take blocks of KEYS keys in turn and meet once, at the end.
 // Scores are formed as K q^T (a lane holds one query head's scores of four keys of each 16-key tile), the output as V^T p^T: the contraction runs over the
 // keys in the order in which the lanes hold the scores, so the probabilities go from one product into the other without leaving their lanes.  V's operand
@@ -152,11 +164,12 @@ __global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_ker
   // this lane's query head as an operand column
   at_u4 q[KP];
   {
-    const char *qp = (const char *)a.q + (it.b * a.ldq + (int64_t)(head0 + (c16 < rows ? c16 : 0)) * dh) * E;
+    const int head = head0 + (c16 < rows ? c16 : 0);
+    const char *qp = (const char *)a.q + (a.q_tiles ? (((int64_t)head * a.q_tiles + (it.b >> 4)) * (dh / 32) * 64 + (it.b & 15)) * 16 : (it.b * a.ldq + (int64_t)head * dh) * E);
 #pragma unroll
     for (int i = 0; i < KP; ++i) {
       const int at = 64 * i + 16 * q4;
-      q[i] = FULL || at < dh * E ? *(const at_u4 *)(qp + at) : at_u4{0, 0, 0, 0};
+      q[i] = FULL || at < dh * E ? *(const at_u4 *)(qp + (a.q_tiles ? 1024 * i + 256 * q4 : at)) : at_u4{0, 0, 0, 0};
     }
   }
   const float to_log2 = a.scale * AT_LOG2E;
@@ -402,6 +415,11 @@ __global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_ker
     for (int e = 0; e < 4; ++e) {
       const int ch = 16 * VC * u + VC * (4 * q4 + e);
       if (!FULL && ch >= dh) continue;
+      if (a.kind != AT_OUT_ROWS) {
+#pragma unroll
+        for (int w = 0; w < VC; ++w) at_store_row(a, it.b, head * dh + ch + w, o[u * VC + w][e] * inv);
+        continue;
+      }
       unsigned y[VW / 4];
 #pragma unroll
       for (int w = 0; w < VW / 4; ++w) {
@@ -451,6 +469,10 @@ __global__ __launch_bounds__(AT_THREADS) void paged_join_kernel(PagedAttend a) {
     if (ch >= a.dh) break;
     for (int w = 0; w < AT_WAVES - 1; ++w) acc[c] += sums[w][ch];
     const float y = acc[c] * inv;
+    if (a.kind != AT_OUT_ROWS) {
+      at_store_row(a, it.b, head * a.dh + ch, y);
+      continue;
+    }
     T *to = (T *)a.out + it.b * a.ldo + (int64_t)head * a.dh + ch;
     if constexpr (sizeof(T) == 4) *to = y;
     else *(uint16_t *)to = (uint16_t)at_pack<T>(y, 0.f);
@@ -510,6 +532,24 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   return sized(std::integral_constant<int, 256>{});
 }
 
+static int at_run(const PagedAttend &a, int dtype, const AtPlan &plan, hipStream_t s) {
+  if (dtype == LA_F32) return at_launch<float>(a, plan, s);
+  if (dtype == LA_F16) return at_launch<_Float16>(a, plan, s);
+  return at_launch<uint16_t>(a, plan, s);
+}
+
+size_t paged_attend_bytes(const la_pages_desc &p, int Hq, int B) { return at_plan(p, Hq, 0x7fffffff / p.page_size, B).bytes; }
+
+int paged_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_tiles, int Hq, float scale, const PagedRows &r, PagedOut kind, void *out, void *workspace,
+                      hipStream_t s) {
+  const size_t at = layer * layer_bytes(&p);
+  const int64_t ld = (int64_t)Hq * p.head_dim;
+  const AtPlan plan = at_plan(p, Hq, r.max_blocks, r.B);
+  const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, ld, Hq, scale, r.table, r.ldt,
+                      r.n_req, r.max_blocks, r.req, r.pos, r.B, out, ld, plan.target, q_tiles, kind, p.head_dim + 4, (float *)workspace};
+  return at_run(a, p.dtype, plan, s);
+}
+
 }  // namespace la
 
 using namespace la;
@@ -541,8 +581,6 @@ extern "C" int la_paged_attend(const la_pages_desc *pages, int layer, const void
   hipStream_t s = (hipStream_t)stream;
   const size_t at = layer * layer_bytes(&p);
   const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride,
-                      n_requests, max_blocks, req, pos, B, out, out_stride, plan.target, p.head_dim + 4, (float *)workspace};
-  if (p.dtype == LA_F32) return at_launch<float>(a, plan, s);
-  if (p.dtype == LA_F16) return at_launch<_Float16>(a, plan, s);
-  return at_launch<uint16_t>(a, plan, s);
+                      n_requests, max_blocks, req, pos, B, out, out_stride, plan.target, 0, AT_OUT_ROWS, p.head_dim + 4, (float *)workspace};
+  return at_run(a, p.dtype, plan, s);
 }

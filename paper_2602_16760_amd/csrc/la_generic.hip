@@ -6,6 +6,7 @@
 
 #include "la_device.h"
 #include "la_internal.h"
+#include "la_paged.h"
 #include "la_plain.h"
 
 namespace la {
@@ -207,6 +208,25 @@ __global__ void rope_kvwrite_kernel(float *qkv, int Hq, int Hkv, int dh, const f
   }
   for (int e = threadIdx.x; e < nkv; e += blockDim.x)
     store_from_float<T>(Vc + (size_t)(L + b) * nkv + e, row[nq + nkv + e]);
+}
+
+// The same for rows of several requests: q goes to rows of the pages' type, K and V to the row's slot (none: nowhere).
+template <typename T>
+__global__ __launch_bounds__(256) void rope_pages_kernel(const float *qkv, int Hq, int Hkv, int dh, const float *cs, T *q, T *Kp, T *Vp, int page, int n_pages, const int32_t *slot) {
+  const int b = blockIdx.x, half = dh / 2, nq = Hq * dh, nkv = Hkv * dh, s = slot[b], pg = s / page;
+  const bool in = s >= 0 && pg < n_pages;
+  const float *row = qkv + (size_t)b * (nq + 2 * nkv);
+  auto at = [&](int h) { return (((size_t)pg * Hkv + h) * page + (s - pg * page)) * dh; };
+  for (int e = threadIdx.x; e < (Hq + Hkv) * half; e += blockDim.x) {
+    const int hd = e / half, i = e - hd * half;
+    if (hd >= Hq && !in) continue;
+    const float c = cs[((size_t)b * half + i) * 2], sn = cs[((size_t)b * half + i) * 2 + 1], x0 = row[hd * dh + i], x1 = row[hd * dh + i + half];
+    T *to = hd < Hq ? q + (size_t)b * nq + hd * dh : Kp + at(hd - Hq);
+    store_from_float<T>(to + i, x0 * c - x1 * sn);
+    store_from_float<T>(to + i + half, x1 * c + x0 * sn);
+  }
+  if (in)
+    for (int e = threadIdx.x; e < nkv; e += blockDim.x) store_from_float<T>(Vp + at(e / dh) + e % dh, row[nq + nkv + e]);
 }
 
 // One workgroup per (row b, query head): online softmax over the visible keys in chunks of blockDim.x keys, a key per
@@ -501,6 +521,36 @@ int generic_forward(la_model *m, int lb, int le, float *hidden, int Bp, const in
   if (m->d.dtype == LA_F32) return forward_t<float>(m, lb, le, hidden, Bp, pos, vis, kv, s);
   if (m->d.dtype == LA_F16) return forward_t<_Float16>(m, lb, le, hidden, Bp, pos, vis, kv, s);
   return forward_t<uint16_t>(m, lb, le, hidden, Bp, pos, vis, kv, s);
+}
+
+// One token each of several requests through the general products (norms, SwiGLU and residual sums are parts of them), RoPE and pages, and the paged attention.
+template <typename T>
+static int forward_paged_t(la_model *m, int lb, int le, float *hidden, const PagedRows &r, const la_pages_desc &pages, void *q, void *workspace, hipStream_t s) {
+  const la_model_desc &d = m->d;
+  const int nqkv = m->nqkv(), qd = m->qdim(), F = d.d_ffn, dm = d.d_model, B = r.B;
+  la_kv always{};  // (the products that add look at a length: there is no cache that this block could not fit)
+  always.L_dev = m->zero_len;
+  always.max_len = LA_MAX_ROWS;
+  int rc = launch_rope_table(m, r.pos, B, s);
+  for (int l = lb; !rc && l < le; ++l) {
+    const GenericLayer &w = m->layers[l];
+    if ((rc = gemm<T>("gemm_qkv", hidden, dm, w.g_attn, d.rms_eps, w.wqkv, nqkv, m->qkv, nqkv, B, dm, nqkv, nullptr, false, s))) return rc;
+    {
+      ProfScope p("rope_pages", s);
+      rope_pages_kernel<T><<<B, 256, 0, s>>>(m->qkv, d.n_q_heads, d.n_kv_heads, d.head_dim, m->rope_cs, (T *)q, (T *)((char *)pages.k + l * layer_bytes(&pages)),
+                                             (T *)((char *)pages.v + l * layer_bytes(&pages)), pages.page_size, pages.n_pages, r.slot);
+    }
+    if ((rc = paged_attend_rows(pages, l, q, 0, d.n_q_heads, 1.0f / sqrtf((float)d.head_dim), r, AT_OUT_FLOAT, m->attn, workspace, s))) return rc;
+    if ((rc = gemm<T>("gemm_o", m->attn, qd, nullptr, 0.f, w.wo, dm, hidden, dm, B, qd, dm, &always, false, s))) return rc;
+    if ((rc = gemm<T>("gemm_gateup", hidden, dm, w.g_mlp, d.rms_eps, w.wgu, 2 * F, m->act, F, B, dm, F, nullptr, true, s))) return rc;
+    rc = gemm<T>("gemm_down", m->act, F, nullptr, 0.f, w.wdown, dm, hidden, dm, B, F, dm, &always, false, s);
+  }
+  return rc;
+}
+int generic_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRows &r, const la_pages_desc &pages, void *q, void *workspace, hipStream_t s) {
+  if (m->d.dtype == LA_F32) return forward_paged_t<float>(m, lb, le, hidden, r, pages, q, workspace, s);
+  if (m->d.dtype == LA_F16) return forward_paged_t<_Float16>(m, lb, le, hidden, r, pages, q, workspace, s);
+  return forward_paged_t<uint16_t>(m, lb, le, hidden, r, pages, q, workspace, s);
 }
 
 // A prompt through the small layers' launches, PL_PROMPT rows at a time: every row is summed as it is in a block, in one launch instead of one for each 64

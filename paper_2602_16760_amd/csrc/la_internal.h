@@ -66,6 +66,8 @@ struct la_model {
   int32_t *pf_pos = nullptr;
   uint64_t *pf_vis = nullptr;
   float *prompt = nullptr;  // generic_prefill_rows: scratch of a prompt's rows
+  uint8_t *paged = nullptr;  // la_forward_paged: q rows or staged K and V rows, and the attention's workspace
+  int32_t *zero_len = nullptr;  // a cache length of 0 (plain path)
   la::MfmaModel *mf = nullptr;
   // Errors raised by kernels (a block that does not fit the cache: 1; a grid barrier that gave up: 4).  err_dev is the
   // device word the kernels OR into (the caches of this model alias it); err_host is one word of mapped pinned host
@@ -119,6 +121,9 @@ int generic_forward(la_model *m, int lb, int le, float *hidden, int Bp, const in
                     const uint64_t *vis, la_kv *kv, hipStream_t s);
 int generic_unembed_argmax(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2,
                            hipStream_t s);
+struct PagedRows;  // (la_paged.h)
+int generic_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRows &r, const la_pages_desc &pages, void *q, void *workspace, hipStream_t s);
+int mfma_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRows &r, const la_pages_desc &pages, void *stage_k, void *stage_v, void *workspace, hipStream_t s);
 int generic_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int ldl, hipStream_t s);
 int generic_prefill_rows(la_model *m, const la_kv *kv, int n, int *rows);  // of a chunk of an n-token prompt, scratch allocated; 0: by la_forward_layers
 int generic_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0, hipStream_t s);

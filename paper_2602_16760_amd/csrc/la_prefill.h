@@ -13,6 +13,7 @@
 // Both operands of the products are MFMA fragments of 1 KB: the activations are stored as [k-tile][row tile][lane][8
 // halves] by their producers, and a weight fragment is the 1 KB block of the per-CU streams the block kernel reads.
 #pragma once
+#include "la_paged.h"
 #include "la_prefill_plan.h"
 
 namespace la {
@@ -860,6 +861,42 @@ int mfma_prefill_rows(la_model *m, int n, int *rows) {
   return rc;
 }
 
+// A product of layer l: 0 QKV, 1 O, 2 gate/up, 3 down (its rows' rotations, cache and start are the caller's).
+static PfGemm pf_gemm_args(const la_model *m, int l, int gi, const uint16_t *A, const PfBuffers &b, int RT, int M) {
+  const MfmaModel *f = m->mf;
+  const la_model_desc &d = m->d;
+  const GemmPlan *plans[4] = {&f->p_qkv, &f->p_o, &f->p_gu, &f->p_down};
+  PfGemm p{};
+  p.wstream = f->wstream;
+  p.cu_bytes = f->cu_bytes;
+  p.frag0 = (unsigned)l * f->seg_frags;
+  p.G = f->n_wgs;
+  p.NW = R_NW;
+  p.n_prev = gi;
+  for (int i = 0; i < gi; ++i) {
+    p.prev_ntiles[i] = plans[i]->ntiles;
+    p.prev_KT[i] = plans[i]->KT;
+  }
+  p.ntiles = plans[gi]->ntiles;
+  p.KT = plans[gi]->KT;
+  p.A = A;
+  p.S = 1;
+  p.RT = RT;
+  p.M = M;
+  p.part = b.part;
+  p.d = d.d_model;
+  p.ss = b.ss;
+  p.inv_d = 1.0f / (float)d.d_model;
+  p.eps = d.rms_eps;
+  p.Q = b.Q;
+  p.Hq = d.n_q_heads;
+  p.Hkv = d.n_kv_heads;
+  p.dh = d.head_dim;
+  p.f16 = d.dtype == LA_F16;
+  p.act = b.act;
+  return p;
+}
+
 // One prompt chunk of M tokens (as many as mfma_prefill_rows says at most) at positions L0 .. L0 + M - 1 through every layer (the caller sets the cache
 // length afterwards).
 int mfma_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0, hipStream_t s) {
@@ -874,42 +911,14 @@ int mfma_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0
     pf_embed_kernel<<<M, 256, 0, s>>>((const uint16_t *)m->embed, tok, d.vocab, d.d_model, f16, b.x, b.cs, half, L0, (double)d.rope_theta, kv->L_dev);
   }
   LA_HIP(hipGetLastError());
-  const GemmPlan *plans[4] = {&f->p_qkv, &f->p_o, &f->p_gu, &f->p_down};
   int S_down = 0;  // slices of the products that x has not taken in yet
   for (int l = 0; l < d.n_layers; ++l) {
     auto gemm_args = [&](int gi, const uint16_t *A) {
-      PfGemm p{};
-      p.wstream = f->wstream;
-      p.cu_bytes = f->cu_bytes;
-      p.frag0 = (unsigned)l * f->seg_frags;
-      p.G = f->n_wgs;
-      p.NW = R_NW;
-      p.n_prev = gi;
-      for (int i = 0; i < gi; ++i) {
-        p.prev_ntiles[i] = plans[i]->ntiles;
-        p.prev_KT[i] = plans[i]->KT;
-      }
-      p.ntiles = plans[gi]->ntiles;
-      p.KT = plans[gi]->KT;
-      p.A = A;
-      p.S = 1;
-      p.RT = RT;
-      p.M = M;
-      p.part = b.part;
-      p.d = d.d_model;
-      p.ss = b.ss;
-      p.inv_d = 1.0f / (float)d.d_model;
-      p.eps = d.rms_eps;
+      PfGemm p = pf_gemm_args(m, l, gi, A, b, RT, M);
       p.cs = b.cs;
       p.Kc = (uint16_t *)kv->K + (size_t)l * kv->layer_elems();
       p.Vc = (uint16_t *)kv->V + (size_t)l * kv->layer_elems();
-      p.Q = b.Q;
       p.L0 = L0;
-      p.Hq = d.n_q_heads;
-      p.Hkv = d.n_kv_heads;
-      p.dh = d.head_dim;
-      p.f16 = f16;
-      p.act = b.act;
       return p;
     };
     const bool last = l + 1 == d.n_layers;  // its K and V rows are all that anybody reads: the pass ends with them
@@ -929,6 +938,65 @@ int mfma_prefill_chunk(la_model *m, la_kv *kv, const int32_t *tok, int M, int L0
   }
   LA_HIP(hipGetLastError());
   return LA_OK;
+}
+
+// ---- one token each of several requests ------------------------------------------------------------------
+// Rows of a block's cache, V key-blocked, into the slots of a layer's pages: a thread per eight channels of K and of V.
+__global__ __launch_bounds__(256) void unstage_kernel(const uint16_t *K, const uint16_t *V, uint16_t *Kp, uint16_t *Vp, const int32_t *slot, int n, int Hkv, int dh, int page,
+                                                      int n_pages) {
+  const int per_head = dh >> 3, i = blockIdx.x * 256 + (int)threadIdx.x, row = i / (Hkv * per_head), rest = i - row * Hkv * per_head, h = rest / per_head, c = 8 * (rest - h * per_head);
+  if (row >= n) return;
+  const int s = slot[row], pg = s / page;
+  if (s < 0 || pg >= n_pages) return;
+  const size_t to = (((size_t)pg * Hkv + h) * page + (s - pg * page)) * dh + c;
+  *(u32x4 *)(Kp + to) = *(const u32x4 *)(K + ((size_t)row * Hkv + h) * dh + c);
+  u32x4 v;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    v[j] = (unsigned)V[v_index(true, row, h, c + 2 * j, Hkv, dh)] | (unsigned)V[v_index(true, row, h, c + 2 * j + 1, Hkv, dh)] << 16;
+  *(u32x4 *)(Vp + to) = v;
+}
+
+// The prompt pass's launches with the rows' own positions: the QKV product leaves K and V as a block's cache (stage_k, stage_v), from which they go to their slots, and the
+// paged attention takes the causal one's place, from and to the same operand fragments.
+int mfma_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRows &r, const la_pages_desc &pages, void *stage_k, void *stage_v, void *workspace, hipStream_t s) {
+  MfmaModel *f = m->mf;
+  const la_model_desc &d = m->d;
+  LA_REQUIRE(f->use_r, LA_EINVAL, "la_forward_paged reads the register-streaming kernel's weight layout");
+  int rc = LA_OK;
+  if (!f->pf.base && !f->pf_few.base) rc = pf_alloc(m, PF_LONG, PF_LONG, f->pf_few);
+  if (rc) return rc;
+  PfBuffers &b = pf_buffers(f);
+  LA_REQUIRE(b.base != nullptr, LA_ENOMEM, "no memory for the products' buffers");
+  const int M = r.B, RT = LA_MAX_ROWS / 16;
+  if ((rc = launch_rope_table(m, r.pos, M, s))) return rc;
+  int S_down = 0;
+  for (int l = lb; l < le; ++l) {
+    auto args = [&](int gi, const uint16_t *A) {
+      PfGemm p = pf_gemm_args(m, l, gi, A, b, RT, M);
+      p.cs = m->rope_cs;
+      p.Kc = (uint16_t *)stage_k;
+      p.Vc = (uint16_t *)stage_v;
+      return p;
+    };
+    int S_o = 0;
+    if ((rc = pf_launch_norm(S_down, hidden, b.part, m->layers[l].g_attn, M, d.d_model, RT, b.ss, b.A, s))) return rc;
+    if ((rc = pf_launch_gemm<PF_QKV>(args(0, b.A), s, "pf_gemm_qkv", f->n_wgs))) return rc;
+    {
+      ProfScope ps("unstage", s);
+      unstage_kernel<<<ceil_div(M * d.n_kv_heads * (d.head_dim / 8), 256), 256, 0, s>>>((const uint16_t *)stage_k, (const uint16_t *)stage_v,
+                                                                                      (uint16_t *)((char *)pages.k + l * layer_bytes(&pages)),
+                                                                                      (uint16_t *)((char *)pages.v + l * layer_bytes(&pages)), r.slot, M, d.n_kv_heads,
+                                                                                      d.head_dim, pages.page_size, pages.n_pages);
+    }
+    if ((rc = paged_attend_rows(pages, l, b.Q, RT, d.n_q_heads, 1.f, r, AT_OUT_FRAGMENTS, b.attn, workspace, s))) return rc;
+    if ((rc = pf_launch_gemm<PF_PART>(args(1, b.attn), s, "pf_gemm_o", f->n_wgs, b.part_rows, &S_o))) return rc;
+    if ((rc = pf_launch_norm(S_o, hidden, b.part, m->layers[l].g_mlp, M, d.d_model, RT, b.ss, b.A, s))) return rc;
+    if ((rc = pf_launch_gemm<PF_GATEUP>(args(2, b.A), s, "pf_gemm_gateup", f->n_wgs))) return rc;
+    if ((rc = pf_launch_gemm<PF_PART>(args(3, b.act), s, "pf_gemm_down", f->n_wgs, b.part_rows, &S_down))) return rc;
+  }
+  // (the last down projection's sums go into the residual stream; what else this launch writes is not read)
+  return S_down ? pf_launch_norm(S_down, hidden, b.part, m->layers[le - 1].g_mlp, M, d.d_model, RT, b.ss, b.A, s) : LA_OK;
 }
 
 // ---- stored logits ------------------------------------------------------------------------------------

@@ -1,0 +1,189 @@
+"""Several requests at once: rows of them through the layers on pages, generation with shared pages, sampled generation."""
+import numpy as np
+import pytest
+import torch
+
+import synth
+from gpu_util import gpu_engine, launch_names, oracle_model, row_rel_err
+from oracle import transformer as otf
+
+pytestmark = pytest.mark.gpu
+BAR = {"f32": 1e-4, "bf16": 2e-2, "f16": 2e-3}
+
+
+def binding():
+    from paper_2602_16760_amd import binding as B
+    return B
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def bits(a, dtype):
+    """numpy rows of synth -> torch rows of the pages' type."""
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return t.view(torch.bfloat16) if dtype == "bf16" and t.dtype != torch.float32 else t.to(dict(f32=torch.float32, bf16=torch.bfloat16, f16=torch.float16)[dtype])
+
+
+@pytest.mark.parametrize("name,lens,page", [("tiny_f32", [0, 5, 47, 300], 16), ("small_bf16", [0, 1, 31, 33, 700], 16), ("small_bf16", list(range(3, 67)), 24),
+                                            ("small64_bf16", [100, 2], 8), ("small_f16", [64, 12, 1000], 32), ("small64_f16", [7] * 17, 16)])
+def test_forward_against_the_oracle(name, lens, page):
+    """A row per request, one of the batch padding: hidden states against the oracle's decode step of each request, K and V where the slots say."""
+    shape = synth.SHAPES[name]
+    eng, om, B = gpu_engine(shape, 64, head=False), oracle_model(shape, head=False), binding()
+    R, H, dh, dt = len(lens), shape.n_kv_heads, shape.head_dim, shape.dtype
+    try:
+        blocks = max(lens) // page + 1
+        n_pages = sum(n // page + 1 for n in lens)
+        order = np.random.default_rng(2).permutation(n_pages)
+        table = np.full((R, blocks), -1, dtype=np.int32)
+        k = torch.zeros((shape.n_layers, n_pages, H, page, dh), dtype=bits(np.zeros(1, np.float32), dt).dtype)
+        v, at, rows = torch.zeros_like(k), 0, []
+        for r, n in enumerate(lens):
+            u = n // page + 1
+            table[r, :u] = order[at:at + u]
+            at += u
+            okv = otf.KVCache(shape, n + 1)
+            for l in range(shape.n_layers):
+                if n:
+                    kk, vv = synth.kv_fill(shape, l, n, r)
+                    okv.fill(l, kk, vv)
+                    for dst, src in ((k, bits(kk, dt)), (v, bits(vv, dt))):
+                        for b in range(u):
+                            part = src[b * page:(b + 1) * page]
+                            dst[l, table[r, b], :, :len(part)] = part.transpose(0, 1)
+            okv.L = n
+            rows.append(okv)
+        x = synth.hidden_block(shape, R, 0)
+        pad = min(3, R)
+        B_rows = min(R + 1, 64)
+        req, pos = list(range(R)), list(lens)
+        slot = [int(table[r, n // page]) * page + n % page for r, n in enumerate(lens)]
+        if B_rows > R:
+            req.insert(pad, -1), pos.insert(pad, -1), slot.insert(pad, -1)
+            x = np.insert(x, pad, 1.0, axis=0)
+        pages = B.la_pages(k.cuda(), v.cuda())
+        before = pages.k.clone()
+        hidden = torch.from_numpy(x.astype(np.float32)).cuda()
+        run = lambda h: B.la_forward_paged(eng.model, 0, shape.n_layers, h, i32(pos), i32(req), i32(slot), pages, i32(table.tolist()))
+        used = launch_names(lambda: run(hidden.clone()))
+        assert {"paged_attend"} <= used and ("pf_gemm_qkv" in used) == (dt != "f32"), used
+        run(hidden)
+        got = hidden.cpu().numpy()
+        again = torch.from_numpy(x.astype(np.float32)).cuda()
+        run(again)
+        assert torch.equal(again, hidden)
+        touched = torch.zeros(pages.k.shape[1:4], dtype=torch.bool)
+        for i, r in enumerate(req):
+            if r < 0:
+                continue
+            want = otf.forward_block(om, rows[r], x[i:i + 1], [lens[r]], [1])
+            err = row_rel_err(got[i:i + 1], want).max()
+            assert err <= BAR[dt], f"request {r} of {lens[r]} positions: {err:.2e}"
+            p, c = slot[i] // page, slot[i] % page
+            touched[p, :, c] = True
+            for cache, theirs in ((pages.k, rows[r].K), (pages.v, rows[r].V)):
+                row = cache[shape.n_layers - 1, p, :, c].float().cpu().numpy()
+                ref = np.asarray(theirs[shape.n_layers - 1][lens[r]], dtype=np.float64).reshape(H, dh)
+                assert np.abs(row - ref).max() <= (BAR[dt] + 2.0 ** -8) * np.abs(ref).max()
+        assert torch.equal(pages.k.cpu()[:, ~touched], before.cpu()[:, ~touched])
+    finally:
+        eng.close()
+
+
+def test_forward_in_ranges_of_layers_and_without_a_row_map():
+    shape = synth.SHAPES["small_bf16"]
+    eng, B = gpu_engine(shape, 64, head=False), binding()
+    try:
+        mk = lambda: B.la_pages(*(torch.zeros((3, 6, 2, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+        table, pos, slot = i32([[4, 2], [1, 0], [3, 5]]), i32([0, 0, 0]), i32([64, 16, 48])
+        x = torch.from_numpy(synth.hidden_block(shape, 3, 1).astype(np.float32)).cuda()
+        a, b, pa, pb = x.clone(), x.clone(), mk(), mk()
+        B.la_forward_paged(eng.model, 0, 3, a, pos, i32([0, 1, 2]), slot, pa, table)
+        for l in range(3):
+            B.la_forward_paged(eng.model, l, l + 1, b, pos, None, slot, pb, table)
+        assert torch.equal(pa.k, pb.k) and torch.equal(pa.v, pb.v) and torch.equal(a, b)
+        B.la_forward_paged(eng.model, 1, 1, b, pos, None, slot, pb, table)
+        assert torch.equal(a, b)
+    finally:
+        eng.close()
+
+
+def greedy_is_the_oracles(shape, om, prompt, tokens, bar):
+    """Every emitted token is the oracle's choice behind the tokens in front of it, wherever its margin is clear of the bar."""
+    seq = np.concatenate([prompt, tokens]).astype(np.int64)
+    logits = otf.causal_forward(om, seq[:-1])[1][len(prompt) - 1:]
+    t1, t2 = otf.top2_margin(logits)
+    safe = (t1 - t2) > bar
+    assert np.array_equal(otf.argmax_ids(logits)[safe], tokens[safe])
+    return int(safe.sum())
+
+
+@pytest.mark.parametrize("name,margin", [("tiny_f32", 1e-3), ("small_bf16", 3e-2), ("small64_f16", 1e-2)])
+def test_batch_generation_against_the_oracle(name, margin):
+    shape = synth.SHAPES[name]
+    eng, om = gpu_engine(shape, 300, seed=1), oracle_model(shape, seed=1)
+    g = np.random.default_rng(5)
+    prompts = [g.integers(0, shape.vocab, size=n).astype(np.int32) for n in (1, 9, 16, 17, 90, 150)]
+    try:
+        tokens, st = eng.generate_batch(prompts, 20, page_size=16)
+        assert st["free_pages"] == st["pages"]
+        safe = sum(greedy_is_the_oracles(shape, om, p, t, margin) for p, t in zip(prompts, tokens))
+        assert safe >= 40, f"only {safe} of 120 tokens have a margin"
+        with pytest.raises(Exception) as e:
+            eng.generate_batch(prompts, 20, page_size=16, n_pages=st["pages"] - 1)
+        assert getattr(e.value, "code", None) == -3
+    finally:
+        eng.close()
+
+
+def test_batch_equals_each_request_alone_in_float32():
+    """The tiny decoder's rounding is far below its margins: the batch emits what sequential decoding emits, greedily and sampled."""
+    shape = synth.SHAPES["tiny_f32"]
+    eng = gpu_engine(shape, 200, seed=2)
+    g = np.random.default_rng(6)
+    prompts = [g.integers(0, shape.vocab, size=n).astype(np.int32) for n in (5, 40, 23)]
+    try:
+        tokens, _ = eng.generate_batch(prompts, 24, page_size=8)
+        for p, t in zip(prompts, tokens):
+            assert np.array_equal(eng.generate(p, 24, 0, 1, 0)[0], t)
+        u = g.random((24, 3)).astype(np.float32)
+        how = dict(temperature=0.8, top_k=30, top_p=0.9, min_p=0.02)
+        tokens, _ = eng.generate_batch(prompts, 24, page_size=8, sampling=dict(how, u=u))
+        for r, p in enumerate(prompts):
+            by_pos = np.zeros(200 + 1, dtype=np.float32)
+            by_pos[len(p) - 1:len(p) - 1 + 24] = u[:, r]
+            assert np.array_equal(eng.generate(p, 24, 0, 1, 0, sampling=dict(how, u=by_pos))[0], tokens[r])
+    finally:
+        eng.close()
+
+
+@pytest.mark.parametrize("name,W,N,G", [("tiny_f32", 4, 3, 4), ("tiny_f32", 5, 4, 5), ("tiny_f32", 1, 2, 1)])
+@pytest.mark.parametrize("how", [dict(temperature=0.7, top_k=8), dict(temperature=0.3, top_p=0.8), dict(temperature=0.0)])
+def test_sampled_lookahead_emits_what_sequential_sampling_emits(name, W, N, G, how):
+    """Random numbers go by position, so a candidate that its row draws is the token that sequential decoding would have drawn there; a low temperature confirms candidates."""
+    shape = synth.SHAPES[name]
+    eng = gpu_engine(shape, 400, seed=3)
+    prompt = np.tile(np.random.default_rng(7).integers(0, shape.vocab, size=12), 4).astype(np.int32)
+    try:
+        one, _ = eng.generate(prompt, 60, 0, 1, 0, sampling=dict(how, seed=11))
+        many, st = eng.generate(prompt, 60, W, N, G, sampling=dict(how, seed=11))
+        assert np.array_equal(one, many)
+        if how == dict(temperature=0.0):
+            assert np.array_equal(one, eng.generate(prompt, 60, W, N, G)[0])
+    finally:
+        eng.close()
+
+
+def test_sampling_parameters_are_checked():
+    eng = gpu_engine(synth.SHAPES["tiny_f32"], 64)
+    try:
+        with pytest.raises(TypeError):
+            eng.generate(np.array([1, 2, 3]), 4, 0, 1, 0, sampling=dict(heat=1.0))
+        with pytest.raises(ValueError):
+            eng.generate(np.array([1, 2, 3]), 4, 0, 1, 0, sampling=dict(u=[0.5]))
+        with pytest.raises(ValueError):
+            eng.generate_batch([], 4)
+    finally:
+        eng.close()
