@@ -8,15 +8,19 @@ namespace la {
 // an octave between its a and the row's largest, the second factor lies in [1, 1.091) and is rounded to 36 bits behind the point, wherever it is used.  Sums over a
 // bin are then sums of whole numbers: they do not depend on the order in which LDS atomics take them, and equal logits have equal shares.  Everything behind them
 // is added in a fixed order.  A sum of n weights is off by about 2^-38 / sqrt(n) of itself.  Bins reach 64 octaves down, below which a weight counts as none.
-constexpr int SMP_CHUNK = 8192;               // tokens of a workgroup of the first launch
 constexpr int SMP_BINS = 514, SMP_HIST = 520;  // (64 octaves below the largest token end in the 514th bin at the latest); row length of a chunk's sums
-constexpr int SMP_LIST = 4096;                // tokens of a bin that fit into LDS
+constexpr int SMP_SUM_THREADS = 512;          // of a workgroup of the first launch
+constexpr int SMP_PER = 16, SMP_PER_SHORT = 4;  // ... tokens of each: chunks of 8192 and of 2048
+constexpr int SMP_LIST = 5120;                // tokens of a cut that fit into LDS
 constexpr int SMP_SUB = 1024;                 // parts that a range of tokens is cut into at a time
 constexpr int SMP_COUNT_SHIFT = 50;           // a chunk's word of a bin: the number of its tokens above that bit, the sum of their factors below, in units of 2^-36
 constexpr unsigned long long SMP_SUM_MASK = (1ull << SMP_COUNT_SHIFT) - 1;
 constexpr double SMP_UNIT = 0x1p36, LEAST_WEIGHT = 0x1p-64;
-static_assert(SMP_CHUNK * 1.1 * SMP_UNIT < (double)SMP_SUM_MASK && SMP_CHUNK <= 1 << 13, "a chunk in one bin");
-static_assert(LA_MAX_SAMPLE_VOCAB * 1.1 * SMP_UNIT < 0x1p64 && LA_MAX_SAMPLE_VOCAB / SMP_CHUNK <= 64, "a row in one bin; a lane per chunk");
+constexpr int SMP_MOST = SMP_SUM_THREADS * SMP_PER;
+static_assert(SMP_MOST * 1.1 * SMP_UNIT < (double)SMP_SUM_MASK && SMP_MOST <= 1 << 13, "a chunk in one bin");
+static_assert(LA_MAX_SAMPLE_VOCAB * 1.1 * SMP_UNIT < 0x1p64 && LA_MAX_SAMPLE_VOCAB / SMP_MOST <= 64, "a row in one bin; a lane per chunk");
+// Short chunks while that leaves a row at most 16 of them: the first launch has four times the workgroups, the second reads as many sums.
+static int sample_per(int V) { return V <= 16 * SMP_SUM_THREADS * SMP_PER_SHORT ? SMP_PER_SHORT : SMP_PER; }
 
 struct Sample {
   const void *x;
@@ -25,8 +29,12 @@ struct Sample {
   la_sampling p;
   int32_t *ids;
   float *prob;
-  unsigned long long *best;  // [B][chunks] first token in order
-  unsigned long long *hist;  // [B][chunks][SMP_HIST]
+  // per row and chunk: its first token in order; sums of weights and numbers of tokens of the bins down to each [SMP_HIST], from that token's bin on; every token's bin from
+  // there on (255: further down, or no token), thread by thread
+  unsigned long long *best;
+  double *sums;
+  int32_t *counts;
+  uint8_t *bins;
 };
 
 // A logit as it counts: NaN like -inf (no token), +inf like the largest finite value, -0 like 0.
@@ -66,6 +74,13 @@ __device__ __forceinline__ double sample_eighths(int t) {  // 2^(-t / 8) units
   return ldexp(v * (1 / SMP_UNIT), -(t >> 3));
 }
 
+// What all threads have alike, as scalars: branches around barriers are then jumps, not masks.
+__device__ __forceinline__ int sample_uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ unsigned long long sample_uni(unsigned long long v) {
+  return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ double sample_uni(double v) { return __builtin_bit_cast(double, sample_uni(__builtin_bit_cast(unsigned long long, v))); }
+
 // How row b is sampled; the filters that are off are out of reach.
 struct SampleRow {
   bool greedy;
@@ -76,8 +91,8 @@ struct SampleRow {
 __device__ __forceinline__ SampleRow sample_row(const Sample &a, int b) {
   SampleRow r;
   const float t = a.p.temperature ? a.p.temperature[b] : 1.f;
-  r.greedy = !(t > 0.f);
-  r.rate = 8 * 1.44269504088896340736 / (double)t;
+  r.greedy = sample_uni(!(t > 0.f)) != 0;
+  r.rate = sample_uni(8 * 1.44269504088896340736 / (double)t);
   const int k = a.p.top_k ? a.p.top_k[b] : 0;
   r.k = k > 0 && k < a.V ? k : a.V;
   r.p = a.p.top_p ? a.p.top_p[b] : 1.f;
@@ -88,20 +103,25 @@ __device__ __forceinline__ SampleRow sample_row(const Sample &a, int b) {
   }
   r.low = a.p.min_p ? a.p.min_p[b] : 0.f;
   r.low = r.low > 0.f ? fminf(r.low, 1.f) : 0.f;
+  r.k = sample_uni(r.k);
+  r.p = __uint_as_float((unsigned)sample_uni((int)__float_as_uint(r.p)));
+  r.low = __uint_as_float((unsigned)sample_uni((int)__float_as_uint(r.low)));
   return r;
 }
 
 // First launch, a workgroup per chunk of a row: its first token in order, and its bins' sums, relative to that token's.
-constexpr int SMP_SUM_THREADS = 512;
-template <typename T>
+template <typename T, int PER>
 __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
-  constexpr int N = SMP_CHUNK / SMP_SUM_THREADS, WAVES = SMP_SUM_THREADS / 64;
-  __shared__ unsigned long long hist[SMP_HIST], red[WAVES];
-  const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, i0 = c * SMP_CHUNK + t;
+  constexpr int WAVES = SMP_SUM_THREADS / 64, CHUNK = SMP_SUM_THREADS * PER;
+  __shared__ __attribute__((aligned(16))) unsigned long long hist[SMP_HIST];
+  __shared__ unsigned long long red[WAVES];
+  __shared__ double red_w[WAVES];
+  __shared__ int red_n[WAVES];
+  const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, wave = t >> 6, lane = t & 63, i0 = c * CHUNK + t;
   const T *x = (const T *)a.x + b * a.ld;
-  float v[N];
+  float v[PER];
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
+  for (int j = 0; j < PER; ++j) {
     const int i = i0 + SMP_SUM_THREADS * j;
     v[j] = i < a.V ? sample_logit<T>(x + i) : -INFINITY;
   }
@@ -109,7 +129,7 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   for (int i = t; i < SMP_HIST; i += SMP_SUM_THREADS) hist[i] = 0;
   unsigned long long best = 0;
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
+  for (int j = 0; j < PER; ++j) {
     const unsigned long long at = sample_place(v[j], i0 + SMP_SUM_THREADS * j);
     best = at > best ? at : best;
   }
@@ -118,23 +138,65 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
     const unsigned long long y = __shfl_xor(best, o, 64);
     best = y > best ? y : best;
   }
-  if ((t & 63) == 0) red[t >> 6] = best;
+  if (lane == 0) red[wave] = best;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) best = red[w] > best ? red[w] : best;
+  best = sample_uni(best);
   const size_t at = (size_t)b * a.chunks + c;
   if (t == 0) a.best[at] = best;
   const float top = sample_value(best);
   if (r.greedy || !(top > -INFINITY)) return;
   const double first = floor((double)top * r.rate);
+  uint32_t code[(PER + 3) / 4] = {};
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const double y = (double)v[j] * r.rate, low = floor(y);
-    const double d = first - low;
-    if (v[j] > -INFINITY && d < SMP_BINS) atomicAdd(&hist[(int)d], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low));
+  for (int j = 0; j < PER; ++j) {
+    const double y = (double)v[j] * r.rate, low = floor(y), d = first - low;
+    const bool in = v[j] > -INFINITY && d < SMP_BINS;
+    const int bin = in ? (int)d : 255;
+    if (in) atomicAdd(&hist[bin], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low));
+    code[j / 4] |= (uint32_t)(bin < 255 ? bin : 255) << (8 * (j % 4));
+  }
+  uint32_t *codes = (uint32_t *)(a.bins + at * CHUNK) + t * (PER / 4);
+  if constexpr (PER == 16) *(uint4 *)codes = uint4{code[0], code[1], code[2], code[3]};
+  else *codes = code[0];
+  __syncthreads();
+  // sums from the front, two bins a thread
+  const bool own = 2 * t < SMP_HIST;
+  double w0 = 0, w1 = 0;
+  int n0 = 0, n1 = 0;
+  if (own) {
+    const unsigned long long h0 = hist[2 * t], h1 = hist[2 * t + 1];
+    w0 = (double)(h0 & SMP_SUM_MASK) * sample_eighths(2 * t);
+    w1 = (double)(h1 & SMP_SUM_MASK) * sample_eighths(2 * t + 1);
+    n0 = (int)(h0 >> SMP_COUNT_SHIFT);
+    n1 = (int)(h1 >> SMP_COUNT_SHIFT);
+  }
+  double w = w0 + w1;
+  int n = n0 + n1;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double yw = __shfl_up(w, o, 64);
+    const int yn = __shfl_up(n, o, 64);
+    if (lane >= o) {
+      w += yw;
+      n += yn;
+    }
+  }
+  if (lane == 63) {
+    red_w[wave] = w;
+    red_n[wave] = n;
   }
   __syncthreads();
-  for (int i = t; i < SMP_HIST; i += SMP_SUM_THREADS) a.hist[at * SMP_HIST + i] = hist[i];
+  if (!own) return;
+  double front_w = 0;
+  int front_n = 0;
+  for (int q = 0; q < wave; ++q) {
+    front_w += red_w[q];
+    front_n += red_n[q];
+  }
+  *(double2 *)(a.sums + at * SMP_HIST + 2 * t) = double2{front_w + (w - w1), front_w + w};
+  *(int2 *)(a.counts + at * SMP_HIST + 2 * t) = int2{front_n + n - n1, front_n + n};
 }
 
 // Second launch, a workgroup per row: where the filters cut, what is left of every chunk, and in the chunk where u falls the token.
@@ -147,7 +209,7 @@ struct SampleShared {
   int through_n[SMP_BINS];
   unsigned long long best[64], chunk_in[64];
   int shift[64];
-  double chunk[64], before[64];
+  double scale[64], before[64];
   double red_d[SMP_WAVES];
   unsigned long long red_u[SMP_WAVES];
   unsigned red_n[SMP_WAVES];
@@ -156,8 +218,9 @@ struct SampleShared {
   int hit, last, where;
 };
 
-template <typename T>
+template <typename T, int PER>
 __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
+  constexpr int CHUNK = SMP_SUM_THREADS * PER;
   __shared__ SampleShared m;
   const int b = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63, V = a.V, C = a.chunks;
   const T *x = (const T *)a.x + b * a.ld;
@@ -174,6 +237,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     const unsigned long long y = __shfl_xor(best, o, 64);
     best = y > best ? y : best;
   }
+  best = sample_uni(best);
   const float top = sample_value(best);
   if (r.greedy || !(top > -INFINITY)) {
     if (t == 0) {
@@ -186,53 +250,34 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   if (t < 64) {
     const double d = t < C ? first - floor((double)sample_value(m.best[t]) * r.rate) : (double)SMP_BINS;
     m.shift[t] = d < SMP_BINS ? (int)d : SMP_BINS;  // (a chunk without a token: NaN or infinite, and never looked at)
+    m.scale[t] = d < SMP_BINS ? sample_eighths((int)d) * SMP_UNIT : 0.0;
   }
   __syncthreads();
-  const unsigned long long *hist = a.hist + (size_t)b * C * SMP_HIST;
-  // ---- the row's bins, summed up from the largest weights on
-  {
+  const double *sums = a.sums + (size_t)b * C * SMP_HIST;
+  const int32_t *counts = a.counts + (size_t)b * C * SMP_HIST;
+  // ---- the row's sums down to each bin
+  if (t < SMP_BINS) {
     double w = 0;
     int n = 0;
-    if (t < SMP_BINS) {
 #pragma unroll 8
-      for (int c = 0; c < C; ++c) {
-        const int l = t - m.shift[c];
-        const unsigned long long h = l >= 0 ? hist[(size_t)c * SMP_HIST + l] : 0;
-        w += (double)(h & SMP_SUM_MASK);
-        n += (int)(h >> SMP_COUNT_SHIFT);
-      }
-      w *= sample_eighths(t);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double yw = __shfl_up(w, o, 64);
-      const int yn = __shfl_up(n, o, 64);
-      if (lane >= o) {
-        w += yw;
-        n += yn;
+    for (int c = 0; c < C; ++c) {
+      const int l = t - m.shift[c];
+      if (l >= 0) {
+        w += sums[c * SMP_HIST + l] * m.scale[c];
+        n += counts[c * SMP_HIST + l];
       }
     }
-    if (lane == 63) {
-      m.red_d[wave] = w;
-      m.red_n[wave] = n;
-    }
-    __syncthreads();
-    for (int q = 0; q < wave; ++q) {
-      w += m.red_d[q];
-      n += m.red_n[q];
-    }
-    if (t < SMP_BINS) {
-      m.through_w[t] = w;
-      m.through_n[t] = n;
-    }
-    if (t == 0) m.hit = SMP_BINS;
-    __syncthreads();
+    m.through_w[t] = w;
+    m.through_n[t] = n;
   }
+  __syncthreads();
   auto in_bins = [&](double y, int t0, int t1) { return y >= first - t1 && (t0 == 0 || y < first - t0 + 1); };
   int listed0 = SMP_BINS, listed1 = -1;            // bins whose tokens are in the list
   unsigned long long ends_lo = 0, ends_hi = ~0ull;  // no token of theirs lies outside
-  // Tokens of bins t0 .. t1 into the list, and their ends of the order (whether they fit or not).
+  // Tokens of bins t0 .. t1 into the list, if they fit, and the ends of their order.  The first launch's bytes say which tokens may be there (255: perhaps); only their logits
+  // are read, all at once.
   auto gather = [&](int t0, int t1) {
+    constexpr int N = 8, WORDS = PER / 4;
     __syncthreads();
     if (t == 0) {
       m.n_list = 0;
@@ -240,24 +285,52 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       m.hi = 0;
     }
     __syncthreads();
-    unsigned long long lo = ~0ull, hi = 0;
-    for (int i0 = 0; i0 < V; i0 += 8 * SMP_THREADS) {
-      float v[8];
+    const uint32_t *codes = (const uint32_t *)(a.bins + (size_t)b * C * CHUNK);
+    for (int s0 = t; s0 < C * SMP_SUM_THREADS; s0 += N * SMP_THREADS) {
+      uint32_t code[N][WORDS];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = i0 + t + SMP_THREADS * j;
-        v[j] = i < V ? sample_logit<T>(x + i) : -INFINITY;
+      for (int u = 0; u < N; ++u) {
+        const int s = s0 + u * SMP_THREADS < C * SMP_SUM_THREADS ? s0 + u * SMP_THREADS : s0;
+        if constexpr (PER == 16) {
+          const uint4 w = *(const uint4 *)(codes + (size_t)s * WORDS);
+          code[u][0] = w.x; code[u][1] = w.y; code[u][2] = w.z; code[u][3] = w.w;
+        } else {
+          code[u][0] = codes[s];
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = i0 + t + SMP_THREADS * j;
-        if (v[j] > -INFINITY && in_bins((double)v[j] * r.rate, t0, t1)) {
-          const unsigned long long c = sample_place(v[j], i);
-          lo = c < lo ? c : lo;
-          hi = c > hi ? c : hi;
-          const unsigned s = atomicAdd(&m.n_list, 1u);
-          if (s < SMP_LIST) m.list[s] = c;
+      for (int u = 0; u < N; ++u) {
+        const int s = s0 + u * SMP_THREADS, c = s / SMP_SUM_THREADS;
+        if (s >= C * SMP_SUM_THREADS) break;
+        const int shift = m.shift[c], lo = t0 > shift ? (t0 - shift < 255 ? t0 - shift : 255) : 0, hi = t1 - shift < 255 ? t1 - shift : 255;
+        if (hi < 0 || shift >= SMP_BINS) continue;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const unsigned bin = (code[u][j / 4] >> (8 * (j % 4))) & 255u;
+          if (bin - (unsigned)lo <= (unsigned)(hi - lo)) {
+            const unsigned at = atomicAdd(&m.n_list, 1u);
+            if (at < SMP_LIST) m.list[at] = (unsigned)(c * CHUNK + s % SMP_SUM_THREADS + SMP_SUM_THREADS * j);
+          }
         }
+      }
+    }
+    __syncthreads();
+    const int n = sample_uni((int)m.n_list);
+    listed0 = n <= SMP_LIST ? t0 : SMP_BINS;
+    listed1 = n <= SMP_LIST ? t1 : -1;
+    ends_lo = 0;
+    ends_hi = ~0ull;
+    if (n > SMP_LIST) return;
+    unsigned long long lo = ~0ull, hi = 0;
+    for (int i = t; i < n; i += SMP_THREADS) {
+      const int at = (int)m.list[i];
+      const float v = at < V ? sample_logit<T>(x + at) : -INFINITY;
+      const bool in = v > -INFINITY && in_bins((double)v * r.rate, t0, t1);
+      const unsigned long long place = in ? sample_place(v, at) : 0;  // (0 is the place of no token: its value is none, and in no bin)
+      m.list[i] = place;
+      if (in) {
+        lo = place < lo ? place : lo;
+        hi = place > hi ? place : hi;
       }
     }
 #pragma unroll
@@ -271,10 +344,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       atomicMax(&m.hi, hi);
     }
     __syncthreads();
-    ends_lo = m.lo;
-    ends_hi = m.hi;
-    listed0 = m.n_list <= SMP_LIST ? t0 : SMP_BINS;
-    listed1 = m.n_list <= SMP_LIST ? t1 : -1;
+    ends_lo = sample_uni(m.lo);
+    ends_hi = sample_uni(m.hi);
   };
   // Every token of bin `bin` and of places lo .. hi: f(its place, its factor).
   auto each = [&](int bin, unsigned long long lo, unsigned long long hi, auto f) {
@@ -283,12 +354,16 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       if (c >= lo && c <= hi && in_bins(y, bin, bin)) f(c, sample_factor(y - floor(y)));
     };
     if (bin >= listed0 && bin <= listed1) {
-      const int n = (int)m.n_list;
+      const int n = sample_uni((int)m.n_list);
       for (int i = t; i < n; i += SMP_THREADS) take(m.list[i], sample_value(m.list[i]));
     } else {
-      for (int i = t; i < V; i += SMP_THREADS) {
-        const float v = sample_logit<T>(x + i);
-        if (v > -INFINITY) take(sample_place(v, i), v);
+      for (int i0 = t; i0 < V; i0 += 8 * SMP_THREADS) {  // (more tokens than the list holds)
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = i0 + SMP_THREADS * j < V ? sample_logit<T>(x + i0 + SMP_THREADS * j) : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (v[j] > -INFINITY) take(sample_place(v[j], i0 + SMP_THREADS * j), v[j]);
       }
     }
   };
@@ -306,7 +381,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     }
     __syncthreads();
     for (int turn = 0; turn < 8; ++turn) {
-      const unsigned long long lo = m.lo, hi = m.hi;
+      const unsigned long long lo = sample_uni(m.lo), hi = sample_uni(m.hi);
       const int bits = 64 - __builtin_clzll((hi - lo) | 1), sh = bits > 10 ? bits - 10 : 0;
       m.sub_n[t] = 0;
       m.sub_w[t] = 0;
@@ -351,8 +426,9 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         atomicMax(&m.last, t);
       }
       __syncthreads();
-      if (m.last < 0) break;
-      if (t == (m.hit < SMP_THREADS ? m.hit : m.last)) {
+      const int hit = sample_uni(m.hit), last = sample_uni(m.last);
+      if (last < 0) break;
+      if (t == (hit < SMP_THREADS ? hit : last)) {
         const unsigned long long at = lo + ((unsigned long long)s << sh), end = at + ((1ull << sh) - 1);
         m.lo = at;
         m.hi = end < at || end > hi ? hi : end;
@@ -362,13 +438,13 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         m.part_n = own_n;
       }
       __syncthreads();
-      if (m.part_n == 1) {
-        each(bin, m.lo, m.hi, [&](unsigned long long c, unsigned long long) { m.found = c; });  // (one thread has it)
+      if (sample_uni((int)m.part_n) == 1) {
+        each(bin, sample_uni(m.lo), sample_uni(m.hi), [&](unsigned long long c, unsigned long long) { m.found = c; });  // (one thread has it)
         break;
       }
     }
     __syncthreads();
-    return m.found;
+    return sample_uni(m.found);
   };
   // ---- what is kept: the bins in front of `cut_bin`, and of that one the tokens at `cut` or in front of it
   int cut_bin = SMP_BINS;
@@ -380,22 +456,23 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     __syncthreads();
     if (t < SMP_BINS && ok(t)) atomicMin(&m.hit, t);
     __syncthreads();
-    return m.hit;
+    return sample_uni(m.hit);
   };
   auto cut_at = [&](int bin, unsigned long long from, unsigned rank, double want) {
     cut = last_kept(bin, from, rank, want);
     cut_bin = bin;
-    partial = (double)m.kept_w * sample_eighths(bin);
+    partial = (double)sample_uni(m.kept_w) * sample_eighths(bin);
   };
   if (r.k < V) {
     const int h = first_bin([&](int i) { return m.through_n[i] >= r.k; });
     if (h < SMP_BINS) {
-      if (m.through_n[h] == r.k) {
+      const int through = sample_uni(m.through_n[h]);
+      if (through == r.k) {
         cut_bin = h + 1;
         cut = ~0ull;
       } else {
-        gather(m.through_n[h] <= SMP_LIST ? 0 : h, h);
-        cut_at(h, 0, (unsigned)(r.k - (h > 0 ? m.through_n[h - 1] : 0)), 0);
+        gather(through <= SMP_LIST ? 0 : h, h);
+        cut_at(h, 0, (unsigned)(r.k - (h > 0 ? sample_uni(m.through_n[h - 1]) : 0)), 0);
       }
     }
   }
@@ -413,8 +490,9 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   if (r.low > 0.f) {
     const double d = first - floor(y_top + 8 * log2((double)r.low));
     w_least = fmax(w_least, (double)r.low * w_top);
-    if (d < cut_bin) {
-      cut_bin = (int)d;
+    const int bin = sample_uni(d < SMP_BINS ? (int)d : SMP_BINS);
+    if (bin < cut_bin) {
+      cut_bin = bin;
       cut = 0;
     }
   }
@@ -424,20 +502,20 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   };
   // ---- what is left of each chunk
   __syncthreads();
-  for (int c = wave; c < C; c += SMP_WAVES) {
-    double s = 0;
-    for (int l = lane; l + m.shift[c] < (cut_bin < SMP_BINS ? cut_bin : SMP_BINS); l += 64)
-      s += (double)(hist[(size_t)c * SMP_HIST + l] & SMP_SUM_MASK) * sample_eighths(l + m.shift[c]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if (lane == 0) m.chunk[c] = s;
+  double mine = 0.0;
+  if (lane < C) {
+    const int l = (cut_bin < SMP_BINS ? cut_bin : SMP_BINS) - 1 - m.shift[lane];
+    if (l >= 0) mine = sums[lane * SMP_HIST + l] * m.scale[lane];
   }
-  if (cut_bin < SMP_BINS && cut != ~0ull)
+  if (cut_bin < SMP_BINS && cut != ~0ull) {
+    if (cut_bin < listed0 || cut_bin > listed1) gather(cut_bin, cut_bin);
     each(cut_bin, cut, ~0ull, [&](unsigned long long c, unsigned long long f) {
-      if (kept(f, cut_bin, c) > 0.0) atomicAdd(&m.chunk_in[sample_index(c) / SMP_CHUNK], f);
+      if (kept(f, cut_bin, c) > 0.0) atomicAdd(&m.chunk_in[sample_index(c) / CHUNK], f);
     });
+  }
   __syncthreads();
-  double mine = lane < C ? m.chunk[lane] + (double)m.chunk_in[lane] * sample_eighths(cut_bin) : 0.0, ends = mine;
+  mine += (double)m.chunk_in[lane] * sample_eighths(cut_bin);
+  double ends = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const double y = __shfl_up(ends, o, 64);
@@ -447,13 +525,13 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
   u = u > 0.f ? fminf(u, 1.f) : 0.f;
   const double want = (double)u * total;
-  const unsigned long long past = __ballot(mine > 0.0 && ends > want), some = __ballot(mine > 0.0);
+  const unsigned long long past = __ballot(mine > 0.0 && ends > want), some = __ballot(mine > 0.0);  // (the same in every wave)
   if (wave == 0) m.before[lane] = ends - mine;
   // ---- the token in the chunk (in the last chunk that has any where u is 1; a chunk whose sum is all of weights that count as none is passed over)
   for (int c = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some | 1); c < C; ++c) {
     if (!((some >> c) & 1)) continue;
-    constexpr int N = SMP_CHUNK / SMP_THREADS;
-    const int i0 = c * SMP_CHUNK + t * N;
+    constexpr int N = CHUNK / SMP_THREADS;
+    const int i0 = c * CHUNK + t * N;
     double w[N], sum = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -489,7 +567,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     if (hit != 0x7fffffff) atomicMin(&m.where, hit);
     if (last >= 0) atomicMax(&m.last, last);
     __syncthreads();
-    const int id = m.where != 0x7fffffff ? m.where : m.last;
+    const int id = sample_uni(m.where != 0x7fffffff ? m.where : m.last);
     if (id < 0) continue;
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -509,25 +587,43 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
 
 using namespace la;
 
-static size_t sample_best_bytes(int B, int chunks) { return ((size_t)B * chunks * 8 + 15) / 16 * 16; }
+struct SampleLayout {
+  int per, chunks;
+  size_t sums, counts, bins, total;  // byte offsets behind the first tokens, size of all
+};
+static SampleLayout sample_layout(int B, int V) {
+  SampleLayout l{};
+  l.per = sample_per(V);
+  l.chunks = ceil_div(V, SMP_SUM_THREADS * l.per);
+  const size_t n = (size_t)B * l.chunks;
+  l.sums = (n * 8 + 15) / 16 * 16;
+  l.counts = l.sums + n * SMP_HIST * 8;
+  l.bins = l.counts + n * SMP_HIST * 4;
+  l.total = l.bins + n * SMP_SUM_THREADS * l.per;
+  return l;
+}
+static_assert(SMP_HIST % 4 == 0, "16-byte aligned parts");
 extern "C" size_t la_sample_workspace(int B, int V) {
   if (B < 1 || V < 1 || V > LA_MAX_SAMPLE_VOCAB) return 0;  // (what the call itself refuses)
-  const int chunks = ceil_div(V, SMP_CHUNK);
-  return sample_best_bytes(B, chunks) + (size_t)B * chunks * SMP_HIST * 8;
+  return sample_layout(B, V).total;
 }
 
-template <typename T>
+template <typename T, int PER>
 static int sample_launch(const Sample &a, int B, hipStream_t s) {
   {
     ProfScope ps("sample_sum", s);
-    sample_sum_kernel<T><<<dim3(a.chunks, B), SMP_SUM_THREADS, 0, s>>>(a);
+    sample_sum_kernel<T, PER><<<dim3(a.chunks, B), SMP_SUM_THREADS, 0, s>>>(a);
   }
   {
     ProfScope ps("sample", s);
-    sample_kernel<T><<<B, SMP_THREADS, 0, s>>>(a);
+    sample_kernel<T, PER><<<B, SMP_THREADS, 0, s>>>(a);
   }
   LA_HIP(hipGetLastError());
   return LA_OK;
+}
+template <typename T>
+static int sample_launch(const Sample &a, int per, int B, hipStream_t s) {
+  return per == SMP_PER ? sample_launch<T, SMP_PER>(a, B, s) : sample_launch<T, SMP_PER_SHORT>(a, B, s);
 }
 
 extern "C" int la_sample(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_sampling *how, int32_t *ids, float *prob, void *workspace,
@@ -540,14 +636,13 @@ extern "C" int la_sample(const void *logits, int dtype, int64_t row_stride, int 
   LA_REQUIRE(V >= 1 && V <= LA_MAX_SAMPLE_VOCAB, LA_EINVAL, "vocab %d outside [1, %d]", V, LA_MAX_SAMPLE_VOCAB);
   LA_REQUIRE(row_stride >= V || B == 1, LA_EINVAL, "rows overlap");
   LA_REQUIRE(how->n_u >= (how->u_index ? 1 : B), LA_EINVAL, "%d random numbers for %d rows", how->n_u, B);
-  const size_t need = la_sample_workspace(B, V);
-  LA_REQUIRE(workspace && workspace_bytes >= need, LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  const SampleLayout l = sample_layout(B, V);
+  LA_REQUIRE(workspace && workspace_bytes >= l.total, LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, l.total);
   LA_REQUIRE((uintptr_t)workspace % 16 == 0, LA_EINVAL, "workspace must be 16-byte aligned");
   hipStream_t s = (hipStream_t)stream;
-  const int chunks = ceil_div(V, SMP_CHUNK);
-  const Sample a{logits, row_stride, V, chunks, *how, ids, prob, (unsigned long long *)workspace,
-                 (unsigned long long *)((char *)workspace + sample_best_bytes(B, chunks))};
-  if (dtype == LA_F32) return sample_launch<float>(a, B, s);
-  if (dtype == LA_F16) return sample_launch<_Float16>(a, B, s);
-  return sample_launch<uint16_t>(a, B, s);
+  uint8_t *w = (uint8_t *)workspace;
+  const Sample a{logits, row_stride, V, l.chunks, *how, ids, prob, (unsigned long long *)w, (double *)(w + l.sums), (int32_t *)(w + l.counts), w + l.bins};
+  if (dtype == LA_F32) return sample_launch<float>(a, l.per, B, s);
+  if (dtype == LA_F16) return sample_launch<_Float16>(a, l.per, B, s);
+  return sample_launch<uint16_t>(a, l.per, B, s);
 }
