@@ -11,13 +11,16 @@ namespace la {
 constexpr int SMP_BINS = 514, SMP_HIST = 520;  // (64 octaves below the largest token end in the 514th bin at the latest); row length of a chunk's sums
 constexpr int SMP_SUM_THREADS = 512;          // of a workgroup of the first launch
 constexpr int SMP_PER = 16, SMP_PER_SHORT = 4;  // ... tokens of each: chunks of 8192 and of 2048
-constexpr int SMP_LIST = 5120;                // tokens of a cut that fit into LDS
+constexpr int SMP_HEAD = 64;                  // a chunk's first tokens, whole bins of them, that the first launch lists
+constexpr int SMP_LIST = 4608;                // tokens of a cut that fit into LDS
+constexpr int SMP_SHORT = 1024, SMP_FEW = 128;  // tokens down to a cut that are listed with it, a thread each; of them kept that are drawn from without looking at a chunk
 constexpr int SMP_SUB = 1024;                 // parts that a range of tokens is cut into at a time
 constexpr int SMP_COUNT_SHIFT = 50;           // a chunk's word of a bin: the number of its tokens above that bit, the sum of their factors below, in units of 2^-36
 constexpr unsigned long long SMP_SUM_MASK = (1ull << SMP_COUNT_SHIFT) - 1;
 constexpr double SMP_UNIT = 0x1p36, LEAST_WEIGHT = 0x1p-64;
 constexpr int SMP_MOST = SMP_SUM_THREADS * SMP_PER;
 static_assert(SMP_MOST * 1.1 * SMP_UNIT < (double)SMP_SUM_MASK && SMP_MOST <= 1 << 13, "a chunk in one bin");
+static_assert(64 * SMP_HEAD <= SMP_LIST, "all chunks' first tokens");
 static_assert(LA_MAX_SAMPLE_VOCAB * 1.1 * SMP_UNIT < 0x1p64 && LA_MAX_SAMPLE_VOCAB / SMP_MOST <= 64, "a row in one bin; a lane per chunk");
 // Short chunks while that leaves a row at most 16 of them: the first launch has four times the workgroups, the second reads as many sums.
 static int sample_per(int V) { return V <= 16 * SMP_SUM_THREADS * SMP_PER_SHORT ? SMP_PER_SHORT : SMP_PER; }
@@ -35,6 +38,8 @@ struct Sample {
   double *sums;
   int32_t *counts;
   uint8_t *bins;
+  unsigned long long *head;  // [SMP_HEAD] the places of its first tokens ...
+  int4 *heads;               // ... the bins they make up, from the first one, and their number; the bins up to the last that has a token
 };
 
 // A logit as it counts: NaN like -inf (no token), +inf like the largest finite value, -0 like 0.
@@ -54,17 +59,17 @@ __device__ __forceinline__ float sample_value(unsigned long long c) {
 }
 __device__ __forceinline__ int sample_index(unsigned long long c) { return (int)(0xffffffffu - (uint32_t)c); }
 
-// 2^(f / 8), 0 <= f < 1, in units of 2^-36: the exponential's series around f = 1 / 2, whose seventh term is below 6e-14.
+// 2^(f / 8), 0 <= f <= 1, in units of 2^-36: a polynomial that meets it in the six Chebyshev nodes (off by 3e-13 at most, a unit is 1.5e-11); 2^52 added to a number
+// below it leaves the nearest whole number in the low bits.
 __device__ __forceinline__ unsigned long long sample_factor(double f) {
-  const double z = (f - 0.5) * (0.6931471805599453094 / 8);
-  double s = 1.0 / 720;
-  s = __builtin_fma(s, z, 1.0 / 120);
-  s = __builtin_fma(s, z, 1.0 / 24);
-  s = __builtin_fma(s, z, 1.0 / 6);
-  s = __builtin_fma(s, z, 0.5);
-  s = __builtin_fma(s, z, 1.0);
-  s = __builtin_fma(s, z, 1.0);
-  return __double2ull_rn(s * (1.0442737824274138403 * SMP_UNIT));  // 2^(1 / 16)
+  const double z = f - 0.5;
+  double s = 4.2495173672986880985e-8;
+  s = __builtin_fma(s, z, 2.4523688009211048058e-6);
+  s = __builtin_fma(s, z, 0.00011320602609171660186);
+  s = __builtin_fma(s, z, 0.0039197225262626394621);
+  s = __builtin_fma(s, z, 0.09047942850278266672);
+  s = __builtin_fma(s, z, 1.0442737824277134712);
+  return __builtin_bit_cast(unsigned long long, __builtin_fma(s, SMP_UNIT, 0x1p52)) & ((1ull << 52) - 1);
 }
 __device__ __forceinline__ double sample_eighths(int t) {  // 2^(-t / 8) units
   constexpr double e[8] = {1.0, 0.91700404320467123, 0.84089641525371454, 0.77110541270397041, 0.70710678118654752, 0.64841977732550483, 0.59460355750136053, 0.54525386633262883};
@@ -80,6 +85,50 @@ __device__ __forceinline__ unsigned long long sample_uni(unsigned long long v) {
   return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
 }
 __device__ __forceinline__ double sample_uni(double v) { return __builtin_bit_cast(double, sample_uni(__builtin_bit_cast(unsigned long long, v))); }
+
+// Sums over the lanes in front and this one, and the largest of a wave's values, by moves between lanes that do not go through LDS (rows of 16 lanes first, then rows onto
+// those behind them).  A lane without a partner adds nothing.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int sample_from(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned sample_from(unsigned v) { return (unsigned)sample_from<CTRL, ROWS>((int)v); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned long long sample_from(unsigned long long v) {
+  return (unsigned long long)sample_from<CTRL, ROWS>((unsigned)(v >> 32)) << 32 | sample_from<CTRL, ROWS>((unsigned)v);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double sample_from(double v) { return __builtin_bit_cast(double, sample_from<CTRL, ROWS>(__builtin_bit_cast(unsigned long long, v))); }
+template <typename N>
+__device__ __forceinline__ N sample_through(N v) {
+  v += sample_from<0x111, 0xf>(v);  // row_shr by 1, 2, 4, 8
+  v += sample_from<0x112, 0xf>(v);
+  v += sample_from<0x114, 0xf>(v);
+  v += sample_from<0x118, 0xf>(v);
+  v += sample_from<0x142, 0xa>(v);  // the last lane of rows 0 and 2 onto rows 1 and 3, of row 1 onto 2 and 3
+  v += sample_from<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ int sample_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
+__device__ __forceinline__ double sample_last(double v) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+  return __builtin_bit_cast(double, (unsigned long long)(unsigned)sample_last((int)(u >> 32)) << 32 | (unsigned)sample_last((int)u));
+}
+// The sum of the first `n` <= 16 of an array in LDS, in every lane.
+template <typename N>
+__device__ __forceinline__ N sample_sum_of(const N *a, int n) {
+  const int lane = threadIdx.x & 63;
+  N v = lane < n ? a[lane] : N(0);
+  v += sample_from<0x111, 0xf>(v);
+  v += sample_from<0x112, 0xf>(v);
+  v += sample_from<0x114, 0xf>(v);
+  v += sample_from<0x118, 0xf>(v);
+  if constexpr (sizeof(N) == 8) {
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+    return __builtin_bit_cast(N, (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(b >> 32), 15) << 32 | (unsigned)__builtin_amdgcn_readlane((int)b, 15));
+  } else {
+    return (N)__builtin_amdgcn_readlane((int)v, 15);
+  }
+}
 
 // How row b is sampled; the filters that are off are out of reach.
 struct SampleRow {
@@ -116,7 +165,7 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   __shared__ __attribute__((aligned(16))) unsigned long long hist[SMP_HIST];
   __shared__ unsigned long long red[WAVES];
   __shared__ double red_w[WAVES];
-  __shared__ int red_n[WAVES];
+  __shared__ int red_n[WAVES], red_last[WAVES], n_head, head_bins;
   const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, wave = t >> 6, lane = t & 63, i0 = c * CHUNK + t;
   const T *x = (const T *)a.x + b * a.ld;
   float v[PER];
@@ -127,18 +176,25 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   }
   const SampleRow r = sample_row(a, b);
   for (int i = t; i < SMP_HIST; i += SMP_SUM_THREADS) hist[i] = 0;
-  unsigned long long best = 0;
+  float top_v = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const unsigned long long at = sample_place(v[j], i0 + SMP_SUM_THREADS * j);
-    best = at > best ? at : best;
-  }
+  for (int j = 0; j < PER; ++j) top_v = fmaxf(top_v, v[j]);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const unsigned long long y = __shfl_xor(best, o, 64);
-    best = y > best ? y : best;
+  for (int o = 32; o > 0; o >>= 1) top_v = fmaxf(top_v, __shfl_xor(top_v, o, 64));
+  int top_i = 0;
+  if (r.greedy) {  // (nobody else asks for it)
+    top_i = 0x7fffffff;
+#pragma unroll
+    for (int j = PER - 1; j >= 0; --j) top_i = v[j] == top_v ? i0 + SMP_SUM_THREADS * j : top_i;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top_i = min(top_i, __shfl_xor(top_i, o, 64));
   }
+  unsigned long long best = sample_place(top_v, top_i);
   if (lane == 0) red[wave] = best;
+  if (t == 0) {
+    n_head = 0;
+    head_bins = 0;
+  }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) best = red[w] > best ? red[w] : best;
@@ -149,13 +205,14 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   if (r.greedy || !(top > -INFINITY)) return;
   const double first = floor((double)top * r.rate);
   uint32_t code[(PER + 3) / 4] = {};
+  int bin[PER];
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const double y = (double)v[j] * r.rate, low = floor(y), d = first - low;
     const bool in = v[j] > -INFINITY && d < SMP_BINS;
-    const int bin = in ? (int)d : 255;
-    if (in) atomicAdd(&hist[bin], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low));
-    code[j / 4] |= (uint32_t)(bin < 255 ? bin : 255) << (8 * (j % 4));
+    bin[j] = in ? (int)d : SMP_BINS;
+    if (in) atomicAdd(&hist[bin[j]], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low));
+    code[j / 4] |= (uint32_t)min(bin[j], 255) << (8 * (j % 4));
   }
   uint32_t *codes = (uint32_t *)(a.bins + at * CHUNK) + t * (PER / 4);
   if constexpr (PER == 16) *(uint4 *)codes = uint4{code[0], code[1], code[2], code[3]};
@@ -164,39 +221,43 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   // sums from the front, two bins a thread
   const bool own = 2 * t < SMP_HIST;
   double w0 = 0, w1 = 0;
-  int n0 = 0, n1 = 0;
+  int n0 = 0, n1 = 0, last = 0;
   if (own) {
     const unsigned long long h0 = hist[2 * t], h1 = hist[2 * t + 1];
     w0 = (double)(h0 & SMP_SUM_MASK) * sample_eighths(2 * t);
     w1 = (double)(h1 & SMP_SUM_MASK) * sample_eighths(2 * t + 1);
     n0 = (int)(h0 >> SMP_COUNT_SHIFT);
     n1 = (int)(h1 >> SMP_COUNT_SHIFT);
+    last = n1 ? 2 * t + 2 : n0 ? 2 * t + 1 : 0;
   }
-  double w = w0 + w1;
-  int n = n0 + n1;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double yw = __shfl_up(w, o, 64);
-    const int yn = __shfl_up(n, o, 64);
-    if (lane >= o) {
-      w += yw;
-      n += yn;
-    }
-  }
+  const unsigned long long any = __ballot(last > 0);
+  if (lane == 0) red_last[wave] = any ? 2 * (64 * wave + 64 - (int)__builtin_clzll(any)) : 0;  // (rounded up to a whole thread's)
+  const double w = sample_through(w0 + w1);
+  int n = sample_through(n0 + n1);
   if (lane == 63) {
     red_w[wave] = w;
     red_n[wave] = n;
   }
   __syncthreads();
-  if (!own) return;
-  double front_w = 0;
-  int front_n = 0;
-  for (int q = 0; q < wave; ++q) {
-    front_w += red_w[q];
-    front_n += red_n[q];
+  const double front_w = sample_sum_of(red_w, wave);
+  n += sample_sum_of(red_n, wave);
+  int used = 0;
+#pragma unroll
+  for (int q = 0; q < WAVES; ++q) used = max(used, red_last[q]);
+  if (2 * t < used) {
+    *(double2 *)(a.sums + at * SMP_HIST + 2 * t) = double2{front_w + (w - w1), front_w + w};
+    *(int2 *)(a.counts + at * SMP_HIST + 2 * t) = int2{n - n1, n};
   }
-  *(double2 *)(a.sums + at * SMP_HIST + 2 * t) = double2{front_w + (w - w1), front_w + w};
-  *(int2 *)(a.counts + at * SMP_HIST + 2 * t) = int2{front_n + n - n1, front_n + n};
+  // (the numbers only grow: how many bins stay within SMP_HEAD is the first one that does not)
+  const int in_head = __builtin_popcountll(__ballot(own && n - n1 <= SMP_HEAD)) + __builtin_popcountll(__ballot(own && n <= SMP_HEAD));
+  if (lane == 0 && in_head) atomicAdd(&head_bins, in_head);
+  __syncthreads();
+  const int bins = head_bins;
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (bin[j] < bins && bin[j] < SMP_BINS) a.head[at * SMP_HEAD + atomicAdd(&n_head, 1)] = sample_place(v[j], i0 + SMP_SUM_THREADS * j);
+  __syncthreads();
+  if (t == 0) a.heads[at] = int4{bins, n_head, used, 0};
 }
 
 // Second launch, a workgroup per row: where the filters cut, what is left of every chunk, and in the chunk where u falls the token.
@@ -214,8 +275,12 @@ struct SampleShared {
   unsigned long long red_u[SMP_WAVES];
   unsigned red_n[SMP_WAVES];
   unsigned long long lo, hi, base_w, kept_w, found;
-  unsigned n_list, base_n, part_n;
-  int hit, last, where;
+  unsigned n_list, base_n, part_n, n_few;
+  int hit, last, where, uncovered;
+  unsigned long long few_c[SMP_FEW], few_w[SMP_FEW];
+  int rank[SMP_FEW];
+  int head_bins[64], head_n[64], used[64];
+  double eighths[8];
 };
 
 template <typename T, int PER>
@@ -229,6 +294,11 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     unsigned long long best = t < C ? a.best[(size_t)b * C + t] : 0;
     m.best[t] = best;
     m.chunk_in[t] = 0;
+    const int4 h = t < C && !r.greedy ? a.heads[(size_t)b * C + t] : int4{0, 0, 0, 0};  // (a chunk without a token has none of its own, and is never looked at)
+    m.head_bins[t] = h.x;
+    m.head_n[t] = h.y;
+    m.used[t] = h.z;
+    if (t < 8) m.eighths[t] = sample_eighths(t);
   }
   __syncthreads();
   unsigned long long best = m.best[lane];
@@ -259,58 +329,88 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   if (t < SMP_BINS) {
     double w = 0;
     int n = 0;
-#pragma unroll 8
-    for (int c = 0; c < C; ++c) {
-      const int l = t - m.shift[c];
-      if (l >= 0) {
-        w += sums[c * SMP_HIST + l] * m.scale[c];
-        n += counts[c * SMP_HIST + l];
-      }
+#pragma unroll 16
+    for (int c = 0; c < C; ++c) {  // (loads without a condition: many are on their way)
+      const int l = t - m.shift[c], top = m.used[c] - 1, at = l > 0 ? c * SMP_HIST + (l < top ? l : top) : c * SMP_HIST;
+      const double sw = sums[at];
+      const int sn = counts[at];
+      w += l >= 0 ? sw * m.scale[c] : 0.0;
+      n += l >= 0 ? sn : 0;
     }
     m.through_w[t] = w;
     m.through_n[t] = n;
   }
   __syncthreads();
   auto in_bins = [&](double y, int t0, int t1) { return y >= first - t1 && (t0 == 0 || y < first - t0 + 1); };
-  int listed0 = SMP_BINS, listed1 = -1;            // bins whose tokens are in the list
-  unsigned long long ends_lo = 0, ends_hi = ~0ull;  // no token of theirs lies outside
-  // Tokens of bins t0 .. t1 into the list, if they fit, and the ends of their order.  The first launch's bytes say which tokens may be there (255: perhaps); only their logits
-  // are read, all at once.
+  int listed0 = SMP_BINS, listed1 = -1;  // bins whose tokens are in the list
+  // Tokens of bins t0 .. t1 into the list, if they fit: from the chunks' first tokens where those reach that far.  Otherwise the first launch's
+  // bytes say which tokens may be there (255: perhaps); only their logits are read, all at once.
   auto gather = [&](int t0, int t1) {
     constexpr int N = 8, WORDS = PER / 4;
     __syncthreads();
     if (t == 0) {
       m.n_list = 0;
-      m.lo = ~0ull;
-      m.hi = 0;
+      m.uncovered = 0;
     }
     __syncthreads();
-    const uint32_t *codes = (const uint32_t *)(a.bins + (size_t)b * C * CHUNK);
-    for (int s0 = t; s0 < C * SMP_SUM_THREADS; s0 += N * SMP_THREADS) {
-      uint32_t code[N][WORDS];
-#pragma unroll
-      for (int u = 0; u < N; ++u) {
-        const int s = s0 + u * SMP_THREADS < C * SMP_SUM_THREADS ? s0 + u * SMP_THREADS : s0;
-        if constexpr (PER == 16) {
-          const uint4 w = *(const uint4 *)(codes + (size_t)s * WORDS);
-          code[u][0] = w.x; code[u][1] = w.y; code[u][2] = w.z; code[u][3] = w.w;
-        } else {
-          code[u][0] = codes[s];
+    if (t < C && m.shift[t] < SMP_BINS && t1 - m.shift[t] >= m.head_bins[t]) m.uncovered = 1;
+    __syncthreads();
+    const bool heads = sample_uni(m.uncovered) == 0;
+    if (heads) {
+      for (int s = t; s < C * SMP_HEAD; s += SMP_THREADS) {
+        const int c = s / SMP_HEAD;
+        if (m.shift[c] < SMP_BINS && s % SMP_HEAD < m.head_n[c]) {
+          const unsigned long long place = a.head[(size_t)b * C * SMP_HEAD + s];
+          if (in_bins((double)sample_value(place) * r.rate, t0, t1)) m.list[atomicAdd(&m.n_list, 1u)] = place;  // (64 of 64 chunks at most)
         }
       }
+    } else {
+      const uint32_t *codes = (const uint32_t *)(a.bins + (size_t)b * C * CHUNK);
+      for (int s0 = t - lane; s0 < C * SMP_SUM_THREADS; s0 += N * SMP_THREADS) {  // (whole waves)
+        uint32_t code[N][WORDS];
 #pragma unroll
-      for (int u = 0; u < N; ++u) {
-        const int s = s0 + u * SMP_THREADS, c = s / SMP_SUM_THREADS;
-        if (s >= C * SMP_SUM_THREADS) break;
-        const int shift = m.shift[c], lo = t0 > shift ? (t0 - shift < 255 ? t0 - shift : 255) : 0, hi = t1 - shift < 255 ? t1 - shift : 255;
-        if (hi < 0 || shift >= SMP_BINS) continue;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-          const unsigned bin = (code[u][j / 4] >> (8 * (j % 4))) & 255u;
-          if (bin - (unsigned)lo <= (unsigned)(hi - lo)) {
-            const unsigned at = atomicAdd(&m.n_list, 1u);
-            if (at < SMP_LIST) m.list[at] = (unsigned)(c * CHUNK + s % SMP_SUM_THREADS + SMP_SUM_THREADS * j);
+        for (int u = 0; u < N; ++u) {
+          const int s = (s0 + u * SMP_THREADS < C * SMP_SUM_THREADS ? s0 + u * SMP_THREADS : s0) + lane;
+          if constexpr (PER == 16) {
+            const uint4 w = *(const uint4 *)(codes + (size_t)s * WORDS);
+            code[u][0] = w.x; code[u][1] = w.y; code[u][2] = w.z; code[u][3] = w.w;
+          } else {
+            code[u][0] = codes[s];
           }
+        }
+        // of each word, the top bits of the bytes that may be meant
+        int found = 0;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          const int s = s0 + u * SMP_THREADS, shift = s < C * SMP_SUM_THREADS ? m.shift[s / SMP_SUM_THREADS] : SMP_BINS;
+          const unsigned lo = t0 > shift ? (t0 - shift < 255 ? t0 - shift : 255) : 0, hi = t1 - shift < 255 ? t1 - shift : 255;
+          const bool any = t1 >= shift && shift < SMP_BINS;
+#pragma unroll
+          for (int k = 0; k < WORDS; ++k) {
+            const uint32_t w = code[u][k];
+            uint32_t z;
+            if (t0 == t1) {  // bytes equal to one: what they differ in by is 0
+              const uint32_t d = w ^ (lo * 0x01010101u);
+              z = ~(((d & 0x7f7f7f7fu) + 0x7f7f7f7fu) | d | 0x7f7f7f7fu);
+            } else {  // every second byte in 16 bits: bit 8 of 256 + hi - byte and of 256 + byte - lo
+              const uint32_t e = w & 0x00ff00ffu, o = (w >> 8) & 0x00ff00ffu, high = (256 + hi) * 0x00010001u, low = (256 - lo) * 0x00010001u;
+              z = ((high - e) & (e + low) & 0x01000100u) >> 1 | ((high - o) & (o + low) & 0x01000100u) << 7;
+            }
+            code[u][k] = any ? z : 0u;
+            found += __builtin_popcount(code[u][k]);
+          }
+        }
+        const int ends = sample_through(found);
+        unsigned at = 0;
+        if (lane == 63) at = atomicAdd(&m.n_list, (unsigned)ends);
+        at = (unsigned)__builtin_amdgcn_readlane((int)at, 63) + (unsigned)(ends - found);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          const int s = s0 + u * SMP_THREADS + lane, i0 = s / SMP_SUM_THREADS * CHUNK + s % SMP_SUM_THREADS;
+#pragma unroll
+          for (int k = 0; k < WORDS; ++k)
+            for (uint32_t z = code[u][k]; z; z &= z - 1, ++at)
+              if (at < SMP_LIST) m.list[at] = (unsigned)(i0 + SMP_SUM_THREADS * (4 * k + (__builtin_ctz(z) >> 3)));
         }
       }
     }
@@ -318,34 +418,13 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     const int n = sample_uni((int)m.n_list);
     listed0 = n <= SMP_LIST ? t0 : SMP_BINS;
     listed1 = n <= SMP_LIST ? t1 : -1;
-    ends_lo = 0;
-    ends_hi = ~0ull;
-    if (n > SMP_LIST) return;
-    unsigned long long lo = ~0ull, hi = 0;
+    if (n > SMP_LIST || heads) return;
     for (int i = t; i < n; i += SMP_THREADS) {
       const int at = (int)m.list[i];
       const float v = at < V ? sample_logit<T>(x + at) : -INFINITY;
-      const bool in = v > -INFINITY && in_bins((double)v * r.rate, t0, t1);
-      const unsigned long long place = in ? sample_place(v, at) : 0;  // (0 is the place of no token: its value is none, and in no bin)
-      m.list[i] = place;
-      if (in) {
-        lo = place < lo ? place : lo;
-        hi = place > hi ? place : hi;
-      }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const unsigned long long yl = __shfl_xor(lo, o, 64), yh = __shfl_xor(hi, o, 64);
-      lo = yl < lo ? yl : lo;
-      hi = yh > hi ? yh : hi;
-    }
-    if (lane == 0) {
-      atomicMin(&m.lo, lo);
-      atomicMax(&m.hi, hi);
+      m.list[i] = v > -INFINITY && in_bins((double)v * r.rate, t0, t1) ? sample_place(v, at) : 0;  // (0 is the place of no token: its value is none, and in no bin)
     }
     __syncthreads();
-    ends_lo = sample_uni(m.lo);
-    ends_hi = sample_uni(m.hi);
   };
   // Every token of bin `bin` and of places lo .. hi: f(its place, its factor).
   auto each = [&](int bin, unsigned long long lo, unsigned long long hi, auto f) {
@@ -369,18 +448,51 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   };
   // The last of the tokens that are kept of a bin: the rank-th in order, or the first with which their sum of factors reaches want;
   // the last one at `from` or in front of it if none does.  m.kept_w: their sum.  The range of places is cut into SMP_SUB parts until one token is left, which
-  // takes seven turns at most (a place has 64 bits, a turn settles ten); a range without any token ends it too.
+  // takes seven turns at most (a place has 64 bits, a turn settles ten), or until 64 tokens are left, which a wave compares with each other; a range without any token ends it too.
   auto last_kept = [&](int bin, unsigned long long from, unsigned rank, double want) {
     __syncthreads();
     if (t == 0) {
-      m.lo = ends_lo > from ? ends_lo : from;
-      m.hi = ends_hi;
+      // no token of the bin lies outside of its ends, which a float's rounding moves by less than they are widened here (no temperature's: everywhere)
+      const double low = (first - bin) / r.rate, high = (first - bin + 1) / r.rate;
+      const float l = (float)(low - fabs(low) * 0x1p-20 - 0x1p-120), h = (float)(high + fabs(high) * 0x1p-20 + 0x1p-120);
+      const unsigned long long lo = r.rate > 0 && l > -3e38f && l < 3e38f ? sample_place(l, -1) & ~0xffffffffull : 0;
+      const unsigned long long hi = r.rate > 0 && h > -3e38f && h < 3e38f ? sample_place(h, 0) | 0xffffffffull : ~0ull;
+      m.lo = lo > from ? lo : from;
+      m.hi = hi;
       m.base_n = 0;
       m.base_w = m.kept_w = 0;
       m.found = ~0ull;
+      m.n_few = 0;
+      m.part_n = (unsigned)(m.through_n[bin] - (bin > 0 ? m.through_n[bin - 1] : 0));
     }
     __syncthreads();
     for (int turn = 0; turn < 8; ++turn) {
+      if (sample_uni((int)m.part_n) <= 64) {
+        each(bin, sample_uni(m.lo), sample_uni(m.hi), [&](unsigned long long c, unsigned long long f) {
+          const unsigned at = atomicAdd(&m.n_few, 1u);
+          m.few_c[at] = c;
+          m.few_w[at] = f;
+        });
+        __syncthreads();
+        if (wave == 0) {
+          const int n = sample_uni((int)m.n_few);
+          const unsigned long long c = lane < n ? m.few_c[lane] : 0, f = lane < n ? m.few_w[lane] : 0;
+          unsigned in_front = m.base_n;
+          unsigned long long w = m.base_w;
+          for (int j = 0; j < n; ++j) {
+            const bool ahead = m.few_c[j] >= c;
+            in_front += ahead ? 1 : 0;
+            w += ahead ? m.few_w[j] : 0;
+          }
+          const unsigned long long hit = __ballot(lane < n && (rank ? in_front == rank : (double)w >= want && (double)(w - f) < want));
+          const unsigned long long last = __ballot(lane < n && in_front == m.base_n + (unsigned)n);
+          if (n > 0 && lane == (int)__builtin_ctzll(hit ? hit : last)) {
+            m.found = c;
+            m.kept_w = w;
+          }
+        }
+        break;
+      }
       const unsigned long long lo = sample_uni(m.lo), hi = sample_uni(m.hi);
       const int bits = 64 - __builtin_clzll((hi - lo) | 1), sh = bits > 10 ? bits - 10 : 0;
       m.sub_n[t] = 0;
@@ -399,31 +511,19 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       const int s = SMP_SUB - 1 - t;  // from the front of the order on
       const unsigned own_n = m.sub_n[s];
       const unsigned long long own_w = m.sub_w[s];
-      unsigned n = own_n;
-      unsigned long long w = own_w;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const unsigned yn = __shfl_up(n, o, 64);
-        const unsigned long long yw = __shfl_up(w, o, 64);
-        if (lane >= o) {
-          n += yn;
-          w += yw;
-        }
-      }
+      unsigned n = sample_through(own_n);
+      unsigned long long w = sample_through(own_w);
       if (lane == 63) {
         m.red_n[wave] = n;
         m.red_u[wave] = w;
       }
       __syncthreads();
-      n += m.base_n;
-      w += m.base_w;
-      for (int q = 0; q < wave; ++q) {
-        n += m.red_n[q];
-        w += m.red_u[q];
-      }
-      if (own_n > 0) {
-        if (rank ? n >= rank : (double)w >= want) atomicMin(&m.hit, t);
-        atomicMax(&m.last, t);
+      n += m.base_n + sample_sum_of(m.red_n, wave);
+      w += m.base_w + sample_sum_of(m.red_u, wave);
+      const unsigned long long filled = __ballot(own_n > 0), enough = __ballot(own_n > 0 && (rank ? n >= rank : (double)w >= want));
+      if (lane == 0) {
+        if (enough) atomicMin(&m.hit, t + (int)__builtin_ctzll(enough));
+        if (filled) atomicMax(&m.last, t + 63 - (int)__builtin_clzll(filled));
       }
       __syncthreads();
       const int hit = sample_uni(m.hit), last = sample_uni(m.last);
@@ -438,10 +538,6 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         m.part_n = own_n;
       }
       __syncthreads();
-      if (sample_uni((int)m.part_n) == 1) {
-        each(bin, sample_uni(m.lo), sample_uni(m.hi), [&](unsigned long long c, unsigned long long) { m.found = c; });  // (one thread has it)
-        break;
-      }
     }
     __syncthreads();
     return sample_uni(m.found);
@@ -454,7 +550,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     __syncthreads();
     if (t == 0) m.hit = SMP_BINS;
     __syncthreads();
-    if (t < SMP_BINS && ok(t)) atomicMin(&m.hit, t);
+    const unsigned long long yes = __ballot(t < SMP_BINS && ok(t < SMP_BINS ? t : 0));
+    if (lane == 0 && yes) atomicMin(&m.hit, t + (int)__builtin_ctzll(yes));
     __syncthreads();
     return sample_uni(m.hit);
   };
@@ -471,7 +568,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         cut_bin = h + 1;
         cut = ~0ull;
       } else {
-        gather(through <= SMP_LIST ? 0 : h, h);
+        gather(through <= SMP_SHORT ? 0 : h, h);
         cut_at(h, 0, (unsigned)(r.k - (h > 0 ? sample_uni(m.through_n[h - 1]) : 0)), 0);
       }
     }
@@ -482,7 +579,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     const bool inside = h < SMP_BINS;
     if (inside || (cut_bin < SMP_BINS && cut != ~0ull)) {
       const int bin = inside ? h : cut_bin;
-      if (bin < listed0 || bin > listed1) gather(bin, bin);
+      if (bin < listed0 || bin > listed1) gather(sample_uni(m.through_n[bin]) <= SMP_SHORT ? 0 : bin, bin);
       cut_at(bin, inside ? 0 : cut, 0, (want - (bin > 0 ? m.through_w[bin - 1] : 0)) / sample_eighths(bin));
     }
   }
@@ -497,15 +594,84 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     }
   }
   auto kept = [&](unsigned long long f, int bin, unsigned long long c) {  // the token's weight, 0: not kept
-    const double w = (double)f * sample_eighths(bin);
+    const double w = ldexp((double)f * m.eighths[bin & 7], -(bin >> 3));
     return (bin < cut_bin || (bin == cut_bin && c >= cut)) && w >= w_least ? w : 0.0;
   };
+  float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
+  u = u > 0.f ? fminf(u, 1.f) : 0.f;
+  // ---- few tokens: those that are kept, put into the order of their indexes, and the sums over them
+  if (cut_bin < SMP_BINS && sample_uni(m.through_n[cut_bin]) <= SMP_SHORT) {
+    if (listed0 > 0 || cut_bin > listed1) gather(0, cut_bin);
+    __syncthreads();
+    if (t < SMP_FEW) m.rank[t] = 0;
+    if (t == 0) m.n_few = 0;
+    __syncthreads();
+    const int n_list = listed0 == 0 && cut_bin <= listed1 ? sample_uni((int)m.n_list) : 0;  // (0: more may be there than the list holds)
+    for (int i = t; i < n_list; i += SMP_THREADS) {
+      const unsigned long long c = m.list[i];
+      const double y = (double)sample_value(c) * r.rate, low = floor(y), d = first - low;
+      const double w = c && d < SMP_BINS ? kept(sample_factor(y - low), (int)d, c) : 0.0;
+      if (w > 0.0) {
+        const unsigned at = atomicAdd(&m.n_few, 1u);
+        if (at < SMP_FEW) {
+          m.few_c[at] = (unsigned)sample_index(c);
+          m.few_w[at] = __builtin_bit_cast(unsigned long long, w);
+        }
+      }
+    }
+    __syncthreads();
+    const int n = sample_uni((int)m.n_few);
+    if (n > 0 && n <= SMP_FEW) {
+      constexpr int PARTS = SMP_THREADS / SMP_FEW;
+      const int i = t % SMP_FEW, part = t / SMP_FEW;
+      const unsigned long long mine = i < n ? m.few_c[i] : 0;
+      int in_front = 0;
+      for (int j = part; j < n; j += PARTS) in_front += m.few_c[j] < mine ? 1 : 0;
+      if (i < n && in_front) atomicAdd(&m.rank[i], in_front);
+      __syncthreads();
+      if (t < n) m.list[m.rank[t]] = (unsigned long long)t;  // (the list is through)
+      __syncthreads();
+      if (wave == 0) {
+        constexpr int PAIR = SMP_FEW / 64;
+        double w[PAIR], sum = 0;
+        int id[PAIR];
+#pragma unroll
+        for (int q = 0; q < PAIR; ++q) {
+          const int at = PAIR * lane + q, from = at < n ? (int)m.list[at] : 0;
+          w[q] = at < n ? __builtin_bit_cast(double, m.few_w[from]) : 0.0;
+          id[q] = (int)m.few_c[from];
+          sum += w[q];
+        }
+        double run = sample_through(sum);
+        const double total = sample_last(run), want = (double)u * total;
+        run -= sum;
+        int hit = PAIR;
+#pragma unroll
+        for (int q = 0; q < PAIR; ++q) {
+          run += w[q];
+          if (hit == PAIR && w[q] > 0.0 && run > want) hit = q;
+        }
+        const unsigned long long past = __ballot(hit < PAIR);
+        const int who = past ? (int)__builtin_ctzll(past) : (n - 1) / PAIR;  // (u is 1: the last one)
+        if (lane == who) {
+          if (!past) hit = (n - 1) % PAIR;
+#pragma unroll
+          for (int q = 0; q < PAIR; ++q)
+            if (q == hit) {
+              a.ids[b] = id[q];
+              if (a.prob) a.prob[b] = (float)(w[q] / total);
+            }
+        }
+      }
+      return;
+    }
+  }
   // ---- what is left of each chunk
   __syncthreads();
   double mine = 0.0;
   if (lane < C) {
     const int l = (cut_bin < SMP_BINS ? cut_bin : SMP_BINS) - 1 - m.shift[lane];
-    if (l >= 0) mine = sums[lane * SMP_HIST + l] * m.scale[lane];
+    if (l >= 0) mine = sums[lane * SMP_HIST + min(l, m.used[lane] - 1)] * m.scale[lane];
   }
   if (cut_bin < SMP_BINS && cut != ~0ull) {
     if (cut_bin < listed0 || cut_bin > listed1) gather(cut_bin, cut_bin);
@@ -515,15 +681,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   }
   __syncthreads();
   mine += (double)m.chunk_in[lane] * sample_eighths(cut_bin);
-  double ends = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(ends, o, 64);
-    if (lane >= o) ends += y;
-  }
-  const double total = __shfl(ends, 63, 64);
-  float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
-  u = u > 0.f ? fminf(u, 1.f) : 0.f;
+  const double ends = sample_through(mine), total = sample_last(ends);
   const double want = (double)u * total;
   const unsigned long long past = __ballot(mine > 0.0 && ends > want), some = __ballot(mine > 0.0);  // (the same in every wave)
   if (wave == 0) m.before[lane] = ends - mine;
@@ -540,12 +698,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       w[j] = v > -INFINITY && d < SMP_BINS ? kept(sample_factor(y - low), (int)d, sample_place(v, i0 + j)) : 0.0;
       sum += w[j];
     }
-    double run = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(run, o, 64);
-      if (lane >= o) run += y;
-    }
+    double run = sample_through(sum);
     __syncthreads();
     if (lane == 63) m.red_d[wave] = run;
     if (t == 0) {
@@ -553,8 +706,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       m.last = -1;
     }
     __syncthreads();
-    run = (run - sum) + m.before[c];
-    for (int q = 0; q < wave; ++q) run += m.red_d[q];
+    run = (run - sum) + (m.before[c] + sample_sum_of(m.red_d, wave));
     int hit = 0x7fffffff, last = -1;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -589,7 +741,7 @@ using namespace la;
 
 struct SampleLayout {
   int per, chunks;
-  size_t sums, counts, bins, total;  // byte offsets behind the first tokens, size of all
+  size_t sums, counts, heads, head, bins, total;  // byte offsets behind the first tokens, size of all
 };
 static SampleLayout sample_layout(int B, int V) {
   SampleLayout l{};
@@ -598,7 +750,9 @@ static SampleLayout sample_layout(int B, int V) {
   const size_t n = (size_t)B * l.chunks;
   l.sums = (n * 8 + 15) / 16 * 16;
   l.counts = l.sums + n * SMP_HIST * 8;
-  l.bins = l.counts + n * SMP_HIST * 4;
+  l.heads = l.counts + n * SMP_HIST * 4;
+  l.head = l.heads + n * 16;
+  l.bins = l.head + n * SMP_HEAD * 8;
   l.total = l.bins + n * SMP_SUM_THREADS * l.per;
   return l;
 }
@@ -641,7 +795,8 @@ extern "C" int la_sample(const void *logits, int dtype, int64_t row_stride, int 
   LA_REQUIRE((uintptr_t)workspace % 16 == 0, LA_EINVAL, "workspace must be 16-byte aligned");
   hipStream_t s = (hipStream_t)stream;
   uint8_t *w = (uint8_t *)workspace;
-  const Sample a{logits, row_stride, V, l.chunks, *how, ids, prob, (unsigned long long *)w, (double *)(w + l.sums), (int32_t *)(w + l.counts), w + l.bins};
+  const Sample a{logits, row_stride, V, l.chunks, *how, ids, prob, (unsigned long long *)w, (double *)(w + l.sums), (int32_t *)(w + l.counts), w + l.bins,
+                 (unsigned long long *)(w + l.head), (int4 *)(w + l.heads)};
   if (dtype == LA_F32) return sample_launch<float>(a, l.per, B, s);
   if (dtype == LA_F16) return sample_launch<_Float16>(a, l.per, B, s);
   return sample_launch<uint16_t>(a, l.per, B, s);
