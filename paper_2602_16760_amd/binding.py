@@ -251,30 +251,35 @@ def la_unembed_argmax_noalloc(model, hidden, ids, top2=None, stream=None):
 
 # ---- sampling and the shared cache: operators on plain tensors, of any model or none ---------------------
 _DTYPES = {torch.float32: LA_F32, torch.bfloat16: LA_BF16, torch.float16: LA_F16}
+_F32, _I32 = torch.float32, torch.int32
 
 
-def _need(cond, text):
-    if not cond:
-        raise LaError(-1, text)
+def _refuse(text):
+    raise LaError(-1, text)
+
+
+def _here(t, name):
+    """Index of the current device, on which every tensor of the call has to be: the launch goes to one of its streams."""
+    device = t.get_device()
+    if device < 0 or device != _torch._cuda_getDevice():
+        _refuse(f"{name} is on {t.device}, not on the current CUDA device")
+    return device
 
 
 def _array(t, name, dtype, shape, device):
     """Address of a contiguous array of that type and shape on that device."""
-    _need(t.dtype is dtype and t.is_contiguous() and t.device == device and t.shape == shape,
-          f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on device {device}, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
     return t.data_ptr()
 
 
-def _here(t, name):
-    """The current device, on which every tensor of the call has to be: the launch goes to one of its streams."""
-    device = t.device
-    _need(t.is_cuda and device.index == _torch._cuda_getDevice(), f"{name} is on {device}, not on the current CUDA device")
-    return device
+def _optional(t, name, dtype, shape, device):
+    return None if t is None else _array(t, name, dtype, shape, device)
 
 
-def _workspace(size, device, stream):
+def _workspace(size, like, stream):
     """Memory for one call: of the stream that runs it, so that nobody else is given it before the call is through."""
-    ws = torch.empty(size, dtype=torch.uint8, device=device)
+    ws = torch.empty(size, dtype=torch.uint8, device=like.device)
     if stream is not None and stream != torch.cuda.current_stream():
         ws.record_stream(stream)
     return ws
@@ -282,55 +287,76 @@ def _workspace(size, device, stream):
 
 def la_unembed_logits(model, hidden, logits, stream=None):
     """logits: float32 [Bp, vocab], rows may be strided."""
-    _need(hidden.dtype is torch.float32 and hidden.dim() == 2, "hidden: need float32 [Bp, d_model]")
-    _need(logits.is_cuda and logits.dtype is torch.float32 and logits.dim() == 2 and logits.shape[0] == hidden.shape[0] and logits.stride(1) == 1,
-          "logits: need float32 [Bp, vocab] with contiguous rows")
-    _check(lib.la_unembed_logits(model, _ptr(hidden), hidden.shape[0], logits.data_ptr(), logits.stride(0) if logits.shape[0] > 1 else logits.shape[1], _stream(stream)))
+    device = _here(hidden, "hidden")
+    if hidden.dtype is not _F32 or hidden.dim() != 2:
+        _refuse("hidden: need float32 [Bp, d_model]")
+    if logits.get_device() != device or logits.dtype is not _F32 or logits.dim() != 2 or logits.shape[0] != hidden.shape[0] or logits.stride(1) != 1:
+        _refuse(f"logits: need float32 [{hidden.shape[0]}, vocab] with contiguous rows on device {device}")
+    n, V = logits.shape
+    _check(lib.la_unembed_logits(model, _ptr(hidden), n, logits.data_ptr(), logits.stride(0) if n > 1 else V, _stream(stream)))
+
+
+@functools.lru_cache(maxsize=256)
+def _sample_bytes(B, V):
+    return lib.la_sample_workspace(B, V)
 
 
 def la_sample(logits, u, ids, prob=None, temperature=None, top_k=None, top_p=None, min_p=None, u_index=None, stream=None):
     """ids[b] = a token of row b of logits [B, V] (float32, bfloat16 or float16, rows may be strided), drawn by u[b] (with u_index: by
     u[u_index[b]]).  temperature, top_p, min_p: float32 [B] or None; top_k, u_index: int32 [B] or None; prob: float32 [B] or None."""
-    _need(logits.dim() == 2 and logits.dtype in _DTYPES and logits.stride(1) == 1, "logits: need [B, V] of float32, bfloat16 or float16 with contiguous rows")
     device = _here(logits, "logits")
+    if logits.dim() != 2 or logits.dtype not in _DTYPES or logits.stride(1) != 1:
+        _refuse("logits: need [B, V] of float32, bfloat16 or float16 with contiguous rows")
     B, V = logits.shape
-    n, f32, i32 = (B,), torch.float32, torch.int32
-    opt = lambda t, name, dtype: None if t is None else _array(t, name, dtype, n, device)
-    how = la_sampling(opt(temperature, "temperature", f32), opt(top_k, "top_k", i32), opt(top_p, "top_p", f32), opt(min_p, "min_p", f32),
-                      _array(u, "u", f32, u.shape if u_index is not None and u.dim() == 1 else n, device), opt(u_index, "u_index", i32), u.shape[0])
-    size = lib.la_sample_workspace(B, V)
-    ws = _workspace(size, device, stream) if size else None
-    _check(lib.la_sample(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, B, V, C.byref(how), _array(ids, "ids", i32, n, device),
-                         opt(prob, "prob", f32), ws.data_ptr() if size else None, size, _stream(stream)))
+    n = (B,)
+    if u.dim() != 1:
+        _refuse("u: need a float32 array")
+    how = la_sampling(_optional(temperature, "temperature", _F32, n, device), _optional(top_k, "top_k", _I32, n, device), _optional(top_p, "top_p", _F32, n, device),
+                      _optional(min_p, "min_p", _F32, n, device), _array(u, "u", _F32, n if u_index is None else u.shape, device), _optional(u_index, "u_index", _I32, n, device),
+                      u.shape[0])
+    size = _sample_bytes(B, V)
+    ws = _workspace(size, logits, stream)
+    _check(lib.la_sample(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, B, V, C.byref(how), _array(ids, "ids", _I32, n, device),
+                         _optional(prob, "prob", _F32, n, device), ws.data_ptr(), size, _stream(stream)))
 
 
 class la_pages:
     """Pages of K and V, both [n_layers, n_pages, n_kv_heads, page_size, head_dim], and the descriptor that calls on them take."""
 
     def __init__(self, k, v):
-        _need(k.dim() == 5 and k.dtype in _DTYPES and k.is_cuda and k.is_contiguous(), "k: need a contiguous CUDA tensor [n_layers, n_pages, n_kv_heads, page_size, head_dim]")
-        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        if k.dim() != 5 or k.dtype not in _DTYPES or not k.is_cuda or not k.is_contiguous():
+            _refuse("k: need a contiguous CUDA tensor [n_layers, n_pages, n_kv_heads, page_size, head_dim] of float32, bfloat16 or float16")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.get_device()
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
-        self.desc = la_pages_desc(k.data_ptr(), _array(v, "v", k.dtype, k.shape, k.device), self.n_layers, self.n_pages, self.page_size, self.n_kv_heads,
+        self.desc = la_pages_desc(k.data_ptr(), _array(v, "v", k.dtype, k.shape, self.device), self.n_layers, self.n_pages, self.page_size, self.n_kv_heads,
                                   self.head_dim, _DTYPES[k.dtype])
         self.ref = C.byref(self.desc)
+        self._bytes = {}
 
-    @property
-    def is_cuda(self):
-        return True
+    def _here(self):
+        if self.device != _torch._cuda_getDevice():
+            _refuse(f"the pages are on device {self.device}, not on the current CUDA device")
+        return self.device
 
-    def _rows(self, t, name, heads):
+    def _rows(self, t, name, n, heads):
         """Address and row stride of [n, heads, head_dim] rows of the pages' type."""
         s = t.stride()
-        _need(t.dtype is self.dtype and t.device == self.device and t.dim() == 3 and t.shape[2] == self.head_dim and t.shape[1] == heads and
-              s[2] == 1 and s[1] == self.head_dim,
-              f"{name}: need {self.dtype} [n, {heads}, {self.head_dim}] with contiguous rows on {self.device}, got {t.dtype}, {tuple(t.shape)}, strides {s} on {t.device}")
+        if t.dtype is not self.dtype or t.get_device() != self.device or t.shape != (n, heads, self.head_dim) or s[2] != 1 or s[1] != self.head_dim:
+            _refuse(f"{name}: need {self.dtype} [{n}, {heads}, {self.head_dim}] with contiguous rows on device {self.device}, got {t.dtype}, {tuple(t.shape)}, strides {s} on {t.device}")
         return t.data_ptr(), s[0]
+
+    def _attend_bytes(self, heads, blocks, rows):
+        """Workspace of an attention call, by its sizes."""
+        key = (heads, blocks, rows)
+        size = self._bytes.get(key)
+        if size is None:
+            size = self._bytes[key] = lib.la_paged_attend_workspace(self.ref, heads, blocks, rows)
+        return size
 
 
 def _table(table, device):
-    _need(table.dtype is torch.int32 and table.device == device and table.dim() == 2 and table.stride(1) == 1,
-          f"table: need int32 [n_requests, max_blocks] with contiguous rows on {device}")
+    if table.dtype is not _I32 or table.get_device() != device or table.dim() != 2 or table.stride(1) != 1:
+        _refuse(f"table: need int32 [n_requests, max_blocks] with contiguous rows on device {device}")
     R, blocks = table.shape
     return table.data_ptr(), table.stride(0) if R > 1 else blocks, R, blocks
 
@@ -338,51 +364,52 @@ def _table(table, device):
 def la_page_map(old_len, new_len, page_size, table, ring, heads_in, heads_out, slot, pos, req, first, stream=None):
     """Pages and slots of the requests' new tokens: see la.h.  All int32: old_len, new_len [R], table [R, max_blocks], ring [n_pages],
     heads_in, heads_out [4] = {head, free pages, rows, error}, slot, pos, req [max_rows], first [R + 1]."""
-    device, i32 = _here(old_len, "old_len"), torch.int32
+    device = _here(old_len, "old_len")
     tp, ld, R, blocks = _table(table, device)
-    n, rows, four = (R,), slot.shape, (4,)
-    _check(lib.la_page_map(_array(old_len, "old_len", i32, n, device), _array(new_len, "new_len", i32, n, device), R, page_size, tp, ld, blocks,
-                           _array(ring, "ring", i32, (ring.numel(),), device), ring.numel(), _array(heads_in, "heads_in", i32, four, device),
-                           _array(heads_out, "heads_out", i32, four, device), _array(slot, "slot", i32, (slot.numel(),), device), _array(pos, "pos", i32, rows, device),
-                           _array(req, "req", i32, rows, device), slot.numel(), _array(first, "first", i32, (R + 1,), device), _stream(stream)))
+    n, rows, n_pages = (R,), slot.shape, ring.numel()
+    if slot.dim() != 1:
+        _refuse("slot: need an int32 array")
+    _check(lib.la_page_map(_array(old_len, "old_len", _I32, n, device), _array(new_len, "new_len", _I32, n, device), R, page_size, tp, ld, blocks,
+                           _array(ring, "ring", _I32, (n_pages,), device), n_pages, _array(heads_in, "heads_in", _I32, (4,), device),
+                           _array(heads_out, "heads_out", _I32, (4,), device), _array(slot, "slot", _I32, rows, device), _array(pos, "pos", _I32, rows, device),
+                           _array(req, "req", _I32, rows, device), rows[0], _array(first, "first", _I32, (R + 1,), device), _stream(stream)))
 
 
 def la_paged_write(pages, layer, k, v, slot, stream=None):
     """Rows of k, v [n, n_kv_heads, head_dim] (the rows themselves may be strided) into the slots slot [n] of one layer."""
-    device = _here(pages, "pages")
-    kp, ldk = pages._rows(k, "k", pages.n_kv_heads)
-    vp, ldv = pages._rows(v, "v", pages.n_kv_heads)
-    n = k.shape[0]
-    _need(v.shape[0] == n, f"{n} rows of k and {v.shape[0]} of v")
-    _check(lib.la_paged_write(pages.ref, layer, kp, vp, ldk, ldv, _array(slot, "slot", torch.int32, (n,), device), n, _stream(stream)))
+    device, n = pages._here(), k.shape[0]
+    kp, ldk = pages._rows(k, "k", n, pages.n_kv_heads)
+    vp, ldv = pages._rows(v, "v", n, pages.n_kv_heads)
+    _check(lib.la_paged_write(pages.ref, layer, kp, vp, ldk, ldv, _array(slot, "slot", _I32, (n,), device), n, _stream(stream)))
 
 
 def la_paged_attend(pages, layer, q, table, req, pos, out, scale=None, stream=None):
     """out[b] = attention of q[b] over positions 0 .. pos[b] of request req[b] (None: request b); q, out [B, n_q_heads, head_dim], rows may be
     strided; scale None: head_dim ** -0.5."""
-    device, i32 = _here(pages, "pages"), torch.int32
-    _need(q.dim() == 3, "q: need [B, n_q_heads, head_dim]")
-    B, Hq = q.shape[:2]
-    qp, ldq = pages._rows(q, "q", Hq)
-    op, ldo = pages._rows(out, "out", Hq)
-    _need(out.shape[0] == B, f"{B} rows of q and {out.shape[0]} of out")
-    _need(B < 2 or ldo >= Hq * pages.head_dim, "out: rows overlap")
+    device = pages._here()
+    if q.dim() != 3:
+        _refuse("q: need [B, n_q_heads, head_dim]")
+    B, Hq, dh = q.shape
+    qp, ldq = pages._rows(q, "q", B, Hq)
+    op, ldo = pages._rows(out, "out", B, Hq)
+    if B > 1 and ldo < Hq * dh:
+        _refuse("out: rows overlap")
     tp, ld, R, blocks = _table(table, device)
-    size = lib.la_paged_attend_workspace(pages.ref, Hq, blocks, B)
-    ws = _workspace(size, device, stream) if size else None
-    _check(lib.la_paged_attend(pages.ref, layer, qp, ldq, Hq, pages.head_dim ** -0.5 if scale is None else scale, tp, ld, R, blocks,
-                               None if req is None else _array(req, "req", i32, (B,), device), _array(pos, "pos", i32, (B,), device), B, op, ldo,
-                               ws.data_ptr() if size else None, size, _stream(stream)))
+    size = pages._attend_bytes(Hq, blocks, B)
+    ws = _workspace(size, q, stream) if size else None
+    _check(lib.la_paged_attend(pages.ref, layer, qp, ldq, Hq, dh ** -0.5 if scale is None else scale, tp, ld, R, blocks, _optional(req, "req", _I32, (B,), device),
+                               _array(pos, "pos", _I32, (B,), device), B, op, ldo, ws.data_ptr() if size else None, size, _stream(stream)))
 
 
 def la_forward_paged(model, layer_begin, layer_end, hidden, pos, req, slot, pages, table, stream=None):
     """One token each of several requests through the layers: hidden float32 [B, d_model] in place, pos, req (None: row b is request b), slot int32 [B]."""
-    device, i32 = _here(pages, "pages"), torch.int32
+    device = pages._here()
+    if hidden.dtype is not _F32 or hidden.dim() != 2 or hidden.get_device() != device:
+        _refuse(f"hidden: need float32 [B, d_model] on device {device}")
     n = (hidden.shape[0],)
-    _need(hidden.dtype is torch.float32 and hidden.dim() == 2, "hidden: need float32 [B, d_model]")
     tp, ld, R, blocks = _table(table, device)
-    _check(lib.la_forward_paged(model, layer_begin, layer_end, _ptr(hidden), n[0], _array(pos, "pos", i32, n, device), None if req is None else _array(req, "req", i32, n, device),
-                                _array(slot, "slot", i32, n, device), pages.ref, tp, ld, R, blocks, _stream(stream)))
+    _check(lib.la_forward_paged(model, layer_begin, layer_end, _ptr(hidden), n[0], _array(pos, "pos", _I32, n, device), _optional(req, "req", _I32, n, device),
+                                _array(slot, "slot", _I32, n, device), pages.ref, tp, ld, R, blocks, _stream(stream)))
 
 
 def la_pool_alloc(vocab, N, G):
