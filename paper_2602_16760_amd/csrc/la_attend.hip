@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "la_lanes.h"
 #include "la_paged.h"
 
 namespace la {
@@ -34,7 +35,8 @@ struct PagedAttend {
   float *part;   // [item][Hq][rec]
 };
 
-constexpr int AT_WAVES = 4, AT_THREADS = 64 * AT_WAVES;
+constexpr int AT_WAVES = 4, AT_WHOLE_WAVES = 8;  // of a workgroup; where rows are not cut and heads are few
+constexpr int AT_JOIN_WAVES = 4;
 constexpr int AT_ROWS = 16;       // query heads of a tile
 constexpr int AT_PIECE = 128;     // an item's keys are a multiple of this
 constexpr float AT_LOG2E = 1.4426950408889634f;
@@ -46,8 +48,8 @@ __device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
   return (unsigned)r >= (unsigned)a.n_req || n < 0 ? 0 : (int)(n < cap ? n : cap);
 }
 
-// The items: row b has max(1, ceil(keys / C)) of them, C = all rows' keys over `target`, rounded up to AT_PIECE.  Every wave forms that from the rows'
-// positions by itself.
+// The items: row b has max(1, ceil(keys / C)) of them, C = a multiple of AT_PIECE for which that is at most `target` items in all (or nearly: rows of few keys have one each).
+// Every wave forms that from the rows' positions by itself.
 struct AtItem {
   int b, r, n, C, index, first, count;  // row, its request and keys; keys per item; which of the row's items; the row's first item; how many it has
 };
@@ -56,40 +58,37 @@ template <bool BY_ROW>
 __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {  // the wanted item; BY_ROW: item 0 of the wanted row.  b = -1: there is none
   const int lane = threadIdx.x & 63;
   AtItem it;
-  int r = 0, n = 0;
-  it.C = 0x7fffffff;
+  int r = 0, n = lane < a.B ? at_keys(a, lane, r) : 0;
+  it.C = 0x7fffff80;
   if (a.target > 0) {
-    long long all = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-      n = b0 + lane < a.B ? at_keys(a, b0 + lane, r) : 0;
-      long long s = n;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-      all += s;
+    long long all = n;
+    for (int b0 = 64; b0 < a.B; b0 += 64) {
+      int r1;
+      all += b0 + lane < a.B ? at_keys(a, b0 + lane, r1) : 0;
     }
-    const long long c = ((all + a.target - 1) / a.target + AT_PIECE - 1) / AT_PIECE * AT_PIECE;
-    it.C = (int)(c < AT_PIECE ? AT_PIECE : c < 0x7fffff80 ? c : 0x7fffff80);
+    all = lane_value(lane_through(all), 63);
+    auto pieces = [](long long keys) { return (int)((keys + AT_PIECE - 1) / AT_PIECE < 1 ? 1 : (keys + AT_PIECE - 1) / AT_PIECE < 0xffffff ? (keys + AT_PIECE - 1) / AT_PIECE : 0xffffff) * AT_PIECE; };
+    it.C = pieces((all + a.target - 1) / a.target);
+    // the rows' last items are not full: longer ones, until all of them are resident at once
+    for (int turn = 0; turn < 3 && a.B <= 64; ++turn) {
+      const int items = lane_value(lane_through(lane < a.B ? at_rows_items(n, it.C) : 0), 63);
+      if (items <= a.target || items <= a.B) break;
+      it.C = pieces((long long)it.C * items / a.target + 1);
+    }
   }
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     const bool in = b0 + lane < a.B;
-    if (a.target == 0 || a.B > 64) n = in ? at_keys(a, b0 + lane, r) : 0;
-    const int c = in ? at_rows_items(n, it.C) : 0;
-    int ends = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(ends, o, 64);
-      if (lane >= o) ends += y;
-    }
-    const int total = __builtin_amdgcn_readlane(ends, 63);
+    if (b0 > 0 || a.B > 64) n = in ? at_keys(a, b0 + lane, r) : 0;
+    const int c = in ? at_rows_items(n, it.C) : 0, ends = lane_through(c), total = lane_value(ends, 63);
     const bool here = BY_ROW ? wanted < b0 + 64 : wanted < before + total;
     if (here) {
       const int l = BY_ROW ? wanted - b0 : __builtin_popcountll(__ballot(before + ends <= wanted));
       it.b = b0 + l;
-      it.r = __builtin_amdgcn_readlane(r, l);
-      it.n = __builtin_amdgcn_readlane(n, l);
-      it.count = __builtin_amdgcn_readlane(c, l);
-      it.first = before + __builtin_amdgcn_readlane(ends, l) - it.count;
+      it.r = lane_value(r, l);
+      it.n = lane_value(n, l);
+      it.count = lane_value(c, l);
+      it.first = before + lane_value(ends, l) - it.count;
       it.index = BY_ROW ? 0 : wanted - it.first;
       return it;
     }
@@ -144,8 +143,8 @@ __device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int co
 //   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
 // PAGED16: page_size is a multiple of 16, so that a 16-key tile lies in one page and its address is a scalar; otherwise a lane looks up its own keys' places.
 // FULL: head_dim = DH; otherwise what a lane would load behind a row's end is replaced by zeros.
-template <typename T, int DH, bool PAGED16, bool FULL>
-__global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_kernel(PagedAttend a) {
+template <typename T, int DH, bool PAGED16, bool FULL, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_kernel(PagedAttend a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES;
   constexpr int KP = DH * E / 64;                  // 16-byte pieces of a key row per lane (four lanes a row)
@@ -175,7 +174,7 @@ __global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_ker
   const float to_log2 = a.scale * AT_LOG2E;
   const int row_bytes = dh * E;
   const int32_t *tab = a.table + it.r * a.ldt;
-  const int n_blocks = (k_end - k_first + KEYS - 1) / KEYS, mine = n_blocks > wave ? (n_blocks - wave + AT_WAVES - 1) / AT_WAVES : 0;
+  const int n_blocks = (k_end - k_first + KEYS - 1) / KEYS, mine = n_blocks > wave ? (n_blocks - wave + WAVES - 1) / WAVES : 0;
   // Where the tiles lie: PAGED16: lane i holds byte offset and number of keys of tile i of the next 64 of this wave; else lane j < KEYS the offset of key j of the block, -1: none.
   unsigned off_lo = 0, off_hi = 0;
   int n_keys = 0;
@@ -185,8 +184,8 @@ __global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_ker
   };
   auto look_up = [&](int i) {  // for block i of this wave
     if (PAGED16 ? i % (64 / TILES) == 0 : true) {
-      const long long key = PAGED16 ? k_first + (long long)KEYS * (wave + (long long)AT_WAVES * (i + lane / TILES)) + 16 * (lane % TILES)
-                                    : k_first + (long long)KEYS * (wave + (long long)AT_WAVES * i) + lane;
+      const long long key = PAGED16 ? k_first + (long long)KEYS * (wave + (long long)WAVES * (i + lane / TILES)) + 16 * (lane % TILES)
+                                    : k_first + (long long)KEYS * (wave + (long long)WAVES * i) + lane;
       long long at = -1;
       if (key < k_end && (PAGED16 || lane < KEYS)) at = place(key);
       off_lo = (unsigned)at;
@@ -340,16 +339,19 @@ __global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_ker
     }
   }
   l_run = at_sum4(l_run);
-  // waves 1 .. leave their sums, wave 0 adds them in order: per wave and row [m, l, -, -][DH]; output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w
-  constexpr int REC = DH + 4;
-  float *rec = at_lds + (size_t)((wave - 1) * AT_ROWS + c16) * REC;
-  if (wave > 0 && c16 < rows) {
-    if (q4 == 0) {
-      rec[0] = m_run;
-      rec[1] = l_run;
-    }
+  // The waves' sums meet in LDS, a part of 16 VC channels at a time: [wave][row][channels + 4], and in front of them [wave][row] maximum and sum; a thread adds the waves'
+  // sums of four channels, in order.  Output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w.
+  constexpr int PART = 16 * VC, PITCH = PART + 4, QUADS = PART / 4;
+  float *stat = at_lds, *sums = at_lds + 2 * WAVES * AT_ROWS;
+  if (q4 == 0) {
+    stat[2 * (wave * AT_ROWS + c16)] = m_run;
+    stat[2 * (wave * AT_ROWS + c16) + 1] = l_run;
+  }
 #pragma unroll
-    for (int u = 0; u < VH; ++u)
+  for (int u = 0; u < VH; ++u) {
+    if (u > 0) __syncthreads();
+    if (c16 < rows) {
+      float *to = sums + (size_t)(wave * rows + c16) * PITCH;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -357,118 +359,96 @@ __global__ __launch_bounds__(AT_THREADS, DH > 128 ? 1 : 2) void paged_attend_ker
           at_f4 v;
 #pragma unroll
           for (int x = 0; x < 4; ++x) v[x] = o[u * VC + w + x][e];
-          *(at_f4 *)(rec + 4 + 16 * VC * u + VC * (4 * q4 + e) + w) = v;
+          *(at_f4 *)(to + VC * (4 * q4 + e) + w) = v;
         }
-  }
-  __syncthreads();
-  if (wave > 0 || c16 >= rows) return;
-  float m = m_run;
-  const float *recs = at_lds + (size_t)c16 * REC;
-  for (int w = 1; w < AT_WAVES; ++w) m = fmaxf(m, recs[(size_t)(w - 1) * AT_ROWS * REC]);
-  const float base = m > -INFINITY ? m : 0.f;
-  float f = __builtin_amdgcn_exp2f(m_run - base), l = l_run * f;
-#pragma unroll
-  for (int d = 0; d < DT; ++d) o[d] *= f;
-  for (int w = 1; w < AT_WAVES; ++w) {
-    const float *p = recs + (size_t)(w - 1) * AT_ROWS * REC;
-    f = __builtin_amdgcn_exp2f(p[0] - base);
-    l += p[1] * f;
-#pragma unroll
-    for (int u = 0; u < VH; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int c = 0; c < VC; c += 4) {
-          const at_f4 v = *(const at_f4 *)(p + 4 + 16 * VC * u + VC * (4 * q4 + e) + c);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) o[u * VC + c + x][e] += v[x] * f;
-        }
-  }
-  const int head = head0 + c16;
-  if (it.count > 1) {
-    float *to = a.part + ((size_t)blockIdx.x * a.Hq + head) * a.rec;
-    if (q4 == 0) {
-      to[0] = m;
-      to[1] = l;
     }
-#pragma unroll
-    for (int u = 0; u < VH; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int ch = 16 * VC * u + VC * (4 * q4 + e);
-        if (!FULL && ch >= dh) continue;
-#pragma unroll
-        for (int w = 0; w < VC; w += 4) {
-          at_f4 v;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) v[x] = o[u * VC + w + x][e];
-          *(at_f4 *)(to + 4 + ch + w) = v;
-        }
-      }
-    return;
-  }
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // (nothing seen: zeros)
-  T *to = (T *)a.out + it.b * a.ldo + (int64_t)head * dh;
-#pragma unroll
-  for (int u = 0; u < VH; ++u)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int ch = 16 * VC * u + VC * (4 * q4 + e);
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * QUADS; i += 64 * WAVES) {
+      const int row = i / QUADS, at = 4 * (i - row * QUADS), ch = PART * u + at, head = head0 + row;
       if (!FULL && ch >= dh) continue;
-      if (a.kind != AT_OUT_ROWS) {
+      float m = stat[2 * row];
 #pragma unroll
-        for (int w = 0; w < VC; ++w) at_store_row(a, it.b, head * dh + ch + w, o[u * VC + w][e] * inv);
+      for (int w = 1; w < WAVES; ++w) m = fmaxf(m, stat[2 * (w * AT_ROWS + row)]);
+      const float base = m > -INFINITY ? m : 0.f;
+      float l = 0.f;
+      at_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(stat[2 * (w * AT_ROWS + row)] - base);
+        l += stat[2 * (w * AT_ROWS + row) + 1] * f;
+        y += *(const at_f4 *)(sums + (size_t)(w * rows + row) * PITCH + at) * f;
+      }
+      if (it.count > 1) {
+        float *to = a.part + ((size_t)blockIdx.x * a.Hq + head) * a.rec;
+        if (u == 0 && at == 0) *(float2 *)to = float2{m, l};
+        *(at_f4 *)(to + 4 + ch) = y;
         continue;
       }
-      unsigned y[VW / 4];
+      y *= l > 0.f || l != l ? 1.f / l : 0.f;  // (nothing seen: zeros)
+      if (a.kind != AT_OUT_ROWS) {
 #pragma unroll
-      for (int w = 0; w < VW / 4; ++w) {
-        if constexpr (F32) y[w] = __float_as_uint(o[u * VC + w][e] * inv);
-        else y[w] = at_pack<T>(o[u * VC + 2 * w][e] * inv, o[u * VC + 2 * w + 1][e] * inv);
+        for (int x = 0; x < 4; ++x) at_store_row(a, it.b, head * dh + ch + x, y[x]);
+      } else {
+        T *to = (T *)a.out + it.b * a.ldo + (int64_t)head * dh + ch;
+        if constexpr (F32) *(at_f4 *)to = y;
+        else *(at_u2 *)to = at_u2{at_pack<T>(y[0], y[1]), at_pack<T>(y[2], y[3])};
       }
-      if constexpr (VW == 16) *(at_u4 *)(to + ch) = at_u4{y[0], y[1], y[2], y[3]};
-      else *(at_u2 *)(to + ch) = at_u2{y[0], y[1]};
     }
+  }
 }
 
-// The items of a row and head, in item order: a workgroup each, whose waves take every fourth item; two channels a lane, so up to two turns.
+// The items of a row and head, in item order: a workgroup each, whose waves take every fourth item; a lane takes up to four channels.  What it reads does not wait for what
+// the rows' maxima are: they are applied to it.
 template <typename T>
-__global__ __launch_bounds__(AT_THREADS) void paged_join_kernel(PagedAttend a) {
-  __shared__ float sums[AT_WAVES - 1][256];
+__global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAttend a) {
+  __shared__ float sums[AT_JOIN_WAVES][256];
   const AtItem it = at_find<true>(a, blockIdx.x);
   if (it.count < 2) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.y;
-  const float *rec = a.part + ((size_t)it.first * a.Hq + head) * a.rec;
   const size_t step = (size_t)a.Hq * a.rec;
-  float m = -INFINITY;
-  for (int i = lane; i < it.count; i += 64) m = fmaxf(m, rec[i * step]);
+  const float *rec = a.part + ((size_t)it.first * a.Hq + head) * a.rec;
+  float m = -INFINITY, l = 0.f;
+  for (int i0 = 0; i0 < it.count; i0 += 64) {
+    const float2 s = i0 + lane < it.count ? *(const float2 *)(rec + (i0 + lane) * step) : float2{-INFINITY, 0.f};
+    const float m_new = fmaxf(m, s.x), base = m_new > -INFINITY ? m_new : 0.f;
+    l = l * __builtin_amdgcn_exp2f(m - base) + s.y * __builtin_amdgcn_exp2f(s.x - base);
+    m = m_new;
+  }
+  float top = m;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const float base = m > -INFINITY ? m : 0.f;
-  float l = 0.f;
-  for (int i = lane; i < it.count; i += 64) l += rec[i * step + 1] * __builtin_amdgcn_exp2f(rec[i * step] - base);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float base = top > -INFINITY ? top : 0.f;
+  l *= __builtin_amdgcn_exp2f(m - base);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
   float acc[4] = {0.f, 0.f, 0.f, 0.f};  // channels lane, lane + 64, ...
-#pragma unroll 4
-  for (int i = wave; i < it.count; i += AT_WAVES) {
-    const float f = __builtin_amdgcn_exp2f(rec[i * step] - base);
+  const int parts = (a.dh + 63) / 64;
+  constexpr int N = 4;
+  for (int i0 = wave; i0 < it.count; i0 += N * AT_JOIN_WAVES) {
+    float v[N][4], s[N];
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (lane + 64 * c < a.dh) acc[c] += rec[i * step + 4 + lane + 64 * c] * f;
+    for (int k = 0; k < N; ++k) {
+      const int i = i0 + AT_JOIN_WAVES * k < it.count ? i0 + AT_JOIN_WAVES * k : i0;
+      s[k] = rec[i * step];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[k][c] = c < parts ? rec[i * step + 4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float f = i0 + AT_JOIN_WAVES * k < it.count ? __builtin_amdgcn_exp2f(s[k] - base) : 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] += f > 0.f || f != f ? v[k][c] * f : 0.f;
+    }
   }
-  if (wave > 0)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) sums[wave - 1][lane + 64 * c] = acc[c];
+  for (int c = 0; c < 4; ++c) sums[wave][lane + 64 * c] = acc[c];
   __syncthreads();
-  if (wave > 0) return;
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  for (int ch = threadIdx.x; ch < a.dh; ch += 64 * AT_JOIN_WAVES) {
+    float y = sums[0][ch];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int ch = lane + 64 * c;
-    if (ch >= a.dh) break;
-    for (int w = 0; w < AT_WAVES - 1; ++w) acc[c] += sums[w][ch];
-    const float y = acc[c] * inv;
+    for (int w = 1; w < AT_JOIN_WAVES; ++w) y += sums[w][ch];
+    y *= inv;
     if (a.kind != AT_OUT_ROWS) {
       at_store_row(a, it.b, head * a.dh + ch, y);
       continue;
@@ -502,15 +482,21 @@ static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
 
 template <typename T, int DH, bool PAGED16, bool FULL>
 static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
-  constexpr int lds = (AT_WAVES - 1) * AT_ROWS * (DH + 4) * 4;
-  static_assert(lds <= 64 * 1024, "LDS that a launch may ask for");
+  const int g = a.Hq / a.Hkv, rows = std::min(g, AT_ROWS);
+  constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
+  auto lds = [&](int waves) { return (2 * waves * AT_ROWS + waves * rows * (16 * VC + 4)) * 4; };  // (37 KB at most)
+  const dim3 grid(plan.items, a.Hkv * plan.tiles);
+  bool wide = false;
+  if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8;
   {
     ProfScope ps("paged_attend", s);
-    paged_attend_kernel<T, DH, PAGED16, FULL><<<dim3(plan.items, a.Hkv * plan.tiles), AT_THREADS, lds, s>>>(a);
+    if constexpr (DH <= 128)
+      if (wide) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WHOLE_WAVES><<<grid, 64 * AT_WHOLE_WAVES, lds(AT_WHOLE_WAVES), s>>>(a);
+    if (!wide) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WAVES><<<grid, 64 * AT_WAVES, lds(AT_WAVES), s>>>(a);
   }
   if (plan.target > 0) {
     ProfScope ps("paged_join", s);
-    paged_join_kernel<T><<<dim3(a.B, a.Hq), AT_THREADS, 0, s>>>(a);
+    paged_join_kernel<T><<<dim3(a.B, a.Hq), 64 * AT_JOIN_WAVES, 0, s>>>(a);
   }
   LA_HIP(hipGetLastError());
   return LA_OK;

@@ -1,6 +1,7 @@
 // Sampling of a token per row from stored logits: temperature, top-k, top-p, min-p, a given random number per row (la_sample).
 #include "la_device.h"
 #include "la_internal.h"
+#include "la_lanes.h"
 
 namespace la {
 
@@ -79,57 +80,6 @@ __device__ __forceinline__ double sample_eighths(int t) {  // 2^(-t / 8) units
   return ldexp(v * (1 / SMP_UNIT), -(t >> 3));
 }
 
-// What all threads have alike, as scalars: branches around barriers are then jumps, not masks.
-__device__ __forceinline__ int sample_uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ unsigned long long sample_uni(unsigned long long v) {
-  return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
-}
-__device__ __forceinline__ double sample_uni(double v) { return __builtin_bit_cast(double, sample_uni(__builtin_bit_cast(unsigned long long, v))); }
-
-// Sums over the lanes in front and this one, and the largest of a wave's values, by moves between lanes that do not go through LDS (rows of 16 lanes first, then rows onto
-// those behind them).  A lane without a partner adds nothing.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int sample_from(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ unsigned sample_from(unsigned v) { return (unsigned)sample_from<CTRL, ROWS>((int)v); }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ unsigned long long sample_from(unsigned long long v) {
-  return (unsigned long long)sample_from<CTRL, ROWS>((unsigned)(v >> 32)) << 32 | sample_from<CTRL, ROWS>((unsigned)v);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double sample_from(double v) { return __builtin_bit_cast(double, sample_from<CTRL, ROWS>(__builtin_bit_cast(unsigned long long, v))); }
-template <typename N>
-__device__ __forceinline__ N sample_through(N v) {
-  v += sample_from<0x111, 0xf>(v);  // row_shr by 1, 2, 4, 8
-  v += sample_from<0x112, 0xf>(v);
-  v += sample_from<0x114, 0xf>(v);
-  v += sample_from<0x118, 0xf>(v);
-  v += sample_from<0x142, 0xa>(v);  // the last lane of rows 0 and 2 onto rows 1 and 3, of row 1 onto 2 and 3
-  v += sample_from<0x143, 0xc>(v);
-  return v;
-}
-__device__ __forceinline__ int sample_last(int v) { return __builtin_amdgcn_readlane(v, 63); }
-__device__ __forceinline__ double sample_last(double v) {
-  const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
-  return __builtin_bit_cast(double, (unsigned long long)(unsigned)sample_last((int)(u >> 32)) << 32 | (unsigned)sample_last((int)u));
-}
-// The sum of the first `n` <= 16 of an array in LDS, in every lane.
-template <typename N>
-__device__ __forceinline__ N sample_sum_of(const N *a, int n) {
-  const int lane = threadIdx.x & 63;
-  N v = lane < n ? a[lane] : N(0);
-  v += sample_from<0x111, 0xf>(v);
-  v += sample_from<0x112, 0xf>(v);
-  v += sample_from<0x114, 0xf>(v);
-  v += sample_from<0x118, 0xf>(v);
-  if constexpr (sizeof(N) == 8) {
-    const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
-    return __builtin_bit_cast(N, (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(b >> 32), 15) << 32 | (unsigned)__builtin_amdgcn_readlane((int)b, 15));
-  } else {
-    return (N)__builtin_amdgcn_readlane((int)v, 15);
-  }
-}
-
 // How row b is sampled; the filters that are off are out of reach.
 struct SampleRow {
   bool greedy;
@@ -140,8 +90,8 @@ struct SampleRow {
 __device__ __forceinline__ SampleRow sample_row(const Sample &a, int b) {
   SampleRow r;
   const float t = a.p.temperature ? a.p.temperature[b] : 1.f;
-  r.greedy = sample_uni(!(t > 0.f)) != 0;
-  r.rate = sample_uni(8 * 1.44269504088896340736 / (double)t);
+  r.greedy = uniform(!(t > 0.f)) != 0;
+  r.rate = uniform(8 * 1.44269504088896340736 / (double)t);
   const int k = a.p.top_k ? a.p.top_k[b] : 0;
   r.k = k > 0 && k < a.V ? k : a.V;
   r.p = a.p.top_p ? a.p.top_p[b] : 1.f;
@@ -152,9 +102,9 @@ __device__ __forceinline__ SampleRow sample_row(const Sample &a, int b) {
   }
   r.low = a.p.min_p ? a.p.min_p[b] : 0.f;
   r.low = r.low > 0.f ? fminf(r.low, 1.f) : 0.f;
-  r.k = sample_uni(r.k);
-  r.p = __uint_as_float((unsigned)sample_uni((int)__float_as_uint(r.p)));
-  r.low = __uint_as_float((unsigned)sample_uni((int)__float_as_uint(r.low)));
+  r.k = uniform(r.k);
+  r.p = __uint_as_float((unsigned)uniform((int)__float_as_uint(r.p)));
+  r.low = __uint_as_float((unsigned)uniform((int)__float_as_uint(r.low)));
   return r;
 }
 
@@ -198,7 +148,7 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) best = red[w] > best ? red[w] : best;
-  best = sample_uni(best);
+  best = uniform(best);
   const size_t at = (size_t)b * a.chunks + c;
   if (t == 0) a.best[at] = best;
   const float top = sample_value(best);
@@ -232,15 +182,15 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   }
   const unsigned long long any = __ballot(last > 0);
   if (lane == 0) red_last[wave] = any ? 2 * (64 * wave + 64 - (int)__builtin_clzll(any)) : 0;  // (rounded up to a whole thread's)
-  const double w = sample_through(w0 + w1);
-  int n = sample_through(n0 + n1);
+  const double w = lane_through(w0 + w1);
+  int n = lane_through(n0 + n1);
   if (lane == 63) {
     red_w[wave] = w;
     red_n[wave] = n;
   }
   __syncthreads();
-  const double front_w = sample_sum_of(red_w, wave);
-  n += sample_sum_of(red_n, wave);
+  const double front_w = sum_of(red_w, wave);
+  n += sum_of(red_n, wave);
   int used = 0;
 #pragma unroll
   for (int q = 0; q < WAVES; ++q) used = max(used, red_last[q]);
@@ -307,7 +257,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     const unsigned long long y = __shfl_xor(best, o, 64);
     best = y > best ? y : best;
   }
-  best = sample_uni(best);
+  best = uniform(best);
   const float top = sample_value(best);
   if (r.greedy || !(top > -INFINITY)) {
     if (t == 0) {
@@ -355,7 +305,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     __syncthreads();
     if (t < C && m.shift[t] < SMP_BINS && t1 - m.shift[t] >= m.head_bins[t]) m.uncovered = 1;
     __syncthreads();
-    const bool heads = sample_uni(m.uncovered) == 0;
+    const bool heads = uniform(m.uncovered) == 0;
     if (heads) {
       for (int s = t; s < C * SMP_HEAD; s += SMP_THREADS) {
         const int c = s / SMP_HEAD;
@@ -400,7 +350,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
             found += __builtin_popcount(code[u][k]);
           }
         }
-        const int ends = sample_through(found);
+        const int ends = lane_through(found);
         unsigned at = 0;
         if (lane == 63) at = atomicAdd(&m.n_list, (unsigned)ends);
         at = (unsigned)__builtin_amdgcn_readlane((int)at, 63) + (unsigned)(ends - found);
@@ -415,7 +365,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       }
     }
     __syncthreads();
-    const int n = sample_uni((int)m.n_list);
+    const int n = uniform((int)m.n_list);
     listed0 = n <= SMP_LIST ? t0 : SMP_BINS;
     listed1 = n <= SMP_LIST ? t1 : -1;
     if (n > SMP_LIST || heads) return;
@@ -433,7 +383,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       if (c >= lo && c <= hi && in_bins(y, bin, bin)) f(c, sample_factor(y - floor(y)));
     };
     if (bin >= listed0 && bin <= listed1) {
-      const int n = sample_uni((int)m.n_list);
+      const int n = uniform((int)m.n_list);
       for (int i = t; i < n; i += SMP_THREADS) take(m.list[i], sample_value(m.list[i]));
     } else {
       for (int i0 = t; i0 < V; i0 += 8 * SMP_THREADS) {  // (more tokens than the list holds)
@@ -467,15 +417,15 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     }
     __syncthreads();
     for (int turn = 0; turn < 8; ++turn) {
-      if (sample_uni((int)m.part_n) <= 64) {
-        each(bin, sample_uni(m.lo), sample_uni(m.hi), [&](unsigned long long c, unsigned long long f) {
+      if (uniform((int)m.part_n) <= 64) {
+        each(bin, uniform(m.lo), uniform(m.hi), [&](unsigned long long c, unsigned long long f) {
           const unsigned at = atomicAdd(&m.n_few, 1u);
           m.few_c[at] = c;
           m.few_w[at] = f;
         });
         __syncthreads();
         if (wave == 0) {
-          const int n = sample_uni((int)m.n_few);
+          const int n = uniform((int)m.n_few);
           const unsigned long long c = lane < n ? m.few_c[lane] : 0, f = lane < n ? m.few_w[lane] : 0;
           unsigned in_front = m.base_n;
           unsigned long long w = m.base_w;
@@ -493,7 +443,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         }
         break;
       }
-      const unsigned long long lo = sample_uni(m.lo), hi = sample_uni(m.hi);
+      const unsigned long long lo = uniform(m.lo), hi = uniform(m.hi);
       const int bits = 64 - __builtin_clzll((hi - lo) | 1), sh = bits > 10 ? bits - 10 : 0;
       m.sub_n[t] = 0;
       m.sub_w[t] = 0;
@@ -511,22 +461,22 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       const int s = SMP_SUB - 1 - t;  // from the front of the order on
       const unsigned own_n = m.sub_n[s];
       const unsigned long long own_w = m.sub_w[s];
-      unsigned n = sample_through(own_n);
-      unsigned long long w = sample_through(own_w);
+      unsigned n = lane_through(own_n);
+      unsigned long long w = lane_through(own_w);
       if (lane == 63) {
         m.red_n[wave] = n;
         m.red_u[wave] = w;
       }
       __syncthreads();
-      n += m.base_n + sample_sum_of(m.red_n, wave);
-      w += m.base_w + sample_sum_of(m.red_u, wave);
+      n += m.base_n + sum_of(m.red_n, wave);
+      w += m.base_w + sum_of(m.red_u, wave);
       const unsigned long long filled = __ballot(own_n > 0), enough = __ballot(own_n > 0 && (rank ? n >= rank : (double)w >= want));
       if (lane == 0) {
         if (enough) atomicMin(&m.hit, t + (int)__builtin_ctzll(enough));
         if (filled) atomicMax(&m.last, t + 63 - (int)__builtin_clzll(filled));
       }
       __syncthreads();
-      const int hit = sample_uni(m.hit), last = sample_uni(m.last);
+      const int hit = uniform(m.hit), last = uniform(m.last);
       if (last < 0) break;
       if (t == (hit < SMP_THREADS ? hit : last)) {
         const unsigned long long at = lo + ((unsigned long long)s << sh), end = at + ((1ull << sh) - 1);
@@ -540,7 +490,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       __syncthreads();
     }
     __syncthreads();
-    return sample_uni(m.found);
+    return uniform(m.found);
   };
   // ---- what is kept: the bins in front of `cut_bin`, and of that one the tokens at `cut` or in front of it
   int cut_bin = SMP_BINS;
@@ -553,23 +503,23 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     const unsigned long long yes = __ballot(t < SMP_BINS && ok(t < SMP_BINS ? t : 0));
     if (lane == 0 && yes) atomicMin(&m.hit, t + (int)__builtin_ctzll(yes));
     __syncthreads();
-    return sample_uni(m.hit);
+    return uniform(m.hit);
   };
   auto cut_at = [&](int bin, unsigned long long from, unsigned rank, double want) {
     cut = last_kept(bin, from, rank, want);
     cut_bin = bin;
-    partial = (double)sample_uni(m.kept_w) * sample_eighths(bin);
+    partial = (double)uniform(m.kept_w) * sample_eighths(bin);
   };
   if (r.k < V) {
     const int h = first_bin([&](int i) { return m.through_n[i] >= r.k; });
     if (h < SMP_BINS) {
-      const int through = sample_uni(m.through_n[h]);
+      const int through = uniform(m.through_n[h]);
       if (through == r.k) {
         cut_bin = h + 1;
         cut = ~0ull;
       } else {
         gather(through <= SMP_SHORT ? 0 : h, h);
-        cut_at(h, 0, (unsigned)(r.k - (h > 0 ? sample_uni(m.through_n[h - 1]) : 0)), 0);
+        cut_at(h, 0, (unsigned)(r.k - (h > 0 ? uniform(m.through_n[h - 1]) : 0)), 0);
       }
     }
   }
@@ -579,7 +529,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     const bool inside = h < SMP_BINS;
     if (inside || (cut_bin < SMP_BINS && cut != ~0ull)) {
       const int bin = inside ? h : cut_bin;
-      if (bin < listed0 || bin > listed1) gather(sample_uni(m.through_n[bin]) <= SMP_SHORT ? 0 : bin, bin);
+      if (bin < listed0 || bin > listed1) gather(uniform(m.through_n[bin]) <= SMP_SHORT ? 0 : bin, bin);
       cut_at(bin, inside ? 0 : cut, 0, (want - (bin > 0 ? m.through_w[bin - 1] : 0)) / sample_eighths(bin));
     }
   }
@@ -587,7 +537,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   if (r.low > 0.f) {
     const double d = first - floor(y_top + 8 * log2((double)r.low));
     w_least = fmax(w_least, (double)r.low * w_top);
-    const int bin = sample_uni(d < SMP_BINS ? (int)d : SMP_BINS);
+    const int bin = uniform(d < SMP_BINS ? (int)d : SMP_BINS);
     if (bin < cut_bin) {
       cut_bin = bin;
       cut = 0;
@@ -600,13 +550,13 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
   u = u > 0.f ? fminf(u, 1.f) : 0.f;
   // ---- few tokens: those that are kept, put into the order of their indexes, and the sums over them
-  if (cut_bin < SMP_BINS && sample_uni(m.through_n[cut_bin]) <= SMP_SHORT) {
+  if (cut_bin < SMP_BINS && uniform(m.through_n[cut_bin]) <= SMP_SHORT) {
     if (listed0 > 0 || cut_bin > listed1) gather(0, cut_bin);
     __syncthreads();
     if (t < SMP_FEW) m.rank[t] = 0;
     if (t == 0) m.n_few = 0;
     __syncthreads();
-    const int n_list = listed0 == 0 && cut_bin <= listed1 ? sample_uni((int)m.n_list) : 0;  // (0: more may be there than the list holds)
+    const int n_list = listed0 == 0 && cut_bin <= listed1 ? uniform((int)m.n_list) : 0;  // (0: more may be there than the list holds)
     for (int i = t; i < n_list; i += SMP_THREADS) {
       const unsigned long long c = m.list[i];
       const double y = (double)sample_value(c) * r.rate, low = floor(y), d = first - low;
@@ -620,7 +570,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       }
     }
     __syncthreads();
-    const int n = sample_uni((int)m.n_few);
+    const int n = uniform((int)m.n_few);
     if (n > 0 && n <= SMP_FEW) {
       constexpr int PARTS = SMP_THREADS / SMP_FEW;
       const int i = t % SMP_FEW, part = t / SMP_FEW;
@@ -642,8 +592,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
           id[q] = (int)m.few_c[from];
           sum += w[q];
         }
-        double run = sample_through(sum);
-        const double total = sample_last(run), want = (double)u * total;
+        double run = lane_through(sum);
+        const double total = lane_value(run, 63), want = (double)u * total;
         run -= sum;
         int hit = PAIR;
 #pragma unroll
@@ -681,7 +631,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   }
   __syncthreads();
   mine += (double)m.chunk_in[lane] * sample_eighths(cut_bin);
-  const double ends = sample_through(mine), total = sample_last(ends);
+  const double ends = lane_through(mine), total = lane_value(ends, 63);
   const double want = (double)u * total;
   const unsigned long long past = __ballot(mine > 0.0 && ends > want), some = __ballot(mine > 0.0);  // (the same in every wave)
   if (wave == 0) m.before[lane] = ends - mine;
@@ -698,7 +648,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       w[j] = v > -INFINITY && d < SMP_BINS ? kept(sample_factor(y - low), (int)d, sample_place(v, i0 + j)) : 0.0;
       sum += w[j];
     }
-    double run = sample_through(sum);
+    double run = lane_through(sum);
     __syncthreads();
     if (lane == 63) m.red_d[wave] = run;
     if (t == 0) {
@@ -706,7 +656,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       m.last = -1;
     }
     __syncthreads();
-    run = (run - sum) + (m.before[c] + sample_sum_of(m.red_d, wave));
+    run = (run - sum) + (m.before[c] + sum_of(m.red_d, wave));
     int hit = 0x7fffffff, last = -1;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -719,7 +669,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     if (hit != 0x7fffffff) atomicMin(&m.where, hit);
     if (last >= 0) atomicMax(&m.last, last);
     __syncthreads();
-    const int id = sample_uni(m.where != 0x7fffffff ? m.where : m.last);
+    const int id = uniform(m.where != 0x7fffffff ? m.where : m.last);
     if (id < 0) continue;
 #pragma unroll
     for (int j = 0; j < N; ++j)
