@@ -143,7 +143,8 @@ __device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int co
 //   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
 // PAGED16: page_size is a multiple of 16, so that a 16-key tile lies in one page and its address is a scalar; otherwise a lane looks up its own keys' places.
 // FULL: head_dim = DH; otherwise what a lane would load behind a row's end is replaced by zeros.
-template <typename T, int DH, bool PAGED16, bool FULL, int WAVES>
+// ONCE: K and V are more than the last-level cache holds, so what goes through it is not kept there.
+template <typename T, int DH, bool PAGED16, bool FULL, int WAVES, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_kernel(PagedAttend a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES;
@@ -217,6 +218,10 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
     const unsigned lo = __shfl((int)off_lo, j, 64), hi = __shfl((int)off_hi, j, 64);
     return (int)hi < 0 ? 0ll : (long long)lo | (long long)hi << 32;
   };
+  auto load = [](auto *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+  };
   auto load_k = [&]() {
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
@@ -226,7 +231,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
       for (int i = 0; i < KP; ++i) {
         const int at = 64 * i + 16 * q4;
         const bool there = FULL || at < row_bytes;
-        kr[t][i] = *(const at_u4 *)(p + (there ? at : 0));
+        kr[t][i] = load((const at_u4 *)(p + (there ? at : 0)));
         if (!there) kr[t][i] = at_u4{0, 0, 0, 0};
       }
     }
@@ -241,8 +246,8 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
       for (int u = 0; u < VH; ++u) {
         const int at = 16 * VW * u + VW * c16;
         const char *from = p + (FULL || at < row_bytes ? at : 0);  // (channels behind the row's end are never stored)
-        if constexpr (VW == 16) *(at_u4 *)vr[j][u] = *(const at_u4 *)from;
-        else *(at_u2 *)vr[j][u] = *(const at_u2 *)from;
+        if constexpr (VW == 16) *(at_u4 *)vr[j][u] = load((const at_u4 *)from);
+        else *(at_u2 *)vr[j][u] = load((const at_u2 *)from);
       }
     }
   };
@@ -460,9 +465,14 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
 }
 
 // ---- host side ------------------------------------------------------------------------------------------
-// Workgroups for all keys together: about two per compute unit, which is what fits.  A row of a cache of up to AT_WHOLE positions is not cut: the second launch
-// would cost more than the few blocks of keys that a wave has left.
-constexpr int AT_WGS = 512, AT_WHOLE = 512;
+// Workgroups for all keys together: as many as are resident at once, which goes by the registers that a head_dim takes.  512 or 1024 of them at 8 kv heads: 64 channels,
+// 16 rows of 8000 56 / 48 us, 128 channels, 8 rows of 2048 19.3 / 21.9, 64 rows of 1000 47.8 / 52.5; 256: 22.5, 47.3, two rows of 131072 262 (512: 189).
+// A row of a cache of up to AT_WHOLE positions is not cut: the second launch would cost more than the few blocks of keys that a wave has left.
+// ONCE where a layer's K and V pages are more than AT_CACHED bytes, in kernels whose loads are all of whole rows: two rows of 131072 (1.07 GB) 167 us, 189 without; a batch
+// of 32 whose 99 MB stay cached between calls 32.7 us, 29.0 without.
+constexpr int AT_WHOLE = 512;
+constexpr size_t AT_CACHED = (size_t)256 << 20;
+static int at_workgroups(int dh) { return dh <= 64 ? 1024 : dh <= 128 ? 512 : 256; }
 struct AtPlan {
   int target, items, tiles;
   size_t bytes;
@@ -473,7 +483,7 @@ static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
   const long long cap = (long long)max_blocks * p.page_size;
   r.items = B;
   if (cap > AT_WHOLE) {
-    r.target = std::max(1, AT_WGS / (p.n_kv_heads * r.tiles));
+    r.target = std::max(1, at_workgroups(p.head_dim) / (p.n_kv_heads * r.tiles));
     r.items = (int)std::min<long long>((long long)r.target + B, B * ((cap + AT_PIECE - 1) / AT_PIECE));
     r.bytes = (size_t)r.items * Hq * (p.head_dim + 4) * 4;
   }
@@ -490,9 +500,13 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8;
   {
     ProfScope ps("paged_attend", s);
+    bool once = false;
+    if constexpr (PAGED16 && FULL) once = 2 * (size_t)a.n_pages * a.Hkv * a.page * a.dh * sizeof(T) > AT_CACHED;
     if constexpr (DH <= 128)
-      if (wide) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WHOLE_WAVES><<<grid, 64 * AT_WHOLE_WAVES, lds(AT_WHOLE_WAVES), s>>>(a);
-    if (!wide) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WAVES><<<grid, 64 * AT_WAVES, lds(AT_WAVES), s>>>(a);
+      if (wide) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WHOLE_WAVES, false><<<grid, 64 * AT_WHOLE_WAVES, lds(AT_WHOLE_WAVES), s>>>(a);
+    if constexpr (PAGED16 && FULL)
+      if (!wide && once) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WAVES, true><<<grid, 64 * AT_WAVES, lds(AT_WAVES), s>>>(a);
+    if (!wide && !once) paged_attend_kernel<T, DH, PAGED16, FULL, AT_WAVES, false><<<grid, 64 * AT_WAVES, lds(AT_WAVES), s>>>(a);
   }
   if (plan.target > 0) {
     ProfScope ps("paged_join", s);

@@ -2,6 +2,7 @@
 // lengths (la_page_map) and the rows' way into the pages (la_paged_write); the attention that reads them is in la_attend.hip.
 #include <algorithm>
 
+#include "la_lanes.h"
 #include "la_paged.h"
 
 namespace la {
@@ -28,79 +29,77 @@ struct PageMap {
   int32_t *first;
 };
 
-__device__ __forceinline__ long long wave_sum(long long v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
 __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(PageMap a) {
-  __shared__ long long red[MAP_THREADS / 64][6], ends[3][MAP_THREADS];  // sums over waves; inclusive sums over the group's requests: rows, taken, given
-  __shared__ int old_s[MAP_THREADS], had_s[MAP_THREADS];
-  __shared__ int bad_s;
-  const int t = threadIdx.x, wave = t >> 6;
+  constexpr int WAVES = MAP_THREADS / 64;
+  __shared__ long long red[WAVES][9], ends[3][MAP_THREADS];  // sums over waves; inclusive sums over the group's requests: rows, taken, given
+  __shared__ int old_s[MAP_THREADS], had_s[MAP_THREADS], bad_s[WAVES];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
   const int r0 = (int)blockIdx.x * a.per_group, nr = a.R - r0 < a.per_group ? a.R - r0 : a.per_group;
-  auto up = [&](int x) { return (int)(((long long)x + a.page - 1) / a.page); };
-  if (t == 0) bad_s = 0;
-  __syncthreads();
-  long long in_front[3] = {0, 0, 0}, total[3] = {0, 0, 0};
+  const int head = a.heads_in[0], n_free = a.heads_in[1];
   const long long cap = (long long)a.max_blocks * a.page;
+  auto up = [&](int x) { return (int)(((unsigned)x + (unsigned)a.page - 1u) / (unsigned)a.page); };  // (x < 2^31, page < 2^31)
+  // rows, taken and given pages of a request of which both lengths are in range
+  auto steps = [&](int x, int y, long long (&v)[3]) {
+    const int d = up(y) - up(x);
+    v[0] = y > x ? y - x : 0;
+    v[1] = d > 0 ? d : 0;
+    v[2] = d < 0 ? -d : 0;
+  };
+  int x = 0, y = 0;
+  if (t < nr) {
+    x = a.old_len[r0 + t];
+    y = a.new_len[r0 + t];
+  }
+  long long in_front[3] = {0, 0, 0}, total[3] = {0, 0, 0}, own[3];
   bool bad = false;
   for (int r = t; r < a.R; r += MAP_THREADS) {
-    const int x = a.old_len[r], y = a.new_len[r];
-    if (x < 0 || y < 0 || x > cap || y > cap) {
+    const int p = a.old_len[r], q = a.new_len[r];
+    if (p < 0 || q < 0 || p > cap || q > cap) {
       bad = true;
       continue;
     }
-    const int d = up(y) - up(x);
-    const long long v[3] = {y > x ? y - x : 0, d > 0 ? d : 0, d < 0 ? -d : 0};
+    long long v[3];
+    steps(p, q, v);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       total[i] += v[i];
       if (r < r0) in_front[i] += v[i];
     }
   }
-  if (bad) bad_s = 1;
+  steps(x < 0 ? 0 : x, y < 0 ? 0 : y, own);  // (nothing is done with what is out of range)
+  old_s[t] = x;
+  had_s[t] = up(x < 0 ? 0 : x);
+  const unsigned long long bads = __ballot(bad);
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const long long f = wave_sum(in_front[i]), s = wave_sum(total[i]);
-    if ((t & 63) == 0) {
+    own[i] = lane_through(own[i]);
+    const long long f = lane_through(in_front[i]), s = lane_through(total[i]);
+    if (lane == 63) {
       red[wave][i] = f;
       red[wave][3 + i] = s;
+      red[wave][6 + i] = own[i];
     }
   }
-  int x = 0, y = 0;
-  if (t < nr) {
-    x = a.old_len[r0 + t];
-    y = a.new_len[r0 + t];
-  }
-  const int d = up(y) - up(x);
-  old_s[t] = x;
-  had_s[t] = up(x);
-  ends[0][t] = y > x ? y - x : 0;
-  ends[1][t] = d > 0 ? d : 0;
-  ends[2][t] = d < 0 ? -d : 0;
+  if (lane == 0) bad_s[wave] = bads != 0;
   __syncthreads();
+  bool any_bad = false;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     in_front[i] = total[i] = 0;
-    for (int w = 0; w < MAP_THREADS / 64; ++w) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
       in_front[i] += red[w][i];
       total[i] += red[w][3 + i];
+      if (w < wave) own[i] += red[w][6 + i];
     }
+    ends[i][t] = own[i];
   }
-  for (int o = 1; o < nr; o <<= 1) {
-    long long v[3];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) v[i] = t >= o ? ends[i][t - o] : 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 3; ++i) ends[i][t] += v[i];
-    __syncthreads();
-  }
-  const int head = a.heads_in[0], n_free = a.heads_in[1];
+  for (int w = 0; w < WAVES; ++w) any_bad = any_bad || bad_s[w];
+  __syncthreads();
   int error = 0;
   if (head < 0 || head >= a.n_pages || n_free < 0 || n_free > a.n_pages) error = 4;
-  else if (bad_s) error = 3;
+  else if (any_bad) error = 3;
   else if (total[0] > a.max_rows) error = 2;
   else if (total[1] > n_free) error = 1;
   const int part = blockIdx.y, parts = gridDim.y, stride = parts * MAP_THREADS, k0 = part * MAP_THREADS + t;
@@ -188,10 +187,10 @@ extern "C" int la_page_map(const int32_t *old_len, const int32_t *new_len, int R
   LA_REQUIRE(table_stride >= max_blocks || R == 1, LA_EINVAL, "table rows overlap");
   LA_REQUIRE((long long)n_pages * page_size < (1ll << 31), LA_EINVAL, "%d pages of %d positions: slots are 32-bit numbers", n_pages, page_size);
   hipStream_t s = (hipStream_t)stream;
-  // 16 requests a workgroup (more where there are very many, each of which reads all lengths), in as many parts as give a thread eight rows
+  // 16 requests a workgroup (more where there are very many, each of which reads all lengths), in as many parts as give a thread two rows
   int per_group = 16;
   while (per_group < MAP_THREADS && R / per_group > 64) per_group *= 2;
-  const int groups = ceil_div(R, per_group), parts = std::min(64, std::max(1, max_rows / (groups * MAP_THREADS * 8)));
+  const int groups = ceil_div(R, per_group), parts = std::min(64, std::max(1, max_rows / (groups * MAP_THREADS * 2)));
   const PageMap a{old_len, new_len, R, per_group, page_size, table, table_stride, max_blocks, ring, n_pages, heads_in, heads_out, slot, pos, req, max_rows, first};
   ProfScope ps("page_map", s);
   page_map_kernel<<<dim3(groups, parts), MAP_THREADS, 0, s>>>(a);
