@@ -12,7 +12,6 @@ namespace la {
 constexpr int SMP_BINS = 514, SMP_HIST = 520;  // (64 octaves below the largest token end in the 514th bin at the latest); row length of a chunk's sums
 constexpr int SMP_SUM_THREADS = 512;          // of a workgroup of the first launch
 constexpr int SMP_PER = 16, SMP_PER_SHORT = 4;  // ... tokens of each: chunks of 8192 and of 2048
-constexpr int SMP_HEAD = 64;                  // a chunk's first tokens, whole bins of them, that the first launch lists
 constexpr int SMP_LIST = 4608;                // tokens of a cut that fit into LDS
 constexpr int SMP_SHORT = 1024, SMP_FEW = 128;  // tokens down to a cut that are listed with it, a thread each; of them kept that are drawn from without looking at a chunk
 constexpr int SMP_SUB = 1024;                 // parts that a range of tokens is cut into at a time
@@ -21,7 +20,6 @@ constexpr unsigned long long SMP_SUM_MASK = (1ull << SMP_COUNT_SHIFT) - 1;
 constexpr double SMP_UNIT = 0x1p36, LEAST_WEIGHT = 0x1p-64;
 constexpr int SMP_MOST = SMP_SUM_THREADS * SMP_PER;
 static_assert(SMP_MOST * 1.1 * SMP_UNIT < (double)SMP_SUM_MASK && SMP_MOST <= 1 << 13, "a chunk in one bin");
-static_assert(64 * SMP_HEAD <= SMP_LIST, "all chunks' first tokens");
 static_assert(LA_MAX_SAMPLE_VOCAB * 1.1 * SMP_UNIT < 0x1p64 && LA_MAX_SAMPLE_VOCAB / SMP_MOST <= 64, "a row in one bin; a lane per chunk");
 // Short chunks while that leaves a row at most 16 of them: the first launch has four times the workgroups, the second reads as many sums.
 static int sample_per(int V) { return V <= 16 * SMP_SUM_THREADS * SMP_PER_SHORT ? SMP_PER_SHORT : SMP_PER; }
@@ -33,14 +31,12 @@ struct Sample {
   la_sampling p;
   int32_t *ids;
   float *prob;
-  // per row and chunk: its first token in order; sums of weights and numbers of tokens of the bins down to each [SMP_HIST], from that token's bin on; every token's bin from
-  // there on (255: further down, or no token), thread by thread
+  // per row and chunk: its first token in order; sums of weights and numbers of tokens of the bins down to each [SMP_HIST], from that token's bin on, up to the last bin that
+  // has a token; its tokens by bin, as places in the chunk
   unsigned long long *best;
   double *sums;
-  int32_t *counts;
-  uint8_t *bins;
-  unsigned long long *head;  // [SMP_HEAD] the places of its first tokens ...
-  int4 *heads;               // ... the bins they make up, from the first one, and their number; the bins up to the last that has a token
+  int32_t *counts, *used;
+  uint16_t *sorted;
 };
 
 // A logit as it counts: NaN like -inf (no token), +inf like the largest finite value, -0 like 0.
@@ -115,7 +111,8 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   __shared__ __attribute__((aligned(16))) unsigned long long hist[SMP_HIST];
   __shared__ unsigned long long red[WAVES];
   __shared__ double red_w[WAVES];
-  __shared__ int red_n[WAVES], red_last[WAVES], n_head, head_bins;
+  __shared__ int red_n[WAVES], red_last[WAVES], before[SMP_HIST];
+  __shared__ __attribute__((aligned(16))) uint16_t sorted[CHUNK];
   const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, wave = t >> 6, lane = t & 63, i0 = c * CHUNK + t;
   const T *x = (const T *)a.x + b * a.ld;
   float v[PER];
@@ -141,10 +138,6 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   }
   unsigned long long best = sample_place(top_v, top_i);
   if (lane == 0) red[wave] = best;
-  if (t == 0) {
-    n_head = 0;
-    head_bins = 0;
-  }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) best = red[w] > best ? red[w] : best;
@@ -154,19 +147,16 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   const float top = sample_value(best);
   if (r.greedy || !(top > -INFINITY)) return;
   const double first = floor((double)top * r.rate);
-  uint32_t code[(PER + 3) / 4] = {};
-  int bin[PER];
+  int at_bin[PER];  // bin and, from bit 10 on, the number of its tokens that were counted before
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const double y = (double)v[j] * r.rate, low = floor(y), d = first - low;
-    const bool in = v[j] > -INFINITY && d < SMP_BINS;
-    bin[j] = in ? (int)d : SMP_BINS;
-    if (in) atomicAdd(&hist[bin[j]], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low));
-    code[j / 4] |= (uint32_t)min(bin[j], 255) << (8 * (j % 4));
+    at_bin[j] = -1;
+    if (v[j] > -INFINITY && d < SMP_BINS) {
+      const int bin = (int)d;
+      at_bin[j] = bin | (int)(atomicAdd(&hist[bin], (1ull << SMP_COUNT_SHIFT) + sample_factor(y - low)) >> SMP_COUNT_SHIFT) << 10;
+    }
   }
-  uint32_t *codes = (uint32_t *)(a.bins + at * CHUNK) + t * (PER / 4);
-  if constexpr (PER == 16) *(uint4 *)codes = uint4{code[0], code[1], code[2], code[3]};
-  else *codes = code[0];
   __syncthreads();
   // sums from the front, two bins a thread
   const bool own = 2 * t < SMP_HIST;
@@ -189,25 +179,28 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
     red_n[wave] = n;
   }
   __syncthreads();
+  // (a place is written once: by the token that the atomics gave its number; which of a bin's tokens that is changes nothing)
   const double front_w = sum_of(red_w, wave);
   n += sum_of(red_n, wave);
   int used = 0;
 #pragma unroll
   for (int q = 0; q < WAVES; ++q) used = max(used, red_last[q]);
+  if (own) {
+    before[2 * t] = n - n1 - n0;
+    before[2 * t + 1] = n - n1;
+  }
   if (2 * t < used) {
     *(double2 *)(a.sums + at * SMP_HIST + 2 * t) = double2{front_w + (w - w1), front_w + w};
     *(int2 *)(a.counts + at * SMP_HIST + 2 * t) = int2{n - n1, n};
   }
-  // (the numbers only grow: how many bins stay within SMP_HEAD is the first one that does not)
-  const int in_head = __builtin_popcountll(__ballot(own && n - n1 <= SMP_HEAD)) + __builtin_popcountll(__ballot(own && n <= SMP_HEAD));
-  if (lane == 0 && in_head) atomicAdd(&head_bins, in_head);
+  if (t == 0) a.used[at] = used;
   __syncthreads();
-  const int bins = head_bins;
 #pragma unroll
   for (int j = 0; j < PER; ++j)
-    if (bin[j] < bins && bin[j] < SMP_BINS) a.head[at * SMP_HEAD + atomicAdd(&n_head, 1)] = sample_place(v[j], i0 + SMP_SUM_THREADS * j);
+    if (at_bin[j] >= 0) sorted[before[at_bin[j] & 1023] + (at_bin[j] >> 10)] = (uint16_t)(t + SMP_SUM_THREADS * j);
   __syncthreads();
-  if (t == 0) a.heads[at] = int4{bins, n_head, used, 0};
+  const int all = before[SMP_HIST - 1];  // (the last bin is past any token)
+  for (int q = t; 8 * q < all; q += SMP_SUM_THREADS) *(uint4 *)(a.sorted + at * CHUNK + 8 * q) = *(const uint4 *)(sorted + 8 * q);
 }
 
 // Second launch, a workgroup per row: where the filters cut, what is left of every chunk, and in the chunk where u falls the token.
@@ -225,11 +218,11 @@ struct SampleShared {
   unsigned long long red_u[SMP_WAVES];
   unsigned red_n[SMP_WAVES];
   unsigned long long lo, hi, base_w, kept_w, found;
-  unsigned n_list, base_n, part_n, n_few;
-  int hit, last, where, uncovered;
+  unsigned base_n, part_n, n_few;
+  int hit, last, where;
   unsigned long long few_c[SMP_FEW], few_w[SMP_FEW];
   int rank[SMP_FEW];
-  int head_bins[64], head_n[64], used[64];
+  int used[64], from[64], ends[64];  // of a bin: where its tokens begin in each chunk's, how many there are up to and with each
   double eighths[8];
 };
 
@@ -244,10 +237,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     unsigned long long best = t < C ? a.best[(size_t)b * C + t] : 0;
     m.best[t] = best;
     m.chunk_in[t] = 0;
-    const int4 h = t < C && !r.greedy ? a.heads[(size_t)b * C + t] : int4{0, 0, 0, 0};  // (a chunk without a token has none of its own, and is never looked at)
-    m.head_bins[t] = h.x;
-    m.head_n[t] = h.y;
-    m.used[t] = h.z;
+    m.used[t] = t < C && !r.greedy ? a.used[(size_t)b * C + t] : 0;  // (a chunk without a token has none of its own, and is never looked at)
     if (t < 8) m.eighths[t] = sample_eighths(t);
   }
   __syncthreads();
@@ -292,87 +282,40 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   }
   __syncthreads();
   auto in_bins = [&](double y, int t0, int t1) { return y >= first - t1 && (t0 == 0 || y < first - t0 + 1); };
-  int listed0 = SMP_BINS, listed1 = -1;  // bins whose tokens are in the list
-  // Tokens of bins t0 .. t1 into the list, if they fit: from the chunks' first tokens where those reach that far.  Otherwise the first launch's
-  // bytes say which tokens may be there (255: perhaps); only their logits are read, all at once.
+  int listed0 = SMP_BINS, listed1 = -1, n_list = 0;  // bins whose tokens are in the list, how many they are
+  // Where the tokens of bins t0 .. t1 lie; their number.
+  auto slices = [&](int t0, int t1) {
+    __syncthreads();
+    if (wave == 0) {
+      const int shift = lane < C ? m.shift[lane] : SMP_BINS, top = m.used[lane] - 1, l0 = t0 - 1 - shift, l1 = t1 - shift;
+      const bool any = l1 >= 0 && shift < SMP_BINS;
+      const int32_t *n = counts + (any ? lane * SMP_HIST : 0);
+      const int from = any && l0 >= 0 ? n[min(l0, top)] : 0, end = any ? n[min(l1, top)] : 0;
+      m.from[lane] = from;
+      m.ends[lane] = lane_through(end - from);
+    }
+    __syncthreads();
+    return uniform(m.ends[63]);
+  };
+  // The i-th of them: its index.
+  auto nth = [&](int i) {
+    int lo = 0, hi = C - 1;
+    while (lo < hi) {
+      const int c = (lo + hi) / 2;
+      if (m.ends[c] > i) hi = c; else lo = c + 1;
+    }
+    return lo * CHUNK + a.sorted[((size_t)b * C + lo) * CHUNK + m.from[lo] + i - (lo > 0 ? m.ends[lo - 1] : 0)];
+  };
+  // Tokens of bins t0 .. t1 into the list, if they fit.
   auto gather = [&](int t0, int t1) {
-    constexpr int N = 8, WORDS = PER / 4;
-    __syncthreads();
-    if (t == 0) {
-      m.n_list = 0;
-      m.uncovered = 0;
-    }
-    __syncthreads();
-    if (t < C && m.shift[t] < SMP_BINS && t1 - m.shift[t] >= m.head_bins[t]) m.uncovered = 1;
-    __syncthreads();
-    const bool heads = uniform(m.uncovered) == 0;
-    if (heads) {
-      for (int s = t; s < C * SMP_HEAD; s += SMP_THREADS) {
-        const int c = s / SMP_HEAD;
-        if (m.shift[c] < SMP_BINS && s % SMP_HEAD < m.head_n[c]) {
-          const unsigned long long place = a.head[(size_t)b * C * SMP_HEAD + s];
-          if (in_bins((double)sample_value(place) * r.rate, t0, t1)) m.list[atomicAdd(&m.n_list, 1u)] = place;  // (64 of 64 chunks at most)
-        }
-      }
-    } else {
-      const uint32_t *codes = (const uint32_t *)(a.bins + (size_t)b * C * CHUNK);
-      for (int s0 = t - lane; s0 < C * SMP_SUM_THREADS; s0 += N * SMP_THREADS) {  // (whole waves)
-        uint32_t code[N][WORDS];
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-          const int s = (s0 + u * SMP_THREADS < C * SMP_SUM_THREADS ? s0 + u * SMP_THREADS : s0) + lane;
-          if constexpr (PER == 16) {
-            const uint4 w = *(const uint4 *)(codes + (size_t)s * WORDS);
-            code[u][0] = w.x; code[u][1] = w.y; code[u][2] = w.z; code[u][3] = w.w;
-          } else {
-            code[u][0] = codes[s];
-          }
-        }
-        // of each word, the top bits of the bytes that may be meant
-        int found = 0;
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-          const int s = s0 + u * SMP_THREADS, shift = s < C * SMP_SUM_THREADS ? m.shift[s / SMP_SUM_THREADS] : SMP_BINS;
-          const unsigned lo = t0 > shift ? (t0 - shift < 255 ? t0 - shift : 255) : 0, hi = t1 - shift < 255 ? t1 - shift : 255;
-          const bool any = t1 >= shift && shift < SMP_BINS;
-#pragma unroll
-          for (int k = 0; k < WORDS; ++k) {
-            const uint32_t w = code[u][k];
-            uint32_t z;
-            if (t0 == t1) {  // bytes equal to one: what they differ in by is 0
-              const uint32_t d = w ^ (lo * 0x01010101u);
-              z = ~(((d & 0x7f7f7f7fu) + 0x7f7f7f7fu) | d | 0x7f7f7f7fu);
-            } else {  // every second byte in 16 bits: bit 8 of 256 + hi - byte and of 256 + byte - lo
-              const uint32_t e = w & 0x00ff00ffu, o = (w >> 8) & 0x00ff00ffu, high = (256 + hi) * 0x00010001u, low = (256 - lo) * 0x00010001u;
-              z = ((high - e) & (e + low) & 0x01000100u) >> 1 | ((high - o) & (o + low) & 0x01000100u) << 7;
-            }
-            code[u][k] = any ? z : 0u;
-            found += __builtin_popcount(code[u][k]);
-          }
-        }
-        const int ends = lane_through(found);
-        unsigned at = 0;
-        if (lane == 63) at = atomicAdd(&m.n_list, (unsigned)ends);
-        at = (unsigned)__builtin_amdgcn_readlane((int)at, 63) + (unsigned)(ends - found);
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-          const int s = s0 + u * SMP_THREADS + lane, i0 = s / SMP_SUM_THREADS * CHUNK + s % SMP_SUM_THREADS;
-#pragma unroll
-          for (int k = 0; k < WORDS; ++k)
-            for (uint32_t z = code[u][k]; z; z &= z - 1, ++at)
-              if (at < SMP_LIST) m.list[at] = (unsigned)(i0 + SMP_SUM_THREADS * (4 * k + (__builtin_ctz(z) >> 3)));
-        }
-      }
-    }
-    __syncthreads();
-    const int n = uniform((int)m.n_list);
+    const int n = slices(t0, t1);
     listed0 = n <= SMP_LIST ? t0 : SMP_BINS;
     listed1 = n <= SMP_LIST ? t1 : -1;
-    if (n > SMP_LIST || heads) return;
+    n_list = n;
+    if (n > SMP_LIST) return;
     for (int i = t; i < n; i += SMP_THREADS) {
-      const int at = (int)m.list[i];
-      const float v = at < V ? sample_logit<T>(x + at) : -INFINITY;
-      m.list[i] = v > -INFINITY && in_bins((double)v * r.rate, t0, t1) ? sample_place(v, at) : 0;  // (0 is the place of no token: its value is none, and in no bin)
+      const int at = nth(i);
+      m.list[i] = sample_place(sample_logit<T>(x + at), at);
     }
     __syncthreads();
   };
@@ -383,16 +326,19 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       if (c >= lo && c <= hi && in_bins(y, bin, bin)) f(c, sample_factor(y - floor(y)));
     };
     if (bin >= listed0 && bin <= listed1) {
-      const int n = uniform((int)m.n_list);
-      for (int i = t; i < n; i += SMP_THREADS) take(m.list[i], sample_value(m.list[i]));
-    } else {
-      for (int i0 = t; i0 < V; i0 += 8 * SMP_THREADS) {  // (more tokens than the list holds)
-        float v[8];
+      for (int i = t; i < n_list; i += SMP_THREADS) take(m.list[i], sample_value(m.list[i]));
+    } else {  // (more tokens than the list holds)
+      const int n = slices(bin, bin);
+      for (int i0 = t; i0 < n; i0 += 4 * SMP_THREADS) {
+        int at[4];
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = i0 + SMP_THREADS * j < V ? sample_logit<T>(x + i0 + SMP_THREADS * j) : -INFINITY;
+        for (int j = 0; j < 4; ++j) at[j] = i0 + SMP_THREADS * j < n ? nth(i0 + SMP_THREADS * j) : -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (v[j] > -INFINITY) take(sample_place(v[j], i0 + SMP_THREADS * j), v[j]);
+        for (int j = 0; j < 4; ++j) v[j] = at[j] >= 0 ? sample_logit<T>(x + at[j]) : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (at[j] >= 0) take(sample_place(v[j], at[j]), v[j]);
       }
     }
   };
@@ -556,11 +502,10 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     if (t < SMP_FEW) m.rank[t] = 0;
     if (t == 0) m.n_few = 0;
     __syncthreads();
-    const int n_list = listed0 == 0 && cut_bin <= listed1 ? uniform((int)m.n_list) : 0;  // (0: more may be there than the list holds)
     for (int i = t; i < n_list; i += SMP_THREADS) {
       const unsigned long long c = m.list[i];
       const double y = (double)sample_value(c) * r.rate, low = floor(y), d = first - low;
-      const double w = c && d < SMP_BINS ? kept(sample_factor(y - low), (int)d, c) : 0.0;
+      const double w = d < SMP_BINS ? kept(sample_factor(y - low), (int)d, c) : 0.0;
       if (w > 0.0) {
         const unsigned at = atomicAdd(&m.n_few, 1u);
         if (at < SMP_FEW) {
@@ -640,12 +585,19 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     if (!((some >> c) & 1)) continue;
     constexpr int N = CHUNK / SMP_THREADS;
     const int i0 = c * CHUNK + t * N;
+    const double y_least = first - (cut_bin < SMP_BINS ? cut_bin : SMP_BINS - 1);  // (of a token that can be kept)
+    float v[N];
     double w[N], sum = 0;
 #pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = i0 + j < V ? sample_logit<T>(x + i0 + j) : -INFINITY;
+#pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float v = i0 + j < V ? sample_logit<T>(x + i0 + j) : -INFINITY;
-      const double y = (double)v * r.rate, low = floor(y), d = first - low;
-      w[j] = v > -INFINITY && d < SMP_BINS ? kept(sample_factor(y - low), (int)d, sample_place(v, i0 + j)) : 0.0;
+      const double y = (double)v[j] * r.rate;
+      w[j] = 0.0;
+      if (v[j] > -INFINITY && y >= y_least) {
+        const double low = floor(y);
+        w[j] = kept(sample_factor(y - low), (int)(first - low), sample_place(v[j], i0 + j));
+      }
       sum += w[j];
     }
     double run = lane_through(sum);
@@ -691,7 +643,7 @@ using namespace la;
 
 struct SampleLayout {
   int per, chunks;
-  size_t sums, counts, heads, head, bins, total;  // byte offsets behind the first tokens, size of all
+  size_t sums, counts, used, sorted, total;  // byte offsets behind the first tokens, size of all
 };
 static SampleLayout sample_layout(int B, int V) {
   SampleLayout l{};
@@ -700,10 +652,9 @@ static SampleLayout sample_layout(int B, int V) {
   const size_t n = (size_t)B * l.chunks;
   l.sums = (n * 8 + 15) / 16 * 16;
   l.counts = l.sums + n * SMP_HIST * 8;
-  l.heads = l.counts + n * SMP_HIST * 4;
-  l.head = l.heads + n * 16;
-  l.bins = l.head + n * SMP_HEAD * 8;
-  l.total = l.bins + n * SMP_SUM_THREADS * l.per;
+  l.used = l.counts + n * SMP_HIST * 4;
+  l.sorted = (l.used + n * 4 + 15) / 16 * 16;
+  l.total = l.sorted + n * SMP_SUM_THREADS * l.per * 2;
   return l;
 }
 static_assert(SMP_HIST % 4 == 0, "16-byte aligned parts");
@@ -745,8 +696,8 @@ extern "C" int la_sample(const void *logits, int dtype, int64_t row_stride, int 
   LA_REQUIRE((uintptr_t)workspace % 16 == 0, LA_EINVAL, "workspace must be 16-byte aligned");
   hipStream_t s = (hipStream_t)stream;
   uint8_t *w = (uint8_t *)workspace;
-  const Sample a{logits, row_stride, V, l.chunks, *how, ids, prob, (unsigned long long *)w, (double *)(w + l.sums), (int32_t *)(w + l.counts), w + l.bins,
-                 (unsigned long long *)(w + l.head), (int4 *)(w + l.heads)};
+  const Sample a{logits, row_stride, V, l.chunks, *how, ids, prob, (unsigned long long *)w, (double *)(w + l.sums), (int32_t *)(w + l.counts), (int32_t *)(w + l.used),
+                 (uint16_t *)(w + l.sorted)};
   if (dtype == LA_F32) return sample_launch<float>(a, l.per, B, s);
   if (dtype == LA_F16) return sample_launch<_Float16>(a, l.per, B, s);
   return sample_launch<uint16_t>(a, l.per, B, s);
