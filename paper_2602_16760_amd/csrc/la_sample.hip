@@ -41,8 +41,8 @@ struct Sample {
 
 // A logit as it counts: NaN like -inf (no token), +inf like the largest finite value, -0 like 0.
 template <typename T>
-__device__ __forceinline__ float sample_logit(const T *p) {
-  const float x = load_as_float<T>(p);
+__device__ __forceinline__ float sample_logit(T raw) {
+  const float x = load_as_float<T>(&raw);
   return x != x ? -INFINITY : fminf(x, 3.402823466e38f) + 0.f;
 }
 // A token as a number: larger is in front, (value descending, index ascending).
@@ -58,7 +58,7 @@ __device__ __forceinline__ int sample_index(unsigned long long c) { return (int)
 
 // 2^(f / 8), 0 <= f <= 1, in units of 2^-36: a polynomial that meets it in the six Chebyshev nodes (off by 3e-13 at most, a unit is 1.5e-11); 2^52 added to a number
 // below it leaves the nearest whole number in the low bits.
-__device__ __forceinline__ unsigned long long sample_factor(double f) {
+__device__ __forceinline__ double sample_factor_52(double f) {
   const double z = f - 0.5;
   double s = 4.2495173672986880985e-8;
   s = __builtin_fma(s, z, 2.4523688009211048058e-6);
@@ -66,8 +66,10 @@ __device__ __forceinline__ unsigned long long sample_factor(double f) {
   s = __builtin_fma(s, z, 0.0039197225262626394621);
   s = __builtin_fma(s, z, 0.09047942850278266672);
   s = __builtin_fma(s, z, 1.0442737824277134712);
-  return __builtin_bit_cast(unsigned long long, __builtin_fma(s, SMP_UNIT, 0x1p52)) & ((1ull << 52) - 1);
+  return __builtin_fma(s, SMP_UNIT, 0x1p52);
 }
+__device__ __forceinline__ unsigned long long sample_factor(double f) { return __builtin_bit_cast(unsigned long long, sample_factor_52(f)) & ((1ull << 52) - 1); }
+__device__ __forceinline__ double sample_factor_of(double f) { return sample_factor_52(f) - 0x1p52; }  // the same number
 __device__ __forceinline__ double sample_eighths(int t) {  // 2^(-t / 8) units
   constexpr double e[8] = {1.0, 0.91700404320467123, 0.84089641525371454, 0.77110541270397041, 0.70710678118654752, 0.64841977732550483, 0.59460355750136053, 0.54525386633262883};
   double v = e[0];
@@ -115,12 +117,13 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   __shared__ __attribute__((aligned(16))) uint16_t sorted[CHUNK];
   const int c = blockIdx.x, b = blockIdx.y, t = threadIdx.x, wave = t >> 6, lane = t & 63, i0 = c * CHUNK + t;
   const T *x = (const T *)a.x + b * a.ld;
+  // (loads without a condition, and nothing done with one before all are requested)
+  T raw[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) raw[j] = x[min(i0 + SMP_SUM_THREADS * j, a.V - 1)];
   float v[PER];
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int i = i0 + SMP_SUM_THREADS * j;
-    v[j] = i < a.V ? sample_logit<T>(x + i) : -INFINITY;
-  }
+  for (int j = 0; j < PER; ++j) v[j] = i0 + SMP_SUM_THREADS * j < a.V ? sample_logit<T>(raw[j]) : -INFINITY;
   const SampleRow r = sample_row(a, b);
   for (int i = t; i < SMP_HIST; i += SMP_SUM_THREADS) hist[i] = 0;
   float top_v = -INFINITY;
@@ -211,9 +214,8 @@ struct SampleShared {
   unsigned sub_n[SMP_SUB];
   double through_w[SMP_BINS];  // sums over the bins up to and with this one
   int through_n[SMP_BINS];
-  unsigned long long best[64], chunk_in[64];
-  int shift[64];
-  double scale[64], before[64];
+  unsigned long long chunk_in[64];
+  double before[64];
   double red_d[SMP_WAVES];
   unsigned long long red_u[SMP_WAVES];
   unsigned red_n[SMP_WAVES];
@@ -222,7 +224,7 @@ struct SampleShared {
   int hit, last, where;
   unsigned long long few_c[SMP_FEW], few_w[SMP_FEW];
   int rank[SMP_FEW];
-  int used[64], from[64], ends[64];  // of a bin: where its tokens begin in each chunk's, how many there are up to and with each
+  int from[64], ends[64];  // of a bin: where its tokens begin in each chunk's, how many there are up to and with each
   double eighths[8];
 };
 
@@ -233,49 +235,57 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   const int b = blockIdx.x, t = threadIdx.x, wave = t >> 6, lane = t & 63, V = a.V, C = a.chunks;
   const T *x = (const T *)a.x + b * a.ld;
   const SampleRow r = sample_row(a, b);
-  if (t < 64) {
-    unsigned long long best = t < C ? a.best[(size_t)b * C + t] : 0;
-    m.best[t] = best;
-    m.chunk_in[t] = 0;
-    m.used[t] = t < C && !r.greedy ? a.used[(size_t)b * C + t] : 0;  // (a chunk without a token has none of its own, and is never looked at)
-    if (t < 8) m.eighths[t] = sample_eighths(t);
-  }
-  __syncthreads();
-  unsigned long long best = m.best[lane];
+  // lane c of every wave: chunk c's first token, and the bins up to its last (without a token: nothing of its own was written, and nothing is looked at)
+  const bool chunk = lane < C;
+  const unsigned long long c_best = chunk ? a.best[(size_t)b * C + lane] : 0;
+  const int c_used = chunk ? a.used[(size_t)b * C + lane] : 0;
+  if (t < 64) m.chunk_in[t] = 0;
+  if (t < 8) m.eighths[t] = sample_eighths(t);
+  const float c_top = chunk ? sample_value(c_best) : -INFINITY;
+  float top = c_top;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const unsigned long long y = __shfl_xor(best, o, 64);
-    best = y > best ? y : best;
-  }
-  best = uniform(best);
-  const float top = sample_value(best);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  top = __uint_as_float((unsigned)uniform((int)__float_as_uint(top)));
   if (r.greedy || !(top > -INFINITY)) {
+    unsigned long long best = c_best;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const unsigned long long y = __shfl_xor(best, o, 64);
+      best = y > best ? y : best;
+    }
     if (t == 0) {
       a.ids[b] = top > -INFINITY ? sample_index(best) : -1;
       if (a.prob) a.prob[b] = top > -INFINITY ? 1.f : 0.f;
     }
     return;
   }
-  const double y_top = (double)top * r.rate, first = floor(y_top), w_top = (double)sample_factor(y_top - first) * (1 / SMP_UNIT);
-  if (t < 64) {
-    const double d = t < C ? first - floor((double)sample_value(m.best[t]) * r.rate) : (double)SMP_BINS;
-    m.shift[t] = d < SMP_BINS ? (int)d : SMP_BINS;  // (a chunk without a token: NaN or infinite, and never looked at)
-    m.scale[t] = d < SMP_BINS ? sample_eighths((int)d) * SMP_UNIT : 0.0;
-  }
-  __syncthreads();
+  const double y_top = uniform((double)top * r.rate), first = uniform(floor(y_top)), w_top = (double)sample_factor(y_top - first) * (1 / SMP_UNIT);
+  const double c_down = first - floor((double)c_top * r.rate);
+  const int c_shift = c_down < SMP_BINS ? (int)c_down : SMP_BINS;
+  const double c_scale = c_down < SMP_BINS ? sample_eighths((int)c_down) * SMP_UNIT : 0.0;
   const double *sums = a.sums + (size_t)b * C * SMP_HIST;
   const int32_t *counts = a.counts + (size_t)b * C * SMP_HIST;
   // ---- the row's sums down to each bin
   if (t < SMP_BINS) {
     double w = 0;
     int n = 0;
-#pragma unroll 16
-    for (int c = 0; c < C; ++c) {  // (loads without a condition: many are on their way)
-      const int l = t - m.shift[c], top = m.used[c] - 1, at = l > 0 ? c * SMP_HIST + (l < top ? l : top) : c * SMP_HIST;
-      const double sw = sums[at];
-      const int sn = counts[at];
-      w += l >= 0 ? sw * m.scale[c] : 0.0;
-      n += l >= 0 ? sn : 0;
+    constexpr int N = 16;
+    for (int c0 = 0; c0 < C; c0 += N) {  // (loads without a condition, all on their way at once)
+      double sw[N];
+      int sn[N], l[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = min(c0 + k, C - 1);
+        l[k] = c0 + k < C ? t - lane_value(c_shift, c) : -1;
+        const int at = max(min(l[k], lane_value(c_used, c) - 1), 0);
+        sw[k] = sums[c * SMP_HIST + at];
+        sn[k] = counts[c * SMP_HIST + at];
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        w += l[k] >= 0 ? sw[k] * lane_value(c_scale, min(c0 + k, C - 1)) : 0.0;
+        n += l[k] >= 0 ? sn[k] : 0;
+      }
     }
     m.through_w[t] = w;
     m.through_n[t] = n;
@@ -287,8 +297,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   auto slices = [&](int t0, int t1) {
     __syncthreads();
     if (wave == 0) {
-      const int shift = lane < C ? m.shift[lane] : SMP_BINS, top = m.used[lane] - 1, l0 = t0 - 1 - shift, l1 = t1 - shift;
-      const bool any = l1 >= 0 && shift < SMP_BINS;
+      const int top = c_used - 1, l0 = t0 - 1 - c_shift, l1 = t1 - c_shift;
+      const bool any = l1 >= 0 && c_shift < SMP_BINS;
       const int32_t *n = counts + (any ? lane * SMP_HIST : 0);
       const int from = any && l0 >= 0 ? n[min(l0, top)] : 0, end = any ? n[min(l1, top)] : 0;
       m.from[lane] = from;
@@ -315,7 +325,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     if (n > SMP_LIST) return;
     for (int i = t; i < n; i += SMP_THREADS) {
       const int at = nth(i);
-      m.list[i] = sample_place(sample_logit<T>(x + at), at);
+      m.list[i] = sample_place(sample_logit<T>(x[at]), at);
     }
     __syncthreads();
   };
@@ -331,14 +341,14 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       const int n = slices(bin, bin);
       for (int i0 = t; i0 < n; i0 += 4 * SMP_THREADS) {
         int at[4];
-        float v[4];
+        T raw[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) at[j] = i0 + SMP_THREADS * j < n ? nth(i0 + SMP_THREADS * j) : -1;
+        for (int j = 0; j < 4; ++j) at[j] = nth(min(i0 + SMP_THREADS * j, n - 1));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = at[j] >= 0 ? sample_logit<T>(x + at[j]) : -INFINITY;
+        for (int j = 0; j < 4; ++j) raw[j] = x[at[j]];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (at[j] >= 0) take(sample_place(v[j], at[j]), v[j]);
+          if (i0 + SMP_THREADS * j < n) take(sample_place(sample_logit<T>(raw[j]), at[j]), sample_logit<T>(raw[j]));
       }
     }
   };
@@ -489,9 +499,9 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       cut = 0;
     }
   }
-  auto kept = [&](unsigned long long f, int bin, unsigned long long c) {  // the token's weight, 0: not kept
-    const double w = ldexp((double)f * m.eighths[bin & 7], -(bin >> 3));
-    return (bin < cut_bin || (bin == cut_bin && c >= cut)) && w >= w_least ? w : 0.0;
+  auto kept = [&](double f, int bin, float v, int i) {  // the token's weight, 0: not kept
+    const double w = ldexp(f * m.eighths[bin & 7], -(bin >> 3));
+    return (bin < cut_bin || (bin == cut_bin && sample_place(v, i) >= cut)) && w >= w_least ? w : 0.0;
   };
   float u = a.p.u_index ? a.p.u[min(max(a.p.u_index[b], 0), a.p.n_u - 1)] : a.p.u[b];
   u = u > 0.f ? fminf(u, 1.f) : 0.f;
@@ -504,8 +514,9 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     __syncthreads();
     for (int i = t; i < n_list; i += SMP_THREADS) {
       const unsigned long long c = m.list[i];
-      const double y = (double)sample_value(c) * r.rate, low = floor(y), d = first - low;
-      const double w = d < SMP_BINS ? kept(sample_factor(y - low), (int)d, c) : 0.0;
+      const float v = sample_value(c);
+      const double y = (double)v * r.rate, low = floor(y);
+      const double w = kept(sample_factor_of(y - low), (int)(first - low), v, sample_index(c));
       if (w > 0.0) {
         const unsigned at = atomicAdd(&m.n_few, 1u);
         if (at < SMP_FEW) {
@@ -565,13 +576,13 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   __syncthreads();
   double mine = 0.0;
   if (lane < C) {
-    const int l = (cut_bin < SMP_BINS ? cut_bin : SMP_BINS) - 1 - m.shift[lane];
-    if (l >= 0) mine = sums[lane * SMP_HIST + min(l, m.used[lane] - 1)] * m.scale[lane];
+    const int l = (cut_bin < SMP_BINS ? cut_bin : SMP_BINS) - 1 - c_shift;
+    if (l >= 0) mine = sums[lane * SMP_HIST + min(l, c_used - 1)] * c_scale;
   }
   if (cut_bin < SMP_BINS && cut != ~0ull) {
     if (cut_bin < listed0 || cut_bin > listed1) gather(cut_bin, cut_bin);
     each(cut_bin, cut, ~0ull, [&](unsigned long long c, unsigned long long f) {
-      if (kept(f, cut_bin, c) > 0.0) atomicAdd(&m.chunk_in[sample_index(c) / CHUNK], f);
+      if (kept((double)f, cut_bin, sample_value(c), sample_index(c)) > 0.0) atomicAdd(&m.chunk_in[sample_index(c) / CHUNK], f);
     });
   }
   __syncthreads();
@@ -586,17 +597,27 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     constexpr int N = CHUNK / SMP_THREADS;
     const int i0 = c * CHUNK + t * N;
     const double y_least = first - (cut_bin < SMP_BINS ? cut_bin : SMP_BINS - 1);  // (of a token that can be kept)
-    float v[N];
+    constexpr int VEC = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;  // bytes of a load, where rows and chunks begin on such
+    __attribute__((aligned(16))) T raw[N];
     double w[N], sum = 0;
+    if ((uintptr_t)x % 16 == 0 && (c + 1) * CHUNK <= V && (VEC == 16 || VEC == 8)) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = i0 + j < V ? sample_logit<T>(x + i0 + j) : -INFINITY;
+      for (int j = 0; j < N; j += VEC / (int)sizeof(T)) {
+        if constexpr (VEC == 16) *(uint4 *)(raw + j) = *(const uint4 *)(x + i0 + j);
+        else if constexpr (VEC == 8) *(uint2 *)(raw + j) = *(const uint2 *)(x + i0 + j);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) raw[j] = x[min(i0 + j, V - 1)];
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const double y = (double)v[j] * r.rate;
+      const float v = i0 + j < V ? sample_logit<T>(raw[j]) : -INFINITY;
+      const double y = (double)v * r.rate;
       w[j] = 0.0;
-      if (v[j] > -INFINITY && y >= y_least) {
+      if (v > -INFINITY && y >= y_least) {
         const double low = floor(y);
-        w[j] = kept(sample_factor(y - low), (int)(first - low), sample_place(v[j], i0 + j));
+        w[j] = kept(sample_factor_of(y - low), (int)(first - low), v, i0 + j);
       }
       sum += w[j];
     }
@@ -618,8 +639,11 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         if (run > want && hit == 0x7fffffff) hit = i0 + j;
       }
     }
-    if (hit != 0x7fffffff) atomicMin(&m.where, hit);
-    if (last >= 0) atomicMax(&m.last, last);
+    const unsigned long long hits = __ballot(hit != 0x7fffffff), keeps = __ballot(last >= 0);  // (lanes are in the order of their tokens)
+    if (lane == 0) {
+      if (hits) atomicMin(&m.where, lane_value(hit, (int)__builtin_ctzll(hits)));
+      if (keeps) atomicMax(&m.last, lane_value(last, 63 - (int)__builtin_clzll(keeps)));
+    }
     __syncthreads();
     const int id = uniform(m.where != 0x7fffffff ? m.where : m.last);
     if (id < 0) continue;
@@ -632,8 +656,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     return;
   }
   if (t == 0) {  // (not reached: the largest token is always kept)
-    a.ids[b] = sample_index(best);
-    if (a.prob) a.prob[b] = 1.f;
+    a.ids[b] = -1;
+    if (a.prob) a.prob[b] = 0.f;
   }
 }
 
