@@ -183,10 +183,16 @@ def _layer_struct(w: dict) -> la_layer_weights:
     return la_layer_weights(*[_ptr(w[k]) for k in ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown", "g_attn", "g_mlp")])
 
 
+class _Model(C.c_void_p):
+    """A la_model handle and the widths of its rows."""
+    d_model = vocab = None
+
+
 # ---- thin wrappers, one per C entry point ---------------------------------------------
 def la_init_model(shape, embed=None, g_final=None, unembed=None, stream=None):
     """Creates an empty model (layers are added with la_model_set_layer).  Returns the handle."""
-    out = C.c_void_p()
+    out = _Model()
+    out.d_model, out.vocab = shape.d_model, shape.vocab
     d = make_desc(shape)
     _check(lib.la_init_model(C.byref(d), None, _ptr(embed), _ptr(g_final), _ptr(unembed), _stream(stream), C.byref(out)))
     return out
@@ -288,12 +294,10 @@ def _workspace(size, like, stream):
 def la_unembed_logits(model, hidden, logits, stream=None):
     """logits: float32 [Bp, vocab], rows may be strided."""
     device = _here(hidden, "hidden")
-    if hidden.dtype is not _F32 or hidden.dim() != 2:
-        _refuse("hidden: need float32 [Bp, d_model]")
-    if logits.get_device() != device or logits.dtype is not _F32 or logits.dim() != 2 or logits.shape[0] != hidden.shape[0] or logits.stride(1) != 1:
-        _refuse(f"logits: need float32 [{hidden.shape[0]}, vocab] with contiguous rows on device {device}")
-    n, V = logits.shape
-    _check(lib.la_unembed_logits(model, _ptr(hidden), n, logits.data_ptr(), logits.stride(0) if n > 1 else V, _stream(stream)))
+    n, V = hidden.shape[0], model.vocab
+    if logits.get_device() != device or logits.dtype is not _F32 or logits.shape != (n, V) or logits.stride(1) != 1:
+        _refuse(f"logits: need float32 [{n}, {V}] with contiguous rows on device {device}, got {logits.dtype}, {tuple(logits.shape)}, strides {logits.stride()} on {logits.device}")
+    _check(lib.la_unembed_logits(model, _array(hidden, "hidden", _F32, (n, model.d_model), device), n, logits.data_ptr(), logits.stride(0) if n > 1 else V, _stream(stream)))
 
 
 @functools.lru_cache(maxsize=256)
@@ -404,11 +408,9 @@ def la_paged_attend(pages, layer, q, table, req, pos, out, scale=None, stream=No
 def la_forward_paged(model, layer_begin, layer_end, hidden, pos, req, slot, pages, table, stream=None):
     """One token each of several requests through the layers: hidden float32 [B, d_model] in place, pos, req (None: row b is request b), slot int32 [B]."""
     device = pages._here()
-    if hidden.dtype is not _F32 or hidden.dim() != 2 or hidden.get_device() != device:
-        _refuse(f"hidden: need float32 [B, d_model] on device {device}")
     n = (hidden.shape[0],)
     tp, ld, R, blocks = _table(table, device)
-    _check(lib.la_forward_paged(model, layer_begin, layer_end, _ptr(hidden), n[0], _array(pos, "pos", _I32, n, device), _optional(req, "req", _I32, n, device),
+    _check(lib.la_forward_paged(model, layer_begin, layer_end, _array(hidden, "hidden", _F32, (n[0], model.d_model), device), n[0], _array(pos, "pos", _I32, n, device), _optional(req, "req", _I32, n, device),
                                 _array(slot, "slot", _I32, n, device), pages.ref, tp, ld, R, blocks, _stream(stream)))
 
 

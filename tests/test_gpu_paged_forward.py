@@ -26,10 +26,15 @@ def bits(a, dtype):
     return t.view(torch.bfloat16) if dtype == "bf16" and t.dtype != torch.float32 else t.to(dict(f32=torch.float32, bf16=torch.bfloat16, f16=torch.float16)[dtype])
 
 
-@pytest.mark.parametrize("name,lens,page", [("tiny_f32", [0, 5, 47, 300], 16), ("small_bf16", [0, 1, 31, 33, 700], 16), ("small_bf16", list(range(3, 67)), 24),
-                                            ("small64_bf16", [100, 2], 8), ("small_f16", [64, 12, 1000], 32), ("small64_f16", [7] * 17, 16)])
-def test_forward_against_the_oracle(name, lens, page):
-    """A row per request, one of the batch padding: hidden states against the oracle's decode step of each request, K and V where the slots say."""
+@pytest.mark.parametrize("name,lens,page,env", [("tiny_f32", [0, 5, 47, 300], 16, {}), ("small_bf16", [0, 1, 31, 33, 700], 16, {}), ("small_bf16", list(range(3, 67)), 24, {}),
+                                                ("small64_bf16", [100, 2], 8, {}), ("small_f16", [64, 12, 1000], 32, {}), ("small64_f16", [7] * 17, 16, {}),
+                                                ("small_bf16", [0, 40, 600], 16, {"LA_FORCE_GENERIC": "1"}), ("small64_f16", [5, 90, 1], 12, {"LA_FORCE_GENERIC": "1"}),
+                                                ("small_bf16", [3, 33], 16, {"LA_WGS": "37"})])
+def test_forward_against_the_oracle(name, lens, page, env, monkeypatch):
+    """A row per request, one of the batch padding: hidden states against the oracle's decode step of each request, K and V where the slots say.  16-bit models also
+    on the plain kernels, and with weights laid out for another number of workgroups."""
+    for key, value in env.items():
+        monkeypatch.setenv(key, value)
     shape = synth.SHAPES[name]
     eng, om, B = gpu_engine(shape, 64, head=False), oracle_model(shape, head=False), binding()
     R, H, dh, dt = len(lens), shape.n_kv_heads, shape.head_dim, shape.dtype
@@ -68,7 +73,7 @@ def test_forward_against_the_oracle(name, lens, page):
         hidden = torch.from_numpy(x.astype(np.float32)).cuda()
         run = lambda h: B.la_forward_paged(eng.model, 0, shape.n_layers, h, i32(pos), i32(req), i32(slot), pages, i32(table.tolist()))
         used = launch_names(lambda: run(hidden.clone()))
-        assert {"paged_attend"} <= used and ("pf_gemm_qkv" in used) == (dt != "f32"), used
+        assert {"paged_attend"} <= used and ("pf_gemm_qkv" in used) == (dt != "f32" and "LA_FORCE_GENERIC" not in env), used
         run(hidden)
         got = hidden.cpu().numpy()
         again = torch.from_numpy(x.astype(np.float32)).cuda()
