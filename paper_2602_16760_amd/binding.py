@@ -284,11 +284,12 @@ def _optional(t, name, dtype, shape, device):
 
 
 def _workspace(size, like, stream):
-    """Memory for one call: of the stream that runs it, so that nobody else is given it before the call is through."""
-    ws = torch.empty(size, dtype=torch.uint8, device=like.device)
-    if stream is not None and stream != torch.cuda.current_stream():
-        ws.record_stream(stream)
-    return ws
+    """Memory for one call, out of the memory of the stream that runs it: what that stream did with it before is through when the call starts, and nobody
+    is given it before the call is through.  (The current stream's may still be written by that stream.)"""
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=torch.uint8, device=like.device)
 
 
 def la_unembed_logits(model, hidden, logits, stream=None):
