@@ -287,7 +287,8 @@ typedef struct {
  * The new tokens, old_len[r] <= t < new_len[r] of request 0, 1, ...: row i of them has slot[i], pos[i] = t and req[i] = r (device int32
  * [max_rows]; -1 in rows behind the last token), and request r's begin at row first[r] (device int32 [R + 1]).
  * Errors that only the device sees go to heads_out[3], and then nothing is taken, given back or mapped (all rows -1, first all 0): 1 too few free pages,
- * 2 more than max_rows new tokens, 3 a length outside [0, max_blocks * page_size], 4 heads that are no place in the ring.
+ * 2 more than max_rows new tokens, 3 a length outside [0, max_blocks * page_size], 4 heads that are
+ * no place in the ring, or more pages given back than are out of it.
  * LA_EINVAL: a NULL pointer, a size that is not positive, heads_in == heads_out, table rows that overlap, n_pages * page_size >= 2^31. */
 int la_page_map(const int32_t *old_len, const int32_t *new_len, int R, int page_size, int32_t *table, int64_t table_stride, int max_blocks,
                 int32_t *ring, int n_pages, const int32_t *heads_in, int32_t *heads_out, int32_t *slot, int32_t *pos, int32_t *req, int max_rows,

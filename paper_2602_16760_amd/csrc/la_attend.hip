@@ -1,5 +1,5 @@
 // Attention of single tokens over a paged cache (la_paged_attend): the keys of a row are split into items, an item is a workgroup, and a second launch joins
-// the items of rows that have several.
+// the items of rows that have several.  What bounds it is K and V, which are read once for all query heads of a kv head.
 #include <algorithm>
 #include <type_traits>
 
@@ -13,6 +13,11 @@ typedef _Float16 __attribute__((ext_vector_type(8))) at_h8;
 typedef float __attribute__((ext_vector_type(4))) at_f4;
 typedef unsigned __attribute__((ext_vector_type(4))) at_u4;
 typedef unsigned __attribute__((ext_vector_type(2))) at_u2;
+
+struct AtItem {
+  int b, r, n, C, index, first, count;  // row, its request and keys; keys per item; which of the row's items; the row's first item; how many it has
+  int pad;
+};
 
 struct PagedAttend {
   const void *K, *V;  // of the layer
@@ -33,6 +38,8 @@ struct PagedAttend {
   int kind;      // PagedOut
   int rec;       // floats of a head's record of an item: running maximum, sum, two of padding, dh sums
   float *part;   // [item][Hq][rec]
+  AtItem *list;  // the items as paged_plan_kernel leaves them; NULL: every wave finds its own
+  int32_t *firsts;  // ... and the rows' first ones
 };
 
 constexpr int AT_WAVES = 4, AT_WHOLE_WAVES = 8;  // of a workgroup; where rows are not cut and heads are few
@@ -49,53 +56,89 @@ __device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
 }
 
 // The items: row b has max(1, ceil(keys / C)) of them, C = a multiple of AT_PIECE for which that is at most `target` items in all (or nearly: rows of few keys have one each).
-// Every wave forms that from the rows' positions by itself.
-struct AtItem {
-  int b, r, n, C, index, first, count;  // row, its request and keys; keys per item; which of the row's items; the row's first item; how many it has
-};
+__device__ __forceinline__ int at_pieces(long long keys) {
+  const long long n = (keys + AT_PIECE - 1) / AT_PIECE;
+  return (int)(n < 1 ? 1 : n < 0xffffff ? n : 0xffffff) * AT_PIECE;
+}
 __device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (n + C - 1) / C : 1; }
+constexpr int AT_TURNS = 3;  // the rows' last items are not full: longer ones, until all of them are resident at once
+// The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
+// positions, a lane each; of more it was written down by a launch of its own (formed by every workgroup from all rows' positions, 64 at a time, it took 5 of 57 us at 65 rows,
+// and its time grows with the square of the rows).
 template <bool BY_ROW>
-__device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {  // the wanted item; BY_ROW: item 0 of the wanted row.  b = -1: there is none
+__device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
+  AtItem it{};
+  if (a.target <= 0) {
+    int r;
+    const int n = at_keys(a, wanted, r);
+    it.b = wanted;
+    it.r = uniform(r);
+    it.n = uniform(n);
+    it.C = 0x7fffff80;
+    it.first = wanted;
+    it.count = 1;
+    return it;
+  }
+  if (a.list) return a.list[BY_ROW ? a.firsts[wanted] : wanted];
   const int lane = threadIdx.x & 63;
-  AtItem it;
-  int r = 0, n = lane < a.B ? at_keys(a, lane, r) : 0;
-  it.C = 0x7fffff80;
-  if (a.target > 0) {
-    long long all = n;
-    for (int b0 = 64; b0 < a.B; b0 += 64) {
-      int r1;
-      all += b0 + lane < a.B ? at_keys(a, b0 + lane, r1) : 0;
-    }
-    all = lane_value(lane_through(all), 63);
-    auto pieces = [](long long keys) { return (int)((keys + AT_PIECE - 1) / AT_PIECE < 1 ? 1 : (keys + AT_PIECE - 1) / AT_PIECE < 0xffffff ? (keys + AT_PIECE - 1) / AT_PIECE : 0xffffff) * AT_PIECE; };
-    it.C = pieces((all + a.target - 1) / a.target);
-    // the rows' last items are not full: longer ones, until all of them are resident at once
-    for (int turn = 0; turn < 3 && a.B <= 64; ++turn) {
-      const int items = lane_value(lane_through(lane < a.B ? at_rows_items(n, it.C) : 0), 63);
-      if (items <= a.target || items <= a.B) break;
-      it.C = pieces((long long)it.C * items / a.target + 1);
-    }
+  int r = 0;
+  const int n = lane < a.B ? at_keys(a, lane, r) : 0;
+  it.C = at_pieces((lane_value(lane_through((long long)n), 63) + a.target - 1) / a.target);
+  int c = 0, ends = 0, items = 0;
+  for (int turn = 0;; ++turn) {
+    c = lane < a.B ? at_rows_items(n, it.C) : 0;
+    ends = lane_through(c);
+    items = lane_value(ends, 63);
+    if (turn == AT_TURNS || items <= a.target || items <= a.B) break;
+    it.C = at_pieces((long long)it.C * items / a.target + 1);
+  }
+  const int l = BY_ROW ? wanted : __builtin_popcountll(__ballot(ends <= wanted));
+  it.b = -1;
+  if (l >= a.B) return it;
+  it.b = l;
+  it.r = lane_value(r, l);
+  it.n = lane_value(n, l);
+  it.count = lane_value(c, l);
+  it.first = lane_value(ends, l) - it.count;
+  it.index = BY_ROW ? 0 : wanted - it.first;
+  return it;
+}
+
+// The same items of more than 64 rows, by one workgroup that goes through the rows a thread each; `items`: places in the list.
+constexpr int AT_PLAN_THREADS = 1024;
+__global__ __launch_bounds__(AT_PLAN_THREADS) void paged_plan_kernel(PagedAttend a, int items) {
+  constexpr int WAVES = AT_PLAN_THREADS / 64;
+  __shared__ long long red[WAVES];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  auto all_of = [&](long long v) {  // its sum over the threads
+    v = lane_through(v);
+    __syncthreads();
+    if (lane == 63) red[wave] = v;
+    __syncthreads();
+    return uniform((unsigned long long)sum_of(red, WAVES));
+  };
+  long long keys = 0;
+  int r;
+  for (int b = t; b < a.B; b += AT_PLAN_THREADS) keys += at_keys(a, b, r);
+  int C = at_pieces(((long long)all_of(keys) + a.target - 1) / a.target);
+  for (int turn = 0; turn < AT_TURNS; ++turn) {
+    long long c = 0;
+    for (int b = t; b < a.B; b += AT_PLAN_THREADS) c += at_rows_items(at_keys(a, b, r), C);
+    const long long n = (long long)all_of(c);
+    if (n <= a.target || n <= a.B) break;
+    C = at_pieces((long long)C * n / a.target + 1);
   }
   int before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const bool in = b0 + lane < a.B;
-    if (b0 > 0 || a.B > 64) n = in ? at_keys(a, b0 + lane, r) : 0;
-    const int c = in ? at_rows_items(n, it.C) : 0, ends = lane_through(c), total = lane_value(ends, 63);
-    const bool here = BY_ROW ? wanted < b0 + 64 : wanted < before + total;
-    if (here) {
-      const int l = BY_ROW ? wanted - b0 : __builtin_popcountll(__ballot(before + ends <= wanted));
-      it.b = b0 + l;
-      it.r = lane_value(r, l);
-      it.n = lane_value(n, l);
-      it.count = lane_value(c, l);
-      it.first = before + lane_value(ends, l) - it.count;
-      it.index = BY_ROW ? 0 : wanted - it.first;
-      return it;
-    }
+  for (int b0 = 0; b0 < a.B; b0 += AT_PLAN_THREADS) {
+    const int b = b0 + t, n = b < a.B ? at_keys(a, b, r) : 0, c = b < a.B ? at_rows_items(n, C) : 0;
+    const int through = lane_through(c);
+    const int total = (int)all_of(c);  // (what it leaves in `red` are the waves' sums)
+    const int first = before + (int)sum_of(red, wave) + through - c;
+    if (b < a.B) a.firsts[b] = first;
+    for (int i = 0; i < c && first + i < items; ++i) a.list[first + i] = AtItem{b, r, n, C, i, first, c, 0};
     before += total;
   }
-  it.b = -1;
-  return it;
+  for (int i = before + t; i < items; i += AT_PLAN_THREADS) a.list[i].b = -1;
 }
 
 __device__ __forceinline__ float at_max4(float v) {  // over the four lanes 16 apart
@@ -157,7 +200,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   extern __shared__ __attribute__((aligned(16))) float at_lds[];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
   const AtItem it = at_find<false>(a, blockIdx.x);
-  if (it.b < 0) return;
+  if (it.b < 0) return;  // (all waves)
   const int g = a.Hq / a.Hkv, tiles = (g + AT_ROWS - 1) / AT_ROWS, h = (int)blockIdx.y / tiles, g0 = (int)blockIdx.y % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
   const int rows = g - g0 < AT_ROWS ? g - g0 : AT_ROWS, head0 = h * g + g0;
   const int k_first = it.index * it.C, k_end = it.n - k_first < it.C ? it.n : k_first + it.C;  // (C is a multiple of the block)
@@ -475,7 +518,7 @@ constexpr size_t AT_CACHED = (size_t)256 << 20;
 static int at_workgroups(int dh) { return dh <= 64 ? 1024 : dh <= 128 ? 512 : 256; }
 struct AtPlan {
   int target, items, tiles;
-  size_t bytes;
+  size_t list, bytes;  // where the list of items begins in the workspace, 0: there is none
 };
 static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
   AtPlan r{};
@@ -486,6 +529,10 @@ static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
     r.target = std::max(1, at_workgroups(p.head_dim) / (p.n_kv_heads * r.tiles));
     r.items = (int)std::min<long long>((long long)r.target + B, B * ((cap + AT_PIECE - 1) / AT_PIECE));
     r.bytes = (size_t)r.items * Hq * (p.head_dim + 4) * 4;
+    if (B > 64) {
+      r.list = r.bytes;
+      r.bytes += r.items * sizeof(AtItem) + (size_t)B * 4;
+    }
   }
   return r;
 }
@@ -498,6 +545,10 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   const dim3 grid(plan.items, a.Hkv * plan.tiles);
   bool wide = false;
   if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8;
+  if (a.list) {
+    ProfScope ps("paged_plan", s);
+    paged_plan_kernel<<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
+  }
   {
     ProfScope ps("paged_attend", s);
     bool once = false;
@@ -532,7 +583,11 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   return sized(std::integral_constant<int, 256>{});
 }
 
-static int at_run(const PagedAttend &a, int dtype, const AtPlan &plan, hipStream_t s) {
+static int at_run(PagedAttend a, int dtype, const AtPlan &plan, hipStream_t s) {
+  if (plan.list) {
+    a.list = (AtItem *)((char *)a.part + plan.list);
+    a.firsts = (int32_t *)(a.list + plan.items);
+  }
   if (dtype == LA_F32) return at_launch<float>(a, plan, s);
   if (dtype == LA_F16) return at_launch<_Float16>(a, plan, s);
   return at_launch<uint16_t>(a, plan, s);
@@ -546,7 +601,7 @@ int paged_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_ti
   const int64_t ld = (int64_t)Hq * p.head_dim;
   const AtPlan plan = at_plan(p, Hq, r.max_blocks, r.B);
   const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, ld, Hq, scale, r.table, r.ldt,
-                      r.n_req, r.max_blocks, r.req, r.pos, r.B, out, ld, plan.target, q_tiles, kind, p.head_dim + 4, (float *)workspace};
+                      r.n_req, r.max_blocks, r.req, r.pos, r.B, out, ld, plan.target, q_tiles, kind, p.head_dim + 4, (float *)workspace, nullptr, nullptr};
   return at_run(a, p.dtype, plan, s);
 }
 
@@ -581,6 +636,6 @@ extern "C" int la_paged_attend(const la_pages_desc *pages, int layer, const void
   hipStream_t s = (hipStream_t)stream;
   const size_t at = layer * layer_bytes(&p);
   const PagedAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride,
-                      n_requests, max_blocks, req, pos, B, out, out_stride, plan.target, 0, AT_OUT_ROWS, p.head_dim + 4, (float *)workspace};
+                      n_requests, max_blocks, req, pos, B, out, out_stride, plan.target, 0, AT_OUT_ROWS, p.head_dim + 4, (float *)workspace, nullptr, nullptr};
   return at_run(a, p.dtype, plan, s);
 }

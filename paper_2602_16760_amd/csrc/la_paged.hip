@@ -100,6 +100,7 @@ __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(PageMap a) {
   int error = 0;
   if (head < 0 || head >= a.n_pages || n_free < 0 || n_free > a.n_pages) error = 4;
   else if (any_bad) error = 3;
+  else if (total[2] > a.n_pages - n_free) error = 4;  // (pages given back that the ring has already)
   else if (total[0] > a.max_rows) error = 2;
   else if (total[1] > n_free) error = 1;
   const int part = blockIdx.y, parts = gridDim.y, stride = parts * MAP_THREADS, k0 = part * MAP_THREADS + t;
@@ -210,7 +211,7 @@ extern "C" int la_paged_write(const la_pages_desc *pages, int layer, const void 
   hipStream_t s = (hipStream_t)stream;
   const int per_head = (int)(p.head_dim * e / 16);
   const long long wgs = ((long long)n * p.n_kv_heads * per_head + 255) / 256;
-  LA_REQUIRE(wgs < (1ll << 31), LA_EINVAL, "%d rows are more than one launch takes", n);
+  LA_REQUIRE(wgs < (1ll << 24), LA_EINVAL, "%d rows are more than one launch takes", n);  // (2^32 threads)
   ProfScope ps("paged_write", s);
   paged_write_kernel<<<(unsigned)wgs, 256, 0, s>>>((uint4 *)((char *)p.k + layer * layer_bytes(&p)), (uint4 *)((char *)p.v + layer * layer_bytes(&p)), (const uint4 *)k,
                                                    (const uint4 *)v, k_stride * (int64_t)e / 16, v_stride * (int64_t)e / 16, slot, n, p.n_kv_heads, per_head, p.page_size,

@@ -768,6 +768,10 @@ static int pf_launch_qkv_few(const PfGemm &p, hipStream_t s, bool prepare) {
 }
 static int pf_launch_qkv_few(const PfGemm &p, int row_tiles, hipStream_t s, bool prepare) {
   switch (row_tiles) {
+  case 1: return pf_launch_qkv_few<1, 4>(p, s, prepare);  // (up to four: la_forward_paged)
+  case 2: return pf_launch_qkv_few<2, 4>(p, s, prepare);
+  case 3: return pf_launch_qkv_few<3, 4>(p, s, prepare);
+  case 4: return pf_launch_qkv_few<4, 4>(p, s, prepare);
   case 5: return pf_launch_qkv_few<5, 4>(p, s, prepare);
   case 6: return pf_launch_qkv_few<6, 4>(p, s, prepare);
   case 7: return pf_launch_qkv_few<7, 3>(p, s, prepare);
@@ -827,7 +831,7 @@ static int pf_alloc(la_model *m, int most, int least, PfBuffers &b) {
     if (!rc) rc = pf_launch_tile<PF_PART>(i, PfGemm{}, nullptr, true);
     if (!rc) rc = pf_launch_tile<PF_GATEUP>(i, PfGemm{}, nullptr, true);
   }
-  for (int i = 5; !rc && i <= 8; ++i) rc = pf_launch_qkv_few(PfGemm{}, i, nullptr, true);
+  for (int i = 1; !rc && i <= 8; ++i) rc = pf_launch_qkv_few(PfGemm{}, i, nullptr, true);
   for (int i = 3; !rc && i <= 8; ++i) rc = pf_launch_rows<PF_QKV>(PfGemm{}, i, nullptr, true);
   for (int i = 5; !rc && i <= 8; ++i) rc = pf_launch_rows<PF_PART>(PfGemm{}, i, nullptr, true);
   for (int i : {5, 6, 7, 8, 10, 12})
@@ -981,7 +985,14 @@ int mfma_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRo
     };
     int S_o = 0;
     if ((rc = pf_launch_norm(S_down, hidden, b.part, m->layers[l].g_attn, M, d.d_model, RT, b.ss, b.A, s))) return rc;
-    if ((rc = pf_launch_gemm<PF_QKV>(args(0, b.A), s, "pf_gemm_qkv", f->n_wgs))) return rc;
+    // (without tiles while its workgroups are one round of the chip, as for a prompt of up to 128 rows)
+    if ((f->p_qkv.ntiles + 1) / 2 <= f->n_wgs) {
+      ProfScope ps("pf_gemm_qkv", s);
+      rc = pf_launch_qkv_few(args(0, b.A), ceil_div(M, 16), s, false);
+    } else {
+      rc = pf_launch_gemm<PF_QKV>(args(0, b.A), s, "pf_gemm_qkv", f->n_wgs);
+    }
+    if (rc) return rc;
     {
       ProfScope ps("unstage", s);
       unstage_kernel<<<ceil_div(M * d.n_kv_heads * (d.head_dim / 8), 256), 256, 0, s>>>((const uint16_t *)stage_k, (const uint16_t *)stage_v,

@@ -333,3 +333,38 @@ def test_attend_a_pool_behind_32_bits():
     rows = torch.randn((2, 8, 128), generator=c.g).to(torch.bfloat16)
     B.la_paged_write(B.la_pages(k, v), 0, rows.cuda(), rows.cuda(), i32([n_pages * 16 - 1, (n_pages - 1) * 16]))
     assert torch.equal(k[0, -1, :, 15].cpu(), rows[0]) and torch.equal(v[0, -1, :, 0].cpu(), rows[1])
+
+
+@pytest.mark.parametrize("heads,old,error", [([2, 8, 0, 0], [17, 0], 4), ([2, 8, 0, 0], [16, 0], 0), ([2, 9, 0, 0], [1, 0], 4)])
+def test_map_gives_back_no_more_pages_than_are_out(heads, old, error):
+    """A ring of 9 with 8 (or all) free takes back one (none): more would go where free pages stand."""
+    B = binding()
+    table, ring = i32([[5, 6], [7, 8]]), i32(list(range(9)))
+    slot, pos, req, first, out = i32([3] * 4), i32([3] * 4), i32([3] * 4), i32([3] * 3), i32([9] * 4)
+    B.la_page_map(i32(old), i32([0, 0]), 16, table, ring, i32(heads), out, slot, pos, req, first)
+    assert out.tolist() == [heads[0], heads[1] + (1 if error == 0 else 0), 0, error]
+    want = list(range(9))
+    if error == 0:
+        want[(heads[0] + heads[1]) % 9] = 5
+    assert ring.tolist() == want and table.tolist() == [[5, 6], [7, 8]] and slot.tolist() == [-1] * 4 and first.tolist() == [0] * 3
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,B,long", [("bf16", 8, 2, 64, 16, 65, 9000), ("f16", 4, 1, 128, 16, 300, 5000), ("f32", 2, 1, 64, 12, 1100, 2000), ("bf16", 4, 2, 96, 24, 2500, 700)])
+def test_attend_rows_beyond_a_wave(dtype, Hq, Hkv, dh, page, B, long):
+    """More rows than lanes, and than threads of a workgroup, of fewer requests, a long one among them, with padding rows and unknown requests."""
+    lens = [long, 1, 16, 300, long // 3, 77, 150]
+    c = Case(dtype, Hq, Hkv, dh, page, lens, seed=B)
+    req = [r % 8 if r % 3 else 1 + r % 6 for r in range(B)]
+    pos = [-1 if r % 13 == 5 else (lens[k] if k < 7 else 9) * (1 + r % 5) // 5 - 1 for r, k in enumerate(req)]
+    q = c.queries(B)
+    out = c.run(q, req, pos)
+    c.check(q, req, pos, out)
+    assert torch.equal(out, c.run(q, req, pos))
+
+
+@pytest.mark.parametrize("B", [64, 3000])
+def test_attend_many_rows_that_are_not_cut(B):
+    c = Case("bf16", 4, 2, 64, 16, [512, 1, 100, 33], seed=B)
+    req, pos = [r % 4 for r in range(B)], [[512, 1, 100, 33][r % 4] * (1 + r % 7) // 7 - 1 for r in range(B)]
+    q = c.queries(B)
+    c.check(q, req, pos, c.run(q, req, pos))

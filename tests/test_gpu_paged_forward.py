@@ -1,4 +1,6 @@
 """Several requests at once: rows of them through the layers on pages, generation with shared pages, sampled generation."""
+from dataclasses import replace
+
 import numpy as np
 import pytest
 import torch
@@ -93,6 +95,30 @@ def test_forward_against_the_oracle(name, lens, page, env, monkeypatch):
                 ref = np.asarray(theirs[shape.n_layers - 1][lens[r]], dtype=np.float64).reshape(H, dh)
                 assert np.abs(row - ref).max() <= (BAR[dt] + 2.0 ** -8) * np.abs(ref).max()
         assert torch.equal(pages.k.cpu()[:, ~touched], before.cpu()[:, ~touched])
+    finally:
+        eng.close()
+
+
+@pytest.mark.parametrize("rows", [1, 16, 17, 40, 64])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (64, 8)])
+def test_forward_of_narrow_and_wide_qkv(Hq, Hkv, rows):
+    """QKV products of one round of workgroups, and of more, at every number of row tiles: each row as it comes out alone, and against the oracle."""
+    shape = replace(synth.SHAPES["small_bf16"], n_q_heads=Hq, n_kv_heads=Hkv, n_layers=1)
+    eng, om, B = gpu_engine(shape, 64, head=False), oracle_model(shape, head=False), binding()
+    try:
+        pages = lambda: B.la_pages(*(torch.zeros((1, 70, Hkv, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+        table = torch.randperm(70, generator=torch.Generator().manual_seed(rows))[:rows].to(torch.int32).cuda().view(rows, 1)
+        slot, pos = (table[:, 0] * 16).contiguous(), i32([0] * rows)
+        x = synth.hidden_block(shape, rows, 0)
+        hidden, pg = torch.from_numpy(x.astype(np.float32)).cuda(), pages()
+        B.la_forward_paged(eng.model, 0, 1, hidden, pos, None, slot, pg, table)
+        for r in range(0, rows, 7):
+            want = otf.forward_block(om, otf.KVCache(shape, 1), x[r:r + 1], [0], [1])
+            assert row_rel_err(hidden[r:r + 1].cpu().numpy(), want).max() <= BAR["bf16"]
+        alone, other = torch.from_numpy(x[-1:].astype(np.float32)).cuda(), pages()
+        B.la_forward_paged(eng.model, 0, 1, alone, pos[:1], None, slot[-1:].contiguous(), other, table[-1:].contiguous())
+        at = int(table[-1, 0])
+        assert torch.equal(other.k[0, at], pg.k[0, at]) and torch.equal(other.v[0, at], pg.v[0, at])
     finally:
         eng.close()
 

@@ -128,3 +128,9 @@ def test_binding_refuses_tensors_of_the_host():
 
 def test_descriptors_match_the_header():
     assert C.sizeof(B.la_pages_desc) == 2 * 8 + 6 * 4 and C.sizeof(B.la_sampling) == 6 * 8 + 8
+
+
+def test_write_takes_no_more_threads_than_a_launch_has():
+    """A thread per 16 bytes of a row of K: 2^32 of them are refused, whatever their workgroups number."""
+    rows = (1 << 32) // (64 * 32)
+    refused(lib.la_paged_write(*{**WRITE, "pages": pages(n_kv_heads=64, head_dim=256), "n": rows}.values()), EINVAL, "more than one launch")
