@@ -55,13 +55,29 @@ __device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
   return (unsigned)r >= (unsigned)a.n_req || n < 0 ? 0 : (int)(n < cap ? n : cap);
 }
 
-// The items: row b has max(1, ceil(keys / C)) of them, C = a multiple of AT_PIECE for which that is at most `target` items in all (or nearly: rows of few keys have one each).
+// The items: a row of n keys has max(1, ceil(n / C)) of them, as equal as multiples of AT_PIECE are.
 __device__ __forceinline__ int at_pieces(long long keys) {
   const long long n = (keys + AT_PIECE - 1) / AT_PIECE;
   return (int)(n < 1 ? 1 : n < 0xffffff ? n : 0xffffff) * AT_PIECE;
 }
 __device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (n + C - 1) / C : 1; }
-constexpr int AT_TURNS = 3;  // the rows' last items are not full: longer ones, until all of them are resident at once
+__device__ __forceinline__ int at_item_keys(int n, int count) { return at_pieces((n + count - 1) / count); }
+// C.  `target` items of the same length are all resident at once.
+//   Up to half as many rows: all keys over `target`, and longer while the rows' remainders make more items than are resident (AT_TURNS times at most).
+//   More rows: where the longest row is much longer than what a resident item would have of all keys, a third of that, so that what is left to the last items is little;
+// otherwise rows are not cut.
+constexpr int AT_TURNS = 3, AT_FINE = 3;
+template <typename Items>
+__device__ __forceinline__ int at_cut(const PagedAttend &a, long long keys, int longest, Items items) {
+  if (2 * a.B > a.target) return longest * 4ll * a.target <= 5 * keys ? at_pieces(longest) : at_pieces((keys + AT_FINE * a.target - 1) / (AT_FINE * a.target));
+  int C = at_pieces((keys + a.target - 1) / a.target);
+  for (int turn = 0; turn < AT_TURNS; ++turn) {
+    const int n = items(C);
+    if (n <= a.target) break;
+    C = at_pieces((long long)C * n / a.target + 1);
+  }
+  return C;
+}
 // The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
 // positions, a lane each; of more it was written down by a launch of its own (formed by every workgroup from all rows' positions, 64 at a time, it took 5 of 57 us at 65 rows,
 // and its time grows with the square of the rows).
@@ -83,15 +99,13 @@ __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
   const int lane = threadIdx.x & 63;
   int r = 0;
   const int n = lane < a.B ? at_keys(a, lane, r) : 0;
-  it.C = at_pieces((lane_value(lane_through((long long)n), 63) + a.target - 1) / a.target);
-  int c = 0, ends = 0, items = 0;
-  for (int turn = 0;; ++turn) {
-    c = lane < a.B ? at_rows_items(n, it.C) : 0;
+  int c = 0, ends = 0;
+  auto items = [&](int C) {
+    c = lane < a.B ? at_rows_items(n, C) : 0;
     ends = lane_through(c);
-    items = lane_value(ends, 63);
-    if (turn == AT_TURNS || items <= a.target || items <= a.B) break;
-    it.C = at_pieces((long long)it.C * items / a.target + 1);
-  }
+    return lane_value(ends, 63);
+  };
+  (void)items(at_cut(a, lane_value(lane_through((long long)n), 63), lane_most(n), items));
   const int l = BY_ROW ? wanted : __builtin_popcountll(__ballot(ends <= wanted));
   it.b = -1;
   if (l >= a.B) return it;
@@ -99,6 +113,7 @@ __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
   it.r = lane_value(r, l);
   it.n = lane_value(n, l);
   it.count = lane_value(c, l);
+  it.C = at_item_keys(it.n, it.count);
   it.first = lane_value(ends, l) - it.count;
   it.index = BY_ROW ? 0 : wanted - it.first;
   return it;
@@ -118,16 +133,23 @@ __global__ __launch_bounds__(AT_PLAN_THREADS) void paged_plan_kernel(PagedAttend
     return uniform((unsigned long long)sum_of(red, WAVES));
   };
   long long keys = 0;
-  int r;
-  for (int b = t; b < a.B; b += AT_PLAN_THREADS) keys += at_keys(a, b, r);
-  int C = at_pieces(((long long)all_of(keys) + a.target - 1) / a.target);
-  for (int turn = 0; turn < AT_TURNS; ++turn) {
+  int r, longest = 0;
+  for (int b = t; b < a.B; b += AT_PLAN_THREADS) {
+    const int n = at_keys(a, b, r);
+    keys += n;
+    longest = longest > n ? longest : n;
+  }
+  keys = (long long)all_of(keys);
+  __syncthreads();
+  longest = lane_most(longest);
+  if (lane == 0) red[wave] = longest;
+  __syncthreads();
+  longest = lane_most(lane < WAVES ? (int)red[lane] : 0);
+  const int C = at_cut(a, keys, longest, [&](int C) {
     long long c = 0;
     for (int b = t; b < a.B; b += AT_PLAN_THREADS) c += at_rows_items(at_keys(a, b, r), C);
-    const long long n = (long long)all_of(c);
-    if (n <= a.target || n <= a.B) break;
-    C = at_pieces((long long)C * n / a.target + 1);
-  }
+    return (int)all_of(c);
+  });
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += AT_PLAN_THREADS) {
     const int b = b0 + t, n = b < a.B ? at_keys(a, b, r) : 0, c = b < a.B ? at_rows_items(n, C) : 0;
@@ -135,7 +157,7 @@ __global__ __launch_bounds__(AT_PLAN_THREADS) void paged_plan_kernel(PagedAttend
     const int total = (int)all_of(c);  // (what it leaves in `red` are the waves' sums)
     const int first = before + (int)sum_of(red, wave) + through - c;
     if (b < a.B) a.firsts[b] = first;
-    for (int i = 0; i < c && first + i < items; ++i) a.list[first + i] = AtItem{b, r, n, C, i, first, c, 0};
+    for (int i = 0; i < c && first + i < items; ++i) a.list[first + i] = AtItem{b, r, n, at_item_keys(n, c), i, first, c, 0};
     before += total;
   }
   for (int i = before + t; i < items; i += AT_PLAN_THREADS) a.list[i].b = -1;
@@ -199,9 +221,10 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   constexpr int VK = 4 * TILES;                    // keys whose V a lane loads
   extern __shared__ __attribute__((aligned(16))) float at_lds[];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
-  const AtItem it = at_find<false>(a, blockIdx.x);
+  const int g = a.Hq / a.Hkv, tiles = (g + AT_ROWS - 1) / AT_ROWS, item = (int)blockIdx.x / (a.Hkv * tiles), share = (int)blockIdx.x - item * a.Hkv * tiles;
+  const AtItem it = at_find<false>(a, item);
   if (it.b < 0) return;  // (all waves)
-  const int g = a.Hq / a.Hkv, tiles = (g + AT_ROWS - 1) / AT_ROWS, h = (int)blockIdx.y / tiles, g0 = (int)blockIdx.y % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
+  const int h = share / tiles, g0 = share % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
   const int rows = g - g0 < AT_ROWS ? g - g0 : AT_ROWS, head0 = h * g + g0;
   const int k_first = it.index * it.C, k_end = it.n - k_first < it.C ? it.n : k_first + it.C;  // (C is a multiple of the block)
   // this lane's query head as an operand column
@@ -427,7 +450,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
         y += *(const at_f4 *)(sums + (size_t)(w * rows + row) * PITCH + at) * f;
       }
       if (it.count > 1) {
-        float *to = a.part + ((size_t)blockIdx.x * a.Hq + head) * a.rec;
+        float *to = a.part + ((size_t)item * a.Hq + head) * a.rec;
         if (u == 0 && at == 0) *(float2 *)to = float2{m, l};
         *(at_f4 *)(to + 4 + ch) = y;
         continue;
@@ -510,10 +533,13 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
 // ---- host side ------------------------------------------------------------------------------------------
 // Workgroups for all keys together: as many as are resident at once, which goes by the registers that a head_dim takes.  512 or 1024 of them at 8 kv heads: 64 channels,
 // 16 rows of 8000 56 / 48 us, 128 channels, 8 rows of 2048 19.3 / 21.9, 64 rows of 1000 47.8 / 52.5; 256: 22.5, 47.3, two rows of 131072 262 (512: 189).
-// A row of a cache of up to AT_WHOLE positions is not cut: the second launch would cost more than the few blocks of keys that a wave has left.
+// A row of a cache of up to AT_WHOLE positions is not cut: the second launch costs more than the blocks of keys that a wave has left.  Cut / not, 8 kv heads of 128 channels:
+// one row of 300 10.3 / 7.5, of 500 10.4 / 9.1, of 640 10.4 / 10.2, of 768 10.4 / 11.2, of 1000 10.5 / 13.6; 8 rows of 768 13.2 / 12.0, of 1000 13.7 / 15.0; 16 rows of 600
+// 16.1 / 11.0; 64 rows of 768 38.9 / 35.3.  Where such rows leave every CU at most one workgroup (AT_WIDE), it has eight waves: one row of 300 7.9 -> 7.5, 16 rows of 500
+// 10.4 -> 10.1, but 64 rows of 500 24.3 -> 26.4.
 // ONCE where a layer's K and V pages are more than AT_CACHED bytes, in kernels whose loads are all of whole rows: two rows of 131072 (1.07 GB) 167 us, 189 without; a batch
 // of 32 whose 99 MB stay cached between calls 32.7 us, 29.0 without.
-constexpr int AT_WHOLE = 512;
+constexpr int AT_WHOLE = 768, AT_WIDE = 256;
 constexpr size_t AT_CACHED = (size_t)256 << 20;
 static int at_workgroups(int dh) { return dh <= 64 ? 1024 : dh <= 128 ? 512 : 256; }
 struct AtPlan {
@@ -527,7 +553,7 @@ static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
   r.items = B;
   if (cap > AT_WHOLE) {
     r.target = std::max(1, at_workgroups(p.head_dim) / (p.n_kv_heads * r.tiles));
-    r.items = (int)std::min<long long>((long long)r.target + B, B * ((cap + AT_PIECE - 1) / AT_PIECE));
+    r.items = (int)std::min<long long>((2 * B > r.target ? (long long)AT_FINE : 1) * r.target + B, B * ((cap + AT_PIECE - 1) / AT_PIECE));
     r.bytes = (size_t)r.items * Hq * (p.head_dim + 4) * 4;
     if (B > 64) {
       r.list = r.bytes;
@@ -542,9 +568,9 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   const int g = a.Hq / a.Hkv, rows = std::min(g, AT_ROWS);
   constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
   auto lds = [&](int waves) { return (2 * waves * AT_ROWS + waves * rows * (16 * VC + 4)) * 4; };  // (37 KB at most)
-  const dim3 grid(plan.items, a.Hkv * plan.tiles);
+  const unsigned grid = (unsigned)plan.items * a.Hkv * plan.tiles;
   bool wide = false;
-  if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8;
+  if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8 && plan.items * a.Hkv * plan.tiles <= AT_WIDE;
   if (a.list) {
     ProfScope ps("paged_plan", s);
     paged_plan_kernel<<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);

@@ -43,6 +43,16 @@ __device__ __forceinline__ N lane_through(N v) {
   v += lane_from<0x143, 0xc>(v);
   return v;
 }
+// The largest of a wave's numbers, none of them negative.
+__device__ __forceinline__ int lane_most(int v) {
+  auto most = [](int x, int y) { return x > y ? x : y; };
+  v = most(v, lane_from<0x111, 0xf>(v));
+  v = most(v, lane_from<0x112, 0xf>(v));
+  v = most(v, lane_from<0x114, 0xf>(v));
+  v = most(v, lane_from<0x118, 0xf>(v));
+  v = most(v, lane_from<0x142, 0xa>(v));
+  return lane_value(most(v, lane_from<0x143, 0xc>(v)), 63);
+}
 // The sum of the first n <= 16 of an array in LDS, in every lane.
 template <typename N>
 __device__ __forceinline__ N sum_of(const N *a, int n) {

@@ -368,3 +368,14 @@ def test_attend_many_rows_that_are_not_cut(B):
     req, pos = [r % 4 for r in range(B)], [[512, 1, 100, 33][r % 4] * (1 + r % 7) // 7 - 1 for r in range(B)]
     q = c.queries(B)
     c.check(q, req, pos, c.run(q, req, pos))
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page", SHAPES)
+def test_attend_short_rows_in_a_wide_table(dtype, Hq, Hkv, dh, page):
+    """The same lengths where the table has room for 5000 positions: rows may be cut, and most of them have one item."""
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 127, 128, 129, 700, 1900, 0]
+    c = Case(dtype, Hq, Hkv, dh, page, lens, seed=4, blocks=5000 // page + 1)
+    req = [r for r, n in enumerate(lens) if n] + [11, 12, 3, 14, -1, 4]
+    pos = [n - 1 for n in lens if n] + [0, 350, -1, 5, 5, -9]
+    q = c.queries(len(req))
+    c.check(q, req, pos, c.run(q, req, pos))
