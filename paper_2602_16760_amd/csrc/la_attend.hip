@@ -1,5 +1,7 @@
 // Attention of single tokens over a paged cache (la_paged_attend): the keys of a row are split into items, an item is a workgroup, and a second launch joins
-// the items of rows that have several.  What bounds it is K and V, which are read once for all query heads of a kv head.
+// the items of rows that have several.  K and V are read once for the up to 16 query heads of a kv head that share a tile, and their bytes bound it where they are many: two rows
+// of 131000 positions, 1.07 GB, 167 us, 6.4 TB/s (a large copy here: 5.2); 512 rows of 1000, 2.1 GB, 344 us, 6.1.  A row of 500, 2 MB, takes 9 us, of which the bytes are 0.4: a launch, the
+// positions, the table, K and V, the waves' meeting, each waiting for the one before.
 #include <algorithm>
 #include <type_traits>
 
@@ -64,8 +66,10 @@ __device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (n +
 __device__ __forceinline__ int at_item_keys(int n, int count) { return at_pieces((n + count - 1) / count); }
 // C.  `target` items of the same length are all resident at once.
 //   Up to half as many rows: all keys over `target`, and longer while the rows' remainders make more items than are resident (AT_TURNS times at most).
-//   More rows: where the longest row is much longer than what a resident item would have of all keys, a third of that, so that what is left to the last items is little;
-// otherwise rows are not cut.
+//   More rows: where the longest row is longer than 5/4 of what a resident item would have of all keys, a third of the latter, so that what is left to the last items is little;
+// otherwise rows are not cut.  us with items as for few rows / a half / a third / a quarter, 8 kv heads of 128 channels, rows from one position to n each: 48 rows, n = 4000 48 / 38 / 39 /
+// 39, 64 rows, 4000 60 / 44 / 45 / 45, 64 rows, 30000 386 / 214 / 207 / 205, 256 rows, 4000 152 / 115 / 111 / 112; rows of 2000 each: 40 rows 79 / 65 / 65 / 71, 48 rows 84 / 82 / 76 / 82;
+// 64 rows 89, cut 96 to 102; 96 rows 132, cut 142 to 183.
 constexpr int AT_TURNS = 3, AT_FINE = 3;
 template <typename Items>
 __device__ __forceinline__ int at_cut(const PagedAttend &a, long long keys, int longest, Items items) {
@@ -79,8 +83,8 @@ __device__ __forceinline__ int at_cut(const PagedAttend &a, long long keys, int 
   return C;
 }
 // The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
-// positions, a lane each; of more it was written down by a launch of its own (formed by every workgroup from all rows' positions, 64 at a time, it took 5 of 57 us at 65 rows,
-// and its time grows with the square of the rows).
+// positions, a lane each; of more it was written down by a launch of its own: formed by every workgroup from all rows' positions, 64 at a time, the time grew with the square of the
+// rows (512 rows of 1000 379 us, now 344; 65 rows 57, now 59).
 template <bool BY_ROW>
 __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
   AtItem it{};
@@ -113,7 +117,7 @@ __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
   it.r = lane_value(r, l);
   it.n = lane_value(n, l);
   it.count = lane_value(c, l);
-  it.C = at_item_keys(it.n, it.count);
+  it.C = uniform(at_item_keys(it.n, it.count));
   it.first = lane_value(ends, l) - it.count;
   it.index = BY_ROW ? 0 : wanted - it.first;
   return it;
@@ -206,6 +210,8 @@ __device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int co
 // wants eight keys of one channel in a lane: a lane loads eight channels of its eight keys and turns them around in its registers (half an instruction per
 // element); which channels make up a tile of the output is free, so neighbouring channels of V end up in neighbouring registers.
 //   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
+// Scores, running maximum and sum, and both products' sums are float.  A probability is rounded to the 16-bit type for the second product (half a step of itself, as the output
+// is; its sum is taken before that): in two parts, the rounded one and what it leaves, an infinite V would meet a zero.
 // PAGED16: page_size is a multiple of 16, so that a 16-key tile lies in one page and its address is a scalar; otherwise a lane looks up its own keys' places.
 // FULL: head_dim = DH; otherwise what a lane would load behind a row's end is replaced by zeros.
 // ONCE: K and V are more than the last-level cache holds, so what goes through it is not kept there.
@@ -221,10 +227,10 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   constexpr int VK = 4 * TILES;                    // keys whose V a lane loads
   extern __shared__ __attribute__((aligned(16))) float at_lds[];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
-  const int g = a.Hq / a.Hkv, tiles = (g + AT_ROWS - 1) / AT_ROWS, item = (int)blockIdx.x / (a.Hkv * tiles), share = (int)blockIdx.x - item * a.Hkv * tiles;
+  const int g = uniform(a.Hq / a.Hkv), tiles = uniform((g + AT_ROWS - 1) / AT_ROWS), item = uniform((int)blockIdx.x / (a.Hkv * tiles)), share = (int)blockIdx.x - item * a.Hkv * tiles;
   const AtItem it = at_find<false>(a, item);
   if (it.b < 0) return;  // (all waves)
-  const int h = share / tiles, g0 = share % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
+  const int h = uniform(share / tiles), g0 = share % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
   const int rows = g - g0 < AT_ROWS ? g - g0 : AT_ROWS, head0 = h * g + g0;
   const int k_first = it.index * it.C, k_end = it.n - k_first < it.C ? it.n : k_first + it.C;  // (C is a multiple of the block)
   // this lane's query head as an operand column
@@ -469,7 +475,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
 }
 
 // The items of a row and head, in item order: a workgroup each, whose waves take every fourth item; a lane takes up to four channels.  What it reads does not wait for what
-// the rows' maxima are: they are applied to it.
+// the rows' maxima are: they are applied to it.  5 us for 32 rows of 64 items together (1 MB of records): a launch and two loads' latencies.
 template <typename T>
 __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAttend a) {
   __shared__ float sums[AT_JOIN_WAVES][256];
@@ -532,7 +538,7 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
 
 // ---- host side ------------------------------------------------------------------------------------------
 // Workgroups for all keys together: as many as are resident at once, which goes by the registers that a head_dim takes.  512 or 1024 of them at 8 kv heads: 64 channels,
-// 16 rows of 8000 56 / 48 us, 128 channels, 8 rows of 2048 19.3 / 21.9, 64 rows of 1000 47.8 / 52.5; 256: 22.5, 47.3, two rows of 131072 262 (512: 189).
+// 16 rows of 8000 56 / 48 us, 128 channels, 8 rows of 2048 19.3 / 21.9, 64 rows of 1000 47.8 / 52.5; 256: 22.5, 47.3, two rows of 131072 262 (512: 189, both without ONCE).
 // A row of a cache of up to AT_WHOLE positions is not cut: the second launch costs more than the blocks of keys that a wave has left.  Cut / not, 8 kv heads of 128 channels:
 // one row of 300 10.3 / 7.5, of 500 10.4 / 9.1, of 640 10.4 / 10.2, of 768 10.4 / 11.2, of 1000 10.5 / 13.6; 8 rows of 768 13.2 / 12.0, of 1000 13.7 / 15.0; 16 rows of 600
 // 16.1 / 11.0; 64 rows of 768 38.9 / 35.3.  Where such rows leave every CU at most one workgroup (AT_WIDE), it has eight waves: one row of 300 7.9 -> 7.5, 16 rows of 500

@@ -9,11 +9,14 @@ namespace la {
 // an octave between its a and the row's largest, the second factor lies in [1, 1.091) and is rounded to 36 bits behind the point, wherever it is used.  Sums over a
 // bin are then sums of whole numbers: they do not depend on the order in which LDS atomics take them, and equal logits have equal shares.  Everything behind them
 // is added in a fixed order.  A sum of n weights is off by about 2^-38 / sqrt(n) of itself.  Bins reach 64 octaves down, below which a weight counts as none.
+// Logits are read once, and then, of a row that is cut, the tokens of the cut's bin, of one that is not, a chunk.  The bytes bound neither launch: 64 rows of 131072, 34 MB, 6.5 us at a
+// copy's rate, take 19 + 30 us (factors and atomics of 8.4 million tokens, some 30 instructions each in 64 bits, behind 7 us of loads; then a row's chain of searches, each a few
+// barriers long); one row of 32768 5 + 11 us, all of it that chain.
 constexpr int SMP_BINS = 514, SMP_HIST = 520;  // (64 octaves below the largest token end in the 514th bin at the latest); row length of a chunk's sums
 constexpr int SMP_SUM_THREADS = 512;          // of a workgroup of the first launch
 constexpr int SMP_PER = 16, SMP_PER_SHORT = 4;  // ... tokens of each: chunks of 8192 and of 2048
 constexpr int SMP_LIST = 4608;                // tokens of a cut that fit into LDS
-constexpr int SMP_SHORT = 1024, SMP_FEW = 128;  // tokens down to a cut that are listed with it, a thread each; of them kept that are drawn from without looking at a chunk
+constexpr int SMP_SHORT = 1024, SMP_FEW = 128;  // tokens down to a cut that are listed with it, a thread each; of them kept that are drawn from without looking at a chunk (two a lane)
 constexpr int SMP_SUB = 1024;                 // parts that a range of tokens is cut into at a time
 constexpr int SMP_COUNT_SHIFT = 50;           // a chunk's word of a bin: the number of its tokens above that bit, the sum of their factors below, in units of 2^-36
 constexpr unsigned long long SMP_SUM_MASK = (1ull << SMP_COUNT_SHIFT) - 1;
@@ -21,7 +24,9 @@ constexpr double SMP_UNIT = 0x1p36, LEAST_WEIGHT = 0x1p-64;
 constexpr int SMP_MOST = SMP_SUM_THREADS * SMP_PER;
 static_assert(SMP_MOST * 1.1 * SMP_UNIT < (double)SMP_SUM_MASK && SMP_MOST <= 1 << 13, "a chunk in one bin");
 static_assert(LA_MAX_SAMPLE_VOCAB * 1.1 * SMP_UNIT < 0x1p64 && LA_MAX_SAMPLE_VOCAB / SMP_MOST <= 64, "a row in one bin; a lane per chunk");
-// Short chunks while that leaves a row at most 16 of them: the first launch has four times the workgroups, the second reads as many sums.
+// Short chunks while that leaves a row at most 16 of them: the first launch has four times the workgroups, the second reads as many sums.  us, short / long chunks: 8192 tokens, 1, 8
+// and 64 rows 17.5 / 19.4, 18.2 / 20.6, 18.9 / 21.1; 32768 17.0 / 19.2, 18.9 / 21.3, 24.4 / 22.6; 65536, 1 and 64 rows 20.0 / 19.9, 32.1 / 26.8; 131072, 1 row 24.8 / 20.7.  (Not by the
+// number of rows: a row's sums are added by chunks, and do not depend on the rows beside it.)
 static int sample_per(int V) { return V <= 16 * SMP_SUM_THREADS * SMP_PER_SHORT ? SMP_PER_SHORT : SMP_PER; }
 
 struct Sample {

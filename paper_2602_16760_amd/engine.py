@@ -177,15 +177,15 @@ class Engine:
     # -- several requests at once -----------------------------------------------------------------
     def generate_batch(self, prompts, n_new: int, page_size: int = 16, n_pages: int | None = None, sampling: dict | None = None):
         """Sequential generation of n_new tokens for up to 64 prompts together, a token of each per step, on a cache of pages that they share (n_pages: as many as they need if
-        left out).  sampling: as in generate, the numbers as u[step][request].  Returns (tokens [requests, n_new], stats)."""
+        left out); the contiguous cache takes one prompt after the other on its way there.  sampling: as in generate, the numbers as u[step][request].  Returns (tokens [requests, n_new], stats)."""
         sh, R, dev = self.shape, len(prompts), "cuda"
         prompts = [np.asarray(p, dtype=np.int32) for p in prompts]
         if not 1 <= R <= B.LA_MAX_ROWS or any(len(p) < 1 for p in prompts):
             raise ValueError(f"need 1 to {B.LA_MAX_ROWS} prompts of one token at least")
         lens = [len(p) - 1 for p in prompts]
         pages_of = lambda n: (n + page_size - 1) // page_size
-        blocks = max(pages_of(n + n_new) for n in lens)
-        n_pages = sum(pages_of(n + n_new) for n in lens) if n_pages is None else n_pages
+        blocks = max(1, max(pages_of(n + n_new) for n in lens))
+        n_pages = max(1, sum(pages_of(n + n_new) for n in lens)) if n_pages is None else n_pages
         i32 = lambda n, v=0: torch.full(n if isinstance(n, tuple) else (n,), v, dtype=torch.int32, device=dev)
         dt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[sh.dtype]
         pages = B.la_pages(*(torch.empty((sh.n_layers, n_pages, sh.n_kv_heads, page_size, sh.head_dim), dtype=dt, device=dev) for _ in range(2)))

@@ -218,3 +218,21 @@ def test_sampling_parameters_are_checked():
             eng.generate_batch([], 4)
     finally:
         eng.close()
+
+
+@pytest.mark.parametrize("lens,n_new", [([1], 0), ([4, 1], 0), ([1, 1, 1], 1), ([17], 1)])
+def test_batches_of_next_to_nothing(lens, n_new):
+    """Prompts of one token, no token or one to generate: the shapes, and the pages all given back."""
+    shape = synth.SHAPES["small_bf16"]
+    eng = gpu_engine(shape, 64)
+    try:
+        prompts = [np.arange(3, 3 + n) for n in lens]
+        tokens, stats = eng.generate_batch(prompts, n_new)
+        assert tokens.shape == (len(lens), n_new) and stats["free_pages"] == stats["pages"]
+        for p, t in zip(prompts, tokens):
+            alone, _ = eng.generate_batch([p], n_new)
+            assert (alone[0] == t).all()
+        with pytest.raises(binding().LaError):  # longer than the contiguous cache that prompts go through
+            eng.generate_batch([np.zeros(100, dtype=np.int64)], 2)
+    finally:
+        eng.close()
