@@ -229,7 +229,8 @@ int la_prefill(la_model *m, la_kv *kv, const int32_t *tok, int n, int L0, void *
  * device float, row b at logits + b * row_stride (row_stride >= vocab).  On the matrix-core path the normalised rows are
  * multiplied as two half-precision numbers each, which keep 22 significant bits, so that the logits have float's accuracy
  * (la_unembed_argmax rounds them to 11; logits closer than that may be ordered otherwise here).  Allocates nothing.
- * LA_EINVAL: Bp not in 1..LA_MAX_ROWS, a NULL pointer, rows that overlap, a model without final norm or unembedding. */
+ * (hidden * g_final beyond +-65504 saturates on that path, as in la_unembed_argmax.)
+ * LA_EINVAL: Bp not in 1..LA_MAX_ROWS, a NULL pointer, rows that overlap, a model without final norm or unembedding, the LDS-ring kernel's weight layout. */
 int la_unembed_logits(la_model *m, const float *hidden, int Bp, float *logits, int64_t row_stride, void *stream);
 
 /* ---- sampling ------------------------------------------------------------------------------- */
@@ -308,7 +309,8 @@ int la_paged_write(const la_pages_desc *pages, int layer, const void *k, const v
  * looked at.  Scores, softmax and sums are float; 16-bit types multiply as stored, the probabilities rounded to that type.
  * workspace: device memory of la_paged_attend_workspace bytes (0 where none is needed), 16-byte aligned, which the call may overwrite and which no
  * other call may use meanwhile; nothing is kept in it.
- * LA_EINVAL: a NULL pointer, bad dimensions or alignment; LA_ENOMEM: workspace too small; LA_ERANGE: layer.  B = 0 does nothing. */
+ * LA_EINVAL: a NULL pointer, bad dimensions or alignment, more rows and kv heads than one launch takes (2^24 workgroups: 2^20 rows of 15 heads); LA_ENOMEM: workspace too
+ * small; LA_ERANGE: layer.  B = 0 does nothing. */
 size_t la_paged_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int B);
 int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table,
                     int64_t table_stride, int n_requests, int max_blocks, const int32_t *req, const int32_t *pos, int B, void *out, int64_t out_stride,

@@ -576,7 +576,7 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   auto lds = [&](int waves) { return (2 * waves * AT_ROWS + waves * rows * (16 * VC + 4)) * 4; };  // (37 KB at most)
   const unsigned grid = (unsigned)plan.items * a.Hkv * plan.tiles;
   bool wide = false;
-  if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8 && plan.items * a.Hkv * plan.tiles <= AT_WIDE;
+  if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8 && (long long)plan.items * a.Hkv * plan.tiles <= AT_WIDE;
   if (a.list) {
     ProfScope ps("paged_plan", s);
     paged_plan_kernel<<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
@@ -663,6 +663,7 @@ extern "C" int la_paged_attend(const la_pages_desc *pages, int layer, const void
   LA_REQUIRE(aligned16({q, out}) && q_stride * e % 16 == 0 && out_stride * e % 16 == 0, LA_EINVAL, "q and out rows must be 16-byte aligned");
   LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
   const AtPlan plan = at_plan(p, n_q_heads, max_blocks, B);
+  LA_REQUIRE((long long)plan.items * p.n_kv_heads * plan.tiles < 1ll << 24, LA_EINVAL, "%d rows of %d kv heads are more than one launch takes", B, p.n_kv_heads);  // (2^32 threads)
   LA_REQUIRE(workspace_bytes >= plan.bytes && (workspace || !plan.bytes), LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
   LA_REQUIRE(aligned16({workspace}), LA_EINVAL, "workspace must be 16-byte aligned");
   hipStream_t s = (hipStream_t)stream;

@@ -379,3 +379,16 @@ def test_attend_short_rows_in_a_wide_table(dtype, Hq, Hkv, dh, page):
     pos = [n - 1 for n in lens if n] + [0, 350, -1, 5, 5, -9]
     q = c.queries(len(req))
     c.check(q, req, pos, c.run(q, req, pos))
+
+
+@pytest.mark.parametrize("blocks", [None, 400])
+def test_attend_a_hundred_thousand_rows(blocks):
+    """All rows of a request and position alike, the first, last and some between against 64 bits."""
+    lens, B = [300, 1, 40, 17], 100001
+    c = Case("f16", 2, 1, 8, 16, lens, seed=7, blocks=blocks)
+    req = [r % 4 for r in range(B)]
+    pos = [lens[r] - 1 for r in req]
+    q = c.queries(4).repeat(B // 4 + 1, 1, 1)[:B]
+    out = c.run(q, req, pos)
+    c.check(q[:4], req[:4], pos[:4], out[:4])
+    assert torch.equal(out, out[:4].repeat(B // 4 + 1, 1, 1)[:B])

@@ -134,3 +134,10 @@ def test_write_takes_no_more_threads_than_a_launch_has():
     """A thread per 16 bytes of a row of K: 2^32 of them are refused, whatever their workgroups number."""
     rows = (1 << 32) // (64 * 32)
     refused(lib.la_paged_write(*{**WRITE, "pages": pages(n_kv_heads=64, head_dim=256), "n": rows}.values()), EINVAL, "more than one launch")
+
+
+@pytest.mark.parametrize("rows,heads", [(1 << 20, 16), (1 << 20, 4096), (300, 65535)])
+@pytest.mark.parametrize("blocks", [8, 1000])
+def test_attend_takes_no_more_workgroups_than_a_launch_has(rows, heads, blocks):
+    call = {**ATTEND, "pages": pages(n_kv_heads=heads), "Hq": heads, "B": rows, "blocks": blocks, "ldt": blocks, "ws_bytes": 1 << 62}
+    refused(lib.la_paged_attend(*call.values()), EINVAL, "more than one launch")
