@@ -484,6 +484,19 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.y;
   const size_t step = (size_t)a.Hq * a.rec;
   const float *rec = a.part + ((size_t)it.first * a.Hq + head) * a.rec;
+  const int parts = (a.dh + 63) / 64;
+  constexpr int N = 4;
+  float v[N][4], s[N];  // channels lane, lane + 64, ... of items i0, i0 + AT_JOIN_WAVES, ...
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = i0 + AT_JOIN_WAVES * k < it.count ? i0 + AT_JOIN_WAVES * k : 0;
+      s[k] = rec[i * step];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[k][c] = c < parts ? rec[i * step + 4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)] : 0.f;
+    }
+  };
+  fetch(wave);
   float m = -INFINITY, l = 0.f;
   for (int i0 = 0; i0 < it.count; i0 += 64) {
     const float2 s = i0 + lane < it.count ? *(const float2 *)(rec + (i0 + lane) * step) : float2{-INFINITY, 0.f};
@@ -498,18 +511,9 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
   l *= __builtin_amdgcn_exp2f(m - base);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};  // channels lane, lane + 64, ...
-  const int parts = (a.dh + 63) / 64;
-  constexpr int N = 4;
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
   for (int i0 = wave; i0 < it.count; i0 += N * AT_JOIN_WAVES) {
-    float v[N][4], s[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int i = i0 + AT_JOIN_WAVES * k < it.count ? i0 + AT_JOIN_WAVES * k : i0;
-      s[k] = rec[i * step];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) v[k][c] = c < parts ? rec[i * step + 4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)] : 0.f;
-    }
+    if (i0 > wave) fetch(i0);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const float f = i0 + AT_JOIN_WAVES * k < it.count ? __builtin_amdgcn_exp2f(s[k] - base) : 0.f;
