@@ -62,8 +62,8 @@ __device__ __forceinline__ int at_pieces(long long keys) {
   const long long n = (keys + AT_PIECE - 1) / AT_PIECE;
   return (int)(n < 1 ? 1 : n < 0xffffff ? n : 0xffffff) * AT_PIECE;
 }
-__device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (n + C - 1) / C : 1; }
-__device__ __forceinline__ int at_item_keys(int n, int count) { return at_pieces((n + count - 1) / count); }
+__device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (int)(((unsigned)n + (unsigned)C - 1u) / (unsigned)C) : 1; }  // (n + C passes 31 bits)
+__device__ __forceinline__ int at_item_keys(int n, int count) { return at_pieces(((unsigned)n + (unsigned)count - 1u) / (unsigned)count); }
 // C.  `target` items of the same length are all resident at once.
 //   Up to half as many rows: all keys over `target`, and longer while the rows' remainders make more items than are resident (AT_TURNS times at most).
 //   More rows: where the longest row is longer than 5/4 of what a resident item would have of all keys, a third of the latter, so that what is left to the last items is little;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   const float to_log2 = a.scale * AT_LOG2E;
   const int row_bytes = dh * E;
   const int32_t *tab = a.table + it.r * a.ldt;
-  const int n_blocks = (k_end - k_first + KEYS - 1) / KEYS, mine = n_blocks > wave ? (n_blocks - wave + WAVES - 1) / WAVES : 0;
+  const int n_blocks = (int)(((unsigned)(k_end - k_first) + KEYS - 1u) / KEYS), mine = n_blocks > wave ? (n_blocks - wave + WAVES - 1) / WAVES : 0;
   // Where the tiles lie: PAGED16: lane i holds byte offset and number of keys of tile i of the next 64 of this wave; else lane j < KEYS the offset of key j of the block, -1: none.
   unsigned off_lo = 0, off_hi = 0;
   int n_keys = 0;

@@ -392,3 +392,31 @@ def test_attend_a_hundred_thousand_rows(blocks):
     out = c.run(q, req, pos)
     c.check(q[:4], req[:4], pos[:4], out[:4])
     assert torch.equal(out, out[:4].repeat(B // 4 + 1, 1, 1)[:B])
+
+
+@pytest.mark.parametrize("Hq,dh", [(1, 8), (3, 256)])
+def test_attend_the_longest_row(Hq, dh):
+    """A table of 2^31 - 16 positions, a few pages of it: at its ends, in its middle and around it, beside a short row."""
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("not enough memory")
+    B, blocks, page = binding(), (1 << 27) - 1, 16
+    g = torch.Generator().manual_seed(dh)
+    k, v = (torch.randn((1, 6, 1, page, dh), generator=g).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((2, Hq, dh), generator=g).to(torch.bfloat16)
+    table = torch.full((2, blocks), -1, dtype=torch.int32, device="cuda")
+    at = [0, 1 << 20, blocks // 2, blocks // 2 + 1, blocks - 2, blocks - 1]
+    for p, b in enumerate(at):
+        table[0, b] = (p + 2) % 6
+    table[1, 0] = 4
+    out = torch.empty_like(q, device="cuda")
+    B.la_paged_attend(B.la_pages(k.cuda(), v.cuda()), 0, q.cuda(), table, None, i32([blocks * page - 1, 4]), out)
+    pages = [(p + 2) % 6 for p in range(6)]
+    keys = [k[0, pages, 0].reshape(-1, dh), k[0, 4, 0, :5]]
+    values = [v[0, pages, 0].reshape(-1, dh), v[0, 4, 0, :5]]
+    half = torch.finfo(torch.bfloat16).eps / 2
+    for r in range(2):
+        w = torch.softmax(q[r].double() @ keys[r].double().t() * dh ** -0.5, 1)
+        want, mass = w @ values[r].double(), w @ values[r].double().abs()
+        size = (q[r].double().abs() @ keys[r].double().abs().t()).amax(1, keepdim=True) * dh ** -0.5
+        tol = half * mass + half * want.abs() + 2 * (dh + 8) * 2.0 ** -24 * size * mass + (len(keys[r]) + 16) * 2.0 ** -23 * mass + 1e-30
+        assert ((out[r].cpu().double() - want).abs() <= tol).all()
