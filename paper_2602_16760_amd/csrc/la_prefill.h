@@ -990,7 +990,7 @@ int mfma_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRo
     };
     int S_o = 0;
     if ((rc = pf_launch_norm(S_down, hidden, b.part, m->layers[l].g_attn, M, d.d_model, RT, b.ss, b.A, s))) return rc;
-    // Without tiles, at any number of rows and columns, so that a row's sums do not depend on how many rows there are.  us of a layer without a long context and a wide MLP,
+    // Without tiles, at any number of rows and columns: a row's q, K and V are summed alike at any number of rows.  us of a layer without a long context and a wide MLP,
     // without / with tiles, at 1, 32 and 64 rows: 4096 x 6144 (192 workgroups) 72 / 84, 76 / 86, 86 / 95; 4096 x 8192 (256) 75 / 86, 80 / 91, 94 / 103; 4096 x 12288 (384)
     // 83 / 89, 98 / 100, 122 / 120; 8192 x 10240 (320) 143 / 152, 152 / 156, 174 / 167.
     {
