@@ -212,6 +212,9 @@ __device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int co
 //   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
 // Scores, running maximum and sum, and both products' sums are float.  A probability is rounded to the 16-bit type for the second product (half a step of itself, as the output
 // is; its sum is taken before that): in two parts, the rounded one and what it leaves, an infinite V would meet a zero.
+// Half precision has no small numbers: below 2^-14 its step is 2^-24, below 2^-25 nothing is left, while a thousand such weights beside one of 1 are a thousandth of the sum.  So
+// its weights are up to 2^15 instead of 1 (UP; the sums carry the factor too, and it cancels): a step below 2^-29 of the largest is 2^-39 of it.  Keys behind a first one of 2^22.5,
+// 2^25 and 2^30 times their weight: 512 of them off by 0.8, 12 and 12 % without it, by half a step of the output with it.
 // PAGED16: page_size is a multiple of 16, so that a 16-key tile lies in one page and its address is a scalar; otherwise a lane looks up its own keys' places.
 // FULL: head_dim = DH; otherwise what a lane would load behind a row's end is replaced by zeros.
 // ONCE: K and V are more than the last-level cache holds, so what goes through it is not kept there.
@@ -225,6 +228,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   constexpr int VC = VW / E;                       // channels of one
   constexpr int DT = DH / 16;                      // tiles of the output: channel VH-th part, one of VC
   constexpr int VK = 4 * TILES;                    // keys whose V a lane loads
+  constexpr float UP = std::is_same<T, _Float16>::value ? 15.f : 0.f;  // all weights carry 2^UP
   extern __shared__ __attribute__((aligned(16))) float at_lds[];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
   const int g = uniform(a.Hq / a.Hkv), tiles = uniform((g + AT_ROWS - 1) / AT_ROWS), item = uniform((int)blockIdx.x / (a.Hkv * tiles)), share = (int)blockIdx.x - item * a.Hkv * tiles;
@@ -373,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        s[t][e] = __builtin_amdgcn_exp2f(s[t][e] - base);
+        s[t][e] = __builtin_amdgcn_exp2f(s[t][e] - base + UP);
         l_run += s[t][e];
       }
     if (now != all) {

@@ -420,3 +420,25 @@ def test_attend_the_longest_row(Hq, dh):
         size = (q[r].double().abs() @ keys[r].double().abs().t()).amax(1, keepdim=True) * dh ** -0.5
         tol = half * mass + half * want.abs() + 2 * (dh + 8) * 2.0 ** -24 * size * mass + (len(keys[r]) + 16) * 2.0 ** -23 * mass + 1e-30
         assert ((out[r].cpu().double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("n", [33, 512, 5000])
+@pytest.mark.parametrize("gap", [10, 18, 22.5, 23.5, 25.2, 30, 36])
+def test_attend_one_key_far_above_the_others(dtype, n, gap):
+    """A first key of 2^gap times the weight of every other one, whose values are zeros: the output is what the others leave beside it, n - 1 small weights that are not lost.  Equal
+    values, so the error is that of the weights: half a step of the type each, of the output as much, and of the exponentials and their sums 2^-23 a term; of the first score three
+    roundings of up to 38 at 2^-24 (1 / ln 2, the product, the difference)."""
+    blocks, dh, far = (n + 15) // 16, 64, 2.0 ** 15
+    B = binding()
+    k = torch.zeros((1, blocks, 1, 16, dh), dtype=T[dtype], device="cuda")
+    v = torch.full_like(k, far)
+    k[0, 0, 0, 0, 0], v[0, 0, 0, 0] = gap * float(np.log(2)), 0
+    q, out = torch.zeros((1, 4, dh), dtype=T[dtype], device="cuda"), torch.empty((1, 4, dh), dtype=T[dtype], device="cuda")
+    q[..., 0] = 1
+    B.la_paged_attend(B.la_pages(k, v), 0, q, torch.arange(blocks, dtype=torch.int32, device="cuda")[None], None, i32([n - 1]), out, scale=1.0)
+    w = (n - 1) * float(np.exp(-float(k[0, 0, 0, 0, 0])))
+    want, half = far * w / (1 + w), torch.finfo(T[dtype]).eps / 2
+    least = 2.0 ** -25 if dtype == "f16" else 0.0  # (half a step of half precision below 2^-14)
+    tol = (2 * half + (n + 16) * 2.0 ** -23 + 114 * 2.0 ** -24) * want + least
+    assert (out.double() - want).abs().max() <= tol
