@@ -187,6 +187,17 @@ __device__ __forceinline__ unsigned at_pack(float lo, float hi) {  // to nearest
     return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), b2));
   }
 }
+// Two weights as the sum of two 16-bit numbers each, both above zero where the weight is, so that an infinite V stays one: the first is short of the weight by one to three half
+// steps, the second is what that leaves.  Together they are off by 2^-20 of the weight at most (half precision), 2^-14 (bfloat16).
+template <typename T>
+__device__ __forceinline__ at_u2 at_split(float x, float y) {
+  constexpr bool F16 = std::is_same<T, _Float16>::value;
+  constexpr float SHORT = F16 ? 1.f - 0x1p-10f : 1.f - 0x1p-7f;
+  const unsigned first = at_pack<T>(x * SHORT, y * SHORT);
+  const float x0 = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(first & 0xffffu)) : __uint_as_float(first << 16);
+  const float y0 = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(first >> 16)) : __uint_as_float(first & 0xffff0000u);
+  return at_u2{first, at_pack<T>(x - x0, y - y0)};
+}
 template <typename T>
 __device__ __forceinline__ at_f4 at_mma(at_u4 x, at_u4 y, at_f4 c) {
   if constexpr (std::is_same<T, _Float16>::value)
@@ -210,8 +221,8 @@ __device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int co
 // wants eight keys of one channel in a lane: a lane loads eight channels of its eight keys and turns them around in its registers (half an instruction per
 // element); which channels make up a tile of the output is free, so neighbouring channels of V end up in neighbouring registers.
 //   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
-// Scores, running maximum and sum, and both products' sums are float.  A probability is rounded to the 16-bit type for the second product (half a step of itself, as the output
-// is; its sum is taken before that): in two parts, the rounded one and what it leaves, an infinite V would meet a zero.
+// Scores, running maximum and sum, and both products' sums are float.  A weight goes into the second product as two 16-bit numbers (at_split), which costs a product more for each
+// of V's: rounded to one, its half step comes out as large as the output's own (a row of 500, bfloat16: 1.8e-3 off as a whole, now 1.6e-3, which is what rounding the exact output leaves).
 // Half precision has no small numbers: below 2^-14 its step is 2^-24, below 2^-25 nothing is left, while a thousand such weights beside one of 1 are a thousandth of the sum.  So
 // its weights are up to 2^15 instead of 1 (UP; the sums carry the factor too, and it cancels): a step below 2^-29 of the largest is 2^-39 of it.  Keys behind a first one of 2^22.5,
 // 2^25 and 2^30 times their weight: 512 of them off by 0.8, 12 and 12 % without it, by half a step of the output with it.
@@ -398,7 +409,13 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
           for (int w = 0; w < VC; ++w)
             o[u * VC + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[e][u][w]), s[0][e], o[u * VC + w], 0, 0, 0);
     } else {
-      const at_u4 p = {at_pack<T>(s[0][0], s[0][1]), at_pack<T>(s[0][2], s[0][3]), at_pack<T>(s[TILES - 1][0], s[TILES - 1][1]), at_pack<T>(s[TILES - 1][2], s[TILES - 1][3])};
+      at_u4 p, rest;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const at_u2 both = at_split<T>(s[j / 2 % TILES][2 * (j & 1)], s[j / 2 % TILES][2 * (j & 1) + 1]);
+        p[j] = both[0];
+        rest[j] = both[1];
+      }
 #pragma unroll
       for (int u = 0; u < VH; ++u)
 #pragma unroll
@@ -409,7 +426,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               v[j] = __builtin_amdgcn_perm(vr[(2 * j + 1) % VK][u][w], vr[2 * j % VK][u][w], half ? 0x07060302u : 0x05040100u);
-            o[u * VC + 2 * w + half] = at_mma<T>(v, p, o[u * VC + 2 * w + half]);
+            o[u * VC + 2 * w + half] = at_mma<T>(v, rest, at_mma<T>(v, p, o[u * VC + 2 * w + half]));
           }
     }
     if (i + 1 < mine) {

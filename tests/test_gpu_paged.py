@@ -442,3 +442,46 @@ def test_attend_one_key_far_above_the_others(dtype, n, gap):
     least = 2.0 ** -25 if dtype == "f16" else 0.0  # (half a step of half precision below 2^-14)
     tol = (2 * half + (n + 16) * 2.0 ** -23 + 114 * 2.0 ** -24) * want + least
     assert (out.double() - want).abs().max() <= tol
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page", [s for s in SHAPES if s[0] != "f32"])
+@pytest.mark.parametrize("spread,blocks", [(1.0, None), (3.0, 6000)])
+def test_attend_rounds_its_output_and_little_else(dtype, Hq, Hkv, dh, page, spread, blocks):
+    """16-bit types, rows that are cut and such that are not: beside the output's rounding, and what float scores, exponentials and sums leave, a weight is off by its second part's
+    rounding alone: 3/2 steps of the first times half a step, 2^-20 of it (half precision; 2^-40 of the largest one at least) or 2^-14 (bfloat16)."""
+    lens = [1, 2, 33, 129, 700, 1500]
+    c = Case(dtype, Hq, Hkv, dh, page, lens, seed=21, spread=spread, blocks=blocks and blocks // page + 1)
+    q, pos = c.queries(len(lens)), [n - 1 for n in lens]
+    out = c.run(q, None, pos)
+    half, part, least, g = torch.finfo(T[dtype]).eps / 2, 2.0 ** -20 if dtype == "f16" else 2.0 ** -14, 2.0 ** -40 if dtype == "f16" else 0.0, Hq // Hkv
+    for b, n in enumerate(lens):
+        k, v = (t.double().repeat_interleave(g, 1) for t in c.rows[b])
+        s = torch.einsum("hd,nhd->hn", q[b].double(), k) * dh ** -0.5
+        size = torch.einsum("hd,nhd->hn", q[b].double().abs(), k.abs()).amax(1) * dh ** -0.5
+        w = torch.softmax(s, 1)
+        want, mass = torch.einsum("hn,nhd->hd", w, v), torch.einsum("hn,nhd->hd", w, v.abs())
+        shift = ((dh + 8) * 2.0 ** -24 * size)[:, None]
+        tol = half * want.abs() + (1 + half) * (part + 2 * shift + (n + 16) * 2.0 ** -23) * mass + n * least * v.abs().amax(0) + 2.0 ** -25
+        err = (out[b].double() - want).abs()
+        assert (err <= tol).all(), f"row of {n}: {float((err / tol).max()):.2f} of the bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("gap", [0, 5.5, 13, 20, 27])
+def test_attend_an_infinite_value_of_any_weight(dtype, gap):
+    """Keys of 2^-gap of the largest weight and about it, one of them with an infinite V of each sign: the output is infinite there, and nowhere a NaN."""
+    n, dh = 96, 64
+    g = torch.Generator().manual_seed(int(10 * gap))
+    B = binding()
+    k, v = torch.zeros((1, 6, 1, 16, dh), dtype=T[dtype]), torch.randn((1, 6, 1, 16, dh), generator=g).to(T[dtype])
+    k[0, :, 0, :, 0] = (-(gap + torch.rand((6, 16), generator=g)) * float(np.log(2))).to(T[dtype])
+    k[0, 0, 0, 0, 0] = 0
+    for i, t in enumerate((1, 17, 40, 63, 64, 95)):
+        v[0, t // 16, 0, t % 16, 8 * i + 3] = float("inf") if i % 2 else float("-inf")
+    q, out = torch.zeros((1, 3, dh), dtype=T[dtype], device="cuda"), torch.empty((1, 3, dh), dtype=T[dtype], device="cuda")
+    q[..., 0] = 1
+    B.la_paged_attend(B.la_pages(k.cuda(), v.cuda()), 0, q, i32([[0, 1, 2, 3, 4, 5]]), None, i32([n - 1]), out, scale=1.0)
+    at = [8 * i + 3 for i in range(6)]
+    assert out[0, :, at].tolist() == [[float("inf") if i % 2 else float("-inf") for i in range(6)]] * 3
+    rest = [d for d in range(dh) if d not in at]
+    assert torch.isfinite(out[0][:, rest]).all()
