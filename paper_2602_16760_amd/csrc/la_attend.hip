@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "la_attend_plan.h"
 #include "la_lanes.h"
 #include "la_paged.h"
 
@@ -15,11 +16,6 @@ typedef _Float16 __attribute__((ext_vector_type(8))) at_h8;
 typedef float __attribute__((ext_vector_type(4))) at_f4;
 typedef unsigned __attribute__((ext_vector_type(4))) at_u4;
 typedef unsigned __attribute__((ext_vector_type(2))) at_u2;
-
-struct AtItem {
-  int b, r, n, C, index, first, count;  // row, its request and keys; keys per item; which of the row's items; the row's first item; how many it has
-  int pad;
-};
 
 struct PagedAttend {
   const void *K, *V;  // of the layer
@@ -46,8 +42,6 @@ struct PagedAttend {
 
 constexpr int AT_WAVES = 4, AT_WHOLE_WAVES = 8;  // of a workgroup; where rows are not cut and heads are few
 constexpr int AT_JOIN_WAVES = 4;
-constexpr int AT_ROWS = 16;       // query heads of a tile
-constexpr int AT_PIECE = 128;     // an item's keys are a multiple of this
 constexpr float AT_LOG2E = 1.4426950408889634f;
 
 // Keys that row b sees (none where it is padding or names no request), and its request.
@@ -57,31 +51,6 @@ __device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
   return (unsigned)r >= (unsigned)a.n_req || n < 0 ? 0 : (int)(n < cap ? n : cap);
 }
 
-// The items: a row of n keys has max(1, ceil(n / C)) of them, as equal as multiples of AT_PIECE are.
-__device__ __forceinline__ int at_pieces(long long keys) {
-  const long long n = (keys + AT_PIECE - 1) / AT_PIECE;
-  return (int)(n < 1 ? 1 : n < 0xffffff ? n : 0xffffff) * AT_PIECE;
-}
-__device__ __forceinline__ int at_rows_items(int n, int C) { return n > C ? (int)(((unsigned)n + (unsigned)C - 1u) / (unsigned)C) : 1; }  // (n + C passes 31 bits)
-__device__ __forceinline__ int at_item_keys(int n, int count) { return at_pieces(((unsigned)n + (unsigned)count - 1u) / (unsigned)count); }
-// C.  `target` items of the same length are all resident at once.
-//   Up to half as many rows: all keys over `target`, and longer while the rows' remainders make more items than are resident (AT_TURNS times at most).
-//   More rows: where the longest row is longer than 5/4 of what a resident item would have of all keys, a third of the latter, so that what is left to the last items is little;
-// otherwise rows are not cut.  us with items as for few rows / a half / a third / a quarter, 8 kv heads of 128 channels, rows from one position to n each: 48 rows, n = 4000 48 / 38 / 39 /
-// 39, 64 rows, 4000 60 / 44 / 45 / 45, 64 rows, 30000 386 / 214 / 207 / 205, 256 rows, 4000 152 / 115 / 111 / 112; rows of 2000 each: 40 rows 79 / 65 / 65 / 71, 48 rows 84 / 82 / 76 / 82;
-// 64 rows 89, cut 96 to 102; 96 rows 132, cut 142 to 183.
-constexpr int AT_TURNS = 3, AT_FINE = 3;
-template <typename Items>
-__device__ __forceinline__ int at_cut(const PagedAttend &a, long long keys, int longest, Items items) {
-  if (2 * a.B > a.target) return longest * 4ll * a.target <= 5 * keys ? at_pieces(longest) : at_pieces((keys + AT_FINE * a.target - 1) / (AT_FINE * a.target));
-  int C = at_pieces((keys + a.target - 1) / a.target);
-  for (int turn = 0; turn < AT_TURNS; ++turn) {
-    const int n = items(C);
-    if (n <= a.target) break;
-    C = at_pieces((long long)C * n / a.target + 1);
-  }
-  return C;
-}
 // The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
 // positions, a lane each; of more it was written down by a launch of its own: formed by every workgroup from all rows' positions, 64 at a time, the time grew with the square of the
 // rows (512 rows of 1000 379 us, now 344; 65 rows 57, now 59).
@@ -94,7 +63,7 @@ __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
     it.b = wanted;
     it.r = uniform(r);
     it.n = uniform(n);
-    it.C = 0x7fffff80;
+    it.C = AT_UNCUT;
     it.first = wanted;
     it.count = 1;
     return it;
@@ -109,7 +78,7 @@ __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
     ends = lane_through(c);
     return lane_value(ends, 63);
   };
-  (void)items(at_cut(a, lane_value(lane_through((long long)n), 63), lane_most(n), items));
+  (void)items(at_cut(a.B, a.target, lane_value(lane_through((long long)n), 63), lane_most(n), items));
   const int l = BY_ROW ? wanted : __builtin_popcountll(__ballot(ends <= wanted));
   it.b = -1;
   if (l >= a.B) return it;
@@ -149,7 +118,7 @@ __global__ __launch_bounds__(AT_PLAN_THREADS) void paged_plan_kernel(PagedAttend
   if (lane == 0) red[wave] = longest;
   __syncthreads();
   longest = lane_most(lane < WAVES ? (int)red[lane] : 0);
-  const int C = at_cut(a, keys, longest, [&](int C) {
+  const int C = at_cut(a.B, a.target, keys, longest, [&](int C) {
     long long c = 0;
     for (int b = t; b < a.B; b += AT_PLAN_THREADS) c += at_rows_items(at_keys(a, b, r), C);
     return (int)all_of(c);
@@ -247,7 +216,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   if (it.b < 0) return;  // (all waves)
   const int h = uniform(share / tiles), g0 = share % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
   const int rows = g - g0 < AT_ROWS ? g - g0 : AT_ROWS, head0 = h * g + g0;
-  const int k_first = it.index * it.C, k_end = it.n - k_first < it.C ? it.n : k_first + it.C;  // (C is a multiple of the block)
+  const int k_first = it.index * it.C, k_end = at_item_end(it);  // (C is a multiple of the block)
   // this lane's query head as an operand column
   at_u4 q[KP];
   {
@@ -562,37 +531,13 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
 }
 
 // ---- host side ------------------------------------------------------------------------------------------
-// Workgroups for all keys together: as many as are resident at once, which goes by the registers that a head_dim takes.  512 or 1024 of them at 8 kv heads: 64 channels,
-// 16 rows of 8000 56 / 48 us, 128 channels, 8 rows of 2048 19.3 / 21.9, 64 rows of 1000 47.8 / 52.5; 256: 22.5, 47.3, two rows of 131072 262 (512: 189, both without ONCE).
-// A row of a cache of up to AT_WHOLE positions is not cut: the second launch costs more than the blocks of keys that a wave has left.  Cut / not, 8 kv heads of 128 channels:
-// one row of 300 10.3 / 7.5, of 500 10.4 / 9.1, of 640 10.4 / 10.2, of 768 10.4 / 11.2, of 1000 10.5 / 13.6; 8 rows of 768 13.2 / 12.0, of 1000 13.7 / 15.0; 16 rows of 600
-// 16.1 / 11.0; 64 rows of 768 38.9 / 35.3.  Where such rows leave every CU at most one workgroup (AT_WIDE), it has eight waves: one row of 300 7.9 -> 7.5, 16 rows of 500
+// Where rows that are not cut leave every CU at most one workgroup (AT_WIDE), it has eight waves, 8 kv heads of 128 channels: one row of 300 7.9 -> 7.5 us, 16 rows of 500
 // 10.4 -> 10.1, but 64 rows of 500 24.3 -> 26.4.
 // ONCE where a layer's K and V pages are more than AT_CACHED bytes, in kernels whose loads are all of whole rows: two rows of 131072 (1.07 GB) 167 us, 189 without; a batch
 // of 32 whose 99 MB stay cached between calls 32.7 us, 29.0 without.
-constexpr int AT_WHOLE = 768, AT_WIDE = 256;
+constexpr int AT_WIDE = 256;
 constexpr size_t AT_CACHED = (size_t)256 << 20;
-static int at_workgroups(int dh) { return dh <= 64 ? 1024 : dh <= 128 ? 512 : 256; }
-struct AtPlan {
-  int target, items, tiles;
-  size_t list, bytes;  // where the list of items begins in the workspace, 0: there is none
-};
-static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) {
-  AtPlan r{};
-  r.tiles = ceil_div(Hq / p.n_kv_heads, AT_ROWS);
-  const long long cap = (long long)max_blocks * p.page_size;
-  r.items = B;
-  if (cap > AT_WHOLE) {
-    r.target = std::max(1, at_workgroups(p.head_dim) / (p.n_kv_heads * r.tiles));
-    r.items = (int)std::min<long long>((2 * B > r.target ? (long long)AT_FINE : 1) * r.target + B, B * ((cap + AT_PIECE - 1) / AT_PIECE));
-    r.bytes = (size_t)r.items * Hq * (p.head_dim + 4) * 4;
-    if (B > 64) {
-      r.list = r.bytes;
-      r.bytes += r.items * sizeof(AtItem) + (size_t)B * 4;
-    }
-  }
-  return r;
-}
+static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) { return at_plan(p.head_dim, p.n_kv_heads, p.page_size, Hq, max_blocks, B); }
 
 template <typename T, int DH, bool PAGED16, bool FULL>
 static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
