@@ -157,7 +157,9 @@ class Engine:
                  seed_pool: bool = True, poll: int = 8, sampling: dict | None = None):
         """Greedy generation; {W=0, N=1, G=0} is sequential decoding.  Returns (tokens, stats).
         sampling = {temperature, top_k, top_p, min_p, u or seed}: every token is sampled, the one behind position t with u[t] (max_len + Bp numbers; made from the
-        seed if left out).  A candidate is accepted where it is the token that its row draws, so lookahead and sequential decoding emit the same tokens."""
+        seed if left out).  A candidate is accepted where it is the token that its row draws, so lookahead and sequential decoding emit the same tokens, but for rounding: with 16-bit
+        weights a row's last bits go by the block that it stands in, and a number that falls on a border between two tokens may draw either (about one token in a thousand of the small
+        test models; greedy decoding parts at near-ties alike)."""
         rows = 1 + (W + G) * (N - 1)
         Bp = rows if Bp is None else Bp
         self.start(prompt, W, N, G, Bp, seed_pool, sampling=sampling)

@@ -236,3 +236,47 @@ def test_batches_of_next_to_nothing(lens, n_new):
             eng.generate_batch([np.zeros(100, dtype=np.int64)], 2)
     finally:
         eng.close()
+
+
+@pytest.mark.parametrize("W,N,G", [(4, 3, 4), (5, 4, 5)])
+@pytest.mark.parametrize("how", [dict(temperature=0.0), dict(temperature=0.05, top_p=0.95), dict(temperature=0.1, top_k=8), dict(temperature=1.5, top_k=2)])
+def test_sampled_lookahead_confirms_candidates(W, N, G, how):
+    """Behind a prompt that repeats itself candidates are what their rows draw: there are fewer steps than tokens, and the same tokens."""
+    eng = gpu_engine(synth.SHAPES["tiny_f32"], 400, seed=3)
+    prompt = np.tile(np.random.default_rng(7).integers(0, eng.shape.vocab, size=12), 4).astype(np.int32)
+    try:
+        one, alone = eng.generate(prompt, 60, 0, 1, 0, sampling=dict(how, seed=11))
+        many, st = eng.generate(prompt, 60, W, N, G, sampling=dict(how, seed=11))
+        assert np.array_equal(one, many)
+        assert alone["steps"] == 60 and alone["matched_steps"] == 0 and 0 < st["matched_steps"] <= st["steps"] < 50
+    finally:
+        eng.close()
+
+
+@pytest.mark.parametrize("name,margin", [("small_bf16", 3e-2), ("small64_f16", 1e-2)])
+@pytest.mark.parametrize("temperature", [0.3, 0.7])
+def test_sampled_tokens_of_16_bit_models_are_where_their_numbers_fall(name, margin, temperature):
+    """Every token, of sequential and of lookahead decoding: in the oracle's distribution behind the tokens in front of it, the random number of its position falls into the token's
+    share or next to it.  Logits within `margin` of the oracle's move a sum of shares by exp(2 margin / temperature) - 1 at most.  (A row's last bits go by the block that it
+    stands in, so the two may part where a number falls on a border.)"""
+    shape = synth.SHAPES[name]
+    eng, om = gpu_engine(shape, 400, seed=3), oracle_model(shape, seed=3)
+    W, N, G, matched = 4, 3, 4, 0
+    delta = np.exp(2 * margin / temperature) - 1
+    try:
+        for seed in (7, 8):
+            g = np.random.default_rng(seed)
+            prompt, u = np.tile(g.integers(0, shape.vocab, size=12), 4).astype(np.int32), g.random(400 + 64).astype(np.float32)
+            for which in ((0, 1, 0), (W, N, G)):
+                tokens, st = eng.generate(prompt, 60, *which, sampling=dict(temperature=temperature, u=u))
+                seq = np.concatenate([prompt, tokens]).astype(np.int64)
+                x = otf.causal_forward(om, seq[:-1])[1][len(prompt) - 1:].astype(np.float64) / temperature
+                w = np.exp(x - x.max(1, keepdims=True))
+                ends = np.cumsum(w, 1) / w.sum(1, keepdims=True)
+                i, at = np.arange(60), u[len(prompt) - 1:len(prompt) + 59]
+                hi, lo = ends[i, tokens], ends[i, tokens] - (w / w.sum(1, keepdims=True))[i, tokens]
+                assert ((at >= lo - delta) & (at <= hi + delta)).all()
+                matched += st["matched_steps"]
+        assert temperature > 0.5 or matched > 0
+    finally:
+        eng.close()
