@@ -252,3 +252,18 @@ def test_logits_large_and_tiny_rows():
         assert ((out.cpu().double() - want).abs() <= size * 2.0 ** -18).all()
     finally:
         B.la_free_model(model)
+
+
+@pytest.mark.parametrize("d,V,dtype", [(512, 2048, "bf16"), (384, 5008, "f16"), (256, 1024, "f32"), (520, 5003, "bf16")])
+def test_logits_of_a_row_do_not_go_by_the_rows_beside_it(d, V, dtype):
+    """Bit for bit, whatever tiles the other rows fill: what a sampled row draws rests on it."""
+    B, model, _, _, g = head(d, V, dtype)
+    try:
+        h = (torch.randn((64, d), generator=g) * 2.0).cuda()
+        all_, part = torch.empty((64, V), device="cuda"), torch.empty((64, V), device="cuda")
+        B.la_unembed_logits(model, h, all_)
+        for n in (1, 2, 15, 16, 17, 31, 33, 48, 49, 63):
+            B.la_unembed_logits(model, h[64 - n:], part[:n])
+            assert torch.equal(part[:n], all_[64 - n:]), f"{n} rows"
+    finally:
+        B.la_free_model(model)

@@ -141,3 +141,11 @@ def test_write_takes_no_more_threads_than_a_launch_has():
 def test_attend_takes_no_more_workgroups_than_a_launch_has(rows, heads, blocks):
     call = {**ATTEND, "pages": pages(n_kv_heads=heads), "Hq": heads, "B": rows, "blocks": blocks, "ldt": blocks, "ws_bytes": 1 << 62}
     refused(lib.la_paged_attend(*call.values()), EINVAL, "more than one launch")
+
+
+@pytest.mark.parametrize("b,v", [(1, 1), (1, 2048), (1, 2049), (1, 32768), (1, 32769), (2, 40000), (64, 131072), (3, 1 << 19), (65535, 1000)])
+def test_sample_workspace_holds_what_a_call_writes(b, v):
+    """Per row and chunk: its first token (8 bytes), 520 sums (8) and counts (4), the bins in use (4), a place per token (2); and not much more."""
+    chunk = 2048 if v <= 32768 else 8192
+    need = b * -(-v // chunk) * (8 + 520 * 12 + 4 + 2 * chunk)
+    assert need <= lib.la_sample_workspace(b, v) <= need + 64
