@@ -187,7 +187,10 @@ class Engine:
         lens = [len(p) - 1 for p in prompts]
         pages_of = lambda n: (n + page_size - 1) // page_size
         blocks = max(1, max(pages_of(n + n_new) for n in lens))
-        n_pages = max(1, sum(pages_of(n + n_new) for n in lens)) if n_pages is None else n_pages
+        need = max(1, sum(pages_of(n + n_new) for n in lens))
+        n_pages = need if n_pages is None else n_pages
+        if n_pages < need:  # (requests only grow here: what the last step needs is known)
+            raise B.LaError(-3, f"the batch needs {need} pages of {page_size} positions, there are {n_pages}")
         i32 = lambda n, v=0: torch.full(n if isinstance(n, tuple) else (n,), v, dtype=torch.int32, device=dev)
         dt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[sh.dtype]
         pages = B.la_pages(*(torch.empty((sh.n_layers, n_pages, sh.n_kv_heads, page_size, sh.head_dim), dtype=dt, device=dev) for _ in range(2)))

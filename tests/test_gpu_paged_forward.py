@@ -280,3 +280,23 @@ def test_sampled_tokens_of_16_bit_models_are_where_their_numbers_fall(name, marg
         assert temperature > 0.5 or matched > 0
     finally:
         eng.close()
+
+
+@pytest.mark.parametrize("n_pages,fits", [(8, False), (9, True)])
+def test_a_batch_that_its_pages_do_not_hold_is_refused_before_its_prompts_run(n_pages, fits, monkeypatch):
+    """1 + 60 and 20 + 60 positions of 16 a page: four and five pages at the last step, three with the prompts in."""
+    shape = synth.SHAPES["tiny_f32"]
+    eng, ran = gpu_engine(shape, 64), []
+    prefill = eng.prefill
+    monkeypatch.setattr(eng, "prefill", lambda *a, **k: (ran.append(1), prefill(*a, **k))[1])
+    prompts = [np.arange(2), np.arange(21)]  # (the last token of a prompt is the first step's)
+    try:
+        if fits:
+            tokens, st = eng.generate_batch(prompts, 60, n_pages=n_pages)
+            assert tokens.shape == (2, 60) and st["free_pages"] == st["pages"] == n_pages and len(ran) == 2
+        else:
+            with pytest.raises(binding().LaError) as e:
+                eng.generate_batch(prompts, 60, n_pages=n_pages)
+            assert e.value.code == -3 and not ran
+    finally:
+        eng.close()
