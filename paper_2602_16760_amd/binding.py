@@ -296,7 +296,7 @@ def la_unembed_logits(model, hidden, logits, stream=None):
     """logits: float32 [Bp, vocab], rows may be strided."""
     device = _here(hidden, "hidden")
     n, V = hidden.shape[0], model.vocab
-    if logits.get_device() != device or logits.dtype is not _F32 or logits.shape != (n, V) or logits.stride(1) != 1:
+    if logits.get_device() != device or logits.dtype is not _F32 or logits.shape != (n, V) or (logits.stride(1) != 1 and V > 1):
         _refuse(f"logits: need float32 [{n}, {V}] with contiguous rows on device {device}, got {logits.dtype}, {tuple(logits.shape)}, strides {logits.stride()} on {logits.device}")
     _check(lib.la_unembed_logits(model, _array(hidden, "hidden", _F32, (n, model.d_model), device), n, logits.data_ptr(), logits.stride(0) if n > 1 else V, _stream(stream)))
 
@@ -310,7 +310,7 @@ def la_sample(logits, u, ids, prob=None, temperature=None, top_k=None, top_p=Non
     """ids[b] = a token of row b of logits [B, V] (float32, bfloat16 or float16, rows may be strided), drawn by u[b] (with u_index: by
     u[u_index[b]]).  temperature, top_p, min_p: float32 [B] or None; top_k, u_index: int32 [B] or None; prob: float32 [B] or None."""
     device = _here(logits, "logits")
-    if logits.dim() != 2 or logits.dtype not in _DTYPES or logits.stride(1) != 1:
+    if logits.dim() != 2 or logits.dtype not in _DTYPES or (logits.stride(1) != 1 and logits.shape[1] > 1):
         _refuse("logits: need [B, V] of float32, bfloat16 or float16 with contiguous rows")
     B, V = logits.shape
     n = (B,)
@@ -344,11 +344,11 @@ class la_pages:
         return self.device
 
     def _rows(self, t, name, n, heads):
-        """Address and row stride of [n, heads, head_dim] rows of the pages' type."""
+        """Address and row stride of [n, heads, head_dim] rows of the pages' type (the stride of a dimension of one says nothing)."""
         s = t.stride()
-        if t.dtype is not self.dtype or t.get_device() != self.device or t.shape != (n, heads, self.head_dim) or s[2] != 1 or s[1] != self.head_dim:
+        if t.dtype is not self.dtype or t.get_device() != self.device or t.shape != (n, heads, self.head_dim) or s[2] != 1 or (s[1] != self.head_dim and heads > 1):
             _refuse(f"{name}: need {self.dtype} [{n}, {heads}, {self.head_dim}] with contiguous rows on device {self.device}, got {t.dtype}, {tuple(t.shape)}, strides {s} on {t.device}")
-        return t.data_ptr(), s[0]
+        return t.data_ptr(), s[0] if n > 1 else heads * self.head_dim
 
     def _attend_bytes(self, heads, blocks, rows):
         """Workspace of an attention call, by its sizes."""
@@ -360,7 +360,7 @@ class la_pages:
 
 
 def _table(table, device):
-    if table.dtype is not _I32 or table.get_device() != device or table.dim() != 2 or table.stride(1) != 1:
+    if table.dtype is not _I32 or table.get_device() != device or table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1):
         _refuse(f"table: need int32 [n_requests, max_blocks] with contiguous rows on device {device}")
     R, blocks = table.shape
     return table.data_ptr(), table.stride(0) if R > 1 else blocks, R, blocks

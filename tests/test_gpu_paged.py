@@ -485,3 +485,24 @@ def test_attend_an_infinite_value_of_any_weight(dtype, gap):
     assert out[0, :, at].tolist() == [[float("inf") if i % 2 else float("-inf") for i in range(6)]] * 3
     rest = [d for d in range(dh) if d not in at]
     assert torch.isfinite(out[0][:, rest]).all()
+
+
+def test_strides_of_dimensions_of_one_are_not_asked():
+    """One row, one head, a table of one block, whatever strides the views have there: as their copies."""
+    B, g = binding(), torch.Generator().manual_seed(3)
+    rand = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16).cuda()
+    pages, copy = (B.la_pages(torch.zeros((1, 4, 1, 16, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 4, 1, 16, 64), dtype=torch.bfloat16, device="cuda")) for _ in range(2))
+    k, v = rand(1, 5, 64).transpose(0, 1), rand(1, 5, 64).transpose(0, 1)  # [5, 1, 64], one head of stride 320
+    slot = i32([16, 17, 18, 40, 63])
+    B.la_paged_write(pages, 0, k, v, slot)
+    B.la_paged_write(copy, 0, k.reshape(5, 64).clone().view(5, 1, 64), v.reshape(5, 64).clone().view(5, 1, 64), slot)
+    assert torch.equal(pages.k, copy.k) and torch.equal(pages.v, copy.v) and pages.k.count_nonzero() > 0
+    q = rand(2 * 64 + 3)[:128].as_strided((1, 2, 64), (131, 64, 1))  # one row of a buffer whose rows are not 16-byte aligned
+    out, want = (torch.empty((1, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = i32([[1, 0, 2]]).as_strided((1, 1), (3, 3))
+    B.la_paged_attend(pages, 0, q, table, None, i32([2]), out)
+    B.la_paged_attend(pages, 0, q.reshape(128).clone().view(1, 2, 64), i32([[1]]), None, i32([2]), want)
+    assert torch.equal(out, want) and out.count_nonzero() > 0
+    ids = i32([7, 7])
+    B.la_sample(torch.zeros((2, 1), device="cuda").as_strided((2, 1), (1, 5)), torch.zeros(2, device="cuda"), ids)
+    assert ids.tolist() == [0, 0]
