@@ -271,7 +271,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   const double *sums = a.sums + (size_t)b * C * SMP_HIST;
   const int32_t *counts = a.counts + (size_t)b * C * SMP_HIST;
   // ---- the row's sums down to each bin
-  if (t < SMP_BINS) {
+  if (64 * wave < SMP_BINS) {  // (whole waves: a lane that takes no part does not have to keep what lane_value reads of it)
     double w = 0;
     int n = 0;
     constexpr int N = 16;
@@ -292,8 +292,10 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
         n += l[k] >= 0 ? sn[k] : 0;
       }
     }
-    m.through_w[t] = w;
-    m.through_n[t] = n;
+    if (t < SMP_BINS) {
+      m.through_w[t] = w;
+      m.through_n[t] = n;
+    }
   }
   __syncthreads();
   auto in_bins = [&](double y, int t0, int t1) { return y >= first - t1 && (t0 == 0 || y < first - t0 + 1); };
@@ -645,9 +647,10 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
       }
     }
     const unsigned long long hits = __ballot(hit != 0x7fffffff), keeps = __ballot(last >= 0);  // (lanes are in the order of their tokens)
+    const int first_hit = lane_value(hit, hits ? (int)__builtin_ctzll(hits) : 0), last_keep = lane_value(last, keeps ? 63 - (int)__builtin_clzll(keeps) : 0);
     if (lane == 0) {
-      if (hits) atomicMin(&m.where, lane_value(hit, (int)__builtin_ctzll(hits)));
-      if (keeps) atomicMax(&m.last, lane_value(last, 63 - (int)__builtin_clzll(keeps)));
+      if (hits) atomicMin(&m.where, first_hit);
+      if (keeps) atomicMax(&m.last, last_keep);
     }
     __syncthreads();
     const int id = uniform(m.where != 0x7fffffff ? m.where : m.last);
