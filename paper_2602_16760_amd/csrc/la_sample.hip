@@ -83,6 +83,13 @@ __device__ __forceinline__ double sample_eighths(int t) {  // 2^(-t / 8) units
   return ldexp(v * (1 / SMP_UNIT), -(t >> 3));
 }
 
+// y, rounded: what floor(y) and y - floor(y) are taken of.  (Left to the compiler, it may form the difference from the product as it is before its rounding; beyond 2^53 that is any
+// number, not one of [0, 1), and the weights of equal logits are no longer the same bits wherever they are formed.)
+__device__ __forceinline__ double sample_y(float x, double rate) {
+#pragma clang fp contract(off)
+  return (double)x * rate;
+}
+
 // How row b is sampled; the filters that are off are out of reach.
 struct SampleRow {
   bool greedy;
@@ -154,11 +161,11 @@ __global__ __launch_bounds__(SMP_SUM_THREADS) void sample_sum_kernel(Sample a) {
   if (t == 0) a.best[at] = best;
   const float top = sample_value(best);
   if (r.greedy || !(top > -INFINITY)) return;
-  const double first = floor((double)top * r.rate);
+  const double first = floor(sample_y(top, r.rate));
   int at_bin[PER];  // bin and, from bit 10 on, the number of its tokens that were counted before
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    const double y = (double)v[j] * r.rate, low = floor(y), d = first - low;
+    const double y = sample_y(v[j], r.rate), low = floor(y), d = first - low;
     at_bin[j] = -1;
     if (v[j] > -INFINITY && d < SMP_BINS) {
       const int bin = (int)d;
@@ -264,8 +271,8 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     }
     return;
   }
-  const double y_top = uniform((double)top * r.rate), first = uniform(floor(y_top)), w_top = (double)sample_factor(y_top - first) * (1 / SMP_UNIT);
-  const double c_down = first - floor((double)c_top * r.rate);
+  const double y_top = uniform(sample_y(top, r.rate)), first = uniform(floor(y_top)), w_top = (double)sample_factor(y_top - first) * (1 / SMP_UNIT);
+  const double c_down = first - floor(sample_y(c_top, r.rate));
   const int c_shift = c_down < SMP_BINS ? (int)c_down : SMP_BINS;
   const double c_scale = c_down < SMP_BINS ? sample_eighths((int)c_down) * SMP_UNIT : 0.0;
   const double *sums = a.sums + (size_t)b * C * SMP_HIST;
@@ -339,7 +346,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
   // Every token of bin `bin` and of places lo .. hi: f(its place, its factor).
   auto each = [&](int bin, unsigned long long lo, unsigned long long hi, auto f) {
     auto take = [&](unsigned long long c, float v) {
-      const double y = (double)v * r.rate;
+      const double y = sample_y(v, r.rate);
       if (c >= lo && c <= hi && in_bins(y, bin, bin)) f(c, sample_factor(y - floor(y)));
     };
     if (bin >= listed0 && bin <= listed1) {
@@ -522,7 +529,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
     for (int i = t; i < n_list; i += SMP_THREADS) {
       const unsigned long long c = m.list[i];
       const float v = sample_value(c);
-      const double y = (double)v * r.rate, low = floor(y);
+      const double y = sample_y(v, r.rate), low = floor(y);
       const double w = kept(sample_factor_of(y - low), (int)(first - low), v, sample_index(c));
       if (w > 0.0) {
         const unsigned at = atomicAdd(&m.n_few, 1u);
@@ -620,7 +627,7 @@ __global__ __launch_bounds__(SMP_THREADS) void sample_kernel(Sample a) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float v = i0 + j < V ? sample_logit<T>(raw[j]) : -INFINITY;
-      const double y = (double)v * r.rate;
+      const double y = sample_y(v, r.rate);
       w[j] = 0.0;
       if (v > -INFINITY && y >= y_least) {
         const double low = floor(y);

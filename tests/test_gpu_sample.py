@@ -267,3 +267,16 @@ def test_logits_of_a_row_do_not_go_by_the_rows_beside_it(d, V, dtype):
             assert torch.equal(part[:n], all_[64 - n:]), f"{n} rows"
     finally:
         B.la_free_model(model)
+
+
+@pytest.mark.parametrize("V", [64, 100, 5000, 20000])
+@pytest.mark.parametrize("value", [-3.25, 1e30, -1e30, 1e-10, 7.3, -0.1])
+def test_equal_logits_of_any_size_share_equally(V, value):
+    """Where logit / temperature is so large that it has no fraction left, and where it has: a number on the border of two equal tokens' shares draws the one behind it, with and
+    without filters that leave all of them.  (Sums of up to 2^14 equal weights of 37 bits are exact.)"""
+    for temperature in (1.0, 1e-38, 1e-37, 1e-20, 1e-3):
+        x, u = torch.full((9, V), value), [0.25, 0.5, 0.75] * 3
+        k, low = [0, 0, 0, V, V, V, 0, 0, 0], [0.0] * 3 + [0.07] * 3 + [0.14] * 3
+        ids, prob = sample(x, u, [temperature] * 9, k, [1.0] * 9, low)
+        assert ids == [V // 4, V // 2, 3 * V // 4] * 3, (temperature, ids)
+        assert all(abs(q * V - 1) <= 2.0 ** -24 for q in prob)
