@@ -290,7 +290,7 @@ typedef struct {
  * Errors that only the device sees go to heads_out[3], and then nothing is taken, given back or mapped (all rows -1, first all 0): 1 too few free pages,
  * 2 more than max_rows new tokens, 3 a length outside [0, max_blocks * page_size], 4 heads that are
  * no place in the ring, or more pages given back than are out of it.
- * LA_EINVAL: a NULL pointer, a size that is not positive, heads_in == heads_out, table rows that overlap, n_pages * page_size >= 2^31. */
+ * LA_EINVAL: a NULL pointer, a size that is not positive, more than 2^30 requests, heads_in == heads_out, table rows that overlap, n_pages * page_size >= 2^31. */
 int la_page_map(const int32_t *old_len, const int32_t *new_len, int R, int page_size, int32_t *table, int64_t table_stride, int max_blocks,
                 int32_t *ring, int n_pages, const int32_t *heads_in, int32_t *heads_out, int32_t *slot, int32_t *pos, int32_t *req, int max_rows,
                 int32_t *first, void *stream);

@@ -189,6 +189,7 @@ extern "C" int la_page_map(const int32_t *old_len, const int32_t *new_len, int R
   LA_REQUIRE(old_len && new_len && table && ring && heads_in && heads_out && slot && pos && req && first, LA_EINVAL, "NULL argument");
   LA_REQUIRE(heads_in != heads_out, LA_EINVAL, "heads_out must not be heads_in: every workgroup reads the one while one writes the other");
   LA_REQUIRE(R >= 1 && page_size >= 1 && max_blocks >= 1 && n_pages >= 1 && max_rows >= 1, LA_EINVAL, "dimensions must be positive");
+  LA_REQUIRE(R <= 1 << 30, LA_EINVAL, "R=%d requests, at most 2^30", R);  // (a thread's next request is a 32-bit number too)
   LA_REQUIRE(table_stride >= max_blocks || R == 1, LA_EINVAL, "table rows overlap");
   LA_REQUIRE((long long)n_pages * page_size < (1ll << 31), LA_EINVAL, "%d pages of %d positions: slots are 32-bit numbers", n_pages, page_size);
   hipStream_t s = (hipStream_t)stream;
@@ -196,7 +197,7 @@ extern "C" int la_page_map(const int32_t *old_len, const int32_t *new_len, int R
   // above: 1 9.2, 2 7.5, 4 8.1, 8 10.0.
   int per_group = 16;
   while (per_group < MAP_THREADS && R / per_group > 64) per_group *= 2;
-  const int groups = ceil_div(R, per_group), parts = std::min(64, std::max(1, max_rows / (groups * MAP_THREADS * 2)));
+  const int groups = ceil_div(R, per_group), parts = (int)std::min(64ll, std::max(1ll, max_rows / (groups * MAP_THREADS * 2ll)));
   const PageMap a{old_len, new_len, R, per_group, page_size, table, table_stride, max_blocks, ring, n_pages, heads_in, heads_out, slot, pos, req, max_rows, first};
   ProfScope ps("page_map", s);
   page_map_kernel<<<dim3(groups, parts), MAP_THREADS, 0, s>>>(a);

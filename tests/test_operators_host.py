@@ -149,3 +149,9 @@ def test_sample_workspace_holds_what_a_call_writes(b, v):
     chunk = 2048 if v <= 32768 else 8192
     need = b * -(-v // chunk) * (8 + 520 * 12 + 4 + 2 * chunk)
     assert need <= lib.la_sample_workspace(b, v) <= need + 64
+
+
+@pytest.mark.parametrize("requests", [(1 << 30) + 1, (1 << 31) - 256, (1 << 31) - 1])
+def test_page_map_takes_no_more_requests_than_its_threads_count(requests):
+    """A thread goes from request to request in steps of a workgroup, in 32 bits: beyond 2^31 - 256 it would pass their end."""
+    refused(lib.la_page_map(*{**MAP, "R": requests}.values()), EINVAL, "requests")
