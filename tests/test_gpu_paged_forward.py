@@ -300,3 +300,36 @@ def test_a_batch_that_its_pages_do_not_hold_is_refused_before_its_prompts_run(n_
             assert e.value.code == -3 and not ran
     finally:
         eng.close()
+
+
+@pytest.mark.parametrize("name,page,env", [("tiny_f32", 8, {}), ("small_bf16", 16, {}), ("small64_f16", 12, {}), ("small_bf16", 16, {"LA_FORCE_GENERIC": "1"})])
+def test_rows_of_one_request_see_each_other_up_to_their_own_positions(name, page, env, monkeypatch):
+    """Two prompts in one call, rows in any order, and a second call behind them: a causal block of the oracle each."""
+    for key, value in env.items():
+        monkeypatch.setenv(key, value)
+    shape = synth.SHAPES[name]
+    eng, om, B = gpu_engine(shape, 64, head=False), oracle_model(shape, head=False), binding()
+    try:
+        dt = bits(np.zeros(1, np.float32), shape.dtype).dtype
+        pages = B.la_pages(*(torch.full((shape.n_layers, 10, shape.n_kv_heads, page, shape.head_dim), float("nan"), dtype=dt, device="cuda") for _ in range(2)))
+        table = i32([[7, 2, 9, 0, 4], [1, 8, 5, 3, 6]])
+        okv, g = [otf.KVCache(shape, 40) for _ in range(2)], np.random.default_rng(4)
+        done = [0, 0]
+        for call, counts in enumerate([(24, 13), (6, 1), (1, 20)]):
+            rows = [(r, done[r] + i) for r in range(2) for i in range(counts[r])]
+            order = g.permutation(len(rows))
+            x = synth.hidden_block(shape, len(rows), call)
+            req, pos = [rows[i][0] for i in order], [rows[i][1] for i in order]
+            slot = [int(table[r, p // page]) * page + p % page for r, p in zip(req, pos)]
+            hidden = torch.from_numpy(x[order].astype(np.float32)).cuda()
+            B.la_forward_paged(eng.model, 0, shape.n_layers, hidden, i32(pos), i32(req), i32(slot), pages, table)
+            got = np.empty_like(x)
+            got[order] = hidden.cpu().numpy()
+            for r in range(2):
+                mine = [i for i, row in enumerate(rows) if row[0] == r]
+                okv[r].L = done[r]
+                want = otf.forward_block(om, okv[r], x[mine], [rows[i][1] for i in mine], [(1 << (j + 1)) - 1 for j in range(len(mine))])
+                assert row_rel_err(got[mine], want).max() <= BAR[shape.dtype], f"call {call}, request {r}"
+                done[r] += counts[r]
+    finally:
+        eng.close()
