@@ -321,7 +321,8 @@ int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_
  * req[b] (NULL: request b), output projection + residual, RMSNorm, SwiGLU MLP + residual.  hidden: device float [B, d], 16-byte aligned; pos, req, slot, table: as
  * la_page_map leaves them (rows of pos -1 see nothing, and what becomes of their hidden states is of no use).  pages: n_layers >= layer_end, heads and dtype of
  * the model; head_dim a multiple of 8.  Rows of one request in one call see each other's keys up to their own positions.
- * Sums are cut by the number of rows and their positions: the last bits of a row may differ with the rows beside it.
+ * Sums are cut by the number of rows and their positions: the last bits of a row may differ with the rows beside it.  The plain kernels round q to the pages' type here, for
+ * la_paged_attend, where la_forward_layers keeps it in float: 16-bit models on them differ from it by that rounding too.
  * The model's first call allocates scratch memory that stays with it (of a few MB, on the matrix-core path that of a short prompt beside it), also where it is captured.
  * LA_EINVAL: B not in 1..LA_MAX_ROWS, pages of another shape or type, the LDS-ring kernel's weight layout; LA_ERANGE: layer range; LA_ENOMEM. */
 int la_forward_paged(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const int32_t *req, const int32_t *slot,

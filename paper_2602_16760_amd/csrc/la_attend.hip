@@ -1,7 +1,8 @@
 // Attention of single tokens over a paged cache (la_paged_attend): the keys of a row are split into items, an item is a workgroup, and a second launch joins
 // the items of rows that have several.  K and V are read once for the up to 16 query heads of a kv head that share a tile, and their bytes bound it where they are many: two rows
-// of 131000 positions, 1.07 GB, 167 us, 6.4 TB/s (a large copy here: 5.2); 512 rows of 1000, 2.1 GB, 344 us, 6.1.  A row of 500, 2 MB, takes 9 us, of which the bytes are 0.4: a launch, the
-// positions, the table, K and V, the waves' meeting, each waiting for the one before.
+// of 131000 positions, 1.07 GB, 165 us, 6.5 TB/s (a large copy here: 5.2); 512 rows of 1000, 2.1 GB, 328 us, 6.4.  A row of 500, 2 MB, takes 9 us, of which the bytes are 0.4: a launch, the
+// positions, the table, K and V, the waves' meeting, each waiting for the one before.  Pages that 16 does not divide, and float: the table is looked up for every block of keys, a trip to memory
+// that the block's loads wait for (17 rows of up to 1008, float, pages of 24: 3.6 MB, 8 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -465,7 +466,8 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
 }
 
 // The items of a row and head, in item order: a workgroup each, whose waves take every fourth item; a lane takes up to four channels.  What it reads does not wait for what
-// the rows' maxima are: they are applied to it.  5 us for 32 rows of 64 items together (1 MB of records): a launch and two loads' latencies.
+// the rows' maxima are: they are applied to it.  5.6 to 6.2 us for 32 rows of 64 items together (1 MB of records): the rows' positions and the cut, formed anew by every workgroup, then two
+// loads' latencies.
 template <typename T>
 __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAttend a) {
   __shared__ float sums[AT_JOIN_WAVES][256];
@@ -533,8 +535,9 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
 // ---- host side ------------------------------------------------------------------------------------------
 // Where rows that are not cut leave every CU at most one workgroup (AT_WIDE), it has eight waves, 8 kv heads of 128 channels: one row of 300 7.9 -> 7.5 us, 16 rows of 500
 // 10.4 -> 10.1, but 64 rows of 500 24.3 -> 26.4.
-// ONCE where a layer's K and V pages are more than AT_CACHED bytes, in kernels whose loads are all of whole rows: two rows of 131072 (1.07 GB) 167 us, 189 without; a batch
-// of 32 whose 99 MB stay cached between calls 32.7 us, 29.0 without.
+// ONCE where a layer's K and V pages are more than AT_CACHED bytes, in kernels whose loads are all of whole rows: two rows of 131072 (1.07 GB) 167 us, 189 without.  The pages' bytes, not
+// those that the rows read, which only the device knows: a batch of 32 that reads 99 MB of a large pool has it too, 41.9 us (39.5 in a pool of its own size) where other work went through the
+// caches in between, 36.6 (29.8) where its keys would stay cached from call to call, which other layers' keys and weights prevent in a program.
 constexpr int AT_WIDE = 256;
 constexpr size_t AT_CACHED = (size_t)256 << 20;
 static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) { return at_plan(p.head_dim, p.n_kv_heads, p.page_size, Hq, max_blocks, B); }

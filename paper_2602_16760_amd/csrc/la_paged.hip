@@ -15,7 +15,7 @@ namespace la {
 // lengths (8 bytes a request, from L2): one launch and no words that workgroups pass to each other.  A row's page comes from the ring where the request took
 // it in this call, not from the table, which another workgroup may be writing.
 // Bytes do not bound it (48 requests in a step 1.3 KB, 512 requests in a turn with 400000 rows 4.9 MB = 0.9 us at a copy's rate): it is one chain of dependent steps, the
-// lengths, the sums over a wave and over the waves, the row's request by bisection, its page.  5.5 us for the step, 7.5 for the turn, an empty launch is 3.8.
+// lengths, the sums over a wave and over the waves, the row's request by bisection, its page.  4.4 us for the step, 7.2 for the turn.
 constexpr int MAP_THREADS = 256;
 struct PageMap {
   const int32_t *old_len, *new_len;
@@ -153,8 +153,8 @@ __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(PageMap a) {
 
 // ---- rows into pages ------------------------------------------------------------------------------------------
 // Pages are [page][kv head][place][channel]: what one head has in a page is contiguous, so that the attention reads whole lines.  Thread per 16 bytes of K and of V.
-// Bound by the copy's bytes: 16000 rows of 8 heads of 128 f16 channels, 131 MB read and written, 20 us (6.5 TB/s; replayed from the same memory, part of which the
-// last-level cache holds; a large copy reaches 5.2); 64 rows 2.5 us.
+// Bound by the copy's bytes: 16000 rows of 8 heads of 128 f16 channels, 131 MB read and written, 26 us with new rows every time (5.0 TB/s; a large copy reaches 5.2), 20 with the same ones, part of
+// which the last-level cache holds; 64 rows 2.6 us.
 __global__ __launch_bounds__(256) void paged_write_kernel(uint4 *kp, uint4 *vp, const uint4 *k, const uint4 *v, int64_t ldk, int64_t ldv, const int32_t *slot, int n, int Hkv,
                                                           int per_head, int page, int n_pages) {
   const int per_row = Hkv * per_head;
@@ -194,7 +194,7 @@ extern "C" int la_page_map(const int32_t *old_len, const int32_t *new_len, int R
   LA_REQUIRE((long long)n_pages * page_size < (1ll << 31), LA_EINVAL, "%d pages of %d positions: slots are 32-bit numbers", n_pages, page_size);
   hipStream_t s = (hipStream_t)stream;
   // 16 requests a workgroup (more where there are very many, each of which reads all lengths), in as many parts as give a thread two rows.  Rows a thread, us of the turn
-  // above: 1 9.2, 2 7.5, 4 8.1, 8 10.0.
+  // above: 1 9.1, 2 7.2, 4 7.3, 8 9.0.
   int per_group = 16;
   while (per_group < MAP_THREADS && R / per_group > 64) per_group *= 2;
   const int groups = ceil_div(R, per_group), parts = (int)std::min(64ll, std::max(1ll, max_rows / (groups * MAP_THREADS * 2ll)));

@@ -45,6 +45,9 @@ struct PfGemm {
 };
 
 // LOGITS: a workgroup's column tiles are neighbours in one stream, LG_COLS of a CU's (their 1 KB fragments lie side by side in memory): column tile j of group cg.
+// Where a CU has no multiple of LG_COLS tiles (on 256 CUs: where 32768 does not divide the columns), its last group repeats the last tile for those that it lacks and drops the
+// result, which costs that much of the time: 4096 columns deep, one row, us for 32768 / 36880 / 49152 / 50304 / 65536 / 102400 columns 43 / 76 / 82 / 82 / 99 / 151 (4.0 TB/s of 36880, 4.9 to
+// 5.5 of the wider ones, 6.3 of 32768).
 constexpr int LG_COLS = 8;
 constexpr float LG_LOW = 2048.f;  // what the lower halves of the operand are multiplied by
 __device__ __forceinline__ int lg_tile(const PfGemm &p, int cg, int j) { return (cg / p.G * LG_COLS + j) * p.G + cg % p.G; }
@@ -437,8 +440,9 @@ __global__ __launch_bounds__(256, 2) void pf_qkv_few_kernel(PfGemm p) {
 // The unembedding's operand for stored logits: x * gain as the sum of two half-precision numbers, the nearest one and LG_LOW times what it leaves, in
 // row tiles 0 .. T - 1 and T .. 2 T - 1 of the fragments; and the sums of squares, as pf_norm_kernel forms them.  Rows behind M are zeros.
 // (One rounding to 11 bits would move a logit by up to 2^-12 of the sum of its products' sizes, and with it a sampled token's share; the pair leaves 2^-23.  The second product costs
-// nothing: the weights' bytes bound the launch.  4096 x 32768, one row 38 us, 7.0 TB/s of 268 MB that the last-level cache holds in part; 5120 x 131072, 48 rows 255 us, 5.3 TB/s.)
-// 3 to 5 us, a pass over at most 1.3 MB.
+// little: the weights' bytes bound the launch.  4096 x 32768, one row 39 us, 6.8 TB/s of 268 MB that the last-level cache holds in part; 5120 x 131072, 48 rows 267 us, 5.0 TB/s; 4096 x 131072, both
+// launches, 1 / 32 / 64 rows 198 / 212 / 233 us, la_unembed_argmax, which multiplies once, 172 / 178 / 183.)
+// 5 us, a pass over at most 1.3 MB.
 __global__ __launch_bounds__(256) void logits_operand_kernel(const float *x, const float *gain, int M, int d, int T, float *ss, uint16_t *A) {
   const int rt = blockIdx.x, chunk = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
   const int KT = d >> 5, per = (KT + PF_CHUNKS - 1) / PF_CHUNKS, k1 = (chunk + 1) * per < KT ? (chunk + 1) * per : KT;

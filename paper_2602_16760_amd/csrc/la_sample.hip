@@ -10,8 +10,10 @@ namespace la {
 // bin are then sums of whole numbers: they do not depend on the order in which LDS atomics take them, and equal logits have equal shares.  Everything behind them
 // is added in a fixed order.  A sum of n weights is off by about 2^-38 / sqrt(n) of itself.  Bins reach 64 octaves down, below which a weight counts as none.
 // Logits are read once, and then, of a row that is cut, the tokens of the cut's bin, of one that is not, a chunk.  The bytes bound neither launch: 64 rows of 131072, 34 MB, 6.5 us at a
-// copy's rate, take 19 + 30 us (factors and atomics of 8.4 million tokens, some 30 instructions each in 64 bits, behind 7 us of loads; then a row's chain of searches, each a few
-// barriers long); one row of 32768 5 + 11 us, all of it that chain.
+// copy's rate, take 20 + 30 us.  The first is bound by its instructions: 59 a token, which is 94 % of what the CUs issue in the cycles that they are busy (their LDS is active in 40 %, half of
+// that for lanes that meet in a bank).  The second is a chain in one workgroup a row: the chunks' first tokens, their sums, and for every filter that cuts a search by bins, the listed tokens' places
+// and then their logits (two trips to memory) and a search among them, each with a few barriers; then the draw.  Both launches in a replayed graph, us, all 64 rows alike / one row: greedy 11 / 7,
+// no filter 34 / 20, min-p 34 / 16, top-k of 50 31 / 18, of 1000 41 / 25, top-p of 0.9 39 / 26, top-k of 5000 and top-p of 0.95 43 / 30.  One row of 32768 5 + 11 us.
 constexpr int SMP_BINS = 514, SMP_HIST = 520;  // (64 octaves below the largest token end in the 514th bin at the latest); row length of a chunk's sums
 constexpr int SMP_SUM_THREADS = 512;          // of a workgroup of the first launch
 constexpr int SMP_PER = 16, SMP_PER_SHORT = 4;  // ... tokens of each: chunks of 8192 and of 2048
