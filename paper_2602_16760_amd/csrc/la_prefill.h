@@ -970,7 +970,7 @@ __global__ __launch_bounds__(256) void unstage_kernel(const uint16_t *K, const u
 
 // The prompt pass's launches with the rows' own positions: the QKV product leaves K and V as a block's cache (stage_k, stage_v), from which they go to their slots, and the
 // paged attention takes the causal one's place, from and to the same operand fragments.  The layers' weights and the rows' K and V bound it: eight layers of the 7B shape behind 1000
-// positions each, 1 / 8 / 32 / 64 rows 965 / 1015 / 1186 / 1382 us, where 3.49 GB of weights and 4.1 MB a row and layer take 672 to 1070 at a copy's rate; a layer's ten launches, most of
+// positions each, 1 / 8 / 32 / 64 rows 973 / 1023 / 1206 / 1389 us, where 3.49 GB of weights and 4.1 MB a row and layer take 672 to 1070 at a copy's rate; a layer's ten launches, most of
 // them some microseconds long, are the rest.  (Blocks of one request, one persistent launch: 753 us at one row, 847 at 32.)
 int mfma_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRows &r, const la_pages_desc &pages, void *stage_k, void *stage_v, void *workspace, hipStream_t s) {
   MfmaModel *f = m->mf;
