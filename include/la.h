@@ -306,7 +306,7 @@ int la_paged_write(const la_pages_desc *pages, int layer, const void *k, const v
  * q + b * q_stride elements, rows 16-byte aligned.  table: device int32, request r's pages at table + r * table_stride, max_blocks entries; n_requests rows.
  * A row of pos < 0, or whose request is outside [0, n_requests), sees nothing and gets zeros; pos is clamped to max_blocks * page_size - 1, and
  * positions whose table entry is not a page (outside [0, n_pages)) are not seen.  Whatever lies in places that a row does not see is not
- * looked at.  Scores, softmax and sums are float; 16-bit types multiply as stored, a probability as the sum of two numbers of that type (off by at most 2^-20 of it, bfloat16 2^-14).
+ * looked at.  Scores, softmax and sums are float; 16-bit types multiply as stored, a probability as the sum of two numbers of that type (off by at most 2^-20 of it, or 2^-40 of the largest; bfloat16 2^-14).
  * workspace: device memory of la_paged_attend_workspace bytes (0 where none is needed), 16-byte aligned, which the call may overwrite and which no
  * other call may use meanwhile; nothing is kept in it.
  * LA_EINVAL: a NULL pointer, bad dimensions or alignment, more rows and kv heads than one launch takes (2^24 workgroups: 2^20 rows of 15 heads); LA_ENOMEM: workspace too

@@ -54,7 +54,7 @@ __device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
 
 // The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
 // positions, a lane each; of more it was written down by a launch of its own: formed by every workgroup from all rows' positions, 64 at a time, the time grew with the square of the
-// rows (512 rows of 1000 379 us, now 344; 65 rows 57, now 59).
+// rows (512 rows of 1000 379 us, with the list 344; 65 rows 57 and 59).
 template <bool BY_ROW>
 __device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
   AtItem it{};
@@ -193,7 +193,7 @@ __device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int co
 //   float: 16 keys a block and the float matrix instruction, whose contraction takes one key per lane: nothing to turn around.
 // Scores, running maximum and sum, and both products' sums are float.  A weight goes into the second product as two 16-bit numbers (at_split), which costs a product more for each
 // of V's: rounded to one, its half step comes out as large as the output's own (a row of 500, bfloat16: 1.8e-3 off as a whole, now 1.6e-3, which is what rounding the exact output leaves).
-// Half precision has no small numbers: below 2^-14 its step is 2^-24, below 2^-25 nothing is left, while a thousand such weights beside one of 1 are a thousandth of the sum.  So
+// Half precision has no small numbers: below 2^-14 its step is 2^-24, below 2^-25 nothing is left, while many such weights beside a large one whose V is small are the output.  So
 // its weights are up to 2^15 instead of 1 (UP; the sums carry the factor too, and it cancels): a step below 2^-29 of the largest is 2^-39 of it.  Keys behind a first one of 2^22.5,
 // 2^25 and 2^30 times their weight: 512 of them off by 0.8, 12 and 12 % without it, by half a step of the output with it.
 // PAGED16: page_size is a multiple of 16, so that a 16-key tile lies in one page and its address is a scalar; otherwise a lane looks up its own keys' places.
