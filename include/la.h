@@ -267,6 +267,43 @@ size_t la_sample_workspace(int B, int V);
 int la_sample(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_sampling *how, int32_t *ids, float *prob, void *workspace,
               size_t workspace_bytes, void *stream);
 
+/* How la_logits_adjust changes logits; every pointer is device memory and may be NULL (that part is off).
+ *   req            int32 [B]: the request of each row (NULL: row b is of request b; outside [0, n_requests): of none, only its mask applies)
+ *   repetition, presence, frequency   float [n_requests] (a repetition that is not a positive finite number, or another that is not finite, is off)
+ *   tokens         int32 [n_requests, max_tokens], rows at tokens_stride: the committed tokens, n_tokens[r] of them (int32 [n_requests]), of which the first n_prompt[r] (NULL: 0) are the prompt
+ *   draft          int32 [B]: the step's drafted tokens; first, vis: the block of each request and the rows that each row sees, as la_tree_layout leaves them.  Row b is the step's row b:
+ *                  the tokens of the rows of vis[b], but for row 0, whose token is the last of `tokens`, count as committed
+ *   bias_token, bias   int32, float [n_requests, n_bias], rows at bias_stride (entries outside [0, V) are none; a token that is listed several times has the sum, in the list's order)
+ *   allowed        uint32 [n_allowed, (V + 31) / 32], rows at allowed_stride: bit v & 31 of word v >> 5 says whether token v may come; allowed_index int32 [B] the mask of each row
+ *                  (NULL: row b has mask b; outside [0, n_allowed): any token may come) */
+typedef struct {
+  const int32_t *req;
+  const float *repetition, *presence, *frequency;
+  const int32_t *tokens, *n_tokens, *n_prompt;
+  const int32_t *draft, *first;
+  const uint64_t *vis;
+  const int32_t *bias_token;
+  const float *bias;
+  const uint32_t *allowed;
+  const int32_t *allowed_index;
+  int64_t tokens_stride, bias_stride, allowed_stride;
+  int32_t n_requests, max_tokens, n_bias, n_allowed;
+} la_adjust;
+
+#define LA_MAX_HISTORY (1 << 24)
+#define LA_MAX_BIAS 4096
+
+/* out[b, v] = logits[b, v], in this order:
+ *   divided by repetition where it is above 0, else multiplied by it, if v is among the request's committed tokens, prompt or not
+ *   less frequency times the number of times that v was committed behind the prompt, less presence if it was
+ *   plus v's bias
+ *   -inf where v may not come
+ * in float, rounded to the type once.  logits, out: device, la_dtype `dtype`, rows at row_stride and out_stride elements, any alignment of the type; out may be logits (with the same
+ * stride), and must not overlap it otherwise.  The result does not depend on the rows beside it.  Allocates nothing.
+ * LA_EINVAL: V outside 1..LA_MAX_SAMPLE_VOCAB, B above 65535, more than LA_MAX_HISTORY tokens or LA_MAX_BIAS biases, rows that overlap, a part that lacks one of its arrays, more rows than
+ * requests or masks without a map.  B = 0 does nothing. */
+int la_logits_adjust(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_adjust *how, void *out, int64_t out_stride, void *stream);
+
 /* ---- a cache that several requests share ------------------------------------------------------ */
 
 /* Pages of page_size positions, handed to requests one at a time; k and v are device memory of the caller's, each
@@ -327,6 +364,49 @@ int la_paged_attend(const la_pages_desc *pages, int layer, const void *q, int64_
  * LA_EINVAL: B not in 1..LA_MAX_ROWS, pages of another shape or type, the LDS-ring kernel's weight layout; LA_ERANGE: layer range; LA_ENOMEM. */
 int la_forward_paged(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const int32_t *req, const int32_t *slot,
                      const la_pages_desc *pages, const int32_t *table, int64_t table_stride, int n_requests, int max_blocks, void *stream);
+
+/* Moves rows between slots in layers [layer_begin, layer_end): K and V of slot from[i] to slot to[i], i < n (device int32; a pair with either outside
+ * [0, n_pages * page_size) is skipped).  `run` pairs after another belong together (1 to LA_MAX_ROWS; the last run may be shorter): every source of a run is read before one of its
+ * destinations is written, so they may be each other's, and of two pairs of a run with one destination the later one is left.  A destination of one run must not be
+ * a source or a destination of another (run = 1: of any other pair).  Moves an accepted path up (run = max_path of la_tree_accept) or copies a request's positions for another one that
+ * goes on from them (run = 1, slots of both from la_page_map).
+ * LA_EINVAL: bad pages, a NULL pointer, n or run out of range, more rows and kv heads than one launch takes (2^24 workgroups of 256 pieces of 16 bytes); LA_ERANGE: layers.  n = 0 does nothing. */
+int la_paged_copy(const la_pages_desc *pages, int layer_begin, int layer_end, const int32_t *from, const int32_t *to, int n, int run, void *stream);
+
+/* ---- trees of drafted tokens on the shared cache (Section 4.3's verification, for several requests) ------ */
+
+/* Each request may have a block of up to LA_MAX_ROWS rows behind its len[r] committed positions, as la_page_map leaves them: rows first[r] <= i < first[r + 1] of the packed order,
+ * row j = i - first[r] of the block at place len[r] + j of its cache.  Row 0 is the request's last token, which the cache does not hold yet; every other one is drafted behind the row of
+ * the block that parent[i] names (its number in the block).  What a row chooses (arg-max or sample) is the token behind it.  All arrays are device memory; first: int32 [R + 1], ascending.
+ *
+ * la_tree_layout: pos[i] = len[r] + the number of rows in front on its way to row 0 (for RoPE, and for la_sample's u_index), vis[i] = those rows and itself, bit j for row j, as
+ * la_forward_layers' masks.  parent: int32 [B] (row 0's is not looked at); pos: int32 [B]; vis: uint64 [B].
+ * Rows whose parent is not a row in front of them, or whose way does not end at row 0, rows behind the block's 64th and rows of no request get pos -1 and vis 0: they see nothing.
+ * LA_EINVAL: a NULL pointer, R or B outside 0..LA_MAX_ATTEND_ROWS, rows of no request.  B = 0 does nothing. */
+int la_tree_layout(const int32_t *parent, const int32_t *first, const int32_t *len, int R, int B, int32_t *pos, uint64_t *vis, void *stream);
+
+/* Attention of the rows over the pages of one layer, which hold K and V of the rows themselves already: out[i, h] = sum_t softmax_t(scale * q[i, h] . K[t, h / g]) V[t, h / g] over
+ * t < len[r] and t = len[r] + j for the bits j < min(max_rows, first[r + 1] - first[r]) of vis[i].  q, out, table, scale, workspace: as for la_paged_attend; request r is row r of the table.
+ * max_rows: rows of a request at most (1 to LA_MAX_ROWS; a request's rows behind them see nothing).  K and V are read once for 64 query heads and rows of a kv head, up to 512 where a block has as many.
+ * A row of vis 0, rows of a request with len < 0 and rows of no request see nothing and get zeros; positions behind max_blocks * page_size, or whose table entry is not a page, are
+ * not seen.  Whatever lies in places that a row does not see is not looked at, other rows' K and V of infinities or NaN among them.  Sums and rounding: as in la_paged_attend.
+ * LA_EINVAL, LA_ENOMEM, LA_ERANGE: as there.  B = 0 does nothing. */
+size_t la_paged_tree_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int n_requests, int max_rows);
+int la_paged_tree_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table, int64_t table_stride,
+                         int n_requests, int max_blocks, const int32_t *first, const int32_t *len, const uint64_t *vis, int max_rows, int B, void *out, int64_t out_stride,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* What a step commits.  From row 0 on the path goes to the first row whose parent is the present one and whose tok is what the present one chose (ids >= 0), until there is none or it has
+ * max_path rows, or limit[r] (NULL: no limit).  parent, tok, ids, slot: int32 [B], len, limit: int32 [R].  Of every request:
+ *   n_new      tokens committed: one for each of the path's rows (a last row whose ids is negative commits none; 0 where the request has no row, or limit <= 0)
+ *   new_len    len + the path's rows: positions that its cache then holds (crop it to them with la_page_map; the next block's row 0 is the last committed token)
+ *   last       number of the path's last row, -1: no path
+ *   out        int32 [R, max_path]: the tokens ids of the path's rows, -1 behind them
+ *   from, to   int32 [R, max_path]: for the path's k-th row its slot and the slot of row k, where it belongs; -1 where it lies there already, or where either has none.  For la_paged_copy, run = max_path
+ * Only the first LA_MAX_ROWS rows of a request take part.
+ * LA_EINVAL: a NULL pointer, R or B outside 0..LA_MAX_ATTEND_ROWS, max_path outside 1..LA_MAX_ROWS.  R = 0 does nothing. */
+int la_tree_accept(const int32_t *parent, const int32_t *tok, const int32_t *ids, const int32_t *slot, const int32_t *first, const int32_t *len, const int32_t *limit, int R,
+                   int B, int max_path, int32_t *n_new, int32_t *new_len, int32_t *last, int32_t *out, int32_t *from, int32_t *to, void *stream);
 
 /* ---- n-gram pool and acceptance (Section 4.3) ----------------------------------------- */
 

@@ -56,6 +56,12 @@ class la_sampling(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "u", "u_index")] + [("n_u", C.c_int32)]
 
 
+class la_adjust(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("req", "repetition", "presence", "frequency", "tokens", "n_tokens", "n_prompt", "draft", "first", "vis", "bias_token", "bias", "allowed",
+                                          "allowed_index")] + \
+               [(n, C.c_int64) for n in ("tokens_stride", "bias_stride", "allowed_stride")] + [(n, C.c_int32) for n in ("n_requests", "max_tokens", "n_bias", "n_allowed")]
+
+
 class la_pages_desc(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
                [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
@@ -72,7 +78,8 @@ EXPORTS = [
     "la_init_model", "la_model_set_layer", "la_free_model", "la_kv_alloc", "la_kv_set_len", "la_kv_get_len",
     "la_kv_fill", "la_kv_read", "la_free_kv", "la_embed", "la_forward_layers", "la_unembed_argmax",
     "la_unembed_argmax_noalloc", "la_unembed_logits", "la_sample", "la_sample_workspace", "la_page_map", "la_paged_write", "la_paged_attend",
-    "la_paged_attend_workspace", "la_forward_paged", "la_causal_layout", "la_set_barrier_timeout",
+    "la_paged_attend_workspace", "la_forward_paged", "la_paged_copy", "la_tree_layout", "la_paged_tree_attend", "la_paged_tree_attend_workspace",
+    "la_tree_accept", "la_logits_adjust", "la_causal_layout", "la_set_barrier_timeout",
     "la_prefill", "la_jacobi_init", "la_jacobi_accept", "la_rtt_fixed_overhead", "la_rtt_project", "la_jacobi_project",
     "la_pool_alloc", "la_free_pool", "la_state_init", "la_ngram_accept", "la_lookahead_layout",
     "la_profile_enable", "la_profile_select", "la_profile_read", "la_profile_copy", "la_last_error",
@@ -108,6 +115,12 @@ def _load():
         "la_paged_attend_workspace": (C.c_size_t, [vp, i32, i32, i32]),
         "la_paged_attend": (i32, [vp, i32, vp, i64, i32, f32, vp, i64, i32, i32, vp, vp, i32, vp, i64, vp, C.c_size_t, vp]),
         "la_forward_paged": (i32, [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i64, i32, i32, vp]),
+        "la_paged_copy": (i32, [vp, i32, i32, vp, vp, i32, i32, vp]),
+        "la_tree_layout": (i32, [vp, vp, vp, i32, i32, vp, vp, vp]),
+        "la_paged_tree_attend_workspace": (C.c_size_t, [vp, i32, i32, i32, i32]),
+        "la_paged_tree_attend": (i32, [vp, i32, vp, i64, i32, f32, vp, i64, i32, i32, vp, vp, vp, i32, i32, vp, i64, vp, C.c_size_t, vp]),
+        "la_tree_accept": (i32, [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
+        "la_logits_adjust": (i32, [vp, i32, i64, i32, i32, vp, vp, i64, vp]),
         "la_pool_alloc": (i32, [i32, i32, i32, C.POINTER(vp)]),
         "la_free_pool": (None, [vp]),
         "la_state_init": (i32, [vp, vp, C.POINTER(la_lookahead_desc), vp, i32, i32, i32, vp, vp]),
@@ -257,7 +270,7 @@ def la_unembed_argmax_noalloc(model, hidden, ids, top2=None, stream=None):
 
 # ---- sampling and the shared cache: operators on plain tensors, of any model or none ---------------------
 _DTYPES = {torch.float32: LA_F32, torch.bfloat16: LA_BF16, torch.float16: LA_F16}
-_F32, _I32 = torch.float32, torch.int32
+_F32, _I32, _I64 = torch.float32, torch.int32, torch.int64
 
 
 def _refuse(text):
@@ -325,6 +338,56 @@ def la_sample(logits, u, ids, prob=None, temperature=None, top_k=None, top_p=Non
                          _optional(prob, "prob", _F32, n, device), ws.data_ptr(), size, _stream(stream)))
 
 
+def _lists(t, name, dtype, device, rows=None):
+    """Address, row stride, number and length of lists [rows, n] (their rows may be strided)."""
+    if t.dtype is not dtype or t.get_device() != device or t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (t.stride(1) != 1 and t.shape[1] > 1):
+        _refuse(f"{name}: need {dtype} [{'n' if rows is None else rows}, n] with contiguous rows on device {device}, got {t.dtype}, {tuple(t.shape)}, strides {t.stride()} on {t.device}")
+    R, n = t.shape
+    return t.data_ptr(), t.stride(0) if R > 1 else n, R, n
+
+
+def la_logits_adjust(logits, out, req=None, repetition=None, presence=None, frequency=None, tokens=None, n_tokens=None, n_prompt=None, draft=None, first=None, vis=None, bias=None,
+                     bias_token=None, allowed=None, allowed_index=None, n_requests=None, stream=None):
+    """out [B, V] = logits [B, V] (float32, bfloat16 or float16, rows may be strided; out may be logits) with penalties, biases and masks: see la.h.  repetition, presence, frequency:
+    float32 [R]; tokens int32 [R, max_tokens] with n_tokens, n_prompt int32 [R]; draft int32 [B] with first int32 [R + 1] and vis int64 [B]; bias float32 [R, n_bias] with bias_token int32 of the
+    same shape; allowed int32 [n_masks, ceil(V / 32)] with allowed_index int32 [B]; req int32 [B].  n_requests: R, where none of the arrays says it."""
+    device = _here(logits, "logits")
+    for t, name in ((logits, "logits"), (out, "out")):
+        if t.dim() != 2 or t.dtype not in _DTYPES or (t.stride(1) != 1 and t.shape[1] > 1):
+            _refuse(f"{name}: need [B, V] of float32, bfloat16 or float16 with contiguous rows")
+    if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device:
+        _refuse(f"out: need {logits.dtype} {tuple(logits.shape)} on device {device}, got {out.dtype}, {tuple(out.shape)} on {out.device}")
+    B, V = logits.shape
+    n = (B,)
+    R = n_requests
+    if R is None:
+        of = next((t for t in (repetition, presence, frequency, tokens, bias, n_tokens) if t is not None), None)
+        R = of.shape[0] if of is not None and of.dim() else first.shape[0] - 1 if first is not None and first.dim() else B
+    r = (R,)
+    how = la_adjust(_optional(req, "req", _I32, n, device), _optional(repetition, "repetition", _F32, r, device), _optional(presence, "presence", _F32, r, device),
+                    _optional(frequency, "frequency", _F32, r, device))
+    how.n_requests = R
+    if tokens is not None:
+        how.tokens, how.tokens_stride, _, how.max_tokens = _lists(tokens, "tokens", _I32, device, R)
+        how.n_tokens, how.n_prompt = _optional(n_tokens, "n_tokens", _I32, r, device), _optional(n_prompt, "n_prompt", _I32, r, device)
+    if draft is not None:
+        how.draft, how.first, how.vis = _array(draft, "draft", _I32, n, device), _optional(first, "first", _I32, (R + 1,), device), _optional(vis, "vis", _I64, n, device)
+    if bias is not None or bias_token is not None:
+        if bias is None or bias_token is None or bias.shape != bias_token.shape:
+            _refuse("bias, bias_token: need both, of one shape")
+        how.bias, ld, _, how.n_bias = _lists(bias, "bias", _F32, device, R)
+        how.bias_token, how.bias_stride, _, _ = _lists(bias_token, "bias_token", _I32, device, R)
+        if ld != how.bias_stride:
+            _refuse("bias, bias_token: need rows of one stride")
+    if allowed is not None:
+        how.allowed, how.allowed_stride, how.n_allowed, words = _lists(allowed, "allowed", _I32, device)
+        if words != (V + 31) // 32:
+            _refuse(f"allowed: need {(V + 31) // 32} words a mask, got {words}")
+        how.allowed_index = _optional(allowed_index, "allowed_index", _I32, n, device)
+    _check(lib.la_logits_adjust(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, B, V, C.byref(how), out.data_ptr(), out.stride(0) if B > 1 else V,
+                                _stream(stream)))
+
+
 class la_pages:
     """Pages of K and V, both [n_layers, n_pages, n_kv_heads, page_size, head_dim], and the descriptor that calls on them take."""
 
@@ -349,6 +412,14 @@ class la_pages:
         if t.dtype is not self.dtype or t.get_device() != self.device or t.shape != (n, heads, self.head_dim) or s[2] != 1 or (s[1] != self.head_dim and heads > 1):
             _refuse(f"{name}: need {self.dtype} [{n}, {heads}, {self.head_dim}] with contiguous rows on device {self.device}, got {t.dtype}, {tuple(t.shape)}, strides {s} on {t.device}")
         return t.data_ptr(), s[0] if n > 1 else heads * self.head_dim
+
+    def _tree_bytes(self, heads, blocks, requests, rows):
+        """Workspace of a trees' attention call, by its sizes."""
+        key = (heads, blocks, requests, rows)
+        size = self._bytes.get(key)
+        if size is None:
+            size = self._bytes[key] = lib.la_paged_tree_attend_workspace(self.ref, heads, blocks, requests, rows)
+        return size
 
     def _attend_bytes(self, heads, blocks, rows):
         """Workspace of an attention call, by its sizes."""
@@ -404,6 +475,60 @@ def la_paged_attend(pages, layer, q, table, req, pos, out, scale=None, stream=No
     ws = _workspace(size, q, stream) if size else None
     _check(lib.la_paged_attend(pages.ref, layer, qp, ldq, Hq, dh ** -0.5 if scale is None else scale, tp, ld, R, blocks, _optional(req, "req", _I32, (B,), device),
                                _array(pos, "pos", _I32, (B,), device), B, op, ldo, ws.data_ptr() if size else None, size, _stream(stream)))
+
+
+def la_paged_copy(pages, from_slot, to_slot, run=None, layers=None, stream=None):
+    """K and V of slots from_slot to slots to_slot (int32, of one shape) in layers = (begin, end), None: all.  Two dimensions: each row is a run, whose sources are all read before one of its
+    destinations is written; else runs of `run` (None: 1)."""
+    device, n = pages._here(), from_slot.numel()
+    if run is None:
+        run = from_slot.shape[1] if from_slot.dim() == 2 else 1
+    begin, end = (0, pages.n_layers) if layers is None else layers
+    _check(lib.la_paged_copy(pages.ref, begin, end, _array(from_slot, "from_slot", _I32, from_slot.shape, device), _array(to_slot, "to_slot", _I32, from_slot.shape, device), n,
+                             run if n else 1, _stream(stream)))
+
+
+def la_tree_layout(parent, first, len, pos, vis, stream=None):
+    """Positions and masks of the requests' trees: parent int32 [B], first int32 [R + 1], len int32 [R], pos int32 [B], vis int64 [B]."""
+    device = _here(parent, "parent")
+    n, R = parent.shape, len.numel()
+    if parent.dim() != 1:
+        _refuse("parent: need an int32 array")
+    _check(lib.la_tree_layout(_array(parent, "parent", _I32, n, device), _array(first, "first", _I32, (R + 1,), device), _array(len, "len", _I32, (R,), device), R, n[0],
+                              _array(pos, "pos", _I32, n, device), _array(vis, "vis", _I64, n, device), _stream(stream)))
+
+
+def la_paged_tree_attend(pages, layer, q, table, first, len, vis, max_rows, out, scale=None, stream=None):
+    """out[i] = attention of q[i], row i - first[r] of request r's block, over its len[r] committed positions and the block's rows of vis[i] (int64 [B]); q, out [B, n_q_heads, head_dim], rows
+    may be strided; first int32 [R + 1], len int32 [R]; max_rows: rows of a request at most; scale None: head_dim ** -0.5."""
+    device = pages._here()
+    if q.dim() != 3:
+        _refuse("q: need [B, n_q_heads, head_dim]")
+    B, Hq, dh = q.shape
+    qp, ldq = pages._rows(q, "q", B, Hq)
+    op, ldo = pages._rows(out, "out", B, Hq)
+    if B > 1 and ldo < Hq * dh:
+        _refuse("out: rows overlap")
+    tp, ld, R, blocks = _table(table, device)
+    size = pages._tree_bytes(Hq, blocks, R, max_rows)
+    ws = _workspace(size, q, stream) if size else None
+    _check(lib.la_paged_tree_attend(pages.ref, layer, qp, ldq, Hq, dh ** -0.5 if scale is None else scale, tp, ld, R, blocks, _array(first, "first", _I32, (R + 1,), device),
+                                    _array(len, "len", _I32, (R,), device), _array(vis, "vis", _I64, (B,), device), max_rows, B, op, ldo, ws.data_ptr() if size else None, size,
+                                    _stream(stream)))
+
+
+def la_tree_accept(parent, tok, ids, slot, first, len, n_new, new_len, last, out, from_slot, to_slot, limit=None, stream=None):
+    """The path that each request commits: see la.h.  All int32: parent, tok, ids, slot [B], first [R + 1], len, limit (or None), n_new, new_len, last [R], out, from_slot, to_slot
+    [R, max_path]."""
+    device = _here(parent, "parent")
+    n, R = parent.shape, len.numel()
+    if parent.dim() != 1 or out.dim() != 2:
+        _refuse("parent, out: need int32 [B] and [R, max_path]")
+    r, path = (R,), (R, out.shape[1])
+    _check(lib.la_tree_accept(_array(parent, "parent", _I32, n, device), _array(tok, "tok", _I32, n, device), _array(ids, "ids", _I32, n, device), _array(slot, "slot", _I32, n, device),
+                              _array(first, "first", _I32, (R + 1,), device), _array(len, "len", _I32, r, device), _optional(limit, "limit", _I32, r, device), R, n[0], path[1],
+                              _array(n_new, "n_new", _I32, r, device), _array(new_len, "new_len", _I32, r, device), _array(last, "last", _I32, r, device),
+                              _array(out, "out", _I32, path, device), _array(from_slot, "from_slot", _I32, path, device), _array(to_slot, "to_slot", _I32, path, device), _stream(stream)))
 
 
 def la_forward_paged(model, layer_begin, layer_end, hidden, pos, req, slot, pages, table, stream=None):

@@ -168,6 +168,46 @@ __global__ __launch_bounds__(256) void paged_write_kernel(uint4 *kp, uint4 *vp, 
   vp[to] = v[row * ldv + c];
 }
 
+// ---- slots to other slots, in every layer ---------------------------------------------------------------------
+// A thread takes 16 bytes of a kv head of the rows of one run, of K or V of one layer after the other: it has read all of a run's sources before it writes one of its destinations, and
+// nobody else has to do with those bytes, so a run may move rows onto each other's places.
+struct PagedCopy {
+  uint4 *k, *v;  // of the first layer
+  size_t layer;  // 16-byte pieces of one
+  int layers, Hkv, per_head, page, n_pages;
+  const int32_t *from, *to;
+  int n, run;
+};
+template <int RUN>
+__global__ __launch_bounds__(256) void paged_copy_kernel(PagedCopy a) {
+  const int runs = (a.n + a.run - 1) / a.run, h = blockIdx.y;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int r = (int)(i / a.per_head), c = (int)(i - (long long)r * a.per_head);
+  if (i >= (long long)runs * a.per_head) return;
+  const int n_slots = a.n_pages * a.page;
+  long long src[RUN], dst[RUN];
+#pragma unroll
+  for (int j = 0; j < RUN; ++j) {
+    const long long m = (long long)r * a.run + j;
+    const bool in = j < a.run && m < a.n;
+    const int s = in ? a.from[m] : -1, d = in ? a.to[m] : -1;
+    const bool moves = (unsigned)s < (unsigned)n_slots && (unsigned)d < (unsigned)n_slots;
+    auto at = [&](int slot) { return (((long long)(slot / a.page) * a.Hkv + h) * a.page + slot % a.page) * a.per_head + c; };
+    src[j] = moves ? at(s) : -1;
+    dst[j] = moves ? at(d) : -1;
+  }
+  for (int l = blockIdx.z; l < 2 * a.layers; l += gridDim.z) {
+    uint4 *p = (l & 1 ? a.v : a.k) + (l >> 1) * a.layer;
+    uint4 x[RUN];
+#pragma unroll
+    for (int j = 0; j < RUN; ++j)
+      if (src[j] >= 0) x[j] = p[src[j]];
+#pragma unroll
+    for (int j = 0; j < RUN; ++j)
+      if (dst[j] >= 0) p[dst[j]] = x[j];
+  }
+}
+
 int check_pages(const la_pages_desc *p, int layer) {
   LA_REQUIRE(p && p->k && p->v, LA_EINVAL, "NULL pages");
   LA_REQUIRE(p->n_layers > 0 && p->n_pages > 0 && p->page_size > 0 && p->n_kv_heads > 0, LA_EINVAL, "page dimensions must be positive");
@@ -226,3 +266,29 @@ extern "C" int la_paged_write(const la_pages_desc *pages, int layer, const void 
   return LA_OK;
 }
 
+extern "C" int la_paged_copy(const la_pages_desc *pages, int layer_begin, int layer_end, const int32_t *from, const int32_t *to, int n, int run, void *stream) {
+  if (const int rc = check_pages(pages, 0)) return rc;
+  const la_pages_desc &p = *pages;
+  LA_REQUIRE(layer_begin >= 0 && layer_begin <= layer_end && layer_end <= p.n_layers, LA_ERANGE, "layers [%d, %d) outside the pages' %d layers", layer_begin, layer_end, p.n_layers);
+  LA_REQUIRE(n >= 0, LA_EINVAL, "n=%d is negative", n);
+  LA_REQUIRE(run >= 1 && run <= LA_MAX_ROWS, LA_EINVAL, "run=%d outside [1, %d]", run, LA_MAX_ROWS);
+  if (n == 0 || layer_begin == layer_end) return LA_OK;
+  LA_REQUIRE(from && to, LA_EINVAL, "NULL argument");
+  LA_REQUIRE(p.n_kv_heads <= 65535, LA_EINVAL, "%d kv heads are more than one launch takes", p.n_kv_heads);
+  const size_t e = esize(&p);
+  const int per_head = (int)(p.head_dim * e / 16);
+  const long long runs = ((long long)n + run - 1) / run, wgs = (runs * per_head + 255) / 256;
+  const int layers = layer_end - layer_begin, z = std::min(2 * layers, 65535);
+  LA_REQUIRE(wgs * p.n_kv_heads < 1ll << 24, LA_EINVAL, "%d rows of %d kv heads are more than one launch takes", n, p.n_kv_heads);
+  const size_t layer = layer_bytes(&p);
+  const PagedCopy a{(uint4 *)((char *)p.k + layer_begin * layer), (uint4 *)((char *)p.v + layer_begin * layer), layer / 16, layers, p.n_kv_heads, per_head, p.page_size, p.n_pages,
+                    from, to, n, run};
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps("paged_copy", s);
+  const dim3 grid((unsigned)wgs, p.n_kv_heads, z);
+  if (run == 1) paged_copy_kernel<1><<<grid, 256, 0, s>>>(a);
+  else if (run <= 8) paged_copy_kernel<8><<<grid, 256, 0, s>>>(a);
+  else paged_copy_kernel<64><<<grid, 256, 0, s>>>(a);
+  LA_HIP(hipGetLastError());
+  return LA_OK;
+}

@@ -1,0 +1,460 @@
+"""Trees of drafted tokens on the GPU: layout, accepted paths, rows moved between slots, attention of trees over pages, each against a plain implementation."""
+import random
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+T = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def binding():
+    from paper_2602_16760_amd import binding as B
+    return B
+
+
+def i32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def i64(values):
+    return torch.tensor([v - (1 << 64) if v >> 63 else v for v in values], dtype=torch.int64, device="cuda")
+
+
+def random_tree(rng, n):
+    """Parents of n rows, some of which hang on nothing, on themselves or on a row behind them."""
+    way = rng.randrange(4)
+    parent = [rng.randint(-3, n)]  # (row 0's is not looked at)
+    for j in range(1, n):
+        x = rng.random()
+        parent.append(rng.choice([-1, j, j + 1, 64, 2 ** 31 - 1, -2 ** 31]) if x < 0.06 else [j - 1, max(0, j - rng.randint(1, 5)), (j - 1) // 2, rng.randrange(j)][way])
+    return parent[:n]
+
+
+def paths(parent):
+    """(depth, mask) of a block's rows by the published rules."""
+    out = []
+    for j, p in enumerate(parent):
+        if j == 0:
+            out.append((0, 1))
+        elif j < 64 and 0 <= p < j and out[p][1]:
+            out.append((out[p][0] + 1, out[p][1] | 1 << j))
+        else:
+            out.append((-1, 0))
+    return out
+
+
+# ---- la_tree_layout ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("counts,front,pad", [([1], 0, 0), ([8], 0, 0), ([64], 0, 3), ([0, 5, 0, 64, 1, 33, 0], 0, 7), ([70, 3, 200], 0, 0), ([7] * 65, 2, 400), ([0], 0, 5),
+                                              ([3 + r % 60 for r in range(700)], 0, 1)])
+def test_layout(counts, front, pad):
+    rng = random.Random(len(counts))
+    first, parent, want = [front], [5] * front, [(-1, 0)] * front
+    lens = [rng.randint(0, 100000) for _ in counts]
+    for n, L in zip(counts, lens):
+        tree = random_tree(rng, n)
+        parent += tree
+        want += [(L + d if m else -1, m) for d, m in paths(tree)]
+        first.append(len(parent))
+    parent += [0] * pad
+    want += [(-1, 0)] * pad
+    pos, vis = i32([77] * len(parent)), i64([77] * len(parent))
+    binding().la_tree_layout(i32(parent), i32(first), i32(lens), pos, vis)
+    assert pos.tolist() == [p for p, _ in want]
+    assert vis.tolist() == i64([m for _, m in want]).tolist()
+
+
+def test_layout_of_a_chain_is_the_causal_block_and_of_no_row_nothing():
+    B = binding()
+    pos, vis = i32([0] * 64), i64([0] * 64)
+    B.la_tree_layout(i32([j - 1 for j in range(64)]), i32([0, 64]), i32([1000]), pos, vis)
+    want_pos, want_vis = B.la_causal_layout(1000, 64)
+    assert pos.tolist() == want_pos.tolist() and vis.tolist() == i64([int(v) for v in want_vis]).tolist()
+    B.la_tree_layout(i32([]), i32([0, 0, 0]), i32([4, 5]), i32([]), i64([]))
+
+
+# ---- la_tree_accept ----------------------------------------------------------------------------------------
+def accept_by_hand(parent, tok, ids, slot, L, limit, max_path, f):
+    """One request's results; f: its first row."""
+    path, emitted, n = [], [], min(64, len(parent))
+    while n and limit > 0:
+        path.append(0 if not path else nxt)
+        chosen = ids[path[-1]]
+        if chosen < 0:
+            break
+        emitted.append(chosen)
+        fits = [j for j in range(path[-1] + 1, n) if parent[j] == path[-1] and tok[j] == chosen]
+        if len(emitted) == min(limit, max_path) or not fits:
+            break
+        nxt = fits[0]
+    pad = lambda v: v + [-1] * (max_path - len(v))
+    moves = [(slot[j], slot[k]) if j != k and slot[j] >= 0 and slot[k] >= 0 else (-1, -1) for k, j in enumerate(path)]
+    return len(emitted), L + len(path), f + path[-1] if path else -1, pad(emitted), pad([a for a, _ in moves]), pad([b for _, b in moves])
+
+
+@pytest.mark.parametrize("counts,max_path,limits", [([1], 1, None), ([8], 4, None), ([64, 0, 33, 1], 64, None), ([70, 12, 90], 8, None), ([12] * 40, 6, [0, 1, 2, 3, -5, 100]),
+                                                    ([1 + r % 64 for r in range(600)], 16, [100, 100, 2, 0])])
+@pytest.mark.parametrize("seed", [0, 1])
+def test_accept(counts, max_path, limits, seed):
+    rng = random.Random(seed)
+    parent, tok, ids, slot, first, want = [], [], [], [], [0], []
+    lens = [rng.randint(0, 1000) for _ in counts]
+    limit = None if limits is None else [limits[r % len(limits)] for r in range(len(counts))]
+    for r, n in enumerate(counts):
+        tree = random_tree(rng, n)
+        t = [rng.choice([-1, 0, 1, 2, 5]) for _ in range(n)]  # (few tokens: siblings with the same one; negative ones are never chosen)
+        c = [rng.choice([0, 1, 2, 5, 5, 7]) for _ in range(n)]
+        for j in range(n - 1, 0, -1):
+            if rng.random() < 0.7 and 0 <= tree[j] < j:
+                c[tree[j]] = t[j]
+        c = [rng.choice([-1, -7]) if rng.random() < 0.05 else x for x in c]
+        s = [rng.randrange(10000) if rng.random() < 0.95 else -1 for _ in range(n)]
+        want.append(accept_by_hand(tree, t, c, s, lens[r], 1000 if limit is None else limit[r], max_path, first[-1]))
+        parent, tok, ids, slot = parent + tree, tok + t, ids + c, slot + s
+        first.append(len(parent))
+    R = len(counts)
+    got = [i32([77] * R) for _ in range(3)] + [torch.full((R, max_path), 77, dtype=torch.int32, device="cuda") for _ in range(3)]
+    binding().la_tree_accept(i32(parent), i32(tok), i32(ids), i32(slot), i32(first), i32(lens), *got, limit=None if limit is None else i32(limit))
+    for name, g, w in zip(("n_new", "new_len", "last", "out", "from", "to"), got, zip(*want)):
+        assert g.tolist() == list(w), name
+
+
+def test_accept_of_no_rows():
+    got = [i32([77] * 2) for _ in range(3)] + [torch.full((2, 3), 77, dtype=torch.int32, device="cuda") for _ in range(3)]
+    none = i32([])
+    binding().la_tree_accept(none, none, none, none, i32([0, 0, 0]), i32([9, 0]), *got)
+    assert [g.tolist() for g in got] == [[0, 0], [9, 0], [-1, -1]] + [[[-1] * 3] * 2] * 3
+
+
+# ---- la_paged_copy -----------------------------------------------------------------------------------------
+def copy_by_hand(pages, page, begin, end, frm, to, run):
+    """Run by run: all sources, then all destinations in order."""
+    out = pages.clone()
+    slots = pages.shape[1] * page
+    for i in range(0, len(frm), run):
+        moves = [(a, b) for a, b in zip(frm[i:i + run], to[i:i + run]) if 0 <= a < slots and 0 <= b < slots]
+        rows = [out[begin:end, a // page, :, a % page].clone() for a, _ in moves]
+        for (_, b), row in zip(moves, rows):
+            out[begin:end, b // page, :, b % page] = row
+    return out
+
+
+@pytest.mark.parametrize("dtype,layers,Hkv,dh,page", [("bf16", 3, 8, 128, 16), ("f16", 2, 2, 64, 5), ("f32", 2, 3, 80, 16), ("bf16", 1, 1, 8, 1), ("f32", 40, 1, 256, 24)])
+@pytest.mark.parametrize("run", [1, 2, 7, 8, 9, 64])
+def test_copy(dtype, layers, Hkv, dh, page, run):
+    """Runs whose rows are each other's destinations (paths, swaps, circles), the same destination twice in one, pairs that are none, a last run that is shorter."""
+    rng, B = random.Random(run * dh), binding()
+    runs = 5
+    n_pages = runs * run * 2 // page + 4
+    g = torch.Generator().manual_seed(dh)
+    k, v = (torch.randn((layers, n_pages, Hkv, page, dh), generator=g).to(T[dtype]) for _ in range(2))
+    slots, frm, to = rng.sample(range(n_pages * page), runs * run * 2), [], []
+    for r in range(runs):
+        mine = slots[2 * r * run:2 * (r + 1) * run]
+        a, b = [rng.choice(mine) for _ in range(run)], [rng.choice(mine) for _ in range(run)]  # (anything, twice the same among it)
+        if r == 1:
+            a, b = mine[1:run + 1], mine[:run]  # a path that moves up by one
+        if r == 2:
+            a, b = mine[:run], mine[1:run] + mine[:1]  # a circle
+        frm, to = frm + a, to + b
+    frm[-1], to[0] = -1, n_pages * page
+    frm, to = frm[:len(frm) - run // 2], to[:len(to) - run // 2]
+    begin, end = (0, layers) if run % 2 else (layers // 2, layers)
+    pages = B.la_pages(k.cuda(), v.cuda())
+    B.la_paged_copy(pages, i32(frm), i32(to), run=run, layers=(begin, end))
+    for got, was in ((pages.k, k), (pages.v, v)):
+        assert torch.equal(got.cpu(), copy_by_hand(was, page, begin, end, frm, to, run))
+
+
+def test_copy_of_whole_requests_and_rows_as_runs():
+    """A prompt's positions into pages of another request; two dimensions are runs."""
+    B, page = binding(), 16
+    k, v = (torch.randn((4, 200, 2, page, 64), generator=torch.Generator().manual_seed(s)).to(torch.bfloat16) for s in (1, 2))
+    pages = B.la_pages(k.cuda(), v.cuda())
+    order = torch.randperm(200 * page, generator=torch.Generator().manual_seed(3))
+    frm, to = order[:1500].to(torch.int32), order[1500:3000].to(torch.int32)
+    B.la_paged_copy(pages, frm.cuda(), to.cuda())
+    want = [copy_by_hand(t, page, 0, 4, frm.tolist(), to.tolist(), 1) for t in (k, v)]
+    assert torch.equal(pages.k.cpu(), want[0]) and torch.equal(pages.v.cpu(), want[1])
+    swap = torch.tensor([[3, 4], [100, 101], [-1, -1]], dtype=torch.int32)
+    B.la_paged_copy(pages, swap.cuda(), swap.flip(1).contiguous().cuda())
+    want = [copy_by_hand(t, page, 0, 4, swap.flatten().tolist(), swap.flip(1).flatten().tolist(), 2) for t in want]
+    assert torch.equal(pages.k.cpu(), want[0]) and torch.equal(pages.v.cpu(), want[1])
+
+
+def test_copy_behind_32_bits():
+    """Slots whose offsets pass 2^32 bytes in a layer, and a layer that begins behind them."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough memory")
+    B = binding()
+    n_pages = (5 << 30) // (16 * 8 * 128 * 2)
+    k = torch.empty((2, n_pages, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    slots = [0, 5, n_pages * 8 + 3, n_pages * 16 - 1]
+    rows = torch.randn((2, 2, 4, 8, 128), device="cuda").to(torch.bfloat16)
+    for t, x in ((k, rows[0]), (v, rows[1])):
+        for i, s in enumerate(slots):
+            t[:, s // 16, :, s % 16] = x[:, i]
+    B.la_paged_copy(B.la_pages(k, v), i32(slots), i32(slots[::-1]), run=4)
+    for t, x in ((k, rows[0]), (v, rows[1])):
+        for i, s in enumerate(slots):
+            assert torch.equal(t[:, s // 16, :, s % 16], x[:, 3 - i])
+
+
+# ---- la_paged_tree_attend ------------------------------------------------------------------------------------
+class Case:
+    """Pages in any order, NaN wherever no request has a position; a request's keys are its committed positions and its block's rows."""
+
+    def __init__(self, dtype, Hq, Hkv, dh, page, lens, counts, seed=0, spread=1.0, blocks=None, layers=1, back=0, masks=None):
+        g, rng = torch.Generator().manual_seed(seed), random.Random(seed)
+        self.dtype, self.Hq, self.Hkv, self.dh, self.page, self.lens, self.counts, self.g = T[dtype], Hq, Hkv, dh, page, lens, counts, g
+        total = [max(0, n) + c for n, c in zip(lens, counts)]
+        used = [(n + page - 1) // page for n in total]
+        n_pages = sum(used) + 2
+        order = torch.randperm(n_pages, generator=g).tolist()
+        blocks = blocks or max(1, max(used))
+        self.table = torch.full((len(lens), blocks), -1, dtype=torch.int32)
+        self.k, self.v = (torch.full((layers, n_pages, Hkv, page, dh), float("nan"), dtype=self.dtype) for _ in range(2))
+        self.layer, self.keys, self.first, self.vis, at = layers - 1, [], [0], [], 0
+        for r, n in enumerate(total):
+            mine = order[at:at + used[r]]
+            at += used[r]
+            self.table[r, :used[r]] = torch.tensor(mine, dtype=torch.int32)
+            k, v = ((torch.randn((n, Hkv, dh), generator=g)).to(self.dtype) for _ in range(2))
+            self.keys.append((k, v))
+            for b, p in enumerate(mine):
+                part = slice(b * page, min(n, (b + 1) * page))
+                m = part.stop - part.start
+                self.k[layers - 1, p, :, :m] = k[part].transpose(0, 1)
+                self.v[layers - 1, p, :, :m] = v[part].transpose(0, 1)
+            self.vis += [m for _, m in paths(random_tree(rng, counts[r]))] if masks is None else masks[r]
+            self.first.append(len(self.vis))
+        self.vis += [1] * back  # (rows of no request)
+        self.q = (torch.randn((len(self.vis), Hq, dh), generator=g) * spread).to(self.dtype)
+
+    def place(self, r, t):
+        return (self.layer, int(self.table[r, t // self.page]), slice(None), t % self.page)
+
+    def run(self, max_rows=64, scale=None, lens=None):
+        B = binding()
+        out = torch.full(self.q.shape, 77.0, dtype=self.dtype, device="cuda")
+        B.la_paged_tree_attend(B.la_pages(self.k.cuda(), self.v.cuda()), self.layer, self.q.cuda(), self.table.cuda(), i32(self.first), i32(self.lens if lens is None else lens),
+                               i64(self.vis), max_rows, out, scale=scale)
+        torch.cuda.synchronize()
+        return out.cpu()
+
+    def check(self, out, scale=None, max_rows=64, skip=lambda r, t: False, rows=None):
+        """Against float64, as la_paged_attend's rows are: a probability is rounded to the type (half a step of it), as is the output; scores are sums of dh float products, their error shifts a
+        probability by as much relatively; the exponential and the sums over n keys add 2^-23 a term."""
+        scale = self.dh ** -0.5 if scale is None else scale
+        half, g = torch.finfo(self.dtype).eps / 2, self.Hq // self.Hkv
+        for r, L in enumerate(self.lens):
+            k, v = (t.double().repeat_interleave(g, 1) for t in self.keys[r])
+            for i in range(self.first[r], self.first[r + 1]):
+                if rows is not None and i not in rows:
+                    continue
+                n_rows, j0 = min(max_rows, self.counts[r], 64), i - self.first[r]
+                see = [t for t in range(L)] + [L + j for j in range(n_rows) if self.vis[i] >> j & 1]
+                see = [t for t in see if not skip(r, t)] if self.vis[i] and L >= 0 and j0 < n_rows else []
+                if not see:
+                    assert (out[i] == 0).all(), f"row {i} sees nothing"
+                    continue
+                ks, vs = k[see], v[see]
+                s = torch.einsum("hd,nhd->hn", self.q[i].double(), ks) * scale
+                size = torch.einsum("hd,nhd->hn", self.q[i].double().abs(), ks.abs()).amax(1) * abs(scale)
+                w = torch.softmax(s, 1)
+                want, mass = torch.einsum("hn,nhd->hd", w, vs), torch.einsum("hn,nhd->hd", w, vs.abs())
+                shift = ((self.dh + 8) * 2.0 ** -24 * size)[:, None]
+                tol = (half if self.dtype != torch.float32 else 0.0) * mass + half * want.abs() + 2 * shift * mass + (len(see) + 16) * 2.0 ** -23 * mass + 1e-30
+                err = (out[i].double() - want).abs()
+                assert (err <= tol).all(), f"row {i} (request {r}, {len(see)} keys): {float((err / tol).max()):.2f} of the bound"
+        assert (out[self.first[-1]:] == 0).all()
+
+
+SHAPES = [("bf16", 32, 8, 128, 16), ("f16", 8, 2, 128, 16), ("bf16", 6, 2, 64, 32), ("f32", 4, 2, 64, 24), ("bf16", 24, 2, 96, 16), ("f16", 16, 1, 256, 16), ("bf16", 32, 1, 128, 8),
+          ("bf16", 20, 1, 64, 5), ("f16", 3, 3, 8, 1), ("f32", 6, 3, 80, 16), ("f32", 5, 1, 256, 3), ("bf16", 2, 2, 200, 48), ("f16", 17, 1, 128, 64), ("bf16", 8, 1, 256, 33),
+          ("f16", 9, 1, 64, 16), ("bf16", 5, 5, 128, 16), ("f32", 8, 1, 128, 16)]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page", SHAPES)
+def test_attend_short_and_long_requests(dtype, Hq, Hkv, dh, page):
+    """No committed position, ends inside a page, a tile and a block, blocks of no row to 64, rows of no request behind them."""
+    lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 100, 127, 128, 129, 700, 5]
+    counts = [3, 1, 16, 17, 0, 4, 33, 64, 1, 9, 2, 31, 32, 12, 0]
+    c = Case(dtype, Hq, Hkv, dh, page, lens, counts, back=3)
+    out = c.run()
+    c.check(out)
+    assert torch.equal(out, c.run())
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,lens,counts", [
+    ("bf16", 32, 8, 128, 16, [5000, 1, 900, 4096], [16, 16, 5, 1]), ("bf16", 8, 8, 64, 64, [20000], [64]), ("f32", 4, 2, 64, 24, [3001, 40, 3000], [10, 64, 1]),
+    ("f16", 12, 1, 256, 16, [9000, 77], [7, 40]), ("bf16", 16, 2, 112, 20, [2500, 2501, 600], [8, 1, 63]), ("f16", 40, 1, 128, 16, [3000, 800], [64, 3]), ("f16", 32, 8, 128, 32, [6000, 2047], [64, 50])])
+def test_attend_requests_cut_into_items(dtype, Hq, Hkv, dh, page, lens, counts):
+    """Requests that several workgroups share and a second launch joins, beside ones that are not cut."""
+    c = Case(dtype, Hq, Hkv, dh, page, lens, counts, seed=3, spread=2.0)
+    out = c.run()
+    c.check(out)
+    assert torch.equal(out, c.run())
+
+
+@pytest.mark.parametrize("rows,heads", [(1, 1), (1, 4), (2, 8), (5, 3), (8, 4), (16, 1), (17, 1), (16, 4), (33, 2), (64, 1), (64, 4), (64, 8), (9, 16), (64, 16)])
+def test_attend_columns(rows, heads):
+    """Every number of query heads and rows that share a key, short and cut."""
+    for ctx in (90, 1500):
+        c = Case("bf16", heads, 1, 64, 16, [ctx, 3], [rows, max(1, rows // 2)], seed=rows)
+        c.check(c.run(max_rows=rows), max_rows=rows)
+
+
+@pytest.mark.parametrize("R", [64, 65, 130, 300])
+@pytest.mark.parametrize("ctx", [300, 2000])
+def test_attend_many_requests(R, ctx):
+    """More requests than a wave's lanes look up at once, with and without items."""
+    lens, counts = [(37 * r) % ctx for r in range(R)], [(5 * r) % 4 for r in range(R)]
+    c = Case("bf16", 4, 2, 64, 16, lens, counts, seed=R)
+    c.check(c.run(max_rows=4), max_rows=4)
+
+
+def test_attend_masks_of_any_kind():
+    """Rows that do not see themselves, see later rows, see nothing but the committed positions of their own block, bits behind the block's rows."""
+    full = (1 << 64) - 1
+    masks = [[full, 0, 1 << 63, 0b1010, full << 20 & full, 0b100], [0, 0, 0], [1, 0, full]]
+    c = Case("bf16", 8, 2, 128, 16, [50, 20, 0], [6, 3, 3], masks=masks)
+    c.check(c.run())
+    c.check(c.run(max_rows=6), max_rows=6)
+
+
+@pytest.mark.parametrize("max_rows", [1, 4, 15, 16, 17])
+def test_attend_rows_behind_max_rows_see_nothing(max_rows):
+    c = Case("bf16", 8, 2, 64, 16, [100, 30, 2000], [17, 5, 16])
+    c.check(c.run(max_rows=max_rows), max_rows=max_rows)
+
+
+def test_attend_lengths_that_are_none():
+    """A negative length; a length behind the table's end."""
+    c = Case("bf16", 4, 2, 64, 16, [48, 30], [5, 5])
+    out = c.run(lens=[-1, 30])
+    assert (out[:5] == 0).all()
+    c.check(out, rows=range(5, 10))
+    c = Case("bf16", 4, 2, 64, 16, [64, 64], [1, 2], blocks=5, masks=[[1], [3, 3]])
+    out = c.run(lens=[2 ** 31 - 1, 64])  # (80 positions are the table's, 65 of them are the request's; those behind have no page's data)
+    c.table[0, 4] = -1
+    out = c.run(lens=[2 ** 31 - 1, 64])
+    c.check(out, skip=lambda r, t: r == 0 and t >= 64)
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("bf16", 12), ("f32", 12), ("f16", 64)])
+def test_attend_pages_that_are_none(dtype, page):
+    c = Case(dtype, 4, 2, 64, page, [200, 200, 10], [9, 3, 2])
+    c.table[0, 1], c.table[1, :], c.table[2, 0] = -5, 1 << 20, -1
+    out = c.run()
+    c.check(out, skip=lambda r, t: (r == 0 and t // page == 1) or r == 1 or (r == 2 and t // page == 0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 8.0])
+def test_attend_other_scales(dtype, scale):
+    c = Case(dtype, 4, 1, 64, 16, [200, 33], [6, 20], seed=9)
+    c.check(c.run(scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,ctx", [("f32", 2, 1, 64, 16, 40), ("bf16", 2, 1, 64, 16, 40), ("bf16", 32, 2, 128, 16, 1500), ("f16", 8, 1, 256, 24, 100), ("f16", 8, 2, 96, 16, 900)])
+def test_attend_values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx):
+    """K and V of infinities and NaN in a drafted row reach the rows that see it, in their own channels, and no other row."""
+    n = 40
+    parent = [0, 0, 1, 0, 3, 0, 5, 6] + [0] * (n - 8)  # rows 2, 4 and 7 end three branches
+    masks = [m for _, m in paths(parent)]
+    c = Case(dtype, Hq, Hkv, dh, page, [ctx, 20], [n, 4], masks=[masks, [1, 3, 5, 7]])
+    inf, nan = float("inf"), float("nan")
+    c.v[c.place(0, ctx + 2)][:, 5] = inf      # seen by row 2 alone
+    c.v[c.place(0, ctx + 3)][:, 7] = nan      # by rows 3 and 4
+    c.v[c.place(0, ctx + 4)][:, 9] = -inf     # by row 4
+    c.k[c.place(0, ctx + 7)][:, 1] = nan      # by row 7
+    c.k[c.place(0, ctx + 20)] = inf           # by row 20
+    c.v[c.place(0, ctx + 20)] = nan
+    c.v[c.place(0, ctx + 33)][:, 0] = inf     # (another tile of keys)
+    out = c.run()
+    finite = [i for i in range(n + 4) if i not in (2, 3, 4, 7, 20, 33)]
+    assert torch.isfinite(out[finite]).all()
+    c.check(out, rows=finite)
+    assert (out[2, :, 5] == inf).all() and torch.isfinite(out[2, :, 6:]).all() and torch.isfinite(out[2, :, :5]).all()
+    assert torch.isnan(out[3, :, 7]).all() and torch.isfinite(out[3, :, 8:]).all()
+    assert torch.isnan(out[4, :, 7]).all() and (out[4, :, 9] == -inf).all() and torch.isfinite(out[4, :, 10:]).all() and torch.isfinite(out[4, :, 8]).all()
+    assert torch.isnan(out[7]).all() and torch.isnan(out[20]).all()
+    assert (out[33, :, 0] == inf).all() and torch.isfinite(out[33, :, 1:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attend_committed_values_that_are_none(dtype):
+    """An infinite V of a committed position reaches every row that has a mask, scores of -inf alone give zeros, and a request's NaN stays in it."""
+    c = Case(dtype, 2, 1, 64, 16, [40, 20, 33, 8], [3, 2, 4, 5], masks=[[1, 3, 0], [1, 2], [1, 3, 5, 0], [1, 3, 7, 15, 31]])
+    c.v[c.place(0, 39)][:, 5] = float("inf")
+    c.k[c.layer, c.table[1, :2].long()] = float("-inf")
+    c.q[3:5] = c.q[3:5].abs() + 0.5
+    c.k[c.place(2, 30)][:, 3] = float("nan")
+    out = c.run()
+    assert torch.isinf(out[:2, :, 5]).all() and torch.isfinite(out[:2, :, 6:]).all() and (out[2] == 0).all()
+    assert (out[3:5] == 0).all() and torch.isnan(out[5:8]).all() and (out[8] == 0).all()
+    c.check(out, rows=range(9, 14))
+
+
+def test_attend_strided_rows_and_layers():
+    c = Case("bf16", 8, 2, 128, 16, [40, 300], [5, 7], layers=3)
+    B = binding()
+    wide = torch.randn((12, 8 * 128 + 512), generator=c.g).to(torch.bfloat16)
+    out = torch.full((12, 8 * 128 + 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    tab = torch.full((2, 64), -1, dtype=torch.int32)
+    tab[:, :c.table.shape[1]] = c.table
+    view = lambda t, at: t[:, at:at + 1024].unflatten(1, (8, 128))
+    B.la_paged_tree_attend(B.la_pages(c.k.cuda(), c.v.cuda()), 2, view(wide.cuda(), 512), tab.cuda()[:, :c.table.shape[1]], i32(c.first), i32(c.lens), i64(c.vis), 7, view(out, 64))
+    c.q = view(wide, 512)
+    c.check(view(out, 64).cpu())
+    assert (out[:, :64] == 7).all()
+
+
+def test_attend_small_weights_beside_a_large_one():
+    """Keys of 2^-25 times the first one's weight, 512 of them, whose V are what is left: half precision has no such numbers."""
+    c = Case("f16", 1, 1, 64, 16, [513], [3], masks=[[1, 3, 5]])
+    c.q[:] = 0
+    c.q[:, :, 0] = 8.0
+    for t in range(516):
+        k, v = c.k[c.place(0, t)], c.v[c.place(0, t)]
+        k[:], v[:] = 0, 1.0
+        k[:, 0] = 0.0 if t == 0 else -2.166
+        v[:] = 0.0 if t == 0 else 1.0
+        c.keys[0][0][t], c.keys[0][1][t] = k, v
+    out = c.run(scale=1.0)
+    want = torch.softmax(torch.tensor([0.0] + [8.0 * float(torch.tensor(-2.166).half())] * 515, dtype=torch.float64), 0)[1:].sum()
+    for i, n in ((0, 513), (1, 514), (2, 514)):
+        mass = float(want) * n / 515
+        # (the output, 1.5e-5, lies below 2^-14, where half precision's numbers are 2^-24 apart: rounding alone is off by up to 2^-25)
+        assert (out[i].double() - mass).abs().max() <= 2.0 ** -10 * mass + 2.0 ** -25
+
+
+def test_attend_a_pool_behind_32_bits():
+    """Pages whose offsets pass 2^32 bytes, keys of them at both ends."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("not enough memory")
+    B = binding()
+    n_pages = (5 << 30) // (16 * 8 * 128 * 2)
+    k = torch.empty((1, n_pages, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    for heads, rows in ((8, 12), (32, 64)):
+        c = Case("bf16", heads, 8, 128, 16, [600, 50, 2000], [rows, 3, 1])
+        spots = torch.linspace(0, n_pages - 1, c.k.shape[1]).long()
+        k[0, spots.cuda()], v[0, spots.cuda()] = c.k[0].cuda(), c.v[0].cuda()
+        table = torch.where(c.table >= 0, spots[c.table.clamp(min=0).long()].to(torch.int32), c.table)
+        out = torch.empty_like(c.q, device="cuda")
+        B.la_paged_tree_attend(B.la_pages(k, v), 0, c.q.cuda(), table.cuda(), i32(c.first), i32(c.lens), i64(c.vis), rows, out)
+        c.check(out.cpu())
+
+
+def test_attend_rows_of_one_are_the_paged_attentions():
+    """A block of one row each is a decode step: as la_paged_attend's rows, within two roundings of the output."""
+    B = binding()
+    lens = [0, 5, 900, 3000]
+    c = Case("bf16", 32, 8, 128, 16, lens, [1] * 4, masks=[[1]] * 4)
+    out, pages = torch.empty_like(c.q, device="cuda"), B.la_pages(c.k.cuda(), c.v.cuda())
+    B.la_paged_attend(pages, 0, c.q.cuda(), c.table.cuda(), None, i32(lens), out)
+    assert (c.run(max_rows=1).double() - out.cpu().double()).abs().le(2.0 ** -7 * out.cpu().double().abs() + 1e-4).all()
