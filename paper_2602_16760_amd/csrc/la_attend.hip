@@ -4,19 +4,10 @@
 // positions, the table, K and V, the waves' meeting, each waiting for the one before.  Pages that 16 does not divide, and float: the table is looked up for every block of keys, a trip to memory
 // that the block's loads wait for (17 rows of up to 1008, float, pages of 24: 3.6 MB, 8 us).
 #include <algorithm>
-#include <type_traits>
 
-#include "la_attend_plan.h"
-#include "la_lanes.h"
-#include "la_paged.h"
+#include "la_attend.h"
 
 namespace la {
-
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 at_b8;
-typedef _Float16 __attribute__((ext_vector_type(8))) at_h8;
-typedef float __attribute__((ext_vector_type(4))) at_f4;
-typedef unsigned __attribute__((ext_vector_type(4))) at_u4;
-typedef unsigned __attribute__((ext_vector_type(2))) at_u2;
 
 struct PagedAttend {
   const void *K, *V;  // of the layer
@@ -43,146 +34,12 @@ struct PagedAttend {
 
 constexpr int AT_WAVES = 4, AT_WHOLE_WAVES = 8;  // of a workgroup; where rows are not cut and heads are few
 constexpr int AT_JOIN_WAVES = 4;
-constexpr float AT_LOG2E = 1.4426950408889634f;
 
 // Keys that row b sees (none where it is padding or names no request), and its request.
 __device__ __forceinline__ int at_keys(const PagedAttend &a, int b, int &r) {
   r = a.req ? a.req[b] : b;
   const long long n = (long long)a.pos[b] + 1, cap = (long long)a.max_blocks * a.page;
   return (unsigned)r >= (unsigned)a.n_req || n < 0 ? 0 : (int)(n < cap ? n : cap);
-}
-
-// The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
-// positions, a lane each; of more it was written down by a launch of its own: formed by every workgroup from all rows' positions, 64 at a time, the time grew with the square of the
-// rows (512 rows of 1000 379 us, with the list 344; 65 rows 57 and 59).
-template <bool BY_ROW>
-__device__ __forceinline__ AtItem at_find(const PagedAttend &a, int wanted) {
-  AtItem it{};
-  if (a.target <= 0) {
-    int r;
-    const int n = at_keys(a, wanted, r);
-    it.b = wanted;
-    it.r = uniform(r);
-    it.n = uniform(n);
-    it.C = AT_UNCUT;
-    it.first = wanted;
-    it.count = 1;
-    return it;
-  }
-  if (a.list) return a.list[BY_ROW ? a.firsts[wanted] : wanted];
-  const int lane = threadIdx.x & 63;
-  int r = 0;
-  const int n = lane < a.B ? at_keys(a, lane, r) : 0;
-  int c = 0, ends = 0;
-  auto items = [&](int C) {
-    c = lane < a.B ? at_rows_items(n, C) : 0;
-    ends = lane_through(c);
-    return lane_value(ends, 63);
-  };
-  (void)items(at_cut(a.B, a.target, lane_value(lane_through((long long)n), 63), lane_most(n), items));
-  const int l = BY_ROW ? wanted : __builtin_popcountll(__ballot(ends <= wanted));
-  it.b = -1;
-  if (l >= a.B) return it;
-  it.b = l;
-  it.r = lane_value(r, l);
-  it.n = lane_value(n, l);
-  it.count = lane_value(c, l);
-  it.C = uniform(at_item_keys(it.n, it.count));
-  it.first = lane_value(ends, l) - it.count;
-  it.index = BY_ROW ? 0 : wanted - it.first;
-  return it;
-}
-
-// The same items of more than 64 rows, by one workgroup that goes through the rows a thread each; `items`: places in the list.
-constexpr int AT_PLAN_THREADS = 1024;
-__global__ __launch_bounds__(AT_PLAN_THREADS) void paged_plan_kernel(PagedAttend a, int items) {
-  constexpr int WAVES = AT_PLAN_THREADS / 64;
-  __shared__ long long red[WAVES];
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  auto all_of = [&](long long v) {  // its sum over the threads
-    v = lane_through(v);
-    __syncthreads();
-    if (lane == 63) red[wave] = v;
-    __syncthreads();
-    return uniform((unsigned long long)sum_of(red, WAVES));
-  };
-  long long keys = 0;
-  int r, longest = 0;
-  for (int b = t; b < a.B; b += AT_PLAN_THREADS) {
-    const int n = at_keys(a, b, r);
-    keys += n;
-    longest = longest > n ? longest : n;
-  }
-  keys = (long long)all_of(keys);
-  __syncthreads();
-  longest = lane_most(longest);
-  if (lane == 0) red[wave] = longest;
-  __syncthreads();
-  longest = lane_most(lane < WAVES ? (int)red[lane] : 0);
-  const int C = at_cut(a.B, a.target, keys, longest, [&](int C) {
-    long long c = 0;
-    for (int b = t; b < a.B; b += AT_PLAN_THREADS) c += at_rows_items(at_keys(a, b, r), C);
-    return (int)all_of(c);
-  });
-  int before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += AT_PLAN_THREADS) {
-    const int b = b0 + t, n = b < a.B ? at_keys(a, b, r) : 0, c = b < a.B ? at_rows_items(n, C) : 0;
-    const int through = lane_through(c);
-    const int total = (int)all_of(c);  // (what it leaves in `red` are the waves' sums)
-    const int first = before + (int)sum_of(red, wave) + through - c;
-    if (b < a.B) a.firsts[b] = first;
-    for (int i = 0; i < c && first + i < items; ++i) a.list[first + i] = AtItem{b, r, n, at_item_keys(n, c), i, first, c, 0};
-    before += total;
-  }
-  for (int i = before + t; i < items; i += AT_PLAN_THREADS) a.list[i].b = -1;
-}
-
-__device__ __forceinline__ float at_max4(float v) {  // over the four lanes 16 apart
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-__device__ __forceinline__ float at_sum4(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
-
-template <typename T>
-__device__ __forceinline__ unsigned at_pack(float lo, float hi) {  // to nearest even
-  typedef float f2 __attribute__((ext_vector_type(2)));
-  if constexpr (std::is_same<T, _Float16>::value) {
-    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), h2));
-  } else {
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2{lo, hi}), b2));
-  }
-}
-// Two weights as the sum of two 16-bit numbers each, both above zero where the weight is, so that an infinite V stays one: the first is short of the weight by one to three half
-// steps, the second is what that leaves.  Together they are off by 2^-20 of the weight at most (half precision), 2^-14 (bfloat16).
-template <typename T>
-__device__ __forceinline__ at_u2 at_split(float x, float y) {
-  constexpr bool F16 = std::is_same<T, _Float16>::value;
-  constexpr float SHORT = F16 ? 1.f - 0x1p-10f : 1.f - 0x1p-7f;
-  const unsigned first = at_pack<T>(x * SHORT, y * SHORT);
-  const float x0 = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(first & 0xffffu)) : __uint_as_float(first << 16);
-  const float y0 = F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)(first >> 16)) : __uint_as_float(first & 0xffff0000u);
-  return at_u2{first, at_pack<T>(x - x0, y - y0)};
-}
-template <typename T>
-__device__ __forceinline__ at_f4 at_mma(at_u4 x, at_u4 y, at_f4 c) {
-  if constexpr (std::is_same<T, _Float16>::value)
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(at_h8, x), __builtin_bit_cast(at_h8, y), c, 0, 0, 0);
-  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(at_b8, x), __builtin_bit_cast(at_b8, y), c, 0, 0, 0);
-}
-
-// A value of the output where a model's next product wants it (the fragments' type takes +-65504 at most).
-__device__ __forceinline__ void at_store_row(const PagedAttend &a, int b, int col, float y) {
-  if (a.kind == AT_OUT_FLOAT) {
-    ((float *)a.out)[b * a.ldo + col] = y;
-  } else {
-    _Float16 *to = (_Float16 *)a.out + (((size_t)(col >> 5) * a.q_tiles + (b >> 4)) * 64 + (b & 15) + 16 * ((col & 31) >> 3)) * 8 + (col & 7);
-    *to = (_Float16)fminf(fmaxf(y, -65504.f), 65504.f);
-  }
 }
 
 // A workgroup takes an item's keys for one kv head and up to 16 of its query heads; its waves take blocks of KEYS keys in turn and meet once, at the end.
@@ -213,7 +70,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
   extern __shared__ __attribute__((aligned(16))) float at_lds[];
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
   const int g = uniform(a.Hq / a.Hkv), tiles = uniform((g + AT_ROWS - 1) / AT_ROWS), item = uniform((int)blockIdx.x / (a.Hkv * tiles)), share = (int)blockIdx.x - item * a.Hkv * tiles;
-  const AtItem it = at_find<false>(a, item);
+  const AtItem it = at_find<false, false>(a, item);
   if (it.b < 0) return;  // (all waves)
   const int h = uniform(share / tiles), g0 = share % tiles * AT_ROWS, dh = FULL ? DH : a.dh;
   const int rows = g - g0 < AT_ROWS ? g - g0 : AT_ROWS, head0 = h * g + g0;
@@ -471,7 +328,7 @@ __global__ __launch_bounds__(64 * WAVES, DH > 128 ? 1 : 2) void paged_attend_ker
 template <typename T>
 __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAttend a) {
   __shared__ float sums[AT_JOIN_WAVES][256];
-  const AtItem it = at_find<true>(a, blockIdx.x);
+  const AtItem it = at_find<true, false>(a, blockIdx.x);
   if (it.count < 2) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, head = blockIdx.y;
   const size_t step = (size_t)a.Hq * a.rec;
@@ -552,7 +409,7 @@ static int at_launch(const PagedAttend &a, const AtPlan &plan, hipStream_t s) {
   if constexpr (DH <= 128) wide = plan.target == 0 && rows <= 8 && (long long)plan.items * a.Hkv * plan.tiles <= AT_WIDE;
   if (a.list) {
     ProfScope ps("paged_plan", s);
-    paged_plan_kernel<<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
+    paged_plan_kernel<false><<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
   }
   {
     ProfScope ps("paged_attend", s);

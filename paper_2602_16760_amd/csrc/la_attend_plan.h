@@ -13,7 +13,7 @@ namespace la {
 
 struct AtItem {
   int b, r, n, C, index, first, count;  // row, its request and keys; keys per item; which of the row's items; the row's first item; how many it has
-  int pad;
+  int record;  // of a row that is cut: the item among all such rows' items
 };
 
 constexpr int AT_ROWS = 16;        // query heads of a tile

@@ -1,6 +1,7 @@
 // Attention of trees of drafted tokens over the pages of their requests (la_paged_tree_attend).
-#include "la_lanes.h"
-#include "la_paged.h"
+#include <algorithm>
+
+#include "la_attend.h"
 
 namespace la {
 
@@ -13,67 +14,580 @@ struct TreeAttend {
   float scale;
   const int32_t *table;
   int64_t ldt;
-  int n_req, max_blocks;
+  int B, max_blocks;  // requests
   const int32_t *first, *len;
   const uint64_t *vis;
-  int max_rows, B;
+  int max_rows, N;  // rows of a request at most, of all
   void *out;
   int64_t ldo;
+  int target, tiles;  // as at_plan has them
+  int q_tiles, kind;  // as la_paged_attend's
+  int rec;            // floats of a row's and head's record of an item
+  float *part;        // [record][Hq][max_rows][rec]
+  AtItem *list;
+  int32_t *firsts;
 };
 
-// A wave per row and query head; a lane a key for the scores, a lane four channels for the sums.
+// A request's rows: the first one's number, and how many take part.
+__device__ __forceinline__ int tree_rows(const TreeAttend &a, int r, int &f) {
+  f = a.first[r];
+  const int e = a.first[r + 1], n = (e < a.N ? e : a.N) - f;
+  return f < 0 || n < 0 ? 0 : n < a.max_rows ? n : a.max_rows;
+}
+__device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
+  int f;
+  r = b;
+  const int rows = tree_rows(a, b, f);
+  const long long L = a.len[b], n = L + rows, cap = (long long)a.max_blocks * a.page;
+  return rows == 0 || L < 0 ? 0 : (int)(n < cap ? n : cap);
+}
+
+constexpr int TA_WAVES = 4;
+// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled; weights are up to 2^LAZY then, and half
+// precision's carry 2^UP instead of 2^15.
+template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 4.f : 8.f;
+template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 11.f : 0.f;
+// Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
+// infinite V stays one).  The factor is the same for all weights and goes out with their sum.
+template <typename T> constexpr float TA_REST = std::is_same<T, _Float16>::value ? 0x1p-10f : sizeof(T) == 2 ? 0x1p-12f : 0.f;
 template <typename T>
-__global__ __launch_bounds__(64) void tree_attend_simple_kernel(TreeAttend a) {
-  const int i = blockIdx.x, head = blockIdx.y, lane = threadIdx.x, h = head / (a.Hq / a.Hkv);
-  int lo = 0, hi = a.n_req;  // the last request that begins at or in front of the row
-  while (hi - lo > 1) {
-    const int m = (lo + hi) / 2;
-    if (a.first[m] <= i) lo = m; else hi = m;
+__device__ __forceinline__ at_u2 ta_split(float x, float y) {
+  if constexpr (std::is_same<T, _Float16>::value) {
+    const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
+    return at_u2{__builtin_bit_cast(unsigned, cut), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), __builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1]))};
+  } else {
+    const unsigned u = __float_as_uint(x), v = __float_as_uint(y);
+    return at_u2{__builtin_amdgcn_perm(v, u, 0x07060302u), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -__uint_as_float(u & 0xffff0000u)),
+                                                                      __builtin_fmaf(y, 1.f + TA_REST<T>, -__uint_as_float(v & 0xffff0000u)))};
   }
-  while (lo > 0 && a.first[lo] > i) --lo;
-  const int r = lo, j = i - a.first[r];
-  const bool in = j >= 0 && i < a.first[r + 1] && j < a.max_rows;
-  const unsigned long long vis = in ? a.vis[i] : 0;
-  const long long L = a.len[r], cap = (long long)a.max_blocks * a.page;
-  const T *q = (const T *)a.q + i * a.ldq + (int64_t)head * a.dh;
-  float o[4] = {0.f, 0.f, 0.f, 0.f}, m_run = -INFINITY, l = 0.f;
-  const long long rows = a.first[r + 1] - a.first[r] < a.max_rows ? a.first[r + 1] - a.first[r] : a.max_rows;
-  const long long n = vis && L >= 0 ? (L + rows < cap ? L + rows : cap) : 0;
-  for (long long k0 = 0; k0 < n; k0 += 64) {
-    const long long k = k0 + lane;
-    bool seen = k < n && (k < L || (vis >> (k - L) & 1));
-    long long at = 0;
-    if (seen) {
-      const int pg = a.table[r * a.ldt + k / a.page];
-      seen = (unsigned)pg < (unsigned)a.n_pages;
-      at = (((long long)pg * a.Hkv + h) * a.page + k % a.page) * a.dh;
+}
+template <typename T>
+__device__ __forceinline__ float ta_half(unsigned v, int hi) {
+  const uint16_t bits = (uint16_t)(v >> (16 * hi));
+  if constexpr (std::is_same<T, _Float16>::value) return (float)__builtin_bit_cast(_Float16, bits);
+  else return bf16_to_float(bits);
+}
+template <typename T>
+__device__ __forceinline__ bool ta_odd(unsigned v) {  // an infinity or NaN among a word's numbers
+  if constexpr (sizeof(T) == 4) return (v & 0x7f800000u) == 0x7f800000u;
+  constexpr unsigned E = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
+  return (v & E) == E || (v >> 16 & E) == E;
+}
+
+// Zeros for rows that see nothing: those of no request, and a request's behind the ones that take part.
+template <typename T>
+__device__ __forceinline__ void ta_zero(const TreeAttend &a, long long i, int col0, int cols, int t, int threads) {
+  for (int c = t; c < cols; c += threads) {
+    if (a.kind != AT_OUT_ROWS) at_store_row(a, (int)i, col0 + c, 0.f);
+    else ((T *)a.out)[i * a.ldo + col0 + c] = T(0);
+  }
+}
+
+// A workgroup takes an item's keys for one kv head and 16 NT of its columns; column c of a kv head is query head c % g of the request's row c / g, so that those of a block of few rows lie
+// together.  The waves take blocks of KEYS keys in turn and meet once, at the end.  Products, types and pages as in la_attend.hip, K and V of a block go through the matrix instructions NT times.
+template <typename T, int DH, int NT, bool FAST>
+__global__ __launch_bounds__(64 * TA_WAVES) void tree_attend_kernel(TreeAttend a) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES, WAVES = TA_WAVES;
+  constexpr int KP = DH * E / 64;                  // 16-byte pieces of a key row per lane (four lanes a row)
+  constexpr int VW = DH * E / 16 < 16 ? 8 : 16;    // bytes of a V load: a row's share of each of 16 lanes, at most 16
+  constexpr int VH = DH * E / 16 / VW;             // such loads a row
+  constexpr int VC = VW / E;                       // channels of one
+  constexpr int DT = DH / 16;                      // tiles of the output: channel VH-th part, one of VC
+  constexpr int VK = 4 * TILES;                    // keys whose V a lane loads
+  constexpr float UP = TA_UP<T>, LAZY = TA_LAZY<T>;
+  extern __shared__ __attribute__((aligned(16))) float at_lds[];
+  const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
+  const int g = uniform(a.Hq / a.Hkv), item = uniform((int)blockIdx.x / (a.Hkv * a.tiles)), share = (int)blockIdx.x - item * a.Hkv * a.tiles;
+  const int h = uniform(share / a.tiles), tile = uniform(share % a.tiles), dh = FAST ? DH : a.dh;
+  for (long long i = (long long)max(a.first[a.B], 0) + blockIdx.x; i < a.N; i += gridDim.x) ta_zero<T>(a, i, 0, a.Hq * dh, threadIdx.x, 64 * WAVES);
+  for (long long i = blockIdx.x; i < min(a.first[0], a.N); i += gridDim.x) ta_zero<T>(a, i, 0, a.Hq * dh, threadIdx.x, 64 * WAVES);
+  const AtItem it = at_find<false, true>(a, item);
+  if (it.b < 0) return;  // (all waves)
+  int f0;
+  const int n_rows = uniform(tree_rows(a, it.b, f0)), first = uniform(f0), L = uniform(a.len[it.b]);
+  if (it.index == 0 && tile == 0)
+    for (long long i = first + n_rows; first >= 0 && i < min(a.first[it.b + 1], a.N); ++i) ta_zero<T>(a, i, h * g * dh, g * dh, threadIdx.x, 64 * WAVES);
+  const int cols = n_rows * g - tile * 16 * NT;  // of this workgroup, if it had room for all
+  if (cols <= 0) return;
+  const int k_first = it.index * it.C, k_end = at_item_end(it);  // (C is a multiple of the block)
+  // this lane's columns
+  at_u4 q[NT][KP];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int c = tile * 16 * NT + (16 * t + c16 < cols ? 16 * t + c16 : 0), j = c / g, i = first + j, head = h * g + c - j * g;
+    const char *qp = (const char *)a.q + (a.q_tiles ? (((int64_t)head * a.q_tiles + (i >> 4)) * (dh / 32) * 64 + (i & 15)) * 16 : (i * a.ldq + (int64_t)head * dh) * E);
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+      const int at = 64 * p + 16 * q4;
+      q[t][p] = FAST || at < dh * E ? *(const at_u4 *)(qp + (a.q_tiles ? 1024 * p + 256 * q4 : at)) : at_u4{0, 0, 0, 0};
     }
-    float s = -INFINITY;
-    if (seen) {
-      s = 0.f;
-      for (int c = 0; c < a.dh; ++c) s += load_as_float<T>(q + c) * load_as_float<T>((const T *)a.K + at + c);
-      s *= a.scale;
+    if (a.scale < 0.f)  // (scores are multiplied by what is not negative: the largest stays the largest)
+#pragma unroll
+      for (int p = 0; p < KP; ++p) q[t][p] ^= F32 ? 0x80000000u : 0x80008000u;
+  }
+  const float to_log2 = fabsf(a.scale) * AT_LOG2E;
+  const int row_bytes = dh * E;
+  const int32_t *tab = a.table + it.r * a.ldt;
+  const int n_blocks = (int)(((unsigned)(k_end - k_first) + KEYS - 1u) / KEYS), mine = n_blocks > wave ? (n_blocks - wave + WAVES - 1) / WAVES : 0;
+  // Where the tiles lie: FAST: lane i holds byte offset and number of keys of tile i of the next 64 of this wave; else lane j < KEYS the offset of key j of the block, -1: none.
+  unsigned off_lo = 0, off_hi = 0;
+  int n_keys = 0;
+  auto place = [&](long long key) {  // byte offset of the key's row, -1: not in a page
+    const int block = (int)key / a.page, pg = tab[block];
+    return (unsigned)pg < (unsigned)a.n_pages ? (((long long)pg * a.Hkv + h) * a.page + ((int)key - block * a.page)) * row_bytes : -1ll;
+  };
+  auto look_up = [&](int i) {  // for block i of this wave
+    if (FAST ? i % (64 / TILES) == 0 : true) {
+      const long long key = FAST ? k_first + (long long)KEYS * (wave + (long long)WAVES * (i + lane / TILES)) + 16 * (lane % TILES)
+                                 : k_first + (long long)KEYS * (wave + (long long)WAVES * i) + lane;
+      long long at = -1;
+      if (key < k_end && (FAST || lane < KEYS)) at = place(key);
+      off_lo = (unsigned)at;
+      off_hi = (unsigned)(at >> 32);
+      if (FAST) n_keys = at < 0 ? 0 : k_end - key < 16 ? (int)(k_end - key) : 16;
     }
-    float m = s;
-    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
-    m = fmaxf(m, m_run);
-    const float base = m > -INFINITY ? m : 0.f, f = expf(m_run - base), p = seen ? expf(s - base) : 0.f;
-    m_run = m;
-    float sum = p;
-    for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, 64);
-    l = l * f + sum;
-    for (int x = 0; x < 4; ++x) o[x] *= f;
-    for (int t = 0; t < 64; ++t) {
-      const int s_t = __shfl((int)seen, t, 64);
-      const float p_t = __shfl(p, t, 64);
-      const long long at_t = __shfl(at, t, 64);
-      if (!s_t) continue;
-      for (int x = 0; x < 4; ++x)
-        if (lane + 64 * x < a.dh) o[x] += p_t * load_as_float<T>((const T *)a.V + at_t + lane + 64 * x);
+  };
+  at_u4 kr[TILES][KP];
+  unsigned vr[VK][VH][VW / 4];
+  const char *kb = (const char *)a.K, *vb = (const char *)a.V;
+  unsigned seen = 0;  // bit j: key j of the block is in a page
+  long long tile_at[TILES];  // FAST
+  auto locate = [&](int i) {
+    seen = 0;
+    if constexpr (FAST) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const int l = i % (64 / TILES) * TILES + t, n = __builtin_amdgcn_readlane(n_keys, l);
+        const long long at = (long long)(unsigned)__builtin_amdgcn_readlane((int)off_lo, l) | (long long)__builtin_amdgcn_readlane((int)off_hi, l) << 32;
+        seen |= ((1u << n) - 1u) << (16 * t);
+        tile_at[t] = n > 0 ? at : 0;
+      }
+    } else {
+      seen = (unsigned)__ballot((int)off_hi >= 0) & (F32 ? 0xffffu : 0xffffffffu);
+    }
+  };
+  // (a key that is not seen is read as the first row of all: its score and its V are replaced)
+  auto key_at = [&](int j) {
+    const unsigned lo = __shfl((int)off_lo, j, 64), hi = __shfl((int)off_hi, j, 64);
+    return (int)hi < 0 ? 0ll : (long long)lo | (long long)hi << 32;
+  };
+  auto load_k = [&]() {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const bool in = FAST ? (seen >> (16 * t + c16)) & 1u : true;
+      const char *p = kb + (FAST ? tile_at[t] + (unsigned)((in ? c16 : 0) * row_bytes) : key_at(16 * t + c16));
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        const int at = 64 * i + 16 * q4;
+        const bool there = FAST || at < row_bytes;
+        kr[t][i] = *(const at_u4 *)(p + (there ? at : 0));
+        if (!there) kr[t][i] = at_u4{0, 0, 0, 0};
+      }
+    }
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int j = 0; j < VK; ++j) {
+      const int t = j >> 2, key = 4 * q4 + (j & 3);
+      const bool in = (seen >> (16 * t + key)) & 1u;
+      const char *p = vb + (FAST ? tile_at[t] + (unsigned)((in ? key : 0) * row_bytes) : key_at(16 * t + key));
+#pragma unroll
+      for (int u = 0; u < VH; ++u) {
+        const int at = 16 * VW * u + VW * c16;
+        const char *from = p + (FAST || at < row_bytes ? at : 0);  // (channels behind the row's end are never stored)
+        if constexpr (VW == 16) *(at_u4 *)vr[j][u] = *(const at_u4 *)from;
+        else *(at_u2 *)vr[j][u] = *(const at_u2 *)from;
+      }
+    }
+  };
+  at_f4 o[NT][DT];
+  float m_run[NT], l_run[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = at_f4{0.f, 0.f, 0.f, 0.f};
+    m_run[t] = -INFINITY;
+    l_run[t] = 0.f;
+  }
+  if (mine > 0) {
+    look_up(0);
+    locate(0);
+    load_k();
+    load_v();
+  }
+  unsigned long long odd_rows = 0;  // drafted rows, of those whose keys this wave has, whose V has an infinity or NaN
+  constexpr unsigned ALL = F32 ? 0xffffu : 0xffffffffu;
+  for (int i = 0; i < mine; ++i) {
+    const unsigned now = seen;
+    const int key0 = k_first + KEYS * (wave + WAVES * i);
+    const bool drafted = (long long)key0 + KEYS > L;  // keys of the request's own rows among them
+    at_f4 s[NT][TILES];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) s[n][t] = at_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[t][k][e]), __uint_as_float(q[n][k][e]), s[n][t], 0, 0, 0);
+          } else {
+            s[n][t] = at_mma<T>(kr[t][k], q[n][k], s[n][t]);
+          }
+        }
+    float factor = to_log2;
+    unsigned odd = 0;  // such keys of the block
+    if (drafted || now != ALL) {
+      factor = 1.f;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        unsigned mask = now;  // keys that the column sees
+        if (drafted) {
+          const int c = tile * 16 * NT + (16 * n + c16 < cols ? 16 * n + c16 : 0);
+          const unsigned long long vis = a.vis[first + c / g];
+          const int at = key0 - L;  // of the block's first key in the request's rows
+          mask &= at >= 0 ? (at < 64 ? (unsigned)(vis >> at) : 0u) : (unsigned)(vis << -at) | ((1u << -at) - 1u);  // (at > -KEYS)
+        }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + 4 * q4 + e) & 1u ? s[n][t][e] * to_log2 : -INFINITY;
+      }
+      if (drafted) {
+#pragma unroll
+        for (int j = 0; j < VK; ++j) {
+          bool any = false;
+#pragma unroll
+          for (int u = 0; u < VH; ++u)
+#pragma unroll
+            for (int w = 0; w < VW / 4; ++w) any = any || ((FAST || 16 * VW * u + VW * c16 < row_bytes) && ta_odd<T>(vr[j][u][w]));
+          const unsigned long long lanes = __ballot(any);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) odd |= (lanes >> (16 * x) & 0xffff) != 0 ? 1u << (16 * (j >> 2) + 4 * x + (j & 3)) : 0u;
+        }
+        odd &= now;
+        const int committed = L - key0;  // (their infinities are seen by every row that sees anything)
+        if (committed > 0) odd &= ~((1u << committed) - 1u);  // (< KEYS)
+        odd_rows |= committed > 0 ? (unsigned long long)odd >> committed : (unsigned long long)odd << -committed;
+      }
+      const unsigned zero = ~now | odd;
+#pragma unroll
+      for (int j = 0; j < VK; ++j)
+        if (zero >> (16 * (j >> 2) + 4 * q4 + (j & 3)) & 1u)
+#pragma unroll
+          for (int u = 0; u < VH; ++u)
+#pragma unroll
+            for (int w = 0; w < VW / 4; ++w) vr[j][u][w] = 0u;
+    }
+    if (i + 1 < mine) {
+      look_up(i + 1);
+      locate(i + 1);
+      load_k();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[n][t][e]);
+      mx *= factor;
+      if (__any(mx > m_run[n] + LAZY)) {
+        const float m_new = fmaxf(m_run[n], at_max4(mx)), corr = __builtin_amdgcn_exp2f(m_run[n] - (m_new > -INFINITY ? m_new : 0.f));
+        m_run[n] = m_new;
+        l_run[n] *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[n][d] *= corr;
+      }
+      const float base = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[n][t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][e], factor, base));
+          l_run[n] += s[n][t][e];
+        }
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int u = 0; u < VH; ++u)
+#pragma unroll
+          for (int w = 0; w < VC; ++w)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][u * VC + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[e][u][w]), s[n][0][e], o[n][u * VC + w], 0, 0, 0);
+    } else {
+      at_u4 p[NT], rest[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const at_u2 both = ta_split<T>(s[n][j / 2 % TILES][2 * (j & 1)], s[n][j / 2 % TILES][2 * (j & 1) + 1]);
+          p[n][j] = both[0];
+          rest[n][j] = both[1];
+        }
+#pragma unroll
+      for (int u = 0; u < VH; ++u)
+#pragma unroll
+        for (int w = 0; w < VW / 4; ++w) {
+          at_u4 v[2];
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              v[half][j] = __builtin_amdgcn_perm(vr[(2 * j + 1) % VK][u][w], vr[2 * j % VK][u][w], half ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][u * VC + 2 * w + half] = at_mma<T>(v[half], p[n], o[n][u * VC + 2 * w + half]);
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][u * VC + 2 * w + half] = at_mma<T>(v[half], rest[n], o[n][u * VC + 2 * w + half]);
+        }
+    }
+    if (i + 1 < mine) load_v();
+  }
+  // Those V's, which the products took as zeros (a weight of zero would have made NaN of them in every column), for the columns that see them alone.
+  for (; odd_rows; odd_rows &= odd_rows - 1) {
+    const int row = __builtin_ctzll(odd_rows);
+    const long long at = place((long long)L + row);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int c = tile * 16 * NT + (16 * n + c16 < cols ? 16 * n + c16 : 0);
+      float dot = 0.f;
+#pragma unroll
+      for (int p = 0; p < KP; ++p) {
+        const int b = 64 * p + 16 * q4;
+        const at_u4 k = *(const at_u4 *)(kb + at + (FAST || b < row_bytes ? b : 0));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {  // (q's pieces behind the row's end are zeros; what K has in their place is no number of its own)
+          if (!FAST && b >= row_bytes) continue;
+          const unsigned x = q[n][p][w], y = k[w];
+          if constexpr (F32) dot += __uint_as_float(x) * __uint_as_float(y);
+          else dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
+        }
+      }
+      const float base = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base));
+      if (!(a.vis[first + c / g] >> row & 1u)) continue;
+#pragma unroll
+      for (int u = 0; u < VH; ++u)
+#pragma unroll
+        for (int w = 0; w < VC; ++w)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int ch = 16 * VC * u + VC * (4 * q4 + y) + w;
+            if (FAST || ch < dh) o[n][u * VC + w][y] += p * load_as_float<T>((const T *)(vb + at) + ch);
+          }
     }
   }
-  for (int x = 0; x < 4; ++x)
-    if (lane + 64 * x < a.dh) store_from_float<T>((T *)a.out + i * a.ldo + (int64_t)head * a.dh + lane + 64 * x, l > 0.f || l != l ? o[x] / l : 0.f);
+  // The waves' sums meet in LDS, 16 columns and a part of 16 VC channels at a time: [wave][column][channels + 4], and in front of them [wave][column] offset and sum; a thread adds the waves'
+  // sums of four channels, in order.  Output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w.
+  constexpr int PART = 16 * VC, PITCH = PART + 4, QUADS = PART / 4;
+  float *stat = at_lds, *sums = at_lds + 2 * WAVES * AT_ROWS;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int columns = cols - 16 * n < 16 ? cols - 16 * n : 16;
+    const float l = at_sum4(l_run[n]) * (1.f + TA_REST<T>);
+#pragma unroll
+    for (int u = 0; u < VH; ++u) {
+      if (columns <= 0) continue;
+      if (n + u > 0) __syncthreads();
+      if (u == 0 && q4 == 0) {
+        stat[2 * (wave * AT_ROWS + c16)] = m_run[n];
+        stat[2 * (wave * AT_ROWS + c16) + 1] = l;
+      }
+      if (c16 < columns) {
+        float *to = sums + (size_t)(wave * AT_ROWS + c16) * PITCH;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int w = 0; w < VC; w += 4) {
+            at_f4 v;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] = o[n][u * VC + w + x][e];
+            *(at_f4 *)(to + VC * (4 * q4 + e) + w) = v;
+          }
+      }
+      __syncthreads();
+      for (int x = threadIdx.x; x < columns * QUADS; x += 64 * WAVES) {
+        const int col = x / QUADS, at = 4 * (x - col * QUADS), ch = PART * u + at, c = 16 * (tile * NT + n) + col, j = c / g, head = h * g + c - j * g;
+        if (!FAST && ch >= dh) continue;
+        float m = stat[2 * col];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, stat[2 * (w * AT_ROWS + col)]);
+        const float base = m > -INFINITY ? m : 0.f;
+        float sum = 0.f;
+        at_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+          const float f = __builtin_amdgcn_exp2f(stat[2 * (w * AT_ROWS + col)] - base);
+          sum += stat[2 * (w * AT_ROWS + col) + 1] * f;
+          y += *(const at_f4 *)(sums + (size_t)(w * AT_ROWS + col) * PITCH + at) * f;
+        }
+        if (it.count > 1) {
+          float *to = a.part + (((size_t)it.record * a.Hq + head) * a.max_rows + j) * a.rec;
+          if (u == 0 && at == 0) *(float2 *)to = float2{m, sum};
+          *(at_f4 *)(to + 4 + ch) = y;
+          continue;
+        }
+        y *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;  // (nothing seen: zeros)
+        if (a.vis[first + j] == 0) y = at_f4{0.f, 0.f, 0.f, 0.f};
+        if (a.kind != AT_OUT_ROWS) {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) at_store_row(a, first + j, head * dh + ch + z, y[z]);
+        } else {
+          T *to = (T *)a.out + (first + j) * a.ldo + (int64_t)head * dh + ch;
+          if constexpr (F32) *(at_f4 *)to = y;
+          else *(at_u2 *)to = at_u2{at_pack<T>(y[0], y[1]), at_pack<T>(y[2], y[3])};
+        }
+      }
+    }
+  }
+}
+
+// The items of a request's row and query head, in item order: a wave each, a lane takes up to four channels.
+constexpr int TA_JOIN_WAVES = 4;
+template <typename T>
+__global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAttend a) {
+  const AtItem it = at_find<true, true>(a, (int)(blockIdx.x / a.max_rows));
+  if (it.count < 2) return;
+  const int lane = threadIdx.x & 63, head = uniform((int)(blockIdx.y * TA_JOIN_WAVES + (threadIdx.x >> 6))), j = uniform((int)(blockIdx.x % a.max_rows));
+  int first;
+  const int n_rows = tree_rows(a, it.b, first);
+  if (j >= n_rows || head >= a.Hq) return;
+  const int record = it.record - it.index;
+  const size_t step = (size_t)a.Hq * a.max_rows * a.rec;
+  const float *rec = a.part + (((size_t)record * a.Hq + head) * a.max_rows + j) * a.rec;
+  const int parts = (a.dh + 63) / 64;
+  const bool sees = a.vis[first + j] != 0;
+  float top = -INFINITY;
+  for (int i = lane; i < it.count; i += 64) top = fmaxf(top, rec[i * step]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float base = top > -INFINITY ? top : 0.f;
+  float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int N = 4;
+  for (int i0 = 0; i0 < it.count; i0 += N) {
+    float v[N][4], m[N], s[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float *p = rec + (i0 + k < it.count ? i0 + k : 0) * step;
+      m[k] = p[0];
+      s[k] = p[1];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[k][c] = c < parts ? p[4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float f = i0 + k < it.count ? __builtin_amdgcn_exp2f(m[k] - base) : 0.f;
+      if (!(f > 0.f || f != f)) continue;
+      l += s[k] * f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] += v[k][c] * f;
+    }
+  }
+  const float inv = sees && (l > 0.f || l != l) ? 1.f / l : 0.f;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int ch = lane + 64 * c;
+    if (ch >= a.dh) continue;
+    const float y = sees ? acc[c] * inv : 0.f;
+    if (a.kind != AT_OUT_ROWS) {
+      at_store_row(a, first + j, head * a.dh + ch, y);
+      continue;
+    }
+    T *to = (T *)a.out + (first + j) * a.ldo + (int64_t)head * a.dh + ch;
+    if constexpr (sizeof(T) == 4) *to = y;
+    else *(uint16_t *)to = (uint16_t)at_pack<T>(y, 0.f);
+  }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------
+struct TreePlan {
+  int nt, tiles, target, items;
+  size_t list, bytes;
+};
+static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
+  TreePlan r{};
+  const int columns = Hq / p.n_kv_heads * max_rows;
+  const int most = p.dtype == LA_F32 ? (p.head_dim <= 128 ? 2 : 1) : p.head_dim <= 128 ? 4 : 2;
+  r.nt = columns <= 16 || most == 1 ? 1 : columns <= 32 || most == 2 ? 2 : 4;
+  r.tiles = ceil_div(columns, 16 * r.nt);
+  const long long cap = (long long)max_blocks * p.page_size;
+  r.items = R;
+  if (cap > AT_WHOLE) {
+    const int target = (r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles);
+    r.target = target > 1 ? target : 1;
+    const long long cut = (2 * R > r.target ? (long long)AT_FINE : 1) * r.target + R, pieces = R * ((cap + AT_PIECE - 1) / AT_PIECE);
+    r.items = (int)std::min(cut, pieces);
+    const long long records = std::min((long long)r.items, 2ll * AT_FINE * r.target);
+    r.bytes = (size_t)records * Hq * max_rows * (p.head_dim + 4) * 4;
+    if (R > 64) {
+      r.list = r.bytes;
+      r.bytes += r.items * sizeof(AtItem) + (size_t)R * 4;
+    }
+  }
+  return r;
+}
+
+template <typename T, int DH, int NT, bool FAST>
+static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
+  constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
+  constexpr int LDS = (2 * TA_WAVES * AT_ROWS + TA_WAVES * AT_ROWS * (16 * VC + 4)) * 4;
+  if (a.list) {
+    ProfScope ps("tree_plan", s);
+    paged_plan_kernel<true><<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
+  }
+  {
+    ProfScope ps("tree_attend", s);
+    tree_attend_kernel<T, DH, NT, FAST><<<(unsigned)(plan.items * a.Hkv * a.tiles), 64 * TA_WAVES, LDS, s>>>(a);
+  }
+  if (plan.target > 0) {
+    ProfScope ps("tree_join", s);
+    tree_join_kernel<T><<<dim3((unsigned)a.B * a.max_rows, ceil_div(a.Hq, TA_JOIN_WAVES)), 64 * TA_JOIN_WAVES, 0, s>>>(a);
+  }
+  LA_HIP(hipGetLastError());
+  return LA_OK;
+}
+template <typename T, int DH, int NT>
+static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (a.dh == DH && a.page % 16 == 0) return ta_launch<T, DH, NT, true>(a, plan, s);
+  return ta_launch<T, DH, NT, false>(a, plan, s);
+}
+template <typename T, int DH>
+static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
+  constexpr int MOST = sizeof(T) == 4 ? (DH <= 128 ? 2 : 1) : DH <= 128 ? 4 : 2;
+  if constexpr (MOST >= 4)
+    if (plan.nt == 4) return ta_launch<T, DH, 4>(a, plan, s);
+  if constexpr (MOST >= 2)
+    if (plan.nt == 2) return ta_launch<T, DH, 2>(a, plan, s);
+  return ta_launch<T, DH, 1>(a, plan, s);
+}
+template <typename T>
+static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
+  if (a.dh <= 64) return ta_launch<T, 64>(a, plan, s);
+  if (a.dh <= 128) return ta_launch<T, 128>(a, plan, s);
+  return ta_launch<T, 256>(a, plan, s);
+}
+static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) {
+  a.target = plan.target;
+  a.tiles = plan.tiles;
+  a.rec = a.dh + 4;
+  if (plan.list) {
+    a.list = (AtItem *)((char *)a.part + plan.list);
+    a.firsts = (int32_t *)(a.list + plan.items);
+  }
+  if (dtype == LA_F32) return ta_launch<float>(a, plan, s);
+  if (dtype == LA_F16) return ta_launch<_Float16>(a, plan, s);
+  return ta_launch<uint16_t>(a, plan, s);
 }
 
 }  // namespace la
@@ -82,7 +596,7 @@ using namespace la;
 
 extern "C" size_t la_paged_tree_attend_workspace(const la_pages_desc *pages, int n_q_heads, int max_blocks, int n_requests, int max_rows) {
   if (check_pages(pages, 0) || n_q_heads < 1 || n_q_heads % pages->n_kv_heads || max_blocks < 1 || n_requests < 1 || max_rows < 1 || max_rows > LA_MAX_ROWS) return 0;
-  return 0;
+  return ta_plan(*pages, n_q_heads, max_blocks, n_requests, max_rows).bytes;
 }
 
 extern "C" int la_paged_tree_attend(const la_pages_desc *pages, int layer, const void *q, int64_t q_stride, int n_q_heads, float scale, const int32_t *table, int64_t table_stride,
@@ -103,16 +617,16 @@ extern "C" int la_paged_tree_attend(const la_pages_desc *pages, int layer, const
   LA_REQUIRE(aligned16({q, out}) && q_stride * e % 16 == 0 && out_stride * e % 16 == 0, LA_EINVAL, "q and out rows must be 16-byte aligned");
   LA_REQUIRE((uintptr_t)vis % 8 == 0, LA_EINVAL, "vis must be 8-byte aligned");
   LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
-  (void)workspace, (void)workspace_bytes;
+  const TreePlan plan = ta_plan(p, n_q_heads, max_blocks, n_requests, max_rows);
+  LA_REQUIRE((long long)plan.items * p.n_kv_heads * plan.tiles < 1ll << 24 && (long long)n_requests * max_rows * ceil_div(n_q_heads, TA_JOIN_WAVES) < 1ll << 24, LA_EINVAL,
+             "%d requests of %d rows and %d heads are more than one launch takes", n_requests, max_rows, n_q_heads);  // (2^32 threads)
+  LA_REQUIRE(workspace_bytes >= plan.bytes && (workspace || !plan.bytes), LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
+  LA_REQUIRE(aligned16({workspace}), LA_EINVAL, "workspace must be 16-byte aligned");
   hipStream_t s = (hipStream_t)stream;
   const size_t at = layer * layer_bytes(&p);
-  const TreeAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride,
-                     n_requests, max_blocks, first, len, vis, max_rows, B, out, out_stride};
-  ProfScope ps("tree_attend", s);
-  const dim3 grid(B, n_q_heads);
-  if (p.dtype == LA_F32) tree_attend_simple_kernel<float><<<grid, 64, 0, s>>>(a);
-  else if (p.dtype == LA_F16) tree_attend_simple_kernel<_Float16><<<grid, 64, 0, s>>>(a);
-  else tree_attend_simple_kernel<uint16_t><<<grid, 64, 0, s>>>(a);
-  LA_HIP(hipGetLastError());
-  return LA_OK;
+  TreeAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, q_stride, n_q_heads, scale, table, table_stride, n_requests,
+               max_blocks, first, len, vis, max_rows, B, out, out_stride};
+  a.kind = AT_OUT_ROWS;
+  a.part = (float *)workspace;
+  return ta_run(a, p.dtype, plan, s);
 }
