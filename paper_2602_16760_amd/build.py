@@ -16,7 +16,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liblookahead.so")
 
 SOURCES = ["la_api.hip", "la_generic.hip", "la_accept.hip", "la_mfma.hip", "la_paged.hip", "la_attend.hip", "la_sample.hip",
-           "la_tree.hip", "la_tree_attend.hip", "la_adjust.hip",
+           "la_tree.hip", "la_tree_attend.hip", "la_tree_wide.hip", "la_adjust.hip",
            "la_stack_mt1.hip", "la_stack_mt2.hip", "la_stack_mt3.hip", "la_stack_mt4.hip",
            "la_rstack_mt1.hip", "la_rstack_mt2.hip", "la_rstack_mt3.hip", "la_rstack_mt4.hip"]
 FLAGS = [

@@ -1,0 +1,113 @@
+// What the kernels of the trees' attention share: their arguments, the requests' rows, how weights are formed and split.
+#pragma once
+#include "la_attend.h"
+
+namespace la {
+
+struct TreeAttend {
+  const void *K, *V;  // of the layer
+  int n_pages, page, Hkv, dh;
+  const void *q;
+  int64_t ldq;
+  int Hq;
+  float scale;
+  const int32_t *table;
+  int64_t ldt;
+  int B, max_blocks;  // requests
+  const int32_t *first, *len;
+  const uint64_t *vis;
+  int max_rows, N;  // rows of a request at most, of all
+  void *out;
+  int64_t ldo;
+  int target, tiles, items;  // as at_plan has them
+  int q_tiles, kind;  // as la_paged_attend's
+  int rec;            // floats of a row's and head's record of an item
+  float *part;        // [record][Hq][max_rows][rec]
+  AtItem *list;
+  int32_t *firsts;
+};
+
+// A request's rows: the first one's number, and how many take part.
+__device__ __forceinline__ int tree_rows(const TreeAttend &a, int r, int &f) {
+  f = a.first[r];
+  const int e = a.first[r + 1], n = (e < a.N ? e : a.N) - f;
+  return f < 0 || n < 0 ? 0 : n < a.max_rows ? n : a.max_rows;
+}
+__device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
+  int f;
+  r = b;
+  const int rows = tree_rows(a, b, f);
+  const long long L = a.len[b], n = L + rows, cap = (long long)a.max_blocks * a.page;
+  return rows == 0 || L < 0 ? 0 : (int)(n < cap ? n : cap);
+}
+
+// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled; weights are up to 2^LAZY then, and half
+// precision's carry 2^UP instead of 2^15.
+template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 4.f : 8.f;
+template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 11.f : 0.f;
+// Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
+// infinite V stays one).  The factor is the same for all weights and goes out with their sum.
+template <typename T> constexpr float TA_REST = std::is_same<T, _Float16>::value ? 0x1p-10f : sizeof(T) == 2 ? 0x1p-12f : 0.f;
+template <typename T>
+__device__ __forceinline__ at_u2 ta_split(float x, float y) {
+  if constexpr (std::is_same<T, _Float16>::value) {
+    const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
+    return at_u2{__builtin_bit_cast(unsigned, cut), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), __builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1]))};
+  } else {
+    const unsigned u = __float_as_uint(x), v = __float_as_uint(y);
+    return at_u2{__builtin_amdgcn_perm(v, u, 0x07060302u), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -__uint_as_float(u & 0xffff0000u)),
+                                                                      __builtin_fmaf(y, 1.f + TA_REST<T>, -__uint_as_float(v & 0xffff0000u)))};
+  }
+}
+template <typename T>
+__device__ __forceinline__ float ta_half(unsigned v, int hi) {
+  const uint16_t bits = (uint16_t)(v >> (16 * hi));
+  if constexpr (std::is_same<T, _Float16>::value) return (float)__builtin_bit_cast(_Float16, bits);
+  else return bf16_to_float(bits);
+}
+template <typename T>
+__device__ __forceinline__ bool ta_odd(unsigned v) {  // an infinity or NaN among a word's numbers
+  if constexpr (sizeof(T) == 4) return (v & 0x7f800000u) == 0x7f800000u;
+  constexpr unsigned E = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
+  return (v & E) == E || (v >> 16 & E) == E;
+}
+
+// Zeros for rows that see nothing: those of no request, and a request's behind the ones that take part.
+template <typename T>
+__device__ __forceinline__ void ta_zero(const TreeAttend &a, long long i, int col0, int cols, int t, int threads) {
+  for (int c = t; c < cols; c += threads) {
+    if (a.kind != AT_OUT_ROWS) at_store_row(a, (int)i, col0 + c, 0.f);
+    else ((T *)a.out)[i * a.ldo + col0 + c] = T(0);
+  }
+}
+
+// Rows of no request, over the whole launch; a request's rows behind the ones that take part.
+template <typename T>
+__device__ __forceinline__ void ta_zero_outside(const TreeAttend &a, int threads) {
+  const long long front = a.first[0], back = a.first[a.B];
+  for (long long i = (back > 0 ? back : 0) + blockIdx.x; i < a.N; i += gridDim.x) ta_zero<T>(a, i, 0, a.Hq * a.dh, threadIdx.x, threads);
+  for (long long i = blockIdx.x; i < (front < a.N ? front : a.N); i += gridDim.x) ta_zero<T>(a, i, 0, a.Hq * a.dh, threadIdx.x, threads);
+}
+template <typename T>
+__device__ __forceinline__ void ta_zero_behind(const TreeAttend &a, int b, int first, int n_rows, int col0, int cols, int threads) {
+  const long long end = a.first[b + 1];
+  for (long long i = (long long)first + n_rows; first >= 0 && i < (end < a.N ? end : a.N); ++i) ta_zero<T>(a, i, col0, cols, threadIdx.x, threads);
+}
+// The item, kv head and tile of columns of a workgroup (item -1: none).  The tiles of one item and head read the same keys: they go to one XCD, eight workgroups apart.
+__device__ __forceinline__ void ta_share(const TreeAttend &a, int block, int &item, int &h, int &tile) {
+  const int turn = block / 8, group = a.tiles > 1 ? turn / a.tiles * 8 + block % 8 : block;
+  tile = uniform(a.tiles > 1 ? turn % a.tiles : 0);
+  item = uniform(group / a.Hkv);
+  h = uniform(group - item * a.Hkv);
+  if (item >= a.items) item = -1;
+}
+
+// The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 16 positions, head_dim of 64, 128 or 256.
+struct TreeWide {
+  int columns;  // of a workgroup; 0: it is not for this shape
+  int groups;   // of them resident at once
+};
+TreeWide tree_wide(int dtype, int head_dim, int page_size, int columns);
+int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s);
+
+}  // namespace la

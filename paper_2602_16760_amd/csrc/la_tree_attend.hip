@@ -1,87 +1,11 @@
 // Attention of trees of drafted tokens over the pages of their requests (la_paged_tree_attend).
 #include <algorithm>
 
-#include "la_attend.h"
+#include "la_tree.h"
 
 namespace la {
 
-struct TreeAttend {
-  const void *K, *V;  // of the layer
-  int n_pages, page, Hkv, dh;
-  const void *q;
-  int64_t ldq;
-  int Hq;
-  float scale;
-  const int32_t *table;
-  int64_t ldt;
-  int B, max_blocks;  // requests
-  const int32_t *first, *len;
-  const uint64_t *vis;
-  int max_rows, N;  // rows of a request at most, of all
-  void *out;
-  int64_t ldo;
-  int target, tiles;  // as at_plan has them
-  int q_tiles, kind;  // as la_paged_attend's
-  int rec;            // floats of a row's and head's record of an item
-  float *part;        // [record][Hq][max_rows][rec]
-  AtItem *list;
-  int32_t *firsts;
-};
-
-// A request's rows: the first one's number, and how many take part.
-__device__ __forceinline__ int tree_rows(const TreeAttend &a, int r, int &f) {
-  f = a.first[r];
-  const int e = a.first[r + 1], n = (e < a.N ? e : a.N) - f;
-  return f < 0 || n < 0 ? 0 : n < a.max_rows ? n : a.max_rows;
-}
-__device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
-  int f;
-  r = b;
-  const int rows = tree_rows(a, b, f);
-  const long long L = a.len[b], n = L + rows, cap = (long long)a.max_blocks * a.page;
-  return rows == 0 || L < 0 ? 0 : (int)(n < cap ? n : cap);
-}
-
 constexpr int TA_WAVES = 4;
-// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled; weights are up to 2^LAZY then, and half
-// precision's carry 2^UP instead of 2^15.
-template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 4.f : 8.f;
-template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 11.f : 0.f;
-// Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
-// infinite V stays one).  The factor is the same for all weights and goes out with their sum.
-template <typename T> constexpr float TA_REST = std::is_same<T, _Float16>::value ? 0x1p-10f : sizeof(T) == 2 ? 0x1p-12f : 0.f;
-template <typename T>
-__device__ __forceinline__ at_u2 ta_split(float x, float y) {
-  if constexpr (std::is_same<T, _Float16>::value) {
-    const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
-    return at_u2{__builtin_bit_cast(unsigned, cut), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), __builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1]))};
-  } else {
-    const unsigned u = __float_as_uint(x), v = __float_as_uint(y);
-    return at_u2{__builtin_amdgcn_perm(v, u, 0x07060302u), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -__uint_as_float(u & 0xffff0000u)),
-                                                                      __builtin_fmaf(y, 1.f + TA_REST<T>, -__uint_as_float(v & 0xffff0000u)))};
-  }
-}
-template <typename T>
-__device__ __forceinline__ float ta_half(unsigned v, int hi) {
-  const uint16_t bits = (uint16_t)(v >> (16 * hi));
-  if constexpr (std::is_same<T, _Float16>::value) return (float)__builtin_bit_cast(_Float16, bits);
-  else return bf16_to_float(bits);
-}
-template <typename T>
-__device__ __forceinline__ bool ta_odd(unsigned v) {  // an infinity or NaN among a word's numbers
-  if constexpr (sizeof(T) == 4) return (v & 0x7f800000u) == 0x7f800000u;
-  constexpr unsigned E = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
-  return (v & E) == E || (v >> 16 & E) == E;
-}
-
-// Zeros for rows that see nothing: those of no request, and a request's behind the ones that take part.
-template <typename T>
-__device__ __forceinline__ void ta_zero(const TreeAttend &a, long long i, int col0, int cols, int t, int threads) {
-  for (int c = t; c < cols; c += threads) {
-    if (a.kind != AT_OUT_ROWS) at_store_row(a, (int)i, col0 + c, 0.f);
-    else ((T *)a.out)[i * a.ldo + col0 + c] = T(0);
-  }
-}
 
 // A workgroup takes an item's keys for one kv head and 16 NT of its columns; column c of a kv head is query head c % g of the request's row c / g, so that those of a block of few rows lie
 // together.  The waves take blocks of KEYS keys in turn and meet once, at the end.  Products, types and pages as in la_attend.hip, K and V of a block go through the matrix instructions NT times.
@@ -98,16 +22,16 @@ __global__ __launch_bounds__(64 * TA_WAVES) void tree_attend_kernel(TreeAttend a
   constexpr float UP = TA_UP<T>, LAZY = TA_LAZY<T>;
   extern __shared__ __attribute__((aligned(16))) float at_lds[];
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, q4 = lane >> 4, c16 = lane & 15;
-  const int g = uniform(a.Hq / a.Hkv), item = uniform((int)blockIdx.x / (a.Hkv * a.tiles)), share = (int)blockIdx.x - item * a.Hkv * a.tiles;
-  const int h = uniform(share / a.tiles), tile = uniform(share % a.tiles), dh = FAST ? DH : a.dh;
-  for (long long i = (long long)max(a.first[a.B], 0) + blockIdx.x; i < a.N; i += gridDim.x) ta_zero<T>(a, i, 0, a.Hq * dh, threadIdx.x, 64 * WAVES);
-  for (long long i = blockIdx.x; i < min(a.first[0], a.N); i += gridDim.x) ta_zero<T>(a, i, 0, a.Hq * dh, threadIdx.x, 64 * WAVES);
+  const int g = uniform(a.Hq / a.Hkv), dh = FAST ? DH : a.dh;
+  int item, h, tile;
+  ta_share(a, (int)blockIdx.x, item, h, tile);
+  ta_zero_outside<T>(a, 64 * WAVES);
+  if (item < 0) return;
   const AtItem it = at_find<false, true>(a, item);
   if (it.b < 0) return;  // (all waves)
   int f0;
   const int n_rows = uniform(tree_rows(a, it.b, f0)), first = uniform(f0), L = uniform(a.len[it.b]);
-  if (it.index == 0 && tile == 0)
-    for (long long i = first + n_rows; first >= 0 && i < min(a.first[it.b + 1], a.N); ++i) ta_zero<T>(a, i, h * g * dh, g * dh, threadIdx.x, 64 * WAVES);
+  if (it.index == 0 && tile == 0) ta_zero_behind<T>(a, it.b, first, n_rows, h * g * dh, g * dh, 64 * WAVES);
   const int cols = n_rows * g - tile * 16 * NT;  // of this workgroup, if it had room for all
   if (cols <= 0) return;
   const int k_first = it.index * it.C, k_end = at_item_end(it);  // (C is a multiple of the block)
@@ -511,19 +435,21 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 
 // ---- host side ------------------------------------------------------------------------------------------
 struct TreePlan {
-  int nt, tiles, target, items;
+  int wide, nt, tiles, target, items;
+  unsigned grid;
   size_t list, bytes;
 };
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   TreePlan r{};
   const int columns = Hq / p.n_kv_heads * max_rows;
-  const int most = p.dtype == LA_F32 ? (p.head_dim <= 128 ? 2 : 1) : p.head_dim <= 128 ? 4 : 2;
-  r.nt = columns <= 16 || most == 1 ? 1 : columns <= 32 || most == 2 ? 2 : 4;
-  r.tiles = ceil_div(columns, 16 * r.nt);
+  const TreeWide w = tree_wide(p.dtype, p.head_dim, p.page_size, columns);
+  r.wide = w.columns;
+  r.nt = columns <= 16 || p.head_dim > 128 ? 1 : 2;
+  r.tiles = ceil_div(columns, w.columns ? w.columns : 16 * r.nt);
   const long long cap = (long long)max_blocks * p.page_size;
   r.items = R;
   if (cap > AT_WHOLE) {
-    const int target = (r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles);
+    const int target = (w.columns ? w.groups : r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles);
     r.target = target > 1 ? target : 1;
     const long long cut = (2 * R > r.target ? (long long)AT_FINE : 1) * r.target + R, pieces = R * ((cap + AT_PIECE - 1) / AT_PIECE);
     r.items = (int)std::min(cut, pieces);
@@ -534,6 +460,8 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
       r.bytes += r.items * sizeof(AtItem) + (size_t)R * 4;
     }
   }
+  const long long groups = (long long)r.items * p.n_kv_heads, grid = r.tiles > 1 ? (groups + 7) / 8 * 8 * r.tiles : groups;
+  r.grid = grid < 1ll << 24 ? (unsigned)grid : 1u << 24;
   return r;
 }
 
@@ -541,19 +469,10 @@ template <typename T, int DH, int NT, bool FAST>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
   constexpr int LDS = (2 * TA_WAVES * AT_ROWS + TA_WAVES * AT_ROWS * (16 * VC + 4)) * 4;
-  if (a.list) {
-    ProfScope ps("tree_plan", s);
-    paged_plan_kernel<true><<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
-  }
   {
     ProfScope ps("tree_attend", s);
-    tree_attend_kernel<T, DH, NT, FAST><<<(unsigned)(plan.items * a.Hkv * a.tiles), 64 * TA_WAVES, LDS, s>>>(a);
+    tree_attend_kernel<T, DH, NT, FAST><<<plan.grid, 64 * TA_WAVES, LDS, s>>>(a);
   }
-  if (plan.target > 0) {
-    ProfScope ps("tree_join", s);
-    tree_join_kernel<T><<<dim3((unsigned)a.B * a.max_rows, ceil_div(a.Hq, TA_JOIN_WAVES)), 64 * TA_JOIN_WAVES, 0, s>>>(a);
-  }
-  LA_HIP(hipGetLastError());
   return LA_OK;
 }
 template <typename T, int DH, int NT>
@@ -564,22 +483,35 @@ static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
 }
 template <typename T, int DH>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
-  constexpr int MOST = sizeof(T) == 4 ? (DH <= 128 ? 2 : 1) : DH <= 128 ? 4 : 2;
-  if constexpr (MOST >= 4)
-    if (plan.nt == 4) return ta_launch<T, DH, 4>(a, plan, s);
-  if constexpr (MOST >= 2)
+  if constexpr (DH <= 128)
     if (plan.nt == 2) return ta_launch<T, DH, 2>(a, plan, s);
   return ta_launch<T, DH, 1>(a, plan, s);
 }
 template <typename T>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
-  if (a.dh <= 64) return ta_launch<T, 64>(a, plan, s);
-  if (a.dh <= 128) return ta_launch<T, 128>(a, plan, s);
-  return ta_launch<T, 256>(a, plan, s);
+  if (a.list) {
+    ProfScope ps("tree_plan", s);
+    paged_plan_kernel<true><<<1, AT_PLAN_THREADS, 0, s>>>(a, plan.items);
+  }
+  int rc;
+  if (plan.wide) {
+    ProfScope ps("tree_attend", s);
+    rc = tree_attend_wide(a, std::is_same<T, _Float16>::value ? LA_F16 : LA_BF16, plan.wide, plan.grid, s);
+  } else {
+    rc = a.dh <= 64 ? ta_launch<T, 64>(a, plan, s) : a.dh <= 128 ? ta_launch<T, 128>(a, plan, s) : ta_launch<T, 256>(a, plan, s);
+  }
+  if (rc) return rc;
+  if (plan.target > 0) {
+    ProfScope ps("tree_join", s);
+    tree_join_kernel<T><<<dim3((unsigned)a.B * a.max_rows, ceil_div(a.Hq, TA_JOIN_WAVES)), 64 * TA_JOIN_WAVES, 0, s>>>(a);
+  }
+  LA_HIP(hipGetLastError());
+  return LA_OK;
 }
 static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) {
   a.target = plan.target;
   a.tiles = plan.tiles;
+  a.items = plan.items;
   a.rec = a.dh + 4;
   if (plan.list) {
     a.list = (AtItem *)((char *)a.part + plan.list);
@@ -618,7 +550,7 @@ extern "C" int la_paged_tree_attend(const la_pages_desc *pages, int layer, const
   LA_REQUIRE((uintptr_t)vis % 8 == 0, LA_EINVAL, "vis must be 8-byte aligned");
   LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
   const TreePlan plan = ta_plan(p, n_q_heads, max_blocks, n_requests, max_rows);
-  LA_REQUIRE((long long)plan.items * p.n_kv_heads * plan.tiles < 1ll << 24 && (long long)n_requests * max_rows * ceil_div(n_q_heads, TA_JOIN_WAVES) < 1ll << 24, LA_EINVAL,
+  LA_REQUIRE(plan.grid < 1u << 24 && (long long)n_requests * max_rows * ceil_div(n_q_heads, TA_JOIN_WAVES) < 1ll << 24, LA_EINVAL,
              "%d requests of %d rows and %d heads are more than one launch takes", n_requests, max_rows, n_q_heads);  // (2^32 threads)
   LA_REQUIRE(workspace_bytes >= plan.bytes && (workspace || !plan.bytes), LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
   LA_REQUIRE(aligned16({workspace}), LA_EINVAL, "workspace must be 16-byte aligned");
