@@ -25,6 +25,7 @@ struct TreeAttend {
   float *part;        // [record][Hq][max_rows][rec]
   AtItem *list;
   int32_t *firsts;
+  int2 *notes;  // of each request, where any may be cut: its first record, how many items it has
 };
 
 // A request's rows: the first one's number, and how many take part.
@@ -52,7 +53,8 @@ template <typename T>
 __device__ __forceinline__ at_u2 ta_split(float x, float y) {
   if constexpr (std::is_same<T, _Float16>::value) {
     const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
-    return at_u2{__builtin_bit_cast(unsigned, cut), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), __builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1]))};
+    const auto rest = __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), __builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1]));
+    return at_u2{__builtin_bit_cast(unsigned, cut), __builtin_bit_cast(unsigned, rest)};
   } else {
     const unsigned u = __float_as_uint(x), v = __float_as_uint(y);
     return at_u2{__builtin_amdgcn_perm(v, u, 0x07060302u), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -__uint_as_float(u & 0xffff0000u)),
@@ -100,6 +102,11 @@ __device__ __forceinline__ void ta_share(const TreeAttend &a, int block, int &it
   item = uniform(group / a.Hkv);
   h = uniform(group - item * a.Hkv);
   if (item >= a.items) item = -1;
+}
+
+// What the join asks for, so that it does not form the items anew.
+__device__ __forceinline__ void ta_note(const TreeAttend &a, const AtItem &it, int h, int tile) {
+  if (a.notes && it.index == 0 && h == 0 && tile == 0 && threadIdx.x == 0) a.notes[it.b] = int2{it.record, it.count};
 }
 
 // The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 16 positions, head_dim of 64, 128 or 256.

@@ -29,6 +29,7 @@ __global__ __launch_bounds__(64 * TA_WAVES) void tree_attend_kernel(TreeAttend a
   if (item < 0) return;
   const AtItem it = at_find<false, true>(a, item);
   if (it.b < 0) return;  // (all waves)
+  ta_note(a, it, h, tile);
   int f0;
   const int n_rows = uniform(tree_rows(a, it.b, f0)), first = uniform(f0), L = uniform(a.len[it.b]);
   if (it.index == 0 && tile == 0) ta_zero_behind<T>(a, it.b, first, n_rows, h * g * dh, g * dh, 64 * WAVES);
@@ -177,10 +178,11 @@ __global__ __launch_bounds__(64 * TA_WAVES) void tree_attend_kernel(TreeAttend a
           const int at = key0 - L;  // of the block's first key in the request's rows
           mask &= at >= 0 ? (at < 64 ? (unsigned)(vis >> at) : 0u) : (unsigned)(vis << -at) | ((1u << -at) - 1u);  // (at > -KEYS)
         }
+        mask >>= 4 * q4;
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + 4 * q4 + e) & 1u ? s[n][t][e] * to_log2 : -INFINITY;
+          for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + e) & 1u ? s[n][t][e] * to_log2 : -INFINITY;
       }
       if (drafted) {
 #pragma unroll
@@ -380,29 +382,27 @@ __global__ __launch_bounds__(64 * TA_WAVES) void tree_attend_kernel(TreeAttend a
 constexpr int TA_JOIN_WAVES = 4;
 template <typename T>
 __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAttend a) {
-  const AtItem it = at_find<true, true>(a, (int)(blockIdx.x / a.max_rows));
-  if (it.count < 2) return;
-  const int lane = threadIdx.x & 63, head = uniform((int)(blockIdx.y * TA_JOIN_WAVES + (threadIdx.x >> 6))), j = uniform((int)(blockIdx.x % a.max_rows));
+  const int lane = threadIdx.x & 63, head = uniform((int)(blockIdx.y * TA_JOIN_WAVES + (threadIdx.x >> 6))), r = uniform((int)(blockIdx.x / a.max_rows)), j = (int)blockIdx.x - r * a.max_rows;
   int first;
-  const int n_rows = tree_rows(a, it.b, first);
-  if (j >= n_rows || head >= a.Hq) return;
-  const int record = it.record - it.index;
+  const int2 note = a.notes[r];
+  const int n_rows = tree_rows(a, r, first), record = note.x, count = note.y;
+  if (count < 2 || j >= n_rows || head >= a.Hq) return;
   const size_t step = (size_t)a.Hq * a.max_rows * a.rec;
   const float *rec = a.part + (((size_t)record * a.Hq + head) * a.max_rows + j) * a.rec;
   const int parts = (a.dh + 63) / 64;
   const bool sees = a.vis[first + j] != 0;
   float top = -INFINITY;
-  for (int i = lane; i < it.count; i += 64) top = fmaxf(top, rec[i * step]);
+  for (int i = lane; i < count; i += 64) top = fmaxf(top, rec[i * step]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const float base = top > -INFINITY ? top : 0.f;
   float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int N = 4;
-  for (int i0 = 0; i0 < it.count; i0 += N) {
+  for (int i0 = 0; i0 < count; i0 += N) {
     float v[N][4], m[N], s[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const float *p = rec + (i0 + k < it.count ? i0 + k : 0) * step;
+      const float *p = rec + (i0 + k < count ? i0 + k : 0) * step;
       m[k] = p[0];
       s[k] = p[1];
 #pragma unroll
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const float f = i0 + k < it.count ? __builtin_amdgcn_exp2f(m[k] - base) : 0.f;
+      const float f = i0 + k < count ? __builtin_amdgcn_exp2f(m[k] - base) : 0.f;
       if (!(f > 0.f || f != f)) continue;
       l += s[k] * f;
 #pragma unroll
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 struct TreePlan {
   int wide, nt, tiles, target, items;
   unsigned grid;
-  size_t list, bytes;
+  size_t notes, list, bytes;
 };
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   TreePlan r{};
@@ -455,6 +455,8 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
     r.items = (int)std::min(cut, pieces);
     const long long records = std::min((long long)r.items, 2ll * AT_FINE * r.target);
     r.bytes = (size_t)records * Hq * max_rows * (p.head_dim + 4) * 4;
+    r.notes = r.bytes;
+    r.bytes += ((size_t)R * sizeof(int2) + 15) / 16 * 16;
     if (R > 64) {
       r.list = r.bytes;
       r.bytes += r.items * sizeof(AtItem) + (size_t)R * 4;
@@ -513,6 +515,7 @@ static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) 
   a.tiles = plan.tiles;
   a.items = plan.items;
   a.rec = a.dh + 4;
+  a.notes = plan.target > 0 ? (int2 *)((char *)a.part + plan.notes) : nullptr;
   if (plan.list) {
     a.list = (AtItem *)((char *)a.part + plan.list);
     a.firsts = (int32_t *)(a.list + plan.items);

@@ -10,8 +10,13 @@ typedef short __attribute__((ext_vector_type(4))) tw_s4;
 template <int DH> constexpr int TW_KEYS = DH <= 128 ? 64 : 32;  // of a stage
 template <int DH> constexpr int TW_STAGE = 2 * TW_KEYS<DH> * DH * 2;
 
+// 16 bytes a lane from base + offset to LDS at `to` + 16 lane.  In assembly, as is the wait for them: the compiler does not know which LDS reads they concern, and waits for all of them in
+// front of every transposing read; what it waits for of its own loads is then waited for with them, which is safe.  No register is written but m0, which nothing else here uses; the wait states are those between a vector instruction's write of a scalar and a load that takes it.
+__device__ __forceinline__ void tw_load(unsigned to, const char *base, unsigned offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
+}
 template <int N>
-__device__ __forceinline__ void tw_wait_loads() {
+__device__ __forceinline__ void tw_wait_loads() {  // at most N of this wave's loads on their way
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 __device__ __forceinline__ void tw_wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
@@ -43,6 +48,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
   if (item < 0) return;
   const AtItem it = at_find<false, true>(a, item);
   if (it.b < 0) return;  // (all waves)
+  ta_note(a, it, h, tile);
   int f0;
   const int n_rows = uniform(tree_rows(a, it.b, f0)), first = uniform(f0), L = uniform(a.len[it.b]);
   if (it.index == 0 && tile == 0) ta_zero_behind<T>(a, it.b, first, n_rows, h * g * DH, g * DH, 64 * WAVES);
@@ -91,13 +97,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
   unsigned nx_slot = 0;
   auto request = [&]() {
     if (nx < n_stages) {
-      if (nx % WINDOW == 0) look_up(nx);
+      if (nx > 0 && nx % WINDOW == 0) look_up(nx);
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
         const int n = wave * LPW + i, l = nx % WINDOW * TILES + n % HALF_N * KPI / 16;
         const long long at = (long long)(unsigned)__builtin_amdgcn_readlane((int)off_lo, l) | (long long)__builtin_amdgcn_readlane((int)off_hi, l) << 32;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)((const char *)(n < HALF_N ? a.K : a.V) + at + voff[i]),
-                                         (LDS_AS void *)(uintptr_t)(lds0 + nx_slot + (unsigned)n * 1024u), 16, 0, 0);
+        tw_load(lds0 + nx_slot + (unsigned)n * 1024u, (const char *)(n < HALF_N ? a.K : a.V) + at, voff[i]);
       }
     }
     ++nx;
@@ -112,6 +117,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
     m_run[t] = -INFINITY;
     l_run[t] = 0.f;
   }
+  look_up(0);
+  __builtin_amdgcn_s_waitcnt(0xf70);  // (vmcnt(0): q is in, and the compiler knows it)
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i) request();
   const unsigned rd_k = (unsigned)(c16 * ROWB) + (unsigned)((q4 ^ swz_k(c16)) * 16);  // piece 4 p + q4 of key c16 of a tile: ^ 64 p
@@ -163,14 +170,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int t = 0; t < TILES; ++t) s[n][t] = at_f4{0.f, 0.f, 0.f, 0.f};
+    {
+      at_u4 kf[2][TILES];
+      auto read_k = [&](int k) {
 #pragma unroll
-    for (int k = 0; k < KP; ++k)
+        for (int t = 0; t < TILES; ++t) kf[k & 1][t] = *(LDS_AS const at_u4 *)(uintptr_t)((base + (rd_k ^ (unsigned)(64 * k))) + (unsigned)(16 * t * ROWB));
+      };
+      read_k(0);
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        const at_u4 kf = *(LDS_AS const at_u4 *)(uintptr_t)((base + (rd_k ^ (unsigned)(64 * k))) + (unsigned)(16 * t * ROWB));
+      for (int k = 0; k < KP; ++k) {
+        if (k + 1 < KP) read_k(k + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][t] = at_mma<T>(kf, q[n][k], s[n][t]);
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) s[n][t] = at_mma<T>(kf[k & 1][t], q[n][k], s[n][t]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
     float factor = to_log2;
     if (now != ALL || drafted) {
       factor = 1.f;
@@ -183,10 +200,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
           const int at = key0 - L;  // of the stage's first key in the request's rows
           mask &= at >= 0 ? (at < 64 ? vis >> at : 0ull) : vis << -at | ((1ull << -at) - 1);  // (at > -KEYS)
         }
+        mask >>= 4 * q4;
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + 4 * q4 + e) & 1 ? s[n][t][e] * to_log2 : -INFINITY;
+          for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + e) & 1 ? s[n][t][e] * to_log2 : -INFINITY;
       }
     }
     at_u4 p[NT][TILES / 2], rest[NT][TILES / 2];
@@ -221,19 +239,36 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
         rest[n][t / 2][2 * (t & 1) + 1] = y[1];
       }
     }
+    {
+      constexpr int DG = 4, GROUPS = TILES / 2 * DT / DG;  // V's fragments of four tiles of channels at a time, the next ones on their way
+      at_u4 vf[2][DG];
+      auto read_v = [&](int x) {
+        const int m = x * DG / DT, d0 = x * DG % DT;
 #pragma unroll
-    for (int m = 0; m < TILES / 2; ++m)
+        for (int y = 0; y < DG; ++y) {
+          const unsigned at = base + (rd_v ^ (unsigned)(32 * (d0 + y))) + (unsigned)(32 * m * ROWB);
+          const at_u2 lo = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)at));
+          const at_u2 hi = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + 16u * ROWB)));
+          vf[x & 1][y] = at_u4{lo[0], lo[1], hi[0], hi[1]};
+        }
+      };
+      read_v(0);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const unsigned at = base + (rd_v ^ (unsigned)(32 * d)) + (unsigned)(32 * m * ROWB);
-        const tw_s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + 16u * ROWB));
-        const at_u2 lo2 = __builtin_bit_cast(at_u2, lo), hi2 = __builtin_bit_cast(at_u2, hi);
-        const at_u4 v = {lo2[0], lo2[1], hi2[0], hi2[1]};
+      for (int x = 0; x < GROUPS; ++x) {
+        const int m = x * DG / DT, d0 = x * DG % DT;
+        if (x + 1 < GROUPS) read_v(x + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) o[n][d] = at_mma<T>(v, p[n][m], o[n][d]);
+        for (int y = 0; y < DG; ++y)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) o[n][d] = at_mma<T>(v, rest[n][m], o[n][d]);
+          for (int n = 0; n < NT; ++n) o[n][d0 + y] = at_mma<T>(vf[x & 1][y], p[n][m], o[n][d0 + y]);
+#pragma unroll
+        for (int y = 0; y < DG; ++y)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) o[n][d0 + y] = at_mma<T>(vf[x & 1][y], rest[n][m], o[n][d0 + y]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
   }
   if (cols <= 0) return;
   // Those V's, which the products took as zeros (a weight of zero would have made NaN of them in every column), for the columns that see them alone.
@@ -300,9 +335,8 @@ static int tw_launch(const TreeAttend &a, unsigned grid, hipStream_t s) {
 template <typename T, int DH>
 static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_t s) {
   if (columns == 64) return tw_launch<T, DH, 4, 1, DH == 64 ? 4 : 2>(a, grid, s);
-  if constexpr (DH <= 128)
-    if (columns == 256) return tw_launch<T, DH, 8, 2, 4>(a, grid, s);
-  return tw_launch<T, DH, 8, 1, 4>(a, grid, s);
+  if constexpr (DH <= 128) return columns == 256 ? tw_launch<T, DH, 8, 2, 4>(a, grid, s) : tw_launch<T, DH, 4, 2, DH == 64 ? 4 : 2>(a, grid, s);
+  else return tw_launch<T, DH, 8, 1, 4>(a, grid, s);
 }
 template <typename T>
 static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_t s) {
@@ -314,7 +348,7 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
 TreeWide tree_wide(int dtype, int head_dim, int page_size, int columns) {
   if (dtype == LA_F32 || page_size % 16 || columns <= 32 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return {0, 0};
   const int n = columns <= 64 ? 64 : columns <= 128 || head_dim > 128 ? 128 : 256;
-  return {n, n == 64 ? 512 : 256};
+  return {n, n == 256 || (head_dim > 128 && n == 128) ? 256 : 512};
 }
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s) {
   return dtype == LA_F16 ? tw_launch<_Float16>(a, columns, grid, s) : tw_launch<uint16_t>(a, columns, grid, s);
