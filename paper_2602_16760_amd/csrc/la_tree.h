@@ -1,5 +1,7 @@
 // What the kernels of the trees' attention share: their arguments, the requests' rows, how weights are formed and split.
 #pragma once
+#include <atomic>
+
 #include "la_attend.h"
 
 namespace la {
@@ -109,12 +111,21 @@ __device__ __forceinline__ void ta_note(const TreeAttend &a, const AtItem &it, i
   if (a.notes && it.index == 0 && h == 0 && tile == 0 && threadIdx.x == 0) a.notes[it.b] = int2{it.record, it.count};
 }
 
+// A kernel's right to more LDS than 64 KB, asked for once a device.
+template <auto KERNEL>
+int ta_allow_lds(int bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int device = 0;
+  LA_HIP(hipGetDevice(&device));
+  const unsigned long long bit = 1ull << (device & 63);
+  if (done.load(std::memory_order_relaxed) & bit) return LA_OK;
+  LA_HIP(hipFuncSetAttribute((const void *)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return LA_OK;
+}
+
 // The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 16 positions, head_dim of 64, 128 or 256.
-struct TreeWide {
-  int columns;  // of a workgroup; 0: it is not for this shape
-  int groups;   // of them resident at once
-};
-TreeWide tree_wide(int dtype, int head_dim, int page_size, int columns);
+int tree_wide(int dtype, int head_dim, int page_size, int columns);  // columns of a workgroup; 0: it is not for this shape
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s);
 
 }  // namespace la

@@ -5,14 +5,14 @@
 
 namespace la {
 
-constexpr int TA_WAVES = 4;
+constexpr int TA_WAVES = 4, TA_WHOLE_WAVES = 8;  // of a workgroup; where requests are not cut and workgroups are few
 
 // A workgroup takes an item's keys for one kv head and 16 NT of its columns; column c of a kv head is query head c % g of the request's row c / g, so that those of a block of few rows lie
 // together.  The waves take blocks of KEYS keys in turn and meet once, at the end.  Products, types and pages as in la_attend.hip, K and V of a block go through the matrix instructions NT times.
-template <typename T, int DH, int NT, bool FAST>
-__global__ __launch_bounds__(64 * TA_WAVES) void tree_attend_kernel(TreeAttend a) {
+template <typename T, int DH, int NT, bool FAST, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES, WAVES = TA_WAVES;
+  constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES;
   constexpr int KP = DH * E / 64;                  // 16-byte pieces of a key row per lane (four lanes a row)
   constexpr int VW = DH * E / 16 < 16 ? 8 : 16;    // bytes of a V load: a row's share of each of 16 lanes, at most 16
   constexpr int VH = DH * E / 16 / VW;             // such loads a row
@@ -391,27 +391,29 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
   const float *rec = a.part + (((size_t)record * a.Hq + head) * a.max_rows + j) * a.rec;
   const int parts = (a.dh + 63) / 64;
   const bool sees = a.vis[first + j] != 0;
-  float top = -INFINITY;
-  for (int i = lane; i < count; i += 64) top = fmaxf(top, rec[i * step]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  const float base = top > -INFINITY ? top : 0.f;
-  float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int N = 4;
   for (int i0 = 0; i0 < count; i0 += N) {
-    float v[N][4], m[N], s[N];
+    float v[N][4], m[N], s[N], most = top;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const float *p = rec + (i0 + k < count ? i0 + k : 0) * step;
+      const float *p = rec + (i0 + k < count ? i0 + k : i0) * step;
       m[k] = p[0];
       s[k] = p[1];
 #pragma unroll
       for (int c = 0; c < 4; ++c) v[k][c] = c < parts ? p[4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)] : 0.f;
     }
 #pragma unroll
+    for (int k = 0; k < N; ++k) most = fmaxf(most, m[k]);
+    const float base = most > -INFINITY ? most : 0.f, corr = __builtin_amdgcn_exp2f(top - base);
+    top = most;
+    l *= corr;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] *= corr;
+#pragma unroll
     for (int k = 0; k < N; ++k) {
       const float f = i0 + k < count ? __builtin_amdgcn_exp2f(m[k] - base) : 0.f;
-      if (!(f > 0.f || f != f)) continue;
+      if (!(f > 0.f || f != f)) continue;  // (an item that the row sees nothing of)
       l += s[k] * f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) acc[c] += v[k][c] * f;
@@ -434,22 +436,28 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 }
 
 // ---- host side ------------------------------------------------------------------------------------------
+constexpr int TA_FEW = 256, TA_WHOLE_WIDE = 256;
 struct TreePlan {
-  int wide, nt, tiles, target, items;
+  int wide, nt, waves, tiles, target, items;
   unsigned grid;
   size_t notes, list, bytes;
 };
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   TreePlan r{};
   const int columns = Hq / p.n_kv_heads * max_rows;
-  const TreeWide w = tree_wide(p.dtype, p.head_dim, p.page_size, columns);
-  r.wide = w.columns;
+  r.wide = tree_wide(p.dtype, p.head_dim, p.page_size, columns);
   r.nt = columns <= 16 || p.head_dim > 128 ? 1 : 2;
-  r.tiles = ceil_div(columns, w.columns ? w.columns : 16 * r.nt);
+  r.waves = TA_WAVES;
+  const bool whole = (long long)max_blocks * p.page_size <= (r.wide ? TA_WHOLE_WIDE : AT_WHOLE);
+  if (!r.wide && whole && p.head_dim <= 128 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW) {
+    r.nt = 1;
+    r.waves = TA_WHOLE_WAVES;
+  }
+  r.tiles = ceil_div(columns, r.wide ? r.wide : 16 * r.nt);
   const long long cap = (long long)max_blocks * p.page_size;
   r.items = R;
-  if (cap > AT_WHOLE) {
-    const int target = (w.columns ? w.groups : r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles);
+  if (!whole) {
+    const int target = (!r.wide && r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles);
     r.target = target > 1 ? target : 1;
     const long long cut = (2 * R > r.target ? (long long)AT_FINE : 1) * r.target + R, pieces = R * ((cap + AT_PIECE - 1) / AT_PIECE);
     r.items = (int)std::min(cut, pieces);
@@ -467,27 +475,28 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
   return r;
 }
 
-template <typename T, int DH, int NT, bool FAST>
+template <typename T, int DH, int NT, bool FAST, int WAVES>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
-  constexpr int LDS = (2 * TA_WAVES * AT_ROWS + TA_WAVES * AT_ROWS * (16 * VC + 4)) * 4;
-  {
-    ProfScope ps("tree_attend", s);
-    tree_attend_kernel<T, DH, NT, FAST><<<plan.grid, 64 * TA_WAVES, LDS, s>>>(a);
-  }
+  constexpr int LDS = (2 * WAVES * AT_ROWS + WAVES * AT_ROWS * (16 * VC + 4)) * 4;
+  if constexpr (LDS > 64 * 1024)
+    if (const int rc = ta_allow_lds<tree_attend_kernel<T, DH, NT, FAST, WAVES>>(LDS)) return rc;
+  tree_attend_kernel<T, DH, NT, FAST, WAVES><<<plan.grid, 64 * WAVES, LDS, s>>>(a);
   return LA_OK;
 }
-template <typename T, int DH, int NT>
+template <typename T, int DH, int NT, int WAVES>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
-    if (a.dh == DH && a.page % 16 == 0) return ta_launch<T, DH, NT, true>(a, plan, s);
-  return ta_launch<T, DH, NT, false>(a, plan, s);
+    if (a.dh == DH && a.page % 16 == 0) return ta_launch<T, DH, NT, true, WAVES>(a, plan, s);
+  return ta_launch<T, DH, NT, false, WAVES>(a, plan, s);
 }
 template <typename T, int DH>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
-  if constexpr (DH <= 128)
-    if (plan.nt == 2) return ta_launch<T, DH, 2>(a, plan, s);
-  return ta_launch<T, DH, 1>(a, plan, s);
+  if constexpr (DH <= 128) {
+    if (plan.nt == 2) return ta_launch<T, DH, 2, TA_WAVES>(a, plan, s);
+    if (plan.waves == TA_WHOLE_WAVES) return ta_launch<T, DH, 1, TA_WHOLE_WAVES>(a, plan, s);
+  }
+  return ta_launch<T, DH, 1, TA_WAVES>(a, plan, s);
 }
 template <typename T>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
@@ -500,6 +509,7 @@ static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
     ProfScope ps("tree_attend", s);
     rc = tree_attend_wide(a, std::is_same<T, _Float16>::value ? LA_F16 : LA_BF16, plan.wide, plan.grid, s);
   } else {
+    ProfScope ps("tree_attend", s);
     rc = a.dh <= 64 ? ta_launch<T, 64>(a, plan, s) : a.dh <= 128 ? ta_launch<T, 128>(a, plan, s) : ta_launch<T, 256>(a, plan, s);
   }
   if (rc) return rc;

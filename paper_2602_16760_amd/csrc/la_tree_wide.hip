@@ -328,7 +328,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
 template <typename T, int DH, int WAVES, int NT, int NS>
 static int tw_launch(const TreeAttend &a, unsigned grid, hipStream_t s) {
   constexpr int LDS = NS * TW_STAGE<DH> + 16;
-  if constexpr (LDS > 64 * 1024) LA_HIP(hipFuncSetAttribute((const void *)tree_wide_kernel<T, DH, WAVES, NT, NS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+  if constexpr (LDS > 64 * 1024)
+    if (const int rc = ta_allow_lds<tree_wide_kernel<T, DH, WAVES, NT, NS>>(LDS)) return rc;
   tree_wide_kernel<T, DH, WAVES, NT, NS><<<grid, 64 * WAVES, LDS, s>>>(a);
   return LA_OK;
 }
@@ -345,10 +346,9 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
   return tw_launch<T, 256>(a, columns, grid, s);
 }
 
-TreeWide tree_wide(int dtype, int head_dim, int page_size, int columns) {
-  if (dtype == LA_F32 || page_size % 16 || columns <= 32 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return {0, 0};
-  const int n = columns <= 64 ? 64 : columns <= 128 || head_dim > 128 ? 128 : 256;
-  return {n, n == 256 || (head_dim > 128 && n == 128) ? 256 : 512};
+int tree_wide(int dtype, int head_dim, int page_size, int columns) {
+  if (dtype == LA_F32 || page_size % 16 || columns <= 32 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
+  return columns <= 64 ? 64 : columns <= 128 || head_dim > 128 ? 128 : 256;
 }
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s) {
   return dtype == LA_F16 ? tw_launch<_Float16>(a, columns, grid, s) : tw_launch<uint16_t>(a, columns, grid, s);
