@@ -396,6 +396,13 @@ int la_paged_tree_attend(const la_pages_desc *pages, int layer, const void *q, i
                          int n_requests, int max_blocks, const int32_t *first, const int32_t *len, const uint64_t *vis, int max_rows, int B, void *out, int64_t out_stride,
                          void *workspace, size_t workspace_bytes, void *stream);
 
+/* Runs rows of the requests' blocks, up to LA_MAX_ROWS of them together, through layers [layer_begin, layer_end), in place, as la_forward_paged runs single tokens: the rows' K and V go to
+ * slot[i] (la_page_map's; negative: not written), and la_paged_tree_attend is the attention.  pos, vis: as la_tree_layout leaves them; first, len, max_rows: as there.
+ * hidden, pages and the model's rules as for la_forward_paged; the model's first call of this allocates scratch memory of its own too (up to 64 MB, more where a row's heads are very many).
+ * LA_EINVAL: as there, n_requests above LA_MAX_ROWS, max_rows outside 1..LA_MAX_ROWS; LA_ERANGE; LA_ENOMEM. */
+int la_forward_tree(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const uint64_t *vis, const int32_t *slot, const int32_t *first,
+                    const int32_t *len, int max_rows, const la_pages_desc *pages, const int32_t *table, int64_t table_stride, int n_requests, int max_blocks, void *stream);
+
 /* What a step commits.  From row 0 on the path goes to the first row whose parent is the present one and whose tok is what the present one chose (ids >= 0), until there is none or it has
  * max_path rows, or limit[r] (NULL: no limit).  parent, tok, ids, slot: int32 [B], len, limit: int32 [R].  Of every request:
  *   n_new      tokens committed: one for each of the path's rows (a last row whose ids is negative commits none; 0 where the request has no row, or limit <= 0)

@@ -79,7 +79,7 @@ EXPORTS = [
     "la_kv_fill", "la_kv_read", "la_free_kv", "la_embed", "la_forward_layers", "la_unembed_argmax",
     "la_unembed_argmax_noalloc", "la_unembed_logits", "la_sample", "la_sample_workspace", "la_page_map", "la_paged_write", "la_paged_attend",
     "la_paged_attend_workspace", "la_forward_paged", "la_paged_copy", "la_tree_layout", "la_paged_tree_attend", "la_paged_tree_attend_workspace",
-    "la_tree_accept", "la_logits_adjust", "la_causal_layout", "la_set_barrier_timeout",
+    "la_forward_tree", "la_tree_accept", "la_logits_adjust", "la_causal_layout", "la_set_barrier_timeout",
     "la_prefill", "la_jacobi_init", "la_jacobi_accept", "la_rtt_fixed_overhead", "la_rtt_project", "la_jacobi_project",
     "la_pool_alloc", "la_free_pool", "la_state_init", "la_ngram_accept", "la_lookahead_layout",
     "la_profile_enable", "la_profile_select", "la_profile_read", "la_profile_copy", "la_last_error",
@@ -119,6 +119,7 @@ def _load():
         "la_tree_layout": (i32, [vp, vp, vp, i32, i32, vp, vp, vp]),
         "la_paged_tree_attend_workspace": (C.c_size_t, [vp, i32, i32, i32, i32]),
         "la_paged_tree_attend": (i32, [vp, i32, vp, i64, i32, f32, vp, i64, i32, i32, vp, vp, vp, i32, i32, vp, i64, vp, C.c_size_t, vp]),
+        "la_forward_tree": (i32, [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, i64, i32, i32, vp]),
         "la_tree_accept": (i32, [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
         "la_logits_adjust": (i32, [vp, i32, i64, i32, i32, vp, vp, i64, vp]),
         "la_pool_alloc": (i32, [i32, i32, i32, C.POINTER(vp)]),
@@ -538,6 +539,17 @@ def la_forward_paged(model, layer_begin, layer_end, hidden, pos, req, slot, page
     tp, ld, R, blocks = _table(table, device)
     _check(lib.la_forward_paged(model, layer_begin, layer_end, _array(hidden, "hidden", _F32, (n[0], model.d_model), device), n[0], _array(pos, "pos", _I32, n, device), _optional(req, "req", _I32, n, device),
                                 _array(slot, "slot", _I32, n, device), pages.ref, tp, ld, R, blocks, _stream(stream)))
+
+
+def la_forward_tree(model, layer_begin, layer_end, hidden, pos, vis, slot, first, len, max_rows, pages, table, stream=None):
+    """Rows of the requests' blocks through the layers: hidden float32 [B, d_model] in place, pos, slot int32 [B], vis int64 [B], first int32 [R + 1], len int32 [R]; max_rows: rows of a request
+    at most."""
+    device = pages._here()
+    n = (hidden.shape[0],)
+    tp, ld, R, blocks = _table(table, device)
+    _check(lib.la_forward_tree(model, layer_begin, layer_end, _array(hidden, "hidden", _F32, (n[0], model.d_model), device), n[0], _array(pos, "pos", _I32, n, device),
+                               _array(vis, "vis", _I64, n, device), _array(slot, "slot", _I32, n, device), _array(first, "first", _I32, (R + 1,), device), _array(len, "len", _I32, (R,), device),
+                               max_rows, pages.ref, tp, ld, R, blocks, _stream(stream)))
 
 
 def la_pool_alloc(vocab, N, G):

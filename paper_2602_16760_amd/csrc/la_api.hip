@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <new>
 
@@ -281,7 +282,7 @@ extern "C" void la_free_model(la_model *m) {
       if (p) (void)hipFree(p);
   }
   void *ps[] = {m->embed, m->unembed, m->g_final, m->qkv, m->attn, m->act, m->logits, m->rope_cs, m->err_dev,
-                m->pf_hidden, m->pf_pos, m->pf_vis, m->prompt, m->paged, m->zero_len};
+                m->pf_hidden, m->pf_pos, m->pf_vis, m->prompt, m->paged, m->tree, m->zero_len};
   for (void *p : ps)
     if (p) (void)hipFree(p);
   if (m->err_host) (void)hipHostFree(m->err_host);
@@ -549,11 +550,22 @@ extern "C" int la_forward_layers(la_model *m, int layer_begin, int layer_end, fl
   return generic_forward(m, layer_begin, layer_end, hidden, Bp, pos, vis, kv, s);
 }
 
-extern "C" int la_forward_paged(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const int32_t *req, const int32_t *slot,
-                                const la_pages_desc *pages, const int32_t *table, int64_t table_stride, int n_requests, int max_blocks, void *stream) {
-  LA_REQUIRE(m && hidden && pos && slot && table, LA_EINVAL, "NULL argument");
+// Scratch memory that comes with a model's first call and stays with it (the model's, not the graph's, where that call is captured).
+static int model_scratch(uint8_t **p, size_t bytes) {
+  if (!*p) {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool relaxed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+    *p = (uint8_t *)dev_alloc(bytes);
+    if (!*p) (void)hipGetLastError();
+    if (relaxed) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  }
+  LA_REQUIRE(*p, LA_ENOMEM, "device allocation failed");
+  return LA_OK;
+}
+
+static int forward_rows(la_model *m, int layer_begin, int layer_end, float *hidden, const PagedRows &r, const la_pages_desc *pages, hipStream_t s) {
   LA_PENDING(m);
-  LA_REQUIRE(B >= 1 && B <= LA_MAX_ROWS, LA_EINVAL, "B=%d outside [1, %d]", B, LA_MAX_ROWS);
+  LA_REQUIRE(r.B >= 1 && r.B <= LA_MAX_ROWS, LA_EINVAL, "B=%d outside [1, %d]", r.B, LA_MAX_ROWS);
   LA_REQUIRE(layer_begin >= 0 && layer_begin <= layer_end && layer_end <= m->d.n_layers, LA_ERANGE, "layers [%d, %d) outside the model's %d layers", layer_begin, layer_end,
              m->d.n_layers);
   if (layer_begin == layer_end) return LA_OK;
@@ -561,27 +573,35 @@ extern "C" int la_forward_paged(la_model *m, int layer_begin, int layer_end, flo
   const la_model_desc &d = m->d;
   LA_REQUIRE(pages->n_kv_heads == d.n_kv_heads && pages->head_dim == d.head_dim && pages->dtype == d.dtype, LA_EINVAL, "pages of %d heads of %d, type %d, for a model of %d of %d, type %d",
              pages->n_kv_heads, pages->head_dim, pages->dtype, d.n_kv_heads, d.head_dim, d.dtype);
-  LA_REQUIRE(n_requests >= 1 && max_blocks >= 1 && (table_stride >= max_blocks || n_requests == 1), LA_EINVAL, "bad table dimensions");
-  LA_REQUIRE((long long)max_blocks * pages->page_size < (1ll << 31), LA_EINVAL, "%d blocks of %d positions: positions are 32-bit numbers", max_blocks, pages->page_size);
-  LA_REQUIRE(req || B <= n_requests, LA_EINVAL, "%d rows for %d requests and no row map", B, n_requests);
+  LA_REQUIRE(r.n_req >= 1 && r.max_blocks >= 1 && (r.ldt >= r.max_blocks || r.n_req == 1), LA_EINVAL, "bad table dimensions");
+  LA_REQUIRE((long long)r.max_blocks * pages->page_size < (1ll << 31), LA_EINVAL, "%d blocks of %d positions: positions are 32-bit numbers", r.max_blocks, pages->page_size);
+  LA_REQUIRE(r.req || r.first || r.B <= r.n_req, LA_EINVAL, "%d rows for %d requests and no row map", r.B, r.n_req);
+  LA_REQUIRE(!r.first || (r.n_req <= LA_MAX_ROWS && r.max_rows >= 1 && r.max_rows <= LA_MAX_ROWS), LA_EINVAL, "%d requests of %d rows, each at most %d", r.n_req, r.max_rows, LA_MAX_ROWS);
   LA_REQUIRE((uintptr_t)hidden % 16 == 0, LA_EINVAL, "hidden must be 16-byte aligned");
   for (int l = layer_begin; l < layer_end; ++l) LA_REQUIRE(m->layers[l].set, LA_EINVAL, "layer %d has no weights", l);
   // scratch of LA_MAX_ROWS rows: q (plain path), or K and V as the QKV product leaves them (both no more than this), and the attention's workspace
   const size_t rows = (size_t)LA_MAX_ROWS * (m->use_mfma ? 2 * m->kvdim() : m->qdim()) * m->esize, front = (rows + 255) / 256 * 256;
-  if (!m->paged) {  // (the buffers are the model's, not the graph's, where a first call is captured)
-    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
-    const bool relaxed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
-    m->paged = (uint8_t *)dev_alloc(front + paged_attend_bytes(*pages, d.n_q_heads, LA_MAX_ROWS));
-    if (!m->paged) (void)hipGetLastError();
-    if (relaxed) (void)hipThreadExchangeStreamCaptureMode(&mode);
-  }
-  LA_REQUIRE(m->paged, LA_ENOMEM, "device allocation failed");
-  hipStream_t s = (hipStream_t)stream;
+  if (const int rc = model_scratch(&m->paged, front + paged_attend_bytes(*pages, d.n_q_heads, LA_MAX_ROWS))) return rc;
+  if (r.first && !m->tree)
+    if (const int rc = model_scratch(&m->tree, std::max((size_t)256, tree_attend_bytes(*pages, d.n_q_heads)))) return rc;
+  uint8_t *workspace = r.first ? m->tree : m->paged + front;
   if (const int rc = recover_if_needed(m, s)) return rc;
-  const PagedRows r{table, table_stride, n_requests, max_blocks, req, pos, slot, B};
-  if (m->use_mfma)
-    return mfma_forward_paged(m, layer_begin, layer_end, hidden, r, *pages, m->paged, m->paged + rows / 2, m->paged + front, s);
-  return generic_forward_paged(m, layer_begin, layer_end, hidden, r, *pages, m->paged, m->paged + front, s);
+  if (m->use_mfma) return mfma_forward_paged(m, layer_begin, layer_end, hidden, r, *pages, m->paged, m->paged + rows / 2, workspace, s);
+  return generic_forward_paged(m, layer_begin, layer_end, hidden, r, *pages, m->paged, workspace, s);
+}
+
+extern "C" int la_forward_paged(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const int32_t *req, const int32_t *slot,
+                                const la_pages_desc *pages, const int32_t *table, int64_t table_stride, int n_requests, int max_blocks, void *stream) {
+  LA_REQUIRE(m && hidden && pos && slot && table, LA_EINVAL, "NULL argument");
+  return forward_rows(m, layer_begin, layer_end, hidden, PagedRows{table, table_stride, n_requests, max_blocks, req, pos, slot, B, nullptr, nullptr, nullptr, 0}, pages, (hipStream_t)stream);
+}
+
+extern "C" int la_forward_tree(la_model *m, int layer_begin, int layer_end, float *hidden, int B, const int32_t *pos, const uint64_t *vis, const int32_t *slot, const int32_t *first,
+                               const int32_t *len, int max_rows, const la_pages_desc *pages, const int32_t *table, int64_t table_stride, int n_requests, int max_blocks, void *stream) {
+  LA_REQUIRE(m && hidden && pos && vis && slot && first && len && table, LA_EINVAL, "NULL argument");
+  LA_REQUIRE((uintptr_t)vis % 8 == 0, LA_EINVAL, "vis must be 8-byte aligned");
+  return forward_rows(m, layer_begin, layer_end, hidden, PagedRows{table, table_stride, n_requests, max_blocks, nullptr, pos, slot, B, first, len, vis, max_rows}, pages,
+                      (hipStream_t)stream);
 }
 
 extern "C" int la_unembed_argmax(la_model *m, const float *hidden, int Bp, int32_t *ids, float *top2, void *stream) {

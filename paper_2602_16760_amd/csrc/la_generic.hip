@@ -540,7 +540,7 @@ static int forward_paged_t(la_model *m, int lb, int le, float *hidden, const Pag
       rope_pages_kernel<T><<<B, 256, 0, s>>>(m->qkv, d.n_q_heads, d.n_kv_heads, d.head_dim, m->rope_cs, (T *)q, (T *)((char *)pages.k + l * layer_bytes(&pages)),
                                              (T *)((char *)pages.v + l * layer_bytes(&pages)), pages.page_size, pages.n_pages, r.slot);
     }
-    if ((rc = paged_attend_rows(pages, l, q, 0, d.n_q_heads, 1.0f / sqrtf((float)d.head_dim), r, AT_OUT_FLOAT, m->attn, workspace, s))) return rc;
+    if ((rc = (r.first ? tree_attend_rows : paged_attend_rows)(pages, l, q, 0, d.n_q_heads, 1.0f / sqrtf((float)d.head_dim), r, AT_OUT_FLOAT, m->attn, workspace, s))) return rc;
     if ((rc = gemm<T>("gemm_o", m->attn, qd, nullptr, 0.f, w.wo, dm, hidden, dm, B, qd, dm, &always, false, s))) return rc;
     if ((rc = gemm<T>("gemm_gateup", hidden, dm, w.g_mlp, d.rms_eps, w.wgu, 2 * F, m->act, F, B, dm, F, nullptr, true, s))) return rc;
     rc = gemm<T>("gemm_down", m->act, F, nullptr, 0.f, w.wdown, dm, hidden, dm, B, F, dm, &always, false, s);

@@ -67,6 +67,7 @@ struct la_model {
   uint64_t *pf_vis = nullptr;
   float *prompt = nullptr;  // generic_prefill_rows: scratch of a prompt's rows
   uint8_t *paged = nullptr;  // la_forward_paged: q rows or staged K and V rows, and the attention's workspace
+  uint8_t *tree = nullptr;   // la_forward_tree: the trees' attention's workspace
   int32_t *zero_len = nullptr;  // a cache length of 0 (plain path)
   la::MfmaModel *mf = nullptr;
   // Errors raised by kernels (a block that does not fit the cache: 1; a grid barrier that gave up: 4).  err_dev is the

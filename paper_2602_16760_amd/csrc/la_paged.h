@@ -27,8 +27,15 @@ struct PagedRows {
   int n_req, max_blocks;
   const int32_t *req, *pos, *slot;
   int B;
+  // trees (first != NULL): as la_paged_tree_attend takes them
+  const int32_t *first, *len;
+  const uint64_t *vis;
+  int max_rows;
 };
 int paged_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_tiles, int Hq, float scale, const PagedRows &r, PagedOut kind, void *out, void *workspace,
                       hipStream_t s);
+// The same of trees of up to LA_MAX_ROWS rows of as many requests together: workspace at any of their sizes; the attention.
+size_t tree_attend_bytes(const la_pages_desc &p, int Hq);
+int tree_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_tiles, int Hq, float scale, const PagedRows &r, PagedOut kind, void *out, void *workspace, hipStream_t s);
 
 }  // namespace la

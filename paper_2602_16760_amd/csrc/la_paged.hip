@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(uint4 *kp, uint4 *vp, 
 struct PagedCopy {
   uint4 *k, *v;  // of the first layer
   size_t layer;  // 16-byte pieces of one
-  int layers, Hkv, per_head, page, n_pages;
+  int layers, Hkv, per_head, page, n_pages, shift;  // shift: page_size is 2^shift, -1: no power of two
   const int32_t *from, *to;
   int n, run;
 };
@@ -192,19 +192,21 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedCopy a) {
     const bool in = j < a.run && m < a.n;
     const int s = in ? a.from[m] : -1, d = in ? a.to[m] : -1;
     const bool moves = (unsigned)s < (unsigned)n_slots && (unsigned)d < (unsigned)n_slots;
-    auto at = [&](int slot) { return (((long long)(slot / a.page) * a.Hkv + h) * a.page + slot % a.page) * a.per_head + c; };
+    auto at = [&](int slot) {
+      const int pg = a.shift >= 0 ? slot >> a.shift : slot / a.page;
+      return (((long long)pg * a.Hkv + h) * a.page + (slot - pg * a.page)) * a.per_head + c;
+    };
     src[j] = moves ? at(s) : -1;
     dst[j] = moves ? at(d) : -1;
   }
   for (int l = blockIdx.z; l < 2 * a.layers; l += gridDim.z) {
-    uint4 *p = (l & 1 ? a.v : a.k) + (l >> 1) * a.layer;
-    uint4 x[RUN];
+    typedef unsigned __attribute__((ext_vector_type(4))) piece;
+    piece *p = (piece *)((l & 1 ? a.v : a.k) + (l >> 1) * a.layer), x[RUN];
+#pragma unroll
+    for (int j = 0; j < RUN; ++j) x[j] = p[src[j] >= 0 ? src[j] : 0];  // (no condition around the loads: all are on their way at once)
 #pragma unroll
     for (int j = 0; j < RUN; ++j)
-      if (src[j] >= 0) x[j] = p[src[j]];
-#pragma unroll
-    for (int j = 0; j < RUN; ++j)
-      if (dst[j] >= 0) p[dst[j]] = x[j];
+      if (src[j] >= 0) p[dst[j]] = x[j];
   }
 }
 
@@ -278,16 +280,18 @@ extern "C" int la_paged_copy(const la_pages_desc *pages, int layer_begin, int la
   const size_t e = esize(&p);
   const int per_head = (int)(p.head_dim * e / 16);
   const long long runs = ((long long)n + run - 1) / run, wgs = (runs * per_head + 255) / 256;
-  const int layers = layer_end - layer_begin, z = std::min(2 * layers, 65535);
+  const int layers = layer_end - layer_begin, z = std::min(2 * layers, 32);
   LA_REQUIRE(wgs * p.n_kv_heads < 1ll << 24, LA_EINVAL, "%d rows of %d kv heads are more than one launch takes", n, p.n_kv_heads);
   const size_t layer = layer_bytes(&p);
   const PagedCopy a{(uint4 *)((char *)p.k + layer_begin * layer), (uint4 *)((char *)p.v + layer_begin * layer), layer / 16, layers, p.n_kv_heads, per_head, p.page_size, p.n_pages,
-                    from, to, n, run};
+                    (p.page_size & (p.page_size - 1)) == 0 ? __builtin_ctz(p.page_size) : -1, from, to, n, run};
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps("paged_copy", s);
   const dim3 grid((unsigned)wgs, p.n_kv_heads, z);
   if (run == 1) paged_copy_kernel<1><<<grid, 256, 0, s>>>(a);
+  else if (run <= 4) paged_copy_kernel<4><<<grid, 256, 0, s>>>(a);
   else if (run <= 8) paged_copy_kernel<8><<<grid, 256, 0, s>>>(a);
+  else if (run <= 16) paged_copy_kernel<16><<<grid, 256, 0, s>>>(a);
   else paged_copy_kernel<64><<<grid, 256, 0, s>>>(a);
   LA_HIP(hipGetLastError());
   return LA_OK;

@@ -1009,7 +1009,7 @@ int mfma_forward_paged(la_model *m, int lb, int le, float *hidden, const PagedRo
                                                                                       (uint16_t *)((char *)pages.v + l * layer_bytes(&pages)), r.slot, M, d.n_kv_heads,
                                                                                       d.head_dim, pages.page_size, pages.n_pages);
     }
-    if ((rc = paged_attend_rows(pages, l, b.Q, RT, d.n_q_heads, 1.f, r, AT_OUT_FRAGMENTS, b.attn, workspace, s))) return rc;
+    if ((rc = (r.first ? tree_attend_rows : paged_attend_rows)(pages, l, b.Q, RT, d.n_q_heads, 1.f, r, AT_OUT_FRAGMENTS, b.attn, workspace, s))) return rc;
     if ((rc = pf_launch_gemm<PF_PART>(args(1, b.attn), s, "pf_gemm_o", f->n_wgs, b.part_rows, &S_o))) return rc;
     if ((rc = pf_launch_norm(S_o, hidden, b.part, m->layers[l].g_mlp, M, d.d_model, RT, b.ss, b.A, s))) return rc;
     if ((rc = pf_launch_gemm<PF_GATEUP>(args(2, b.A), s, "pf_gemm_gateup", f->n_wgs))) return rc;

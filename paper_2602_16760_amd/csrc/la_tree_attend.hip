@@ -437,32 +437,41 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 
 // ---- host side ------------------------------------------------------------------------------------------
 constexpr int TA_FEW = 256, TA_WHOLE_WIDE = 256;
+constexpr size_t TA_RECORDS = (size_t)64 << 20;  // bytes of the items' records, which fewer items keep to
 struct TreePlan {
   int wide, nt, waves, tiles, target, items;
   unsigned grid;
   size_t notes, list, bytes;
 };
-static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
+// Kernel, columns of a workgroup and workgroups of an item and kv head.
+static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, bool whole) {
   TreePlan r{};
   const int columns = Hq / p.n_kv_heads * max_rows;
   r.wide = tree_wide(p.dtype, p.head_dim, p.page_size, columns);
   r.nt = columns <= 16 || p.head_dim > 128 ? 1 : 2;
   r.waves = TA_WAVES;
-  const bool whole = (long long)max_blocks * p.page_size <= (r.wide ? TA_WHOLE_WIDE : AT_WHOLE);
   if (!r.wide && whole && p.head_dim <= 128 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW) {
     r.nt = 1;
     r.waves = TA_WHOLE_WAVES;
   }
   r.tiles = ceil_div(columns, r.wide ? r.wide : 16 * r.nt);
+  return r;
+}
+static int ta_target(const TreePlan &r, const la_pages_desc &p) { return std::max(1, (!r.wide && r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles)); }
+static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   const long long cap = (long long)max_blocks * p.page_size;
+  const bool wide = tree_wide(p.dtype, p.head_dim, p.page_size, Hq / p.n_kv_heads * max_rows) != 0, whole = cap <= (wide ? TA_WHOLE_WIDE : AT_WHOLE);
+  TreePlan r = ta_shape(p, Hq, max_rows, R, whole);
   r.items = R;
   if (!whole) {
-    const int target = (!r.wide && r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles);
-    r.target = target > 1 ? target : 1;
-    const long long cut = (2 * R > r.target ? (long long)AT_FINE : 1) * r.target + R, pieces = R * ((cap + AT_PIECE - 1) / AT_PIECE);
-    r.items = (int)std::min(cut, pieces);
-    const long long records = std::min((long long)r.items, 2ll * AT_FINE * r.target);
-    r.bytes = (size_t)records * Hq * max_rows * (p.head_dim + 4) * 4;
+    const size_t record = (size_t)Hq * max_rows * (p.head_dim + 4) * 4;
+    const long long pieces = R * ((cap + AT_PIECE - 1) / AT_PIECE);
+    for (r.target = ta_target(r, p);; r.target = r.target * 3 / 4) {
+      const int cut = (2 * R > r.target ? AT_FINE : 1) * r.target;
+      r.items = (int)std::min((long long)cut + R, pieces);
+      r.bytes = std::min(r.items, 2 * cut) * record;  // (of requests that are cut: fewer than `cut`, with one item more than their share of `cut` each)
+      if (r.bytes <= TA_RECORDS || r.target == 1) break;
+    }
     r.notes = r.bytes;
     r.bytes += ((size_t)R * sizeof(int2) + 15) / 16 * 16;
     if (R > 64) {
@@ -533,6 +542,28 @@ static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) 
   if (dtype == LA_F32) return ta_launch<float>(a, plan, s);
   if (dtype == LA_F16) return ta_launch<_Float16>(a, plan, s);
   return ta_launch<uint16_t>(a, plan, s);
+}
+
+size_t tree_attend_bytes(const la_pages_desc &p, int Hq) {
+  size_t most = 0;
+  la_pages_desc d = p;
+  for (int page : {16, 17})  // (a page size that the wide kernel takes, one that it does not)
+    for (int rows = 1; rows <= LA_MAX_ROWS; ++rows) {
+      d.page_size = page;
+      const size_t record = (size_t)Hq * rows * (p.head_dim + 4) * 4;
+      most = std::max(most, std::min(2 * AT_FINE * (size_t)ta_target(ta_shape(d, Hq, rows, 1, false), d), std::max(TA_RECORDS / record, (size_t)2 * AT_FINE)) * record);
+    }
+  return most + LA_MAX_ROWS * sizeof(int2);
+}
+int tree_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_tiles, int Hq, float scale, const PagedRows &r, PagedOut kind, void *out, void *workspace, hipStream_t s) {
+  const size_t at = layer * layer_bytes(&p);
+  const int64_t ld = (int64_t)Hq * p.head_dim;
+  TreeAttend a{(const char *)p.k + at, (const char *)p.v + at, p.n_pages, p.page_size, p.n_kv_heads, p.head_dim, q, ld, Hq, scale, r.table, r.ldt, r.n_req, r.max_blocks,
+               r.first, r.len, r.vis, r.max_rows, r.B, out, ld};
+  a.q_tiles = q_tiles;
+  a.kind = kind;
+  a.part = (float *)workspace;
+  return ta_run(a, p.dtype, ta_plan(p, Hq, r.max_blocks, r.n_req, r.max_rows), s);
 }
 
 }  // namespace la
