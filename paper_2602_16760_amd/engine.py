@@ -114,9 +114,10 @@ class Engine:
         # (a row's position is below max_len + Bp: guesses reach past the last token that fits)
         self._sample = None if sampling is None else self._sampler(sampling, Bp, self.max_len + Bp)
 
-    def _sampler(self, sampling: dict, rows: int, n_u: int):
-        """choose(hidden, ids, u_index) of rows that are all sampled alike: sampling = {temperature, top_k, top_p, min_p (each may be left out), and u, the random
-        numbers, or seed}.  n_u: random numbers needed."""
+    def _sampler(self, sampling: dict, rows: int, n_u: int, requests: int = 0):
+        """choose(hidden, ids, u_index, **history) of rows that are all sampled alike: sampling = {temperature, top_k, top_p, min_p (each may be left out), and u, the random
+        numbers, or seed}.  n_u: random numbers needed.  Of `requests` whose tokens are at hand: {repetition, presence, frequency, bias} as well, with `history` what la_logits_adjust wants to
+        know of their tokens."""
         how = dict(sampling)
         u, seed = how.pop("u", None), how.pop("seed", 0)
         if u is None:
@@ -124,15 +125,27 @@ class Engine:
         u = torch.as_tensor(u, dtype=torch.float32, device="cuda").flatten().contiguous()
         if u.numel() < n_u:
             raise ValueError(f"{u.numel()} random numbers, {n_u} needed")
+        adjust = {}
+        if requests:
+            bias = how.pop("bias", None)
+            adjust = {k: torch.full((requests,), how.pop(k), dtype=torch.float32, device="cuda") for k in ("repetition", "presence", "frequency") if how.get(k) is not None}
+            if bias:
+                adjust["bias_token"] = torch.tensor([list(bias)] * requests, dtype=torch.int32, device="cuda")
+                adjust["bias"] = torch.tensor([list(bias.values())] * requests, dtype=torch.float32, device="cuda")
+            for k in ("repetition", "presence", "frequency"):
+                how.pop(k, None)
         unknown = set(how) - {"temperature", "top_k", "top_p", "min_p"}
         if unknown:
             raise TypeError(f"unknown sampling parameters {sorted(unknown)}")
         rows_of = {k: torch.full((rows,), v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in how.items() if v is not None}
         logits = torch.empty((rows, self.shape.vocab), dtype=torch.float32, device="cuda")
 
-        def choose(hidden, ids, u_index):
-            B.la_unembed_logits(self.model, hidden, logits)
-            B.la_sample(logits, u, ids, u_index=u_index, **rows_of)
+        def choose(hidden, ids, u_index, **history):
+            x = logits[:hidden.shape[0]]
+            B.la_unembed_logits(self.model, hidden, x)
+            if adjust:
+                B.la_logits_adjust(x, x, **adjust, **history)
+            B.la_sample(x, u, ids, u_index=u_index, **{k: v[:hidden.shape[0]] for k, v in rows_of.items()})
 
         return choose
 
@@ -179,76 +192,85 @@ class Engine:
     # -- several requests at once -----------------------------------------------------------------
     def generate_batch(self, prompts, n_new: int, page_size: int = 16, n_pages: int | None = None, sampling: dict | None = None):
         """Sequential generation of n_new tokens for up to 64 prompts together, a token of each per step, on a cache of pages that they share (n_pages: as many as they need if
-        left out); the contiguous cache takes one prompt after the other on its way there.  sampling: as in generate, the numbers as u[step][request].  Returns (tokens [requests, n_new], stats)."""
-        sh, R, dev = self.shape, len(prompts), "cuda"
-        prompts = [np.asarray(p, dtype=np.int32) for p in prompts]
-        if not 1 <= R <= B.LA_MAX_ROWS or any(len(p) < 1 for p in prompts):
-            raise ValueError(f"need 1 to {B.LA_MAX_ROWS} prompts of one token at least")
-        lens = [len(p) - 1 for p in prompts]
-        pages_of = lambda n: (n + page_size - 1) // page_size
-        blocks = max(1, max(pages_of(n + n_new) for n in lens))
-        need = max(1, sum(pages_of(n + n_new) for n in lens))
-        n_pages = need if n_pages is None else n_pages
-        if n_pages < need:  # (requests only grow here: what the last step needs is known)
-            raise B.LaError(-3, f"the batch needs {need} pages of {page_size} positions, there are {n_pages}")
-        i32 = lambda n, v=0: torch.full(n if isinstance(n, tuple) else (n,), v, dtype=torch.int32, device=dev)
-        dt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[sh.dtype]
-        pages = B.la_pages(*(torch.empty((sh.n_layers, n_pages, sh.n_kv_heads, page_size, sh.head_dim), dtype=dt, device=dev) for _ in range(2)))
-        table, ring = i32((R, blocks), -1), torch.arange(n_pages, dtype=torch.int32, device=dev)
-        heads, heads_out = torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=dev), i32(4)
-        old, new = i32(R), torch.tensor(lens, dtype=torch.int32, device=dev)
-
-        def mapped(rows, error=None):  # pages and slots of the lengths `new`
-            nonlocal heads, heads_out
-            slot, pos, req, first = i32(rows), i32(rows), i32(rows), i32(R + 1)
-            B.la_page_map(old, new, page_size, table, ring, heads, heads_out, slot, pos, req, first)
-            heads, heads_out = heads_out, heads
-            if error is not None:
-                torch.maximum(error, heads[3:], out=error)
-            return slot, pos, req
-
-        def check(error):
-            if int(error):
-                raise B.LaError(-3, f"the pages do not hold the batch (error {int(error)} of la_page_map; {n_pages} pages of {page_size} positions)")
-
-        # prompts one after the other through the contiguous cache, and from there into their pages
-        error = i32(1)
-        if sum(lens):
-            slot, _, _ = mapped(sum(lens), error)
-            check(error)
-            at = 0
-            for p in prompts:
-                n = len(p) - 1
-                if n:
-                    self.prefill(p[:-1])
-                    k = torch.empty((n, sh.n_kv_heads, sh.head_dim), dtype=dt, device=dev)
-                    v = torch.empty_like(k)
-                    for l in range(sh.n_layers):
-                        B.la_kv_read(self.kv, l, 0, n, k, v)
-                        B.la_paged_write(pages, l, k, v, slot[at:at + n])
-                at += n
-        choose = None if sampling is None else self._sampler(sampling, R, n_new * R)
-        which = torch.arange(R, dtype=torch.int32, device=dev)
-        hidden = torch.empty((R, sh.d_model), dtype=torch.float32, device=dev)
-        ids, tokens = torch.tensor([p[-1] for p in prompts], dtype=torch.int32, device=dev), i32((n_new, R))
+        left out); the contiguous cache takes one prompt after the other on its way there.  sampling: as in generate, the numbers as u[step][request], and {repetition, presence, frequency: of
+        the tokens of the request, bias: {token: value}}.  Returns (tokens [requests, n_new], stats)."""
+        b = _Batch(self, prompts, n_new, 0, page_size, n_pages)
+        sh, R = self.shape, b.R
+        choose = None if sampling is None else self._sampler(sampling, R, n_new * R, R)
+        which = torch.arange(R, dtype=torch.int32, device="cuda")
+        hidden = torch.empty((R, sh.d_model), dtype=torch.float32, device="cuda")
+        ids, tokens = torch.tensor([p[-1] for p in b.prompts], dtype=torch.int32, device="cuda"), b.i32((n_new, R))
+        length = b.lens.clone()
         for step in range(n_new):
-            old.copy_(new)
-            new.add_(1)
-            slot, pos, req = mapped(R, error)
+            slot, pos, req, _ = b.mapped(length, length + 1, R)
+            length = length + 1
             B.la_embed(self.model, ids, hidden)
-            B.la_forward_paged(self.model, 0, sh.n_layers, hidden, pos, req, slot, pages, table)
+            B.la_forward_paged(self.model, 0, sh.n_layers, hidden, pos, req, slot, b.pages, b.table)
             ids = tokens[step]
             if choose is None:
                 B.la_unembed_argmax(self.model, hidden, ids)
             else:
-                choose(hidden, ids, which)
+                choose(hidden, ids, which, **b.history())
+                b.append(ids[:, None], torch.ones_like(ids))
                 which = which + R
-        check(error)
-        old.copy_(new)
-        new.zero_()
-        mapped(R, error)
-        check(error)
-        return tokens.t().cpu().numpy().astype(np.int64), dict(steps=n_new, pages=n_pages, free_pages=int(heads[1]))
+        return tokens.t().cpu().numpy().astype(np.int64), dict(steps=n_new, pages=b.n_pages, free_pages=b.finish(length))
+
+    def generate_tree(self, prompts, n_new: int, draft, max_rows: int = 16, page_size: int = 16, n_pages: int | None = None, sampling: dict | None = None):
+        """generate_batch with drafted tokens: in every step a request has a tree of them behind its last token, and commits the path of those that its rows choose, and one token more.
+        draft(texts) -> for each of the texts (a request's tokens so far, a list) a pair (tokens, parents) of lists: row 1 + i of the tree is token tokens[i] behind row parents[i], 0 the text's
+        last token (a request that is through has None for its text, and what is drafted for it is not looked at).  A request has up to max_rows rows, all of them together 64; what is drafted
+        beyond that is left out.  sampling: as in generate_batch; a drafted token is committed where it is the one that the row in front draws, so the tokens are generate_batch's, but for
+        rounding (see generate).  Returns (tokens [requests, n_new], stats)."""
+        if not 1 <= max_rows <= B.LA_MAX_ROWS:
+            raise ValueError(f"max_rows={max_rows}, need 1 to {B.LA_MAX_ROWS}")
+        b = _Batch(self, prompts, n_new, max_rows, page_size, n_pages)
+        sh, R = self.shape, b.R
+        per = min(max_rows, B.LA_MAX_ROWS // R)  # rows of a request
+        choose = None if sampling is None else self._sampler(sampling, R * per, n_new * R, R)
+        texts = [[int(t) for t in p] for p in b.prompts]
+        begin = torch.tensor([len(p) for p in b.prompts], dtype=torch.int32, device="cuda")  # (the position behind which a request's first new token is: begin - 1)
+        length, steps = b.lens.clone(), 0
+        todo = [n_new] * R
+        n_tok, new_len, last = b.i32(R), b.i32(R), b.i32(R)
+        out, from_slot, to_slot = b.i32((R, per)), b.i32((R, per)), b.i32((R, per))
+        hidden = torch.empty((R * per, sh.d_model), dtype=torch.float32, device="cuda")
+        ids = b.i32(R * per)
+        while any(todo):
+            trees = draft([t if n else None for t, n in zip(texts, todo)])
+            tok, parent, rows = [], [], []
+            for text, n, (tokens, parents) in zip(texts, todo, [t or ((), ()) for t in trees]):
+                if len(tokens) != len(parents):
+                    raise ValueError(f"{len(tokens)} drafted tokens with {len(parents)} parents")
+                k = min(len(tokens), per - 1) if n else -1
+                tok += [text[-1], *tokens[:k]] if n else []
+                parent += [-1, *parents[:k]] if n else []
+                rows.append(k + 1)
+            N = len(tok)
+            both = torch.tensor([tok, parent], dtype=torch.int32).cuda()
+            grown = length + torch.tensor(rows, dtype=torch.int32).cuda()
+            slot, pos, req, first = b.mapped(length, grown, N)
+            vis = torch.empty(N, dtype=torch.int64, device="cuda")
+            B.la_tree_layout(both[1], first, length, pos, vis)
+            B.la_embed(self.model, both[0], hidden[:N])
+            B.la_forward_tree(self.model, 0, sh.n_layers, hidden[:N], pos, vis, slot, first, length, per, b.pages, b.table)
+            if choose is None:
+                B.la_unembed_argmax(self.model, hidden[:N], ids[:N])
+            else:
+                at = req.clamp(min=0)
+                choose(hidden[:N], ids[:N], (pos + 1 - begin[at.long()]) * R + at, **b.history(req, draft=both[0], first=first, vis=vis))
+            B.la_tree_accept(both[1], both[0], ids[:N], slot, first, length, n_tok, new_len, last, out, from_slot, to_slot, limit=torch.tensor(todo, dtype=torch.int32).cuda())
+            B.la_paged_copy(b.pages, from_slot, to_slot)
+            b.mapped(grown, new_len, 1)  # (the pages behind the committed path go back)
+            if choose is not None:
+                b.append(out, n_tok)
+            length = new_len.clone()
+            steps += 1
+            b.check()
+            for r, (n, t) in enumerate(zip(n_tok.tolist(), out.tolist())):
+                texts[r] += t[:n]
+                todo[r] = max(0, todo[r] - n) if n or not todo[r] else 0  # (a request that has no token to choose is through)
+        new = [t[len(p):] + [-1] * (n_new - len(t) + len(p)) for t, p in zip(texts, b.prompts)]
+        return np.array(new, dtype=np.int64).reshape(R, n_new), dict(steps=steps, pages=b.n_pages, free_pages=b.finish(length))
 
     # -- the split deployment on one GPU, with an injected round trip ---------------------------------
     def step_split(self, emitted: torch.Tensor, max_total: int, head_layers: int, tail_layers: int, rtt_ms: float):
@@ -333,3 +355,83 @@ class Engine:
             raise B.LaError(-4 if st.error & 4 else -3, f"a kernel raised error word {st.error} during generation")
         return emitted.cpu().numpy().astype(np.int64), dict(passes=st.steps, blocks=st.matched_steps, n_emitted=st.n_emitted,
                                                             L=st.L, tokens_per_pass=n_new / max(st.steps, 1))
+
+
+class _Batch:
+    """Pages, tables and lengths of a batch of requests, the prompts' K and V in them; the tokens that penalties are about."""
+
+    def __init__(self, eng, prompts, n_new, spare, page_size, n_pages):
+        sh, R = eng.shape, len(prompts)
+        self.prompts = prompts = [np.asarray(p, dtype=np.int32) for p in prompts]
+        if not 1 <= R <= B.LA_MAX_ROWS or any(len(p) < 1 for p in prompts):
+            raise ValueError(f"need 1 to {B.LA_MAX_ROWS} prompts of one token at least")
+        lens = [len(p) - 1 for p in prompts]
+        pages_of = lambda n: (n + page_size - 1) // page_size
+        blocks = max(1, max(pages_of(n + n_new + spare) for n in lens))
+        need = max(1, sum(pages_of(n + n_new + spare) for n in lens))  # (spare: rows of a step that are not committed)
+        self.n_pages = n_pages = need if n_pages is None else n_pages
+        if n_pages < need:  # (what the last step needs is known)
+            raise B.LaError(-3, f"the batch needs {need} pages of {page_size} positions, there are {n_pages}")
+        dt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[sh.dtype]
+        self.R, self.page_size = R, page_size
+        self.pages = B.la_pages(*(torch.empty((sh.n_layers, n_pages, sh.n_kv_heads, page_size, sh.head_dim), dtype=dt, device="cuda") for _ in range(2)))
+        self.table, self.ring = self.i32((R, blocks), -1), torch.arange(n_pages, dtype=torch.int32, device="cuda")
+        self.heads, self.spare_heads = torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device="cuda"), self.i32(4)
+        self.error = self.i32(1)
+        self.lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        # prompts one after the other through the contiguous cache, and from there into their pages
+        if sum(lens):
+            slot = self.mapped(self.i32(R), self.lens, sum(lens))[0]
+            self.check()
+            at = 0
+            for p in prompts:
+                n = len(p) - 1
+                if n:
+                    eng.prefill(p[:-1])
+                    k = torch.empty((n, sh.n_kv_heads, sh.head_dim), dtype=dt, device="cuda")
+                    v = torch.empty_like(k)
+                    for l in range(sh.n_layers):
+                        B.la_kv_read(eng.kv, l, 0, n, k, v)
+                        B.la_paged_write(self.pages, l, k, v, slot[at:at + n])
+                at += n
+        # all tokens: the prompts', and room for the new ones
+        self.n_prompt = self.lens + 1
+        self.n_tokens = self.n_prompt.clone()
+        self.tokens = self.i32((R, max(lens) + 1 + n_new), -1)
+        for r, p in enumerate(prompts):
+            self.tokens[r, :len(p)] = torch.from_numpy(p).cuda()
+
+    @staticmethod
+    def i32(n, v=0):
+        return torch.full(n if isinstance(n, tuple) else (n,), v, dtype=torch.int32, device="cuda")
+
+    def mapped(self, old, new, rows):
+        """Pages and slots of the lengths `new`."""
+        slot, pos, req, first = self.i32(rows), self.i32(rows), self.i32(rows), self.i32(self.R + 1)
+        B.la_page_map(old, new, self.page_size, self.table, self.ring, self.heads, self.spare_heads, slot, pos, req, first)
+        self.heads, self.spare_heads = self.spare_heads, self.heads
+        torch.maximum(self.error, self.heads[3:], out=self.error)
+        return slot, pos, req, first
+
+    def check(self):
+        if int(self.error):
+            raise B.LaError(-3, f"the pages do not hold the batch (error {int(self.error)} of la_page_map; {self.n_pages} pages of {self.page_size} positions)")
+
+    def history(self, req=None, **drafted):
+        return dict(tokens=self.tokens, n_tokens=self.n_tokens, n_prompt=self.n_prompt, req=req, **drafted)
+
+    def append(self, tokens, n):
+        """The first n[r] of tokens [R, most] behind those of request r."""
+        at = torch.arange(tokens.shape[1], device="cuda")[None]
+        room = self.tokens.shape[1]
+        to = torch.where((at < n[:, None]) & (self.n_tokens[:, None] + at < room), self.n_tokens[:, None] + at, room).long()
+        wide = torch.cat((self.tokens, self.i32((self.R, 1))), 1)
+        self.tokens = wide.scatter_(1, to, tokens)[:, :room].contiguous()
+        self.n_tokens = self.n_tokens + n
+
+    def finish(self, length):
+        """All pages go back; how many are free then."""
+        self.check()
+        self.mapped(length, torch.zeros_like(length), 1)
+        self.check()
+        return int(self.heads[1])

@@ -64,6 +64,43 @@ def test_attend_refuses(change, code):
     refused(lib.la_paged_tree_attend(*{**ATTEND, "pages": pages(), **change}.values()), code)
 
 
+def test_attend_asks_for_its_workspace():
+    size = lib.la_paged_tree_attend_workspace
+    need = size(pages(), 4, 100, 3, 8)
+    assert need > 0 and size(pages(), 4, 8, 3, 8) == 0  # (a short cache is not cut)
+    long = dict(blocks=100, ldt=100)
+    refused(lib.la_paged_tree_attend(*{**ATTEND, "pages": pages(), **long, "ws_bytes": need - 1}.values()), ENOMEM)
+    refused(lib.la_paged_tree_attend(*{**ATTEND, "pages": pages(), **long, "ws": None}.values()), ENOMEM)
+    refused(lib.la_paged_tree_attend(*{**ATTEND, "pages": pages(), **long, "ws": P + 8}.values()), EINVAL)
+    for args in ((0, 100, 3, 8), (3, 100, 3, 8), (4, 0, 3, 8), (4, 100, 0, 8), (4, 100, 3, 0), (4, 100, 3, 65)):
+        assert size(pages(), *args) == 0
+    for bad in BAD_PAGES:
+        assert size(pages(**bad), 4, 100, 3, 8) == 0
+
+
+@pytest.mark.parametrize("heads,kv,dh,dtype,page", [(32, 8, 128, B.LA_BF16, 16), (32, 8, 128, B.LA_F16, 24), (4, 2, 64, B.LA_F32, 24), (16, 1, 256, B.LA_F16, 16), (128, 1, 128, B.LA_BF16, 16), (8, 8, 64, B.LA_BF16, 64)])
+def test_attend_keeps_its_records_to_a_bound(heads, kv, dh, dtype, page):
+    """64 MB, or six items' where those are more, at any number of requests, rows and positions; and what a request and a list of items take beside them."""
+    p = pages(n_kv_heads=kv, head_dim=dh, dtype=dtype, page_size=page)
+    for rows in (1, 2, 3, 8, 16, 17, 40, 64):
+        record = heads * rows * (dh + 4) * 4
+        for R in (1, 2, 5, 17, 64, 65, 1000):
+            for blocks in (1, 20, 50, 300, 4000, 1 << 20):
+                beside = 8 * R + 16 + (0 if R <= 64 else 36 * R + 32 * 4096)
+                assert lib.la_paged_tree_attend_workspace(p, heads, blocks, R, rows) <= max(64 << 20, 6 * record) + beside
+
+
+def test_attend_takes_no_more_workgroups_than_a_launch_has():
+    call = {**ATTEND, "pages": pages(n_kv_heads=4096), "Hq": 4096, "B": 1 << 20, "n_req": 1 << 20}
+    refused(lib.la_paged_tree_attend(*call.values()), EINVAL, "more than one launch")
+    call = {**ATTEND, "pages": pages(), "B": 1 << 20, "n_req": 1 << 20, "max_rows": 64}
+    refused(lib.la_paged_tree_attend(*call.values()), EINVAL, "more than one launch")
+
+
+def test_model_calls_refuse_null():
+    refused(lib.la_forward_tree(None, 0, 1, P, 1, P, P, P, P, P, 1, pages(), P, 8, 1, 8, None), EINVAL)
+
+
 # ---- la_logits_adjust -------------------------------------------------------------------------------------
 ADJUST = dict(logits=P, dtype=B.LA_F32, ld=100, B=4, V=100, how=None, out=2 * P, ldo=100, stream=None)
 
