@@ -22,6 +22,7 @@ struct TreeAttend {
   void *out;
   int64_t ldo;
   int target, tiles, items;  // as at_plan has them
+  int uncut;          // keys up to which no request is cut
   int q_tiles, kind;  // as la_paged_attend's
   int rec;            // floats of a row's and head's record of an item
   float *part;        // [record][Hq][max_rows][rec]
@@ -48,6 +49,8 @@ __device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
 // precision's carry 2^UP instead of 2^15.
 template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 4.f : 8.f;
 template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 11.f : 0.f;
+__device__ __forceinline__ int whole(const TreeAttend &a) { return a.uncut; }
+
 // Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
 // infinite V stays one).  The factor is the same for all weights and goes out with their sum.
 template <typename T> constexpr float TA_REST = std::is_same<T, _Float16>::value ? 0x1p-10f : sizeof(T) == 2 ? 0x1p-12f : 0.f;

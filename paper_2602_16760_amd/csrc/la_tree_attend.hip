@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
 
 // The items of a request's row and query head, in item order: a wave each, a lane takes up to four channels.
 constexpr int TA_JOIN_WAVES = 4;
-template <typename T>
+template <typename T, int PARTS>
 __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAttend a) {
   const int lane = threadIdx.x & 63, head = uniform((int)(blockIdx.y * TA_JOIN_WAVES + (threadIdx.x >> 6))), r = uniform((int)(blockIdx.x / a.max_rows)), j = (int)blockIdx.x - r * a.max_rows;
   int first;
@@ -389,19 +389,18 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
   if (count < 2 || j >= n_rows || head >= a.Hq) return;
   const size_t step = (size_t)a.Hq * a.max_rows * a.rec;
   const float *rec = a.part + (((size_t)record * a.Hq + head) * a.max_rows + j) * a.rec;
-  const int parts = (a.dh + 63) / 64;
   const bool sees = a.vis[first + j] != 0;
-  float top = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  constexpr int N = 4;
+  float top = -INFINITY, l = 0.f, acc[PARTS] = {};
+  constexpr int N = 8;
   for (int i0 = 0; i0 < count; i0 += N) {
-    float v[N][4], m[N], s[N], most = top;
+    float v[N][PARTS], m[N], s[N], most = top;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const float *p = rec + (i0 + k < count ? i0 + k : i0) * step;
       m[k] = p[0];
       s[k] = p[1];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[k][c] = c < parts ? p[4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)] : 0.f;
+      for (int c = 0; c < PARTS; ++c) v[k][c] = p[4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)];
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) most = fmaxf(most, m[k]);
@@ -409,19 +408,19 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
     top = most;
     l *= corr;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] *= corr;
+    for (int c = 0; c < PARTS; ++c) acc[c] *= corr;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const float f = i0 + k < count ? __builtin_amdgcn_exp2f(m[k] - base) : 0.f;
       if (!(f > 0.f || f != f)) continue;  // (an item that the row sees nothing of)
       l += s[k] * f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] += v[k][c] * f;
+      for (int c = 0; c < PARTS; ++c) acc[c] += v[k][c] * f;
     }
   }
   const float inv = sees && (l > 0.f || l != l) ? 1.f / l : 0.f;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
+  for (int c = 0; c < PARTS; ++c) {
     const int ch = lane + 64 * c;
     if (ch >= a.dh) continue;
     const float y = sees ? acc[c] * inv : 0.f;
@@ -436,10 +435,10 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 }
 
 // ---- host side ------------------------------------------------------------------------------------------
-constexpr int TA_FEW = 256, TA_WHOLE_WIDE = 256;
+constexpr int TA_FEW = 256, TA_WHOLE_WIDE = 256, TA_MANY = 64;
 constexpr size_t TA_RECORDS = (size_t)64 << 20;  // bytes of the items' records, which fewer items keep to
 struct TreePlan {
-  int wide, nt, waves, tiles, target, items;
+  int wide, nt, waves, tiles, uncut, target, items;
   unsigned grid;
   size_t notes, list, bytes;
 };
@@ -460,8 +459,11 @@ static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, bo
 static int ta_target(const TreePlan &r, const la_pages_desc &p) { return std::max(1, (!r.wide && r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles)); }
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   const long long cap = (long long)max_blocks * p.page_size;
-  const bool wide = tree_wide(p.dtype, p.head_dim, p.page_size, Hq / p.n_kv_heads * max_rows) != 0, whole = cap <= (wide ? TA_WHOLE_WIDE : AT_WHOLE);
+  const int wide = tree_wide(p.dtype, p.head_dim, p.page_size, Hq / p.n_kv_heads * max_rows);
+  const int uncut = wide && (long long)R * p.n_kv_heads * ceil_div(Hq / p.n_kv_heads * max_rows, wide) < TA_MANY ? TA_WHOLE_WIDE : AT_WHOLE;
+  const bool whole = cap <= uncut;
   TreePlan r = ta_shape(p, Hq, max_rows, R, whole);
+  r.uncut = uncut;
   r.items = R;
   if (!whole) {
     const size_t record = (size_t)Hq * max_rows * (p.head_dim + 4) * 4;
@@ -524,7 +526,10 @@ static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if (rc) return rc;
   if (plan.target > 0) {
     ProfScope ps("tree_join", s);
-    tree_join_kernel<T><<<dim3((unsigned)a.B * a.max_rows, ceil_div(a.Hq, TA_JOIN_WAVES)), 64 * TA_JOIN_WAVES, 0, s>>>(a);
+    const dim3 grid((unsigned)a.B * a.max_rows, ceil_div(a.Hq, TA_JOIN_WAVES));
+    if (a.dh <= 64) tree_join_kernel<T, 1><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
+    else if (a.dh <= 128) tree_join_kernel<T, 2><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
+    else tree_join_kernel<T, 4><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
   }
   LA_HIP(hipGetLastError());
   return LA_OK;
@@ -533,6 +538,7 @@ static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) 
   a.target = plan.target;
   a.tiles = plan.tiles;
   a.items = plan.items;
+  a.uncut = plan.uncut;
   a.rec = a.dh + 4;
   a.notes = plan.target > 0 ? (int2 *)((char *)a.part + plan.notes) : nullptr;
   if (plan.list) {
