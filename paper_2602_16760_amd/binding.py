@@ -362,29 +362,30 @@ def la_logits_adjust(logits, out, req=None, repetition=None, presence=None, freq
     n = (B,)
     R = n_requests
     if R is None:
-        of = next((t for t in (repetition, presence, frequency, tokens, bias, n_tokens) if t is not None), None)
+        of = repetition if repetition is not None else presence if presence is not None else frequency if frequency is not None else tokens if tokens is not None else bias
         R = of.shape[0] if of is not None and of.dim() else first.shape[0] - 1 if first is not None and first.dim() else B
     r = (R,)
-    how = la_adjust(_optional(req, "req", _I32, n, device), _optional(repetition, "repetition", _F32, r, device), _optional(presence, "presence", _F32, r, device),
-                    _optional(frequency, "frequency", _F32, r, device))
-    how.n_requests = R
+    tokens_p = tokens_ld = most = lens_p = prompt_p = draft_p = first_p = vis_p = token_p = bias_p = bias_ld = n_bias = allowed_p = allowed_ld = n_allowed = index_p = 0
     if tokens is not None:
-        how.tokens, how.tokens_stride, _, how.max_tokens = _lists(tokens, "tokens", _I32, device, R)
-        how.n_tokens, how.n_prompt = _optional(n_tokens, "n_tokens", _I32, r, device), _optional(n_prompt, "n_prompt", _I32, r, device)
+        tokens_p, tokens_ld, _, most = _lists(tokens, "tokens", _I32, device, R)
+        lens_p, prompt_p = _optional(n_tokens, "n_tokens", _I32, r, device), _optional(n_prompt, "n_prompt", _I32, r, device)
     if draft is not None:
-        how.draft, how.first, how.vis = _array(draft, "draft", _I32, n, device), _optional(first, "first", _I32, (R + 1,), device), _optional(vis, "vis", _I64, n, device)
+        draft_p, first_p, vis_p = _array(draft, "draft", _I32, n, device), _optional(first, "first", _I32, (R + 1,), device), _optional(vis, "vis", _I64, n, device)
     if bias is not None or bias_token is not None:
         if bias is None or bias_token is None or bias.shape != bias_token.shape:
             _refuse("bias, bias_token: need both, of one shape")
-        how.bias, ld, _, how.n_bias = _lists(bias, "bias", _F32, device, R)
-        how.bias_token, how.bias_stride, _, _ = _lists(bias_token, "bias_token", _I32, device, R)
-        if ld != how.bias_stride:
+        bias_p, bias_ld, _, n_bias = _lists(bias, "bias", _F32, device, R)
+        token_p, ld, _, _ = _lists(bias_token, "bias_token", _I32, device, R)
+        if ld != bias_ld:
             _refuse("bias, bias_token: need rows of one stride")
     if allowed is not None:
-        how.allowed, how.allowed_stride, how.n_allowed, words = _lists(allowed, "allowed", _I32, device)
+        allowed_p, allowed_ld, n_allowed, words = _lists(allowed, "allowed", _I32, device)
         if words != (V + 31) // 32:
             _refuse(f"allowed: need {(V + 31) // 32} words a mask, got {words}")
-        how.allowed_index = _optional(allowed_index, "allowed_index", _I32, n, device)
+        index_p = _optional(allowed_index, "allowed_index", _I32, n, device)
+    how = la_adjust(_optional(req, "req", _I32, n, device), _optional(repetition, "repetition", _F32, r, device), _optional(presence, "presence", _F32, r, device),
+                    _optional(frequency, "frequency", _F32, r, device), tokens_p, lens_p, prompt_p, draft_p, first_p, vis_p, token_p, bias_p, allowed_p, index_p, tokens_ld, bias_ld, allowed_ld,
+                    R, most, n_bias, n_allowed)
     _check(lib.la_logits_adjust(logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if B > 1 else V, B, V, C.byref(how), out.data_ptr(), out.stride(0) if B > 1 else V,
                                 _stream(stream)))
 

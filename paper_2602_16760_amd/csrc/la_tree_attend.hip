@@ -456,7 +456,10 @@ static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, bo
   r.tiles = ceil_div(columns, r.wide ? r.wide : 16 * r.nt);
   return r;
 }
-static int ta_target(const TreePlan &r, const la_pages_desc &p) { return std::max(1, (!r.wide && r.nt == 1 ? at_workgroups(p.head_dim) : 256) / (p.n_kv_heads * r.tiles)); }
+static int ta_target(const TreePlan &r, const la_pages_desc &p) {
+  const int groups = r.wide ? (r.wide == 128 && p.head_dim <= 128 ? 512 : 256) : r.nt == 1 ? at_workgroups(p.head_dim) : 256;
+  return std::max(1, groups / (p.n_kv_heads * r.tiles));
+}
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   const long long cap = (long long)max_blocks * p.page_size;
   const int wide = tree_wide(p.dtype, p.head_dim, p.page_size, Hq / p.n_kv_heads * max_rows);

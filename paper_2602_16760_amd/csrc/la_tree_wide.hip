@@ -335,8 +335,9 @@ static int tw_launch(const TreeAttend &a, unsigned grid, hipStream_t s) {
 }
 template <typename T, int DH>
 static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_t s) {
-  if (columns == 64) return tw_launch<T, DH, 4, 1, DH == 64 ? 4 : 2>(a, grid, s);
-  if constexpr (DH <= 128) return columns == 256 ? tw_launch<T, DH, 8, 2, 4>(a, grid, s) : tw_launch<T, DH, 4, 2, DH == 64 ? 4 : 2>(a, grid, s);
+  constexpr int NS = DH == 64 ? 4 : 2;  // (64 KB: two workgroups a CU)
+  if (columns == 64) return tw_launch<T, DH, 4, 1, NS>(a, grid, s);
+  if constexpr (DH <= 128) return tw_launch<T, DH, 4, 2, NS>(a, grid, s);
   else return tw_launch<T, DH, 8, 1, 4>(a, grid, s);
 }
 template <typename T>
@@ -348,7 +349,7 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
 
 int tree_wide(int dtype, int head_dim, int page_size, int columns) {
   if (dtype == LA_F32 || page_size % 16 || columns <= 32 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
-  return columns <= 64 ? 64 : columns <= 128 || head_dim > 128 ? 128 : 256;
+  return columns <= 64 ? 64 : 128;
 }
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s) {
   return dtype == LA_F16 ? tw_launch<_Float16>(a, columns, grid, s) : tw_launch<uint16_t>(a, columns, grid, s);
