@@ -18,12 +18,12 @@ typedef unsigned __attribute__((ext_vector_type(2))) at_u2;
 constexpr float AT_LOG2E = 1.4426950408889634f;
 
 template <typename A>
-__device__ __forceinline__ int whole(const A &) { return 0; }
+__device__ __forceinline__ int at_uncut(const A &) { return 0; }
 
 // The wanted item, or item 0 of the wanted row; b = -1: there is none.  Rows that are not cut are items themselves.  Of up to 64 rows every wave finds it from the rows'
 // positions, a lane each; of more it was written down by a launch of its own: formed by every workgroup from all rows' positions, 64 at a time, the time grew with the square of the
 // rows (512 rows of 1000 379 us, with the list 344; 65 rows 57 and 59).
-// RECORDS: its place among the records of rows that are cut is wanted too.  Where no row has more than whole(a) keys, none is cut.
+// RECORDS: its place among the records of rows that are cut is wanted too.  Where no row has more than at_uncut(a) keys, none is cut.
 template <bool BY_ROW, bool RECORDS, typename A>
 __device__ __forceinline__ AtItem at_find(const A &a, int wanted) {
   AtItem it{};
@@ -49,7 +49,7 @@ __device__ __forceinline__ AtItem at_find(const A &a, int wanted) {
     return lane_value(ends, 63);
   };
   const int longest = lane_most(n);
-  (void)items(RECORDS && longest <= whole(a) ? AT_UNCUT : at_cut(a.B, a.target, lane_value(lane_through((long long)n), 63), longest, items));
+  (void)items(RECORDS && longest <= at_uncut(a) ? AT_UNCUT : at_cut(a.B, a.target, lane_value(lane_through((long long)n), 63), longest, items));
   const int l = BY_ROW ? wanted : __builtin_popcountll(__ballot(ends <= wanted));
   it.b = -1;
   if (l >= a.B) return it;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(AT_PLAN_THREADS) void paged_plan_kernel(A a, int it
   if (lane == 0) red[wave] = longest;
   __syncthreads();
   longest = lane_most(lane < WAVES ? (int)red[lane] : 0);
-  const int C = RECORDS && longest <= whole(a) ? AT_UNCUT : at_cut(a.B, a.target, keys, longest, [&](int C) {
+  const int C = RECORDS && longest <= at_uncut(a) ? AT_UNCUT : at_cut(a.B, a.target, keys, longest, [&](int C) {
     long long c = 0;
     for (int b = t; b < a.B; b += AT_PLAN_THREADS) c += at_rows_items(at_keys(a, b, r), C);
     return (int)all_of(c);

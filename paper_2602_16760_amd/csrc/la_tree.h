@@ -49,7 +49,7 @@ __device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
 // precision's carry 2^UP instead of 2^15.
 template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 4.f : 8.f;
 template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 11.f : 0.f;
-__device__ __forceinline__ int whole(const TreeAttend &a) { return a.uncut; }
+__device__ __forceinline__ int at_uncut(const TreeAttend &a) { return a.uncut; }
 
 // Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
 // infinite V stays one).  The factor is the same for all weights and goes out with their sum.

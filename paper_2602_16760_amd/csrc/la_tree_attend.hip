@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
           else dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
         }
       }
-      const float base = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base));
+      const float base = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base)) * (1.f + TA_REST<T>);
       if (!(a.vis[first + c / g] >> row & 1u)) continue;
 #pragma unroll
       for (int u = 0; u < VH; ++u)
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
     for (int k = 0; k < N; ++k) {
       const float *p = rec + (i0 + k < count ? i0 + k : i0) * step;
       m[k] = p[0];
-      s[k] = p[1];
+      s[k] = i0 + k < count ? p[1] : 0.f;
 #pragma unroll
       for (int c = 0; c < PARTS; ++c) v[k][c] = p[4 + (lane + 64 * c < a.dh ? lane + 64 * c : 0)];
     }
@@ -412,8 +412,8 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const float f = i0 + k < count ? __builtin_amdgcn_exp2f(m[k] - base) : 0.f;
-      if (!(f > 0.f || f != f)) continue;  // (an item that the row sees nothing of)
-      l += s[k] * f;
+      l += s[k] * f;  // (scores that are all NaN leave an offset of -inf and a sum of NaN)
+      if (!(f > 0.f || f != f)) continue;
 #pragma unroll
       for (int c = 0; c < PARTS; ++c) acc[c] += v[k][c] * f;
     }

@@ -288,7 +288,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
           dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
         }
       }
-      const float add = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), w = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, add));
+      const float add = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), w = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, add)) * (1.f + TA_REST<T>);
       if (!(a.vis[first + c / g] >> row & 1u)) continue;
 #pragma unroll
       for (int d = 0; d < DT; ++d)

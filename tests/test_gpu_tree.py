@@ -244,7 +244,7 @@ class Case:
         torch.cuda.synchronize()
         return out.cpu()
 
-    def check(self, out, scale=None, max_rows=64, skip=lambda r, t: False, rows=None):
+    def check(self, out, scale=None, max_rows=64, skip=lambda r, t: False, rows=None, but_nan=False):
         """Against float64, as la_paged_attend's rows are: a probability is rounded to the type (half a step of it), as is the output; scores are sums of dh float products, their error shifts a
         probability by as much relatively; the exponential and the sums over n keys add 2^-23 a term."""
         scale = self.dh ** -0.5 if scale is None else scale
@@ -268,7 +268,7 @@ class Case:
                 shift = ((self.dh + 8) * 2.0 ** -24 * size)[:, None]
                 tol = (half if self.dtype != torch.float32 else 0.0) * mass + half * want.abs() + 2 * shift * mass + (len(see) + 16) * 2.0 ** -23 * mass + 1e-30
                 err = (out[i].double() - want).abs()
-                assert (err <= tol).all(), f"row {i} (request {r}, {len(see)} keys): {float((err / tol).max()):.2f} of the bound"
+                assert ((err <= tol) | (torch.isnan(err) if but_nan else torch.zeros_like(err, dtype=torch.bool))).all(), f"row {i} (request {r}, {len(see)} keys): {float((err / tol).max()):.2f} of the bound"
         assert (out[self.first[-1]:] == 0).all()
 
 
@@ -316,6 +316,42 @@ def test_attend_many_requests(R, ctx):
     c.check(c.run(max_rows=4), max_rows=4)
 
 
+@pytest.mark.parametrize("dtype,Hkv,dh,page,rows,ctx", [("bf16", 1, 64, 16, 24, 300), ("f16", 2, 128, 16, 20, 1500), ("bf16", 2, 128, 24, 20, 1500), ("f16", 1, 256, 16, 33, 1200), ("f32", 2, 64, 16, 9, 1200)])
+def test_attend_many_requests_of_many_rows(dtype, Hkv, dh, page, rows, ctx):
+    """More than 64 requests whose rows and heads are many; some have none, one is much longer than the others."""
+    R = 70
+    lens, counts = [(37 * r) % 90 for r in range(R)], [(7 * r) % rows for r in range(R)]
+    lens[5], counts[5], counts[11] = ctx, rows, rows
+    c = Case(dtype, 4 * Hkv, Hkv, dh, page, lens, counts, seed=R)
+    out = c.run(max_rows=rows)
+    c.check(out, max_rows=rows, rows=[i for i in range(len(c.vis)) if i % 5 == 0 or c.first[5] <= i < c.first[6]])
+    assert torch.equal(out, c.run(max_rows=rows))
+
+
+@pytest.mark.parametrize("rows,ctx", [(3, 100), (3, 2000), (30, 100), (30, 2000)])
+def test_attend_rows_in_front_of_the_first_request_and_behind_the_last(rows, ctx):
+    """Rows of no request on both sides are zeros, at one launch and at two."""
+    B = binding()
+    c = Case("bf16", 8, 2, 128, 16, [ctx, 7], [rows, 2])
+    q = torch.cat((c.q[:4], c.q, c.q[:3]))[:, :, :].contiguous()
+    out = torch.full(q.shape, 77.0, dtype=c.dtype, device="cuda")
+    B.la_paged_tree_attend(B.la_pages(c.k.cuda(), c.v.cuda()), 0, q.cuda(), c.table.cuda(), i32([f + 4 for f in c.first]), i32(c.lens), i64([1] * 4 + c.vis + [1] * 3), rows, out)
+    n = len(c.vis)
+    assert (out[:4] == 0).all() and (out[4 + n:] == 0).all()
+    c.check(out[4:4 + n].cpu(), max_rows=rows)
+
+
+@pytest.mark.parametrize("rows,ctx,page", [(4, 60, 16), (4, 1500, 16), (40, 60, 16), (40, 1500, 16), (6, 100, 12)])
+def test_attend_queries_that_are_no_numbers(rows, ctx, page):
+    """A NaN or an infinity in a row's query head reaches that head's output alone; a row that sees nothing has zeros whatever its query holds."""
+    c = Case("bf16", 8, 2, 64, page, [ctx], [rows], masks=[[(2 << j) - 1 for j in range(rows - 1)] + [0]])
+    c.q[0, 3, 5], c.q[1, 6, 0], c.q[rows - 1] = float("nan"), float("inf"), float("nan")
+    out = c.run(max_rows=rows)
+    assert torch.isnan(out[0, 3]).all() and (out[rows - 1] == 0).all()
+    assert torch.isfinite(out[0, [0, 1, 2, 4, 5, 6, 7]]).all() and torch.isfinite(out[1, [0, 1, 2, 3, 4, 5, 7]]).all()
+    c.check(out, max_rows=rows, rows=range(2, rows))
+
+
 def test_attend_masks_of_any_kind():
     """Rows that do not see themselves, see later rows, see nothing but the committed positions of their own block, bits behind the block's rows."""
     full = (1 << 64) - 1
@@ -359,7 +395,8 @@ def test_attend_other_scales(dtype, scale):
     c.check(c.run(scale=scale), scale=scale)
 
 
-@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,ctx", [("f32", 2, 1, 64, 16, 40), ("bf16", 2, 1, 64, 16, 40), ("bf16", 32, 2, 128, 16, 1500), ("f16", 8, 1, 256, 24, 100), ("f16", 8, 2, 96, 16, 900)])
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,ctx", [("f32", 2, 1, 64, 16, 40), ("bf16", 2, 1, 64, 16, 40), ("bf16", 32, 2, 128, 16, 1500), ("f16", 8, 1, 256, 24, 100), ("f16", 8, 2, 96, 16, 900), ("f16", 8, 2, 64, 16, 1100),
+                                                        ("bf16", 4, 1, 256, 32, 1000), ("f16", 4, 1, 128, 16, 50)])
 def test_attend_values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx):
     """K and V of infinities and NaN in a drafted row reach the rows that see it, in their own channels, and no other row."""
     n = 40
@@ -383,6 +420,14 @@ def test_attend_values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx)
     assert torch.isnan(out[4, :, 7]).all() and (out[4, :, 9] == -inf).all() and torch.isfinite(out[4, :, 10:]).all() and torch.isfinite(out[4, :, 8]).all()
     assert torch.isnan(out[7]).all() and torch.isnan(out[20]).all()
     assert (out[33, :, 0] == inf).all() and torch.isfinite(out[33, :, 1:]).all()
+    # the other channels of rows that see them: as if those numbers were not there (a row's channels have nothing to do with each other)
+    for r, t, ch in ((0, ctx + 2, 5), (0, ctx + 3, 7), (0, ctx + 4, 9), (0, ctx + 33, 0)):
+        c.keys[r][1][t][:, ch] = 0.0
+    got = out.clone()
+    for row, chans in ((2, [5]), (3, [7]), (4, [7, 9]), (33, [0])):
+        for ch in chans:
+            got[row, :, ch] = float("nan")
+    c.check(got, rows=(2, 3, 4, 33), but_nan=True)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
