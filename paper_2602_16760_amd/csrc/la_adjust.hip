@@ -10,10 +10,14 @@
 namespace la {
 
 // A workgroup per chunk of a row.  How often each of the chunk's tokens occurred is counted in LDS, from the request's committed tokens and those drafted on the row's path; then the
-// logits, requested before, pass once.  Counts are whole numbers and a token's biases are added in the list's order: results do not depend on the order of the atomics.
+// logits, requested before, pass once.  Counts are whole numbers and a token's biases are added in the list's order: results do not depend on the order of the atomics, nor on the chunks.
+// Bound by a chain (settings, history, LDS, division) at few rows, 5.0 us for one of 32768; by the bytes and that chain at many: 64 rows of 131072, 67.6 MB, 8192 tokens of history each, 19.4 us =
+// 3.5 TB/s, all workgroups resident and in step (64 registers; with 67 a fourth workgroup did not fit a CU: 22.4).  Loads and stores of four bytes, requested as they were needed, took 50; a
+// search through all biases by each token that has one 116 instead of 11.6 us where 300 fall on one row.
 constexpr int ADJ_THREADS = 512;
 constexpr int ADJ_PER = 16, ADJ_PER_SHORT = 4;  // tokens of a thread: chunks of 8192 and of 2048
 constexpr int ADJ_LIST = 256;                   // biases of a chunk that are kept in LDS
+constexpr int ADJ_FEW = 1024;                   // short chunks of a launch at most
 constexpr unsigned ADJ_SEEN = 1u << 31, ADJ_BIASED = 1u << 30, ADJ_COUNT = ADJ_BIASED - 1;  // a token's word: occurred in the prompt; has a bias; times it was emitted
 
 struct Adjust {
@@ -197,7 +201,9 @@ static void adjust_launch(const Adjust &a, hipStream_t s) {
     logits_adjust_kernel<T, PER, decltype(v)::value><<<dim3(ceil_div(a.V, ADJ_THREADS * PER), a.B), ADJ_THREADS, 0, s>>>(a);
   };
   auto sized = [&](auto per) { vec ? launch(per, std::true_type{}) : launch(per, std::false_type{}); };
-  a.V <= 16 * ADJ_THREADS * ADJ_PER_SHORT ? sized(std::integral_constant<int, ADJ_PER_SHORT>{}) : sized(std::integral_constant<int, ADJ_PER>{});
+  // Short chunks while they are no more than the chip takes at once: more workgroups, each of which looks through the whole history.  us, short / long: one row of 32768 5.6 / 8.2, one of 100001
+  // 7.1 / 11.5, 64 of 32768 10.1 / 11.3, 16 of 131072 in bfloat16 8.5 / 9.1, 64 of 131072 27.3 / 20.8.
+  (long long)a.B * ceil_div(a.V, ADJ_THREADS * ADJ_PER_SHORT) <= ADJ_FEW ? sized(std::integral_constant<int, ADJ_PER_SHORT>{}) : sized(std::integral_constant<int, ADJ_PER>{});
 }
 
 }  // namespace la

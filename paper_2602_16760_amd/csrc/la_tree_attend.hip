@@ -438,7 +438,7 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 constexpr int TA_FEW = 256, TA_WHOLE_WIDE = 256, TA_MANY = 64;
 constexpr size_t TA_RECORDS = (size_t)64 << 20;  // bytes of the items' records, which fewer items keep to
 struct TreePlan {
-  int wide, nt, waves, tiles, uncut, target, items;
+  int wide, waves, tiles, uncut, target, items;
   unsigned grid;
   size_t notes, list, bytes;
 };
@@ -446,27 +446,22 @@ struct TreePlan {
 static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, bool whole) {
   TreePlan r{};
   const int columns = Hq / p.n_kv_heads * max_rows;
-  r.wide = tree_wide(p.dtype, p.head_dim, p.page_size, columns);
-  r.nt = columns <= 16 || p.head_dim > 128 ? 1 : 2;
-  r.waves = TA_WAVES;
-  if (!r.wide && whole && p.head_dim <= 128 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW) {
-    r.nt = 1;
-    r.waves = TA_WHOLE_WAVES;
-  }
-  r.tiles = ceil_div(columns, r.wide ? r.wide : 16 * r.nt);
+  const bool few = whole && p.head_dim <= 128 && columns <= 32 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW;
+  r.wide = columns > 16 && !few ? tree_wide(p.dtype, p.head_dim, p.page_size, columns) : 0;
+  r.waves = few ? TA_WHOLE_WAVES : TA_WAVES;
+  r.tiles = ceil_div(columns, r.wide ? r.wide : 16);
   return r;
 }
 static int ta_target(const TreePlan &r, const la_pages_desc &p) {
-  const int groups = r.wide ? (r.wide == 128 && p.head_dim <= 128 ? 512 : 256) : r.nt == 1 ? at_workgroups(p.head_dim) : 256;
+  const int groups = !r.wide ? at_workgroups(p.head_dim) : r.wide == 128 && p.head_dim <= 128 ? 512 : 256;
   return std::max(1, groups / (p.n_kv_heads * r.tiles));
 }
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   const long long cap = (long long)max_blocks * p.page_size;
-  const int wide = tree_wide(p.dtype, p.head_dim, p.page_size, Hq / p.n_kv_heads * max_rows);
-  const int uncut = wide && (long long)R * p.n_kv_heads * ceil_div(Hq / p.n_kv_heads * max_rows, wide) < TA_MANY ? TA_WHOLE_WIDE : AT_WHOLE;
-  const bool whole = cap <= uncut;
-  TreePlan r = ta_shape(p, Hq, max_rows, R, whole);
-  r.uncut = uncut;
+  TreePlan r = ta_shape(p, Hq, max_rows, R, cap <= AT_WHOLE);
+  r.uncut = r.wide && (long long)R * p.n_kv_heads * r.tiles < TA_MANY ? TA_WHOLE_WIDE : p.dtype == LA_F32 ? AT_WHOLE / 2 : AT_WHOLE;
+  const bool whole = cap <= r.uncut;
+  if (!whole) r.waves = TA_WAVES;
   r.items = R;
   if (!whole) {
     const size_t record = (size_t)Hq * max_rows * (p.head_dim + 4) * 4;
@@ -506,10 +501,8 @@ static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
 }
 template <typename T, int DH>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
-  if constexpr (DH <= 128) {
-    if (plan.nt == 2) return ta_launch<T, DH, 2, TA_WAVES>(a, plan, s);
+  if constexpr (DH <= 128)
     if (plan.waves == TA_WHOLE_WAVES) return ta_launch<T, DH, 1, TA_WHOLE_WAVES>(a, plan, s);
-  }
   return ta_launch<T, DH, 1, TA_WAVES>(a, plan, s);
 }
 template <typename T>

@@ -348,7 +348,7 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
 }
 
 int tree_wide(int dtype, int head_dim, int page_size, int columns) {
-  if (dtype == LA_F32 || page_size % 16 || columns <= 32 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
+  if (dtype == LA_F32 || page_size % 16 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
   return columns <= 64 ? 64 : 128;
 }
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s) {
