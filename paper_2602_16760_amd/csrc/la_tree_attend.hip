@@ -7,9 +7,9 @@ namespace la {
 
 constexpr int TA_WAVES = 4, TA_WHOLE_WAVES = 8;  // of a workgroup; where requests are not cut and workgroups are few
 
-// A workgroup takes an item's keys for one kv head and 16 NT of its columns; column c of a kv head is query head c % g of the request's row c / g, so that those of a block of few rows lie
-// together.  The waves take blocks of KEYS keys in turn and meet once, at the end.  Products, types and pages as in la_attend.hip, K and V of a block go through the matrix instructions NT times.
-template <typename T, int DH, int NT, bool FAST, int WAVES>
+// A workgroup takes an item's keys for one kv head and 16 of its columns; column c of a kv head is query head c % g of the request's row c / g, so that those of a block of few rows lie
+// together.  The waves take blocks of KEYS keys in turn and meet once, at the end.  Products, types and pages as in la_attend.hip.
+template <typename T, int DH, bool FAST, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES;
@@ -33,23 +33,22 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   int f0;
   const int n_rows = uniform(tree_rows(a, it.b, f0)), first = uniform(f0), L = uniform(a.len[it.b]);
   if (it.index == 0 && tile == 0) ta_zero_behind<T>(a, it.b, first, n_rows, h * g * dh, g * dh, 64 * WAVES);
-  const int cols = n_rows * g - tile * 16 * NT;  // of this workgroup, if it had room for all
+  const int cols = n_rows * g - 16 * tile;  // of this workgroup, if it had room for all
   if (cols <= 0) return;
   const int k_first = it.index * it.C, k_end = at_item_end(it);  // (C is a multiple of the block)
-  // this lane's columns
-  at_u4 q[NT][KP];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int c = tile * 16 * NT + (16 * t + c16 < cols ? 16 * t + c16 : 0), j = c / g, i = first + j, head = h * g + c - j * g;
-    const char *qp = (const char *)a.q + (a.q_tiles ? (((int64_t)head * a.q_tiles + (i >> 4)) * (dh / 32) * 64 + (i & 15)) * 16 : (i * a.ldq + (int64_t)head * dh) * E);
+  // this lane's column: its row of all, and the query head
+  const int col = 16 * tile + (c16 < cols ? c16 : 0), col_row = first + col / g, col_head = h * g + col % g;
+  at_u4 q[KP];
+  {
+    const char *qp = (const char *)a.q + (a.q_tiles ? (((int64_t)col_head * a.q_tiles + (col_row >> 4)) * (dh / 32) * 64 + (col_row & 15)) * 16 : (col_row * a.ldq + (int64_t)col_head * dh) * E);
 #pragma unroll
     for (int p = 0; p < KP; ++p) {
       const int at = 64 * p + 16 * q4;
-      q[t][p] = FAST || at < dh * E ? *(const at_u4 *)(qp + (a.q_tiles ? 1024 * p + 256 * q4 : at)) : at_u4{0, 0, 0, 0};
+      q[p] = FAST || at < dh * E ? *(const at_u4 *)(qp + (a.q_tiles ? 1024 * p + 256 * q4 : at)) : at_u4{0, 0, 0, 0};
     }
     if (a.scale < 0.f)  // (scores are multiplied by what is not negative: the largest stays the largest)
 #pragma unroll
-      for (int p = 0; p < KP; ++p) q[t][p] ^= F32 ? 0x80000000u : 0x80008000u;
+      for (int p = 0; p < KP; ++p) q[p] ^= F32 ? 0x80000000u : 0x80008000u;
   }
   const float to_log2 = fabsf(a.scale) * AT_LOG2E;
   const int row_bytes = dh * E;
@@ -126,15 +125,10 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
       }
     }
   };
-  at_f4 o[NT][DT];
-  float m_run[NT], l_run[NT];
+  at_f4 o[DT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[t][d] = at_f4{0.f, 0.f, 0.f, 0.f};
-    m_run[t] = -INFINITY;
-    l_run[t] = 0.f;
-  }
+  for (int d = 0; d < DT; ++d) o[d] = at_f4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
   if (mine > 0) {
     look_up(0);
     locate(0);
@@ -147,43 +141,35 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
     const unsigned now = seen;
     const int key0 = k_first + KEYS * (wave + WAVES * i);
     const bool drafted = (long long)key0 + KEYS > L;  // keys of the request's own rows among them
-    at_f4 s[NT][TILES];
+    at_f4 s[TILES];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int t = 0; t < TILES; ++t) {
+      s[t] = at_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) s[n][t] = at_f4{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < KP; ++k) {
+        if constexpr (F32) {
 #pragma unroll
-    for (int k = 0; k < KP; ++k)
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if constexpr (F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[t][k][e]), __uint_as_float(q[n][k][e]), s[n][t], 0, 0, 0);
-          } else {
-            s[n][t] = at_mma<T>(kr[t][k], q[n][k], s[n][t]);
-          }
+          for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[t][k][e]), __uint_as_float(q[k][e]), s[t], 0, 0, 0);
+        } else {
+          s[t] = at_mma<T>(kr[t][k], q[k], s[t]);
         }
+      }
+    }
     float factor = to_log2;
     unsigned odd = 0;  // such keys of the block
     if (drafted || now != ALL) {
       factor = 1.f;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        unsigned mask = now;  // keys that the column sees
-        if (drafted) {
-          const int c = tile * 16 * NT + (16 * n + c16 < cols ? 16 * n + c16 : 0);
-          const unsigned long long vis = a.vis[first + c / g];
-          const int at = key0 - L;  // of the block's first key in the request's rows
-          mask &= at >= 0 ? (at < 64 ? (unsigned)(vis >> at) : 0u) : (unsigned)(vis << -at) | ((1u << -at) - 1u);  // (at > -KEYS)
-        }
-        mask >>= 4 * q4;
-#pragma unroll
-        for (int t = 0; t < TILES; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + e) & 1u ? s[n][t][e] * to_log2 : -INFINITY;
+      unsigned mask = now;  // keys that the column sees
+      if (drafted) {
+        const unsigned long long vis = a.vis[col_row];
+        const int at = key0 - L;  // of the block's first key in the request's rows
+        mask &= at >= 0 ? (at < 64 ? (unsigned)(vis >> at) : 0u) : (unsigned)(vis << -at) | ((1u << -at) - 1u);  // (at > -KEYS)
       }
+      mask >>= 4 * q4;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t][e] = mask >> (16 * t + e) & 1u ? s[t][e] * to_log2 : -INFINITY;
       if (drafted) {
 #pragma unroll
         for (int j = 0; j < VK; ++j) {
@@ -215,68 +201,54 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
       locate(i + 1);
       load_k();
     }
+    float mx = -INFINITY;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float mx = -INFINITY;
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
+    mx *= factor;
+    if (__any(mx > m_run + LAZY)) {
+      const float m_new = fmaxf(m_run, at_max4(mx)), corr = __builtin_amdgcn_exp2f(m_run - (m_new > -INFINITY ? m_new : 0.f));
+      m_run = m_new;
+      l_run *= corr;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[n][t][e]);
-      mx *= factor;
-      if (__any(mx > m_run[n] + LAZY)) {
-        const float m_new = fmaxf(m_run[n], at_max4(mx)), corr = __builtin_amdgcn_exp2f(m_run[n] - (m_new > -INFINITY ? m_new : 0.f));
-        m_run[n] = m_new;
-        l_run[n] *= corr;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[n][d] *= corr;
-      }
-      const float base = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f);
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[n][t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][e], factor, base));
-          l_run[n] += s[n][t][e];
-        }
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
     }
+    const float base = UP - (m_run > -INFINITY ? m_run : 0.f);
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], factor, base));
+        l_run += s[t][e];
+      }
     if constexpr (F32) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int u = 0; u < VH; ++u)
 #pragma unroll
-          for (int w = 0; w < VC; ++w)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][u * VC + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[e][u][w]), s[n][0][e], o[n][u * VC + w], 0, 0, 0);
+          for (int w = 0; w < VC; ++w) o[u * VC + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[e][u][w]), s[0][e], o[u * VC + w], 0, 0, 0);
     } else {
-      at_u4 p[NT], rest[NT];
+      at_u4 p, rest;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const at_u2 both = ta_split<T>(s[n][j / 2 % TILES][2 * (j & 1)], s[n][j / 2 % TILES][2 * (j & 1) + 1]);
-          p[n][j] = both[0];
-          rest[n][j] = both[1];
-        }
+      for (int j = 0; j < 4; ++j) {
+        const at_u2 both = ta_split<T>(s[j / 2 % TILES][2 * (j & 1)], s[j / 2 % TILES][2 * (j & 1) + 1]);
+        p[j] = both[0];
+        rest[j] = both[1];
+      }
 #pragma unroll
       for (int u = 0; u < VH; ++u)
 #pragma unroll
-        for (int w = 0; w < VW / 4; ++w) {
-          at_u4 v[2];
+        for (int w = 0; w < VW / 4; ++w)
 #pragma unroll
-          for (int half = 0; half < 2; ++half)
+          for (int half = 0; half < 2; ++half) {
+            at_u4 v;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              v[half][j] = __builtin_amdgcn_perm(vr[(2 * j + 1) % VK][u][w], vr[2 * j % VK][u][w], half ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][u * VC + 2 * w + half] = at_mma<T>(v[half], p[n], o[n][u * VC + 2 * w + half]);
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][u * VC + 2 * w + half] = at_mma<T>(v[half], rest[n], o[n][u * VC + 2 * w + half]);
-        }
+              v[j] = __builtin_amdgcn_perm(vr[(2 * j + 1) % VK][u][w], vr[2 * j % VK][u][w], half ? 0x07060302u : 0x05040100u);
+            o[u * VC + 2 * w + half] = at_mma<T>(v, rest, at_mma<T>(v, p, o[u * VC + 2 * w + half]));
+          }
     }
     if (i + 1 < mine) load_v();
   }
@@ -284,95 +256,87 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   for (; odd_rows; odd_rows &= odd_rows - 1) {
     const int row = __builtin_ctzll(odd_rows);
     const long long at = place((long long)L + row);
+    float dot = 0.f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int c = tile * 16 * NT + (16 * n + c16 < cols ? 16 * n + c16 : 0);
-      float dot = 0.f;
+    for (int p = 0; p < KP; ++p) {
+      const int b = 64 * p + 16 * q4;
+      const at_u4 k = *(const at_u4 *)(kb + at + (FAST || b < row_bytes ? b : 0));
 #pragma unroll
-      for (int p = 0; p < KP; ++p) {
-        const int b = 64 * p + 16 * q4;
-        const at_u4 k = *(const at_u4 *)(kb + at + (FAST || b < row_bytes ? b : 0));
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {  // (q's pieces behind the row's end are zeros; what K has in their place is no number of its own)
-          if (!FAST && b >= row_bytes) continue;
-          const unsigned x = q[n][p][w], y = k[w];
-          if constexpr (F32) dot += __uint_as_float(x) * __uint_as_float(y);
-          else dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
-        }
+      for (int w = 0; w < 4; ++w) {  // (q's pieces behind the row's end are zeros; what K has in their place is no number of its own)
+        if (!FAST && b >= row_bytes) continue;
+        const unsigned x = q[p][w], y = k[w];
+        if constexpr (F32) dot += __uint_as_float(x) * __uint_as_float(y);
+        else dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
       }
-      const float base = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base)) * (1.f + TA_REST<T>);
-      if (!(a.vis[first + c / g] >> row & 1u)) continue;
-#pragma unroll
-      for (int u = 0; u < VH; ++u)
-#pragma unroll
-        for (int w = 0; w < VC; ++w)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int ch = 16 * VC * u + VC * (4 * q4 + y) + w;
-            if (FAST || ch < dh) o[n][u * VC + w][y] += p * load_as_float<T>((const T *)(vb + at) + ch);
-          }
     }
+    const float base = UP - (m_run > -INFINITY ? m_run : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base)) * (1.f + TA_REST<T>);
+    if (!(a.vis[col_row] >> row & 1u)) continue;
+#pragma unroll
+    for (int u = 0; u < VH; ++u)
+#pragma unroll
+      for (int w = 0; w < VC; ++w)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int ch = 16 * VC * u + VC * (4 * q4 + y) + w;
+          if (FAST || ch < dh) o[u * VC + w][y] += p * load_as_float<T>((const T *)(vb + at) + ch);
+        }
   }
-  // The waves' sums meet in LDS, 16 columns and a part of 16 VC channels at a time: [wave][column][channels + 4], and in front of them [wave][column] offset and sum; a thread adds the waves'
-  // sums of four channels, in order.  Output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w.
+  // The waves' sums meet in LDS, a part of 16 VC channels at a time: [wave][column][channels + 4], and in front of them [wave][column] offset and sum; a thread adds the waves' sums of four
+  // channels, in order.  Output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w.
   constexpr int PART = 16 * VC, PITCH = PART + 4, QUADS = PART / 4;
   float *stat = at_lds, *sums = at_lds + 2 * WAVES * AT_ROWS;
+  const int columns = cols < 16 ? cols : 16;
+  const float l = at_sum4(l_run) * (1.f + TA_REST<T>);
+  if (q4 == 0) {
+    stat[2 * (wave * AT_ROWS + c16)] = m_run;
+    stat[2 * (wave * AT_ROWS + c16) + 1] = l;
+  }
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int columns = cols - 16 * n < 16 ? cols - 16 * n : 16;
-    const float l = at_sum4(l_run[n]) * (1.f + TA_REST<T>);
+  for (int u = 0; u < VH; ++u) {
+    if (u > 0) __syncthreads();
+    if (c16 < columns) {
+      float *to = sums + (size_t)(wave * AT_ROWS + c16) * PITCH;
 #pragma unroll
-    for (int u = 0; u < VH; ++u) {
-      if (columns <= 0) continue;
-      if (n + u > 0) __syncthreads();
-      if (u == 0 && q4 == 0) {
-        stat[2 * (wave * AT_ROWS + c16)] = m_run[n];
-        stat[2 * (wave * AT_ROWS + c16) + 1] = l;
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int w = 0; w < VC; w += 4) {
+          at_f4 v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = o[u * VC + w + x][e];
+          *(at_f4 *)(to + VC * (4 * q4 + e) + w) = v;
+        }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < columns * QUADS; x += 64 * WAVES) {
+      const int row = x / QUADS, at = 4 * (x - row * QUADS), ch = PART * u + at, c = 16 * tile + row, j = c / g, head = h * g + c - j * g;
+      if (!FAST && ch >= dh) continue;
+      float m = stat[2 * row];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) m = fmaxf(m, stat[2 * (w * AT_ROWS + row)]);
+      const float base = m > -INFINITY ? m : 0.f;
+      float sum = 0.f;
+      at_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(stat[2 * (w * AT_ROWS + row)] - base);
+        sum += stat[2 * (w * AT_ROWS + row) + 1] * f;
+        y += *(const at_f4 *)(sums + (size_t)(w * AT_ROWS + row) * PITCH + at) * f;
       }
-      if (c16 < columns) {
-        float *to = sums + (size_t)(wave * AT_ROWS + c16) * PITCH;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int w = 0; w < VC; w += 4) {
-            at_f4 v;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = o[n][u * VC + w + x][e];
-            *(at_f4 *)(to + VC * (4 * q4 + e) + w) = v;
-          }
+      if (it.count > 1) {
+        float *to = a.part + (((size_t)it.record * a.Hq + head) * a.max_rows + j) * a.rec;
+        if (u == 0 && at == 0) *(float2 *)to = float2{m, sum};
+        *(at_f4 *)(to + 4 + ch) = y;
+        continue;
       }
-      __syncthreads();
-      for (int x = threadIdx.x; x < columns * QUADS; x += 64 * WAVES) {
-        const int col = x / QUADS, at = 4 * (x - col * QUADS), ch = PART * u + at, c = 16 * (tile * NT + n) + col, j = c / g, head = h * g + c - j * g;
-        if (!FAST && ch >= dh) continue;
-        float m = stat[2 * col];
+      y *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;  // (nothing seen: zeros)
+      if (a.vis[first + j] == 0) y = at_f4{0.f, 0.f, 0.f, 0.f};
+      if (a.kind != AT_OUT_ROWS) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, stat[2 * (w * AT_ROWS + col)]);
-        const float base = m > -INFINITY ? m : 0.f;
-        float sum = 0.f;
-        at_f4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-          const float f = __builtin_amdgcn_exp2f(stat[2 * (w * AT_ROWS + col)] - base);
-          sum += stat[2 * (w * AT_ROWS + col) + 1] * f;
-          y += *(const at_f4 *)(sums + (size_t)(w * AT_ROWS + col) * PITCH + at) * f;
-        }
-        if (it.count > 1) {
-          float *to = a.part + (((size_t)it.record * a.Hq + head) * a.max_rows + j) * a.rec;
-          if (u == 0 && at == 0) *(float2 *)to = float2{m, sum};
-          *(at_f4 *)(to + 4 + ch) = y;
-          continue;
-        }
-        y *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;  // (nothing seen: zeros)
-        if (a.vis[first + j] == 0) y = at_f4{0.f, 0.f, 0.f, 0.f};
-        if (a.kind != AT_OUT_ROWS) {
-#pragma unroll
-          for (int z = 0; z < 4; ++z) at_store_row(a, first + j, head * dh + ch + z, y[z]);
-        } else {
-          T *to = (T *)a.out + (first + j) * a.ldo + (int64_t)head * dh + ch;
-          if constexpr (F32) *(at_f4 *)to = y;
-          else *(at_u2 *)to = at_u2{at_pack<T>(y[0], y[1]), at_pack<T>(y[2], y[3])};
-        }
+        for (int z = 0; z < 4; ++z) at_store_row(a, first + j, head * dh + ch + z, y[z]);
+      } else {
+        T *to = (T *)a.out + (first + j) * a.ldo + (int64_t)head * dh + ch;
+        if constexpr (F32) *(at_f4 *)to = y;
+        else *(at_u2 *)to = at_u2{at_pack<T>(y[0], y[1]), at_pack<T>(y[2], y[3])};
       }
     }
   }
@@ -484,26 +448,26 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
   return r;
 }
 
-template <typename T, int DH, int NT, bool FAST, int WAVES>
+template <typename T, int DH, bool FAST, int WAVES>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
   constexpr int LDS = (2 * WAVES * AT_ROWS + WAVES * AT_ROWS * (16 * VC + 4)) * 4;
   if constexpr (LDS > 64 * 1024)
-    if (const int rc = ta_allow_lds<tree_attend_kernel<T, DH, NT, FAST, WAVES>>(LDS)) return rc;
-  tree_attend_kernel<T, DH, NT, FAST, WAVES><<<plan.grid, 64 * WAVES, LDS, s>>>(a);
+    if (const int rc = ta_allow_lds<tree_attend_kernel<T, DH, FAST, WAVES>>(LDS)) return rc;
+  tree_attend_kernel<T, DH, FAST, WAVES><<<plan.grid, 64 * WAVES, LDS, s>>>(a);
   return LA_OK;
 }
-template <typename T, int DH, int NT, int WAVES>
+template <typename T, int DH, int WAVES>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
-    if (a.dh == DH && a.page % 16 == 0) return ta_launch<T, DH, NT, true, WAVES>(a, plan, s);
-  return ta_launch<T, DH, NT, false, WAVES>(a, plan, s);
+    if (a.dh == DH && a.page % 16 == 0) return ta_launch<T, DH, true, WAVES>(a, plan, s);
+  return ta_launch<T, DH, false, WAVES>(a, plan, s);
 }
 template <typename T, int DH>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if constexpr (DH <= 128)
-    if (plan.waves == TA_WHOLE_WAVES) return ta_launch<T, DH, 1, TA_WHOLE_WAVES>(a, plan, s);
-  return ta_launch<T, DH, 1, TA_WAVES>(a, plan, s);
+    if (plan.waves == TA_WHOLE_WAVES) return ta_launch<T, DH, TA_WHOLE_WAVES>(a, plan, s);
+  return ta_launch<T, DH, TA_WAVES>(a, plan, s);
 }
 template <typename T>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
