@@ -387,7 +387,7 @@ int la_tree_layout(const int32_t *parent, const int32_t *first, const int32_t *l
 
 /* Attention of the rows over the pages of one layer, which hold K and V of the rows themselves already: out[i, h] = sum_t softmax_t(scale * q[i, h] . K[t, h / g]) V[t, h / g] over
  * t < len[r] and t = len[r] + j for the bits j < min(max_rows, first[r + 1] - first[r]) of vis[i].  q, out, table, scale, workspace: as for la_paged_attend; request r is row r of the table.
- * max_rows: rows of a request at most (1 to LA_MAX_ROWS; a request's rows behind them see nothing).  K and V are read once for 64 query heads and rows of a kv head, up to 512 where a block has as many.
+ * max_rows: rows of a request at most (1 to LA_MAX_ROWS; a request's rows behind them see nothing).  K and V are read once for 16, 64 or 128 pairs of a row and a query head of their kv head, by how many a block has.
  * A row of vis 0, rows of a request with len < 0 and rows of no request see nothing and get zeros; positions behind max_blocks * page_size, or whose table entry is not a page, are
  * not seen.  Whatever lies in places that a row does not see is not looked at, other rows' K and V of infinities or NaN among them.  Sums and rounding: as in la_paged_attend.
  * LA_EINVAL, LA_ENOMEM, LA_ERANGE: as there.  B = 0 does nothing. */

@@ -7,8 +7,13 @@ namespace la {
 
 constexpr int TA_WAVES = 4, TA_WHOLE_WAVES = 8;  // of a workgroup; where requests are not cut and workgroups are few
 
+// A row i of request r at position p sees the committed keys 0 .. len - 1 and row j of its block, at key len + j, where bit j of vis is set:
+//   out_i = sum_k w_k V_k / sum_k w_k,  w_k = 2^(log2(e) scale q_i K_k - m),  m a column's offset, which the factor cancels.
+// One pass over K and V: m follows the largest score (la_tree.h), the sum and the output's sums are rescaled when it moves.
 // A workgroup takes an item's keys for one kv head and 16 of its columns; column c of a kv head is query head c % g of the request's row c / g, so that those of a block of few rows lie
-// together.  The waves take blocks of KEYS keys in turn and meet once, at the end.  Products, types and pages as in la_attend.hip.
+// together and a small tree is one or two matrix operands wide.  The waves take blocks of KEYS keys in turn and meet once, at the end: no barrier in the loop, K and V straight to registers, the
+// next block's K asked for under this one's V.  Products, types and pages as in la_attend.hip.  Bound by latency: one tree of eight rows and two query heads a kv head at 500 keys, 10.2 us of
+// which a launch is 3.8; the rest is a chain of offset, page, K, V, and the waves' meeting.
 template <typename T, int DH, bool FAST, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -342,7 +347,8 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   }
 }
 
-// The items of a request's row and query head, in item order: a wave each, a lane takes up to four channels.
+// The items of a request's row and query head, in item order: a wave each, a lane takes up to four channels.  Eight records at a time are on their way, since a wave's reads are a chain (one after
+// the other 16 requests' join took 8 us, so 5).  Bound by the records' bytes where they are many: two requests of 64 rows at 65000 keys leave 34 KB an item and kv head, 10 us.
 constexpr int TA_JOIN_WAVES = 4;
 template <typename T, int PARTS>
 __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAttend a) {
@@ -399,8 +405,19 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 }
 
 // ---- host side ------------------------------------------------------------------------------------------
-constexpr int TA_FEW = 256, TA_WHOLE_WIDE = 256, TA_MANY = 64;
-constexpr size_t TA_RECORDS = (size_t)64 << 20;  // bytes of the items' records, which fewer items keep to
+// Which kernel, and what is cut; each rule with both sides as measured, in microseconds, 32 query heads of 128 channels unless said.
+// TA_FEW: where no request is cut and workgroups of 16 columns are no more than the CUs, eight waves share a workgroup's keys (1 tree of 8 rows at 500 keys: 11.7, with four waves 14.7; 1 of 16:
+//   13.5 and 16.4).  More than 32 columns, or more workgroups, go through LDS.
+// Wide from 17 columns: 1 x 8 rows at 1000, 11.7 and with the other kernel 14.4; at 2000, 13.7 and 16.2; 8 x 8 at 4000, 35.8 both.  At 16 columns and fewer three quarters of its waves would idle.
+constexpr int TA_FEW = 256;
+// Requests of up to 512 keys, if the table has no room for more, are left whole (16 x 16 rows at 400: 16.4, cut 21.4; 16 x 64 at 500: 35 and 46), float ones of up to 256 (3 x 8 at 500: cut 11.0,
+//   13.5 whole: their products are 1/16 as fast).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64
+//   workgroups: 18.6 whole and cut 16.5, but 4 x 32 at 600, 22.6 and 26.5).
+constexpr int TA_WHOLE_WIDE = 256, TA_MANY = 64;
+// Workgroups that items are cut for: a CU's one of 64 columns (256: 16 of 1 to 16 rows at up to 4096, 25.5; 384: 27.4; 512: 26.1; 32 x 16 rows at 2000, 62, 75 and 69), two of 128; at_workgroups'
+//   for the kernel above.
+// Bytes of the items' records at most; fewer items keep to it.  A record is written and read again: 4 us and 10 us at 34 KB an item and kv head of two requests of 64 rows.
+constexpr size_t TA_RECORDS = (size_t)64 << 20;
 struct TreePlan {
   int wide, waves, tiles, uncut, target, items;
   unsigned grid;

@@ -11,7 +11,8 @@ template <int DH> constexpr int TW_KEYS = DH <= 128 ? 64 : 32;  // of a stage
 template <int DH> constexpr int TW_STAGE = 2 * TW_KEYS<DH> * DH * 2;
 
 // 16 bytes a lane from base + offset to LDS at `to` + 16 lane.  In assembly, as is the wait for them: the compiler does not know which LDS reads they concern, and waits for all of them in
-// front of every transposing read; what it waits for of its own loads is then waited for with them, which is safe.  No register is written but m0, which nothing else here uses; the wait states are those between a vector instruction's write of a scalar and a load that takes it.
+// front of every transposing read; what it waits for of its own loads is then waited for with them, which is safe.
+// m0 is set anew by the compiler where it needs it, and is no register that it gives out (as a clobber it is refused).  The wait states are those between a vector instruction's write of a scalar and a load that takes it.
 __device__ __forceinline__ void tw_load(unsigned to, const char *base, unsigned offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
 }
@@ -30,6 +31,9 @@ __device__ __forceinline__ void tw_barrier() {
 // to add up but the items.  One barrier a stage: past it every wave's part of the stage is in, and nobody reads the stage any more that the next requests overwrite.
 // The 16-byte pieces of a row are permuted by its key, so that sixteen keys' equal pieces, and four keys' neighbouring ones, lie in different banks.  V's operand, eight keys of a channel in a
 // lane, comes out of LDS by transposing reads.
+// Bound by the matrix unit at long requests: two of 64 rows at 65000 keys, 32 query heads of 128 channels, are 205 GFLOP (137, and V's products with the weights' second numbers) in 223 us, 0.92
+// PFLOP/s where a large library product reaches 1.16; the weights' instructions run beside the other workgroup's products.  The next stage's scores in front of a stage's weights took 353, waves'
+// priorities changed nothing.  At 16 requests of 1 to 16 rows at 64 to 4096, 41 MB, 19 us: the chain to a workgroup's first stage, five stages, and 34 KB of sums out of it.
 template <typename T, int DH, int WAVES, int NT, int NS>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) {
   constexpr int KEYS = TW_KEYS<DH>, TILES = KEYS / 16, KP = DH / 32, DT = DH / 16, ROWB = DH * 2, HALF = KEYS * ROWB, STAGE = 2 * HALF;
@@ -335,7 +339,7 @@ static int tw_launch(const TreeAttend &a, unsigned grid, hipStream_t s) {
 }
 template <typename T, int DH>
 static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_t s) {
-  constexpr int NS = DH == 64 ? 4 : 2;  // (64 KB: two workgroups a CU)
+  constexpr int NS = DH == 64 ? 4 : 2;  // (64 KB: two workgroups a CU; four stages of 128 channels, one workgroup: 16 ragged requests 27.5 us, so 25.3)
   if (columns == 64) return tw_launch<T, DH, 4, 1, NS>(a, grid, s);
   if constexpr (DH <= 128) return tw_launch<T, DH, 4, 2, NS>(a, grid, s);
   else return tw_launch<T, DH, 8, 1, 4>(a, grid, s);
@@ -349,6 +353,7 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
 
 int tree_wide(int dtype, int head_dim, int page_size, int columns) {
   if (dtype == LA_F32 || page_size % 16 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
+  // (128 by four waves of 32, two workgroups a CU, and 256 by eight, one: 16 x 64 rows at 500 keys 28 us and 35, 1 x 64 19.6 and 22.6, 2 x 64 at 65000 244 and 237)
   return columns <= 64 ? 64 : 128;
 }
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s) {
