@@ -1,6 +1,4 @@
 // What stands between stored logits and the choice of a token: penalties for tokens that occurred, biases, a grammar's mask (la_logits_adjust).
-#include <limits.h>
-
 #include <type_traits>
 
 #include "la_device.h"
@@ -11,14 +9,14 @@ namespace la {
 
 // A workgroup per chunk of a row.  How often each of the chunk's tokens occurred is counted in LDS, from the request's committed tokens and those drafted on the row's path; then the
 // logits, requested before, pass once.  Counts are whole numbers and a token's biases are added in the list's order: results do not depend on the order of the atomics, nor on the chunks.
-// Bound by a chain (settings, history, LDS, division) at few rows, 5.0 us for one of 32768; by the bytes and that chain at many: 64 rows of 131072, 67.6 MB, 8192 tokens of history each, 19.4 us =
-// 3.5 TB/s, all workgroups resident and in step (64 registers; with 67 a fourth workgroup did not fit a CU: 22.4).  Loads and stores of four bytes, requested as they were needed, took 50; a
-// search through all biases by each token that has one 116 instead of 11.6 us where 300 fall on one row.
+// Bound by a chain (settings, history, LDS, division) at few rows, 4.8 us for one of 32768; by the bytes and that chain at many: 64 rows of 131072, 67.6 MB, 8192 tokens of history each, 19.2 us =
+// 3.5 TB/s, all workgroups resident and in step (64 registers; with 67 a fourth workgroup did not fit a CU: 22.4).  16 bytes at a time wherever a row begins: 64 rows of 100001 in bfloat16, rows
+// at every second byte, 15 us, as rows of 100000; element by element 23, and without asking for all of them first 50.
+// 300 biases for nine rows of 1731: 6.2 us; as a search through the list by each token that has one 80.
 constexpr int ADJ_THREADS = 512;
 constexpr int ADJ_PER = 16, ADJ_PER_SHORT = 4;  // tokens of a thread: chunks of 8192 and of 2048
-constexpr int ADJ_LIST = 256;                   // biases of a chunk that are kept in LDS
 constexpr int ADJ_FEW = 1024;                   // short chunks of a launch at most
-constexpr unsigned ADJ_SEEN = 1u << 31, ADJ_BIASED = 1u << 30, ADJ_COUNT = ADJ_BIASED - 1;  // a token's word: occurred in the prompt; has a bias; times it was emitted
+constexpr unsigned ADJ_SEEN = 1u << 31, ADJ_COUNT = ADJ_SEEN - 1;  // a token's word: occurred in the prompt; times it was emitted
 
 struct Adjust {
   const void *x;
@@ -34,14 +32,15 @@ __device__ __forceinline__ T adjust_round(float f) {  // (float_to_bf16 takes fi
   else return (T)f;
 }
 
-// VEC: rows are 16-byte aligned, a thread has 16 bytes at a time.
-template <typename T, int PER, bool VEC>
+template <typename T, int PER>
 __global__ __launch_bounds__(ADJ_THREADS, 8) void logits_adjust_kernel(Adjust a) {
   constexpr int CHUNK = ADJ_THREADS * PER, G = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER, GROUPS = PER / G;  // tokens of a group; groups of a thread
-  typedef T __attribute__((ext_vector_type(G))) group;
+  typedef T __attribute__((ext_vector_type(G), aligned(sizeof(T)))) group;  // (rows begin at any number)
   __shared__ __attribute__((aligned(16))) unsigned word[CHUNK];
-  __shared__ int list_token[ADJ_LIST], list_at[ADJ_LIST], n_list;
-  __shared__ float list_bias[ADJ_LIST], list_x[ADJ_LIST];
+  __shared__ __attribute__((aligned(16))) unsigned seen[3 * CHUNK / 32];  // a bit a token: has a bias; has more than one, or one of an earlier turn; its word is its logit with biases
+  __shared__ int entry[ADJ_THREADS];
+  __shared__ float entry_bias[ADJ_THREADS];
+  unsigned *twice = seen + CHUNK / 32, *done = twice + CHUNK / 32;
   const int b = blockIdx.y, t = threadIdx.x, v0 = blockIdx.x * CHUNK, n = a.V - v0 < CHUNK ? a.V - v0 : CHUNK;
   const la_adjust &p = a.p;
   const T *x = (const T *)a.x + b * a.ldx + v0;
@@ -51,7 +50,7 @@ __global__ __launch_bounds__(ADJ_THREADS, 8) void logits_adjust_kernel(Adjust a)
 #pragma unroll
   for (int j = 0; j < GROUPS; ++j) {
     const int at = (j * ADJ_THREADS + t) * G;
-    if (VEC && at + G <= n) {
+    if (at + G <= n) {
       const group v = *(const group *)(x + at);
 #pragma unroll
       for (int i = 0; i < G; ++i) in[j][i] = v[i];
@@ -62,30 +61,29 @@ __global__ __launch_bounds__(ADJ_THREADS, 8) void logits_adjust_kernel(Adjust a)
   }
   const int r = uniform(p.req ? p.req[b] : b);
   const bool known = (unsigned)r < (unsigned)p.n_requests;
-  unsigned mask[GROUPS];  // a group's bits, from bit 0 on
-#pragma unroll
-  for (int j = 0; j < GROUPS; ++j) mask[j] = ~0u;
-  const uint32_t *allowed = nullptr;
+  unsigned mask = ~0u;  // a group's bits are those from bit j G on
   if (p.allowed) {
     const int m = uniform(p.allowed_index ? p.allowed_index[b] : b);
     if ((unsigned)m < (unsigned)p.n_allowed) {
-      allowed = p.allowed + m * p.allowed_stride;
+      const uint32_t *allowed = p.allowed + m * p.allowed_stride;
+      mask = 0;
 #pragma unroll
       for (int j = 0; j < GROUPS; ++j) {
         const int at = v0 + (j * ADJ_THREADS + t) * G;
-        mask[j] = allowed[(at < a.V ? at : 0) >> 5] >> (at & 31);  // (a group lies in one word)
+        mask |= (allowed[(at < a.V ? at : 0) >> 5] >> (at & 31) & ((1u << G) - 1)) << (j * G);  // (a group lies in one word)
       }
     }
   }
   auto setting = [&](const float *f, float off, bool positive) {  // (what is no number, or no factor, is off)
     const float v = f && known ? f[r] : off;
-    return v - v == 0.f && (!positive || v > 0.f) ? v : off;
+    return __uint_as_float(uniform((int)__float_as_uint(v - v == 0.f && (!positive || v > 0.f) ? v : off)));
   };
   const float rho = setting(p.repetition, 1.f, true), beta = setting(p.presence, 0.f, false), alpha = setting(p.frequency, 0.f, false);
   const bool counts = rho != 1.f || beta != 0.f || alpha != 0.f, biases = known && p.n_bias > 0;
   if (uniform(counts || biases)) {
     for (int i = 4 * t; i < CHUNK; i += 4 * ADJ_THREADS) *(uint4 *)(word + i) = uint4{0, 0, 0, 0};
-    if (t == 0) n_list = 0;
+    if (biases)
+      for (int i = t; i < 3 * CHUNK / 32; i += ADJ_THREADS) seen[i] = 0;
     __syncthreads();
     if (counts && p.tokens) {
       const int32_t *tokens = p.tokens + r * p.tokens_stride;
@@ -109,19 +107,6 @@ __global__ __launch_bounds__(ADJ_THREADS, 8) void logits_adjust_kernel(Adjust a)
       const int d = row >= 0 && row < a.B ? p.draft[row] : -1, v = d - v0;
       if (d >= v0 && v < n) atomicAdd(&word[v], 1u);
     }
-    if (biases)
-      for (int i = t; i < p.n_bias; i += ADJ_THREADS) {
-        const int d = p.bias_token[r * p.bias_stride + i], v = d - v0;
-        if (d < v0 || v >= n) continue;
-        atomicOr(&word[v], ADJ_BIASED);
-        const int at = atomicAdd(&n_list, 1);
-        if (at < ADJ_LIST) {
-          list_token[at] = v;
-          list_at[at] = i;
-          list_bias[at] = p.bias[r * p.bias_stride + i];
-          list_x[at] = load_as_float<T>(x + v);  // (nobody writes before the barrier)
-        }
-      }
     __syncthreads();
   }
   auto penalized = [&](float f, unsigned w) {
@@ -129,58 +114,54 @@ __global__ __launch_bounds__(ADJ_THREADS, 8) void logits_adjust_kernel(Adjust a)
     if (counts && w & (ADJ_SEEN | ADJ_COUNT)) f = f > 0.f ? f / rho : f * rho;
     return counts && c ? f - alpha * (float)c - beta : f;
   };
-  // Tokens with biases: the thread of the first of a token's entries adds them all up, in the list's order, and stores the token; everybody else leaves it out.  More entries than LDS has room
-  // for: the tokens' own threads go through the whole list.
-  const bool listed = uniform(biases) && n_list <= ADJ_LIST;
-  if (listed && t < n_list) {
-    const int v = list_token[t], at = list_at[t];
-    bool own = true, more = false;
-    for (int k = 0; k < n_list; ++k)
-      if (list_token[k] == v && k != t) {
-        more = true;
-        own = own && list_at[k] > at;
-      }
-    if (own) {
-      float f = penalized(list_x[t], word[v]) + list_bias[t];
-      for (int last = at; more;) {
-        int next = INT_MAX;
-        float add = 0.f;
-        for (int k = 0; k < n_list; ++k)
-          if (list_token[k] == v && list_at[k] > last && list_at[k] < next) {
-            next = list_at[k];
-            add = list_bias[k];
-          }
-        if (next == INT_MAX) break;
-        f += add;
-        last = next;
-      }
-      if (allowed && !(allowed[(v0 + v) >> 5] >> ((v0 + v) & 31) & 1)) f = -INFINITY;
-      y[v] = adjust_round<T>(f);
+  // Biases, a turn of the threads with an entry of the list each: the first entry's thread of a token adds them all to its logit, in the list's order, and leaves the sum in the token's word.
+  // Only where a token's bit was set before can there be more of them to look for.
+#pragma unroll 1
+  for (int i0 = 0; biases && i0 < p.n_bias; i0 += ADJ_THREADS) {
+    const int i = i0 + t, left = p.n_bias - i0 < ADJ_THREADS ? p.n_bias - i0 : ADJ_THREADS;
+    const int d = t < left ? p.bias_token[r * p.bias_stride + i] : -1, v = d >= v0 && d - v0 < n ? d - v0 : -1;
+    const unsigned bit = 1u << (v & 31);
+    float logit = 0.f, bias = 0.f;
+    if (v >= 0) {
+      bias = p.bias[r * p.bias_stride + i];
+      logit = load_as_float<T>(x + v);  // (nobody writes before the last turn)
+      if (atomicOr(&seen[v >> 5], bit) & bit) atomicOr(&twice[v >> 5], bit);
     }
+    entry[t] = v;
+    entry_bias[t] = bias;
+    __syncthreads();
+    if (v >= 0) {
+      const bool more = twice[v >> 5] & bit;
+      bool own = true;
+#pragma unroll 4
+      for (int k = 0; more && k < t; ++k) own = own && entry[k] != v;
+      if (own) {
+        float f = (done[v >> 5] & bit ? __uint_as_float(word[v]) : penalized(logit, word[v])) + bias;
+#pragma unroll 4
+        for (int k = t + 1; more && k < left; ++k)
+          if (entry[k] == v) f += entry_bias[k];
+        word[v] = __float_as_uint(f);
+        atomicOr(&done[v >> 5], bit);
+      }
+    }
+    __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < GROUPS; ++j) {
     const int at = (j * ADJ_THREADS + t) * G;
     if (at >= n) continue;
     T out[G];
-    unsigned whose = 0;  // bit i: token i is stored by another thread
+    const unsigned biased = biases ? done[at >> 5] >> (at & 31) : 0u;  // (a group lies in one word)
 #pragma unroll
     for (int i = 0; i < G; ++i) {
       float f = load_as_float<T>(&in[j][i]);
-      const unsigned w = counts || biases ? word[at + i] : 0;
-      if (w) {
-        f = penalized(f, w);
-        if (w & ADJ_BIASED) {
-          if (listed) whose |= 1u << i;
-          else
-            for (int k = 0; k < p.n_bias; ++k)
-              if (p.bias_token[r * p.bias_stride + k] == v0 + at + i) f += p.bias[r * p.bias_stride + k];
-        }
-      }
-      if (!(mask[j] >> i & 1)) f = -INFINITY;
+      const unsigned w = counts || biases ? word[at + i] : 0u;
+      if (biased >> i & 1) f = __uint_as_float(w);
+      else if (w) f = penalized(f, w);
+      if (!(mask >> (j * G + i) & 1)) f = -INFINITY;
       out[i] = adjust_round<T>(f);
     }
-    if (VEC && at + G <= n && !whose) {
+    if (at + G <= n) {
       group v;
 #pragma unroll
       for (int i = 0; i < G; ++i) v[i] = out[i];
@@ -188,22 +169,20 @@ __global__ __launch_bounds__(ADJ_THREADS, 8) void logits_adjust_kernel(Adjust a)
     } else {
 #pragma unroll
       for (int i = 0; i < G; ++i)
-        if (at + i < n && !(whose >> i & 1)) y[at + i] = out[i];
+        if (at + i < n) y[at + i] = out[i];
     }
   }
 }
 
 template <typename T>
 static void adjust_launch(const Adjust &a, hipStream_t s) {
-  const bool vec = ((uintptr_t)a.x | (uintptr_t)a.y) % 16 == 0 && (a.B == 1 || (a.ldx * sizeof(T) % 16 == 0 && a.ldy * sizeof(T) % 16 == 0));
-  auto launch = [&](auto per, auto v) {
+  auto launch = [&](auto per) {
     constexpr int PER = decltype(per)::value;
-    logits_adjust_kernel<T, PER, decltype(v)::value><<<dim3(ceil_div(a.V, ADJ_THREADS * PER), a.B), ADJ_THREADS, 0, s>>>(a);
+    logits_adjust_kernel<T, PER><<<dim3(ceil_div(a.V, ADJ_THREADS * PER), a.B), ADJ_THREADS, 0, s>>>(a);
   };
-  auto sized = [&](auto per) { vec ? launch(per, std::true_type{}) : launch(per, std::false_type{}); };
   // Short chunks while they are no more than the chip takes at once: more workgroups, each of which looks through the whole history.  us, short / long: one row of 32768 5.6 / 8.2, one of 100001
   // 7.1 / 11.5, 64 of 32768 10.1 / 11.3, 16 of 131072 in bfloat16 8.5 / 9.1, 64 of 131072 27.3 / 20.8.
-  (long long)a.B * ceil_div(a.V, ADJ_THREADS * ADJ_PER_SHORT) <= ADJ_FEW ? sized(std::integral_constant<int, ADJ_PER_SHORT>{}) : sized(std::integral_constant<int, ADJ_PER>{});
+  (long long)a.B * ceil_div(a.V, ADJ_THREADS * ADJ_PER_SHORT) <= ADJ_FEW ? launch(std::integral_constant<int, ADJ_PER_SHORT>{}) : launch(std::integral_constant<int, ADJ_PER>{});
 }
 
 }  // namespace la

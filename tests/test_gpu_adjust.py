@@ -144,6 +144,19 @@ def test_adjust_numbers_that_are_none(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V,n_bias", [(1731, 300), (600, 1300), (3, 513), (10111, 512), (2049, 511), (8200, 1025)])
+def test_adjust_more_biases_than_one_turn_takes(dtype, V, n_bias):
+    """Lists longer than the threads of a workgroup, tokens that are in several parts of them, rows of odd lengths beside each other."""
+    rng = random.Random(V)
+    how = make(rng, V, 4, 3, history=150, n_bias=n_bias, masks=2)
+    x = (torch.randn((4, V), generator=torch.Generator().manual_seed(V)) * 3).to(T[dtype]).cuda()
+    got = go(x, **how)
+    check(x, got, how)
+    go(x, out=x, **how)
+    assert torch.equal(x, got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("V,pad,at", [(1000, 24, 0), (1000, 1, 0), (1000, 24, 3), (4099, 5, 1), (50000, 16, 8)])
 def test_adjust_strides_alignment_and_in_place(dtype, V, pad, at):
     rng = random.Random(V)
