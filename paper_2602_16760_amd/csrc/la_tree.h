@@ -129,7 +129,7 @@ int ta_allow_lds(int bytes) {
   return LA_OK;
 }
 
-// The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 16 positions, head_dim of 64, 128 or 256.
+// The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 8 positions, head_dim of 64, 96, 128 or 256.
 int tree_wide(int dtype, int head_dim, int page_size, int columns);  // columns of a workgroup; 0: it is not for this shape
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s);
 

@@ -8,7 +8,8 @@ namespace la {
 typedef short __attribute__((ext_vector_type(4))) tw_s4;
 
 template <int DH> constexpr int TW_KEYS = DH <= 128 ? 64 : 32;  // of a stage
-template <int DH> constexpr int TW_STAGE = 2 * TW_KEYS<DH> * DH * 2;
+template <int DH> constexpr int TW_PITCH = DH <= 64 ? 128 : DH <= 128 ? 256 : 512;  // bytes of a row in LDS
+template <int DH> constexpr int TW_STAGE = 2 * TW_KEYS<DH> * TW_PITCH<DH>;
 
 // 16 bytes a lane from base + offset to LDS at `to` + 16 lane.  In assembly, as is the wait for them: the compiler does not know which LDS reads they concern, and waits for all of them in
 // front of every transposing read; what it waits for of its own loads is then waited for with them, which is safe.
@@ -36,10 +37,10 @@ __device__ __forceinline__ void tw_barrier() {
 // priorities changed nothing.  At 16 requests of 1 to 16 rows at 64 to 4096, 41 MB, 19 us: the chain to a workgroup's first stage, five stages, and 34 KB of sums out of it.
 template <typename T, int DH, int WAVES, int NT, int NS>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) {
-  constexpr int KEYS = TW_KEYS<DH>, TILES = KEYS / 16, KP = DH / 32, DT = DH / 16, ROWB = DH * 2, HALF = KEYS * ROWB, STAGE = 2 * HALF;
-  constexpr int PPR = ROWB / 16, KPI = 1024 / ROWB;          // pieces of a row; rows of a request
+  constexpr int KEYS = TW_KEYS<DH>, TILES = KEYS / 16, KP = DH / 32, DT = DH / 16, ROWB = DH * 2, PITCH = TW_PITCH<DH>, HALF = KEYS * PITCH, STAGE = 2 * HALF;
+  constexpr int PPR = PITCH / 16, KPI = 1024 / PITCH;        // pieces of a row; rows of a request
   constexpr int LPW = STAGE / 1024 / WAVES, HALF_N = HALF / 1024;  // a wave's requests of a stage; requests of its K
-  constexpr int WINDOW = 64 / TILES;                         // stages whose tiles a wave's lanes look up at once
+  constexpr int EIGHTS = KEYS / 8, WINDOW = 64 / EIGHTS;     // page boundaries lie between eights of keys; stages whose eights a wave's lanes look up at once
   constexpr float UP = TA_UP<T>, LAZY = TA_LAZY<T>;
   static_assert(LPW * WAVES * 1024 == STAGE && (NS - 1) * LPW <= 63, "requests");
   extern __shared__ __attribute__((aligned(1024))) uint8_t tw_lds[];
@@ -73,16 +74,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
   }
   const float to_log2 = fabsf(a.scale) * AT_LOG2E;
   const int32_t *tab = a.table + it.r * a.ldt;
-  // Lane i: where tile i of the next WINDOW stages' lies (the first page where it lies in none: its keys are not seen, whatever they hold).
+  // Lane i: where eight keys, the i-th of the next WINDOW stages', lie (the first page where they lie in none: they are not seen, whatever they hold).
   unsigned off_lo = 0, off_hi = 0;
-  unsigned long long paged = 0, paged_next = 0;  // bit i: tile i lies in a page
-  auto look_up = [&](int stage) {
-    const long long key = k_first + (long long)KEYS * stage + 16 * lane;
-    long long at = -1;
-    if (key < k_end) {
-      const int block = (int)key / a.page, pg = tab[block];
-      if ((unsigned)pg < (unsigned)a.n_pages) at = (((long long)pg * a.Hkv + h) * a.page + ((int)key - block * a.page)) * ROWB;
-    }
+  unsigned long long paged = 0, paged_next = 0;  // bit i: they lie in a page
+  int next_page, next_place;
+  auto ask = [&](int stage) {  // for the window from this stage on: the entry is here when the stage before that has been waited for
+    const long long key = k_first + (long long)KEYS * stage + 8 * lane;
+    const int k = key < k_end ? (int)key : k_end - 1, block = k / a.page;
+    next_page = tab[block];
+    next_place = key < k_end ? k - block * a.page : -1;
+  };
+  auto look_up = [&]() {
+    long long at = next_place >= 0 && (unsigned)next_page < (unsigned)a.n_pages ? (((long long)next_page * a.Hkv + h) * a.page + next_place) * ROWB : -1;
     paged_next = __ballot(at >= 0);
     at = at < 0 ? 0 : at;
     off_lo = (unsigned)at;
@@ -90,21 +93,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
   };
   auto swz_k = [](int key) { return DH == 64 ? (key >> 1) & 7 : key & 15; };
   auto swz_v = [](int key) { return DH == 64 ? 2 * ((key >> 1) & 3) : 2 * (key & 7); };
-  // what this wave brings of a stage: requests wave LPW .., the first HALF_N of a stage are K's
+  // what this wave brings of a stage: requests wave LPW .., the first HALF_N of a stage are K's (places behind a row's end hold its pieces again; nothing reads them as channels)
   unsigned voff[LPW];
 #pragma unroll
   for (int i = 0; i < LPW; ++i) {
-    const int n = wave * LPW + i, key = n % HALF_N * KPI % 16 + lane / PPR;
-    voff[i] = (unsigned)(key * ROWB + (lane % PPR ^ (n < HALF_N ? swz_k(key) : swz_v(key))) * 16);
+    const int n = wave * LPW + i, key = n % HALF_N * KPI % 16 + lane / PPR, piece = lane % PPR ^ (n < HALF_N ? swz_k(key) : swz_v(key));
+    voff[i] = (unsigned)(key % 8 * ROWB + piece % (ROWB / 16) * 16);
   }
   int nx = 0;
   unsigned nx_slot = 0;
   auto request = [&]() {
     if (nx < n_stages) {
-      if (nx > 0 && nx % WINDOW == 0) look_up(nx);
+      if (nx > 0 && nx % WINDOW == 0) {
+        look_up();
+        ask(nx + WINDOW);
+      }
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
-        const int n = wave * LPW + i, l = nx % WINDOW * TILES + n % HALF_N * KPI / 16;
+        const int n = wave * LPW + i, l = nx % WINDOW * EIGHTS + n % HALF_N * KPI / 8;
         const long long at = (long long)(unsigned)__builtin_amdgcn_readlane((int)off_lo, l) | (long long)__builtin_amdgcn_readlane((int)off_hi, l) << 32;
         tw_load(lds0 + nx_slot + (unsigned)n * 1024u, (const char *)(n < HALF_N ? a.K : a.V) + at, voff[i]);
       }
@@ -121,13 +127,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
     m_run[t] = -INFINITY;
     l_run[t] = 0.f;
   }
-  look_up(0);
+  ask(0);
+  look_up();
+  ask(WINDOW);
   __builtin_amdgcn_s_waitcnt(0xf70);  // (vmcnt(0): q is in, and the compiler knows it)
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i) request();
-  const unsigned rd_k = (unsigned)(c16 * ROWB) + (unsigned)((q4 ^ swz_k(c16)) * 16);  // piece 4 p + q4 of key c16 of a tile: ^ 64 p
+  const unsigned rd_k = (unsigned)(c16 * PITCH) + (unsigned)((q4 ^ swz_k(c16)) * 16);  // piece 4 p + q4 of key c16 of a tile: ^ 64 p
   const int v_key = 4 * q4 + (c16 >> 2);
-  const unsigned rd_v = (unsigned)(HALF + v_key * ROWB + (((c16 >> 1) & 1) ^ swz_v(v_key)) * 16 + 8 * (c16 & 1));  // channels 16 d ..: ^ 32 d
+  const unsigned rd_v = (unsigned)(HALF + v_key * PITCH + (((c16 >> 1) & 1) ^ swz_v(v_key)) * 16 + 8 * (c16 & 1));  // channels 16 d ..: ^ 32 d
   LDS_AS unsigned *odd_lds = (LDS_AS unsigned *)(uintptr_t)(lds0 + NS * STAGE);
   unsigned long long odd_rows = 0;  // drafted rows, of those whose keys this item has, whose V has an infinity or NaN
   unsigned slot = 0;
@@ -141,9 +149,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
     const int key0 = k_first + KEYS * i;
     // keys of the stage that lie in a page, in front of the item's end
     constexpr unsigned long long ALL = KEYS == 64 ? ~0ull : (1ull << (KEYS & 63)) - 1;
-    unsigned long long now = 0;
+    const unsigned in = (unsigned)(paged >> (i % WINDOW * EIGHTS)) & ((1u << EIGHTS) - 1u);
+    unsigned long long now = ALL;
+    if (in != (1u << EIGHTS) - 1u)
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) now |= paged >> (i % WINDOW * TILES + t) & 1 ? 0xffffull << (16 * t) : 0ull;
+      for (int t = 0; t < EIGHTS; ++t) now &= in >> t & 1 ? ~0ull : ~(0xffull << (8 * t));
     if (k_end - key0 < KEYS) now &= (1ull << (k_end - key0)) - 1;
     const bool drafted = (long long)key0 + KEYS > L;  // keys of the request's own rows among them
     const unsigned base = lds0 + slot;
@@ -178,7 +188,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
       at_u4 kf[2][TILES];
       auto read_k = [&](int k) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) kf[k & 1][t] = *(LDS_AS const at_u4 *)(uintptr_t)((base + (rd_k ^ (unsigned)(64 * k))) + (unsigned)(16 * t * ROWB));
+        for (int t = 0; t < TILES; ++t) kf[k & 1][t] = *(LDS_AS const at_u4 *)(uintptr_t)((base + (rd_k ^ (unsigned)(64 * k))) + (unsigned)(16 * t * PITCH));
       };
       read_k(0);
 #pragma unroll
@@ -244,15 +254,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
       }
     }
     {
-      constexpr int DG = 4, GROUPS = TILES / 2 * DT / DG;  // V's fragments of four tiles of channels at a time, the next ones on their way
+      constexpr int DG = DT % 4 ? 3 : 4, GROUPS = TILES / 2 * DT / DG;  // V's fragments of some tiles of channels at a time, the next ones on their way
       at_u4 vf[2][DG];
       auto read_v = [&](int x) {
         const int m = x * DG / DT, d0 = x * DG % DT;
 #pragma unroll
         for (int y = 0; y < DG; ++y) {
-          const unsigned at = base + (rd_v ^ (unsigned)(32 * (d0 + y))) + (unsigned)(32 * m * ROWB);
+          const unsigned at = base + (rd_v ^ (unsigned)(32 * (d0 + y))) + (unsigned)(32 * m * PITCH);
           const at_u2 lo = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)at));
-          const at_u2 hi = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + 16u * ROWB)));
+          const at_u2 hi = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + 16u * PITCH)));
           vf[x & 1][y] = at_u4{lo[0], lo[1], hi[0], hi[1]};
         }
       };
@@ -347,12 +357,13 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
 template <typename T>
 static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_t s) {
   if (a.dh == 64) return tw_launch<T, 64>(a, columns, grid, s);
+  if (a.dh == 96) return tw_launch<T, 96>(a, columns, grid, s);
   if (a.dh == 128) return tw_launch<T, 128>(a, columns, grid, s);
   return tw_launch<T, 256>(a, columns, grid, s);
 }
 
 int tree_wide(int dtype, int head_dim, int page_size, int columns) {
-  if (dtype == LA_F32 || page_size % 16 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
+  if (dtype == LA_F32 || page_size % 8 || (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256)) return 0;
   // (128 by four waves of 32, two workgroups a CU, and 256 by eight, one: 16 x 64 rows at 500 keys 28 us and 35, 1 x 64 19.6 and 22.6, 2 x 64 at 65000 244 and 237)
   return columns <= 64 ? 64 : 128;
 }
