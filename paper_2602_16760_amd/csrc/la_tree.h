@@ -130,7 +130,7 @@ int ta_allow_lds(int bytes) {
 }
 
 // The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 8 positions, head_dim of 64, 96, 128 or 256.
-int tree_wide(int dtype, int head_dim, int page_size, int columns);  // columns of a workgroup; 0: it is not for this shape
+bool tree_wide(int dtype, int head_dim, int page_size);  // whether it is for this shape; then 64 or 128 columns of a workgroup
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s);
 
 }  // namespace la

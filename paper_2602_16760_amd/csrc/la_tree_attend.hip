@@ -414,8 +414,13 @@ constexpr int TA_FEW = 256;
 //   13.5 whole: their products are 1/16 as fast).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64
 //   workgroups: 18.6 whole and cut 16.5, but 4 x 32 at 600, 22.6 and 26.5).
 constexpr int TA_WHOLE_WIDE = 256, TA_MANY = 64;
-// Workgroups that items are cut for: a CU's one of 64 columns (256: 16 of 1 to 16 rows at up to 4096, 25.5; 384: 27.4; 512: 26.1; 32 x 16 rows at 2000, 62, 75 and 69), two of 128; at_workgroups'
-//   for the kernel above.
+// 128 columns a workgroup rather than 64 (K and V pass through LDS half as often) where one of 512 then has this many keys, if all requests are as long as the table: 4 x 64 rows at 500, 128
+//   columns 26.4 and 64 20.0, 1 x 40 at 3000, 28.9 and 23.5, 4 x 64 at 4000, 512 keys, 49.9 and 48.3, 4 x 40 of three heads of 96 channels at 16000, 930 keys, 57.4 and 64.5, 16 x 64 at 4000,
+//   2000 keys, 129 and 134, 4 x 64 at 16000, 119 and 134, 2 x 64 at 65000, 230 and 284.  Heads of 256 channels: 128 always (8 x 33 at 2000, 38.4 and 44.0).
+constexpr int TA_LONG = 768;
+// Workgroups that items are cut for: one of 64 columns a CU (16 of 1 to 16 rows at up to 4096, 25.5; 384 of them 27.4, 512 26.1; 32 x 16 rows at 2000 62, 75 and 69), or two where a request has
+//   several and each keeps TA_SHARE keys (1 x 64 rows of 64 heads at 8000: 48.1, one 54.9; 1 x 40 at 3000, 117 keys: 23.5 and 21.9); two of 128; at_workgroups' for the kernel above.
+constexpr int TA_SHARE = 256;
 // Bytes of the items' records at most; fewer items keep to it.  A record is written and read again: 4 us and 10 us at 34 KB an item and kv head of two requests of 64 rows.
 constexpr size_t TA_RECORDS = (size_t)64 << 20;
 struct TreePlan {
@@ -423,23 +428,24 @@ struct TreePlan {
   unsigned grid;
   size_t notes, list, bytes;
 };
-// Kernel, columns of a workgroup and workgroups of an item and kv head.
-static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, bool whole) {
+// Kernel, columns of a workgroup and workgroups of an item and kv head; how many items are resident at once.  cap: positions that the table has room for.
+static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, long long cap) {
   TreePlan r{};
   const int columns = Hq / p.n_kv_heads * max_rows;
-  const bool few = whole && p.head_dim <= 128 && columns <= 32 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW;
-  r.wide = columns > 16 && !few ? tree_wide(p.dtype, p.head_dim, p.page_size, columns) : 0;
+  const bool few = cap <= AT_WHOLE && p.head_dim <= 128 && columns <= 32 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW;
+  const double share = (double)R * p.n_kv_heads * columns * (double)cap / 512;  // columns times keys of one of 512 workgroups
+  if (columns > 16 && !few && tree_wide(p.dtype, p.head_dim, p.page_size)) r.wide = columns > 64 && (p.head_dim > 128 || share >= 128. * TA_LONG) ? 128 : 64;
   r.waves = few ? TA_WHOLE_WAVES : TA_WAVES;
   r.tiles = ceil_div(columns, r.wide ? r.wide : 16);
+  const int groups = !r.wide ? at_workgroups(p.head_dim) : p.head_dim <= 128 && (r.wide == 128 || (r.tiles > 1 && share >= 64. * TA_SHARE)) ? 512 : 256;
+  r.target = std::max(1, groups / (p.n_kv_heads * r.tiles));
   return r;
-}
-static int ta_target(const TreePlan &r, const la_pages_desc &p) {
-  const int groups = !r.wide ? at_workgroups(p.head_dim) : r.wide == 128 && p.head_dim <= 128 ? 512 : 256;
-  return std::max(1, groups / (p.n_kv_heads * r.tiles));
 }
 static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, int max_rows) {
   const long long cap = (long long)max_blocks * p.page_size;
-  TreePlan r = ta_shape(p, Hq, max_rows, R, cap <= AT_WHOLE);
+  TreePlan r = ta_shape(p, Hq, max_rows, R, cap);
+  const int target = r.target;
+  r.target = 0;
   r.uncut = r.wide && (long long)R * p.n_kv_heads * r.tiles < TA_MANY ? TA_WHOLE_WIDE : p.dtype == LA_F32 ? AT_WHOLE / 2 : AT_WHOLE;
   const bool whole = cap <= r.uncut;
   if (!whole) r.waves = TA_WAVES;
@@ -447,7 +453,7 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
   if (!whole) {
     const size_t record = (size_t)Hq * max_rows * (p.head_dim + 4) * 4;
     const long long pieces = R * ((cap + AT_PIECE - 1) / AT_PIECE);
-    for (r.target = ta_target(r, p);; r.target = r.target * 3 / 4) {
+    for (r.target = target;; r.target = r.target * 3 / 4) {
       const int cut = (2 * R > r.target ? AT_FINE : 1) * r.target;
       r.items = (int)std::min((long long)cut + R, pieces);
       r.bytes = std::min(r.items, 2 * cut) * record;  // (of requests that are cut: fewer than `cut`, with one item more than their share of `cut` each)
@@ -530,11 +536,11 @@ static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) 
 size_t tree_attend_bytes(const la_pages_desc &p, int Hq) {
   size_t most = 0;
   la_pages_desc d = p;
-  for (int page : {16, 17})  // (a page size that the wide kernel takes, one that it does not)
+  for (int page : {16, 17})  // (a page size that the wide kernel takes, one that it does not; the longest table, for which the most items are resident)
     for (int rows = 1; rows <= LA_MAX_ROWS; ++rows) {
       d.page_size = page;
       const size_t record = (size_t)Hq * rows * (p.head_dim + 4) * 4;
-      most = std::max(most, std::min(2 * AT_FINE * (size_t)ta_target(ta_shape(d, Hq, rows, 1, false), d), std::max(TA_RECORDS / record, (size_t)2 * AT_FINE)) * record);
+      most = std::max(most, std::min(2 * AT_FINE * (size_t)ta_shape(d, Hq, rows, 1, 1ll << 62).target, std::max(TA_RECORDS / record, (size_t)2 * AT_FINE)) * record);
     }
   return most + LA_MAX_ROWS * sizeof(int2);
 }
