@@ -388,6 +388,20 @@ def test_attend_pages_that_are_none(dtype, page):
     c.check(out, skip=lambda r, t: (r == 0 and t // page == 1) or r == 1 or (r == 2 and t // page == 0))
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh", [("bf16", 8, 2, 128), ("f16", 12, 2, 96), ("bf16", 16, 4, 64), ("f16", 6, 1, 256)])
+@pytest.mark.parametrize("page", [8, 16, 24, 40])
+@pytest.mark.parametrize("cap", [0, 30000, 300000])
+def test_attend_pages_of_eights_and_long_tables(dtype, Hq, Hkv, dh, page, cap):
+    """Blocks of many columns whose stages of keys begin, end and change pages at any eight positions; the table's length decides how many columns share K and V, and how requests are cut.  A page
+    of each long request is none."""
+    lens, counts = [0, 1500, 333, 700, 8], [64, 60, 17, 33, 5]
+    c = Case(dtype, Hq, Hkv, dh, page, lens, counts, seed=page + cap, blocks=cap // page or None)
+    c.table[1, 3], c.table[3, 0] = -1, 1 << 30
+    out = c.run()
+    c.check(out, skip=lambda r, t: (r == 1 and t // page == 3) or (r == 3 and t < page))
+    assert torch.equal(out, c.run())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 8.0])
 def test_attend_other_scales(dtype, scale):
@@ -399,10 +413,19 @@ def test_attend_other_scales(dtype, scale):
                                                         ("bf16", 4, 1, 256, 32, 1000), ("f16", 4, 1, 128, 16, 50)])
 def test_attend_values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx):
     """K and V of infinities and NaN in a drafted row reach the rows that see it, in their own channels, and no other row."""
+    values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,ctx", [("bf16", 8, 2, 128, 16, 1500), ("f16", 8, 2, 128, 8, 100), ("f16", 16, 2, 96, 24, 700), ("bf16", 4, 1, 64, 40, 900), ("f16", 8, 1, 256, 8, 300)])
+def test_attend_values_that_other_rows_do_not_see_in_a_long_table(dtype, Hq, Hkv, dh, page, ctx):
+    values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx, blocks=(1 << 18) // page)
+
+
+def values_that_other_rows_do_not_see(dtype, Hq, Hkv, dh, page, ctx, blocks=None):
     n = 40
     parent = [0, 0, 1, 0, 3, 0, 5, 6] + [0] * (n - 8)  # rows 2, 4 and 7 end three branches
     masks = [m for _, m in paths(parent)]
-    c = Case(dtype, Hq, Hkv, dh, page, [ctx, 20], [n, 4], masks=[masks, [1, 3, 5, 7]])
+    c = Case(dtype, Hq, Hkv, dh, page, [ctx, 20], [n, 4], blocks=blocks, masks=[masks, [1, 3, 5, 7]])
     inf, nan = float("inf"), float("nan")
     c.v[c.place(0, ctx + 2)][:, 5] = inf      # seen by row 2 alone
     c.v[c.place(0, ctx + 3)][:, 7] = nan      # by rows 3 and 4
