@@ -350,15 +350,17 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
 // The items of a request's row and query head, in item order: a wave each, a lane takes up to four channels.  Eight records at a time are on their way, since a wave's reads are a chain (one after
 // the other 16 requests' join took 8 us, so 5).  Bound by the records' bytes where they are many: two requests of 64 rows at 65000 keys leave 34 KB an item and kv head, 10 us.
 constexpr int TA_JOIN_WAVES = 4;
-template <typename T, int PARTS>
+template <typename T, int PARTS, bool SPLIT>
 __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAttend a) {
-  const int lane = threadIdx.x & 63, head = uniform((int)(blockIdx.y * TA_JOIN_WAVES + (threadIdx.x >> 6))), r = uniform((int)(blockIdx.x / a.max_rows)), j = (int)blockIdx.x - r * a.max_rows;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), head = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * TA_JOIN_WAVES + wave;
+  const int r = uniform((int)(blockIdx.x / a.max_rows)), j = (int)blockIdx.x - r * a.max_rows;
   int first;
   const int2 note = a.notes[r];
-  const int n_rows = tree_rows(a, r, first), record = note.x, count = note.y;
-  if (count < 2 || j >= n_rows || head >= a.Hq) return;
+  const int n_rows = tree_rows(a, r, first), all = note.y;
+  if (all < 2 || j >= n_rows || head >= a.Hq) return;  // (SPLIT: all waves)
+  const int own = SPLIT ? (all + TA_JOIN_WAVES - 1) / TA_JOIN_WAVES : all, skip = SPLIT ? wave * own : 0, count = all - skip < own ? all - skip : own;  // this wave's records
   const size_t step = (size_t)a.Hq * a.max_rows * a.rec;
-  const float *rec = a.part + (((size_t)record * a.Hq + head) * a.max_rows + j) * a.rec;
+  const float *rec = a.part + (((size_t)(note.x + skip) * a.Hq + head) * a.max_rows + j) * a.rec;
   const bool sees = a.vis[first + j] != 0;
   float top = -INFINITY, l = 0.f, acc[PARTS] = {};
   constexpr int N = 8;
@@ -388,6 +390,28 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
       for (int c = 0; c < PARTS; ++c) acc[c] += v[k][c] * f;
     }
   }
+  if constexpr (SPLIT) {  // the waves' sums, in order
+    __shared__ float sums[TA_JOIN_WAVES][PARTS + 2][64];
+#pragma unroll
+    for (int c = 0; c < PARTS; ++c) sums[wave][c][lane] = acc[c];
+    sums[wave][PARTS][lane] = top;
+    sums[wave][PARTS + 1][lane] = l;
+    __syncthreads();
+    if (wave > 0) return;
+    float most = top;
+    for (int w = 1; w < TA_JOIN_WAVES; ++w) most = fmaxf(most, sums[w][PARTS][lane]);
+    const float base = most > -INFINITY ? most : 0.f;
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < PARTS; ++c) acc[c] = 0.f;
+    for (int w = 0; w < TA_JOIN_WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sums[w][PARTS][lane] - base);
+      l += sums[w][PARTS + 1][lane] * f;
+      if (!(f > 0.f || f != f)) continue;
+#pragma unroll
+      for (int c = 0; c < PARTS; ++c) acc[c] += sums[w][c][lane] * f;
+    }
+  }
   const float inv = sees && (l > 0.f || l != l) ? 1.f / l : 0.f;
 #pragma unroll
   for (int c = 0; c < PARTS; ++c) {
@@ -412,19 +436,25 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 constexpr int TA_FEW = 256;
 // Requests of up to 512 keys, if the table has no room for more, are left whole (16 x 16 rows at 400: 16.4, cut 21.4; 16 x 64 at 500: 35 and 46), float ones of up to 256 (3 x 8 at 500: cut 11.0,
 //   13.5 whole: their products are 1/16 as fast).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64
-//   workgroups: 18.6 whole and cut 16.5, but 4 x 32 at 600, 22.6 and 26.5).
+//   workgroups: 18.6 whole and cut 16.5, but 4 x 32 at 600, 22.6 and 26.5), and for heads
+//   of 256 channels (22 of 1 to 12 rows at up to 747: cut 21, whole 34).
 constexpr int TA_WHOLE_WIDE = 256, TA_MANY = 64;
 // 128 columns a workgroup rather than 64 (K and V pass through LDS half as often) where one of 512 then has this many keys, if all requests are as long as the table: 4 x 64 rows at 500, 128
 //   columns 26.4 and 64 20.0, 1 x 40 at 3000, 28.9 and 23.5, 4 x 64 at 4000, 512 keys, 49.9 and 48.3, 4 x 40 of three heads of 96 channels at 16000, 930 keys, 57.4 and 64.5, 16 x 64 at 4000,
-//   2000 keys, 129 and 134, 4 x 64 at 16000, 119 and 134, 2 x 64 at 65000, 230 and 284.  Heads of 256 channels: 128 always (8 x 33 at 2000, 38.4 and 44.0).
-constexpr int TA_LONG = 768;
+//   2000 keys, 129 and 134, 4 x 64 at 16000, 119 and 134, 2 x 64 at 65000, 230 and 284.  Heads of 256 channels (one of 16 query heads), one workgroup a CU: 1 x 10 at 15800,
+//   38 keys, 28.5 and 26.9, 8 x 33 at 2000, 129 keys, 38.2 and 44.1, 4 x 30 at 5000, 146 keys, 39.6 and 42.2.
+constexpr int TA_LONG = 768, TA_LONG_256 = 128;
 // Workgroups that items are cut for: one of 64 columns a CU (16 of 1 to 16 rows at up to 4096, 25.5; 384 of them 27.4, 512 26.1; 32 x 16 rows at 2000 62, 75 and 69), or two where a request has
 //   several and each keeps TA_SHARE keys (1 x 64 rows of 64 heads at 8000: 48.1, one 54.9; 1 x 40 at 3000, 117 keys: 23.5 and 21.9); two of 128; at_workgroups' for the kernel above.
 constexpr int TA_SHARE = 256;
 // Bytes of the items' records at most; fewer items keep to it.  A record is written and read again: 4 us and 10 us at 34 KB an item and kv head of two requests of 64 rows.
 constexpr size_t TA_RECORDS = (size_t)64 << 20;
+// The join's waves share a row's and head's records where a request may have that many items and rows and heads are fewer than waves that fill the chip: one row of 8 heads at 30000 keys 37.6, shared
+//   21.0, 1 x 10 of 16 heads of 256 channels at 15800, 37.7 and 28.3, 1 x 8 of 32 at 4000, 17.8 and 16.1; from 8 or 4 items a request on: no difference; 2 x 64 of 32 heads: 231 both.
+constexpr int TA_MANY_RECORDS = 16, TA_PAIRS = 2048;
 struct TreePlan {
   int wide, waves, tiles, uncut, target, items;
+  bool split;  // the join's waves share a row's records
   unsigned grid;
   size_t notes, list, bytes;
 };
@@ -434,7 +464,7 @@ static TreePlan ta_shape(const la_pages_desc &p, int Hq, int max_rows, int R, lo
   const int columns = Hq / p.n_kv_heads * max_rows;
   const bool few = cap <= AT_WHOLE && p.head_dim <= 128 && columns <= 32 && (long long)R * p.n_kv_heads * ceil_div(columns, 16) <= TA_FEW;
   const double share = (double)R * p.n_kv_heads * columns * (double)cap / 512;  // columns times keys of one of 512 workgroups
-  if (columns > 16 && !few && tree_wide(p.dtype, p.head_dim, p.page_size)) r.wide = columns > 64 && (p.head_dim > 128 || share >= 128. * TA_LONG) ? 128 : 64;
+  if (columns > 16 && !few && tree_wide(p.dtype, p.head_dim, p.page_size)) r.wide = columns > 64 && share >= 128. * (p.head_dim <= 128 ? TA_LONG : TA_LONG_256) ? 128 : 64;
   r.waves = few ? TA_WHOLE_WAVES : TA_WAVES;
   r.tiles = ceil_div(columns, r.wide ? r.wide : 16);
   const int groups = !r.wide ? at_workgroups(p.head_dim) : p.head_dim <= 128 && (r.wide == 128 || (r.tiles > 1 && share >= 64. * TA_SHARE)) ? 512 : 256;
@@ -446,7 +476,7 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
   TreePlan r = ta_shape(p, Hq, max_rows, R, cap);
   const int target = r.target;
   r.target = 0;
-  r.uncut = r.wide && (long long)R * p.n_kv_heads * r.tiles < TA_MANY ? TA_WHOLE_WIDE : p.dtype == LA_F32 ? AT_WHOLE / 2 : AT_WHOLE;
+  r.uncut = r.wide && (p.head_dim > 128 || (long long)R * p.n_kv_heads * r.tiles < TA_MANY) ? TA_WHOLE_WIDE : p.dtype == LA_F32 ? AT_WHOLE / 2 : AT_WHOLE;
   const bool whole = cap <= r.uncut;
   if (!whole) r.waves = TA_WAVES;
   r.items = R;
@@ -459,6 +489,7 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
       r.bytes = std::min(r.items, 2 * cut) * record;  // (of requests that are cut: fewer than `cut`, with one item more than their share of `cut` each)
       if (r.bytes <= TA_RECORDS || r.target == 1) break;
     }
+    r.split = std::min((long long)r.target, (cap + AT_PIECE - 1) / AT_PIECE) >= TA_MANY_RECORDS * (long long)R && (long long)R * max_rows * Hq < TA_PAIRS;
     r.notes = r.bytes;
     r.bytes += ((size_t)R * sizeof(int2) + 15) / 16 * 16;
     if (R > 64) {
@@ -492,6 +523,13 @@ static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
     if (plan.waves == TA_WHOLE_WAVES) return ta_launch<T, DH, TA_WHOLE_WAVES>(a, plan, s);
   return ta_launch<T, DH, TA_WAVES>(a, plan, s);
 }
+template <typename T, bool SPLIT>
+static void ta_join(const TreeAttend &a, int heads, hipStream_t s) {
+  const dim3 grid((unsigned)a.B * a.max_rows, heads);
+  if (a.dh <= 64) tree_join_kernel<T, 1, SPLIT><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
+  else if (a.dh <= 128) tree_join_kernel<T, 2, SPLIT><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
+  else tree_join_kernel<T, 4, SPLIT><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
+}
 template <typename T>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if (a.list) {
@@ -509,10 +547,8 @@ static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if (rc) return rc;
   if (plan.target > 0) {
     ProfScope ps("tree_join", s);
-    const dim3 grid((unsigned)a.B * a.max_rows, ceil_div(a.Hq, TA_JOIN_WAVES));
-    if (a.dh <= 64) tree_join_kernel<T, 1><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
-    else if (a.dh <= 128) tree_join_kernel<T, 2><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
-    else tree_join_kernel<T, 4><<<grid, 64 * TA_JOIN_WAVES, 0, s>>>(a);
+    if (plan.split) ta_join<T, true>(a, a.Hq, s);
+    else ta_join<T, false>(a, ceil_div(a.Hq, TA_JOIN_WAVES), s);
   }
   LA_HIP(hipGetLastError());
   return LA_OK;
@@ -583,7 +619,7 @@ extern "C" int la_paged_tree_attend(const la_pages_desc *pages, int layer, const
   LA_REQUIRE((uintptr_t)vis % 8 == 0, LA_EINVAL, "vis must be 8-byte aligned");
   LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
   const TreePlan plan = ta_plan(p, n_q_heads, max_blocks, n_requests, max_rows);
-  LA_REQUIRE(plan.grid < 1u << 24 && (long long)n_requests * max_rows * ceil_div(n_q_heads, TA_JOIN_WAVES) < 1ll << 24, LA_EINVAL,
+  LA_REQUIRE(plan.grid < 1u << 24 && (long long)n_requests * max_rows * (plan.split ? n_q_heads : ceil_div(n_q_heads, TA_JOIN_WAVES)) < 1ll << 24, LA_EINVAL,
              "%d requests of %d rows and %d heads are more than one launch takes", n_requests, max_rows, n_q_heads);  // (2^32 threads)
   LA_REQUIRE(workspace_bytes >= plan.bytes && (workspace || !plan.bytes), LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
   LA_REQUIRE(aligned16({workspace}), LA_EINVAL, "workspace must be 16-byte aligned");
