@@ -437,7 +437,7 @@ constexpr int TA_FEW = 256;
 // Requests of up to 512 keys, if the table has no room for more, are left whole (16 x 16 rows at 400: 16.4, cut 21.4; 16 x 64 at 500: 35 and 46), float ones of up to 256 (3 x 8 at 500: cut 11.0,
 //   13.5 whole: their products are 1/16 as fast).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64
 //   workgroups: 18.6 whole and cut 16.5, but 4 x 32 at 600, 22.6 and 26.5), and for heads
-//   of 256 channels (22 of 1 to 12 rows at up to 747: cut 21, whole 34).
+//   of 256 channels always (22 of 1 to 12 rows at up to 747: cut 21, whole 34; one row at 500 14.3 and 18.3).
 constexpr int TA_WHOLE_WIDE = 256, TA_MANY = 64;
 // 128 columns a workgroup rather than 64 (K and V pass through LDS half as often) where one of 512 then has this many keys, if all requests are as long as the table: 4 x 64 rows at 500, 128
 //   columns 26.4 and 64 20.0, 1 x 40 at 3000, 28.9 and 23.5, 4 x 64 at 4000, 512 keys, 49.9 and 48.3, 4 x 40 of three heads of 96 channels at 16000, 930 keys, 57.4 and 64.5, 16 x 64 at 4000,
@@ -476,9 +476,11 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
   TreePlan r = ta_shape(p, Hq, max_rows, R, cap);
   const int target = r.target;
   r.target = 0;
-  r.uncut = r.wide && (p.head_dim > 128 || (long long)R * p.n_kv_heads * r.tiles < TA_MANY) ? TA_WHOLE_WIDE : p.dtype == LA_F32 ? AT_WHOLE / 2 : AT_WHOLE;
+  const bool sparse = (long long)R * p.n_kv_heads * r.tiles < TA_MANY;
+  r.uncut = p.head_dim > 128 || (r.wide && sparse) ? TA_WHOLE_WIDE : p.dtype == LA_F32 ? AT_WHOLE / 2 : AT_WHOLE;
   const bool whole = cap <= r.uncut;
   if (!whole) r.waves = TA_WAVES;
+  if (!whole && sparse && p.dtype == LA_F32) r.uncut = std::min(r.uncut, TA_WHOLE_WIDE);  // (the join is launched anyway, and four waves have the keys: 1 x 8 rows at 402, 16.4 and 11.8)
   r.items = R;
   if (!whole) {
     const size_t record = (size_t)Hq * max_rows * (p.head_dim + 4) * 4;
