@@ -361,6 +361,35 @@ def test_attend_masks_of_any_kind():
     c.check(c.run(max_rows=6), max_rows=6)
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,lens,counts", [
+    ("bf16", 8, 2, 64, 16, [6000], [5]), ("f16", 8, 2, 128, 8, [700], [9]), ("f32", 4, 2, 80, 24, [2300], [4]), ("bf16", 16, 1, 256, 16, [4100], [3]), ("f16", 8, 1, 96, 16, [3000, 260], [12, 7]),
+    ("bf16", 4, 1, 200, 16, [1300], [2]), ("bf16", 2, 2, 64, 16, [130], [1])])
+def test_attend_few_requests_of_a_long_table(dtype, Hq, Hkv, dh, page, lens, counts):
+    """Many items a request, whose records several waves share: numbers of them that the waves do not divide, fewer than waves; NaN and infinities in queries, scores of -inf and NaN."""
+    blocks = 8192 // page
+    c = Case(dtype, Hq, Hkv, dh, page, lens, counts, blocks=blocks)
+    out = c.run()
+    c.check(out)
+    assert torch.equal(out, c.run())
+    nan, inf, g = float("nan"), float("inf"), Hq // Hkv
+    c.q[0, 0, 3], c.q[len(c.vis) - 1, 1 % Hq, 0] = nan, inf
+    got = c.run()
+    others = [h for h in range(1, Hq) if len(c.vis) > 1 or h != 1 % Hq]  # (of one row both are in it)
+    assert torch.isnan(got[0, 0]).all() and torch.equal(got[0, others], out[0, others])
+    keep = [i for i in range(1, len(c.vis) - 1)]
+    assert torch.equal(got[keep], out[keep])
+    c = Case(dtype, Hq, Hkv, dh, page, lens, counts, blocks=blocks)
+    c.q[:] = c.q.abs() + 0.5
+    for t in range(lens[0] + counts[0]):
+        c.k[c.place(0, t)][0] = -inf  # (of one kv head, nothing but scores of -inf; of the others as before)
+    c.v[c.place(0, lens[0] - 1)][Hkv - 1, 2] = inf
+    got = c.run()
+    sees = [i for i in range(counts[0]) if c.vis[i]]
+    assert (got[:counts[0], :g].masked_fill(torch.isnan(got[:counts[0], :g]), 0.0) == 0).all()  # (weights of nothing: zeros, or NaN where V is infinite)
+    if Hkv > 1:
+        assert (got[sees, (Hkv - 1) * g:, 2] == inf).all() and torch.isfinite(got[sees, (Hkv - 1) * g:, 3:]).all() and (got[:counts[0], :g] == 0).all()
+
+
 @pytest.mark.parametrize("max_rows", [1, 4, 15, 16, 17])
 def test_attend_rows_behind_max_rows_see_nothing(max_rows):
     c = Case("bf16", 8, 2, 64, 16, [100, 30, 2000], [17, 5, 16])
