@@ -432,12 +432,12 @@ __global__ __launch_bounds__(64 * TA_JOIN_WAVES) void tree_join_kernel(TreeAtten
 // Which kernel, and what is cut; each rule with both sides as measured, in microseconds, 32 query heads of 128 channels unless said.
 // TA_FEW: where no request is cut and workgroups of 16 columns are no more than the CUs, eight waves share a workgroup's keys (1 tree of 8 rows at 500 keys: 11.7, with four waves 14.7; 1 of 16:
 //   13.5 and 16.4).  More than 32 columns, or more workgroups, go through LDS.
-// Wide from 17 columns: 1 x 8 rows at 1000, 11.7 and with the other kernel 14.4; at 2000, 13.7 and 16.2; 8 x 8 at 4000, 35.8 both.  At 16 columns and fewer three quarters of its waves would idle.
+// Wide from 17 columns: 1 x 8 rows at 1000, 11.7 and with the other kernel 14.4; at 2000, 13.7 and 16.2; 8 x 8 at 4000, 35.8 both; 2 x 57 at 19000 with pages of 8, 50 and 134.  At 16 columns and
+// fewer three quarters of its waves would idle.
 constexpr int TA_FEW = 256;
-// Requests of up to 512 keys, if the table has no room for more, are left whole (16 x 16 rows at 400: 16.4, cut 21.4; 16 x 64 at 500: 35 and 46), float ones of up to 256 (3 x 8 at 500: cut 11.0,
-//   13.5 whole: their products are 1/16 as fast).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64
-//   workgroups: 18.6 whole and cut 16.5, but 4 x 32 at 600, 22.6 and 26.5), and for heads
-//   of 256 channels always (22 of 1 to 12 rows at up to 747: cut 21, whole 34; one row at 500 14.3 and 18.3).
+// Requests are left whole up to AT_WHOLE keys (16 x 16 rows at 400: 16.4, cut 21.4; 16 x 64 at 500: 35 and 46), float ones up to half as many, their products being 1/16 as fast (3 x 8 at 500: cut
+//   11.0, 13.5 whole).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64 workgroups: 18.6 whole and
+//   cut 16.5, but 4 x 32 at 600, 22.6 and 26.5), and so always for heads of 256 channels (22 of 1 to 12 rows at up to 747: cut 21, whole 34; one row at 500 14.3 and 18.3).
 constexpr int TA_WHOLE_WIDE = 256, TA_MANY = 64;
 // 128 columns a workgroup rather than 64 (K and V pass through LDS half as often) where one of 512 then has this many keys, if all requests are as long as the table: 4 x 64 rows at 500, 128
 //   columns 26.4 and 64 20.0, 1 x 40 at 3000, 28.9 and 23.5, 4 x 64 at 4000, 512 keys, 49.9 and 48.3, 4 x 40 of three heads of 96 channels at 16000, 930 keys, 57.4 and 64.5, 16 x 64 at 4000,
@@ -621,7 +621,7 @@ extern "C" int la_paged_tree_attend(const la_pages_desc *pages, int layer, const
   LA_REQUIRE((uintptr_t)vis % 8 == 0, LA_EINVAL, "vis must be 8-byte aligned");
   LA_REQUIRE(scale - scale == 0.f, LA_EINVAL, "scale is not finite");
   const TreePlan plan = ta_plan(p, n_q_heads, max_blocks, n_requests, max_rows);
-  LA_REQUIRE(plan.grid < 1u << 24 && (long long)n_requests * max_rows * (plan.split ? n_q_heads : ceil_div(n_q_heads, TA_JOIN_WAVES)) < 1ll << 24, LA_EINVAL,
+  LA_REQUIRE(plan.grid < 1u << 24 && (long long)n_requests * max_rows * ceil_div(n_q_heads, TA_JOIN_WAVES) < 1ll << 24, LA_EINVAL,
              "%d requests of %d rows and %d heads are more than one launch takes", n_requests, max_rows, n_q_heads);  // (2^32 threads)
   LA_REQUIRE(workspace_bytes >= plan.bytes && (workspace || !plan.bytes), LA_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
   LA_REQUIRE(aligned16({workspace}), LA_EINVAL, "workspace must be 16-byte aligned");
