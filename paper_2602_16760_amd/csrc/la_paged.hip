@@ -183,10 +183,10 @@ struct PagedCopy {
 };
 template <int RUN>
 __global__ __launch_bounds__(256) void paged_copy_kernel(PagedCopy a) {
-  const int runs = (a.n + a.run - 1) / a.run, h = blockIdx.y;
+  const int h = blockIdx.y;
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   const int r = (int)(i / a.per_head), c = (int)(i - (long long)r * a.per_head);
-  if (i >= (long long)runs * a.per_head) return;
+  if ((long long)r * a.run >= a.n) return;
   const int n_slots = a.n_pages * a.page;
   long long src[RUN], dst[RUN];
 #pragma unroll

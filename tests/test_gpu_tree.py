@@ -202,6 +202,26 @@ def test_copy_behind_32_bits():
             assert torch.equal(t[:, s // 16, :, s % 16], x[:, 3 - i])
 
 
+def test_copy_as_many_pairs_as_there_are_numbers():
+    """2^31 - 1 pairs, all but a few of none."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough memory")
+    B = binding()
+    n = 2 ** 31 - 1
+    k, v = (torch.arange(2 * 16 * 8, dtype=torch.float32, device="cuda").reshape(1, 2, 1, 16, 8).to(torch.bfloat16) + t for t in range(2))
+    frm, to = (torch.full((n,), -1, dtype=torch.int32, device="cuda") for _ in range(2))
+    for at, (f, t) in ((0, (3, 20)), (64, (5, 21)), (n // 2, (7, 22)), (n - 1, (9, 23))):
+        frm[at], to[at] = f, t
+    want = []
+    for x in (k, v):
+        y = x.clone()
+        for f, t in ((3, 20), (5, 21), (7, 22), (9, 23)):
+            y[0, t // 16, 0, t % 16] = x[0, 0, 0, f]
+        want.append(y)
+    B.la_paged_copy(B.la_pages(k, v), frm, to, run=64)
+    assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
 # ---- la_paged_tree_attend ------------------------------------------------------------------------------------
 class Case:
     """Pages in any order, NaN wherever no request has a position; a request's keys are its committed positions and its block's rows."""
