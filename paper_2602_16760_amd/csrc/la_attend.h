@@ -16,6 +16,7 @@ typedef unsigned __attribute__((ext_vector_type(4))) at_u4;
 typedef unsigned __attribute__((ext_vector_type(2))) at_u2;
 
 constexpr float AT_LOG2E = 1.4426950408889634f;
+constexpr size_t AT_CACHED = (size_t)256 << 20;  // a layer's K and V pages of more bytes are not kept in the last-level cache
 
 template <typename A>
 __device__ __forceinline__ int at_uncut(const A &) { return 0; }

@@ -396,7 +396,6 @@ __global__ __launch_bounds__(64 * AT_JOIN_WAVES) void paged_join_kernel(PagedAtt
 // those that the rows read, which only the device knows: a batch of 32 that reads 99 MB of a large pool has it too, 41.9 us (39.5 in a pool of its own size) where other work went through the
 // caches in between, 36.6 (29.8) where its keys would stay cached from call to call, which other layers' keys and weights prevent in a program.
 constexpr int AT_WIDE = 256;
-constexpr size_t AT_CACHED = (size_t)256 << 20;
 static AtPlan at_plan(const la_pages_desc &p, int Hq, int max_blocks, int B) { return at_plan(p.head_dim, p.n_kv_heads, p.page_size, Hq, max_blocks, B); }
 
 template <typename T, int DH, bool PAGED16, bool FULL>

@@ -24,6 +24,7 @@ struct TreeAttend {
   int target, tiles, items;  // as at_plan has them
   int uncut;          // keys up to which no request is cut
   int q_tiles, kind;  // as la_paged_attend's
+  bool once;          // K and V are read by one workgroup each and are more than the last-level cache holds: they are not kept there
   int rec;            // floats of a row's and head's record of an item
   float *part;        // [record][Hq][max_rows][rec]
   AtItem *list;

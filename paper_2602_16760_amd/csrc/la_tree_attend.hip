@@ -14,7 +14,7 @@ constexpr int TA_WAVES = 4, TA_WHOLE_WAVES = 8;  // of a workgroup; where reques
 // together and a small tree is one or two matrix operands wide.  The waves take blocks of KEYS keys in turn and meet once, at the end: no barrier in the loop, K and V straight to registers, the
 // next block's K asked for under this one's V.  Products, types and pages as in la_attend.hip.  Bound by latency: one tree of eight rows and two query heads a kv head at 500 keys, 10.2 us of
 // which a launch is 3.8; the rest is a chain of offset, page, K, V, and the waves' meeting.
-template <typename T, int DH, bool FAST, int WAVES>
+template <typename T, int DH, bool FAST, int WAVES, bool ONCE>
 __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int E = sizeof(T), TILES = F32 ? 1 : 2, KEYS = 16 * TILES;
@@ -101,6 +101,10 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
     const unsigned lo = __shfl((int)off_lo, j, 64), hi = __shfl((int)off_hi, j, 64);
     return (int)hi < 0 ? 0ll : (long long)lo | (long long)hi << 32;
   };
+  auto load = [](auto *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+  };
   auto load_k = [&]() {
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
       for (int i = 0; i < KP; ++i) {
         const int at = 64 * i + 16 * q4;
         const bool there = FAST || at < row_bytes;
-        kr[t][i] = *(const at_u4 *)(p + (there ? at : 0));
+        kr[t][i] = load((const at_u4 *)(p + (there ? at : 0)));
         if (!there) kr[t][i] = at_u4{0, 0, 0, 0};
       }
     }
@@ -125,8 +129,8 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
       for (int u = 0; u < VH; ++u) {
         const int at = 16 * VW * u + VW * c16;
         const char *from = p + (FAST || at < row_bytes ? at : 0);  // (channels behind the row's end are never stored)
-        if constexpr (VW == 16) *(at_u4 *)vr[j][u] = *(const at_u4 *)from;
-        else *(at_u2 *)vr[j][u] = *(const at_u2 *)from;
+        if constexpr (VW == 16) *(at_u4 *)vr[j][u] = load((const at_u4 *)from);
+        else *(at_u2 *)vr[j][u] = load((const at_u2 *)from);
       }
     }
   };
@@ -504,20 +508,24 @@ static TreePlan ta_plan(const la_pages_desc &p, int Hq, int max_blocks, int R, i
   return r;
 }
 
-template <typename T, int DH, bool FAST, int WAVES>
+template <typename T, int DH, bool FAST, int WAVES, bool ONCE>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   constexpr int VC = (DH * (int)sizeof(T) / 16 < 16 ? 8 : 16) / (int)sizeof(T);
   constexpr int LDS = (2 * WAVES * AT_ROWS + WAVES * AT_ROWS * (16 * VC + 4)) * 4;
   if constexpr (LDS > 64 * 1024)
-    if (const int rc = ta_allow_lds<tree_attend_kernel<T, DH, FAST, WAVES>>(LDS)) return rc;
-  tree_attend_kernel<T, DH, FAST, WAVES><<<plan.grid, 64 * WAVES, LDS, s>>>(a);
+    if (const int rc = ta_allow_lds<tree_attend_kernel<T, DH, FAST, WAVES, ONCE>>(LDS)) return rc;
+  tree_attend_kernel<T, DH, FAST, WAVES, ONCE><<<plan.grid, 64 * WAVES, LDS, s>>>(a);
   return LA_OK;
 }
 template <typename T, int DH, int WAVES>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
-    if (a.dh == DH && a.page % 16 == 0) return ta_launch<T, DH, true, WAVES>(a, plan, s);
-  return ta_launch<T, DH, false, WAVES>(a, plan, s);
+    if (a.dh == DH && a.page % 16 == 0) {
+      if constexpr (WAVES == TA_WAVES)
+        if (a.once) return ta_launch<T, DH, true, WAVES, true>(a, plan, s);
+      return ta_launch<T, DH, true, WAVES, false>(a, plan, s);
+    }
+  return ta_launch<T, DH, false, WAVES, false>(a, plan, s);
 }
 template <typename T, int DH>
 static int ta_launch(const TreeAttend &a, const TreePlan &plan, hipStream_t s) {
@@ -560,6 +568,8 @@ static int ta_run(TreeAttend a, int dtype, const TreePlan &plan, hipStream_t s) 
   a.tiles = plan.tiles;
   a.items = plan.items;
   a.uncut = plan.uncut;
+  // (32 x 8 rows at 4000, 537 MB: 98.9 us, kept 104; 16 x 8 at 16000 190 and 200; where two workgroups read what one of them has asked for it has to stay)
+  a.once = plan.tiles == 1 && 2 * (size_t)a.n_pages * a.Hkv * a.page * a.dh * (dtype == LA_F32 ? 4 : 2) > AT_CACHED;
   a.rec = a.dh + 4;
   a.notes = plan.target > 0 ? (int2 *)((char *)a.part + plan.notes) : nullptr;
   if (plan.list) {

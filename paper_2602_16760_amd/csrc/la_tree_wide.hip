@@ -14,8 +14,10 @@ template <int DH> constexpr int TW_STAGE = 2 * TW_KEYS<DH> * TW_PITCH<DH>;
 // 16 bytes a lane from base + offset to LDS at `to` + 16 lane.  In assembly, as is the wait for them: the compiler does not know which LDS reads they concern, and waits for all of them in
 // front of every transposing read; what it waits for of its own loads is then waited for with them, which is safe.
 // m0 is set anew by the compiler where it needs it, and is no register that it gives out (as a clobber it is refused).  The wait states are those between a vector instruction's write of a scalar and a load that takes it.
+template <bool ONCE>
 __device__ __forceinline__ void tw_load(unsigned to, const char *base, unsigned offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(to), "v"(offset), "s"(base) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void tw_wait_loads() {  // at most N of this wave's loads on their way
@@ -108,12 +110,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
         look_up();
         ask(nx + WINDOW);
       }
+      auto all = [&](auto once) {
 #pragma unroll
-      for (int i = 0; i < LPW; ++i) {
-        const int n = wave * LPW + i, l = nx % WINDOW * EIGHTS + n % HALF_N * KPI / 8;
-        const long long at = (long long)(unsigned)__builtin_amdgcn_readlane((int)off_lo, l) | (long long)__builtin_amdgcn_readlane((int)off_hi, l) << 32;
-        tw_load(lds0 + nx_slot + (unsigned)n * 1024u, (const char *)(n < HALF_N ? a.K : a.V) + at, voff[i]);
-      }
+        for (int i = 0; i < LPW; ++i) {
+          const int n = wave * LPW + i, l = nx % WINDOW * EIGHTS + n % HALF_N * KPI / 8;
+          const long long at = (long long)(unsigned)__builtin_amdgcn_readlane((int)off_lo, l) | (long long)__builtin_amdgcn_readlane((int)off_hi, l) << 32;
+          tw_load<decltype(once)::value>(lds0 + nx_slot + (unsigned)n * 1024u, (const char *)(n < HALF_N ? a.K : a.V) + at, voff[i]);
+        }
+      };
+      a.once ? all(std::true_type{}) : all(std::false_type{});
     }
     ++nx;
     nx_slot = nx_slot + STAGE == NS * STAGE ? 0u : nx_slot + STAGE;

@@ -567,6 +567,22 @@ def test_attend_a_pool_behind_32_bits():
         c.check(out.cpu())
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,dh,page,rows", [("bf16", 32, 8, 128, 16, 16), ("f16", 24, 2, 96, 8, 5), ("bf16", 4, 4, 64, 24, 40), ("f16", 4, 1, 256, 16, 9), ("bf16", 8, 8, 128, 32, 3)])
+def test_attend_pages_of_a_pool_that_no_cache_holds(dtype, Hq, Hkv, dh, page, rows):
+    """Pages of more than 256 MB a layer, most of them of nobody."""
+    B = binding()
+    c = Case(dtype, Hq, Hkv, dh, page, [600, 0, 2300], [rows, 3, rows - 1], seed=rows)
+    n_pages = (150 << 20) // (page * Hkv * dh * 2)
+    spots = torch.linspace(0, n_pages - 1, c.k.shape[1]).long()
+    k, v = (torch.full((1, n_pages, Hkv, page, dh), float("nan"), dtype=T[dtype], device="cuda") for _ in range(2))
+    k[0, spots.cuda()], v[0, spots.cuda()] = c.k[0].cuda(), c.v[0].cuda()
+    table = torch.where(c.table >= 0, spots[c.table.clamp(min=0).long()].to(torch.int32), c.table)
+    out = torch.empty_like(c.q, device="cuda")
+    B.la_paged_tree_attend(B.la_pages(k, v), 0, c.q.cuda(), table.cuda(), i32(c.first), i32(c.lens), i64(c.vis), rows, out)
+    c.check(out.cpu(), max_rows=rows)
+    assert torch.equal(out.cpu(), c.run(max_rows=rows))
+
+
 def test_attend_rows_of_one_are_the_paged_attentions():
     """A block of one row each is a decode step: as la_paged_attend's rows, within two roundings of the output."""
     B = binding()
