@@ -54,14 +54,15 @@ template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ?
 __device__ __forceinline__ int at_uncut(const TreeAttend &a) { return a.uncut; }
 
 // Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
-// infinite V stays one).  The factor is the same for all weights and goes out with their sum.  What is left out of a weight is 2^-19 (half precision) or 2^-15 (bfloat16) of it at most, so that
+// infinite V stays one).  The factor is the same for all weights and goes out with their sum.  What is left out of a weight is 2^-20 (half precision) or 2^-15 (bfloat16) of it at most, so that
 // the outputs' own rounding is what an output is off by; one number of 11 or 8 bits would have been half the products, and as far off as that rounding again.
 template <typename T> constexpr float TA_REST = std::is_same<T, _Float16>::value ? 0x1p-10f : sizeof(T) == 2 ? 0x1p-12f : 0.f;
 template <typename T>
 __device__ __forceinline__ at_u2 ta_split(float x, float y) {
   if constexpr (std::is_same<T, _Float16>::value) {
     const auto cut = __builtin_amdgcn_cvt_pkrtz(x, y);
-    const auto rest = __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), __builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1]));
+    typedef _Float16 __attribute__((ext_vector_type(2))) pair;
+    const pair rest = {(_Float16)__builtin_fmaf(x, 1.f + TA_REST<T>, -(float)cut[0]), (_Float16)__builtin_fmaf(y, 1.f + TA_REST<T>, -(float)cut[1])};  // (one instruction each)
     return at_u2{__builtin_bit_cast(unsigned, cut), __builtin_bit_cast(unsigned, rest)};
   } else {
     const unsigned u = __float_as_uint(x), v = __float_as_uint(y);

@@ -192,8 +192,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
     {
       at_u4 kf[2][TILES];
       auto read_k = [&](int k) {
+        unsigned from = base + (rd_k ^ (unsigned)(64 * k));
+        asm("" : "+v"(from));  // (one address for all tiles: what differs fits into the instructions)
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) kf[k & 1][t] = *(LDS_AS const at_u4 *)(uintptr_t)((base + (rd_k ^ (unsigned)(64 * k))) + (unsigned)(16 * t * PITCH));
+        for (int t = 0; t < TILES; ++t) kf[k & 1][t] = *(LDS_AS const at_u4 *)(uintptr_t)(from + (unsigned)(16 * t * PITCH));
       };
       read_k(0);
 #pragma unroll
@@ -265,9 +267,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
         const int m = x * DG / DT, d0 = x * DG % DT;
 #pragma unroll
         for (int y = 0; y < DG; ++y) {
-          const unsigned at = base + (rd_v ^ (unsigned)(32 * (d0 + y))) + (unsigned)(32 * m * PITCH);
-          const at_u2 lo = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)at));
-          const at_u2 hi = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + 16u * PITCH)));
+          unsigned at = base + (rd_v ^ (unsigned)(32 * (d0 + y)));
+          asm("" : "+v"(at));
+          const at_u2 lo = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + (unsigned)(32 * m * PITCH))));
+          const at_u2 hi = __builtin_bit_cast(at_u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS tw_s4 *)(uintptr_t)(at + (unsigned)(32 * m * PITCH) + 16u * PITCH)));
           vf[x & 1][y] = at_u4{lo[0], lo[1], hi[0], hi[1]};
         }
       };
