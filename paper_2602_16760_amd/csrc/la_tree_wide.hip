@@ -34,9 +34,10 @@ __device__ __forceinline__ void tw_barrier() {
 // to add up but the items.  One barrier a stage: past it every wave's part of the stage is in, and nobody reads the stage any more that the next requests overwrite.
 // The 16-byte pieces of a row are permuted by its key, so that sixteen keys' equal pieces, and four keys' neighbouring ones, lie in different banks.  V's operand, eight keys of a channel in a
 // lane, comes out of LDS by transposing reads.
-// Bound by the matrix unit at long requests: two of 64 rows at 65000 keys, 32 query heads of 128 channels, are 205 GFLOP (137, and V's products with the weights' second numbers) in 223 us, 0.92
-// PFLOP/s where a large library product reaches 1.16; the weights' instructions run beside the other workgroup's products.  The next stage's scores in front of a stage's weights took 353, waves'
-// priorities changed nothing.  At 16 requests of 1 to 16 rows at 64 to 4096, 41 MB, 19 us: the chain to a workgroup's first stage, five stages, and 34 KB of sums out of it.
+// Bound by the matrix unit and the power it draws at long requests: two of 64 rows at 65000 keys, 32 query heads of 128 channels, are 205 GFLOP (137, and V's products with the weights' second
+// numbers) in 214 us, 0.96 PFLOP/s where a large library product reaches 1.16; without the weights' instructions it would be 190.  These go first (s_setprio), so that one workgroup's fill the gaps of
+// the other's products: 8 x 64 rows at 16000 227 -> 210, 16 x 64 at 4000 133 -> 124.  The next stage's scores in front of a stage's weights took 353; products of 32 by 32, V asked for in front of the
+// weights, priority for the products: no difference.  At 16 requests of 1 to 16 rows at 64 to 4096, 41 MB, 19 us: the chain to a workgroup's first stage, five stages, and 34 KB of sums out of it.
 template <typename T, int DH, int WAVES, int NT, int NS>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) {
   constexpr int KEYS = TW_KEYS<DH>, TILES = KEYS / 16, KP = DH / 32, DT = DH / 16, ROWB = DH * 2, PITCH = TW_PITCH<DH>, HALF = KEYS * PITCH, STAGE = 2 * HALF;
@@ -228,6 +229,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
           for (int e = 0; e < 4; ++e) s[n][t][e] = mask >> (16 * t + e) & 1 ? s[n][t][e] * to_log2 : -INFINITY;
       }
     }
+    __builtin_amdgcn_s_setprio(1);  // (the other workgroup's products run beside these instructions, and go last where both have one to issue)
     at_u4 p[NT][TILES / 2], rest[NT][TILES / 2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -260,6 +262,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
         rest[n][t / 2][2 * (t & 1) + 1] = y[1];
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     {
       constexpr int DG = DT % 4 ? 3 : 4, GROUPS = TILES / 2 * DT / DG;  // V's fragments of some tiles of channels at a time, the next ones on their way
       at_u4 vf[2][DG];
@@ -357,7 +360,7 @@ static int tw_launch(const TreeAttend &a, unsigned grid, hipStream_t s) {
 }
 template <typename T, int DH>
 static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_t s) {
-  constexpr int NS = DH == 64 ? 4 : 2;  // (64 KB: two workgroups a CU; four stages of 128 channels, one workgroup: 16 ragged requests 27.5 us, so 25.3)
+  constexpr int NS = 2;  // (64 KB at 128 channels, two workgroups a CU; four stages, one workgroup: 16 ragged requests 27.5 us, so 25.3; four of 64 channels, 4 x 64 rows at 32000 135, so 130)
   if (columns == 64) return tw_launch<T, DH, 4, 1, NS>(a, grid, s);
   if constexpr (DH <= 128) return tw_launch<T, DH, 4, 2, NS>(a, grid, s);
   else return tw_launch<T, DH, 8, 1, 4>(a, grid, s);
