@@ -144,6 +144,7 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
     load_k();
     load_v();
   }
+  const unsigned long long vis = a.vis[col_row];  // (asked for here, behind the first keys: where it is needed first, at the request's end, everybody would wait for it)
   unsigned long long odd_rows = 0;  // drafted rows, of those whose keys this wave has, whose V has an infinity or NaN
   constexpr unsigned ALL = F32 ? 0xffffu : 0xffffffffu;
   for (int i = 0; i < mine; ++i) {
@@ -170,7 +171,6 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
       factor = 1.f;
       unsigned mask = now;  // keys that the column sees
       if (drafted) {
-        const unsigned long long vis = a.vis[col_row];
         const int at = key0 - L;  // of the block's first key in the request's rows
         mask &= at >= 0 ? (at < 64 ? (unsigned)(vis >> at) : 0u) : (unsigned)(vis << -at) | ((1u << -at) - 1u);  // (at > -KEYS)
       }
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
       }
     }
     const float base = UP - (m_run > -INFINITY ? m_run : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base)) * (1.f + TA_REST<T>);
-    if (!(a.vis[col_row] >> row & 1u)) continue;
+    if (!(vis >> row & 1u)) continue;
 #pragma unroll
     for (int u = 0; u < VH; ++u)
 #pragma unroll
@@ -289,6 +289,12 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
           const int ch = 16 * VC * u + VC * (4 * q4 + y) + w;
           if (FAST || ch < dh) o[u * VC + w][y] += p * load_as_float<T>((const T *)(vb + at) + ch);
         }
+  }
+  if (vis == 0) {  // (zeros, whatever was multiplied)
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = at_f4{0.f, 0.f, 0.f, 0.f};
   }
   // The waves' sums meet in LDS, a part of 16 VC channels at a time: [wave][column][channels + 4], and in front of them [wave][column] offset and sum; a thread adds the waves' sums of four
   // channels, in order.  Output tile (u, w), lane, register e is channel 16 VC u + VC (4 q4 + e) + w.
@@ -338,7 +344,6 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
         continue;
       }
       y *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;  // (nothing seen: zeros)
-      if (a.vis[first + j] == 0) y = at_f4{0.f, 0.f, 0.f, 0.f};
       if (a.kind != AT_OUT_ROWS) {
 #pragma unroll
         for (int z = 0; z < 4; ++z) at_store_row(a, first + j, head * dh + ch + z, y[z]);

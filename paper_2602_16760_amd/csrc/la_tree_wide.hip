@@ -75,6 +75,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
 #pragma unroll
       for (int p = 0; p < KP; ++p) q[t][p] ^= 0x80008000u;
   }
+  unsigned long long early = 0;  // the column's mask: asked for here, since where it is needed first, at the request's end, everybody would wait for it (of two there are no registers for them)
+  if constexpr (NT == 1) early = a.vis[first + (c16 < cols ? col0 + c16 : 0) / g];
   const float to_log2 = fabsf(a.scale) * AT_LOG2E;
   const int32_t *tab = a.table + it.r * a.ldt;
   // Lane i: where eight keys, the i-th of the next WINDOW stages', lie (the first page where they lie in none: they are not seen, whatever they hold).
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
         unsigned long long mask = now;  // keys that the column sees
         if (drafted) {
           const int c = 16 * n + c16 < cols ? col0 + 16 * n + c16 : 0;
-          const unsigned long long vis = a.vis[first + c / g];
+          const unsigned long long vis = NT == 1 ? early : a.vis[first + c / g];
           const int at = key0 - L;  // of the stage's first key in the request's rows
           mask &= at >= 0 ? (at < 64 ? vis >> at : 0ull) : vis << -at | ((1ull << -at) - 1);  // (at > -KEYS)
         }
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
         }
       }
       const float add = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), w = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, add)) * (1.f + TA_REST<T>);
-      if (!(a.vis[first + c / g] >> row & 1u)) continue;
+      if (!((NT == 1 ? early : a.vis[first + c / g]) >> row & 1u)) continue;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -333,11 +335,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
       for (int d = 0; d < DT; ++d) *(at_f4 *)(to + 4 + 16 * d + 4 * q4) = o[n][d];
       continue;
     }
-    const bool sees = a.vis[first + j] != 0;
+    const bool sees = (NT == 1 ? early : a.vis[first + j]) != 0;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      at_f4 y = sees ? o[n][d] * inv : at_f4{0.f, 0.f, 0.f, 0.f};
+      const at_f4 y = sees ? o[n][d] * inv : at_f4{0.f, 0.f, 0.f, 0.f};
       const int ch = 16 * d + 4 * q4;
       if (a.kind != AT_OUT_ROWS) {
 #pragma unroll
