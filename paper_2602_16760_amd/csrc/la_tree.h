@@ -46,16 +46,18 @@ __device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
   return rows == 0 || L < 0 ? 0 : (int)(n < cap ? n : cap);
 }
 
-// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled (two requests of 64 rows at 65000: 221 us, with
-// an offset that follows each maximum 237; 32 of 4 rows at 8000: 54.8 and 58).  Weights are up to 2^LAZY then: half precision's, at most 65504, carry 2^UP so that 2^(UP + LAZY) is in its range and
-// small ones stay above its smallest; the factor goes out with the sum.  The other types have 8 bits of exponent and need none.
-template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 4.f : 8.f;
-template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 11.f : 0.f;
+// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled (two requests of 64 rows at 65000, half precision:
+// 232 us, with an offset that follows each maximum 237).  Weights are up to 2^LAZY then, and half precision's carry 2^UP besides, as la_paged_attend's do, so that a step of its smallest numbers is
+// 2^-39 of the largest weight; the factor goes out with the sum.  2^(UP + LAZY) has to stay below 65504, so an offset lags by less than an octave.  (With 11 and 4 in place of 15 and 7/8 it took
+// 219, but 600 keys of 2^-31 of a first one's weight came out 3 % off.)  The other types have 8 bits of exponent and need no factor.
+template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 0.875f : 8.f;
+template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 15.f : 0.f;
 __device__ __forceinline__ int at_uncut(const TreeAttend &a) { return a.uncut; }
 
 // Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
-// infinite V stays one).  The factor is the same for all weights and goes out with their sum.  What is left out of a weight is 2^-20 (half precision) or 2^-15 (bfloat16) of it at most, so that
-// the outputs' own rounding is what an output is off by; one number of 11 or 8 bits would have been half the products, and as far off as that rounding again.
+// infinite V stays one), in half precision down to 2^-40 of the largest, below which nothing is left of a weight.  The factor is the same for all weights and goes out with their sum.  What is
+// lost of a weight is 2^-20 of it at most or half a step of half precision's smallest numbers, 2^-40 of the largest (bfloat16: 2^-15 of it), so that the outputs' own rounding is what an output is
+// off by; one number of 11 or 8 bits would have been half the products, and as far off as that rounding again.
 template <typename T> constexpr float TA_REST = std::is_same<T, _Float16>::value ? 0x1p-10f : sizeof(T) == 2 ? 0x1p-12f : 0.f;
 template <typename T>
 __device__ __forceinline__ at_u2 ta_split(float x, float y) {
