@@ -52,6 +52,20 @@ __device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
 // 219, but 600 keys of 2^-31 of a first one's weight came out 3 % off.)  The other types have 8 bits of exponent and need no factor.
 template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 0.875f : 8.f;
 template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 15.f : 0.f;
+// Weights are 2^(factor s - base + UP), formed in one instruction, with factor s not rounded and base rounded: where scores are large that is off by a part of a float's spacing there, and by
+// octaves from 2^24 on, so that the largest weight itself is no number of the type any more, or nothing.  Columns that are TA_FAR octaves from zero, where the part is 2^-14, round factor s as base
+// was: its difference from base is exact then, and nothing for the largest.  Whether a wave has such columns is found out where offsets move; the others' weights are formed as ever.
+constexpr float TA_FAR = 1024.f;
+__device__ __forceinline__ bool ta_far(float m) { return __any(fabsf(m) > TA_FAR && m > -INFINITY); }
+__device__ __forceinline__ float ta_from(float s, float factor, float base) {
+#pragma clang fp contract(off)
+  const float x = s * factor;
+  return x - base;
+}
+template <typename T>
+__device__ __forceinline__ float ta_exponent(float s, float factor, float base) {
+  return fabsf(base) > TA_FAR ? ta_from(s, factor, base) + TA_UP<T> : __builtin_fmaf(s, factor, TA_UP<T> - base);
+}
 __device__ __forceinline__ int at_uncut(const TreeAttend &a) { return a.uncut; }
 
 // Two weights as the sum of two 16-bit numbers each, 1 + TA_REST times the weight together: the first is the weight cut to the type, so the second is above zero where the weight is (an
@@ -71,12 +85,6 @@ __device__ __forceinline__ at_u2 ta_split(float x, float y) {
     return at_u2{__builtin_amdgcn_perm(v, u, 0x07060302u), at_pack<T>(__builtin_fmaf(x, 1.f + TA_REST<T>, -__uint_as_float(u & 0xffff0000u)),
                                                                       __builtin_fmaf(y, 1.f + TA_REST<T>, -__uint_as_float(v & 0xffff0000u)))};
   }
-}
-template <typename T>
-__device__ __forceinline__ float ta_half(unsigned v, int hi) {
-  const uint16_t bits = (uint16_t)(v >> (16 * hi));
-  if constexpr (std::is_same<T, _Float16>::value) return (float)__builtin_bit_cast(_Float16, bits);
-  else return bf16_to_float(bits);
 }
 template <typename T>
 __device__ __forceinline__ bool ta_odd(unsigned v) {  // an infinity or NaN among a word's numbers

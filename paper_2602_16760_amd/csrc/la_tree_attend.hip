@@ -138,6 +138,7 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = at_f4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
+  bool far = false;
   if (mine > 0) {
     look_up(0);
     locate(0);
@@ -219,16 +220,26 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
     if (__any(mx > m_run + LAZY)) {
       const float m_new = fmaxf(m_run, at_max4(mx)), corr = __builtin_amdgcn_exp2f(m_run - (m_new > -INFINITY ? m_new : 0.f));
       m_run = m_new;
+      far = ta_far(m_new);
       l_run *= corr;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= corr;
     }
-    const float base = UP - (m_run > -INFINITY ? m_run : 0.f);
+    const float base = m_run > -INFINITY ? m_run : 0.f;
+    float by = factor, add = UP - base;
+    if (far) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t][e] = ta_exponent<T>(s[t][e], factor, base);
+      by = 1.f;
+      add = 0.f;
+    }
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], factor, base));
+        s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], by, add));
         l_run += s[t][e];
       }
     if constexpr (F32) {
@@ -265,20 +276,20 @@ __global__ __launch_bounds__(64 * WAVES) void tree_attend_kernel(TreeAttend a) {
   for (; odd_rows; odd_rows &= odd_rows - 1) {
     const int row = __builtin_ctzll(odd_rows);
     const long long at = place((long long)L + row);
-    float dot = 0.f;
+    at_f4 score = {0.f, 0.f, 0.f, 0.f};  // (added up as the tile's were: the weight has to be the one in the sum)
 #pragma unroll
-    for (int p = 0; p < KP; ++p) {
-      const int b = 64 * p + 16 * q4;
-      const at_u4 k = *(const at_u4 *)(kb + at + (FAST || b < row_bytes ? b : 0));
+    for (int i = 0; i < KP; ++i) {
+      const int b = 64 * i + 16 * q4;
+      at_u4 k = *(const at_u4 *)(kb + at + (FAST || b < row_bytes ? b : 0));
+      if (!FAST && b >= row_bytes) k = at_u4{0, 0, 0, 0};
+      if constexpr (F32) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {  // (q's pieces behind the row's end are zeros; what K has in their place is no number of its own)
-        if (!FAST && b >= row_bytes) continue;
-        const unsigned x = q[p][w], y = k[w];
-        if constexpr (F32) dot += __uint_as_float(x) * __uint_as_float(y);
-        else dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
+        for (int e = 0; e < 4; ++e) score = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(q[i][e]), score, 0, 0, 0);
+      } else {
+        score = at_mma<T>(k, q[i], score);
       }
     }
-    const float base = UP - (m_run > -INFINITY ? m_run : 0.f), p = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, base)) * (1.f + TA_REST<T>);
+    const float p = __builtin_amdgcn_exp2f(ta_from(score[0], to_log2, m_run > -INFINITY ? m_run : 0.f) + UP) * (1.f + TA_REST<T>);
     if (!(vis >> row & 1u)) continue;
 #pragma unroll
     for (int u = 0; u < VH; ++u)

@@ -128,12 +128,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
   };
   at_f4 o[NT][DT];
   float m_run[NT], l_run[NT];
+  bool far[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[t][d] = at_f4{0.f, 0.f, 0.f, 0.f};
     m_run[t] = -INFINITY;
     l_run[t] = 0.f;
+    far[t] = false;
   }
   ask(0);
   look_up();
@@ -244,17 +246,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
       if (__any(mx > m_run[n] + LAZY)) {
         const float m_new = fmaxf(m_run[n], at_max4(mx)), corr = __builtin_amdgcn_exp2f(m_run[n] - (m_new > -INFINITY ? m_new : 0.f));
         m_run[n] = m_new;
+        far[n] = ta_far(m_new);
         l_run[n] *= corr;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[n][d] *= corr;
       }
-      const float add = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f);
+      const float offset = m_run[n] > -INFINITY ? m_run[n] : 0.f;
+      float by = factor, add = UP - offset;
+      if (far[n]) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][t][e] = ta_exponent<T>(s[n][t][e], factor, offset);
+        by = 1.f;
+        add = 0.f;
+      }
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         float w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][e], factor, add));
+          w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][e], by, add));
           l_run[n] += w[e];
         }
         const at_u2 x = ta_split<T>(w[0], w[1]), y = ta_split<T>(w[2], w[3]);
@@ -305,17 +317,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_wide_kernel(TreeAttend a) 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int c = 16 * n + c16 < cols ? col0 + 16 * n + c16 : 0;
-      float dot = 0.f;
+      at_f4 score = {0.f, 0.f, 0.f, 0.f};  // (added up as the tile's were: the weight has to be the one in the sum)
 #pragma unroll
-      for (int k = 0; k < KP; ++k) {
-        const at_u4 kf = *(const at_u4 *)((const char *)a.K + at + 64 * k + 16 * q4);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const unsigned x = q[n][k][w], y = kf[w];
-          dot += ta_half<T>(x, 0) * ta_half<T>(y, 0) + ta_half<T>(x, 1) * ta_half<T>(y, 1);
-        }
-      }
-      const float add = UP - (m_run[n] > -INFINITY ? m_run[n] : 0.f), w = __builtin_amdgcn_exp2f(__builtin_fmaf(at_sum4(dot), to_log2, add)) * (1.f + TA_REST<T>);
+      for (int k = 0; k < KP; ++k) score = at_mma<T>(*(const at_u4 *)((const char *)a.K + at + 64 * k + 16 * q4), q[n][k], score);
+      const float w = __builtin_amdgcn_exp2f(ta_from(score[0], to_log2, m_run[n] > -INFINITY ? m_run[n] : 0.f) + UP) * (1.f + TA_REST<T>);
       if (!((NT == 1 ? early : a.vis[first + c / g]) >> row & 1u)) continue;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
