@@ -362,7 +362,7 @@ class _Batch:
 
     def __init__(self, eng, prompts, n_new, spare, page_size, n_pages):
         sh, R = eng.shape, len(prompts)
-        self.prompts = prompts = [np.asarray(p, dtype=np.int32) for p in prompts]
+        self.prompts = prompts = [np.array(p, dtype=np.int32, order="C") for p in prompts]  # (copies: a caller's may be views that torch does not take)
         if not 1 <= R <= B.LA_MAX_ROWS or any(len(p) < 1 for p in prompts):
             raise ValueError(f"need 1 to {B.LA_MAX_ROWS} prompts of one token at least")
         lens = [len(p) - 1 for p in prompts]
