@@ -147,6 +147,7 @@ class Engine:
                 B.la_logits_adjust(x, x, **adjust, **history)
             B.la_sample(x, u, ids, u_index=u_index, **{k: v[:hidden.shape[0]] for k, v in rows_of.items()})
 
+        choose.penalizes = bool(set(adjust) & {"repetition", "presence", "frequency"})
         return choose
 
     def _choose(self):
@@ -197,6 +198,8 @@ class Engine:
         b = _Batch(self, prompts, n_new, 0, page_size, n_pages)
         sh, R = self.shape, b.R
         choose = None if sampling is None else self._sampler(sampling, R, n_new * R, R)
+        if choose is not None and choose.penalizes:
+            b.keep_tokens(n_new)
         which = torch.arange(R, dtype=torch.int32, device="cuda")
         hidden = torch.empty((R, sh.d_model), dtype=torch.float32, device="cuda")
         ids, tokens = torch.tensor([p[-1] for p in b.prompts], dtype=torch.int32, device="cuda"), b.i32((n_new, R))
@@ -211,7 +214,8 @@ class Engine:
                 B.la_unembed_argmax(self.model, hidden, ids)
             else:
                 choose(hidden, ids, which, **b.history())
-                b.append(ids[:, None], torch.ones_like(ids))
+                if b.tokens is not None:
+                    b.append(ids[:, None], torch.ones_like(ids))
                 which = which + R
         return tokens.t().cpu().numpy().astype(np.int64), dict(steps=n_new, pages=b.n_pages, free_pages=b.finish(length))
 
@@ -227,6 +231,8 @@ class Engine:
         sh, R = self.shape, b.R
         per = min(max_rows, B.LA_MAX_ROWS // R)  # rows of a request
         choose = None if sampling is None else self._sampler(sampling, R * per, n_new * R, R)
+        if choose is not None and choose.penalizes:
+            b.keep_tokens(n_new)
         texts = [[int(t) for t in p] for p in b.prompts]
         begin = torch.tensor([len(p) for p in b.prompts], dtype=torch.int32, device="cuda")  # (the position behind which a request's first new token is: begin - 1)
         length, steps = b.lens.clone(), 0
@@ -261,7 +267,7 @@ class Engine:
             B.la_tree_accept(both[1], both[0], ids[:N], slot, first, length, n_tok, new_len, last, out, from_slot, to_slot, limit=torch.tensor(todo, dtype=torch.int32).cuda())
             B.la_paged_copy(b.pages, from_slot, to_slot)
             b.mapped(grown, new_len, 1)  # (the pages behind the committed path go back)
-            if choose is not None:
+            if b.tokens is not None:
                 b.append(out, n_tok)
             length = new_len.clone()
             steps += 1
@@ -394,12 +400,7 @@ class _Batch:
                         B.la_kv_read(eng.kv, l, 0, n, k, v)
                         B.la_paged_write(self.pages, l, k, v, slot[at:at + n])
                 at += n
-        # all tokens: the prompts', and room for the new ones
-        self.n_prompt = self.lens + 1
-        self.n_tokens = self.n_prompt.clone()
-        self.tokens = self.i32((R, max(lens) + 1 + n_new), -1)
-        for r, p in enumerate(prompts):
-            self.tokens[r, :len(p)] = torch.from_numpy(p).cuda()
+        self.tokens = None
 
     @staticmethod
     def i32(n, v=0):
@@ -417,17 +418,28 @@ class _Batch:
         if int(self.error):
             raise B.LaError(-3, f"the pages do not hold the batch (error {int(self.error)} of la_page_map; {self.n_pages} pages of {self.page_size} positions)")
 
+    def keep_tokens(self, n_new):
+        """All tokens, for penalties: the prompts', and room for the new ones."""
+        most = max(len(p) for p in self.prompts) + n_new
+        table = np.full((self.R, most + 1), -1, dtype=np.int32)  # (a last column takes what is appended to nobody)
+        for row, p in zip(table, self.prompts):
+            row[:len(p)] = p
+        self._table = B.to_device(table)
+        self.tokens = self._table[:, :most]
+        self.n_prompt = self.lens + 1
+        self.n_tokens = self.n_prompt.clone()
+
     def history(self, req=None, **drafted):
-        return dict(tokens=self.tokens, n_tokens=self.n_tokens, n_prompt=self.n_prompt, req=req, **drafted)
+        """What la_logits_adjust wants to know of the requests' tokens: nothing where none are kept."""
+        return dict(req=req) if self.tokens is None else dict(tokens=self.tokens, n_tokens=self.n_tokens, n_prompt=self.n_prompt, req=req, **drafted)
 
     def append(self, tokens, n):
-        """The first n[r] of tokens [R, most] behind those of request r."""
+        """The first n[r] of tokens [R, most] behind those of request r, in place."""
         at = torch.arange(tokens.shape[1], device="cuda")[None]
         room = self.tokens.shape[1]
         to = torch.where((at < n[:, None]) & (self.n_tokens[:, None] + at < room), self.n_tokens[:, None] + at, room).long()
-        wide = torch.cat((self.tokens, self.i32((self.R, 1))), 1)
-        self.tokens = wide.scatter_(1, to, tokens)[:, :room].contiguous()
-        self.n_tokens = self.n_tokens + n
+        self._table.scatter_(1, to, tokens)
+        self.n_tokens += n
 
     def finish(self, length):
         """All pages go back; how many are free then."""

@@ -29,3 +29,29 @@ def test_prompts_of_any_stride(engine, tree):
     want, _ = go([a[::-1].copy(), b[::2].copy(), b])
     got, _ = go([a[::-1], b[::2], fixed])
     assert np.array_equal(got, want)
+
+
+PENALTIES = [{}, dict(repetition=1.3), dict(presence=0.2), dict(frequency=0.2), dict(bias={3: 2.0})]
+
+
+@pytest.mark.parametrize("penalty", PENALTIES)
+@pytest.mark.parametrize("tree", [False, True])
+def test_tokens_are_kept_where_penalties_want_them_alone(engine, penalty, tree, monkeypatch):
+    """Without penalties of occurred tokens no step copies tokens; with them they stay in one place."""
+    from paper_2602_16760_amd import engine as E
+    places, append = [], E._Batch.append
+
+    def watched(self, *args):
+        append(self, *args)
+        places.append(self.tokens.data_ptr())
+
+    monkeypatch.setattr(E._Batch, "append", watched)
+    sampling = dict(temperature=0.8, seed=1, **penalty)
+    if tree:
+        engine.generate_tree(prompts_of(5, 9), 6, lambda texts: [([7], [0])] * 2, sampling=sampling)
+    else:
+        engine.generate_batch(prompts_of(5, 9), 6, sampling=sampling)
+    if set(penalty) & {"repetition", "presence", "frequency"}:
+        assert places and len(set(places)) == 1
+    else:
+        assert not places
