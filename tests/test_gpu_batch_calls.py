@@ -55,3 +55,9 @@ def test_tokens_are_kept_where_penalties_want_them_alone(engine, penalty, tree, 
         assert places and len(set(places)) == 1
     else:
         assert not places
+
+
+def test_a_draft_for_every_text(engine):
+    for trees in ([], [None], [([7], [0])], [None] * 3):
+        with pytest.raises(ValueError):
+            engine.generate_tree(prompts_of(5, 9), 4, lambda texts: trees)
