@@ -242,7 +242,7 @@ class Engine:
         hidden = torch.empty((R * per, sh.d_model), dtype=torch.float32, device="cuda")
         ids = b.i32(R * per)
         while any(todo):
-            trees = list(draft([t if n else None for t, n in zip(texts, todo)]))
+            trees = list(draft([list(t) if n else None for t, n in zip(texts, todo)]))
             if len(trees) != R:
                 raise ValueError(f"{len(trees)} drafts for {R} texts")
             tok, parent, rows = [], [], []

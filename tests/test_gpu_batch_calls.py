@@ -61,3 +61,20 @@ def test_a_draft_for_every_text(engine):
     for trees in ([], [None], [([7], [0])], [None] * 3):
         with pytest.raises(ValueError):
             engine.generate_tree(prompts_of(5, 9), 4, lambda texts: trees)
+
+
+def test_a_draft_that_writes_into_its_texts(engine):
+    """What a draft does with the lists that it is given is its own affair."""
+    prompts = prompts_of(5, 9)
+    want, _ = engine.generate_batch(prompts, 8)
+
+    def draft(texts):
+        out = []
+        for text in texts:
+            out.append(None if text is None else ([text[-1]], [0]))
+            if text is not None:
+                text += [1, 2, 3]
+        return out
+
+    got, st = engine.generate_tree(prompts, 8, draft)
+    assert np.array_equal(got, want) and st["free_pages"] == st["pages"]
