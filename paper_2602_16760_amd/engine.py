@@ -227,9 +227,9 @@ class Engine:
         rounding (see generate).  Returns (tokens [requests, n_new], stats)."""
         if not 1 <= max_rows <= B.LA_MAX_ROWS:
             raise ValueError(f"max_rows={max_rows}, need 1 to {B.LA_MAX_ROWS}")
-        b = _Batch(self, prompts, n_new, max_rows, page_size, n_pages)
+        per = min(max_rows, B.LA_MAX_ROWS // max(1, len(prompts)))  # rows of a request (too many prompts are refused below)
+        b = _Batch(self, prompts, n_new, per - 1, page_size, n_pages)
         sh, R = self.shape, b.R
-        per = min(max_rows, B.LA_MAX_ROWS // R)  # rows of a request
         choose = None if sampling is None else self._sampler(sampling, R * per, n_new * R, R)
         if choose is not None and choose.penalizes:
             b.keep_tokens(n_new)
@@ -376,7 +376,7 @@ class _Batch:
         lens = [len(p) - 1 for p in prompts]
         pages_of = lambda n: (n + page_size - 1) // page_size
         blocks = max(1, max(pages_of(n + n_new + spare) for n in lens))
-        need = max(1, sum(pages_of(n + n_new + spare) for n in lens))  # (spare: rows of a step that are not committed)
+        need = max(1, sum(pages_of(n + n_new + spare) for n in lens))  # (spare: rows of a last step that no token is wanted of)
         self.n_pages = n_pages = need if n_pages is None else n_pages
         if n_pages < need:  # (what the last step needs is known)
             raise B.LaError(-3, f"the batch needs {need} pages of {page_size} positions, there are {n_pages}")

@@ -78,3 +78,17 @@ def test_a_draft_that_writes_into_its_texts(engine):
 
     got, st = engine.generate_tree(prompts, 8, draft)
     assert np.array_equal(got, want) and st["free_pages"] == st["pages"]
+
+
+@pytest.mark.parametrize("R,max_rows,pages", [(2, 64, 3), (40, 16, 1), (1, 64, 5)])
+def test_pages_for_the_rows_that_a_request_has(engine, R, max_rows, pages):
+    """64 rows are shared by the requests: positions of a request's last step are its prompt's, the tokens in front of the last one's, and its rows'."""
+    prompts, per = prompts_of(*[5] * R), min(max_rows, 64 // R)
+    assert -(-(4 + 5 + per) // 16) == pages
+    draft = lambda texts: [None if t is None else (list(range(100, 163)), [0] * 63) for t in texts]
+    tokens, st = engine.generate_tree(prompts, 6, draft, max_rows=max_rows, n_pages=pages * R)
+    assert st["pages"] == st["free_pages"] == pages * R and np.array_equal(tokens, engine.generate_batch(prompts, 6)[0])
+    assert engine.generate_tree(prompts, 6, draft, max_rows=max_rows)[1]["pages"] == pages * R
+    from paper_2602_16760_amd import binding as B
+    with pytest.raises(B.LaError):
+        engine.generate_tree(prompts, 6, draft, max_rows=max_rows, n_pages=pages * R - 1)
