@@ -11,6 +11,7 @@
 #include "la_device.h"
 #include "la_internal.h"
 #include "la_paged.h"
+#include "la_tree_plan.h"
 
 namespace la {
 

@@ -34,8 +34,7 @@ struct PagedRows {
 };
 int paged_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_tiles, int Hq, float scale, const PagedRows &r, PagedOut kind, void *out, void *workspace,
                       hipStream_t s);
-// The same of trees of up to LA_MAX_ROWS rows of as many requests together: workspace at any of their sizes; the attention.
-size_t tree_attend_bytes(const la_pages_desc &p, int Hq);
+// The same of trees of up to LA_MAX_ROWS rows of as many requests together (workspace: tree_attend_bytes).
 int tree_attend_rows(const la_pages_desc &p, int layer, const void *q, int q_tiles, int Hq, float scale, const PagedRows &r, PagedOut kind, void *out, void *workspace, hipStream_t s);
 
 }  // namespace la

@@ -3,6 +3,7 @@
 #include <atomic>
 
 #include "la_attend.h"
+#include "la_tree_plan.h"
 
 namespace la {
 
@@ -31,6 +32,7 @@ struct TreeAttend {
   int32_t *firsts;
   int2 *notes;  // of each request, where any may be cut: its first record, how many items it has
 };
+static_assert(sizeof(int2) == TA_NOTE, "what the join is told");
 
 // A request's rows: the first one's number, and how many take part.
 __device__ __forceinline__ int tree_rows(const TreeAttend &a, int r, int &f) {
@@ -141,8 +143,7 @@ int ta_allow_lds(int bytes) {
   return LA_OK;
 }
 
-// The wide kernel's launch (la_tree_wide.hip): 16-bit types, pages of a multiple of 8 positions, head_dim of 64, 96, 128 or 256.
-bool tree_wide(int dtype, int head_dim, int page_size);  // whether it is for this shape; then 64 or 128 columns of a workgroup
+// The wide kernel's launch (la_tree_wide.hip), where tree_wide says that it is for the shape; 64 or 128 columns of a workgroup.
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s);
 
 }  // namespace la

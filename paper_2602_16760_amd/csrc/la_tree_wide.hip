@@ -380,9 +380,6 @@ static int tw_launch(const TreeAttend &a, int columns, unsigned grid, hipStream_
   return tw_launch<T, 256>(a, columns, grid, s);
 }
 
-bool tree_wide(int dtype, int head_dim, int page_size) {
-  return dtype != LA_F32 && page_size % 8 == 0 && (head_dim == 64 || head_dim == 96 || head_dim == 128 || head_dim == 256);
-}
 // (128 by four waves of 32, two workgroups a CU, and 256 by eight, one: 16 x 64 rows at 500 keys 28 us and 35, 1 x 64 19.6 and 22.6, 2 x 64 at 65000 244 and 237)
 int tree_attend_wide(const TreeAttend &a, int dtype, int columns, unsigned grid, hipStream_t s) {
   return dtype == LA_F16 ? tw_launch<_Float16>(a, columns, grid, s) : tw_launch<uint16_t>(a, columns, grid, s);
