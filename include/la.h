@@ -272,7 +272,8 @@ int la_sample(const void *logits, int dtype, int64_t row_stride, int B, int V, c
  *   repetition, presence, frequency   float [n_requests] (a repetition that is not a positive finite number, or another that is not finite, is off)
  *   tokens         int32 [n_requests, max_tokens], rows at tokens_stride: the committed tokens, n_tokens[r] of them (int32 [n_requests]), of which the first n_prompt[r] (NULL: 0) are the prompt
  *   draft          int32 [B]: the step's drafted tokens; first, vis: the block of each request and the rows that each row sees, as la_tree_layout leaves them.  Row b is the step's row b:
- *                  the tokens of the rows of vis[b], but for row 0, whose token is the last of `tokens`, count as committed
+ *                  the tokens of the rows of vis[b], but for row 0, whose token is the last of `tokens`, count as committed.  Bit j stands for row first[r] + j of the step, so a mask of the
+ *                  caller's own must have none behind its request's block (la_tree_layout leaves none there): it would name a row of the next request
  *   bias_token, bias   int32, float [n_requests, n_bias], rows at bias_stride (entries outside [0, V) are none; a token that is listed several times has the sum, in the list's order)
  *   allowed        uint32 [n_allowed, (V + 31) / 32], rows at allowed_stride: bit v & 31 of word v >> 5 says whether token v may come; allowed_index int32 [B] the mask of each row
  *                  (NULL: row b has mask b; outside [0, n_allowed): any token may come) */
@@ -299,7 +300,7 @@ typedef struct {
  *   plus v's bias
  *   -inf where v may not come
  * in float, rounded to the type once.  logits, out: device, la_dtype `dtype`, rows at row_stride and out_stride elements, any alignment of the type; out may be logits (with the same
- * stride), and must not overlap it otherwise.  The result does not depend on the rows beside it.  Allocates nothing.
+ * stride), and must not overlap it otherwise.  The result does not depend on rows beside it that vis does not name.  Allocates nothing.
  * LA_EINVAL: V outside 1..LA_MAX_SAMPLE_VOCAB, B above 65535, more than LA_MAX_HISTORY tokens or LA_MAX_BIAS biases, rows that overlap, a part that lacks one of its arrays, more rows than
  * requests or masks without a map.  B = 0 does nothing. */
 int la_logits_adjust(const void *logits, int dtype, int64_t row_stride, int B, int V, const la_adjust *how, void *out, int64_t out_stride, void *stream);
