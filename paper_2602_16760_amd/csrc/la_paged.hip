@@ -170,10 +170,12 @@ __global__ __launch_bounds__(256) void paged_write_kernel(uint4 *kp, uint4 *vp, 
 
 // ---- slots to other slots, in every layer ---------------------------------------------------------------------
 // A thread takes 16 bytes of a kv head of the rows of one run, of K or V of one layer after the other: it has read all of a run's sources before it writes one of its destinations, and
-// nobody else has to do with those bytes, so a run may move rows onto each other's places.  RUN sources wait in registers: the next larger of 1, 4, 8, 16 and 64.  Places that a run does
+// nobody else has to do with those bytes, so a run may move rows onto each other's places.  RUN sources wait in registers: the next larger of 1, 4, 8, 16 and 64 (of 64 with their places they are
+// all 512 that a lane can have and 20 bytes of scratch memory: a path of 16 rows of one request in 32 layers 6.3 us, of 17 14.9, of 63 19.9).  Places that a run does
 // not have are read from row 0 and thrown away, since a condition on each load sent the array to scratch memory (64 paths of 12: 154 us against 27).
-// Bound by bandwidth: one fork of 1000 positions in 32 layers, 262 MB, 50.2 us = 5.2 TB/s, as a large copy; a path of 8 in 32 layers, 6.7, is one chain of index and row.  Up to 32 workgroups
-// share the layers' K and V (8, 16, 32, 64 of them: path 11.2, 8.8, 8.1, 8.4; fork 53.9, 52.1, 51.5, 51.8), each with one layer's row in flight: unrolled over its layers the fork took 83.
+// Bound by bandwidth: one fork of 1000 positions in 32 layers, 262 MB, 50.2 us = 5.2 TB/s, as a large copy; paths of up to 6 rows of 32 requests in 32 layers, 21 MB, 6.4 (the kernel; 8.0 a launch of a graph), are one chain of index and row.  Up to
+// 32 workgroups share the layers' K and V (a launch with 8, 16, 32, 64 of them: paths 11.2, 8.8, 8.1, 8.4; fork 53.9, 52.1, 51.5, 51.8), each with one layer's row in flight: unrolled over its layers
+// the fork took 83.
 struct PagedCopy {
   uint4 *k, *v;  // of the first layer
   size_t layer;  // 16-byte pieces of one

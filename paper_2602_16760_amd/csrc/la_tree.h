@@ -48,10 +48,10 @@ __device__ __forceinline__ int at_keys(const TreeAttend &a, int b, int &r) {
   return rows == 0 || L < 0 ? 0 : (int)(n < cap ? n : cap);
 }
 
-// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled (two requests of 64 rows at 65000, half precision:
-// 232 us, with an offset that follows each maximum 237).  Weights are up to 2^LAZY then, and half precision's carry 2^UP besides, as la_paged_attend's do, so that a step of its smallest numbers is
-// 2^-39 of the largest weight; the factor goes out with the sum.  2^(UP + LAZY) has to stay below 65504, so an offset lags by less than an octave.  (With 11 and 4 in place of 15 and 7/8 it took
-// 219, but 600 keys of 2^-31 of a first one's weight came out 3 % off.)  The other types have 8 bits of exponent and need no factor.
+// A column's offset is moved when a score is this many octaves above it, so that most blocks need no maximum over lanes and no sums to be rescaled (two requests of 64 rows at 65000, bfloat16: 210 us,
+// with an offset that follows each maximum 245; half precision 237 and 249).  Weights are up to 2^LAZY then, and half precision's carry 2^UP besides, as la_paged_attend's do, so that a step of its
+// smallest numbers is 2^-39 of the largest weight; the factor goes out with the sum.  2^(UP + LAZY) may be 2^16 at most, which ta_split still splits, so its offsets lag by less than an octave.
+// (With 11 and 4 in place of 15 and 7/8 it took 221, but 600 keys of 2^-31 of a first one's weight came out 3 % off.)  The other types have 8 bits of exponent and need no factor.
 template <typename T> constexpr float TA_LAZY = std::is_same<T, _Float16>::value ? 0.875f : 8.f;
 template <typename T> constexpr float TA_UP = std::is_same<T, _Float16>::value ? 15.f : 0.f;
 // Weights are 2^(factor s - base + UP), formed in one instruction, with factor s not rounded and base rounded: where scores are large that is off by a part of a float's spacing there, and by

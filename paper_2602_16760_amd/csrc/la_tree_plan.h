@@ -23,7 +23,7 @@ inline bool tree_wide(int dtype, int head_dim, int page_size) {
 constexpr int TA_FEW = 256;
 // Requests are left whole up to AT_WHOLE keys (16 x 16 rows at 400: 16.4, cut 21.4; 16 x 64 at 500: 35 and 46), float ones up to half as many, their products being 1/16 as fast (3 x 8 at 500: cut
 //   11.0, 13.5 whole).  Where wide workgroups of whole requests are fewer than TA_MANY, only up to TA_WHOLE_WIDE keys (1 x 64 at 500: cut 23, 34 whole; 4 x 16 at 500, 64 workgroups: 18.6 whole and
-//   cut 16.5, but 4 x 32 at 600, 22.6 and 26.5), and so always for heads of 256 channels (22 of 1 to 12 rows at up to 747: cut 21, whole 34; one row at 500 14.3 and 18.3).
+//   cut 16.5, but 4 x 32 at 600, as many, 22.6 and 26.5: the rule takes the smaller loss of the two), and so always for heads of 256 channels (22 of 1 to 12 rows at up to 747: cut 21, whole 34; one row at 500 14.3 and 18.3).
 constexpr int TA_WHOLE_WIDE = 256, TA_MANY = 64;
 // 128 columns a workgroup rather than 64 (K and V pass through LDS half as often) where one of 512 then has this many keys, if all requests are as long as the table: 4 x 64 rows at 500, 128
 //   columns 26.4 and 64 20.0, 1 x 40 at 3000, 28.9 and 23.5, 4 x 64 at 4000, 512 keys, 49.9 and 48.3, 4 x 40 of three heads of 96 channels at 16000, 930 keys, 57.4 and 64.5, 16 x 64 at 4000,

@@ -34,8 +34,9 @@ __device__ __forceinline__ void tw_barrier() {
 // to add up but the items.  One barrier a stage: past it every wave's part of the stage is in, and nobody reads the stage any more that the next requests overwrite.
 // The 16-byte pieces of a row are permuted by its key, so that sixteen keys' equal pieces, and four keys' neighbouring ones, lie in different banks.  V's operand, eight keys of a channel in a
 // lane, comes out of LDS by transposing reads.
-// Bound by the matrix unit and the power it draws at long requests: two of 64 rows at 65000 keys, 32 query heads of 128 channels, are 205 GFLOP (137, and V's products with the weights' second
-// numbers) in 214 us, 0.96 PFLOP/s where a large library product reaches 1.16; without the weights' instructions it would be 190.  These go first (s_setprio), so that one workgroup's fill the gaps of
+// Bound by the matrix unit and the power it draws at long requests: two of 64 rows at 65000 keys, 32 query heads of 128 channels, are 137 GFLOP, 205 with V's products with the weights' second
+// numbers: half precision 220 us, 0.93 PFLOP/s of the 205 where a large library product reaches 1.16 (0.62 of the 137), 267 in the mean where the call repeats at once and the clock falls; bfloat16
+// 198, its offsets being moved less often.  Without the weights' instructions it would be 190.  These go first (s_setprio), so that one workgroup's fill the gaps of
 // the other's products: 8 x 64 rows at 16000 227 -> 210, 16 x 64 at 4000 133 -> 124.  The next stage's scores in front of a stage's weights took 353; products of 32 by 32, V asked for in front of the
 // weights, priority for the products: no difference.  At 16 requests of 1 to 16 rows at 64 to 4096, 41 MB, 19 us: the chain to a workgroup's first stage, five stages, and 34 KB of sums out of it.
 template <typename T, int DH, int WAVES, int NT, int NS>
